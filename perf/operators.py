@@ -264,17 +264,24 @@ def run(s):
     if not own:
         return {"tables": _plain_tables, "append": _plain_append, "attention": _plain_attention}[s["op"]](s)
     import paper_2512_23367_b200 as pq
+    # Objects and buffers that a user's program keeps from step to step: the cache with its geometry, the step's
+    # outputs, the workspace.
     if s["op"] == "tables":
-        step = pq.pq_block_tables(s["kv_len"], s["new_len"], s["table"], s["free_list"], s["free_head"], s["page"], s["tokens"])
-        return (s["table"], *step)
-    cache = pq.PagedKV(s["k"], s["v"], s["k_scale"], s["v_scale"])
+        if "step" not in s:
+            s["step"] = pq.PagedStep.empty(s["kv_len"].shape[0], s["tokens"], DEV)
+        step = pq.pq_block_tables(s["kv_len"], s["new_len"], s["table"], s["free_list"], s["free_head"], s["page"], step=s["step"])
+        return (s["table"], step.q_start, step.kv_len, step.slots, step.pos, step.free_head)
+    if "cache" not in s:
+        s["cache"] = pq.PagedKV(s["k"], s["v"], s["k_scale"], s["v_scale"])
+    cache = s["cache"]
     if s["op"] == "append":
         pq.pq_kv_append(cache, s["new_k"], s["new_v"], s["slots"])
         return (s["k"], s["v"]) if s["k_scale"] is None else pq.pq_kv_read(cache, s["slots"])
-    if "workspace" not in s:  # kept by a user's program from step to step
+    if "out" not in s:
+        s["out"] = torch.empty_like(s["q"])
         s["workspace"] = pq.pq_attention_workspace(s["q"], cache, s["table"].shape[0], s["max_q"], s["max_kv"])
     return pq.pq_paged_attention(s["q"], cache, s["table"], s["q_start"], s["kv_len"], s["max_q"], s["max_kv"],
-                                 window=s["window"], workspace=s["workspace"])
+                                 window=s["window"], out=s["out"], workspace=s["workspace"])
 
 
 def exact(case, seed):
