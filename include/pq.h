@@ -354,6 +354,104 @@ PQ_API int pq_plan_w8a8(int64_t M, int64_t N, int64_t K, int32_t sms, size_t scr
 PQ_API int pq_gemm_w8a8_noalloc(const int8_t* q, const float* s_tok, const void* wq, const float* s_ch,
                                 int64_t M, int64_t N, int64_t K, void* y_f16, void* stream);
 
+/* ------------------------------------------------------------------------------------------------
+ * Paged key/value cache and attention over it: what stands between the q/k/v linears of a decoder layer
+ * and its output linear when many requests are served at once.  (The paper quantizes the linears and
+ * times whole prefill and decode passes; it describes no cache.)
+ *
+ * A cache holds `pages` pages of `page` tokens for `heads` key/value heads of `dim` values:
+ *   k, v              [pages, heads, page, dim]  FP16 (PQ_KV_F16) or INT8 codes (PQ_KV_INT8)
+ *   k_scale, v_scale  [pages, heads, page]       FP32, PQ_KV_INT8 only (NULL otherwise): the scale of one
+ *                                                token's vector of one head, value = code * scale
+ * A SLOT is page_id * page + offset.  Rules (else PQ_ERR_SHAPE): page a multiple of 16, at most 1024;
+ * dim 64 or 128; 1 <= heads <= 1024; pages >= 1 and pages * heads * page < 2^31; type one of the two.
+ */
+#define PQ_KV_F16 0
+#define PQ_KV_INT8 1
+typedef struct {
+  void* k;
+  void* v;
+  float* k_scale;
+  float* v_scale;
+  int64_t pages;
+  int32_t heads;
+  int32_t page;
+  int32_t dim;
+  int32_t type;
+} pq_kv_cache;
+
+/*
+ * Block tables, slot map and positions of one step, built on the GPU from the requests' lengths.
+ * Request b has kv_len[b] cached tokens and brings new_len[b] (either may be 0; a negative length counts
+ * as 0).  With have = ceil(kv_len / page) and want = ceil((kv_len + new_len) / page), the want - have
+ * pages it needs are taken from free_list in request order, beginning at *free_head:
+ *   block_table [requests, width]  columns have .. want - 1 of every row are written, the others are left
+ *   q_start [requests + 1]         exclusive prefix sums of new_len (row ranges of the step's tokens)
+ *   kv_total [requests]            kv_len + new_len
+ *   slots [tokens]                 where each new token's key and value go; -1 for rows beyond
+ *                                  q_start[requests] and for tokens without a page
+ *   pos [tokens]                   the token's position in its request; -1 beyond q_start[requests]
+ *   free_next [1]                  *free_head + the pages needed (above free_count: the list was too short)
+ * A token has no page when the free list is used up (its table entry becomes -1), when its column is
+ * beyond `width`, or when the table's own entry is negative.  The caller gives `tokens` >= the sum of
+ * new_len: tokens beyond are not mapped and pages that only they would begin are not entered.
+ *   kv_len, new_len i32 [requests], free_list i32 [free_count], free_head i32 [1]: in.  free_next must not
+ *   overlap free_head, nor kv_total kv_len (PQ_ERR_SHAPE when they are the same address).
+ *   0 <= requests <= PQ_MAX_REQUESTS (PQ_ERR_LIMIT beyond), 0 <= tokens < 2^31, width >= 1, free_count >= 0.
+ *   Index arrays need the alignment of their type only.
+ */
+#define PQ_MAX_REQUESTS 4096
+PQ_API int pq_block_tables(const int32_t* kv_len, const int32_t* new_len, int64_t requests, int32_t* block_table,
+                           int64_t width, const int32_t* free_list, int64_t free_count, const int32_t* free_head,
+                           int32_t page, int64_t tokens, int32_t* q_start, int32_t* kv_total, int64_t* slots,
+                           int32_t* pos, int32_t* free_next, void* stream);
+
+/*
+ * Writes the keys and values of `tokens` new tokens into the cache, token t at slots[t] (rows whose slot is
+ * negative or beyond the cache are skipped; two rows with one slot leave either).  PQ_KV_INT8: every
+ * (token, head) vector is quantized by the rule of pq_quantize_act (one scale over its `dim` values).
+ *   k, v: FP16, row t at k + t * stride elements, heads * dim values each (stride >= heads * dim, a
+ *   multiple of 8, so that slices of one wide q/k/v output serve as they are); 16-byte aligned.
+ */
+PQ_API int pq_kv_append(const pq_kv_cache* cache, const void* k_f16, int64_t k_stride, const void* v_f16,
+                        int64_t v_stride, const int64_t* slots, int64_t tokens, void* stream);
+
+/* The reverse: the values at `slots` as FP16 [tokens, heads, dim], dense (PQ_KV_INT8: code * scale in FP32,
+ * rounded once; zeros where the slot is negative or beyond the cache).  For interchange and checking. */
+PQ_API int pq_kv_read(const pq_kv_cache* cache, const int64_t* slots, int64_t tokens, void* k_f16, void* v_f16,
+                      void* stream);
+
+/*
+ * Attention of the step's tokens over the paged cache, which already holds their own keys and values.
+ * Row t of request b, q_start[b] <= t < q_start[b + 1], with n = q_start[b + 1] - q_start[b] rows and
+ * L = kv_len[b] cached tokens, stands at position p = L - n + (t - q_start[b]) and sees the keys
+ *   j <= p, j >= 0, and j > p - window when window > 0:
+ *   s_j = scale * sum_d q[d] k_j[d],  y = sum_j e^(s_j - max) v_j / sum_j e^(s_j - max)
+ * for query head h over the key/value head h / (heads / cache->heads).  Scores, maxima and sums are FP32;
+ * the weights are rounded to FP16 for their product with the values (they lie in [0, 256]), and the
+ * product is summed in FP32.  A row that sees no key (kv_len shorter than the chunk, window or not) gives 0.
+ *   q: FP16, row t at q + t * q_stride elements (a multiple of 8, >= heads * dim), heads * dim values
+ *   block_table i32 [requests, width]; q_start i32 [requests + 1]; kv_len i32 [requests], tokens in the
+ *     cache with the chunk's own (kv_total of pq_block_tables).  A page id outside the cache reads as
+ *     zeros; keys beyond width * page are not seen.
+ *   max_q, max_kv: bounds of the rows and the cached tokens of any request of this step, for the choice
+ *     of the schedule.  A request with more rows than max_q leaves outputs unspecified; max_kv
+ *     only steers how the keys are split.
+ *   out: FP16 [tokens, heads, dim] dense.  Rows outside every request are left as they are.
+ *   heads a multiple of cache->heads, heads / cache->heads <= 64; scale finite; window >= 0.
+ *   workspace: as for pq_gemm_w8a8 (optional, prepared once with pq_workspace_init, one per stream of calls
+ *     that may overlap): partial results of keys that are split over several SMs, summed in a fixed order.
+ *     Without it, or with too little, the keys of a request are not split.
+ * pq_attention_workspace_bytes: host-only; 0 when nothing is split or an argument is invalid.
+ */
+PQ_API int pq_paged_attention(const void* q_f16, int64_t q_stride, int32_t heads, const pq_kv_cache* cache,
+                              const int32_t* block_table, int64_t width, const int32_t* q_start,
+                              const int32_t* kv_len, int64_t requests, int64_t tokens, int64_t max_q,
+                              int64_t max_kv, float scale, int32_t window, void* out_f16, void* workspace,
+                              size_t workspace_bytes, void* stream);
+PQ_API size_t pq_attention_workspace_bytes(int64_t requests, int64_t tokens, int64_t max_q, int64_t max_kv,
+                                           int32_t heads, int32_t kv_heads, int32_t dim, int32_t sms);
+
 /*
  * Reads the device status word of the current device into *host_status (PQ_OK or
  * PQ_ERR_TIMEOUT) and clears it.  Synchronizes the device; call it outside timed

@@ -8,10 +8,15 @@ raises if it cannot be loaded -- there is no CPU or library fallback.
 """
 from . import synth  # noqa: F401
 from .binding import (  # noqa: F401
+    PagedKV,
+    PagedStep,
     PQError,
     lib,
     pq_acc_w4a8,
     pq_acc_w8a8,
+    pq_attention_workspace,
+    pq_attention_workspace_bytes,
+    pq_block_tables,
     pq_col_absmax,
     pq_device_status,
     pq_gemm_w4a8,
@@ -20,12 +25,15 @@ from .binding import (  # noqa: F401
     pq_gemm_w8a8_group,
     pq_gemm_w8a8_noalloc,
     pq_hadamard_block,
+    pq_kv_append,
+    pq_kv_read,
     pq_pack_w4,
     pq_pack_w4_hadamard,
     pq_linear_w4a8,
     pq_linear_w8a8,
     pq_pack_w8,
     pq_pack_w8_hadamard,
+    pq_paged_attention,
     pq_plan_w8a8,
     pq_quantize_act,
     pq_quantize_act_hadamard,

@@ -5,6 +5,7 @@ from __future__ import annotations
 
 import ctypes
 import os
+from typing import NamedTuple
 
 import torch
 
@@ -57,8 +58,15 @@ SIGNATURES = {
     "pq_pack_w4_smooth": (ctypes.c_int, [_vp, _vp, _i64, _i64, _i32, _vp, _vp, _vp]),
     "pq_gemm_w4a8_group": (ctypes.c_int, [_vp, _vp, _i32, ctypes.POINTER(_vp), ctypes.POINTER(_vp), _i32,
                                           ctypes.POINTER(_i64), ctypes.POINTER(_vp), _i64, _i64, _vp]),
+    "pq_block_tables": (ctypes.c_int, [_vp, _vp, _i64, _vp, _i64, _vp, _i64, _vp, _i32, _i64, _vp, _vp, _vp, _vp, _vp, _vp]),
+    "pq_kv_append": (ctypes.c_int, [_vp, _vp, _i64, _vp, _i64, _vp, _i64, _vp]),
+    "pq_kv_read": (ctypes.c_int, [_vp, _vp, _i64, _vp, _vp, _vp]),
+    "pq_paged_attention": (ctypes.c_int, [_vp, _i64, _i32, _vp, _vp, _i64, _vp, _vp, _i64, _i64, _i64, _i64,
+                                          ctypes.c_float, _i32, _vp, _vp, ctypes.c_size_t, _vp]),
+    "pq_attention_workspace_bytes": (ctypes.c_size_t, [_i64, _i64, _i64, _i64, _i32, _i32, _i32, _i32]),
 }
 MAX_GROUP = 4
+MAX_REQUESTS = 4096
 
 
 class PQError(RuntimeError):
@@ -507,6 +515,201 @@ def pq_acc_w4a8(q, wp, N: int, group: int = GROUP) -> torch.Tensor:
     acc = torch.empty((K // group, M, N), dtype=torch.int32, device=q.device)
     _check("pq_acc_w4a8", lib().pq_acc_w4a8(q.data_ptr(), wp.data_ptr(), group, M, N, K, acc.data_ptr(), _stream()))
     return acc
+
+
+# ---- paged key/value cache and attention over it ---------------------------------------------------------
+
+class _KVCache(ctypes.Structure):   # pq_kv_cache of include/pq.h
+    _fields_ = [("k", _vp), ("v", _vp), ("k_scale", _vp), ("v_scale", _vp), ("pages", _i64), ("heads", _i32),
+                ("page", _i32), ("dim", _i32), ("type", _i32)]
+
+
+class PagedKV:
+    """A paged key/value cache: k, v f16 or int8 [pages, heads, page, dim], for int8 with k_scale, v_scale
+    f32 [pages, heads, page].  Measures its tensors once and keeps them; page a multiple of 16, dim 64 or 128."""
+
+    __slots__ = ("k", "v", "k_scale", "v_scale", "pages", "heads", "page", "dim", "device", "_struct", "_ref")
+
+    def __init__(self, k: torch.Tensor, v: torch.Tensor, k_scale: torch.Tensor | None = None,
+                 v_scale: torch.Tensor | None = None):
+        if k.dim() != 4:
+            raise ValueError("k: expected a 4-D tensor [pages, heads, page, dim]")
+        pages, heads, page, dim = k.shape
+        if k.dtype not in (torch.float16, torch.int8):
+            raise TypeError(f"k: expected torch.float16 or torch.int8, got {k.dtype}")
+        int8 = k.dtype == torch.int8
+        _sized(k, k.dtype, k.numel(), "k"), _sized(v, k.dtype, k.numel(), "v")
+        if v.shape != k.shape:
+            raise ValueError(f"v: expected the shape of k {tuple(k.shape)}, got {tuple(v.shape)}")
+        for s, name in ((k_scale, "k_scale"), (v_scale, "v_scale")):
+            if int8 != (s is not None):
+                raise ValueError(f"{name}: {'required for an int8 cache' if int8 else 'an f16 cache has none'}")
+            if s is not None:
+                _sized(s, torch.float32, pages * heads * page, name)
+        _together(k, v, k_scale, v_scale)
+        put = object.__setattr__
+        put(self, "k", k), put(self, "v", v), put(self, "k_scale", k_scale), put(self, "v_scale", v_scale)
+        put(self, "pages", pages), put(self, "heads", heads), put(self, "page", page), put(self, "dim", dim)
+        put(self, "device", k.device)
+        put(self, "_struct", _KVCache(k.data_ptr(), v.data_ptr(), k_scale.data_ptr() if int8 else None,
+                                      v_scale.data_ptr() if int8 else None, pages, heads, page, dim, int(int8)))
+        put(self, "_ref", ctypes.addressof(self._struct))
+
+    def __setattr__(self, name, value):
+        raise AttributeError("a PagedKV is fixed; make another one over other tensors")
+
+    @classmethod
+    def empty(cls, pages: int, heads: int, page: int, dim: int, dtype: torch.dtype = torch.float16, device="cuda"):
+        """A zero-filled cache."""
+        k, v = (torch.zeros((pages, heads, page, dim), dtype=dtype, device=device) for _ in range(2))
+        if dtype != torch.int8:
+            return cls(k, v)
+        return cls(k, v, *(torch.zeros((pages, heads, page), dtype=torch.float32, device=device) for _ in range(2)))
+
+
+class PagedStep(NamedTuple):
+    """What pq_block_tables gives for one step: row ranges, cached tokens with the new ones, slots and positions of
+    the new tokens, and the head of the free list after the step."""
+    q_start: torch.Tensor    # i32 [requests + 1]
+    kv_len: torch.Tensor     # i32 [requests]
+    slots: torch.Tensor      # i64 [tokens]
+    pos: torch.Tensor        # i32 [tokens]
+    free_head: torch.Tensor  # i32 [1]
+
+    @classmethod
+    def empty(cls, requests: int, tokens: int, device="cuda"):
+        """Buffers for a step of up to `tokens` new tokens."""
+        i32 = lambda n: torch.empty((n,), dtype=torch.int32, device=device)  # noqa: E731
+        return cls(i32(requests + 1), i32(requests), torch.empty((tokens,), dtype=torch.int64, device=device),
+                   i32(tokens), i32(1))
+
+
+def _here(t: torch.Tensor) -> None:
+    """The call launches on the current device's current stream: its operands have to live there."""
+    if t.device.index != torch.cuda.current_device():
+        raise ValueError(f"operands on {t.device}, but the current device is cuda:{torch.cuda.current_device()}")
+
+
+def pq_block_tables(kv_len, new_len, block_table, free_list, free_head, page: int, tokens: int | None = None,
+                    step: PagedStep | None = None) -> PagedStep:
+    """Block tables, slot map and positions of one step.  kv_len, new_len i32 [requests]; block_table
+    i32 [requests, width], updated in place; free_list i32 [F] page ids, taken from free_head i32 [1] on.
+    tokens: rows of the step, at least the sum of new_len; or step: buffers from PagedStep.empty, filled and
+    returned."""
+    B = kv_len.numel()
+    if block_table.dim() != 2:
+        raise ValueError("block_table: expected a 2-D tensor [requests, width]")
+    width = block_table.shape[1]
+    _sized(kv_len, torch.int32, B, "kv_len"), _sized(new_len, torch.int32, B, "new_len")
+    _sized(block_table, torch.int32, B * width, "block_table")
+    _sized(free_list, torch.int32, free_list.numel(), "free_list"), _sized(free_head, torch.int32, 1, "free_head")
+    if step is None:
+        if tokens is None:
+            raise ValueError("tokens: required without step")
+        if tokens < 0:
+            raise ValueError("tokens: expected a size")
+        _together(kv_len, new_len, block_table, free_list, free_head)
+        step = PagedStep.empty(B, tokens, kv_len.device)
+    else:
+        if tokens is not None and tokens != step.slots.numel():
+            raise ValueError("tokens: differs from the step's buffers")
+        tokens = step.slots.numel()
+        _sized(step.q_start, torch.int32, B + 1, "step.q_start"), _sized(step.kv_len, torch.int32, B, "step.kv_len")
+        _sized(step.slots, torch.int64, tokens, "step.slots"), _sized(step.pos, torch.int32, tokens, "step.pos")
+        _sized(step.free_head, torch.int32, 1, "step.free_head")
+        _together(kv_len, new_len, block_table, free_list, free_head, *step)
+    _here(kv_len)
+    _check("pq_block_tables", lib().pq_block_tables(
+        kv_len.data_ptr(), new_len.data_ptr(), B, block_table.data_ptr(), width, free_list.data_ptr(),
+        free_list.numel(), free_head.data_ptr(), page, tokens, step.q_start.data_ptr(), step.kv_len.data_ptr(),
+        step.slots.data_ptr(), step.pos.data_ptr(), step.free_head.data_ptr(), _stream()))
+    return step
+
+
+def _token_rows(x: torch.Tensor, heads: int | None, dim: int, what: str) -> tuple[int, int, int]:
+    """Rows of f16 head vectors, [T, heads, dim] or [T, heads * dim], dense inside a row; the rows may be slices of
+    a wider matrix.  Returns (T, heads, row stride in elements)."""
+    if x.dtype != torch.float16:
+        raise TypeError(f"{what}: expected torch.float16, got {x.dtype}")
+    shape, stride = x.shape, x.stride()
+    if len(shape) == 3:
+        T, H, D = shape
+        dense = D == dim and stride[2] == 1 and (H == 1 or stride[1] == dim)
+    elif len(shape) == 2:
+        T, H, dense = shape[0], shape[1] // dim, shape[1] % dim == 0 and stride[1] == 1
+    else:
+        dense = False
+    if not dense or (heads is not None and H != heads):
+        raise ValueError(f"{what}: expected rows of {'heads' if heads is None else heads} x {dim} contiguous values")
+    return T, H, (stride[0] if T > 1 else H * dim)
+
+
+def pq_kv_append(cache: PagedKV, k: torch.Tensor, v: torch.Tensor, slots: torch.Tensor) -> None:
+    """Writes k, v f16 [T, heads, dim] (or [T, heads * dim]; rows may be slices of a wider matrix) into the cache
+    at slots i64 [T]; rows with a negative slot are skipped.  An int8 cache quantizes every head's vector."""
+    T, _, ks = _token_rows(k, cache.heads, cache.dim, "k")
+    Tv, _, vs = _token_rows(v, cache.heads, cache.dim, "v")
+    if Tv != T:
+        raise ValueError(f"v: expected {T} rows, got {Tv}")
+    _sized(slots, torch.int64, T, "slots")
+    _together(cache.k, k, v, slots)
+    _here(k)
+    _check("pq_kv_append", lib().pq_kv_append(cache._ref, k.data_ptr(), ks, v.data_ptr(), vs, slots.data_ptr(), T,
+                                              _stream()))
+
+
+def pq_kv_read(cache: PagedKV, slots: torch.Tensor) -> tuple[torch.Tensor, torch.Tensor]:
+    """Keys and values at slots i64 [T] as f16 [T, heads, dim]; zeros where a slot is outside the cache."""
+    T = slots.numel()
+    _sized(slots, torch.int64, T, "slots")
+    _together(cache.k, slots)
+    _here(slots)
+    k, v = (torch.empty((T, cache.heads, cache.dim), dtype=torch.float16, device=slots.device) for _ in range(2))
+    _check("pq_kv_read", lib().pq_kv_read(cache._ref, slots.data_ptr(), T, k.data_ptr(), v.data_ptr(), _stream()))
+    return k, v
+
+
+def pq_attention_workspace_bytes(requests: int, tokens: int, max_q: int, max_kv: int, heads: int, kv_heads: int,
+                                 dim: int, sms: int = 148) -> int:
+    """Bytes of workspace with which pq_paged_attention splits the keys as it would with unlimited room; 0 if it
+    does not split them.  Host-only, needs no GPU."""
+    return int(lib().pq_attention_workspace_bytes(requests, tokens, max_q, max_kv, heads, kv_heads, dim, sms))
+
+
+def pq_attention_workspace(q: torch.Tensor, cache: PagedKV, requests: int, max_q: int, max_kv: int) -> torch.Tensor | None:
+    """A prepared workspace for pq_paged_attention over these sizes (None where the call has no use for one)."""
+    T, H, _ = _token_rows(q, None, cache.dim, "q")
+    sms = torch.cuda.get_device_properties(q.device).multi_processor_count
+    n = pq_attention_workspace_bytes(requests, T, max_q, max_kv, H, cache.heads, cache.dim, sms)
+    return pq_workspace_init(torch.empty((n,), dtype=torch.uint8, device=q.device)) if n else None
+
+
+def pq_paged_attention(q: torch.Tensor, cache: PagedKV, block_table: torch.Tensor, q_start: torch.Tensor,
+                       kv_len: torch.Tensor, max_q: int, max_kv: int, scale: float | None = None, window: int = 0,
+                       out: torch.Tensor | None = None, workspace: torch.Tensor | None = None) -> torch.Tensor:
+    """Attention of a step's tokens over the paged cache that already holds their keys and values.  q f16
+    [T, heads, dim] or [T, heads * dim] (rows may be slices of a wider matrix) -> out f16 of the same shape.
+    block_table i32 [requests, width], q_start i32 [requests + 1], kv_len i32 [requests] (with the step's own
+    tokens); max_q, max_kv: bounds over the requests; scale: 1 / sqrt(dim) by default; window: keys that a row
+    sees at most (0: all); workspace: from pq_attention_workspace (without it the keys are not split)."""
+    T, H, qs = _token_rows(q, None, cache.dim, "q")
+    B = kv_len.numel()
+    if block_table.dim() != 2:
+        raise ValueError("block_table: expected a 2-D tensor [requests, width]")
+    width = block_table.shape[1]
+    _sized(block_table, torch.int32, B * width, "block_table")
+    _sized(q_start, torch.int32, B + 1, "q_start"), _sized(kv_len, torch.int32, B, "kv_len")
+    if out is None:
+        out = torch.empty(q.shape, dtype=torch.float16, device=q.device)
+    else:
+        _sized(out, torch.float16, T * H * cache.dim, "out")
+    ws, ws_bytes = _ws(workspace)
+    _together(q, cache.k, block_table, q_start, kv_len, out, workspace)
+    _here(q)
+    _check("pq_paged_attention", lib().pq_paged_attention(
+        q.data_ptr(), qs, H, cache._ref, block_table.data_ptr(), width, q_start.data_ptr(), kv_len.data_ptr(), B, T,
+        max_q, max_kv, cache.dim ** -0.5 if scale is None else scale, window, out.data_ptr(), ws, ws_bytes, _stream()))
+    return out
 
 
 def pq_device_status() -> int:

@@ -59,17 +59,6 @@ DeviceInfo* current_device() {
   return &d;
 }
 
-int check_arch() {
-  DeviceInfo* d = current_device();
-  if (d == nullptr) {
-    cudaGetLastError();
-    return PQ_ERR_CUDA;
-  }
-  return d->ok ? PQ_OK : PQ_ERR_ARCH;
-}
-
-bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
-
 int check_rows(int64_t rows, int64_t K) {
   if (rows < 1 || rows > 0x7fffffff) return PQ_ERR_SHAPE;
   if (K < 16 || K % 16 != 0 || K >= 131072) return PQ_ERR_SHAPE;
@@ -104,6 +93,15 @@ EncodeTiledFn encode_fn() {
 }
 
 }  // namespace
+
+int check_arch() {
+  DeviceInfo* d = current_device();
+  if (d == nullptr) {
+    cudaGetLastError();
+    return PQ_ERR_CUDA;
+  }
+  return d->ok ? PQ_OK : PQ_ERR_ARCH;
+}
 
 int* device_status_ptr() {
   DeviceInfo* d = current_device();
@@ -371,8 +369,6 @@ int pq_unpack_w4(const void* wp, int64_t N, int64_t K, int8_t* codes, void* stre
   if ((rc = check_arch()) != PQ_OK) return rc;
   return launch_unpack_w4(wp, N, K, codes, static_cast<cudaStream_t>(stream));
 }
-
-static bool aligned256(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 255u) == 0; }
 
 // 129..256 tokens: a narrow linear gives the pair kernel few 256 x 256 tiles (256 x 4096 -> 4096: 16 on 74 SM
 // pairs); the weight-streaming kernel takes it in two token blocks and splits K over clusters instead.

@@ -74,6 +74,13 @@ bool pdl_enabled();
 int make_tmap_2d(CUtensorMap* out, const void* base, uint64_t rows, uint64_t cols, uint32_t box_rows,
                  uint32_t box_cols, uint32_t elem_bytes, int swizzle_bytes);
 
+// PQ_OK if the current device is compute capability 10.0, else PQ_ERR_ARCH / PQ_ERR_CUDA.
+int check_arch();
+inline bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
+inline bool aligned256(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 255u) == 0; }
+// The rules of pq.h for a paged cache's geometry and pointers.
+int check_kv_cache(const pq_kv_cache* c);
+
 // ---- launchers (each returns a pq_status; all are asynchronous on `stream`) ----
 // col (nullable, [K] FP32): per-column factor applied before the maximum is taken (Eq. 3).
 int launch_quantize_act(const void* x, int64_t M, int64_t K, int8_t* q, float* s, bool divide_by_scale,
@@ -157,6 +164,23 @@ inline int cuda_status(cudaError_t e) {
   if (e == cudaSuccess) return PQ_OK;
   note_cuda_error(e);
   return PQ_ERR_CUDA;
+}
+
+// Launches a kernel with programmatic stream serialization (unless PQ_PDL=0): it may begin while the kernel
+// before it in the stream drains, and calls grid_dep_wait() before it touches what that kernel may touch.
+template <typename... Params, typename... Args>
+int launch_dependent(void (*kern)(Params...), dim3 grid, dim3 block, size_t smem, cudaStream_t stream, Args... args) {
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = grid;
+  cfg.blockDim = block;
+  cfg.dynamicSmemBytes = smem;
+  cfg.stream = stream;
+  cudaLaunchAttribute attr[1];
+  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[0].val.programmaticStreamSerializationAllowed = 1;
+  cfg.attrs = attr;
+  cfg.numAttrs = pdl_enabled() ? 1 : 0;
+  return cuda_status(cudaLaunchKernelEx(&cfg, kern, args...));
 }
 
 }  // namespace pq

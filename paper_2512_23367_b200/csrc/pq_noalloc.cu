@@ -74,7 +74,6 @@ int static_scratch(Scratch* out) {
   return PQ_OK;
 }
 
-bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
 
 }  // namespace
 
