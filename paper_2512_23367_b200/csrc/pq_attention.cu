@@ -3,26 +3,12 @@
 
 #include <cmath>
 
-#include "pq_internal.h"
+#include "pq_attention.h"
 #include "pq_ptx.cuh"
 
 namespace pq {
 
 namespace {
-
-struct AttnArgs {
-  const __half* q;
-  int64_t q_stride;
-  pq_kv_cache c;
-  const int* table;
-  int64_t width;
-  const int* q_start;
-  const int* kv_len;
-  __half* out;
-  int requests, heads, window;
-  int64_t tokens;
-  float scale_log2;   // scale * log2(e): scores in powers of two
-};
 
 // One warp per (row, head); a lane holds dim / 32 values of the query and of the sum; keys one after the other
 // with a running maximum and sum.
@@ -42,6 +28,7 @@ __global__ void __launch_bounds__(128) attention_kernel(const AttnArgs a) {
     if (a.q_start[mid] <= t) lo = mid; else hi = mid - 1;
   }
   const int q0 = a.q_start[lo], n = a.q_start[lo + 1] - q0, L = a.kv_len[lo];
+  if (static_cast<int64_t>(n) * (a.heads / a.c.heads) <= kAttnRows) return;   // the row kernel's
   const int64_t p = static_cast<int64_t>(L) - n + (t - q0);
   const int64_t end = min(p + 1, a.width * a.c.page);
   const int64_t begin = a.window > 0 ? max(static_cast<int64_t>(0), p + 1 - a.window) : 0;
@@ -110,9 +97,16 @@ int pq_paged_attention(const void* q_f16, int64_t q_stride, int32_t heads, const
   if (!q_f16 || !block_table || !q_start || !kv_len || !out_f16) return PQ_ERR_NULL;
   if (!aligned16(q_f16) || !aligned16(out_f16) || !aligned256(workspace)) return PQ_ERR_ALIGN;
   if ((rc = check_arch()) != PQ_OK) return rc;
-  const AttnArgs a{static_cast<const __half*>(q_f16), q_stride, *cache, block_table, width, q_start, kv_len,
-                   static_cast<__half*>(out_f16), static_cast<int>(requests), heads, window, tokens,
-                   scale * 1.44269504f};
+  AttnArgs a{static_cast<const __half*>(q_f16), q_stride, *cache, block_table, width, q_start, kv_len,
+             static_cast<__half*>(out_f16), tokens, static_cast<int>(requests), heads, window, scale * 1.44269504f,
+             0, nullptr, nullptr};
+  const Scratch sc = scratch_from(workspace, workspace_bytes);
+  const AttnPlan plan = plan_attn_rows(requests, max_kv, cache->heads, cache->dim, sm_count(), sc.partial_bytes);
+  a.part_keys = plan.part_keys;
+  a.counters = sc.counters;
+  a.partials = reinterpret_cast<float*>(sc.partials);
+  rc = launch_attn_rows(a, plan, static_cast<cudaStream_t>(stream));
+  if (rc != PQ_OK || max_q * (heads / cache->heads) <= kAttnRows) return rc;
   const int64_t blocks = (tokens * heads + 3) / 4;
   if (blocks > 0x7fffffff) return PQ_ERR_SHAPE;
   const dim3 grid(static_cast<unsigned>(blocks)), block(128);
@@ -127,8 +121,12 @@ int pq_paged_attention(const void* q_f16, int64_t q_stride, int32_t heads, const
 
 size_t pq_attention_workspace_bytes(int64_t requests, int64_t tokens, int64_t max_q, int64_t max_kv, int32_t heads,
                                     int32_t kv_heads, int32_t dim, int32_t sms) {
-  (void)requests, (void)tokens, (void)max_q, (void)max_kv, (void)heads, (void)kv_heads, (void)dim, (void)sms;
-  return 0;
+  if (requests < 1 || requests > PQ_MAX_REQUESTS || tokens < 1 || max_q < 1 || max_kv < 1 || kv_heads < 1 ||
+      heads < kv_heads || heads % kv_heads != 0 || (dim != 64 && dim != 128) || sms < 1) {
+    return 0;
+  }
+  const AttnPlan plan = plan_attn_rows(requests, max_kv, kv_heads, dim, sms, ~size_t(0));
+  return plan.parts > 1 ? kScratchHeaderBytes + plan.partial_bytes : 0;
 }
 
 }  // extern "C"

@@ -1,0 +1,65 @@
+// What the attention kernels share: arguments, the split of the keys over CTAs and the joining of the parts.
+#pragma once
+#include <cuda_fp16.h>
+
+#include <cstdint>
+
+#include "pq_internal.h"
+
+namespace pq {
+
+struct AttnArgs {
+  const __half* q;
+  int64_t q_stride;
+  pq_kv_cache c;
+  const int* table;
+  int64_t width;
+  const int* q_start;
+  const int* kv_len;
+  __half* out;
+  int64_t tokens;
+  int requests, heads, window;
+  float scale_log2;          // scale * log2(e): scores are powers of two
+  int part_keys;             // keys of one part, a multiple of 128
+  unsigned int* counters;    // arrivals per unit, zero between calls; nullptr: the keys are not split
+  float* partials;           // per unit and part: rows x dim sums, then rows x (maximum, sum)
+};
+
+// Rows of a (request, key/value head) that the row kernel takes: one m16 tile of the legacy matrix instruction.
+// Requests with more rows go to the tile kernel.
+constexpr int kAttnRows = 16;
+
+// Schedule of a call, from sizes that the host knows: how many parts a unit's keys may be cut into.
+struct AttnPlan {
+  int64_t units = 0;      // units of the row kernel: requests x key/value heads
+  int parts = 1;          // grid parts per unit
+  int part_keys = 128;
+  size_t partial_bytes = 0;
+};
+AttnPlan plan_attn_rows(int64_t requests, int64_t max_kv, int kv_heads, int dim, int sms, size_t room);
+
+int launch_attn_rows(const AttnArgs& a, const AttnPlan& plan, cudaStream_t stream);
+
+__device__ __forceinline__ float exp2_approx(float x) {
+  float y;
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
+}
+
+// Keys [lo, hi) that a request's rows may see: lo from the window of its first row, hi from its length and its table.
+struct AttnRange {
+  int n, L, lo, hi;
+};
+__device__ __forceinline__ AttnRange attn_range(const AttnArgs& a, int b) {
+  AttnRange r;
+  const int q0 = a.q_start[b];
+  r.n = a.q_start[b + 1] - q0;
+  r.L = a.kv_len[b];
+  const int64_t cap = a.width * a.c.page;
+  r.hi = static_cast<int>(min(static_cast<int64_t>(r.L), cap));
+  const int64_t lo = static_cast<int64_t>(r.L) - r.n + 1 - a.window;
+  r.lo = (a.window > 0 && lo > 0) ? static_cast<int>(lo) : 0;
+  return r;
+}
+
+}  // namespace pq

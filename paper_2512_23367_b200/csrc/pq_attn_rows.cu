@@ -1,0 +1,516 @@
+// Attention of up to 16 query rows per (request, key/value head) over the paged cache: decode steps and short drafts.
+#include <cstdlib>
+
+#include "pq_attention.h"
+#include "pq_ptx.cuh"
+
+namespace pq {
+
+namespace {
+
+constexpr int kWarps = 4;
+constexpr int kStages = 3;
+constexpr int kStageBytes = 8192;   // keys and values of one step of one warp
+
+// A warp's step: as many keys as fill a stage, in blocks of 16 (a block never leaves its page).
+template <bool kInt8, int D>
+struct RowCfg {
+  static constexpr int kRowBytes = kInt8 ? D : 2 * D;
+  static constexpr int kKeys = kStageBytes / (2 * kRowBytes);   // 16, 32 or 64
+  static constexpr int kBlocks = kKeys / 16;
+  static constexpr int kHalf = kKeys * kRowBytes;               // the keys' share of a stage; the values follow
+  static constexpr int kScaleBytes = kInt8 ? 2 * kKeys * 4 : 0;
+  static constexpr int kStage = kStageBytes + kScaleBytes;
+  static constexpr int kSmem = kWarps * kStages * kStage;
+  static constexpr int kChunksPerRow = kRowBytes / 16;
+};
+
+__device__ __forceinline__ void cp_async16(uint32_t dst, const void* src, bool live) {
+  const int n = live ? 16 : 0;   // 0: the 16 bytes are filled with zeros and nothing is read
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(n) : "memory");
+}
+__device__ __forceinline__ void cp_async4(uint32_t dst, const void* src, bool live) {
+  const int n = live ? 4 : 0;
+  asm volatile("cp.async.ca.shared.global [%0], [%1], 4, %2;" ::"r"(dst), "l"(src), "r"(n) : "memory");
+}
+__device__ __forceinline__ void cp_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+template <int N>
+__device__ __forceinline__ void cp_wait() {
+  asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory");
+}
+__device__ __forceinline__ void ldsm4(uint32_t addr, uint32_t (&r)[4]) {
+  asm volatile("ldmatrix.sync.aligned.m8n8.x4.shared.b16 {%0, %1, %2, %3}, [%4];"
+               : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(addr) : "memory");
+}
+__device__ __forceinline__ void ldsm4_t(uint32_t addr, uint32_t (&r)[4]) {
+  asm volatile("ldmatrix.sync.aligned.m8n8.x4.trans.shared.b16 {%0, %1, %2, %3}, [%4];"
+               : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(addr) : "memory");
+}
+__device__ __forceinline__ uint4 lds128(uint32_t addr) {
+  uint4 v;
+  asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(addr) : "memory");
+  return v;
+}
+__device__ __forceinline__ uint2 lds64(uint32_t addr) {
+  uint2 v;
+  asm volatile("ld.shared.v2.u32 {%0, %1}, [%2];" : "=r"(v.x), "=r"(v.y) : "r"(addr) : "memory");
+  return v;
+}
+__device__ __forceinline__ float2 lds_f2(uint32_t addr) {
+  float2 v;
+  asm volatile("ld.shared.v2.f32 {%0, %1}, [%2];" : "=f"(v.x), "=f"(v.y) : "r"(addr) : "memory");
+  return v;
+}
+// D += A (16 x 16) B (16 x 8), FP16 in, FP32 sums.
+__device__ __forceinline__ void mma16816(float (&d)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
+  asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
+               : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
+               : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+}
+// Four INT8 codes, offset by 128 (bytes u = code + 128), as FP16: 0x6400 | u is 1024 + u, and 1024 + u - 1152 is the
+// code, exactly.  sel picks the two bytes.
+__device__ __forceinline__ uint32_t codes_f16(uint32_t u, uint32_t sel) {
+  const uint32_t h = __byte_perm(u, 0x64646464u, sel);
+  const __half2 r = __hsub2(*reinterpret_cast<const __half2*>(&h), __half2(__ushort_as_half(0x6480), __ushort_as_half(0x6480)));
+  return *reinterpret_cast<const uint32_t*>(&r);
+}
+__device__ __forceinline__ uint32_t pack_f16(float a, float b) {
+  const __half2 h = __floats2half2_rn(a, b);
+  return *reinterpret_cast<const uint32_t*>(&h);
+}
+
+// HBM bound: every cached key and value is read once, 2 * dim * (2 | 1 + 4 / dim) bytes per key and head, against
+// 16 rows' worth of arithmetic at most, of which the tensor cores do the products (m16n8k16: the rows of a group
+// of query heads and of a draft's tokens share one tile).
+//
+// Grid: (part, key/value head, request).  A CTA owns a run of keys; its four warps take steps of 8 KB in turn, each
+// with a ring of its own that it fills with 16-byte asynchronous copies two steps ahead (no barrier between the
+// warps until the end) and page ids fetched 32 blocks ahead.  Every warp keeps the running maximum and sum of its
+// keys; the four are merged through shared memory, and parts of one unit through the workspace by the CTA that
+// arrives last, in the order of the parts.
+//
+// INT8: the codes go to the tensor cores as FP16 (exact).  The key's scale multiplies the score; the value's scale
+// multiplies the weight, taken relative to a running power of two >= every scale seen, so that the FP16 weight
+// stays in [0, 1] whatever the scales are.  The feature order of a matrix step is permuted so that a lane's codes
+// are 16 consecutive bytes; queries (and the result's columns) are permuted alike.
+template <bool kInt8, int D>
+__global__ void __launch_bounds__(kWarps * 32, 2) attn_rows_kernel(const AttnArgs a) {
+  using C = RowCfg<kInt8, D>;
+  constexpr int KS = D / 16;   // matrix steps over the features
+  constexpr int NT = D / 8;    // 8-wide column tiles of the result
+  extern __shared__ __align__(128) uint8_t smem[];
+  __shared__ bool s_last;
+
+  grid_dep_launch();
+  grid_dep_wait();
+
+  const int b = blockIdx.z, hk = blockIdx.y, part = blockIdx.x;
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+  const int g = lane >> 2, c = lane & 3;
+  const int G = a.heads / a.c.heads;
+  const AttnRange rg = attn_range(a, b);
+  if (rg.n <= 0 || rg.n > kAttnRows / G) return;   // nothing to do, or the tile kernel's
+  const int rows = rg.n * G;
+  const int64_t row0 = a.q_start[b];
+  if (row0 < 0 || row0 + rg.n > a.tokens) return;
+
+  const int lo16 = rg.lo & ~15;
+  const int span = rg.hi - lo16;
+  const int parts = span <= 0 ? 1 : static_cast<int>(min(static_cast<int64_t>(gridDim.x), (static_cast<int64_t>(span) + a.part_keys - 1) / a.part_keys));
+  if (part >= parts) return;
+  const int k_begin = lo16 + part * a.part_keys;
+  const int k_end = part == parts - 1 ? rg.hi : k_begin + a.part_keys;
+  const int steps = max(0, (k_end - k_begin + C::kKeys - 1) / C::kKeys);
+  const int my_steps = (steps - warp + kWarps - 1) / kWarps;   // steps warp, warp + 4, ...
+
+  const uint32_t ring = smem_u32(smem) + warp * kStages * C::kStage;
+  const int page16 = a.c.page >> 4;
+  const int64_t head_bytes = static_cast<int64_t>(a.c.page) * C::kRowBytes;
+  const int* trow = a.table + static_cast<int64_t>(b) * a.width;
+
+  // Page ids of 32 blocks of 16 keys at a time (lane l: block l of the warp's current group of steps).
+  constexpr int kGroup = 32 / C::kBlocks;   // steps per group
+  auto fetch_ids = [&](int group) {
+    const int s = group * kGroup + lane / C::kBlocks;
+    const int64_t key = static_cast<int64_t>(k_begin) + static_cast<int64_t>(s * kWarps + warp) * C::kKeys + (lane % C::kBlocks) * 16;
+    int id = -1;
+    if (s < my_steps && key < k_end) {
+      id = trow[static_cast<int>(key >> 4) / page16];
+      if (id < 0 || id >= a.c.pages) id = -1;
+    }
+    return id;
+  };
+  int ids_next = fetch_ids(0), ids = -1;
+
+  // Requests the copies of the warp's step s into stage s % kStages (an empty group beyond the end).
+  auto load_step = [&](int s) {
+    if (s < my_steps) {
+      if (s % kGroup == 0) {
+        ids = ids_next;
+        ids_next = fetch_ids(s / kGroup + 1);
+      }
+      const uint32_t st = ring + (s % kStages) * C::kStage;
+      const int key0 = k_begin + (s * kWarps + warp) * C::kKeys;
+#pragma unroll
+      for (int blk = 0; blk < C::kBlocks; ++blk) {
+        const int id = __shfl_sync(0xffffffffu, ids, (s % kGroup) * C::kBlocks + blk);
+        const int kb = key0 + blk * 16;
+        const bool there = id >= 0;
+        const int off = kb - (kb >> 4) / page16 * a.c.page;   // first key of the block inside its page
+        const int64_t vec = (static_cast<int64_t>(there ? id : 0) * a.c.heads + hk) * a.c.page + (there ? off : 0);
+        const uint8_t* kp = static_cast<const uint8_t*>(a.c.k) + vec * C::kRowBytes;
+        const uint8_t* vp = static_cast<const uint8_t*>(a.c.v) + vec * C::kRowBytes;
+        constexpr int kPer = 16 * C::kChunksPerRow / 32;   // chunks of one lane per block
+        if (there && kb >= rg.lo && kb + 16 <= k_end) {
+#pragma unroll
+          for (int i = 0; i < kPer; ++i) {
+            const int idx = i * 32 + lane, r = idx / C::kChunksPerRow, ch = idx % C::kChunksPerRow;
+            const int R = blk * 16 + r;
+            const int kx = kInt8 ? (D == 128 ? ch ^ ((R & 1) << 2) : ch) : ch ^ (R & 7);
+            const int vx = kInt8 ? (D == 128 ? ch ^ (((R >> 1) & 3) << 1) : ch ^ (((R >> 2) & 1) << 1)) : ch ^ (R & 7);
+            cp_async16(st + R * C::kRowBytes + kx * 16, kp + idx * 16, true);
+            cp_async16(st + C::kHalf + R * C::kRowBytes + vx * 16, vp + idx * 16, true);
+          }
+        } else {
+#pragma unroll
+          for (int i = 0; i < kPer; ++i) {
+            const int idx = i * 32 + lane, r = idx / C::kChunksPerRow, ch = idx % C::kChunksPerRow;
+            const int R = blk * 16 + r;
+            const int kx = kInt8 ? (D == 128 ? ch ^ ((R & 1) << 2) : ch) : ch ^ (R & 7);
+            const int vx = kInt8 ? (D == 128 ? ch ^ (((R >> 1) & 3) << 1) : ch ^ (((R >> 2) & 1) << 1)) : ch ^ (R & 7);
+            const bool live = there && kb + r >= rg.lo && kb + r < k_end;
+            cp_async16(st + R * C::kRowBytes + kx * 16, live ? kp + idx * 16 : kp, live);
+            cp_async16(st + C::kHalf + R * C::kRowBytes + vx * 16, live ? vp + idx * 16 : vp, live);
+          }
+        }
+        if constexpr (kInt8) {
+          const int r = lane & 15;
+          const bool live = there && kb + r >= rg.lo && kb + r < k_end;
+          const float* sp = (lane < 16 ? a.c.k_scale : a.c.v_scale) + vec;
+          cp_async4(st + kStageBytes + (lane < 16 ? 0 : C::kKeys * 4) + (blk * 16 + r) * 4, live ? sp + r : sp, live);
+        }
+      }
+    }
+    cp_commit();
+  };
+
+#pragma unroll
+  for (int s = 0; s < kStages - 1; ++s) load_step(s);
+
+  // The rows' queries as A fragments: rows g and g + 8 of the tile; row r is token r / G, query head hk * G + r % G.
+  uint32_t qa[KS][4];
+  {
+    const __half* qp[2];
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      const int r = g + 8 * i;
+      qp[i] = r < rows ? a.q + (row0 + r / G) * a.q_stride + (hk * G + r % G) * D : nullptr;
+    }
+#pragma unroll
+    for (int s = 0; s < KS; ++s) {
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const int d = kInt8 ? 16 * (c + 4 * (s / 4)) + 4 * (s % 4) + 2 * (i >> 1) : 16 * s + 2 * c + 8 * (i >> 1);
+        const __half* p = qp[i & 1];
+        qa[s][i] = p != nullptr ? __ldg(reinterpret_cast<const uint32_t*>(p + d)) : 0u;
+      }
+    }
+  }
+  // Last key that each of the thread's two rows sees, and the first (window).
+  int p_row[2], w_row[2];
+#pragma unroll
+  for (int i = 0; i < 2; ++i) {
+    const int r = g + 8 * i;
+    const int p = rg.L - rg.n + r / G;
+    p_row[i] = r < rows ? min(p, rg.hi - 1) : -1;
+    w_row[i] = a.window > 0 ? p - a.window : -1;   // keys above it
+  }
+  const int all_from = a.window > 0 ? rg.L - a.window : 0;      // keys that every row sees: [all_from, all_to)
+  const int all_to = min(rg.L - rg.n + 1, rg.hi);
+
+  float o[NT][4];
+#pragma unroll
+  for (int i = 0; i < NT; ++i) o[i][0] = o[i][1] = o[i][2] = o[i][3] = 0.0f;
+  float m[2] = {-INFINITY, -INFINITY}, l[2] = {0.0f, 0.0f};
+  float vref = 0.0f;   // INT8: o is in units of vref
+
+  for (int s = 0; s < my_steps; ++s) {
+    cp_wait<kStages - 2>();
+    __syncwarp();
+    load_step(s + kStages - 1);
+    const uint32_t st = ring + (s % kStages) * C::kStage;
+    const int key0 = k_begin + (s * kWarps + warp) * C::kKeys;
+
+    float sc[C::kBlocks][2][4];
+#pragma unroll
+    for (int blk = 0; blk < C::kBlocks; ++blk) {
+#pragma unroll
+      for (int t = 0; t < 2; ++t) sc[blk][t][0] = sc[blk][t][1] = sc[blk][t][2] = sc[blk][t][3] = 0.0f;
+      if constexpr (!kInt8) {
+        const int R = blk * 16 + (lane & 7) + ((lane >> 4) << 3);
+#pragma unroll
+        for (int k = 0; k < KS; ++k) {
+          uint32_t r[4];
+          ldsm4(st + R * C::kRowBytes + (((k * 2 + ((lane >> 3) & 1)) ^ (R & 7)) * 16), r);
+          mma16816(sc[blk][0], qa[k], r[0], r[1]);
+          mma16816(sc[blk][1], qa[k], r[2], r[3]);
+        }
+      } else {
+#pragma unroll
+        for (int t = 0; t < 2; ++t) {
+          const int R = blk * 16 + t * 8 + g;
+#pragma unroll
+          for (int q4 = 0; q4 < KS / 4; ++q4) {
+            const int ch = c + 4 * q4;
+            const uint4 w = lds128(st + R * C::kRowBytes + (D == 128 ? ch ^ ((R & 1) << 2) : ch) * 16);
+            const uint32_t u[4] = {w.x ^ 0x80808080u, w.y ^ 0x80808080u, w.z ^ 0x80808080u, w.w ^ 0x80808080u};
+#pragma unroll
+            for (int i = 0; i < 4; ++i) mma16816(sc[blk][t], qa[q4 * 4 + i], codes_f16(u[i], 0x4140), codes_f16(u[i], 0x4342));
+          }
+        }
+      }
+    }
+
+    // Scores in powers of two, masked; the step's maxima.
+    const bool all = key0 >= all_from && key0 + C::kKeys <= all_to;
+    float vs[C::kBlocks][2][2];
+    float top[2] = {-INFINITY, -INFINITY}, vtop = 0.0f;
+#pragma unroll
+    for (int blk = 0; blk < C::kBlocks; ++blk) {
+#pragma unroll
+      for (int t = 0; t < 2; ++t) {
+        float2 ks = make_float2(a.scale_log2, a.scale_log2);
+        const int j = blk * 16 + t * 8 + 2 * c;
+        if constexpr (kInt8) {
+          const float2 kk = lds_f2(st + kStageBytes + j * 4), vv = lds_f2(st + kStageBytes + (C::kKeys + j) * 4);
+          ks = make_float2(ks.x * kk.x, ks.y * kk.y);
+          vs[blk][t][0] = vv.x, vs[blk][t][1] = vv.y;
+          vtop = fmaxf(vtop, fmaxf(vv.x, vv.y));
+        }
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+          sc[blk][t][2 * i] *= ks.x;
+          sc[blk][t][2 * i + 1] *= ks.y;
+          if (!all) {
+            const int key = key0 + j;
+            if (key > p_row[i] || key <= w_row[i]) sc[blk][t][2 * i] = -INFINITY;
+            if (key + 1 > p_row[i] || key + 1 <= w_row[i]) sc[blk][t][2 * i + 1] = -INFINITY;
+          }
+          top[i] = fmaxf(top[i], fmaxf(sc[blk][t][2 * i], sc[blk][t][2 * i + 1]));
+        }
+      }
+    }
+#pragma unroll
+    for (int d = 1; d < 4; d <<= 1) {
+      top[0] = fmaxf(top[0], __shfl_xor_sync(0xffffffffu, top[0], d));
+      top[1] = fmaxf(top[1], __shfl_xor_sync(0xffffffffu, top[1], d));
+      if constexpr (kInt8) vtop = fmaxf(vtop, __shfl_xor_sync(0xffffffffu, vtop, d));
+    }
+    const bool grown = top[0] > m[0] || top[1] > m[1] || (kInt8 && vtop > vref);
+    if (__any_sync(0xffffffffu, grown)) {
+      float f[2];
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        const float mn = fmaxf(m[i], top[i]);
+        f[i] = m[i] == -INFINITY ? 0.0f : exp2_approx(m[i] - mn);
+        m[i] = mn;
+        l[i] *= f[i];
+      }
+      if (kInt8 && vtop > vref) {   // the same in every lane: all rows share the keys
+        const float vn = __uint_as_float((__float_as_uint(fminf(vtop, 1e37f)) + 0x7fffffu) & 0x7f800000u);
+        const float fv = vref / vn;
+        vref = vn;
+        f[0] *= fv, f[1] *= fv;
+      }
+#pragma unroll
+      for (int i = 0; i < NT; ++i) o[i][0] *= f[0], o[i][1] *= f[0], o[i][2] *= f[1], o[i][3] *= f[1];
+    }
+    const float vinv = kInt8 ? (vref > 0.0f ? 1.0f / vref : 0.0f) : 1.0f;
+    const float mm[2] = {m[0] == -INFINITY ? 0.0f : m[0], m[1] == -INFINITY ? 0.0f : m[1]};
+
+    // Weights as A fragments, then the product with the values.
+#pragma unroll
+    for (int blk = 0; blk < C::kBlocks; ++blk) {
+      uint32_t pa[4];
+#pragma unroll
+      for (int t = 0; t < 2; ++t) {
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+          const float e0 = exp2_approx(sc[blk][t][2 * i] - mm[i]), e1 = exp2_approx(sc[blk][t][2 * i + 1] - mm[i]);
+          l[i] += e0 + e1;
+          pa[t * 2 + i] = kInt8 ? pack_f16(e0 * (vs[blk][t][0] * vinv), e1 * (vs[blk][t][1] * vinv)) : pack_f16(e0, e1);
+        }
+      }
+      const uint32_t sv = st + C::kHalf;
+      if constexpr (!kInt8) {
+        const int R = blk * 16 + (lane & 7) + (((lane >> 3) & 1) << 3);
+#pragma unroll
+        for (int n2 = 0; n2 < NT / 2; ++n2) {
+          uint32_t r[4];
+          ldsm4_t(sv + R * C::kRowBytes + (((n2 * 2 + (lane >> 4)) ^ (R & 7)) * 16), r);
+          mma16816(o[2 * n2], pa, r[0], r[1]);
+          mma16816(o[2 * n2 + 1], pa, r[2], r[3]);
+        }
+      } else {
+        uint32_t w[4][NT / 4];   // four keys (2c, 2c + 1, 2c + 8, 2c + 9), NT consecutive features from NT * g
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const int R = blk * 16 + 2 * c + (i & 1) + 8 * (i >> 1);
+          if constexpr (D == 128) {
+            const uint4 x = lds128(sv + R * C::kRowBytes + (g ^ (((R >> 1) & 3) << 1)) * 16);
+            w[i][0] = x.x, w[i][1] = x.y, w[i][2] = x.z, w[i][3] = x.w;
+          } else {
+            const uint2 x = lds64(sv + R * C::kRowBytes + ((g >> 1) ^ (((R >> 2) & 1) << 1)) * 16 + (g & 1) * 8);
+            w[i][0] = x.x, w[i][1] = x.y;
+          }
+        }
+#pragma unroll
+        for (int i = 0; i < NT / 4; ++i) {
+          const uint32_t x0 = __byte_perm(w[0][i], w[1][i], 0x5140) ^ 0x80808080u, x1 = __byte_perm(w[0][i], w[1][i], 0x7362) ^ 0x80808080u;
+          const uint32_t y0 = __byte_perm(w[2][i], w[3][i], 0x5140) ^ 0x80808080u, y1 = __byte_perm(w[2][i], w[3][i], 0x7362) ^ 0x80808080u;
+          mma16816(o[4 * i], pa, codes_f16(x0, 0x4140), codes_f16(y0, 0x4140));
+          mma16816(o[4 * i + 1], pa, codes_f16(x0, 0x4342), codes_f16(y0, 0x4342));
+          mma16816(o[4 * i + 2], pa, codes_f16(x1, 0x4140), codes_f16(y1, 0x4140));
+          mma16816(o[4 * i + 3], pa, codes_f16(x1, 0x4342), codes_f16(y1, 0x4342));
+        }
+      }
+    }
+    __syncwarp();   // the stage is free
+  }
+  cp_wait<0>();
+  __syncthreads();   // the rings become the merging room
+
+  // Merge of the four warps: [warp][row][dim] sums, then [warp][row] (maximum, sum).
+  float* so = reinterpret_cast<float*>(smem);
+  float2* sml = reinterpret_cast<float2*>(so + kWarps * kAttnRows * D);
+#pragma unroll
+  for (int i = 0; i < 2; ++i) {
+#pragma unroll
+    for (int d = 1; d < 4; d <<= 1) l[i] += __shfl_xor_sync(0xffffffffu, l[i], d);
+    const int r = g + 8 * i;
+    if (r < rows) {
+      if (c == 0) sml[warp * kAttnRows + r] = make_float2(m[i], l[i]);
+      float* dst = so + (warp * kAttnRows + r) * D;
+#pragma unroll
+      for (int t = 0; t < NT; ++t) {
+        if constexpr (kInt8) {
+          dst[NT * 2 * c + t] = o[t][2 * i] * vref;
+          dst[NT * (2 * c + 1) + t] = o[t][2 * i + 1] * vref;
+        } else {
+          *reinterpret_cast<float2*>(dst + 8 * t + 2 * c) = make_float2(o[t][2 * i], o[t][2 * i + 1]);
+        }
+      }
+    }
+  }
+  __syncthreads();
+
+  const int64_t unit = static_cast<int64_t>(b) * a.c.heads + hk;
+  constexpr int kPart = kAttnRows * (D + 2);   // floats of one part
+  float* pu = a.partials + unit * gridDim.x * kPart;
+  auto store_out = [&](int r, int d4, float4 v) {
+    uint2 h = make_uint2(pack_f16(v.x, v.y), pack_f16(v.z, v.w));
+    *reinterpret_cast<uint2*>(a.out + ((row0 + r / G) * a.heads + hk * G + r % G) * D + 4 * d4) = h;
+  };
+  for (int idx = tid; idx < rows * (D / 4); idx += kWarps * 32) {
+    const int r = idx / (D / 4), d4 = idx % (D / 4);
+    float M = -INFINITY;
+#pragma unroll
+    for (int w = 0; w < kWarps; ++w) M = fmaxf(M, sml[w * kAttnRows + r].x);
+    const float Ms = M == -INFINITY ? 0.0f : M;
+    float sum = 0.0f;
+    float4 v = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+#pragma unroll
+    for (int w = 0; w < kWarps; ++w) {
+      const float2 ml = sml[w * kAttnRows + r];
+      const float f = exp2_approx(ml.x - Ms);
+      const float4 x = *reinterpret_cast<const float4*>(so + (w * kAttnRows + r) * D + 4 * d4);
+      sum = fmaf(ml.y, f, sum);
+      v.x = fmaf(x.x, f, v.x), v.y = fmaf(x.y, f, v.y), v.z = fmaf(x.z, f, v.z), v.w = fmaf(x.w, f, v.w);
+    }
+    if (parts == 1) {
+      const float inv = sum > 0.0f ? 1.0f / sum : 0.0f;
+      store_out(r, d4, make_float4(v.x * inv, v.y * inv, v.z * inv, v.w * inv));
+    } else {
+      *reinterpret_cast<float4*>(pu + part * kPart + r * D + 4 * d4) = v;
+      if (d4 == 0) *reinterpret_cast<float2*>(pu + part * kPart + kAttnRows * D + 2 * r) = make_float2(M, sum);
+    }
+  }
+  if (parts == 1) return;
+
+  // The CTA that arrives last joins the parts, in their order.
+  __threadfence();
+  __syncthreads();
+  if (tid == 0) {
+    const unsigned int before = atomicAdd(a.counters + unit, 1u);
+    s_last = before == static_cast<unsigned int>(parts) - 1u;
+    if (s_last) a.counters[unit] = 0u;
+  }
+  __syncthreads();
+  if (!s_last) return;
+  __threadfence();
+  for (int idx = tid; idx < rows * (D / 4); idx += kWarps * 32) {
+    const int r = idx / (D / 4), d4 = idx % (D / 4);
+    float M = -INFINITY, sum = 0.0f;
+    float4 v = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+#pragma unroll 4
+    for (int p = 0; p < parts; ++p) {
+      const float2 ml = __ldcg(reinterpret_cast<const float2*>(pu + p * kPart + kAttnRows * D + 2 * r));
+      const float4 x = __ldcg(reinterpret_cast<const float4*>(pu + p * kPart + r * D + 4 * d4));
+      const float mn = fmaxf(M, ml.x), ms = mn == -INFINITY ? 0.0f : mn;
+      const float f = exp2_approx(M - ms), e = exp2_approx(ml.x - ms);
+      M = mn;
+      sum = fmaf(sum, f, ml.y * e);
+      v.x = fmaf(v.x, f, x.x * e), v.y = fmaf(v.y, f, x.y * e), v.z = fmaf(v.z, f, x.z * e), v.w = fmaf(v.w, f, x.w * e);
+    }
+    const float inv = sum > 0.0f ? 1.0f / sum : 0.0f;
+    store_out(r, d4, make_float4(v.x * inv, v.y * inv, v.z * inv, v.w * inv));
+  }
+}
+
+template <bool kInt8, int D>
+int launch(const AttnArgs& a, const AttnPlan& plan, cudaStream_t stream) {
+  using C = RowCfg<kInt8, D>;
+  static_assert(C::kSmem >= kWarps * kAttnRows * (D + 2) * 4, "the merge has to fit the rings");
+  static PerDeviceOnce once;
+  if (const int rc = set_dynamic_smem_once(once, attn_rows_kernel<kInt8, D>, C::kSmem); rc != PQ_OK) return rc;
+  const dim3 grid(static_cast<unsigned>(plan.parts), static_cast<unsigned>(a.c.heads), static_cast<unsigned>(a.requests));
+  return launch_dependent(attn_rows_kernel<kInt8, D>, grid, dim3(kWarps * 32), C::kSmem, stream, a);
+}
+
+}  // namespace
+
+// Two CTAs are resident on an SM.  Few units: as many parts as fill the machine once.  Many units: parts of about
+// 1024 keys, so that requests of different lengths even out over the waves.
+AttnPlan plan_attn_rows(int64_t requests, int64_t max_kv, int kv_heads, int dim, int sms, size_t room) {
+  AttnPlan p;
+  p.units = requests * kv_heads;
+  static const int forced = [] { const char* e = getenv("PQ_ATTN_PART"); return e ? atoi(e) : 0; }();   // ablation knob
+  const int64_t slots = 2 * sms;
+  int64_t keys = 1024;
+  if (p.units * ((max_kv + 1023) / 1024) < 2 * slots) {
+    const int64_t want = slots / p.units < 1 ? 1 : slots / p.units;
+    keys = (max_kv + want - 1) / want;
+    keys = keys < 256 ? 256 : (keys + 127) / 128 * 128;
+  }
+  if (forced > 0) keys = (forced + 127) / 128 * 128;
+  p.part_keys = static_cast<int>(keys);
+  int64_t parts = (max_kv + 15 + keys - 1) / keys;   // the first part begins at a multiple of 16
+  if (p.units > kScratchCounters || parts < 1) parts = 1;
+  if (parts > 65535) parts = 65535;
+  const size_t one = static_cast<size_t>(kAttnRows) * (dim + 2) * 4;
+  if (parts > 1 && static_cast<size_t>(p.units) * parts * one > room) {
+    const int64_t fit = static_cast<int64_t>(room / (static_cast<size_t>(p.units) * one));
+    parts = fit < 2 ? 1 : fit;   // the last part takes the keys that are left: fewer parts have to be longer
+    p.part_keys = static_cast<int>(((max_kv + parts - 1) / parts + 127) / 128 * 128);
+  }
+  p.parts = static_cast<int>(parts);
+  p.partial_bytes = parts > 1 ? static_cast<size_t>(p.units) * parts * one : 0;
+  return p;
+}
+
+int launch_attn_rows(const AttnArgs& a, const AttnPlan& plan, cudaStream_t stream) {
+  if (a.c.type == PQ_KV_INT8) return a.c.dim == 128 ? launch<true, 128>(a, plan, stream) : launch<true, 64>(a, plan, stream);
+  return a.c.dim == 128 ? launch<false, 128>(a, plan, stream) : launch<false, 64>(a, plan, stream);
+}
+
+}  // namespace pq
