@@ -107,6 +107,11 @@ int pq_paged_attention(const void* q_f16, int64_t q_stride, int32_t heads, const
   a.partials = reinterpret_cast<float*>(sc.partials);
   rc = launch_attn_rows(a, plan, static_cast<cudaStream_t>(stream));
   if (rc != PQ_OK || max_q * (heads / cache->heads) <= kAttnRows) return rc;
+  if (cache->type == PQ_KV_F16) {
+    const TilePlan tile = plan_attn_tile(requests, tokens, max_q, max_kv, heads / cache->heads, cache->heads, cache->dim,
+                                         sm_count(), sc.partial_bytes);
+    return launch_attn_tile(a, tile, static_cast<cudaStream_t>(stream));
+  }
   const int64_t blocks = (tokens * heads + 3) / 4;
   if (blocks > 0x7fffffff) return PQ_ERR_SHAPE;
   const dim3 grid(static_cast<unsigned>(blocks)), block(128);
@@ -126,7 +131,12 @@ size_t pq_attention_workspace_bytes(int64_t requests, int64_t tokens, int64_t ma
     return 0;
   }
   const AttnPlan plan = plan_attn_rows(requests, max_kv, kv_heads, dim, sms, ~size_t(0));
-  return plan.parts > 1 ? kScratchHeaderBytes + plan.partial_bytes : 0;
+  size_t bytes = plan.partial_bytes;
+  if (max_q * (heads / kv_heads) > kAttnRows) {
+    const TilePlan tile = plan_attn_tile(requests, tokens, max_q, max_kv, heads / kv_heads, kv_heads, dim, sms, ~size_t(0));
+    bytes = bytes > tile.partial_bytes ? bytes : tile.partial_bytes;   // the two kernels follow each other
+  }
+  return bytes > 0 ? kScratchHeaderBytes + bytes : 0;
 }
 
 }  // extern "C"

@@ -40,6 +40,17 @@ AttnPlan plan_attn_rows(int64_t requests, int64_t max_kv, int kv_heads, int dim,
 
 int launch_attn_rows(const AttnArgs& a, const AttnPlan& plan, cudaStream_t stream);
 
+// The tile kernel's schedule: a unit is one tile of 2 x (128 / group) tokens of one key/value head.
+struct TilePlan {
+  int64_t units = 0;      // CTAs per part: an upper bound of the units there are
+  int parts = 1;
+  int part_keys = 128;
+  size_t partial_bytes = 0;
+};
+TilePlan plan_attn_tile(int64_t requests, int64_t tokens, int64_t max_q, int64_t max_kv, int group, int kv_heads, int dim,
+                        int sms, size_t room);
+int launch_attn_tile(const AttnArgs& a, const TilePlan& plan, cudaStream_t stream);
+
 __device__ __forceinline__ float exp2_approx(float x) {
   float y;
   asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));

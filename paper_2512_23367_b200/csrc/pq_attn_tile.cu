@@ -1,0 +1,594 @@
+// Attention of more than 16 query rows per (request, key/value head) over the paged cache, on the tcgen05 tensor
+// cores: prompts, chunks of prompts and wide drafts.
+#include <cstdlib>
+
+#include "pq_attention.h"
+#include "pq_ptx.cuh"
+
+namespace pq {
+
+namespace {
+
+constexpr int kTile = 128;          // query rows of one accumulator, keys of one step
+constexpr int kThreads = 384;       // two softmax warpgroups; MMA issuer, producer and two idle warps
+constexpr int kSoftRegs = 216, kRestRegs = 72;   // 2 x 128 x 216 + 128 x 72 = 384 x 168, what the launch holds
+
+template <int D>
+struct TileCfg {
+  static constexpr int kTileBytes = kTile * D * 2;            // one operand tile: D / 64 panels of 128 rows x 128 B
+  static constexpr int kPanel = kTile * 128;
+  static constexpr int kStages = 163840 / kTileBytes;         // 5 (D = 128) or 10: keys and values alternate
+  static constexpr int kBars = 2 * kStages + 9;
+  static constexpr int kSmem = 2 * kTileBytes + kStages * kTileBytes + 1024 /* alignment */;
+};
+
+// ---- tcgen05 with 16-bit floating-point operands
+// kind::f16, FP16 A and B, FP32 accumulator, M = 128; b_mn: B is stored with its N dimension contiguous.
+__host__ __device__ constexpr uint32_t umma_idesc_f16(uint32_t N, bool b_mn) {
+  return (1u << 4) | (b_mn ? (1u << 16) : 0u) | ((N >> 3) << 17) | ((128u >> 4) << 24);
+}
+__device__ __forceinline__ void umma_f16_ss(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, uint32_t acc) {
+  asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\ttcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n\t}"
+               ::"r"(d), "l"(a), "l"(b), "r"(idesc), "r"(acc) : "memory");
+}
+// A in tensor memory: lane = row, a 32-bit column holds two neighbouring k.
+__device__ __forceinline__ void umma_f16_ts(uint32_t d, uint32_t a, uint64_t b, uint32_t idesc, uint32_t acc) {
+  asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\ttcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}"
+               ::"r"(d), "r"(a), "l"(b), "r"(idesc), "r"(acc) : "memory");
+}
+// B operand whose N dimension is contiguous, 128-byte swizzle: panels of 64 columns (`panel` bytes apart), inside
+// a panel groups of 8 k-rows of 128 bytes, 1024 bytes apart.
+__device__ __forceinline__ uint64_t umma_desc_mn_sw128(uint32_t saddr, uint32_t panel) {
+  uint64_t d = 0;
+  d |= static_cast<uint64_t>((saddr & 0x3FFFFu) >> 4);
+  d |= static_cast<uint64_t>(panel >> 4) << 16;
+  d |= static_cast<uint64_t>(1024 >> 4) << 32;
+  d |= static_cast<uint64_t>(1) << 46;
+  d |= static_cast<uint64_t>(2) << 61;
+  return d;
+}
+__device__ __forceinline__ void tmem_st_32x32(uint32_t taddr, const uint32_t (&r)[32]) {
+  asm volatile(
+      "tcgen05.st.sync.aligned.32x32b.x32.b32 [%0], "
+      "{%1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16, "
+      "%17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31, %32};" ::"r"(taddr),
+      "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]), "r"(r[9]),
+      "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15]), "r"(r[16]), "r"(r[17]), "r"(r[18]),
+      "r"(r[19]), "r"(r[20]), "r"(r[21]), "r"(r[22]), "r"(r[23]), "r"(r[24]), "r"(r[25]), "r"(r[26]), "r"(r[27]),
+      "r"(r[28]), "r"(r[29]), "r"(r[30]), "r"(r[31])
+      : "memory");
+}
+__device__ __forceinline__ void tmem_st_wait() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
+
+__device__ __forceinline__ uint32_t pack_f16(float a, float b) {
+  const __half2 h = __floats2half2_rn(a, b);
+  return *reinterpret_cast<const uint32_t*>(&h);
+}
+
+// A wait of a whole warp whose lanes go on, or give up, together.
+__device__ __forceinline__ bool warp_wait(uint32_t bar, uint32_t parity, const WaitCtx& wc) {
+  return __all_sync(0xffffffffu, mbar_wait(bar, parity, wc));
+}
+
+struct TileArgs {
+  AttnArgs a;
+  int* status;
+  uint32_t wait_limit;
+  int box;               // rows of a TMA box: the largest power of two that divides both the page and 128
+  uint32_t q_and, q_xor; // a scale of 0 or below is folded into the queries: (q & q_and) ^ q_xor
+};
+
+// Tensor bound for long chunks, HBM bound for wide drafts over long caches.
+//
+// A CTA owns 256 query rows of one key/value head (row = token x query heads of the group) as two accumulators of
+// 128, or up to 128 rows as two accumulators that take the even and the odd key tiles and are joined at the end:
+// either way one warpgroup's softmax runs while the tensor core works for the other.  Per 128 keys and accumulator:
+//   S = Q K^T            8 (D / 16) MMAs from shared memory into tensor memory
+//   softmax              one thread per row: S to registers, running maximum, P = 2^(S - max) as FP16 over S
+//   O += P V             8 MMAs with P from tensor memory, V as it lies in the cache (features contiguous)
+// The reference that is subtracted is only moved (and O rescaled, in tensor memory) when the maximum has grown by
+// more than 2^8: P stays within [0, 256], exact enough in FP16, and O is almost never touched.
+// MMA order: QK(u), PV(u - 1), u counting the accumulators in turn; the tensor core executes in order, so S (which
+// P overlays) is free when its next QK is issued.
+// Keys and values come through TMA boxes of whole page pieces (one lane looks up and requests one box); boxes that
+// no visible key needs, or of an unusable page id, are requested beyond the tensor and arrive as zeros.
+// Value rows that were never written (beyond the request's length, before its window) are zeroed in shared memory:
+// their weight is 0, but 0 x NaN is not.
+template <int D>
+__global__ void __launch_bounds__(kThreads, 1)
+attn_tile_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtensorMap map_v, const TileArgs ta) {
+  using C = TileCfg<D>;
+  constexpr int KS = D / 16;        // MMAs of one QK
+  constexpr int PS = kTile / 16;    // MMAs of one PV
+  extern __shared__ uint8_t smem_raw[];
+  __shared__ __align__(8) uint64_t bars[C::kBars];
+  __shared__ uint32_t s_tmem;
+  __shared__ volatile int s_abort;
+  __shared__ int s_assign[2];
+  __shared__ int s_warp_sum[kThreads / 32];
+  __shared__ int s_last;
+
+  const AttnArgs& a = ta.a;
+  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+  const int G = a.heads / a.c.heads;
+  const int tpt = kTile / G;          // tokens of one accumulator
+  const int qt = 2 * tpt;             // tokens of one CTA
+  const int slot = blockIdx.x / a.c.heads, hk = blockIdx.x - slot * a.c.heads;
+
+  const uint32_t bar0 = smem_u32(bars);
+  const uint32_t bar_full = bar0, bar_free = bar0 + 8 * C::kStages;
+  const uint32_t bar_s = bar0 + 16 * C::kStages, bar_p = bar_s + 16, bar_o = bar_p + 16;   // two of each
+  const uint32_t bar_q = bar_o + 16, bar_fix = bar_q + 8, bar_drain = bar_fix + 8;
+  if (tid == 0) {
+    for (int i = 0; i < C::kStages; ++i) mbar_init(bar_full + 8 * i, 1), mbar_init(bar_free + 8 * i, 1);
+    for (int i = 0; i < 2; ++i) mbar_init(bar_s + 8 * i, 1), mbar_init(bar_p + 8 * i, 4), mbar_init(bar_o + 8 * i, 1);
+    mbar_init(bar_q, 8);
+    mbar_init(bar_fix, 1);
+    mbar_init(bar_drain, 1);
+    fence_mbar_init();
+    s_abort = 0;
+    s_assign[0] = -1;
+    tma_prefetch_desc(&map_k);
+    tma_prefetch_desc(&map_v);
+  }
+  grid_dep_wait();
+  __syncthreads();
+
+  // Which request and which of its tiles: the slot-th over all requests that this kernel serves.  A request's
+  // last tile, which sees most keys, comes first.
+  {
+    int before = 0;
+    for (int base = 0; base < a.requests; base += kThreads) {
+      const int b = base + tid;
+      int cnt = 0;
+      if (b < a.requests) {
+        const int n = a.q_start[b + 1] - a.q_start[b];
+        if (n > kAttnRows / G) cnt = (n - 1) / qt + 1;
+      }
+      int in = cnt;
+#pragma unroll
+      for (int o = 1; o < 32; o <<= 1) {
+        const int x = __shfl_up_sync(0xffffffffu, in, o);
+        if (lane >= o) in += x;
+      }
+      if (lane == 31) s_warp_sum[warp] = in;
+      __syncthreads();
+      int off = before;
+      for (int w = 0; w < kThreads / 32; ++w) {
+        if (w < warp) off += s_warp_sum[w];
+        before += s_warp_sum[w];
+      }
+      const int mine = slot - (off + in - cnt);
+      if (mine >= 0 && mine < cnt) s_assign[0] = b, s_assign[1] = cnt - 1 - mine;
+      __syncthreads();
+      if (slot < before) break;
+    }
+  }
+  const int b = s_assign[0];
+  if (b < 0) return;
+  const int tok0 = s_assign[1] * qt;
+  const AttnRange rg = attn_range(a, b);
+  const int64_t row0 = a.q_start[b];
+  const int toks = min(qt, rg.n - tok0);
+  const bool two = toks > tpt;
+  const int p_base = rg.L - rg.n + tok0;                        // position of the CTA's first row
+  const int k_hi = min(rg.hi, p_base + toks);                   // keys that some row sees: [k_lo, k_hi)
+  const int k_lo = (a.window > 0 ? max(0, p_base + 1 - a.window) : 0) & ~(kTile - 1);
+  const int all_tiles = k_hi > k_lo ? (k_hi - k_lo + kTile - 1) / kTile : 0;
+  const int per = a.part_keys / kTile;
+  const int parts = max(1, min(static_cast<int>(gridDim.y), (all_tiles + per - 1) / per));
+  const int part = blockIdx.y;
+  if (part >= parts) return;
+  const int t0 = part * per;
+  const int n_tiles = part == parts - 1 ? all_tiles - t0 : per;   // key tiles of this CTA
+  const int key_base = k_lo + t0 * kTile;
+  const int N = two ? 2 * n_tiles : n_tiles;                      // (QK, PV) steps
+
+  const uint32_t base = (smem_u32(smem_raw) + 1023u) & ~1023u;
+  const uint32_t sq = base, ring = base + 2 * C::kTileBytes;
+  if (warp == 8) tmem_alloc(smem_u32(&s_tmem), 512);
+  tc_fence_before_sync();
+  __syncthreads();
+  tc_fence_after_sync();
+  grid_dep_launch();   // only now: a later launch's CTA may take this SM's tensor memory when it is given back
+  const uint32_t tmem = s_tmem;
+  const uint32_t t_s[2] = {tmem, tmem + 128}, t_o[2] = {tmem + 256, tmem + 256 + D};
+  const WaitCtx wc{&s_abort, ta.wait_limit};
+  int issued = 0;   // producer: loads requested so far
+
+  if (warp >= 8) {
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kRestRegs));
+    if (warp == 9) {
+      // ------------------------------------------------------------------ producer
+      const int boxes = kTile / ta.box;
+      const int halves = D / 64;
+      const int rows_all = static_cast<int>(a.c.pages * a.c.heads * a.c.page);
+      uint32_t fix_phase = 0;
+      for (int i = 0; i < 2 * n_tiles; ++i) {
+        const int st = i % C::kStages;
+        if (i >= C::kStages && !warp_wait(bar_free + 8 * st, ((i / C::kStages) & 1) ^ 1, wc)) break;
+        const int key0 = key_base + (i >> 1) * kTile;
+        const bool is_v = i & 1;
+        // rows of the tile that were never written: before the request's window, beyond its length
+        const int dead_lo = min(max(rg.lo - key0, 0), kTile), dead_hi = min(max(rg.L - key0, 0), kTile);
+        const bool fix = is_v && (dead_lo > 0 || dead_hi < kTile);
+        const uint32_t dst = ring + st * C::kTileBytes, bar = fix ? bar_fix : bar_full + 8 * st;
+        if (lane == 0) mbar_arrive_expect_tx(bar, C::kTileBytes);
+        __syncwarp();
+        if (lane < boxes * halves) {
+          const int x = lane / boxes, y = lane - x * boxes;
+          const int key = key0 + y * ta.box;
+          int row = rows_all;   // beyond the tensor: zeros
+          if (key < rg.hi && key + ta.box > rg.lo) {
+            const int col = key / a.c.page;
+            const int id = a.table[static_cast<int64_t>(b) * a.width + col];
+            if (id >= 0 && id < a.c.pages) row = static_cast<int>((static_cast<int64_t>(id) * a.c.heads + hk) * a.c.page) + key - col * a.c.page;
+          }
+          tma_load_2d(dst + x * C::kPanel + y * ta.box * 128, is_v ? &map_v : &map_k, bar, x * 64, row);
+        }
+        issued = i + 1;
+        if (fix) {
+          if (!warp_wait(bar_fix, fix_phase & 1, wc)) break;
+          ++fix_phase;
+          const int dead = dead_lo + (kTile - dead_hi);
+          for (int j = lane; j < dead * halves * 8; j += 32) {
+            const int chunk = j & 7, x = (j >> 3) % halves, r = (j >> 3) / halves;
+            const int rr = r < dead_lo ? r : dead_hi + r - dead_lo;
+            asm volatile("st.shared.v4.u32 [%0], {%1, %1, %1, %1};" ::"r"(dst + x * C::kPanel + rr * 128 + chunk * 16), "r"(0) : "memory");
+          }
+          fence_proxy_async_smem();
+          __syncwarp();
+          if (lane == 0) mbar_arrive(bar_full + 8 * st);
+        }
+        __syncwarp();
+      }
+    } else if (warp == 8 && lane == 0) {
+      // ------------------------------------------------------------------ MMA issuer
+      constexpr uint32_t id_qk = umma_idesc_f16(kTile, false), id_pv = umma_idesc_f16(D, true);
+      bool ok = mbar_wait(bar_q, 0, wc);
+      tc_fence_after_sync();
+      for (int u = 0; ok && u <= N; ++u) {
+        if (u < N) {   // S(u) = Q K^T
+          const int acc = u & 1, kt = two ? u >> 1 : u;
+          const int i = 2 * kt, st = i % C::kStages;
+          if (!(ok = mbar_wait(bar_full + 8 * st, (i / C::kStages) & 1, wc))) break;
+          tc_fence_after_sync();
+          const uint32_t qs = sq + (two ? acc * C::kTileBytes : 0), ks = ring + st * C::kTileBytes;
+#pragma unroll
+          for (int k = 0; k < KS; ++k) {
+            const uint32_t off = (k / 4) * C::kPanel + (k % 4) * 32;
+            umma_f16_ss(t_s[acc], umma_desc_k_sw128(qs + off), umma_desc_k_sw128(ks + off), id_qk, k > 0);
+          }
+          umma_commit(bar_s + 8 * acc);
+          if (!two || acc == 1) umma_commit(bar_free + 8 * st);
+        }
+        if (u > 0) {   // O(u - 1) += P V
+          const int v = u - 1, acc = v & 1, kt = two ? v >> 1 : v;
+          const int i = 2 * kt + 1, st = i % C::kStages;
+          if (!(ok = mbar_wait(bar_full + 8 * st, (i / C::kStages) & 1, wc))) break;
+          if (!(ok = mbar_wait(bar_p + 8 * acc, (v >> 1) & 1, wc))) break;
+          tc_fence_after_sync();
+          const uint32_t vs = ring + st * C::kTileBytes;
+#pragma unroll
+          for (int k = 0; k < PS; ++k)
+            umma_f16_ts(t_o[acc], t_s[acc] + 8 * k, umma_desc_mn_sw128(vs + k * 2048, C::kPanel), id_pv, (v >> 1) > 0 || k > 0);
+          umma_commit(bar_o + 8 * acc);
+          if (!two || acc == 1) umma_commit(bar_free + 8 * st);
+        }
+      }
+    }
+  } else {
+    // -------------------------------------------------------------------- softmax, one thread per row
+    asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kSoftRegs));
+    const int acc = warp >> 2;                       // accumulator
+    const int r = tid & 127;                         // row of the tile
+    const uint32_t lane_off = static_cast<uint32_t>(warp & 3) << 21;   // 32 lanes per warp, lane in bits 16 and up
+    const int q_tile = two ? acc : 0;
+    const int tok = q_tile * tpt + r / G;            // token of the row, from tok0
+    const bool live = r < tpt * G && tok < toks && row0 + tok0 + tok >= 0 && row0 + tok0 + tok < a.tokens;
+    const int64_t out_row = (row0 + tok0 + tok) * a.heads + hk * G + r % G;
+
+    if (two || acc == 0) {
+      const uint4* qp = live ? reinterpret_cast<const uint4*>(a.q + (row0 + tok0 + tok) * a.q_stride + (hk * G + r % G) * D) : nullptr;
+      uint4 x[D / 8];
+#pragma unroll
+      for (int i = 0; i < D / 8; ++i) x[i] = live ? __ldg(qp + i) : make_uint4(0, 0, 0, 0);
+      const uint32_t dst = sq + q_tile * C::kTileBytes + r * 128;
+#pragma unroll
+      for (int i = 0; i < D / 8; ++i) {
+        x[i].x = (x[i].x & ta.q_and) ^ ta.q_xor, x[i].y = (x[i].y & ta.q_and) ^ ta.q_xor;
+        x[i].z = (x[i].z & ta.q_and) ^ ta.q_xor, x[i].w = (x[i].w & ta.q_and) ^ ta.q_xor;
+        asm volatile("st.shared.v4.u32 [%0], {%1, %2, %3, %4};" ::"r"(dst + (i >> 3) * C::kPanel + (((i & 7) ^ (r & 7)) << 4)),
+                     "r"(x[i].x), "r"(x[i].y), "r"(x[i].z), "r"(x[i].w) : "memory");
+      }
+      fence_proxy_async_smem();
+    }
+    __syncwarp();
+    if (lane == 0) mbar_arrive(bar_q);
+
+    const int p = p_base + tok;
+    const int see_to = min(p, rg.hi - 1);                           // last key of the row
+    const int see_from = a.window > 0 ? p - a.window : -1;          // keys above it
+    const int all_to = min(p_base + q_tile * tpt + 1, rg.hi);       // every row of the tile sees [all_from, all_to)
+    const int all_from = a.window > 0 ? p_base + toks - a.window : 0;
+    const int mine = two ? n_tiles : (n_tiles - acc + 1) >> 1;
+    const float sc = a.scale_log2;
+    float m = -INFINITY, l = 0.0f;   // m: the reference that is subtracted, in powers of two
+
+    bool ok = true;
+    for (int i = 0; i < mine; ++i) {
+      const int key0 = key_base + (two ? i : 2 * i + acc) * kTile;
+      if (!(ok = warp_wait(bar_s + 8 * acc, i & 1, wc))) break;
+      tc_fence_after_sync();
+      uint32_t s[4][32];
+#pragma unroll
+      for (int h = 0; h < 4; ++h) tmem_ld_32x32(t_s[acc] + lane_off + 32 * h, s[h]);
+      tmem_ld_wait();
+      if (key0 < all_from || key0 + kTile > all_to) {
+        const int to = see_to - key0, from = see_from - key0;
+#pragma unroll
+        for (int h = 0; h < 4; ++h) {
+#pragma unroll
+          for (int j = 0; j < 32; ++j)
+            if (32 * h + j > to || 32 * h + j <= from) s[h][j] = 0xff800000u;   // -inf
+        }
+      }
+      float top[4];
+#pragma unroll
+      for (int h = 0; h < 4; ++h) {
+        top[h] = __uint_as_float(s[h][0]);
+#pragma unroll
+        for (int j = 1; j < 32; ++j) top[h] = fmaxf(top[h], __uint_as_float(s[h][j]));
+      }
+      const float t = fmaxf(fmaxf(top[0], top[1]), fmaxf(top[2], top[3])) * sc;
+      const bool grown = t > m + 8.0f;
+      if (__any_sync(0xffffffffu, grown)) {
+        const float f = grown ? (m == -INFINITY ? 0.0f : exp2_approx(m - t)) : 1.0f;
+        if (grown) m = t;
+        l *= f;
+        if (i > 0) {   // O holds the sums up to the tile before
+          if (!(ok = warp_wait(bar_o + 8 * acc, (i - 1) & 1, wc))) break;
+          tc_fence_after_sync();
+#pragma unroll 1
+          for (int h = 0; h < D / 32; ++h) {
+            uint32_t o[32];
+            tmem_ld_32x32(t_o[acc] + lane_off + 32 * h, o);
+            tmem_ld_wait();
+#pragma unroll
+            for (int j = 0; j < 32; ++j) o[j] = __float_as_uint(__uint_as_float(o[j]) * f);
+            tmem_st_32x32(t_o[acc] + lane_off + 32 * h, o);
+          }
+        }
+      }
+      const float ms = m == -INFINITY ? 0.0f : m;
+      float sum[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        uint32_t w[32];
+#pragma unroll
+        for (int j = 0; j < 32; ++j) {
+          const float e0 = exp2_approx(fmaf(__uint_as_float(s[2 * h + (j >> 4)][(2 * j) & 31]), sc, -ms));
+          const float e1 = exp2_approx(fmaf(__uint_as_float(s[2 * h + (j >> 4)][(2 * j + 1) & 31]), sc, -ms));
+          sum[j & 1] += e0;
+          sum[2 + (j & 1)] += e1;
+          w[j] = pack_f16(e0, e1);
+        }
+        tmem_st_32x32(t_s[acc] + lane_off + 32 * h, w);
+      }
+      l += (sum[0] + sum[1]) + (sum[2] + sum[3]);
+      tmem_st_wait();
+      tc_fence_before_sync();
+      __syncwarp();
+      if (lane == 0) mbar_arrive(bar_p + 8 * acc);
+    }
+    if (ok && mine > 0) warp_wait(bar_o + 8 * acc, (mine - 1) & 1, wc);
+    tc_fence_after_sync();
+
+    // -------------------------------------------------------------------- epilogue
+    // Accumulators of the even and the odd tiles are joined in the first one's threads.
+    float f0 = 1.0f, f1 = 0.0f;
+    const bool join = !two && n_tiles > 1;
+    float4* room = reinterpret_cast<float4*>(smem_raw + (ring - smem_u32(smem_raw)));   // [D / 4][128 rows]
+    float2* room_ml = reinterpret_cast<float2*>(smem_raw + (sq - smem_u32(smem_raw)));
+    if (join) {
+      named_bar_sync(1, 256);   // every MMA has completed: the operand tiles are free
+      if (acc == 1) {
+#pragma unroll 1
+        for (int h = 0; h < D / 32; ++h) {
+          uint32_t o[32];
+          tmem_ld_32x32(t_o[1] + lane_off + 32 * h, o);
+          tmem_ld_wait();
+#pragma unroll
+          for (int j = 0; j < 8; ++j)
+            room[(8 * h + j) * kTile + r] = make_float4(__uint_as_float(o[4 * j]), __uint_as_float(o[4 * j + 1]),
+                                                        __uint_as_float(o[4 * j + 2]), __uint_as_float(o[4 * j + 3]));
+        }
+        room_ml[r] = make_float2(m, l);
+      }
+      named_bar_sync(1, 256);
+      if (acc == 0) {
+        const float2 ml = room_ml[r];
+        const float M = fmaxf(m, ml.x), Ms = M == -INFINITY ? 0.0f : M;
+        f0 = exp2_approx(m - Ms), f1 = exp2_approx(ml.x - Ms);
+        l = l * f0 + ml.y * f1;
+        m = M;
+      }
+    }
+    const bool writes = two || acc == 0;
+    const int64_t unit = blockIdx.x;
+    constexpr int kPart = 2 * kTile * (D + 2);   // floats of one part: per tile [D / 4][128] x 4, then [128] x 2
+    float* pu = a.partials + unit * gridDim.y * kPart;
+    const float inv = l > 0.0f ? 1.0f / l : 0.0f;
+    if (writes) {
+      float* pp = pu + part * kPart + q_tile * kTile * (D + 2);
+#pragma unroll 1
+      for (int h = 0; h < D / 32; ++h) {
+        uint32_t o[32];
+        if (n_tiles > 0) {
+          tmem_ld_32x32(t_o[acc] + lane_off + 32 * h, o);
+          tmem_ld_wait();
+        }
+        float v[32];
+#pragma unroll
+        for (int j = 0; j < 32; ++j) v[j] = n_tiles > 0 ? __uint_as_float(o[j]) * f0 : 0.0f;
+        if (join) {
+#pragma unroll
+          for (int j = 0; j < 8; ++j) {
+            const float4 x = room[(8 * h + j) * kTile + r];
+            v[4 * j] = fmaf(x.x, f1, v[4 * j]), v[4 * j + 1] = fmaf(x.y, f1, v[4 * j + 1]);
+            v[4 * j + 2] = fmaf(x.z, f1, v[4 * j + 2]), v[4 * j + 3] = fmaf(x.w, f1, v[4 * j + 3]);
+          }
+        }
+        if (parts > 1) {
+#pragma unroll
+          for (int j = 0; j < 8; ++j)
+            reinterpret_cast<float4*>(pp)[(8 * h + j) * kTile + r] = make_float4(v[4 * j], v[4 * j + 1], v[4 * j + 2], v[4 * j + 3]);
+        } else if (live) {
+          uint4* dst = reinterpret_cast<uint4*>(a.out + out_row * D + 32 * h);
+#pragma unroll
+          for (int j = 0; j < 4; ++j)
+            dst[j] = make_uint4(pack_f16(v[8 * j] * inv, v[8 * j + 1] * inv), pack_f16(v[8 * j + 2] * inv, v[8 * j + 3] * inv),
+                                pack_f16(v[8 * j + 4] * inv, v[8 * j + 5] * inv), pack_f16(v[8 * j + 6] * inv, v[8 * j + 7] * inv));
+        }
+      }
+      if (parts > 1) reinterpret_cast<float2*>(pp + kTile * D)[r] = make_float2(m, l);
+    }
+    if (parts > 1) {
+      // The CTA that arrives last joins the parts, in their order.
+      __threadfence();
+      named_bar_sync(1, 256);
+      if (tid == 0) {
+        const unsigned int before = atomicAdd(a.counters + unit, 1u);
+        s_last = before == static_cast<unsigned int>(parts) - 1u;
+        if (s_last) a.counters[unit] = 0u;
+      }
+      named_bar_sync(1, 256);
+      if (s_last && writes && live) {
+        __threadfence();
+        const float* p0 = pu + q_tile * kTile * (D + 2);
+        float M = -INFINITY, L = 0.0f;
+        for (int q = 0; q < parts; ++q) M = fmaxf(M, __ldcg(reinterpret_cast<const float2*>(p0 + static_cast<int64_t>(q) * kPart + kTile * D) + r).x);
+        const float Ms = M == -INFINITY ? 0.0f : M;
+        for (int q = 0; q < parts; ++q) {
+          const float2 ml = __ldcg(reinterpret_cast<const float2*>(p0 + static_cast<int64_t>(q) * kPart + kTile * D) + r);
+          L = fmaf(ml.y, exp2_approx(ml.x - Ms), L);
+        }
+        const float Li = L > 0.0f ? 1.0f / L : 0.0f;
+#pragma unroll 1
+        for (int h = 0; h < D / 32; ++h) {
+          float4 v[8];
+#pragma unroll
+          for (int j = 0; j < 8; ++j) v[j] = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+          for (int q = 0; q < parts; ++q) {
+            const float* pq_ = p0 + static_cast<int64_t>(q) * kPart;
+            const float f = exp2_approx(__ldcg(reinterpret_cast<const float2*>(pq_ + kTile * D) + r).x - Ms) * Li;
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+              const float4 x = __ldcg(reinterpret_cast<const float4*>(pq_) + (8 * h + j) * kTile + r);
+              v[j].x = fmaf(x.x, f, v[j].x), v[j].y = fmaf(x.y, f, v[j].y), v[j].z = fmaf(x.z, f, v[j].z), v[j].w = fmaf(x.w, f, v[j].w);
+            }
+          }
+          uint4* dst = reinterpret_cast<uint4*>(a.out + out_row * D + 32 * h);
+#pragma unroll
+          for (int j = 0; j < 4; ++j)
+            dst[j] = make_uint4(pack_f16(v[2 * j].x, v[2 * j].y), pack_f16(v[2 * j].z, v[2 * j].w),
+                                pack_f16(v[2 * j + 1].x, v[2 * j + 1].y), pack_f16(v[2 * j + 1].z, v[2 * j + 1].w));
+        }
+      }
+    }
+  }
+
+  // ---------------------------------------------------------------------- teardown
+  __syncwarp();
+  tc_fence_before_sync();
+  __syncthreads();
+  if (s_abort) {
+    // Some role gave up.  What has been handed to the hardware still completes by itself and must have done so
+    // before shared and tensor memory go away: the producer's loads and the issuer's MMAs.
+    if (tid == 9 * 32) {
+      const int first = issued > C::kStages ? issued - C::kStages : 0;
+      for (int i = first; i < issued; ++i) mbar_drain(bar_full + 8 * (i % C::kStages), (i / C::kStages) & 1u);
+      mbar_drain(bar_fix, 0u);
+    } else if (tid == 8 * 32) {
+      umma_commit(bar_drain);
+      mbar_drain(bar_drain, 0u);
+    }
+    __syncthreads();
+    if (tid == 0) atomicExch(ta.status, static_cast<int>(PQ_ERR_TIMEOUT));
+  }
+  tc_fence_after_sync();
+  if (warp == 8) {
+    tmem_relinquish();
+    tmem_dealloc(tmem, 512);
+  }
+}
+
+template <int D>
+int launch(TileArgs& t, const TilePlan& plan, cudaStream_t stream) {
+  using C = TileCfg<D>;
+  auto kern = attn_tile_kernel<D>;
+  static PerDeviceOnce once;
+  if (const int rc = set_dynamic_smem_once(once, kern, C::kSmem); rc != PQ_OK) return rc;
+  // The kernel's register split draws on what the launch holds: a build whose launch holds less must not run.
+  static const int regs = [] {
+    cudaFuncAttributes f = {};
+    return cudaFuncGetAttributes(&f, attn_tile_kernel<D>) == cudaSuccess ? f.numRegs : 0;
+  }();
+  if (regs * kThreads < 256 * kSoftRegs + 128 * kRestRegs) return PQ_ERR_CUDA;
+  CUtensorMap mk, mv;
+  const pq_kv_cache& c = t.a.c;
+  const uint64_t rows = static_cast<uint64_t>(c.pages) * c.heads * c.page;
+  if (const int rc = make_tmap_2d(&mk, c.k, rows, D, t.box, 64, 2, 128); rc != PQ_OK) return rc;
+  if (const int rc = make_tmap_2d(&mv, c.v, rows, D, t.box, 64, 2, 128); rc != PQ_OK) return rc;
+  const dim3 grid(static_cast<unsigned>(plan.units), static_cast<unsigned>(plan.parts));
+  return launch_dependent(kern, grid, dim3(kThreads), C::kSmem, stream, mk, mv, t);
+}
+
+}  // namespace
+
+// Fewer units than SMs: the keys of each are cut into parts, of 512 keys at least.
+TilePlan plan_attn_tile(int64_t requests, int64_t tokens, int64_t max_q, int64_t max_kv, int group, int kv_heads, int dim,
+                        int sms, size_t room) {
+  TilePlan p;
+  const int64_t qt = 2 * (kTile / group);
+  const int64_t by_rows = tokens / qt + requests, by_request = requests * ((max_q + qt - 1) / qt);
+  p.units = (by_rows < by_request ? by_rows : by_request) * kv_heads;
+  int64_t parts = 1, keys = (max_kv + kTile - 1) / kTile * kTile;
+  if (p.units < sms && p.units <= kScratchCounters) {
+    parts = sms / p.units;
+    keys = (max_kv + parts - 1) / parts;
+    keys = keys < 512 ? 512 : (keys + kTile - 1) / kTile * kTile;
+    parts = (max_kv + kTile + keys - 1) / keys;   // the first part begins at a multiple of 128 before the window
+    if (parts > 65535) parts = 65535;
+  }
+  const size_t one = static_cast<size_t>(2 * kTile) * (dim + 2) * 4;
+  if (parts > 1 && static_cast<size_t>(p.units) * parts * one > room) {
+    const int64_t fit = static_cast<int64_t>(room / (static_cast<size_t>(p.units) * one));
+    parts = fit < 2 ? 1 : fit;
+    keys = ((max_kv + parts - 1) / parts + kTile - 1) / kTile * kTile;
+  }
+  if (keys > (1 << 30)) keys = 1 << 30;
+  p.parts = static_cast<int>(parts);
+  p.part_keys = static_cast<int>(keys < kTile ? kTile : keys);
+  p.partial_bytes = parts > 1 ? static_cast<size_t>(p.units) * parts * one : 0;
+  return p;
+}
+
+int launch_attn_tile(const AttnArgs& a, const TilePlan& plan, cudaStream_t stream) {
+  if (plan.units < 1) return PQ_OK;
+  if (plan.units > 0x7fffffff) return PQ_ERR_SHAPE;
+  TileArgs t{a, device_status_ptr(), wait_limit(), 128, 0xffffffffu, 0u};
+  if (t.status == nullptr) return PQ_ERR_CUDA;
+  while (a.c.page % t.box != 0) t.box /= 2;   // the page is a multiple of 16
+  t.a.part_keys = plan.part_keys;
+  if (a.scale_log2 == 0.0f) {
+    t.q_and = 0u;
+    t.a.scale_log2 = 1.0f;
+  } else if (a.scale_log2 < 0.0f) {
+    t.q_xor = 0x80008000u;
+    t.a.scale_log2 = -a.scale_log2;
+  }
+  return a.c.dim == 128 ? launch<128>(t, plan, stream) : launch<64>(t, plan, stream);
+}
+
+}  // namespace pq
