@@ -10,15 +10,17 @@ namespace pq {
 namespace {
 
 constexpr int kTile = 128;          // query rows of one accumulator, keys of one step
-constexpr int kThreads = 384;       // two softmax warpgroups; MMA issuer, producer and two idle warps
+constexpr int kThreads = 384;       // two softmax warpgroups; MMA issuer, producer, watcher and an idle warp
 constexpr int kSoftRegs = 216, kRestRegs = 72;   // 2 x 128 x 216 + 128 x 72 = 384 x 168, what the launch holds
+
+constexpr int kPolyEvery = 4;       // every 4th pair of weights on the FMA pipe instead of the special-function unit
 
 template <int D>
 struct TileCfg {
   static constexpr int kTileBytes = kTile * D * 2;            // one operand tile: D / 64 panels of 128 rows x 128 B
   static constexpr int kPanel = kTile * 128;
   static constexpr int kStages = 163840 / kTileBytes;         // 5 (D = 128) or 10: keys and values alternate
-  static constexpr int kBars = 2 * kStages + 9;
+  static constexpr int kBars = 2 * kStages + 7;
   static constexpr int kSmem = 2 * kTileBytes + kStages * kTileBytes + 1024 /* alignment */;
 };
 
@@ -27,25 +29,26 @@ struct TileCfg {
 __host__ __device__ constexpr uint32_t umma_idesc_f16(uint32_t N, bool b_mn) {
   return (1u << 4) | (b_mn ? (1u << 16) : 0u) | ((N >> 3) << 17) | ((128u >> 4) << 24);
 }
-__device__ __forceinline__ void umma_f16_ss(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, uint32_t acc) {
-  asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\ttcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n\t}"
-               ::"r"(d), "l"(a), "l"(b), "r"(idesc), "r"(acc) : "memory");
+// Shared-memory operand descriptors, low word: start address in 16-byte units and the leading byte offset.  The high
+// word is the same for both kinds: groups of 8 rows of 128 bytes lie 1024 bytes apart, 128-byte swizzle.
+//   K-major (Q, K):   64 features per 128-byte row; a k step of 16 is 32 bytes further.
+//   MN-major (V):     panels of 64 columns, `panel` bytes apart; a k step of 16 keys is 2048 bytes further.
+constexpr uint32_t kDescHi = (1024u >> 4) | (1u << 14) | (2u << 29);
+__device__ __forceinline__ uint32_t desc_k(uint32_t saddr) { return ((saddr & 0x3FFFFu) >> 4) | (1u << 16); }
+__device__ __forceinline__ uint32_t desc_mn(uint32_t saddr, uint32_t panel) { return ((saddr & 0x3FFFFu) >> 4) | ((panel >> 4) << 16); }
+// One MMA of 128 x N x 16.  Operands stay in uniform registers (the whole warp computes them, one elected thread
+// issues): with per-thread operands an issue took 93 to 120 cycles against the 64 that the tensor core needs.
+template <int kAccumulate>
+__device__ __forceinline__ void umma_f16_ss(uint32_t d, uint32_t a_lo, uint32_t b_lo, uint32_t idesc) {
+  asm volatile("{\n\t.reg .pred p;\n\t.reg .b64 a, b;\n\tsetp.ne.b32 p, %4, 0;\n\tmov.b64 a, {%1, %5};\n\tmov.b64 b, {%2, %5};\n\t"
+               "tcgen05.mma.cta_group::1.kind::f16 [%0], a, b, %3, p;\n\t}"
+               ::"r"(d), "r"(a_lo), "r"(b_lo), "r"(idesc), "n"(kAccumulate), "n"(kDescHi) : "memory");
 }
 // A in tensor memory: lane = row, a 32-bit column holds two neighbouring k.
-__device__ __forceinline__ void umma_f16_ts(uint32_t d, uint32_t a, uint64_t b, uint32_t idesc, uint32_t acc) {
-  asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\ttcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}"
-               ::"r"(d), "r"(a), "l"(b), "r"(idesc), "r"(acc) : "memory");
-}
-// B operand whose N dimension is contiguous, 128-byte swizzle: panels of 64 columns (`panel` bytes apart), inside
-// a panel groups of 8 k-rows of 128 bytes, 1024 bytes apart.
-__device__ __forceinline__ uint64_t umma_desc_mn_sw128(uint32_t saddr, uint32_t panel) {
-  uint64_t d = 0;
-  d |= static_cast<uint64_t>((saddr & 0x3FFFFu) >> 4);
-  d |= static_cast<uint64_t>(panel >> 4) << 16;
-  d |= static_cast<uint64_t>(1024 >> 4) << 32;
-  d |= static_cast<uint64_t>(1) << 46;
-  d |= static_cast<uint64_t>(2) << 61;
-  return d;
+__device__ __forceinline__ void umma_f16_ts(uint32_t d, uint32_t a, uint32_t b_lo, uint32_t idesc, uint32_t accumulate) {
+  asm volatile("{\n\t.reg .pred p;\n\t.reg .b64 b;\n\tsetp.ne.b32 p, %4, 0;\n\tmov.b64 b, {%2, %5};\n\t"
+               "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], b, %3, p;\n\t}"
+               ::"r"(d), "r"(a), "r"(b_lo), "r"(idesc), "r"(accumulate), "n"(kDescHi) : "memory");
 }
 __device__ __forceinline__ void tmem_st_32x32(uint32_t taddr, const uint32_t (&r)[32]) {
   asm volatile(
@@ -63,6 +66,57 @@ __device__ __forceinline__ void tmem_st_wait() { asm volatile("tcgen05.wait::st.
 __device__ __forceinline__ uint32_t pack_f16(float a, float b) {
   const __half2 h = __floats2half2_rn(a, b);
   return *reinterpret_cast<const uint32_t*>(&h);
+}
+
+__device__ __forceinline__ void named_bar_arrive(uint32_t id, uint32_t nthreads) {
+  asm volatile("bar.arrive %0, %1;" ::"r"(id), "r"(nthreads) : "memory");
+}
+// Named barriers (0 is __syncthreads): the softmax warpgroups among themselves; "P written", one per accumulator
+// (128 threads arrive, the issuer's warp waits); "operand tile landed", between the watcher's and the issuer's warp.
+// They do not pass through shared memory, which the tensor core keeps busy: a wait on an mbarrier that has long
+// completed takes 200 to 400 cycles here, one on a named barrier about 30.
+constexpr uint32_t kBarSoft = 1, kBarP = 2, kBarTile = 4;
+
+// Two FP32 operations in one instruction.
+__device__ __forceinline__ uint64_t pair_f32(float a, float b) {
+  uint64_t r;
+  asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(a), "f"(b));
+  return r;
+}
+__device__ __forceinline__ void unpair_f32(uint64_t v, float& a, float& b) { asm("mov.b64 {%0, %1}, %2;" : "=f"(a), "=f"(b) : "l"(v)); }
+__device__ __forceinline__ uint64_t fma_f32x2(uint64_t a, uint64_t b, uint64_t c) {
+  uint64_t d;
+  asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(d) : "l"(a), "l"(b), "l"(c));
+  return d;
+}
+__device__ __forceinline__ uint64_t add_f32x2(uint64_t a, uint64_t b) {
+  uint64_t d;
+  asm("add.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b));
+  return d;
+}
+__device__ __forceinline__ float max3(float a, float b, float c) {
+  float d;
+  asm("max.f32 %0, %1, %2, %3;" : "=f"(d) : "f"(a), "f"(b), "f"(c));
+  return d;
+}
+// 2^x for x <= 9 on the FMA pipe, two at a time: x = n + f with n = rne(x) (taken as (x + 1.5 * 2^23) - 1.5 * 2^23,
+// whose low mantissa bits are n), 2^f by a degree-4 polynomial, and n added to the exponent.  Coefficients: least
+// squares of the relative error over [-1/2, 1/2], reweighted towards its largest values (2.6e-6, against 2.4e-4 for
+// the FP16 rounding that follows).  Below 2^-125 the result is 2^-125, which rounds to 0 in FP16.
+__device__ __forceinline__ uint64_t exp2_poly2(uint64_t x) {
+  float x0, x1;
+  unpair_f32(x, x0, x1);
+  x = pair_f32(fmaxf(x0, -125.0f), fmaxf(x1, -125.0f));
+  const uint64_t t = add_f32x2(x, pair_f32(12582912.0f, 12582912.0f));
+  const uint64_t f = fma_f32x2(add_f32x2(t, pair_f32(-12582912.0f, -12582912.0f)), pair_f32(-1.0f, -1.0f), x);
+  uint64_t p = fma_f32x2(pair_f32(0.009570102207362652f, 0.009570102207362652f), f, pair_f32(0.05591785907745361f, 0.05591785907745361f));
+  p = fma_f32x2(p, f, pair_f32(0.240247443318367f, 0.240247443318367f));
+  p = fma_f32x2(p, f, pair_f32(0.6931217908859253f, 0.6931217908859253f));
+  p = fma_f32x2(p, f, pair_f32(0.9999992847442627f, 0.9999992847442627f));
+  float p0, p1, t0, t1;
+  unpair_f32(p, p0, p1);
+  unpair_f32(t, t0, t1);
+  return pair_f32(__int_as_float(__float_as_int(p0) + (__float_as_int(t0) << 23)), __int_as_float(__float_as_int(p1) + (__float_as_int(t1) << 23)));
 }
 
 // A wait of a whole warp whose lanes go on, or give up, together.
@@ -109,7 +163,7 @@ attn_tile_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constan
   __shared__ int s_last;
 
   const AttnArgs& a = ta.a;
-  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+  const int tid = threadIdx.x, warp = __shfl_sync(0xffffffffu, tid >> 5, 0), lane = tid & 31;
   const int G = a.heads / a.c.heads;
   const int tpt = kTile / G;          // tokens of one accumulator
   const int qt = 2 * tpt;             // tokens of one CTA
@@ -117,11 +171,11 @@ attn_tile_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constan
 
   const uint32_t bar0 = smem_u32(bars);
   const uint32_t bar_full = bar0, bar_free = bar0 + 8 * C::kStages;
-  const uint32_t bar_s = bar0 + 16 * C::kStages, bar_p = bar_s + 16, bar_o = bar_p + 16;   // two of each
+  const uint32_t bar_s = bar0 + 16 * C::kStages, bar_o = bar_s + 16;   // two of each
   const uint32_t bar_q = bar_o + 16, bar_fix = bar_q + 8, bar_drain = bar_fix + 8;
   if (tid == 0) {
     for (int i = 0; i < C::kStages; ++i) mbar_init(bar_full + 8 * i, 1), mbar_init(bar_free + 8 * i, 1);
-    for (int i = 0; i < 2; ++i) mbar_init(bar_s + 8 * i, 1), mbar_init(bar_p + 8 * i, 4), mbar_init(bar_o + 8 * i, 1);
+    for (int i = 0; i < 2; ++i) mbar_init(bar_s + 8 * i, 1), mbar_init(bar_o + 8 * i, 1);
     mbar_init(bar_q, 8);
     mbar_init(bar_fix, 1);
     mbar_init(bar_drain, 1);
@@ -191,7 +245,7 @@ attn_tile_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constan
   __syncthreads();
   tc_fence_after_sync();
   grid_dep_launch();   // only now: a later launch's CTA may take this SM's tensor memory when it is given back
-  const uint32_t tmem = s_tmem;
+  const uint32_t tmem = __shfl_sync(0xffffffffu, s_tmem, 0);
   const uint32_t t_s[2] = {tmem, tmem + 128}, t_o[2] = {tmem + 256, tmem + 256 + D};
   const WaitCtx wc{&s_abort, ta.wait_limit};
   int issued = 0;   // producer: loads requested so far
@@ -242,38 +296,58 @@ attn_tile_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constan
         }
         __syncwarp();
       }
-    } else if (warp == 8 && lane == 0) {
+    } else if (warp == 8) {
       // ------------------------------------------------------------------ MMA issuer
+      // The whole warp walks the steps, so that every operand is uniform; one elected thread issues.  After a role has
+      // given up the steps go on (the barriers stay in step), on whatever the tiles hold.
       constexpr uint32_t id_qk = umma_idesc_f16(kTile, false), id_pv = umma_idesc_f16(D, true);
-      bool ok = mbar_wait(bar_q, 0, wc);
-      tc_fence_after_sync();
-      for (int u = 0; ok && u <= N; ++u) {
+      constexpr uint32_t kStageUnits = C::kTileBytes / 16;
+      const uint32_t leader = elect_one();
+      const uint32_t q_lo = desc_k(sq), k_lo0 = desc_k(ring), v_lo0 = desc_mn(ring, C::kPanel);
+      const uint32_t q_step = two ? kStageUnits : 0;
+      warp_wait(bar_q, 0, wc);
+      for (int u = 0; u <= N; ++u) {
         if (u < N) {   // S(u) = Q K^T
-          const int acc = u & 1, kt = two ? u >> 1 : u;
-          const int i = 2 * kt, st = i % C::kStages;
-          if (!(ok = mbar_wait(bar_full + 8 * st, (i / C::kStages) & 1, wc))) break;
+          const int acc = u & 1, st = (2 * (two ? u >> 1 : u)) % C::kStages;
+          if (!two || acc == 0) named_bar_sync(kBarTile, 64);
           tc_fence_after_sync();
-          const uint32_t qs = sq + (two ? acc * C::kTileBytes : 0), ks = ring + st * C::kTileBytes;
+          if (leader) {
+            const uint32_t ql = q_lo + acc * q_step, kl = k_lo0 + st * kStageUnits, d = tmem + acc * 128;
+            umma_f16_ss<0>(d, ql, kl, id_qk);
 #pragma unroll
-          for (int k = 0; k < KS; ++k) {
-            const uint32_t off = (k / 4) * C::kPanel + (k % 4) * 32;
-            umma_f16_ss(t_s[acc], umma_desc_k_sw128(qs + off), umma_desc_k_sw128(ks + off), id_qk, k > 0);
+            for (int k = 1; k < KS; ++k) umma_f16_ss<1>(d, ql + (k / 4) * (C::kPanel / 16) + (k % 4) * 2, kl + (k / 4) * (C::kPanel / 16) + (k % 4) * 2, id_qk);
+            umma_commit(bar_s + 8 * acc);
+            if (!two || acc == 1) umma_commit(bar_free + 8 * st);
           }
-          umma_commit(bar_s + 8 * acc);
-          if (!two || acc == 1) umma_commit(bar_free + 8 * st);
+          __syncwarp();
         }
         if (u > 0) {   // O(u - 1) += P V
-          const int v = u - 1, acc = v & 1, kt = two ? v >> 1 : v;
-          const int i = 2 * kt + 1, st = i % C::kStages;
-          if (!(ok = mbar_wait(bar_full + 8 * st, (i / C::kStages) & 1, wc))) break;
-          if (!(ok = mbar_wait(bar_p + 8 * acc, (v >> 1) & 1, wc))) break;
+          const int v = u - 1, acc = v & 1, st = (2 * (two ? v >> 1 : v) + 1) % C::kStages;
+          if (!two || acc == 0) named_bar_sync(kBarTile, 64);
+          named_bar_sync(kBarP + acc, 160);
           tc_fence_after_sync();
-          const uint32_t vs = ring + st * C::kTileBytes;
+          if (leader) {
+            const uint32_t vl = v_lo0 + st * kStageUnits, d = tmem + 256 + acc * D, p = tmem + acc * 128;
+            umma_f16_ts(d, p, vl, id_pv, (v >> 1) > 0);
 #pragma unroll
-          for (int k = 0; k < PS; ++k)
-            umma_f16_ts(t_o[acc], t_s[acc] + 8 * k, umma_desc_mn_sw128(vs + k * 2048, C::kPanel), id_pv, (v >> 1) > 0 || k > 0);
-          umma_commit(bar_o + 8 * acc);
-          if (!two || acc == 1) umma_commit(bar_free + 8 * st);
+            for (int k = 1; k < PS; ++k) umma_f16_ts(d, p + 8 * k, vl + k * 128, id_pv, 1u);
+            umma_commit(bar_o + 8 * acc);
+            if (!two || acc == 1) umma_commit(bar_free + 8 * st);
+          }
+          __syncwarp();
+        }
+      }
+    } else if (warp == 10) {
+      // ------------------------------------------------------------------ watcher: waits for the operand tiles a step ahead
+      bool ok = true;
+      for (int u = 0; u <= N; ++u) {
+#pragma unroll
+        for (int is_v = 0; is_v < 2; ++is_v) {
+          const int w = u - is_v;
+          if (w < 0 || w >= N || (two && (w & 1))) continue;
+          const int i = 2 * (two ? w >> 1 : w) + is_v;
+          ok = ok && warp_wait(bar_full + 8 * (i % C::kStages), (i / C::kStages) & 1, wc);
+          named_bar_sync(kBarTile, 64);
         }
       }
     }
@@ -318,7 +392,7 @@ attn_tile_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constan
     bool ok = true;
     for (int i = 0; i < mine; ++i) {
       const int key0 = key_base + (two ? i : 2 * i + acc) * kTile;
-      if (!(ok = warp_wait(bar_s + 8 * acc, i & 1, wc))) break;
+      ok = ok && warp_wait(bar_s + 8 * acc, i & 1, wc);
       tc_fence_after_sync();
       uint32_t s[4][32];
 #pragma unroll
@@ -336,18 +410,20 @@ attn_tile_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constan
       float top[4];
 #pragma unroll
       for (int h = 0; h < 4; ++h) {
-        top[h] = __uint_as_float(s[h][0]);
+        top[h] = max3(__uint_as_float(s[h][0]), __uint_as_float(s[h][1]), __uint_as_float(s[h][2]));
 #pragma unroll
-        for (int j = 1; j < 32; ++j) top[h] = fmaxf(top[h], __uint_as_float(s[h][j]));
+        for (int j = 3; j < 31; j += 2) top[h] = max3(top[h], __uint_as_float(s[h][j]), __uint_as_float(s[h][j + 1]));
       }
-      const float t = fmaxf(fmaxf(top[0], top[1]), fmaxf(top[2], top[3])) * sc;
+      top[0] = max3(top[0], __uint_as_float(s[0][31]), top[1]);
+      top[2] = max3(top[2], __uint_as_float(s[1][31]), top[3]);
+      const float t = max3(fmaxf(top[0], top[2]), __uint_as_float(s[2][31]), __uint_as_float(s[3][31])) * sc;
       const bool grown = t > m + 8.0f;
       if (__any_sync(0xffffffffu, grown)) {
         const float f = grown ? (m == -INFINITY ? 0.0f : exp2_approx(m - t)) : 1.0f;
         if (grown) m = t;
         l *= f;
         if (i > 0) {   // O holds the sums up to the tile before
-          if (!(ok = warp_wait(bar_o + 8 * acc, (i - 1) & 1, wc))) break;
+          ok = ok && warp_wait(bar_o + 8 * acc, (i - 1) & 1, wc);
           tc_fence_after_sync();
 #pragma unroll 1
           for (int h = 0; h < D / 32; ++h) {
@@ -361,25 +437,36 @@ attn_tile_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constan
         }
       }
       const float ms = m == -INFINITY ? 0.0f : m;
-      float sum[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+      const uint64_t sc2 = pair_f32(sc, sc), ms2 = pair_f32(-ms, -ms);
+      uint64_t sum[2] = {0, 0};
 #pragma unroll
       for (int h = 0; h < 2; ++h) {
         uint32_t w[32];
 #pragma unroll
         for (int j = 0; j < 32; ++j) {
-          const float e0 = exp2_approx(fmaf(__uint_as_float(s[2 * h + (j >> 4)][(2 * j) & 31]), sc, -ms));
-          const float e1 = exp2_approx(fmaf(__uint_as_float(s[2 * h + (j >> 4)][(2 * j + 1) & 31]), sc, -ms));
-          sum[j & 1] += e0;
-          sum[2 + (j & 1)] += e1;
+          const int q = 2 * h + (j >> 4), e = (2 * j) & 31;
+          uint64_t x = fma_f32x2(pair_f32(__uint_as_float(s[q][e]), __uint_as_float(s[q][e + 1])), sc2, ms2);
+          float e0, e1;
+          if (j % kPolyEvery == kPolyEvery - 1) {
+            x = exp2_poly2(x);
+            unpair_f32(x, e0, e1);
+          } else {
+            unpair_f32(x, e0, e1);
+            e0 = exp2_approx(e0);
+            e1 = exp2_approx(e1);
+            x = pair_f32(e0, e1);
+          }
+          sum[j & 1] = add_f32x2(sum[j & 1], x);
           w[j] = pack_f16(e0, e1);
         }
         tmem_st_32x32(t_s[acc] + lane_off + 32 * h, w);
       }
-      l += (sum[0] + sum[1]) + (sum[2] + sum[3]);
+      float l0, l1;
+      unpair_f32(add_f32x2(sum[0], sum[1]), l0, l1);
+      l += l0 + l1;
       tmem_st_wait();
       tc_fence_before_sync();
-      __syncwarp();
-      if (lane == 0) mbar_arrive(bar_p + 8 * acc);
+      named_bar_arrive(kBarP + acc, 160);
     }
     if (ok && mine > 0) warp_wait(bar_o + 8 * acc, (mine - 1) & 1, wc);
     tc_fence_after_sync();
@@ -391,7 +478,7 @@ attn_tile_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constan
     float4* room = reinterpret_cast<float4*>(smem_raw + (ring - smem_u32(smem_raw)));   // [D / 4][128 rows]
     float2* room_ml = reinterpret_cast<float2*>(smem_raw + (sq - smem_u32(smem_raw)));
     if (join) {
-      named_bar_sync(1, 256);   // every MMA has completed: the operand tiles are free
+      named_bar_sync(kBarSoft, 256);   // every MMA has completed: the operand tiles are free
       if (acc == 1) {
 #pragma unroll 1
         for (int h = 0; h < D / 32; ++h) {
@@ -405,7 +492,7 @@ attn_tile_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constan
         }
         room_ml[r] = make_float2(m, l);
       }
-      named_bar_sync(1, 256);
+      named_bar_sync(kBarSoft, 256);
       if (acc == 0) {
         const float2 ml = room_ml[r];
         const float M = fmaxf(m, ml.x), Ms = M == -INFINITY ? 0.0f : M;
@@ -456,13 +543,13 @@ attn_tile_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constan
     if (parts > 1) {
       // The CTA that arrives last joins the parts, in their order.
       __threadfence();
-      named_bar_sync(1, 256);
+      named_bar_sync(kBarSoft, 256);
       if (tid == 0) {
         const unsigned int before = atomicAdd(a.counters + unit, 1u);
         s_last = before == static_cast<unsigned int>(parts) - 1u;
         if (s_last) a.counters[unit] = 0u;
       }
-      named_bar_sync(1, 256);
+      named_bar_sync(kBarSoft, 256);
       if (s_last && writes && live) {
         __threadfence();
         const float* p0 = pu + q_tile * kTile * (D + 2);
