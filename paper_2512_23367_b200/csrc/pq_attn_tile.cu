@@ -10,8 +10,10 @@ namespace pq {
 namespace {
 
 constexpr int kTile = 128;          // query rows of one accumulator, keys of one step
-constexpr int kThreads = 384;       // two softmax warpgroups; MMA issuer, producer, watcher and an idle warp
-constexpr int kSoftRegs = 216, kRestRegs = 72;   // 2 x 128 x 216 + 128 x 72 = 384 x 168, what the launch holds
+constexpr int kThreads = 640;       // four softmax warpgroups, two per accumulator; issuer, two producers, watcher
+constexpr int kSoft = 512;
+constexpr int kIssuer = 16, kLoadK = 17, kWatcher = 18, kLoadV = 19;   // warps
+constexpr int kSoftRegs = 104, kRestRegs = 64;   // 512 x 104 + 128 x 64 = 640 x 96, what the launch holds
 
 constexpr int kPolyEvery = 4;       // every 4th pair of weights on the FMA pipe instead of the special-function unit
 
@@ -61,6 +63,21 @@ __device__ __forceinline__ void tmem_st_32x32(uint32_t taddr, const uint32_t (&r
       "r"(r[28]), "r"(r[29]), "r"(r[30]), "r"(r[31])
       : "memory");
 }
+__device__ __forceinline__ void tmem_st_32x16(uint32_t taddr, const uint32_t (&r)[16]) {
+  asm volatile(
+      "tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16};" ::"r"(taddr),
+      "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]), "r"(r[9]),
+      "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15])
+      : "memory");
+}
+__device__ __forceinline__ void tmem_st_1(uint32_t taddr, float v) {
+  asm volatile("tcgen05.st.sync.aligned.32x32b.x1.b32 [%0], {%1};" ::"r"(taddr), "r"(__float_as_uint(v)) : "memory");
+}
+__device__ __forceinline__ float tmem_ld_1(uint32_t taddr) {
+  uint32_t r;
+  asm volatile("tcgen05.ld.sync.aligned.32x32b.x1.b32 {%0}, [%1];" : "=r"(r) : "r"(taddr) : "memory");
+  return __uint_as_float(r);
+}
 __device__ __forceinline__ void tmem_st_wait() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
 
 __device__ __forceinline__ uint32_t pack_f16(float a, float b) {
@@ -72,10 +89,18 @@ __device__ __forceinline__ void named_bar_arrive(uint32_t id, uint32_t nthreads)
   asm volatile("bar.arrive %0, %1;" ::"r"(id), "r"(nthreads) : "memory");
 }
 // Named barriers (0 is __syncthreads): the softmax warpgroups among themselves; "P written", one per accumulator
-// (128 threads arrive, the issuer's warp waits); "operand tile landed", between the watcher's and the issuer's warp.
+// (256 threads arrive, the issuer's warp waits); "operand tile landed", between the watcher's and the issuer's warp;
+// the two warps that share 32 rows, eight pairs.
 // They do not pass through shared memory, which the tensor core keeps busy: a wait on an mbarrier that has long
 // completed takes 200 to 400 cycles here, one on a named barrier about 30.
-constexpr uint32_t kBarSoft = 1, kBarP = 2, kBarTile = 4;
+constexpr uint32_t kBarSoft = 1, kBarP = 2, kBarTile = 4, kBarPair = 5;
+// Meets the other warp of the pair; whether any of the 64 threads says yes.
+__device__ __forceinline__ bool pair_any(uint32_t id, bool yes) {
+  uint32_t r;
+  asm volatile("{\n\t.reg .pred p, q;\n\tsetp.ne.b32 p, %2, 0;\n\tbar.red.or.pred q, %1, 64, p;\n\tselp.u32 %0, 1, 0, q;\n\t}"
+               : "=r"(r) : "r"(id), "r"(static_cast<uint32_t>(yes)) : "memory");
+  return r != 0;
+}
 
 // Two FP32 operations in one instruction.
 __device__ __forceinline__ uint64_t pair_f32(float a, float b) {
@@ -136,9 +161,9 @@ struct TileArgs {
 //
 // A CTA owns 256 query rows of one key/value head (row = token x query heads of the group) as two accumulators of
 // 128, or up to 128 rows as two accumulators that take the even and the odd key tiles and are joined at the end:
-// either way one warpgroup's softmax runs while the tensor core works for the other.  Per 128 keys and accumulator:
+// either way one accumulator's softmax runs while the tensor core works for the other.  Per 128 keys and accumulator:
 //   S = Q K^T            8 (D / 16) MMAs from shared memory into tensor memory
-//   softmax              one thread per row: S to registers, running maximum, P = 2^(S - max) as FP16 over S
+//   softmax              two threads per row: S to registers, running maximum, P = 2^(S - max) as FP16 over S
 //   O += P V             8 MMAs with P from tensor memory, V as it lies in the cache (features contiguous)
 // The reference that is subtracted is only moved (and O rescaled, in tensor memory) when the maximum has grown by
 // more than 2^8: P stays within [0, 256], exact enough in FP16, and O is almost never touched.
@@ -176,7 +201,7 @@ attn_tile_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constan
   if (tid == 0) {
     for (int i = 0; i < C::kStages; ++i) mbar_init(bar_full + 8 * i, 1), mbar_init(bar_free + 8 * i, 1);
     for (int i = 0; i < 2; ++i) mbar_init(bar_s + 8 * i, 1), mbar_init(bar_o + 8 * i, 1);
-    mbar_init(bar_q, 8);
+    mbar_init(bar_q, kSoft / 32);
     mbar_init(bar_fix, 1);
     mbar_init(bar_drain, 1);
     fence_mbar_init();
@@ -240,55 +265,59 @@ attn_tile_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constan
 
   const uint32_t base = (smem_u32(smem_raw) + 1023u) & ~1023u;
   const uint32_t sq = base, ring = base + 2 * C::kTileBytes;
-  if (warp == 8) tmem_alloc(smem_u32(&s_tmem), 512);
+  if (warp == kIssuer) tmem_alloc(smem_u32(&s_tmem), 512);
   tc_fence_before_sync();
   __syncthreads();
   tc_fence_after_sync();
   grid_dep_launch();   // only now: a later launch's CTA may take this SM's tensor memory when it is given back
   const uint32_t tmem = __shfl_sync(0xffffffffu, s_tmem, 0);
-  const uint32_t t_s[2] = {tmem, tmem + 128}, t_o[2] = {tmem + 256, tmem + 256 + D};
   const WaitCtx wc{&s_abort, ta.wait_limit};
-  int issued = 0;   // producer: loads requested so far
+  int issued = 0;   // producers: tiles requested so far
 
-  if (warp >= 8) {
+  if (warp >= kSoft / 32) {
     asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kRestRegs));
-    if (warp == 9) {
-      // ------------------------------------------------------------------ producer
+    if (warp == kLoadK || warp == kLoadV) {
+      // ------------------------------------------------------------------ producers, one for keys and one for values
+      // A lane requests one box; its page id is looked up a tile ahead.
+      const bool is_v = warp == kLoadV;
       const int boxes = kTile / ta.box;
-      const int halves = D / 64;
+      constexpr int halves = D / 64;
+      const int x = lane / boxes, y = lane - x * boxes;
+      const bool mine = lane < boxes * halves;
       const int rows_all = static_cast<int>(a.c.pages * a.c.heads * a.c.page);
+      const int* trow = a.table + static_cast<int64_t>(b) * a.width;
+      auto row_of = [&](int t) {   // of the tensor map; rows_all lies beyond the tensor: zeros
+        const int key = key_base + t * kTile + y * ta.box;
+        if (!mine || t >= n_tiles || key >= rg.hi || key + ta.box <= rg.lo) return rows_all;
+        const int col = key / a.c.page;
+        const int id = trow[col];
+        if (id < 0 || id >= a.c.pages) return rows_all;
+        return static_cast<int>((static_cast<int64_t>(id) * a.c.heads + hk) * a.c.page) + key - col * a.c.page;
+      };
       uint32_t fix_phase = 0;
-      for (int i = 0; i < 2 * n_tiles; ++i) {
-        const int st = i % C::kStages;
+      int row = row_of(0);
+      for (int t = 0; t < n_tiles; ++t) {
+        const int i = 2 * t + is_v, st = i % C::kStages;
+        const int next = row_of(t + 1);
         if (i >= C::kStages && !warp_wait(bar_free + 8 * st, ((i / C::kStages) & 1) ^ 1, wc)) break;
-        const int key0 = key_base + (i >> 1) * kTile;
-        const bool is_v = i & 1;
+        const int key0 = key_base + t * kTile;
         // rows of the tile that were never written: before the request's window, beyond its length
         const int dead_lo = min(max(rg.lo - key0, 0), kTile), dead_hi = min(max(rg.L - key0, 0), kTile);
         const bool fix = is_v && (dead_lo > 0 || dead_hi < kTile);
         const uint32_t dst = ring + st * C::kTileBytes, bar = fix ? bar_fix : bar_full + 8 * st;
         if (lane == 0) mbar_arrive_expect_tx(bar, C::kTileBytes);
         __syncwarp();
-        if (lane < boxes * halves) {
-          const int x = lane / boxes, y = lane - x * boxes;
-          const int key = key0 + y * ta.box;
-          int row = rows_all;   // beyond the tensor: zeros
-          if (key < rg.hi && key + ta.box > rg.lo) {
-            const int col = key / a.c.page;
-            const int id = a.table[static_cast<int64_t>(b) * a.width + col];
-            if (id >= 0 && id < a.c.pages) row = static_cast<int>((static_cast<int64_t>(id) * a.c.heads + hk) * a.c.page) + key - col * a.c.page;
-          }
-          tma_load_2d(dst + x * C::kPanel + y * ta.box * 128, is_v ? &map_v : &map_k, bar, x * 64, row);
-        }
-        issued = i + 1;
+        if (mine) tma_load_2d(dst + x * C::kPanel + y * ta.box * 128, is_v ? &map_v : &map_k, bar, x * 64, row);
+        row = next;
+        issued = t + 1;
         if (fix) {
           if (!warp_wait(bar_fix, fix_phase & 1, wc)) break;
           ++fix_phase;
           const int dead = dead_lo + (kTile - dead_hi);
           for (int j = lane; j < dead * halves * 8; j += 32) {
-            const int chunk = j & 7, x = (j >> 3) % halves, r = (j >> 3) / halves;
+            const int chunk = j & 7, xx = (j >> 3) % halves, r = (j >> 3) / halves;
             const int rr = r < dead_lo ? r : dead_hi + r - dead_lo;
-            asm volatile("st.shared.v4.u32 [%0], {%1, %1, %1, %1};" ::"r"(dst + x * C::kPanel + rr * 128 + chunk * 16), "r"(0) : "memory");
+            asm volatile("st.shared.v4.u32 [%0], {%1, %1, %1, %1};" ::"r"(dst + xx * C::kPanel + rr * 128 + chunk * 16), "r"(0) : "memory");
           }
           fence_proxy_async_smem();
           __syncwarp();
@@ -296,7 +325,7 @@ attn_tile_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constan
         }
         __syncwarp();
       }
-    } else if (warp == 8) {
+    } else if (warp == kIssuer) {
       // ------------------------------------------------------------------ MMA issuer
       // The whole warp walks the steps, so that every operand is uniform; one elected thread issues.  After a role has
       // given up the steps go on (the barriers stay in step), on whatever the tiles hold.
@@ -324,7 +353,7 @@ attn_tile_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constan
         if (u > 0) {   // O(u - 1) += P V
           const int v = u - 1, acc = v & 1, st = (2 * (two ? v >> 1 : v) + 1) % C::kStages;
           if (!two || acc == 0) named_bar_sync(kBarTile, 64);
-          named_bar_sync(kBarP + acc, 160);
+          named_bar_sync(kBarP + acc, 288);
           tc_fence_after_sync();
           if (leader) {
             const uint32_t vl = v_lo0 + st * kStageUnits, d = tmem + 256 + acc * D, p = tmem + acc * 128;
@@ -337,7 +366,7 @@ attn_tile_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constan
           __syncwarp();
         }
       }
-    } else if (warp == 10) {
+    } else {
       // ------------------------------------------------------------------ watcher: waits for the operand tiles a step ahead
       bool ok = true;
       for (int u = 0; u <= N; ++u) {
@@ -352,27 +381,32 @@ attn_tile_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constan
       }
     }
   } else {
-    // -------------------------------------------------------------------- softmax, one thread per row
+    // -------------------------------------------------------------------- softmax, two threads per row
     asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kSoftRegs));
-    const int acc = warp >> 2;                       // accumulator
+    const int acc = warp >> 3;                       // accumulator
+    const int half = (warp >> 2) & 1;                // the thread's 64 keys of a tile, and its half of the features
     const int r = tid & 127;                         // row of the tile
     const uint32_t lane_off = static_cast<uint32_t>(warp & 3) << 21;   // 32 lanes per warp, lane in bits 16 and up
+    const uint32_t t_sc = tmem + acc * 128 + lane_off, t_out = tmem + 256 + acc * D + half * (D / 2) + lane_off;
+    const uint32_t t_swap = t_sc + 64;               // columns that P leaves free: words between the row's two threads
+    const uint32_t pair = kBarPair + acc * 4 + (warp & 3);
     const int q_tile = two ? acc : 0;
     const int tok = q_tile * tpt + r / G;            // token of the row, from tok0
     const bool live = r < tpt * G && tok < toks && row0 + tok0 + tok >= 0 && row0 + tok0 + tok < a.tokens;
     const int64_t out_row = (row0 + tok0 + tok) * a.heads + hk * G + r % G;
 
     if (two || acc == 0) {
-      const uint4* qp = live ? reinterpret_cast<const uint4*>(a.q + (row0 + tok0 + tok) * a.q_stride + (hk * G + r % G) * D) : nullptr;
-      uint4 x[D / 8];
+      const uint4* qp = live ? reinterpret_cast<const uint4*>(a.q + (row0 + tok0 + tok) * a.q_stride + (hk * G + r % G) * D) + half * (D / 16) : nullptr;
+      uint4 x[D / 16];
 #pragma unroll
-      for (int i = 0; i < D / 8; ++i) x[i] = live ? __ldg(qp + i) : make_uint4(0, 0, 0, 0);
+      for (int i = 0; i < D / 16; ++i) x[i] = live ? __ldg(qp + i) : make_uint4(0, 0, 0, 0);
       const uint32_t dst = sq + q_tile * C::kTileBytes + r * 128;
 #pragma unroll
-      for (int i = 0; i < D / 8; ++i) {
+      for (int i = 0; i < D / 16; ++i) {
+        const int ch = half * (D / 16) + i;
         x[i].x = (x[i].x & ta.q_and) ^ ta.q_xor, x[i].y = (x[i].y & ta.q_and) ^ ta.q_xor;
         x[i].z = (x[i].z & ta.q_and) ^ ta.q_xor, x[i].w = (x[i].w & ta.q_and) ^ ta.q_xor;
-        asm volatile("st.shared.v4.u32 [%0], {%1, %2, %3, %4};" ::"r"(dst + (i >> 3) * C::kPanel + (((i & 7) ^ (r & 7)) << 4)),
+        asm volatile("st.shared.v4.u32 [%0], {%1, %2, %3, %4};" ::"r"(dst + (ch >> 3) * C::kPanel + (((ch & 7) ^ (r & 7)) << 4)),
                      "r"(x[i].x), "r"(x[i].y), "r"(x[i].z), "r"(x[i].w) : "memory");
       }
       fence_proxy_async_smem();
@@ -381,27 +415,27 @@ attn_tile_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constan
     if (lane == 0) mbar_arrive(bar_q);
 
     const int p = p_base + tok;
-    const int see_to = min(p, rg.hi - 1);                           // last key of the row
-    const int see_from = a.window > 0 ? p - a.window : -1;          // keys above it
-    const int all_to = min(p_base + q_tile * tpt + 1, rg.hi);       // every row of the tile sees [all_from, all_to)
+    const int see_to = min(p, rg.hi - 1) - 64 * half;                        // last key of the row, from the thread's first
+    const int see_from = (a.window > 0 ? p - a.window : -1) - 64 * half;     // keys above it
+    const int all_to = min(p_base + q_tile * tpt + 1, rg.hi);                // every row of the tile sees [all_from, all_to)
     const int all_from = a.window > 0 ? p_base + toks - a.window : 0;
     const int mine = two ? n_tiles : (n_tiles - acc + 1) >> 1;
     const float sc = a.scale_log2;
-    float m = -INFINITY, l = 0.0f;   // m: the reference that is subtracted, in powers of two
+    float m = -INFINITY, l = 0.0f;   // m: the reference that is subtracted, in powers of two; l: the thread's own keys
 
     bool ok = true;
     for (int i = 0; i < mine; ++i) {
       const int key0 = key_base + (two ? i : 2 * i + acc) * kTile;
       ok = ok && warp_wait(bar_s + 8 * acc, i & 1, wc);
       tc_fence_after_sync();
-      uint32_t s[4][32];
-#pragma unroll
-      for (int h = 0; h < 4; ++h) tmem_ld_32x32(t_s[acc] + lane_off + 32 * h, s[h]);
+      uint32_t s[2][32];
+      tmem_ld_32x32(t_sc + 64 * half, s[0]);
+      tmem_ld_32x32(t_sc + 64 * half + 32, s[1]);
       tmem_ld_wait();
       if (key0 < all_from || key0 + kTile > all_to) {
         const int to = see_to - key0, from = see_from - key0;
 #pragma unroll
-        for (int h = 0; h < 4; ++h) {
+        for (int h = 0; h < 2; ++h) {
 #pragma unroll
           for (int j = 0; j < 32; ++j)
             if (32 * h + j > to || 32 * h + j <= from) s[h][j] = 0xff800000u;   // -inf
@@ -410,15 +444,23 @@ attn_tile_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constan
       float top[4];
 #pragma unroll
       for (int h = 0; h < 4; ++h) {
-        top[h] = max3(__uint_as_float(s[h][0]), __uint_as_float(s[h][1]), __uint_as_float(s[h][2]));
+        const uint32_t* v = s[h >> 1] + 16 * (h & 1);
+        top[h] = max3(__uint_as_float(v[0]), __uint_as_float(v[1]), __uint_as_float(v[2]));
 #pragma unroll
-        for (int j = 3; j < 31; j += 2) top[h] = max3(top[h], __uint_as_float(s[h][j]), __uint_as_float(s[h][j + 1]));
+        for (int j = 3; j < 15; j += 2) top[h] = max3(top[h], __uint_as_float(v[j]), __uint_as_float(v[j + 1]));
+        top[h] = fmaxf(top[h], __uint_as_float(v[15]));
       }
-      top[0] = max3(top[0], __uint_as_float(s[0][31]), top[1]);
-      top[2] = max3(top[2], __uint_as_float(s[1][31]), top[3]);
-      const float t = max3(fmaxf(top[0], top[2]), __uint_as_float(s[2][31]), __uint_as_float(s[3][31])) * sc;
-      const bool grown = t > m + 8.0f;
-      if (__any_sync(0xffffffffu, grown)) {
+      float t = fmaxf(max3(top[0], top[1], top[2]), top[3]) * sc;
+      if (pair_any(pair, t > m + 8.0f)) {   // rare after the first tiles: some row of the 32 moves its reference
+        tmem_st_1(t_swap + half, t);
+        tmem_st_wait();
+        tc_fence_before_sync();
+        named_bar_sync(pair, 64);
+        tc_fence_after_sync();
+        const float other = tmem_ld_1(t_swap + (half ^ 1));
+        tmem_ld_wait();
+        t = fmaxf(t, other);
+        const bool grown = t > m + 8.0f;
         const float f = grown ? (m == -INFINITY ? 0.0f : exp2_approx(m - t)) : 1.0f;
         if (grown) m = t;
         l *= f;
@@ -427,72 +469,79 @@ attn_tile_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constan
           tc_fence_after_sync();
 #pragma unroll 1
           for (int h = 0; h < D / 32; ++h) {
-            uint32_t o[32];
-            tmem_ld_32x32(t_o[acc] + lane_off + 32 * h, o);
+            uint32_t o[16];
+            tmem_ld_32x16(t_out + 16 * h, o);
             tmem_ld_wait();
 #pragma unroll
-            for (int j = 0; j < 32; ++j) o[j] = __float_as_uint(__uint_as_float(o[j]) * f);
-            tmem_st_32x32(t_o[acc] + lane_off + 32 * h, o);
+            for (int j = 0; j < 16; ++j) o[j] = __float_as_uint(__uint_as_float(o[j]) * f);
+            tmem_st_32x16(t_out + 16 * h, o);
           }
         }
       }
       const float ms = m == -INFINITY ? 0.0f : m;
       const uint64_t sc2 = pair_f32(sc, sc), ms2 = pair_f32(-ms, -ms);
       uint64_t sum[2] = {0, 0};
+      uint32_t w[32];
 #pragma unroll
-      for (int h = 0; h < 2; ++h) {
-        uint32_t w[32];
-#pragma unroll
-        for (int j = 0; j < 32; ++j) {
-          const int q = 2 * h + (j >> 4), e = (2 * j) & 31;
-          uint64_t x = fma_f32x2(pair_f32(__uint_as_float(s[q][e]), __uint_as_float(s[q][e + 1])), sc2, ms2);
-          float e0, e1;
-          if (j % kPolyEvery == kPolyEvery - 1) {
-            x = exp2_poly2(x);
-            unpair_f32(x, e0, e1);
-          } else {
-            unpair_f32(x, e0, e1);
-            e0 = exp2_approx(e0);
-            e1 = exp2_approx(e1);
-            x = pair_f32(e0, e1);
-          }
-          sum[j & 1] = add_f32x2(sum[j & 1], x);
-          w[j] = pack_f16(e0, e1);
+      for (int j = 0; j < 32; ++j) {
+        const int q = j >> 4, e = (2 * j) & 31;
+        uint64_t x = fma_f32x2(pair_f32(__uint_as_float(s[q][e]), __uint_as_float(s[q][e + 1])), sc2, ms2);
+        float e0, e1;
+        if (j % kPolyEvery == kPolyEvery - 1) {
+          x = exp2_poly2(x);
+          unpair_f32(x, e0, e1);
+        } else {
+          unpair_f32(x, e0, e1);
+          e0 = exp2_approx(e0);
+          e1 = exp2_approx(e1);
+          x = pair_f32(e0, e1);
         }
-        tmem_st_32x32(t_s[acc] + lane_off + 32 * h, w);
+        sum[j & 1] = add_f32x2(sum[j & 1], x);
+        w[j] = pack_f16(e0, e1);
       }
+      tmem_st_32x32(t_sc + 32 * half, w);
       float l0, l1;
       unpair_f32(add_f32x2(sum[0], sum[1]), l0, l1);
       l += l0 + l1;
       tmem_st_wait();
       tc_fence_before_sync();
-      named_bar_arrive(kBarP + acc, 160);
+      named_bar_arrive(kBarP + acc, 288);
     }
     if (ok && mine > 0) warp_wait(bar_o + 8 * acc, (mine - 1) & 1, wc);
     tc_fence_after_sync();
 
-    // -------------------------------------------------------------------- epilogue
+    // -------------------------------------------------------------------- epilogue: a thread has half of its row's features
+    tmem_st_1(t_swap + half, l);   // the sum of the row's two threads
+    tmem_st_wait();
+    tc_fence_before_sync();
+    named_bar_sync(pair, 64);
+    tc_fence_after_sync();
+    {
+      const float other = tmem_ld_1(t_swap + (half ^ 1));
+      tmem_ld_wait();
+      l = half == 0 ? l + other : other + l;
+    }
     // Accumulators of the even and the odd tiles are joined in the first one's threads.
     float f0 = 1.0f, f1 = 0.0f;
     const bool join = !two && n_tiles > 1;
-    float4* room = reinterpret_cast<float4*>(smem_raw + (ring - smem_u32(smem_raw)));   // [D / 4][128 rows]
+    float4* room = reinterpret_cast<float4*>(smem_raw + (ring - smem_u32(smem_raw))) + half * (D / 8) * kTile;   // [D / 4][128 rows]
     float2* room_ml = reinterpret_cast<float2*>(smem_raw + (sq - smem_u32(smem_raw)));
     if (join) {
-      named_bar_sync(kBarSoft, 256);   // every MMA has completed: the operand tiles are free
+      named_bar_sync(kBarSoft, kSoft);   // every MMA has completed: the operand tiles are free
       if (acc == 1) {
 #pragma unroll 1
         for (int h = 0; h < D / 32; ++h) {
-          uint32_t o[32];
-          tmem_ld_32x32(t_o[1] + lane_off + 32 * h, o);
+          uint32_t o[16];
+          tmem_ld_32x16(t_out + 16 * h, o);
           tmem_ld_wait();
 #pragma unroll
-          for (int j = 0; j < 8; ++j)
-            room[(8 * h + j) * kTile + r] = make_float4(__uint_as_float(o[4 * j]), __uint_as_float(o[4 * j + 1]),
+          for (int j = 0; j < 4; ++j)
+            room[(4 * h + j) * kTile + r] = make_float4(__uint_as_float(o[4 * j]), __uint_as_float(o[4 * j + 1]),
                                                         __uint_as_float(o[4 * j + 2]), __uint_as_float(o[4 * j + 3]));
         }
-        room_ml[r] = make_float2(m, l);
+        if (half == 0) room_ml[r] = make_float2(m, l);
       }
-      named_bar_sync(kBarSoft, 256);
+      named_bar_sync(kBarSoft, kSoft);
       if (acc == 0) {
         const float2 ml = room_ml[r];
         const float M = fmaxf(m, ml.x), Ms = M == -INFINITY ? 0.0f : M;
@@ -510,46 +559,46 @@ attn_tile_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constan
       float* pp = pu + part * kPart + q_tile * kTile * (D + 2);
 #pragma unroll 1
       for (int h = 0; h < D / 32; ++h) {
-        uint32_t o[32];
+        uint32_t o[16];
         if (n_tiles > 0) {
-          tmem_ld_32x32(t_o[acc] + lane_off + 32 * h, o);
+          tmem_ld_32x16(t_out + 16 * h, o);
           tmem_ld_wait();
         }
-        float v[32];
+        float v[16];
 #pragma unroll
-        for (int j = 0; j < 32; ++j) v[j] = n_tiles > 0 ? __uint_as_float(o[j]) * f0 : 0.0f;
+        for (int j = 0; j < 16; ++j) v[j] = n_tiles > 0 ? __uint_as_float(o[j]) * f0 : 0.0f;
         if (join) {
 #pragma unroll
-          for (int j = 0; j < 8; ++j) {
-            const float4 x = room[(8 * h + j) * kTile + r];
+          for (int j = 0; j < 4; ++j) {
+            const float4 x = room[(4 * h + j) * kTile + r];
             v[4 * j] = fmaf(x.x, f1, v[4 * j]), v[4 * j + 1] = fmaf(x.y, f1, v[4 * j + 1]);
             v[4 * j + 2] = fmaf(x.z, f1, v[4 * j + 2]), v[4 * j + 3] = fmaf(x.w, f1, v[4 * j + 3]);
           }
         }
         if (parts > 1) {
 #pragma unroll
-          for (int j = 0; j < 8; ++j)
-            reinterpret_cast<float4*>(pp)[(8 * h + j) * kTile + r] = make_float4(v[4 * j], v[4 * j + 1], v[4 * j + 2], v[4 * j + 3]);
-        } else if (live) {
-          uint4* dst = reinterpret_cast<uint4*>(a.out + out_row * D + 32 * h);
-#pragma unroll
           for (int j = 0; j < 4; ++j)
+            reinterpret_cast<float4*>(pp)[(half * (D / 8) + 4 * h + j) * kTile + r] = make_float4(v[4 * j], v[4 * j + 1], v[4 * j + 2], v[4 * j + 3]);
+        } else if (live) {
+          uint4* dst = reinterpret_cast<uint4*>(a.out + out_row * D + half * (D / 2) + 16 * h);
+#pragma unroll
+          for (int j = 0; j < 2; ++j)
             dst[j] = make_uint4(pack_f16(v[8 * j] * inv, v[8 * j + 1] * inv), pack_f16(v[8 * j + 2] * inv, v[8 * j + 3] * inv),
                                 pack_f16(v[8 * j + 4] * inv, v[8 * j + 5] * inv), pack_f16(v[8 * j + 6] * inv, v[8 * j + 7] * inv));
         }
       }
-      if (parts > 1) reinterpret_cast<float2*>(pp + kTile * D)[r] = make_float2(m, l);
+      if (parts > 1 && half == 0) reinterpret_cast<float2*>(pp + kTile * D)[r] = make_float2(m, l);
     }
     if (parts > 1) {
       // The CTA that arrives last joins the parts, in their order.
       __threadfence();
-      named_bar_sync(kBarSoft, 256);
+      named_bar_sync(kBarSoft, kSoft);
       if (tid == 0) {
         const unsigned int before = atomicAdd(a.counters + unit, 1u);
         s_last = before == static_cast<unsigned int>(parts) - 1u;
         if (s_last) a.counters[unit] = 0u;
       }
-      named_bar_sync(kBarSoft, 256);
+      named_bar_sync(kBarSoft, kSoft);
       if (s_last && writes && live) {
         __threadfence();
         const float* p0 = pu + q_tile * kTile * (D + 2);
@@ -563,21 +612,21 @@ attn_tile_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constan
         const float Li = L > 0.0f ? 1.0f / L : 0.0f;
 #pragma unroll 1
         for (int h = 0; h < D / 32; ++h) {
-          float4 v[8];
+          float4 v[4];
 #pragma unroll
-          for (int j = 0; j < 8; ++j) v[j] = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+          for (int j = 0; j < 4; ++j) v[j] = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
           for (int q = 0; q < parts; ++q) {
             const float* pq_ = p0 + static_cast<int64_t>(q) * kPart;
             const float f = exp2_approx(__ldcg(reinterpret_cast<const float2*>(pq_ + kTile * D) + r).x - Ms) * Li;
 #pragma unroll
-            for (int j = 0; j < 8; ++j) {
-              const float4 x = __ldcg(reinterpret_cast<const float4*>(pq_) + (8 * h + j) * kTile + r);
+            for (int j = 0; j < 4; ++j) {
+              const float4 x = __ldcg(reinterpret_cast<const float4*>(pq_) + (half * (D / 8) + 4 * h + j) * kTile + r);
               v[j].x = fmaf(x.x, f, v[j].x), v[j].y = fmaf(x.y, f, v[j].y), v[j].z = fmaf(x.z, f, v[j].z), v[j].w = fmaf(x.w, f, v[j].w);
             }
           }
-          uint4* dst = reinterpret_cast<uint4*>(a.out + out_row * D + 32 * h);
+          uint4* dst = reinterpret_cast<uint4*>(a.out + out_row * D + half * (D / 2) + 16 * h);
 #pragma unroll
-          for (int j = 0; j < 4; ++j)
+          for (int j = 0; j < 2; ++j)
             dst[j] = make_uint4(pack_f16(v[2 * j].x, v[2 * j].y), pack_f16(v[2 * j].z, v[2 * j].w),
                                 pack_f16(v[2 * j + 1].x, v[2 * j + 1].y), pack_f16(v[2 * j + 1].z, v[2 * j + 1].w));
         }
@@ -592,11 +641,11 @@ attn_tile_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constan
   if (s_abort) {
     // Some role gave up.  What has been handed to the hardware still completes by itself and must have done so
     // before shared and tensor memory go away: the producer's loads and the issuer's MMAs.
-    if (tid == 9 * 32) {
-      const int first = issued > C::kStages ? issued - C::kStages : 0;
-      for (int i = first; i < issued; ++i) mbar_drain(bar_full + 8 * (i % C::kStages), (i / C::kStages) & 1u);
-      mbar_drain(bar_fix, 0u);
-    } else if (tid == 8 * 32) {
+    if (lane == 0 && (warp == kLoadK || warp == kLoadV)) {
+      for (int i = 2 * issued + (warp == kLoadV) - 2; i >= 0 && i >= 2 * issued - C::kStages; i -= 2)
+        mbar_drain(bar_full + 8 * (i % C::kStages), (i / C::kStages) & 1u);
+      if (warp == kLoadV) mbar_drain(bar_fix, 0u);
+    } else if (tid == kIssuer * 32) {
       umma_commit(bar_drain);
       mbar_drain(bar_drain, 0u);
     }
@@ -604,7 +653,7 @@ attn_tile_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constan
     if (tid == 0) atomicExch(ta.status, static_cast<int>(PQ_ERR_TIMEOUT));
   }
   tc_fence_after_sync();
-  if (warp == 8) {
+  if (warp == kIssuer) {
     tmem_relinquish();
     tmem_dealloc(tmem, 512);
   }
@@ -621,7 +670,7 @@ int launch(TileArgs& t, const TilePlan& plan, cudaStream_t stream) {
     cudaFuncAttributes f = {};
     return cudaFuncGetAttributes(&f, attn_tile_kernel<D>) == cudaSuccess ? f.numRegs : 0;
   }();
-  if (regs * kThreads < 256 * kSoftRegs + 128 * kRestRegs) return PQ_ERR_CUDA;
+  if (regs * kThreads < kSoft * kSoftRegs + (kThreads - kSoft) * kRestRegs) return PQ_ERR_CUDA;
   CUtensorMap mk, mv;
   const pq_kv_cache& c = t.a.c;
   const uint64_t rows = static_cast<uint64_t>(c.pages) * c.heads * c.page;
