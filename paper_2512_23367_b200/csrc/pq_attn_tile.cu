@@ -70,14 +70,6 @@ __device__ __forceinline__ void tmem_st_32x16(uint32_t taddr, const uint32_t (&r
       "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15])
       : "memory");
 }
-__device__ __forceinline__ void tmem_st_1(uint32_t taddr, float v) {
-  asm volatile("tcgen05.st.sync.aligned.32x32b.x1.b32 [%0], {%1};" ::"r"(taddr), "r"(__float_as_uint(v)) : "memory");
-}
-__device__ __forceinline__ float tmem_ld_1(uint32_t taddr) {
-  uint32_t r;
-  asm volatile("tcgen05.ld.sync.aligned.32x32b.x1.b32 {%0}, [%1];" : "=r"(r) : "r"(taddr) : "memory");
-  return __uint_as_float(r);
-}
 __device__ __forceinline__ void tmem_st_wait() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
 
 __device__ __forceinline__ uint32_t pack_f16(float a, float b) {
@@ -90,16 +82,31 @@ __device__ __forceinline__ void named_bar_arrive(uint32_t id, uint32_t nthreads)
 }
 // Named barriers (0 is __syncthreads): the softmax warpgroups among themselves; "P written", one per accumulator
 // (256 threads arrive, the issuer's warp waits); "operand tile landed", between the watcher's and the issuer's warp;
-// the two warps that share 32 rows, eight pairs.
+// the two warps that share 32 rows, eight pairs; "S read", 256 threads of an accumulator to the issuer.
 // They do not pass through shared memory, which the tensor core keeps busy: a wait on an mbarrier that has long
 // completed takes 200 to 400 cycles here, one on a named barrier about 30.
-constexpr uint32_t kBarSoft = 1, kBarP = 2, kBarTile = 4, kBarPair = 5;
+constexpr uint32_t kBarSoft = 1, kBarP = 2, kBarTile = 4, kBarPair = 5, kBarRead = 13;
 // Meets the other warp of the pair; whether any of the 64 threads says yes.
 __device__ __forceinline__ bool pair_any(uint32_t id, bool yes) {
   uint32_t r;
   asm volatile("{\n\t.reg .pred p, q;\n\tsetp.ne.b32 p, %2, 0;\n\tbar.red.or.pred q, %1, 64, p;\n\tselp.u32 %0, 1, 0, q;\n\t}"
                : "=r"(r) : "r"(id), "r"(static_cast<uint32_t>(yes)) : "memory");
   return r != 0;
+}
+
+// The sum, or the larger, of a value of the row's two threads, the same in both: the second half's goes to the first
+// and the result back.
+template <bool kSum>
+__device__ __forceinline__ float pair_combine(float* word, uint32_t id, int half, float v) {
+  if (half == 1) *word = v;
+  named_bar_sync(id, 64);
+  if (half == 0) {
+    v = kSum ? v + *word : fmaxf(v, *word);
+    *word = v;
+  }
+  named_bar_sync(id, 64);
+  if (half == 1) v = *word;
+  return v;
 }
 
 // Two FP32 operations in one instruction.
@@ -163,12 +170,14 @@ struct TileArgs {
 // 128, or up to 128 rows as two accumulators that take the even and the odd key tiles and are joined at the end:
 // either way one accumulator's softmax runs while the tensor core works for the other.  Per 128 keys and accumulator:
 //   S = Q K^T            8 (D / 16) MMAs from shared memory into tensor memory
-//   softmax              two threads per row: S to registers, running maximum, P = 2^(S - max) as FP16 over S
+//   softmax              two threads per row: S to registers, running maximum, P = 2^(S - max) as FP16
 //   O += P V             8 MMAs with P from tensor memory, V as it lies in the cache (features contiguous)
 // The reference that is subtracted is only moved (and O rescaled, in tensor memory) when the maximum has grown by
 // more than 2^8: P stays within [0, 256], exact enough in FP16, and O is almost never touched.
-// MMA order: QK(u), PV(u - 1), u counting the accumulators in turn; the tensor core executes in order, so S (which
-// P overlays) is free when its next QK is issued.
+// Tensor memory (512 columns): S, shared by the accumulators in turn, 128; P of each, 64; O of each, 64 or 128.  S is
+// free as soon as the softmax threads hold it in registers, so that QK(u + 1) runs under the softmax of u; MMA order
+// QK(u), PV(u - 2), u counting the accumulators in turn.  With P over S and one S per accumulator the chain
+// QK -> softmax -> PV of an accumulator set the pace: 3240 cycles per 256 x 128 scores.
 // Keys and values come through TMA boxes of whole page pieces (one lane looks up and requests one box); boxes that
 // no visible key needs, or of an unusable page id, are requested beyond the tensor and arrive as zeros.
 // Value rows that were never written (beyond the request's length, before its window) are zeroed in shared memory:
@@ -186,6 +195,7 @@ attn_tile_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constan
   __shared__ int s_assign[2];
   __shared__ int s_warp_sum[kThreads / 32];
   __shared__ int s_last;
+  __shared__ float s_swap[2 * kTile];   // one word between the two threads of a row
 
   const AttnArgs& a = ta.a;
   const int tid = threadIdx.x, warp = __shfl_sync(0xffffffffu, tid >> 5, 0), lane = tid & 31;
@@ -262,6 +272,9 @@ attn_tile_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constan
   const int n_tiles = part == parts - 1 ? all_tiles - t0 : per;   // key tiles of this CTA
   const int key_base = k_lo + t0 * kTile;
   const int N = two ? 2 * n_tiles : n_tiles;                      // (QK, PV) steps
+  // Steps that a PV follows its QK by: with two query tiles S(u + 1) is computed while the softmax of u runs; with
+  // one, where memory is the bound, operand tiles are given back a step earlier instead.
+  const int lag = two ? 2 : 1;
 
   const uint32_t base = (smem_u32(smem_raw) + 1023u) & ~1023u;
   const uint32_t sq = base, ring = base + 2 * C::kTileBytes;
@@ -335,28 +348,29 @@ attn_tile_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constan
       const uint32_t q_lo = desc_k(sq), k_lo0 = desc_k(ring), v_lo0 = desc_mn(ring, C::kPanel);
       const uint32_t q_step = two ? kStageUnits : 0;
       warp_wait(bar_q, 0, wc);
-      for (int u = 0; u <= N; ++u) {
+      for (int u = 0; u < N + lag; ++u) {
+        if (u > 0 && u <= N) named_bar_sync(kBarRead, 288);   // S(u - 1) is in registers
         if (u < N) {   // S(u) = Q K^T
           const int acc = u & 1, st = (2 * (two ? u >> 1 : u)) % C::kStages;
           if (!two || acc == 0) named_bar_sync(kBarTile, 64);
           tc_fence_after_sync();
           if (leader) {
-            const uint32_t ql = q_lo + acc * q_step, kl = k_lo0 + st * kStageUnits, d = tmem + acc * 128;
-            umma_f16_ss<0>(d, ql, kl, id_qk);
+            const uint32_t ql = q_lo + acc * q_step, kl = k_lo0 + st * kStageUnits;
+            umma_f16_ss<0>(tmem, ql, kl, id_qk);
 #pragma unroll
-            for (int k = 1; k < KS; ++k) umma_f16_ss<1>(d, ql + (k / 4) * (C::kPanel / 16) + (k % 4) * 2, kl + (k / 4) * (C::kPanel / 16) + (k % 4) * 2, id_qk);
+            for (int k = 1; k < KS; ++k) umma_f16_ss<1>(tmem, ql + (k / 4) * (C::kPanel / 16) + (k % 4) * 2, kl + (k / 4) * (C::kPanel / 16) + (k % 4) * 2, id_qk);
             umma_commit(bar_s + 8 * acc);
             if (!two || acc == 1) umma_commit(bar_free + 8 * st);
           }
           __syncwarp();
         }
-        if (u > 0) {   // O(u - 1) += P V
-          const int v = u - 1, acc = v & 1, st = (2 * (two ? v >> 1 : v) + 1) % C::kStages;
+        if (u >= lag) {   // O(u - lag) += P V
+          const int v = u - lag, acc = v & 1, st = (2 * (two ? v >> 1 : v) + 1) % C::kStages;
           if (!two || acc == 0) named_bar_sync(kBarTile, 64);
           named_bar_sync(kBarP + acc, 288);
           tc_fence_after_sync();
           if (leader) {
-            const uint32_t vl = v_lo0 + st * kStageUnits, d = tmem + 256 + acc * D, p = tmem + acc * 128;
+            const uint32_t vl = v_lo0 + st * kStageUnits, d = tmem + 256 + acc * D, p = tmem + 128 + acc * 64;
             umma_f16_ts(d, p, vl, id_pv, (v >> 1) > 0);
 #pragma unroll
             for (int k = 1; k < PS; ++k) umma_f16_ts(d, p + 8 * k, vl + k * 128, id_pv, 1u);
@@ -369,10 +383,10 @@ attn_tile_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constan
     } else {
       // ------------------------------------------------------------------ watcher: waits for the operand tiles a step ahead
       bool ok = true;
-      for (int u = 0; u <= N; ++u) {
+      for (int u = 0; u < N + lag; ++u) {
 #pragma unroll
         for (int is_v = 0; is_v < 2; ++is_v) {
-          const int w = u - is_v;
+          const int w = u - is_v * lag;
           if (w < 0 || w >= N || (two && (w & 1))) continue;
           const int i = 2 * (two ? w >> 1 : w) + is_v;
           ok = ok && warp_wait(bar_full + 8 * (i % C::kStages), (i / C::kStages) & 1, wc);
@@ -387,8 +401,8 @@ attn_tile_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constan
     const int half = (warp >> 2) & 1;                // the thread's 64 keys of a tile, and its half of the features
     const int r = tid & 127;                         // row of the tile
     const uint32_t lane_off = static_cast<uint32_t>(warp & 3) << 21;   // 32 lanes per warp, lane in bits 16 and up
-    const uint32_t t_sc = tmem + acc * 128 + lane_off, t_out = tmem + 256 + acc * D + half * (D / 2) + lane_off;
-    const uint32_t t_swap = t_sc + 64;               // columns that P leaves free: words between the row's two threads
+    const uint32_t t_sc = tmem + 64 * half + lane_off, t_p = tmem + 128 + 64 * acc + 32 * half + lane_off, t_out = tmem + 256 + acc * D + half * (D / 2) + lane_off;
+    float* swap = s_swap + acc * kTile + r;
     const uint32_t pair = kBarPair + acc * 4 + (warp & 3);
     const int q_tile = two ? acc : 0;
     const int tok = q_tile * tpt + r / G;            // token of the row, from tok0
@@ -429,9 +443,11 @@ attn_tile_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constan
       ok = ok && warp_wait(bar_s + 8 * acc, i & 1, wc);
       tc_fence_after_sync();
       uint32_t s[2][32];
-      tmem_ld_32x32(t_sc + 64 * half, s[0]);
-      tmem_ld_32x32(t_sc + 64 * half + 32, s[1]);
+      tmem_ld_32x32(t_sc, s[0]);
+      tmem_ld_32x32(t_sc + 32, s[1]);
       tmem_ld_wait();
+      tc_fence_before_sync();
+      named_bar_arrive(kBarRead, 288);
       if (key0 < all_from || key0 + kTile > all_to) {
         const int to = see_to - key0, from = see_from - key0;
 #pragma unroll
@@ -450,22 +466,17 @@ attn_tile_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constan
         for (int j = 3; j < 15; j += 2) top[h] = max3(top[h], __uint_as_float(v[j]), __uint_as_float(v[j + 1]));
         top[h] = fmaxf(top[h], __uint_as_float(v[15]));
       }
+      bool done = i == 0;   // the product with the weights before these has been taken
       float t = fmaxf(max3(top[0], top[1], top[2]), top[3]) * sc;
       if (pair_any(pair, t > m + 8.0f)) {   // rare after the first tiles: some row of the 32 moves its reference
-        tmem_st_1(t_swap + half, t);
-        tmem_st_wait();
-        tc_fence_before_sync();
-        named_bar_sync(pair, 64);
-        tc_fence_after_sync();
-        const float other = tmem_ld_1(t_swap + (half ^ 1));
-        tmem_ld_wait();
-        t = fmaxf(t, other);
+        t = pair_combine<false>(swap, pair, half, t);
         const bool grown = t > m + 8.0f;
         const float f = grown ? (m == -INFINITY ? 0.0f : exp2_approx(m - t)) : 1.0f;
         if (grown) m = t;
         l *= f;
         if (i > 0) {   // O holds the sums up to the tile before
           ok = ok && warp_wait(bar_o + 8 * acc, (i - 1) & 1, wc);
+          done = true;
           tc_fence_after_sync();
 #pragma unroll 1
           for (int h = 0; h < D / 32; ++h) {
@@ -481,7 +492,7 @@ attn_tile_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constan
       const float ms = m == -INFINITY ? 0.0f : m;
       const uint64_t sc2 = pair_f32(sc, sc), ms2 = pair_f32(-ms, -ms);
       uint64_t sum[2] = {0, 0};
-      uint32_t w[32];
+      uint32_t w[32], asked = 0;
 #pragma unroll
       for (int j = 0; j < 32; ++j) {
         const int q = j >> 4, e = (2 * j) & 31;
@@ -498,8 +509,11 @@ attn_tile_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constan
         }
         sum[j & 1] = add_f32x2(sum[j & 1], x);
         w[j] = pack_f16(e0, e1);
+        if (j == 15) asked = mbar_test2(bar_o + 8 * acc, (i - 1) & 1, bar_o + 8 * acc, (i - 1) & 1);
       }
-      tmem_st_32x32(t_sc + 32 * half, w);
+      if (!done && !__all_sync(0xffffffffu, asked)) ok = ok && warp_wait(bar_o + 8 * acc, (i - 1) & 1, wc);
+      tc_fence_after_sync();
+      tmem_st_32x32(t_p, w);
       float l0, l1;
       unpair_f32(add_f32x2(sum[0], sum[1]), l0, l1);
       l += l0 + l1;
@@ -511,16 +525,7 @@ attn_tile_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constan
     tc_fence_after_sync();
 
     // -------------------------------------------------------------------- epilogue: a thread has half of its row's features
-    tmem_st_1(t_swap + half, l);   // the sum of the row's two threads
-    tmem_st_wait();
-    tc_fence_before_sync();
-    named_bar_sync(pair, 64);
-    tc_fence_after_sync();
-    {
-      const float other = tmem_ld_1(t_swap + (half ^ 1));
-      tmem_ld_wait();
-      l = half == 0 ? l + other : other + l;
-    }
+    l = pair_combine<true>(swap, pair, half, l);   // the sum of the row's two threads
     // Accumulators of the even and the odd tiles are joined in the first one's threads.
     float f0 = 1.0f, f1 = 0.0f;
     const bool join = !two && n_tiles > 1;
