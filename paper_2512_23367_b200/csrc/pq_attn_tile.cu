@@ -15,8 +15,6 @@ constexpr int kSoft = 512;
 constexpr int kIssuer = 16, kLoadK = 17, kWatcher = 18, kLoadV = 19;   // warps
 constexpr int kSoftRegs = 104, kRestRegs = 64;   // 512 x 104 + 128 x 64 = 640 x 96, what the launch holds
 
-constexpr int kPolyEvery = 4;       // every 4th pair of weights on the FMA pipe instead of the special-function unit
-
 template <int D>
 struct TileCfg {
   static constexpr int kTileBytes = kTile * D * 2;            // one operand tile: D / 64 panels of 128 rows x 128 B
@@ -131,26 +129,6 @@ __device__ __forceinline__ float max3(float a, float b, float c) {
   asm("max.f32 %0, %1, %2, %3;" : "=f"(d) : "f"(a), "f"(b), "f"(c));
   return d;
 }
-// 2^x for x <= 9 on the FMA pipe, two at a time: x = n + f with n = rne(x) (taken as (x + 1.5 * 2^23) - 1.5 * 2^23,
-// whose low mantissa bits are n), 2^f by a degree-4 polynomial, and n added to the exponent.  Coefficients: least
-// squares of the relative error over [-1/2, 1/2], reweighted towards its largest values (2.6e-6, against 2.4e-4 for
-// the FP16 rounding that follows).  Below 2^-125 the result is 2^-125, which rounds to 0 in FP16.
-__device__ __forceinline__ uint64_t exp2_poly2(uint64_t x) {
-  float x0, x1;
-  unpair_f32(x, x0, x1);
-  x = pair_f32(fmaxf(x0, -125.0f), fmaxf(x1, -125.0f));
-  const uint64_t t = add_f32x2(x, pair_f32(12582912.0f, 12582912.0f));
-  const uint64_t f = fma_f32x2(add_f32x2(t, pair_f32(-12582912.0f, -12582912.0f)), pair_f32(-1.0f, -1.0f), x);
-  uint64_t p = fma_f32x2(pair_f32(0.009570102207362652f, 0.009570102207362652f), f, pair_f32(0.05591785907745361f, 0.05591785907745361f));
-  p = fma_f32x2(p, f, pair_f32(0.240247443318367f, 0.240247443318367f));
-  p = fma_f32x2(p, f, pair_f32(0.6931217908859253f, 0.6931217908859253f));
-  p = fma_f32x2(p, f, pair_f32(0.9999992847442627f, 0.9999992847442627f));
-  float p0, p1, t0, t1;
-  unpair_f32(p, p0, p1);
-  unpair_f32(t, t0, t1);
-  return pair_f32(__int_as_float(__float_as_int(p0) + (__float_as_int(t0) << 23)), __int_as_float(__float_as_int(p1) + (__float_as_int(t1) << 23)));
-}
-
 // A wait of a whole warp whose lanes go on, or give up, together.
 __device__ __forceinline__ bool warp_wait(uint32_t bar, uint32_t parity, const WaitCtx& wc) {
   return __all_sync(0xffffffffu, mbar_wait(bar, parity, wc));
@@ -496,18 +474,12 @@ attn_tile_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constan
 #pragma unroll
       for (int j = 0; j < 32; ++j) {
         const int q = j >> 4, e = (2 * j) & 31;
-        uint64_t x = fma_f32x2(pair_f32(__uint_as_float(s[q][e]), __uint_as_float(s[q][e + 1])), sc2, ms2);
+        const uint64_t x = fma_f32x2(pair_f32(__uint_as_float(s[q][e]), __uint_as_float(s[q][e + 1])), sc2, ms2);
         float e0, e1;
-        if (j % kPolyEvery == kPolyEvery - 1) {
-          x = exp2_poly2(x);
-          unpair_f32(x, e0, e1);
-        } else {
-          unpair_f32(x, e0, e1);
-          e0 = exp2_approx(e0);
-          e1 = exp2_approx(e1);
-          x = pair_f32(e0, e1);
-        }
-        sum[j & 1] = add_f32x2(sum[j & 1], x);
+        unpair_f32(x, e0, e1);
+        e0 = exp2_approx(e0);
+        e1 = exp2_approx(e1);
+        sum[j & 1] = add_f32x2(sum[j & 1], pair_f32(e0, e1));
         w[j] = pack_f16(e0, e1);
         if (j == 15) asked = mbar_test2(bar_o + 8 * acc, (i - 1) & 1, bar_o + 8 * acc, (i - 1) & 1);
       }
