@@ -57,6 +57,23 @@ __device__ __forceinline__ float exp2_approx(float x) {
   return y;
 }
 
+__device__ __forceinline__ uint32_t pack_f16(float a, float b) {
+  const __half2 h = __floats2half2_rn(a, b);
+  return *reinterpret_cast<const uint32_t*>(&h);
+}
+// Four INT8 codes, offset by 128 (bytes u = code + 128), as FP16: 0x6400 | u is 1024 + u, and 1024 + u - 1152 is the
+// code, exactly.  sel picks the two bytes.
+__device__ __forceinline__ uint32_t codes_f16(uint32_t u, uint32_t sel) {
+  const uint32_t h = __byte_perm(u, 0x64646464u, sel);
+  const __half2 r = __hsub2(*reinterpret_cast<const __half2*>(&h), __half2(__ushort_as_half(0x6480), __ushort_as_half(0x6480)));
+  return *reinterpret_cast<const uint32_t*>(&r);
+}
+// The smallest power of two >= v (at least 2^-126): the unit that a run of INT8 value scales is taken in.
+__device__ __forceinline__ float scale_unit(float v) {
+  const uint32_t u = (__float_as_uint(fminf(fmaxf(v, 0.0f), 1e37f)) + 0x7fffffu) & 0x7f800000u;
+  return __uint_as_float(u < 0x00800000u ? 0x00800000u : u);
+}
+
 // Keys [lo, hi) that a request's rows may see: lo from the window of its first row, hi from its length and its table.
 struct AttnRange {
   int n, L, lo, hi;

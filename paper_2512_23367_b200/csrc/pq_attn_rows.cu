@@ -67,18 +67,6 @@ __device__ __forceinline__ void mma16816(float (&d)[4], const uint32_t (&a)[4], 
                : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
                : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
 }
-// Four INT8 codes, offset by 128 (bytes u = code + 128), as FP16: 0x6400 | u is 1024 + u, and 1024 + u - 1152 is the
-// code, exactly.  sel picks the two bytes.
-__device__ __forceinline__ uint32_t codes_f16(uint32_t u, uint32_t sel) {
-  const uint32_t h = __byte_perm(u, 0x64646464u, sel);
-  const __half2 r = __hsub2(*reinterpret_cast<const __half2*>(&h), __half2(__ushort_as_half(0x6480), __ushort_as_half(0x6480)));
-  return *reinterpret_cast<const uint32_t*>(&r);
-}
-__device__ __forceinline__ uint32_t pack_f16(float a, float b) {
-  const __half2 h = __floats2half2_rn(a, b);
-  return *reinterpret_cast<const uint32_t*>(&h);
-}
-
 // HBM bound: every cached key and value is read once, 2 * dim * (2 | 1 + 4 / dim) bytes per key and head, against
 // 16 rows' worth of arithmetic at most, of which the tensor cores do the products (m16n8k16: the rows of a group
 // of query heads and of a draft's tokens share one tile).
@@ -317,7 +305,7 @@ __global__ void __launch_bounds__(kWarps * 32, 2) attn_rows_kernel(const AttnArg
         l[i] *= f[i];
       }
       if (kInt8 && vtop > vref) {   // the same in every lane: all rows share the keys
-        const float vn = __uint_as_float((__float_as_uint(fminf(vtop, 1e37f)) + 0x7fffffu) & 0x7f800000u);
+        const float vn = scale_unit(vtop);
         const float fv = vref / vn;
         vref = vn;
         f[0] *= fv, f[1] *= fv;

@@ -10,18 +10,25 @@ namespace pq {
 namespace {
 
 constexpr int kTile = 128;          // query rows of one accumulator, keys of one step
-constexpr int kThreads = 640;       // four softmax warpgroups, two per accumulator; issuer, two producers, watcher
-constexpr int kSoft = 512;
-constexpr int kIssuer = 16, kLoadK = 17, kWatcher = 18, kLoadV = 19;   // warps
-constexpr int kSoftRegs = 104, kRestRegs = 64;   // 512 x 104 + 128 x 64 = 640 x 96, what the launch holds
+constexpr int kSoft = 512;          // threads of the four softmax warpgroups, two per accumulator
+constexpr int kIssuer = 16, kLoadK = 17, kWatcher = 18, kLoadV = 19;   // warps; from 20 on the INT8 converters
 
-template <int D>
+template <bool kInt8, int D>
 struct TileCfg {
+  static constexpr int kThreads = kInt8 ? 768 : 640;
+  // Registers: softmax, issuer's warpgroup, converters.  512 x 104 + 128 x 64 = 640 x 96 and
+  // 512 x 96 + 128 x 40 + 128 x 56 = 768 x 80, what the launch holds.
+  static constexpr int kSoftRegs = kInt8 ? 96 : 104, kRestRegs = kInt8 ? 40 : 64, kConvRegs = 56;
+  static constexpr int kRegsNeeded = kSoft * kSoftRegs + 128 * kRestRegs + (kInt8 ? 128 * kConvRegs : 0);
   static constexpr int kTileBytes = kTile * D * 2;            // one operand tile: D / 64 panels of 128 rows x 128 B
   static constexpr int kPanel = kTile * 128;
-  static constexpr int kStages = 163840 / kTileBytes;         // 5 (D = 128) or 10: keys and values alternate
+  static constexpr int kStages = (kInt8 ? 131072 : 163840) / kTileBytes;   // keys and values alternate
+  // INT8: scales of a tile (keys', values', and the values' units of 32 keys each).  Tile t is written when V of tile
+  // t - kStages / 2 - 1 has been given back, so its softmax is over.
+  static constexpr int kScaleTiles = kInt8 ? kStages / 2 + 1 : 0;
+  static constexpr int kScaleFloats = 2 * kTile + 4;
   static constexpr int kBars = 2 * kStages + 7;
-  static constexpr int kSmem = 2 * kTileBytes + kStages * kTileBytes + 1024 /* alignment */;
+  static constexpr int kSmem = (2 + kStages) * kTileBytes + kScaleTiles * kScaleFloats * 4 + 1024 /* alignment */;
 };
 
 // ---- tcgen05 with 16-bit floating-point operands
@@ -69,11 +76,6 @@ __device__ __forceinline__ void tmem_st_32x16(uint32_t taddr, const uint32_t (&r
       : "memory");
 }
 __device__ __forceinline__ void tmem_st_wait() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
-
-__device__ __forceinline__ uint32_t pack_f16(float a, float b) {
-  const __half2 h = __floats2half2_rn(a, b);
-  return *reinterpret_cast<const uint32_t*>(&h);
-}
 
 __device__ __forceinline__ void named_bar_arrive(uint32_t id, uint32_t nthreads) {
   asm volatile("bar.arrive %0, %1;" ::"r"(id), "r"(nthreads) : "memory");
@@ -124,6 +126,16 @@ __device__ __forceinline__ uint64_t add_f32x2(uint64_t a, uint64_t b) {
   asm("add.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b));
   return d;
 }
+__device__ __forceinline__ uint64_t mul_f32x2(uint64_t a, uint64_t b) {
+  uint64_t d;
+  asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b));
+  return d;
+}
+__device__ __forceinline__ float4 lds_f4(uint32_t addr) {
+  float4 v;
+  asm volatile("ld.shared.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w) : "r"(addr) : "memory");
+  return v;
+}
 __device__ __forceinline__ float max3(float a, float b, float c) {
   float d;
   asm("max.f32 %0, %1, %2, %3;" : "=f"(d) : "f"(a), "f"(b), "f"(c));
@@ -160,10 +172,17 @@ struct TileArgs {
 // no visible key needs, or of an unusable page id, are requested beyond the tensor and arrive as zeros.
 // Value rows that were never written (beyond the request's length, before its window) are zeroed in shared memory:
 // their weight is 0, but 0 x NaN is not.
-template <int D>
-__global__ void __launch_bounds__(kThreads, 1)
+//
+// INT8: a warpgroup of converters takes the place of the TMA producers.  A thread keeps one tile's share of the codes
+// in flight in registers, turns them into FP16 (exact) and stores them in the layout that TMA would have left.  The
+// key's scale (times the softmax scale) multiplies the score.  The value's scale multiplies the weight before it is
+// rounded, relative to the power of two above the largest scale of its 32 keys, and the quotient of that unit and
+// the running unit of O goes into the exponent, exactly.
+template <bool kInt8, int D>
+__global__ void __launch_bounds__((TileCfg<kInt8, D>::kThreads), 1)
 attn_tile_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtensorMap map_v, const TileArgs ta) {
-  using C = TileCfg<D>;
+  using C = TileCfg<kInt8, D>;
+  constexpr int kThreads = C::kThreads;
   constexpr int KS = D / 16;        // MMAs of one QK
   constexpr int PS = kTile / 16;    // MMAs of one PV
   extern __shared__ uint8_t smem_raw[];
@@ -187,7 +206,7 @@ attn_tile_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constan
   const uint32_t bar_s = bar0 + 16 * C::kStages, bar_o = bar_s + 16;   // two of each
   const uint32_t bar_q = bar_o + 16, bar_fix = bar_q + 8, bar_drain = bar_fix + 8;
   if (tid == 0) {
-    for (int i = 0; i < C::kStages; ++i) mbar_init(bar_full + 8 * i, 1), mbar_init(bar_free + 8 * i, 1);
+    for (int i = 0; i < C::kStages; ++i) mbar_init(bar_full + 8 * i, kInt8 ? 4 : 1), mbar_init(bar_free + 8 * i, 1);
     for (int i = 0; i < 2; ++i) mbar_init(bar_s + 8 * i, 1), mbar_init(bar_o + 8 * i, 1);
     mbar_init(bar_q, kSoft / 32);
     mbar_init(bar_fix, 1);
@@ -195,8 +214,7 @@ attn_tile_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constan
     fence_mbar_init();
     s_abort = 0;
     s_assign[0] = -1;
-    tma_prefetch_desc(&map_k);
-    tma_prefetch_desc(&map_v);
+    if (!kInt8) tma_prefetch_desc(&map_k), tma_prefetch_desc(&map_v);
   }
   grid_dep_wait();
   __syncthreads();
@@ -255,7 +273,7 @@ attn_tile_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constan
   const int lag = two ? 2 : 1;
 
   const uint32_t base = (smem_u32(smem_raw) + 1023u) & ~1023u;
-  const uint32_t sq = base, ring = base + 2 * C::kTileBytes;
+  const uint32_t sq = base, ring = base + 2 * C::kTileBytes, scales = ring + C::kStages * C::kTileBytes;
   if (warp == kIssuer) tmem_alloc(smem_u32(&s_tmem), 512);
   tc_fence_before_sync();
   __syncthreads();
@@ -265,9 +283,91 @@ attn_tile_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constan
   const WaitCtx wc{&s_abort, ta.wait_limit};
   int issued = 0;   // producers: tiles requested so far
 
-  if (warp >= kSoft / 32) {
-    asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kRestRegs));
-    if (warp == kLoadK || warp == kLoadV) {
+  if (kInt8 && warp >= 20) {
+    // -------------------------------------------------------------------- INT8 converters
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(C::kConvRegs));
+    if constexpr (kInt8) {
+      constexpr int kRow = D / 16;                      // 16-byte pieces of one key
+      constexpr int kItems = kTile * kRow / 128;        // of a thread per tile
+      const int c = tid - 20 * 32;
+      const int piece = c % kRow, row_in = c / kRow;    // item k: row k * (128 / kRow) + row_in
+      const int* trow = a.table + static_cast<int64_t>(b) * a.width;
+      // First cache vector of each of the tile's eight blocks of 16 keys (lane & 7); -1: nothing to read.
+      auto vectors_of = [&](int t) {
+        const int key = key_base + t * kTile + (lane & 7) * 16;
+        if (t >= n_tiles || key >= rg.hi || key + 16 <= rg.lo) return -1;
+        const int col = key / a.c.page;
+        const int id = trow[col];
+        if (id < 0 || id >= a.c.pages) return -1;
+        return static_cast<int>((static_cast<int64_t>(id) * a.c.heads + hk) * a.c.page) + key - col * a.c.page;
+      };
+      uint4 buf[kItems];
+      int vec = vectors_of(0), vec_next = -1;
+      auto item = [&](int k, const void* codes, int v) {
+        const int r = k * (128 / kRow) + row_in;
+        const int first = __shfl_sync(0xffffffffu, v, r >> 4);
+        return first < 0 ? make_uint4(0x0u, 0x0u, 0x0u, 0x0u)
+                         : __ldg(static_cast<const uint4*>(codes) + (static_cast<int64_t>(first) + (r & 15)) * kRow + piece);
+      };
+      // Scales of key c of a tile; 0 where nothing was written.
+      float ks = 0.0f, vs = 0.0f;
+      auto load_scales = [&](int t, int v) {
+        const int first = __shfl_sync(0xffffffffu, v, c >> 4);
+        const int key = key_base + t * kTile + c;
+        const bool there = first >= 0 && key >= rg.lo && key < rg.hi;
+        ks = there ? __ldg(a.c.k_scale + first + (c & 15)) * a.scale_log2 : 0.0f;
+        vs = there ? __ldg(a.c.v_scale + first + (c & 15)) : 0.0f;
+      };
+#pragma unroll
+      for (int k = 0; k < kItems; ++k) buf[k] = item(k, a.c.k, vec);
+      load_scales(0, vec);
+      bool ok = true;
+      for (int i = 0; i < 2 * n_tiles; ++i) {
+        const int st = i % C::kStages, t = i >> 1;
+        const bool is_v = i & 1;
+        if (!is_v) vec_next = vectors_of(t + 1);
+        if (i >= C::kStages) ok = ok && warp_wait(bar_free + 8 * st, ((i / C::kStages) & 1) ^ 1, wc);
+        const uint32_t dst = ring + st * C::kTileBytes;
+        const void* next_codes = is_v ? a.c.k : a.c.v;
+        const int next_vec = is_v ? vec_next : vec;
+#pragma unroll
+        for (int k = 0; k < kItems; ++k) {
+          const int r = k * (128 / kRow) + row_in;
+          const uint32_t u[4] = {buf[k].x ^ 0x80808080u, buf[k].y ^ 0x80808080u, buf[k].z ^ 0x80808080u, buf[k].w ^ 0x80808080u};
+          // 16 codes are two 16-byte pieces of the FP16 row; half of the threads store the second one first, so that
+          // eight neighbours hit all banks
+#pragma unroll
+          for (int h = 0; h < 2; ++h) {
+            const int second = h ^ ((piece >> 2) & 1);
+            const uint32_t w0 = second ? u[2] : u[0], w1 = second ? u[3] : u[1];
+            const int ch = 2 * piece + second;
+            asm volatile("st.shared.v4.u32 [%0], {%1, %2, %3, %4};" ::"r"(dst + (ch >> 3) * C::kPanel + r * 128 + (((ch & 7) ^ (r & 7)) << 4)),
+                         "r"(codes_f16(w0, 0x4140)), "r"(codes_f16(w0, 0x4342)), "r"(codes_f16(w1, 0x4140)), "r"(codes_f16(w1, 0x4342)) : "memory");
+          }
+          if (i + 1 < 2 * n_tiles) buf[k] = item(k, next_codes, next_vec);
+        }
+        if (!is_v) {
+          float top = vs;
+#pragma unroll
+          for (int o = 16; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
+          const float unit = scale_unit(top);
+          const uint32_t s0 = scales + (t % C::kScaleTiles) * (C::kScaleFloats * 4);
+          const float rel = vs * __uint_as_float(0x7f000000u - __float_as_uint(unit));   // vs / unit, a power of two
+          asm volatile("st.shared.f32 [%0], %1;" ::"r"(s0 + 4 * c), "f"(ks) : "memory");
+          asm volatile("st.shared.f32 [%0], %1;" ::"r"(s0 + 4 * (kTile + c)), "f"(rel) : "memory");
+          if (lane == 0) asm volatile("st.shared.f32 [%0], %1;" ::"r"(s0 + 4 * (2 * kTile + (c >> 5))), "f"(unit) : "memory");
+        } else {
+          vec = vec_next;
+          load_scales(t + 1, vec);
+        }
+        fence_proxy_async_smem();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(bar_full + 8 * st);
+      }
+    }
+  } else if (warp >= kSoft / 32) {
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(C::kRestRegs));
+    if (!kInt8 && (warp == kLoadK || warp == kLoadV)) {
       // ------------------------------------------------------------------ producers, one for keys and one for values
       // A lane requests one box; its page id is looked up a tile ahead.
       const bool is_v = warp == kLoadV;
@@ -358,7 +458,7 @@ attn_tile_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constan
           __syncwarp();
         }
       }
-    } else {
+    } else if (warp == kWatcher) {
       // ------------------------------------------------------------------ watcher: waits for the operand tiles a step ahead
       bool ok = true;
       for (int u = 0; u < N + lag; ++u) {
@@ -374,7 +474,7 @@ attn_tile_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constan
     }
   } else {
     // -------------------------------------------------------------------- softmax, two threads per row
-    asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kSoftRegs));
+    asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(C::kSoftRegs));
     const int acc = warp >> 3;                       // accumulator
     const int half = (warp >> 2) & 1;                // the thread's 64 keys of a tile, and its half of the features
     const int r = tid & 127;                         // row of the tile
@@ -412,7 +512,9 @@ attn_tile_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constan
     const int all_to = min(p_base + q_tile * tpt + 1, rg.hi);                // every row of the tile sees [all_from, all_to)
     const int all_from = a.window > 0 ? p_base + toks - a.window : 0;
     const int mine = two ? n_tiles : (n_tiles - acc + 1) >> 1;
-    const float sc = a.scale_log2;
+    const float sc = kInt8 ? 1.0f : a.scale_log2;   // INT8: in the keys' scales
+    float vref = 1.0f;               // INT8: the unit of O; 0 as long as there is none
+    if (kInt8) vref = 0.0f;
     float m = -INFINITY, l = 0.0f;   // m: the reference that is subtracted, in powers of two; l: the thread's own keys
 
     bool ok = true;
@@ -426,6 +528,22 @@ attn_tile_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constan
       tmem_ld_wait();
       tc_fence_before_sync();
       named_bar_arrive(kBarRead, 288);
+      const uint32_t sct = scales + (((key0 - key_base) / kTile) % (kInt8 ? C::kScaleTiles : 1)) * (C::kScaleFloats * 4) + half * 256;
+      float units[2] = {1.0f, 1.0f}, vtop = 0.0f;
+      if constexpr (kInt8) {
+#pragma unroll
+        for (int j = 0; j < 64; j += 4) {
+          const float4 k = lds_f4(sct + 4 * j);
+          uint32_t* v = &s[j >> 5][j & 31];
+          float x0, x1, x2, x3;
+          unpair_f32(mul_f32x2(pair_f32(__uint_as_float(v[0]), __uint_as_float(v[1])), pair_f32(k.x, k.y)), x0, x1);
+          unpair_f32(mul_f32x2(pair_f32(__uint_as_float(v[2]), __uint_as_float(v[3])), pair_f32(k.z, k.w)), x2, x3);
+          v[0] = __float_as_uint(x0), v[1] = __float_as_uint(x1), v[2] = __float_as_uint(x2), v[3] = __float_as_uint(x3);
+        }
+        const float4 u = lds_f4(sct - half * 256 + 8 * kTile);
+        units[0] = half ? u.z : u.x, units[1] = half ? u.w : u.y;
+        vtop = fmaxf(fmaxf(u.x, u.y), fmaxf(u.z, u.w));
+      }
       if (key0 < all_from || key0 + kTile > all_to) {
         const int to = see_to - key0, from = see_from - key0;
 #pragma unroll
@@ -446,12 +564,16 @@ attn_tile_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constan
       }
       bool done = i == 0;   // the product with the weights before these has been taken
       float t = fmaxf(max3(top[0], top[1], top[2]), top[3]) * sc;
-      if (pair_any(pair, t > m + 8.0f)) {   // rare after the first tiles: some row of the 32 moves its reference
+      if (pair_any(pair, t > m + 8.0f || (kInt8 && vtop > vref))) {   // rare after the first tiles: some row of the 32 moves its reference
         t = pair_combine<false>(swap, pair, half, t);
         const bool grown = t > m + 8.0f;
-        const float f = grown ? (m == -INFINITY ? 0.0f : exp2_approx(m - t)) : 1.0f;
+        float f = grown ? (m == -INFINITY ? 0.0f : exp2_approx(m - t)) : 1.0f;
         if (grown) m = t;
         l *= f;
+        if (kInt8 && vtop > vref) {   // the same in every thread
+          f *= vref / vtop;
+          vref = vtop;
+        }
         if (i > 0) {   // O holds the sums up to the tile before
           ok = ok && warp_wait(bar_o + 8 * acc, (i - 1) & 1, wc);
           done = true;
@@ -468,27 +590,38 @@ attn_tile_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constan
         }
       }
       const float ms = m == -INFINITY ? 0.0f : m;
-      const uint64_t sc2 = pair_f32(sc, sc), ms2 = pair_f32(-ms, -ms);
-      uint64_t sum[2] = {0, 0};
+      const uint64_t sc2 = pair_f32(sc, sc);
       uint32_t w[32], asked = 0;
 #pragma unroll
-      for (int j = 0; j < 32; ++j) {
-        const int q = j >> 4, e = (2 * j) & 31;
-        const uint64_t x = fma_f32x2(pair_f32(__uint_as_float(s[q][e]), __uint_as_float(s[q][e + 1])), sc2, ms2);
-        float e0, e1;
-        unpair_f32(x, e0, e1);
-        e0 = exp2_approx(e0);
-        e1 = exp2_approx(e1);
-        sum[j & 1] = add_f32x2(sum[j & 1], pair_f32(e0, e1));
-        w[j] = pack_f16(e0, e1);
-        if (j == 15) asked = mbar_test2(bar_o + 8 * acc, (i - 1) & 1, bar_o + 8 * acc, (i - 1) & 1);
+      for (int q = 0; q < 2; ++q) {
+        // INT8: weights in units of units[q] / vref, a power of two <= 1 (2^-60 at least, where all weights round to 0)
+        const int shift = kInt8 ? max(static_cast<int>(__float_as_uint(units[q]) >> 23) - static_cast<int>(__float_as_uint(vref) >> 23), -60) : 0;
+        const float off = kInt8 ? static_cast<float>(shift) - ms : -ms;
+        const uint64_t off2 = pair_f32(off, off);
+        uint64_t sum = 0;
+#pragma unroll
+        for (int j = 0; j < 16; ++j) {
+          const uint64_t x = fma_f32x2(pair_f32(__uint_as_float(s[q][2 * j]), __uint_as_float(s[q][2 * j + 1])), sc2, off2);
+          float e0, e1;
+          unpair_f32(x, e0, e1);
+          e0 = exp2_approx(e0);
+          e1 = exp2_approx(e1);
+          sum = add_f32x2(sum, pair_f32(e0, e1));
+          if constexpr (kInt8) {
+            float2 v;
+            asm volatile("ld.shared.v2.f32 {%0, %1}, [%2];" : "=f"(v.x), "=f"(v.y) : "r"(sct + 4 * (kTile + 32 * q + 2 * j)) : "memory");
+            unpair_f32(mul_f32x2(pair_f32(e0, e1), pair_f32(v.x, v.y)), e0, e1);
+          }
+          w[16 * q + j] = pack_f16(e0, e1);
+        }
+        if (q == 0) asked = mbar_test2(bar_o + 8 * acc, (i - 1) & 1, bar_o + 8 * acc, (i - 1) & 1);
+        float l0, l1;
+        unpair_f32(sum, l0, l1);
+        l += kInt8 ? (l0 + l1) * __uint_as_float(static_cast<uint32_t>(127 - shift) << 23) : l0 + l1;
       }
       if (!done && !__all_sync(0xffffffffu, asked)) ok = ok && warp_wait(bar_o + 8 * acc, (i - 1) & 1, wc);
       tc_fence_after_sync();
       tmem_st_32x32(t_p, w);
-      float l0, l1;
-      unpair_f32(add_f32x2(sum[0], sum[1]), l0, l1);
-      l += l0 + l1;
       tmem_st_wait();
       tc_fence_before_sync();
       named_bar_arrive(kBarP + acc, 288);
@@ -513,8 +646,8 @@ attn_tile_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constan
           tmem_ld_wait();
 #pragma unroll
           for (int j = 0; j < 4; ++j)
-            room[(4 * h + j) * kTile + r] = make_float4(__uint_as_float(o[4 * j]), __uint_as_float(o[4 * j + 1]),
-                                                        __uint_as_float(o[4 * j + 2]), __uint_as_float(o[4 * j + 3]));
+            room[(4 * h + j) * kTile + r] = make_float4(__uint_as_float(o[4 * j]) * vref, __uint_as_float(o[4 * j + 1]) * vref,
+                                                        __uint_as_float(o[4 * j + 2]) * vref, __uint_as_float(o[4 * j + 3]) * vref);
         }
         if (half == 0) room_ml[r] = make_float2(m, l);
       }
@@ -527,6 +660,7 @@ attn_tile_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constan
         m = M;
       }
     }
+    f0 *= vref;
     const bool writes = two || acc == 0;
     const int64_t unit = blockIdx.x;
     constexpr int kPart = 2 * kTile * (D + 2);   // floats of one part: per tile [D / 4][128] x 4, then [128] x 2
@@ -618,7 +752,7 @@ attn_tile_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constan
   if (s_abort) {
     // Some role gave up.  What has been handed to the hardware still completes by itself and must have done so
     // before shared and tensor memory go away: the producer's loads and the issuer's MMAs.
-    if (lane == 0 && (warp == kLoadK || warp == kLoadV)) {
+    if (!kInt8 && lane == 0 && (warp == kLoadK || warp == kLoadV)) {
       for (int i = 2 * issued + (warp == kLoadV) - 2; i >= 0 && i >= 2 * issued - C::kStages; i -= 2)
         mbar_drain(bar_full + 8 * (i % C::kStages), (i / C::kStages) & 1u);
       if (warp == kLoadV) mbar_drain(bar_fix, 0u);
@@ -636,25 +770,27 @@ attn_tile_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constan
   }
 }
 
-template <int D>
+template <bool kInt8, int D>
 int launch(TileArgs& t, const TilePlan& plan, cudaStream_t stream) {
-  using C = TileCfg<D>;
-  auto kern = attn_tile_kernel<D>;
+  using C = TileCfg<kInt8, D>;
+  auto kern = attn_tile_kernel<kInt8, D>;
   static PerDeviceOnce once;
   if (const int rc = set_dynamic_smem_once(once, kern, C::kSmem); rc != PQ_OK) return rc;
   // The kernel's register split draws on what the launch holds: a build whose launch holds less must not run.
   static const int regs = [] {
     cudaFuncAttributes f = {};
-    return cudaFuncGetAttributes(&f, attn_tile_kernel<D>) == cudaSuccess ? f.numRegs : 0;
+    return cudaFuncGetAttributes(&f, attn_tile_kernel<kInt8, D>) == cudaSuccess ? f.numRegs : 0;
   }();
-  if (regs * kThreads < kSoft * kSoftRegs + (kThreads - kSoft) * kRestRegs) return PQ_ERR_CUDA;
-  CUtensorMap mk, mv;
+  if (regs * C::kThreads < C::kRegsNeeded) return PQ_ERR_CUDA;
+  CUtensorMap mk = {}, mv = {};
   const pq_kv_cache& c = t.a.c;
-  const uint64_t rows = static_cast<uint64_t>(c.pages) * c.heads * c.page;
-  if (const int rc = make_tmap_2d(&mk, c.k, rows, D, t.box, 64, 2, 128); rc != PQ_OK) return rc;
-  if (const int rc = make_tmap_2d(&mv, c.v, rows, D, t.box, 64, 2, 128); rc != PQ_OK) return rc;
+  if (!kInt8) {
+    const uint64_t rows = static_cast<uint64_t>(c.pages) * c.heads * c.page;
+    if (const int rc = make_tmap_2d(&mk, c.k, rows, D, t.box, 64, 2, 128); rc != PQ_OK) return rc;
+    if (const int rc = make_tmap_2d(&mv, c.v, rows, D, t.box, 64, 2, 128); rc != PQ_OK) return rc;
+  }
   const dim3 grid(static_cast<unsigned>(plan.units), static_cast<unsigned>(plan.parts));
-  return launch_dependent(kern, grid, dim3(kThreads), C::kSmem, stream, mk, mv, t);
+  return launch_dependent(kern, grid, dim3(C::kThreads), C::kSmem, stream, mk, mv, t);
 }
 
 }  // namespace
@@ -701,7 +837,8 @@ int launch_attn_tile(const AttnArgs& a, const TilePlan& plan, cudaStream_t strea
     t.q_xor = 0x80008000u;
     t.a.scale_log2 = -a.scale_log2;
   }
-  return a.c.dim == 128 ? launch<128>(t, plan, stream) : launch<64>(t, plan, stream);
+  if (a.c.type == PQ_KV_INT8) return a.c.dim == 128 ? launch<true, 128>(t, plan, stream) : launch<true, 64>(t, plan, stream);
+  return a.c.dim == 128 ? launch<false, 128>(t, plan, stream) : launch<false, 64>(t, plan, stream);
 }
 
 }  // namespace pq
