@@ -28,7 +28,8 @@ struct TileCfg {
   static constexpr int kScaleTiles = kInt8 ? kStages / 2 + 1 : 0;
   static constexpr int kScaleFloats = 2 * kTile + 4;
   static constexpr int kBars = 2 * kStages + 7;
-  static constexpr int kSmem = (2 + kStages) * kTileBytes + kScaleTiles * kScaleFloats * 4 + 1024 /* alignment */;
+  static constexpr int kSmem = (2 + kStages) * kTileBytes + kScaleTiles * kScaleFloats * 4 +
+                               (kInt8 ? 16384 : 0) /* the converters' slots */ + 1024 /* alignment */;
 };
 
 // ---- tcgen05 with 16-bit floating-point operands
@@ -131,11 +132,6 @@ __device__ __forceinline__ uint64_t mul_f32x2(uint64_t a, uint64_t b) {
   asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b));
   return d;
 }
-__device__ __forceinline__ float4 lds_f4(uint32_t addr) {
-  float4 v;
-  asm volatile("ld.shared.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w) : "r"(addr) : "memory");
-  return v;
-}
 __device__ __forceinline__ float max3(float a, float b, float c) {
   float d;
   asm("max.f32 %0, %1, %2, %3;" : "=f"(d) : "f"(a), "f"(b), "f"(c));
@@ -173,8 +169,9 @@ struct TileArgs {
 // Value rows that were never written (beyond the request's length, before its window) are zeroed in shared memory:
 // their weight is 0, but 0 x NaN is not.
 //
-// INT8: a warpgroup of converters takes the place of the TMA producers.  A thread keeps one tile's share of the codes
-// in flight in registers, turns them into FP16 (exact) and stores them in the layout that TMA would have left.  The
+// INT8: a warpgroup of converters takes the place of the TMA producers.  A thread keeps eight asynchronous copies of
+// 16 codes in flight into slots of its own, turns the codes into FP16 (exact) and stores them in the layout that TMA
+// would have left.  (Copies into registers cost spills: 4000 cycles per operand tile.)  The
 // key's scale (times the softmax scale) multiplies the score.  The value's scale multiplies the weight before it is
 // rounded, relative to the power of two above the largest scale of its 32 keys, and the quotient of that unit and
 // the running unit of O goes into the exponent, exactly.
@@ -301,13 +298,18 @@ attn_tile_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constan
         if (id < 0 || id >= a.c.pages) return -1;
         return static_cast<int>((static_cast<int64_t>(id) * a.c.heads + hk) * a.c.page) + key - col * a.c.page;
       };
-      uint4 buf[kItems];
-      int vec = vectors_of(0), vec_next = -1;
-      auto item = [&](int k, const void* codes, int v) {
-        const int r = k * (128 / kRow) + row_in;
-        const int first = __shfl_sync(0xffffffffu, v, r >> 4);
-        return first < 0 ? make_uint4(0x0u, 0x0u, 0x0u, 0x0u)
-                         : __ldg(static_cast<const uint4*>(codes) + (static_cast<int64_t>(first) + (r & 15)) * kRow + piece);
+      int vec = vectors_of(0), vec_ahead = vectors_of(1);   // tiles t and t + 1
+      // Copies item k of load i into the thread's slot (its own: no other thread reads it), or zeros.
+      constexpr int kAhead = 8 / kItems;                // loads in flight: 8 slots of 16 bytes per thread
+      const uint32_t raw = scales + C::kScaleTiles * C::kScaleFloats * 4 + c * 16;
+      auto request = [&](int i, int k, int v) {
+        if (i < 2 * n_tiles) {
+          const int r = k * (128 / kRow) + row_in;
+          const int first = __shfl_sync(0xffffffffu, v, r >> 4);
+          const uint4* src = static_cast<const uint4*>((i & 1) ? a.c.v : a.c.k) + (static_cast<int64_t>(max(first, 0)) + (r & 15)) * kRow + piece;
+          asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(raw + ((i % kAhead) * kItems + k) * 2048), "l"(src), "r"(first < 0 ? 0 : 16) : "memory");
+        }
+        asm volatile("cp.async.commit_group;" ::: "memory");
       };
       // Scales of key c of a tile; 0 where nothing was written.
       float ks = 0.0f, vs = 0.0f;
@@ -319,32 +321,42 @@ attn_tile_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constan
         vs = there ? __ldg(a.c.v_scale + first + (c & 15)) : 0.0f;
       };
 #pragma unroll
-      for (int k = 0; k < kItems; ++k) buf[k] = item(k, a.c.k, vec);
+      for (int i = 0; i < kAhead; ++i) {
+#pragma unroll
+        for (int k = 0; k < kItems; ++k) request(i, k, vec);
+      }
       load_scales(0, vec);
       bool ok = true;
       for (int i = 0; i < 2 * n_tiles; ++i) {
         const int st = i % C::kStages, t = i >> 1;
         const bool is_v = i & 1;
-        if (!is_v) vec_next = vectors_of(t + 1);
         if (i >= C::kStages) ok = ok && warp_wait(bar_free + 8 * st, ((i / C::kStages) & 1) ^ 1, wc);
         const uint32_t dst = ring + st * C::kTileBytes;
-        const void* next_codes = is_v ? a.c.k : a.c.v;
-        const int next_vec = is_v ? vec_next : vec;
+        const int v_next = (i + kAhead) / 2 == t ? vec : vec_ahead;
 #pragma unroll
-        for (int k = 0; k < kItems; ++k) {
-          const int r = k * (128 / kRow) + row_in;
-          const uint32_t u[4] = {buf[k].x ^ 0x80808080u, buf[k].y ^ 0x80808080u, buf[k].z ^ 0x80808080u, buf[k].w ^ 0x80808080u};
-          // 16 codes are two 16-byte pieces of the FP16 row; half of the threads store the second one first, so that
-          // eight neighbours hit all banks
+        for (int k4 = 0; k4 < kItems; k4 += 4) {
+          asm volatile("cp.async.wait_group 4;" ::: "memory");
+          uint32_t u[4][4];
 #pragma unroll
-          for (int h = 0; h < 2; ++h) {
-            const int second = h ^ ((piece >> 2) & 1);
-            const uint32_t w0 = second ? u[2] : u[0], w1 = second ? u[3] : u[1];
-            const int ch = 2 * piece + second;
-            asm volatile("st.shared.v4.u32 [%0], {%1, %2, %3, %4};" ::"r"(dst + (ch >> 3) * C::kPanel + r * 128 + (((ch & 7) ^ (r & 7)) << 4)),
-                         "r"(codes_f16(w0, 0x4140)), "r"(codes_f16(w0, 0x4342)), "r"(codes_f16(w1, 0x4140)), "r"(codes_f16(w1, 0x4342)) : "memory");
+          for (int q = 0; q < 4; ++q)
+            asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(u[q][0]), "=r"(u[q][1]), "=r"(u[q][2]), "=r"(u[q][3])
+                         : "r"(raw + ((i % kAhead) * kItems + k4 + q) * 2048) : "memory");
+#pragma unroll
+          for (int q = 0; q < 4; ++q) {
+            const int r = (k4 + q) * (128 / kRow) + row_in;
+            // 16 codes are two 16-byte pieces of the FP16 row; half of the threads store the second one first, so that
+            // eight neighbours hit all banks
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+              const int second = h ^ ((piece >> 2) & 1);
+              const uint32_t w0 = (second ? u[q][2] : u[q][0]) ^ 0x80808080u, w1 = (second ? u[q][3] : u[q][1]) ^ 0x80808080u;
+              const int ch = 2 * piece + second;
+              asm volatile("st.shared.v4.u32 [%0], {%1, %2, %3, %4};" ::"r"(dst + (ch >> 3) * C::kPanel + r * 128 + (((ch & 7) ^ (r & 7)) << 4)),
+                           "r"(codes_f16(w0, 0x4140)), "r"(codes_f16(w0, 0x4342)), "r"(codes_f16(w1, 0x4140)), "r"(codes_f16(w1, 0x4342)) : "memory");
+            }
           }
-          if (i + 1 < 2 * n_tiles) buf[k] = item(k, next_codes, next_vec);
+#pragma unroll
+          for (int q = 0; q < 4; ++q) request(i + kAhead, k4 + q, v_next);
         }
         if (!is_v) {
           float top = vs;
@@ -357,7 +369,8 @@ attn_tile_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constan
           asm volatile("st.shared.f32 [%0], %1;" ::"r"(s0 + 4 * (kTile + c)), "f"(rel) : "memory");
           if (lane == 0) asm volatile("st.shared.f32 [%0], %1;" ::"r"(s0 + 4 * (2 * kTile + (c >> 5))), "f"(unit) : "memory");
         } else {
-          vec = vec_next;
+          vec = vec_ahead;
+          vec_ahead = vectors_of(t + 2);
           load_scales(t + 1, vec);
         }
         fence_proxy_async_smem();
@@ -528,19 +541,20 @@ attn_tile_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constan
       tmem_ld_wait();
       tc_fence_before_sync();
       named_bar_arrive(kBarRead, 288);
-      const uint32_t sct = scales + (((key0 - key_base) / kTile) % (kInt8 ? C::kScaleTiles : 1)) * (C::kScaleFloats * 4) + half * 256;
+      const float* sct = reinterpret_cast<const float*>(smem_raw + (scales - smem_u32(smem_raw))) +
+                         (((key0 - key_base) / kTile) % (kInt8 ? C::kScaleTiles : 1)) * C::kScaleFloats;
       float units[2] = {1.0f, 1.0f}, vtop = 0.0f;
       if constexpr (kInt8) {
 #pragma unroll
         for (int j = 0; j < 64; j += 4) {
-          const float4 k = lds_f4(sct + 4 * j);
+          const float4 k = *reinterpret_cast<const float4*>(sct + 64 * half + j);
           uint32_t* v = &s[j >> 5][j & 31];
           float x0, x1, x2, x3;
           unpair_f32(mul_f32x2(pair_f32(__uint_as_float(v[0]), __uint_as_float(v[1])), pair_f32(k.x, k.y)), x0, x1);
           unpair_f32(mul_f32x2(pair_f32(__uint_as_float(v[2]), __uint_as_float(v[3])), pair_f32(k.z, k.w)), x2, x3);
           v[0] = __float_as_uint(x0), v[1] = __float_as_uint(x1), v[2] = __float_as_uint(x2), v[3] = __float_as_uint(x3);
         }
-        const float4 u = lds_f4(sct - half * 256 + 8 * kTile);
+        const float4 u = *reinterpret_cast<const float4*>(sct + 2 * kTile);
         units[0] = half ? u.z : u.x, units[1] = half ? u.w : u.y;
         vtop = fmaxf(fmaxf(u.x, u.y), fmaxf(u.z, u.w));
       }
@@ -608,8 +622,7 @@ attn_tile_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constan
           e1 = exp2_approx(e1);
           sum = add_f32x2(sum, pair_f32(e0, e1));
           if constexpr (kInt8) {
-            float2 v;
-            asm volatile("ld.shared.v2.f32 {%0, %1}, [%2];" : "=f"(v.x), "=f"(v.y) : "r"(sct + 4 * (kTile + 32 * q + 2 * j)) : "memory");
+            const float2 v = *reinterpret_cast<const float2*>(sct + kTile + 64 * half + 32 * q + 2 * j);
             unpair_f32(mul_f32x2(pair_f32(e0, e1), pair_f32(v.x, v.y)), e0, e1);
           }
           w[16 * q + j] = pack_f16(e0, e1);
