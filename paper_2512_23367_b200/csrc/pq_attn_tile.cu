@@ -15,11 +15,12 @@ constexpr int kIssuer = 16, kLoadK = 17, kWatcher = 18, kLoadV = 19;   // warps;
 
 template <bool kInt8, int D>
 struct TileCfg {
-  static constexpr int kThreads = kInt8 ? 768 : 640;
+  static constexpr int kConv = kInt8 ? 256 : 0;                // converter threads
+  static constexpr int kThreads = 640 + kConv;
   // Registers: softmax, issuer's warpgroup, converters.  512 x 104 + 128 x 64 = 640 x 96 and
-  // 512 x 96 + 128 x 40 + 128 x 56 = 768 x 80, what the launch holds.
-  static constexpr int kSoftRegs = kInt8 ? 96 : 104, kRestRegs = kInt8 ? 40 : 64, kConvRegs = 56;
-  static constexpr int kRegsNeeded = kSoft * kSoftRegs + 128 * kRestRegs + (kInt8 ? 128 * kConvRegs : 0);
+  // 512 x 88 + 128 x 40 + 256 x 56 = 896 x 72, what the launch holds.
+  static constexpr int kSoftRegs = kInt8 ? 88 : 104, kRestRegs = kInt8 ? 40 : 64, kConvRegs = 56;
+  static constexpr int kRegsNeeded = kSoft * kSoftRegs + 128 * kRestRegs + kConv * kConvRegs;
   static constexpr int kTileBytes = kTile * D * 2;            // one operand tile: D / 64 panels of 128 rows x 128 B
   static constexpr int kPanel = kTile * 128;
   static constexpr int kStages = (kInt8 ? 131072 : 163840) / kTileBytes;   // keys and values alternate
@@ -29,7 +30,7 @@ struct TileCfg {
   static constexpr int kScaleFloats = 2 * kTile + 4;
   static constexpr int kBars = 2 * kStages + 7;
   static constexpr int kSmem = (2 + kStages) * kTileBytes + kScaleTiles * kScaleFloats * 4 +
-                               (kInt8 ? 16384 : 0) /* the converters' slots */ + 1024 /* alignment */;
+                               6 * 16 * kConv /* the converters' slots */ + 1024 /* alignment */;
 };
 
 // ---- tcgen05 with 16-bit floating-point operands
@@ -169,7 +170,7 @@ struct TileArgs {
 // Value rows that were never written (beyond the request's length, before its window) are zeroed in shared memory:
 // their weight is 0, but 0 x NaN is not.
 //
-// INT8: a warpgroup of converters takes the place of the TMA producers.  A thread keeps eight asynchronous copies of
+// INT8: two warpgroups of converters take the place of the TMA producers.  A thread keeps six asynchronous copies of
 // 16 codes in flight into slots of its own, turns the codes into FP16 (exact) and stores them in the layout that TMA
 // would have left.  (Copies into registers cost spills: 4000 cycles per operand tile.)  The
 // key's scale (times the softmax scale) multiplies the score.  The value's scale multiplies the weight before it is
@@ -203,7 +204,7 @@ attn_tile_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constan
   const uint32_t bar_s = bar0 + 16 * C::kStages, bar_o = bar_s + 16;   // two of each
   const uint32_t bar_q = bar_o + 16, bar_fix = bar_q + 8, bar_drain = bar_fix + 8;
   if (tid == 0) {
-    for (int i = 0; i < C::kStages; ++i) mbar_init(bar_full + 8 * i, kInt8 ? 4 : 1), mbar_init(bar_free + 8 * i, 1);
+    for (int i = 0; i < C::kStages; ++i) mbar_init(bar_full + 8 * i, kInt8 ? C::kConv / 32 : 1), mbar_init(bar_free + 8 * i, 1);
     for (int i = 0; i < 2; ++i) mbar_init(bar_s + 8 * i, 1), mbar_init(bar_o + 8 * i, 1);
     mbar_init(bar_q, kSoft / 32);
     mbar_init(bar_fix, 1);
@@ -285,65 +286,72 @@ attn_tile_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constan
     asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(C::kConvRegs));
     if constexpr (kInt8) {
       constexpr int kRow = D / 16;                      // 16-byte pieces of one key
-      constexpr int kItems = kTile * kRow / 128;        // of a thread per tile
+      constexpr int kItems = kTile * kRow / C::kConv;     // of a thread per tile: 4 or 2
       const int c = tid - 20 * 32;
-      const int piece = c % kRow, row_in = c / kRow;    // item k: row k * (128 / kRow) + row_in
+      constexpr int kStep = C::kConv / kRow;
+      const int piece = c % kRow, row_in = c / kRow;    // item k: row k * kStep + row_in
       const int* trow = a.table + static_cast<int64_t>(b) * a.width;
-      // First cache vector of each of the tile's eight blocks of 16 keys (lane & 7); -1: nothing to read.
-      auto vectors_of = [&](int t) {
+      // Page ids of the tile's eight blocks of 16 keys (lane & 7), fetched long before they are looked at; then the
+      // block's first cache vector, -1 where there is nothing to read.
+      auto fetch_id = [&](int t) {
         const int key = key_base + t * kTile + (lane & 7) * 16;
-        if (t >= n_tiles || key >= rg.hi || key + 16 <= rg.lo) return -1;
-        const int col = key / a.c.page;
-        const int id = trow[col];
-        if (id < 0 || id >= a.c.pages) return -1;
-        return static_cast<int>((static_cast<int64_t>(id) * a.c.heads + hk) * a.c.page) + key - col * a.c.page;
+        return t < n_tiles && key < rg.hi && key + 16 > rg.lo ? trow[key / a.c.page] : -1;
       };
-      int vec = vectors_of(0), vec_ahead = vectors_of(1);   // tiles t and t + 1
-      // Copies item k of load i into the thread's slot (its own: no other thread reads it), or zeros.
-      constexpr int kAhead = 8 / kItems;                // loads in flight: 8 slots of 16 bytes per thread
+      auto vectors_of = [&](int t, int id) {
+        const int key = key_base + t * kTile + (lane & 7) * 16;
+        return id < 0 || id >= a.c.pages ? -1 : static_cast<int>((static_cast<int64_t>(id) * a.c.heads + hk) * a.c.page) + key % a.c.page;
+      };
+      int id = fetch_id(3);
+      int vec = vectors_of(0, fetch_id(0)), vec1 = vectors_of(1, fetch_id(1)), vec2 = vectors_of(2, fetch_id(2));   // tiles t, t + 1, t + 2
+      // Work goes in batches of two items; the batch three further on is copied into the slots that one leaves (the
+      // thread's own: no other thread reads them), or zeros.
+      constexpr int kBatches = kItems / 2;              // per operand tile
       const uint32_t raw = scales + C::kScaleTiles * C::kScaleFloats * 4 + c * 16;
-      auto request = [&](int i, int k, int v) {
+      auto request = [&](int n, int v) {                // batch n of all
+        const int i = n / kBatches;
         if (i < 2 * n_tiles) {
-          const int r = k * (128 / kRow) + row_in;
-          const int first = __shfl_sync(0xffffffffu, v, r >> 4);
-          const uint4* src = static_cast<const uint4*>((i & 1) ? a.c.v : a.c.k) + (static_cast<int64_t>(max(first, 0)) + (r & 15)) * kRow + piece;
-          asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(raw + ((i % kAhead) * kItems + k) * 2048), "l"(src), "r"(first < 0 ? 0 : 16) : "memory");
+#pragma unroll
+          for (int q = 0; q < 2; ++q) {
+            const int r = ((n % kBatches) * 2 + q) * kStep + row_in;
+            const int first = __shfl_sync(0xffffffffu, v, r >> 4);
+            const uint4* src = static_cast<const uint4*>((i & 1) ? a.c.v : a.c.k) + (static_cast<int64_t>(max(first, 0)) + (r & 15)) * kRow + piece;
+            asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(raw + ((n % 3) * 2 + q) * (16 * C::kConv)), "l"(src), "r"(first < 0 ? 0 : 16) : "memory");
+          }
         }
         asm volatile("cp.async.commit_group;" ::: "memory");
       };
-      // Scales of key c of a tile; 0 where nothing was written.
+      // Scales of key c of the next tile, fetched a tile ahead; 0 where nothing was written.
       float ks = 0.0f, vs = 0.0f;
       auto load_scales = [&](int t, int v) {
         const int first = __shfl_sync(0xffffffffu, v, c >> 4);
         const int key = key_base + t * kTile + c;
-        const bool there = first >= 0 && key >= rg.lo && key < rg.hi;
-        ks = there ? __ldg(a.c.k_scale + first + (c & 15)) * a.scale_log2 : 0.0f;
-        vs = there ? __ldg(a.c.v_scale + first + (c & 15)) : 0.0f;
+        ks = 0.0f, vs = 0.0f;
+        if (first >= 0 && key >= rg.lo && key < rg.hi) ks = __ldg(a.c.k_scale + first + (c & 15)), vs = __ldg(a.c.v_scale + first + (c & 15));
       };
 #pragma unroll
-      for (int i = 0; i < kAhead; ++i) {
-#pragma unroll
-        for (int k = 0; k < kItems; ++k) request(i, k, vec);
-      }
-      load_scales(0, vec);
-      bool ok = true;
+      for (int n = 0; n < 3; ++n) request(n, n / kBatches < 2 ? vec : vec1);
+      if (c < kTile) load_scales(0, vec);
+      bool ok = true, free_next = false;
       for (int i = 0; i < 2 * n_tiles; ++i) {
         const int st = i % C::kStages, t = i >> 1;
         const bool is_v = i & 1;
-        if (i >= C::kStages) ok = ok && warp_wait(bar_free + 8 * st, ((i / C::kStages) & 1) ^ 1, wc);
+        if (i >= C::kStages && !free_next) ok = ok && warp_wait(bar_free + 8 * st, ((i / C::kStages) & 1) ^ 1, wc);
+        // asked a tile ahead: a wait that succeeds at once takes about 300 cycles
+        const int i1 = i + 1, st1 = i1 % C::kStages;
+        const uint32_t asked = i1 < C::kStages ? 1u : mbar_test2(bar_free + 8 * st1, ((i1 / C::kStages) & 1) ^ 1, bar_free + 8 * st1, ((i1 / C::kStages) & 1) ^ 1);
         const uint32_t dst = ring + st * C::kTileBytes;
-        const int v_next = (i + kAhead) / 2 == t ? vec : vec_ahead;
 #pragma unroll
-        for (int k4 = 0; k4 < kItems; k4 += 4) {
-          asm volatile("cp.async.wait_group 4;" ::: "memory");
-          uint32_t u[4][4];
+        for (int j = 0; j < kBatches; ++j) {
+          const int n = i * kBatches + j;
+          asm volatile("cp.async.wait_group 2;" ::: "memory");
+          uint32_t u[2][4];
 #pragma unroll
-          for (int q = 0; q < 4; ++q)
+          for (int q = 0; q < 2; ++q)
             asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(u[q][0]), "=r"(u[q][1]), "=r"(u[q][2]), "=r"(u[q][3])
-                         : "r"(raw + ((i % kAhead) * kItems + k4 + q) * 2048) : "memory");
+                         : "r"(raw + ((n % 3) * 2 + q) * (16 * C::kConv)) : "memory");
 #pragma unroll
-          for (int q = 0; q < 4; ++q) {
-            const int r = (k4 + q) * (128 / kRow) + row_in;
+          for (int q = 0; q < 2; ++q) {
+            const int r = (2 * j + q) * kStep + row_in;
             // 16 codes are two 16-byte pieces of the FP16 row; half of the threads store the second one first, so that
             // eight neighbours hit all banks
 #pragma unroll
@@ -355,24 +363,30 @@ attn_tile_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constan
                            "r"(codes_f16(w0, 0x4140)), "r"(codes_f16(w0, 0x4342)), "r"(codes_f16(w1, 0x4140)), "r"(codes_f16(w1, 0x4342)) : "memory");
             }
           }
-#pragma unroll
-          for (int q = 0; q < 4; ++q) request(i + kAhead, k4 + q, v_next);
+          const int ahead = ((n + 3) / kBatches) / 2 - t;   // tiles
+          request(n + 3, ahead == 0 ? vec : (ahead == 1 ? vec1 : vec2));
         }
-        if (!is_v) {
+        if (c >= kTile) {
+          // scales are the first four warps' work
+        } else if (!is_v) {
           float top = vs;
 #pragma unroll
           for (int o = 16; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
           const float unit = scale_unit(top);
           const uint32_t s0 = scales + (t % C::kScaleTiles) * (C::kScaleFloats * 4);
           const float rel = vs * __uint_as_float(0x7f000000u - __float_as_uint(unit));   // vs / unit, a power of two
-          asm volatile("st.shared.f32 [%0], %1;" ::"r"(s0 + 4 * c), "f"(ks) : "memory");
+          asm volatile("st.shared.f32 [%0], %1;" ::"r"(s0 + 4 * c), "f"(ks * a.scale_log2) : "memory");
           asm volatile("st.shared.f32 [%0], %1;" ::"r"(s0 + 4 * (kTile + c)), "f"(rel) : "memory");
           if (lane == 0) asm volatile("st.shared.f32 [%0], %1;" ::"r"(s0 + 4 * (2 * kTile + (c >> 5))), "f"(unit) : "memory");
-        } else {
-          vec = vec_ahead;
-          vec_ahead = vectors_of(t + 2);
-          load_scales(t + 1, vec);
         }
+        if (is_v) {
+          vec = vec1;
+          vec1 = vec2;
+          vec2 = vectors_of(t + 3, id);
+          id = fetch_id(t + 4);
+          if (c < kTile) load_scales(t + 1, vec);
+        }
+        free_next = __all_sync(0xffffffffu, asked);
         fence_proxy_async_smem();
         __syncwarp();
         if (lane == 0) mbar_arrive(bar_full + 8 * st);
