@@ -138,6 +138,32 @@ __device__ __forceinline__ float max3(float a, float b, float c) {
   asm("max.f32 %0, %1, %2, %3;" : "=f"(d) : "f"(a), "f"(b), "f"(c));
   return d;
 }
+// Blocks of 16 keys of one request, eight to a tile (`block` of them): the index of the block's first cache vector, tile
+// by tile, or -1 where there is nothing to read.  The page id of a tile is fetched while the one before is in use.
+template <bool kUsed>
+struct BlockWalk {
+  const int* trow;
+  int key, hi, lo, left, page16, col, off, step_col, step_off, heads, hk, id;
+  int64_t pages;
+  __device__ __forceinline__ BlockWalk(const AttnArgs& a, const AttnRange& rg, int b, int head, int key_base, int tiles, int block)
+      : trow(a.table + static_cast<int64_t>(b) * a.width), key(key_base + 16 * block), hi(rg.hi), lo(rg.lo), left(tiles),
+        page16(a.c.page >> 4), heads(a.c.heads), hk(head), pages(a.c.pages) {
+    col = (key >> 4) / page16, off = (key >> 4) - col * page16;
+    step_col = 8 / page16, step_off = 8 - step_col * page16;
+    fetch();
+  }
+  __device__ __forceinline__ void fetch() { id = left > 0 && key < hi && key + 16 > lo ? trow[col] : -1; }
+  __device__ __forceinline__ int next() {
+    const int v = id < 0 || id >= pages ? -1 : static_cast<int>(((static_cast<int64_t>(id) * heads + hk) * page16 + off) * 16);
+    key += kTile;
+    --left;
+    col += step_col, off += step_off;
+    if (off >= page16) off -= page16, ++col;
+    fetch();
+    return v;
+  }
+};
+
 // A wait of a whole warp whose lanes go on, or give up, together.
 __device__ __forceinline__ bool warp_wait(uint32_t bar, uint32_t parity, const WaitCtx& wc) {
   return __all_sync(0xffffffffu, mbar_wait(bar, parity, wc));
@@ -204,7 +230,7 @@ attn_tile_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constan
   const uint32_t bar_s = bar0 + 16 * C::kStages, bar_o = bar_s + 16;   // two of each
   const uint32_t bar_q = bar_o + 16, bar_fix = bar_q + 8, bar_drain = bar_fix + 8;
   if (tid == 0) {
-    for (int i = 0; i < C::kStages; ++i) mbar_init(bar_full + 8 * i, kInt8 ? C::kConv / 32 : 1), mbar_init(bar_free + 8 * i, 1);
+    for (int i = 0; i < C::kStages; ++i) mbar_init(bar_full + 8 * i, kInt8 ? C::kConv / 32 + (i & 1 ? 0 : 2) : 1), mbar_init(bar_free + 8 * i, 1);
     for (int i = 0; i < 2; ++i) mbar_init(bar_s + 8 * i, 1), mbar_init(bar_o + 8 * i, 1);
     mbar_init(bar_q, kSoft / 32);
     mbar_init(bar_fix, 1);
@@ -290,19 +316,8 @@ attn_tile_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constan
       const int c = tid - 20 * 32;
       constexpr int kStep = C::kConv / kRow;
       const int piece = c % kRow, row_in = c / kRow;    // item k: row k * kStep + row_in
-      const int* trow = a.table + static_cast<int64_t>(b) * a.width;
-      // Page ids of the tile's eight blocks of 16 keys (lane & 7), fetched long before they are looked at; then the
-      // block's first cache vector, -1 where there is nothing to read.
-      auto fetch_id = [&](int t) {
-        const int key = key_base + t * kTile + (lane & 7) * 16;
-        return t < n_tiles && key < rg.hi && key + 16 > rg.lo ? trow[key / a.c.page] : -1;
-      };
-      auto vectors_of = [&](int t, int id) {
-        const int key = key_base + t * kTile + (lane & 7) * 16;
-        return id < 0 || id >= a.c.pages ? -1 : static_cast<int>((static_cast<int64_t>(id) * a.c.heads + hk) * a.c.page) + key % a.c.page;
-      };
-      int id = fetch_id(3);
-      int vec = vectors_of(0, fetch_id(0)), vec1 = vectors_of(1, fetch_id(1)), vec2 = vectors_of(2, fetch_id(2));   // tiles t, t + 1, t + 2
+      BlockWalk<kInt8> walk(a, rg, b, hk, key_base, n_tiles, lane & 7);
+      int vec = walk.next(), vec1 = walk.next(), vec2 = walk.next();   // tiles t, t + 1, t + 2
       // Work goes in batches of two items; the batch three further on is copied into the slots that one leaves (the
       // thread's own: no other thread reads them), or zeros.
       constexpr int kBatches = kItems / 2;              // per operand tile
@@ -320,17 +335,8 @@ attn_tile_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constan
         }
         asm volatile("cp.async.commit_group;" ::: "memory");
       };
-      // Scales of key c of the next tile, fetched a tile ahead; 0 where nothing was written.
-      float ks = 0.0f, vs = 0.0f;
-      auto load_scales = [&](int t, int v) {
-        const int first = __shfl_sync(0xffffffffu, v, c >> 4);
-        const int key = key_base + t * kTile + c;
-        ks = 0.0f, vs = 0.0f;
-        if (first >= 0 && key >= rg.lo && key < rg.hi) ks = __ldg(a.c.k_scale + first + (c & 15)), vs = __ldg(a.c.v_scale + first + (c & 15));
-      };
 #pragma unroll
       for (int n = 0; n < 3; ++n) request(n, n / kBatches < 2 ? vec : vec1);
-      if (c < kTile) load_scales(0, vec);
       bool ok = true, free_next = false;
       for (int i = 0; i < 2 * n_tiles; ++i) {
         const int st = i % C::kStages, t = i >> 1;
@@ -366,26 +372,7 @@ attn_tile_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constan
           const int ahead = ((n + 3) / kBatches) / 2 - t;   // tiles
           request(n + 3, ahead == 0 ? vec : (ahead == 1 ? vec1 : vec2));
         }
-        if (c >= kTile) {
-          // scales are the first four warps' work
-        } else if (!is_v) {
-          float top = vs;
-#pragma unroll
-          for (int o = 16; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
-          const float unit = scale_unit(top);
-          const uint32_t s0 = scales + (t % C::kScaleTiles) * (C::kScaleFloats * 4);
-          const float rel = vs * __uint_as_float(0x7f000000u - __float_as_uint(unit));   // vs / unit, a power of two
-          asm volatile("st.shared.f32 [%0], %1;" ::"r"(s0 + 4 * c), "f"(ks * a.scale_log2) : "memory");
-          asm volatile("st.shared.f32 [%0], %1;" ::"r"(s0 + 4 * (kTile + c)), "f"(rel) : "memory");
-          if (lane == 0) asm volatile("st.shared.f32 [%0], %1;" ::"r"(s0 + 4 * (2 * kTile + (c >> 5))), "f"(unit) : "memory");
-        }
-        if (is_v) {
-          vec = vec1;
-          vec1 = vec2;
-          vec2 = vectors_of(t + 3, id);
-          id = fetch_id(t + 4);
-          if (c < kTile) load_scales(t + 1, vec);
-        }
+        if (is_v) vec = vec1, vec1 = vec2, vec2 = walk.next();
         free_next = __all_sync(0xffffffffu, asked);
         fence_proxy_async_smem();
         __syncwarp();
@@ -442,6 +429,43 @@ attn_tile_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constan
           if (lane == 0) mbar_arrive(bar_full + 8 * st);
         }
         __syncwarp();
+      }
+    } else if (kInt8 && (warp == kLoadK || warp == kLoadV)) {
+      // ------------------------------------------------------------------ INT8: a tile's scales, four keys per lane
+      if constexpr (kInt8) {
+        const bool is_v = warp == kLoadV;
+        const float* from = is_v ? a.c.v_scale : a.c.k_scale;
+        BlockWalk<kInt8> walk(a, rg, b, hk, key_base, n_tiles, lane >> 2);
+        auto load = [&]() {
+          const int v = walk.next();
+          return v < 0 ? make_float4(0.0f, 0.0f, 0.0f, 0.0f) : __ldg(reinterpret_cast<const float4*>(from + v) + (lane & 3));
+        };
+        float4 next = load();
+        bool ok = true;
+        for (int t = 0; t < n_tiles; ++t) {
+          float4 s = next;
+          next = load();
+          const int key = key_base + t * kTile + 4 * lane;   // 0 where nothing was written
+          s.x = key >= rg.lo && key < rg.hi ? s.x : 0.0f, s.y = key + 1 >= rg.lo && key + 1 < rg.hi ? s.y : 0.0f;
+          s.z = key + 2 >= rg.lo && key + 2 < rg.hi ? s.z : 0.0f, s.w = key + 3 >= rg.lo && key + 3 < rg.hi ? s.w : 0.0f;
+          float factor = a.scale_log2, unit = 0.0f;
+          if (is_v) {   // relative to the unit of 32 keys
+            float top = fmaxf(fmaxf(s.x, s.y), fmaxf(s.z, s.w));
+#pragma unroll
+            for (int o = 1; o < 8; o <<= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
+            unit = scale_unit(top);
+            factor = __uint_as_float(0x7f000000u - __float_as_uint(unit));   // 1 / unit, a power of two
+          }
+          // The slot's last tile is over once V of tile t - kStages / 2 - 1 has been given back: what the loading of V
+          // of tile t - 1 waits for.
+          const int i = 2 * t - 1;
+          if (i >= C::kStages) ok = ok && warp_wait(bar_free + 8 * (i % C::kStages), ((i / C::kStages) & 1) ^ 1, wc);
+          const uint32_t s0 = scales + (t % C::kScaleTiles) * (C::kScaleFloats * 4) + (is_v ? 4 * kTile : 0);
+          asm volatile("st.shared.v4.f32 [%0], {%1, %2, %3, %4};" ::"r"(s0 + 16 * lane), "f"(s.x * factor), "f"(s.y * factor), "f"(s.z * factor), "f"(s.w * factor) : "memory");
+          if (is_v && (lane & 7) == 0) asm volatile("st.shared.f32 [%0], %1;" ::"r"(s0 + 4 * kTile + (lane >> 1)), "f"(unit) : "memory");
+          __syncwarp();
+          if (lane == 0) mbar_arrive(bar_full + 8 * ((2 * t) % C::kStages));
+        }
       }
     } else if (warp == kIssuer) {
       // ------------------------------------------------------------------ MMA issuer
@@ -627,6 +651,7 @@ attn_tile_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constan
         const float off = kInt8 ? static_cast<float>(shift) - ms : -ms;
         const uint64_t off2 = pair_f32(off, off);
         uint64_t sum = 0;
+        float4 vsc = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
 #pragma unroll
         for (int j = 0; j < 16; ++j) {
           const uint64_t x = fma_f32x2(pair_f32(__uint_as_float(s[q][2 * j]), __uint_as_float(s[q][2 * j + 1])), sc2, off2);
@@ -636,8 +661,8 @@ attn_tile_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constan
           e1 = exp2_approx(e1);
           sum = add_f32x2(sum, pair_f32(e0, e1));
           if constexpr (kInt8) {
-            const float2 v = *reinterpret_cast<const float2*>(sct + kTile + 64 * half + 32 * q + 2 * j);
-            unpair_f32(mul_f32x2(pair_f32(e0, e1), pair_f32(v.x, v.y)), e0, e1);
+            if (j % 2 == 0) vsc = *reinterpret_cast<const float4*>(sct + kTile + 64 * half + 32 * q + 2 * j);
+            unpair_f32(mul_f32x2(pair_f32(e0, e1), j % 2 == 0 ? pair_f32(vsc.x, vsc.y) : pair_f32(vsc.z, vsc.w)), e0, e1);
           }
           w[16 * q + j] = pack_f16(e0, e1);
         }
