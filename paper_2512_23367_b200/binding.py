@@ -5,7 +5,6 @@ from __future__ import annotations
 
 import ctypes
 import os
-from typing import NamedTuple
 
 import torch
 
@@ -95,8 +94,14 @@ def lib() -> ctypes.CDLL:
     return _lib
 
 
+# The current device and its current stream's handle.  torch.cuda.current_stream() builds a Stream object, 3 us of a
+# call that takes 7; torch's own launchers read the handle directly, and so does this where torch offers it.
+_device = getattr(torch._C, "_cuda_getDevice", torch.cuda.current_device)
+_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+
+
 def _stream() -> int:
-    return torch.cuda.current_stream().cuda_stream
+    return torch.cuda.current_stream().cuda_stream if _raw_stream is None else _raw_stream(_device())
 
 
 def _dev(t: torch.Tensor, dtype: torch.dtype, what: str) -> torch.Tensor:
@@ -550,7 +555,7 @@ class PagedKV:
         put = object.__setattr__
         put(self, "k", k), put(self, "v", v), put(self, "k_scale", k_scale), put(self, "v_scale", v_scale)
         put(self, "pages", pages), put(self, "heads", heads), put(self, "page", page), put(self, "dim", dim)
-        put(self, "device", k.device)
+        put(self, "device", k.get_device())
         put(self, "_struct", _KVCache(k.data_ptr(), v.data_ptr(), k_scale.data_ptr() if int8 else None,
                                       v_scale.data_ptr() if int8 else None, pages, heads, page, dim, int(int8)))
         put(self, "_ref", ctypes.addressof(self._struct))
@@ -567,14 +572,27 @@ class PagedKV:
         return cls(k, v, *(torch.zeros((pages, heads, page), dtype=torch.float32, device=device) for _ in range(2)))
 
 
-class PagedStep(NamedTuple):
+class PagedStep:
     """What pq_block_tables gives for one step: row ranges, cached tokens with the new ones, slots and positions of
-    the new tokens, and the head of the free list after the step."""
-    q_start: torch.Tensor    # i32 [requests + 1]
-    kv_len: torch.Tensor     # i32 [requests]
-    slots: torch.Tensor      # i64 [tokens]
-    pos: torch.Tensor        # i32 [tokens]
-    free_head: torch.Tensor  # i32 [1]
+    the new tokens, and the head of the free list after the step.  Measures its tensors once and keeps them."""
+
+    __slots__ = ("q_start", "kv_len", "slots", "pos", "free_head", "requests", "tokens", "device", "_ptrs")
+
+    def __init__(self, q_start: torch.Tensor, kv_len: torch.Tensor, slots: torch.Tensor, pos: torch.Tensor,
+                 free_head: torch.Tensor):
+        B, T = kv_len.numel(), slots.numel()
+        _sized(q_start, torch.int32, B + 1, "q_start"), _sized(kv_len, torch.int32, B, "kv_len")
+        _sized(slots, torch.int64, T, "slots"), _sized(pos, torch.int32, T, "pos")
+        _sized(free_head, torch.int32, 1, "free_head")
+        _together(q_start, kv_len, slots, pos, free_head)
+        put = object.__setattr__
+        put(self, "q_start", q_start), put(self, "kv_len", kv_len), put(self, "slots", slots), put(self, "pos", pos)
+        put(self, "free_head", free_head), put(self, "requests", B), put(self, "tokens", T)
+        put(self, "device", q_start.get_device())
+        put(self, "_ptrs", tuple(x.data_ptr() for x in (q_start, kv_len, slots, pos, free_head)))
+
+    def __setattr__(self, name, value):
+        raise AttributeError("a PagedStep is fixed; make another one over other tensors")
 
     @classmethod
     def empty(cls, requests: int, tokens: int, device="cuda"):
@@ -584,10 +602,19 @@ class PagedStep(NamedTuple):
                    i32(tokens), i32(1))
 
 
-def _here(t: torch.Tensor) -> None:
-    """The call launches on the current device's current stream: its operands have to live there."""
-    if t.device.index != torch.cuda.current_device():
-        raise ValueError(f"operands on {t.device}, but the current device is cuda:{torch.cuda.current_device()}")
+def _operands(device: int, *checks) -> None:
+    """(tensor, dtype, elements, name) of every operand of a call, on `device`, which has to be the current one: the
+    call launches on its current stream."""
+    for x, dtype, n, name in checks:
+        if x.dtype is not dtype or x.numel() != n or not x.is_contiguous():
+            _sized(x, dtype, n, name)
+    if device < 0:
+        raise ValueError("expected CUDA tensors (this library has no CPU path)")
+    for x, _, _, name in checks:
+        if x.get_device() != device:
+            raise ValueError(f"{name}: on {x.device}, other operands on cuda:{device}")
+    if device != _device():
+        raise ValueError(f"operands on cuda:{device}, but the current device is cuda:{_device()}")
 
 
 def pq_block_tables(kv_len, new_len, block_table, free_list, free_head, page: int, tokens: int | None = None,
@@ -599,30 +626,23 @@ def pq_block_tables(kv_len, new_len, block_table, free_list, free_head, page: in
     B = kv_len.numel()
     if block_table.dim() != 2:
         raise ValueError("block_table: expected a 2-D tensor [requests, width]")
-    width = block_table.shape[1]
-    _sized(kv_len, torch.int32, B, "kv_len"), _sized(new_len, torch.int32, B, "new_len")
-    _sized(block_table, torch.int32, B * width, "block_table")
-    _sized(free_list, torch.int32, free_list.numel(), "free_list"), _sized(free_head, torch.int32, 1, "free_head")
+    width, F = block_table.shape[1], free_list.numel()
+    checks = ((kv_len, torch.int32, B, "kv_len"), (new_len, torch.int32, B, "new_len"),
+              (block_table, torch.int32, B * width, "block_table"), (free_list, torch.int32, F, "free_list"),
+              (free_head, torch.int32, 1, "free_head"))
     if step is None:
-        if tokens is None:
-            raise ValueError("tokens: required without step")
-        if tokens < 0:
-            raise ValueError("tokens: expected a size")
-        _together(kv_len, new_len, block_table, free_list, free_head)
+        if tokens is None or tokens < 0:
+            raise ValueError("tokens: expected the rows of the step, or step")
+        _operands(kv_len.get_device(), *checks)
         step = PagedStep.empty(B, tokens, kv_len.device)
     else:
-        if tokens is not None and tokens != step.slots.numel():
-            raise ValueError("tokens: differs from the step's buffers")
-        tokens = step.slots.numel()
-        _sized(step.q_start, torch.int32, B + 1, "step.q_start"), _sized(step.kv_len, torch.int32, B, "step.kv_len")
-        _sized(step.slots, torch.int64, tokens, "step.slots"), _sized(step.pos, torch.int32, tokens, "step.pos")
-        _sized(step.free_head, torch.int32, 1, "step.free_head")
-        _together(kv_len, new_len, block_table, free_list, free_head, *step)
-    _here(kv_len)
+        if step.requests != B or (tokens is not None and tokens != step.tokens):
+            raise ValueError(f"step: made for {step.requests} requests and {step.tokens} tokens")
+        _operands(step.device, *checks)
+    q_start, total, slots, pos, head = step._ptrs
     _check("pq_block_tables", lib().pq_block_tables(
-        kv_len.data_ptr(), new_len.data_ptr(), B, block_table.data_ptr(), width, free_list.data_ptr(),
-        free_list.numel(), free_head.data_ptr(), page, tokens, step.q_start.data_ptr(), step.kv_len.data_ptr(),
-        step.slots.data_ptr(), step.pos.data_ptr(), step.free_head.data_ptr(), _stream()))
+        kv_len.data_ptr(), new_len.data_ptr(), B, block_table.data_ptr(), width, free_list.data_ptr(), F,
+        free_head.data_ptr(), page, step.tokens, q_start, total, slots, pos, head, _stream()))
     return step
 
 
@@ -651,9 +671,9 @@ def pq_kv_append(cache: PagedKV, k: torch.Tensor, v: torch.Tensor, slots: torch.
     Tv, _, vs = _token_rows(v, cache.heads, cache.dim, "v")
     if Tv != T:
         raise ValueError(f"v: expected {T} rows, got {Tv}")
-    _sized(slots, torch.int64, T, "slots")
-    _together(cache.k, k, v, slots)
-    _here(k)
+    _operands(cache.device, (slots, torch.int64, T, "slots"))
+    if k.get_device() != cache.device or v.get_device() != cache.device:
+        raise ValueError(f"k, v: expected them on the cache's device cuda:{cache.device}")
     _check("pq_kv_append", lib().pq_kv_append(cache._ref, k.data_ptr(), ks, v.data_ptr(), vs, slots.data_ptr(), T,
                                               _stream()))
 
@@ -661,9 +681,7 @@ def pq_kv_append(cache: PagedKV, k: torch.Tensor, v: torch.Tensor, slots: torch.
 def pq_kv_read(cache: PagedKV, slots: torch.Tensor) -> tuple[torch.Tensor, torch.Tensor]:
     """Keys and values at slots i64 [T] as f16 [T, heads, dim]; zeros where a slot is outside the cache."""
     T = slots.numel()
-    _sized(slots, torch.int64, T, "slots")
-    _together(cache.k, slots)
-    _here(slots)
+    _operands(cache.device, (slots, torch.int64, T, "slots"))
     k, v = (torch.empty((T, cache.heads, cache.dim), dtype=torch.float16, device=slots.device) for _ in range(2))
     _check("pq_kv_read", lib().pq_kv_read(cache._ref, slots.data_ptr(), T, k.data_ptr(), v.data_ptr(), _stream()))
     return k, v
@@ -697,15 +715,19 @@ def pq_paged_attention(q: torch.Tensor, cache: PagedKV, block_table: torch.Tenso
     if block_table.dim() != 2:
         raise ValueError("block_table: expected a 2-D tensor [requests, width]")
     width = block_table.shape[1]
-    _sized(block_table, torch.int32, B * width, "block_table")
-    _sized(q_start, torch.int32, B + 1, "q_start"), _sized(kv_len, torch.int32, B, "kv_len")
+    checks = ((block_table, torch.int32, B * width, "block_table"), (q_start, torch.int32, B + 1, "q_start"),
+              (kv_len, torch.int32, B, "kv_len"))
+    if out is not None:
+        checks += ((out, torch.float16, T * H * cache.dim, "out"),)
+    ws = ws_bytes = 0
+    if workspace is not None:
+        ws, ws_bytes = workspace.data_ptr(), workspace.numel()
+        checks += ((workspace, torch.uint8, ws_bytes, "workspace"),)
+    _operands(cache.device, *checks)
+    if q.get_device() != cache.device:
+        raise ValueError(f"q: expected it on the cache's device cuda:{cache.device}")
     if out is None:
         out = torch.empty(q.shape, dtype=torch.float16, device=q.device)
-    else:
-        _sized(out, torch.float16, T * H * cache.dim, "out")
-    ws, ws_bytes = _ws(workspace)
-    _together(q, cache.k, block_table, q_start, kv_len, out, workspace)
-    _here(q)
     _check("pq_paged_attention", lib().pq_paged_attention(
         q.data_ptr(), qs, H, cache._ref, block_table.data_ptr(), width, q_start.data_ptr(), kv_len.data_ptr(), B, T,
         max_q, max_kv, cache.dim ** -0.5 if scale is None else scale, window, out.data_ptr(), ws, ws_bytes, _stream()))

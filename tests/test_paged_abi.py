@@ -112,13 +112,19 @@ def test_binding_measures_every_operand():
         pq.pq_block_tables(i32(2), i32(2), i32(3, 4), i32(5), i32(1), 16, 3)
     with pytest.raises(ValueError, match="tokens"):
         pq.pq_block_tables(i32(2), i32(2), i32(2, 4), i32(5), i32(1), 16)
-    with pytest.raises(ValueError, match="step.slots|step.pos"):
-        s = pq.PagedStep.empty(2, 3, "cpu")
-        pq.pq_block_tables(i32(2), i32(2), i32(2, 4), i32(5), i32(1), 16, step=s._replace(pos=i32(2)))
+    with pytest.raises(ValueError, match="pos: expected 3"):
+        pq.PagedStep(i32(3), i32(2), i32(3).long(), i32(2), i32(1))
+    with pytest.raises(ValueError, match="CUDA"):
+        pq.PagedStep(i32(3), i32(2), i32(3).long(), i32(3), i32(1))
+    step = types.SimpleNamespace(requests=2, tokens=3, device=-1)
+    with pytest.raises(ValueError, match="step: made for 2 requests and 3 tokens"):
+        pq.pq_block_tables(i32(3), i32(3), i32(3, 4), i32(5), i32(1), 16, step=step)
+    with pytest.raises(ValueError, match="step: made for"):
+        pq.pq_block_tables(i32(2), i32(2), i32(2, 4), i32(5), i32(1), 16, 4, step=step)
     with pytest.raises(ValueError, match="CUDA"):
         pq.pq_block_tables(i32(2), i32(2), i32(2, 4), i32(5), i32(1), 16, 3)
 
-    Fake = types.SimpleNamespace(heads=2, dim=64, page=16, pages=4, k=k)   # no call gets as far as its memory
+    Fake = types.SimpleNamespace(heads=2, dim=64, page=16, pages=4, device=-1, _ref=0)   # no call gets as far as its memory
     with pytest.raises(ValueError, match="k: expected rows"):
         pq.pq_kv_append(Fake, f16(3, 1, 64), f16(3, 2, 64), torch.zeros(3, dtype=torch.int64))
     with pytest.raises(ValueError, match="k: expected rows"):
