@@ -28,7 +28,8 @@ int pq_paged_attention(const void* q_f16, int64_t q_stride, int32_t heads, const
              static_cast<__half*>(out_f16), tokens, static_cast<int>(requests), heads, window, scale * 1.44269504f,
              0, nullptr, nullptr};
   const Scratch sc = scratch_from(workspace, workspace_bytes);
-  const AttnPlan plan = plan_attn_rows(requests, max_kv, cache->heads, cache->dim, sm_count(), sc.partial_bytes);
+  const AttnPlan plan = plan_attn_rows(requests, max_q, max_kv, window, cache->heads, cache->dim, cache->type == PQ_KV_INT8,
+                                       sm_count(), sc.partial_bytes);
   a.part_keys = plan.part_keys;
   a.counters = sc.counters;
   a.partials = reinterpret_cast<float*>(sc.partials);
@@ -45,8 +46,11 @@ size_t pq_attention_workspace_bytes(int64_t requests, int64_t tokens, int64_t ma
       heads < kv_heads || heads % kv_heads != 0 || (dim != 64 && dim != 128) || sms < 1) {
     return 0;
   }
-  const AttnPlan plan = plan_attn_rows(requests, max_kv, kv_heads, dim, sms, ~size_t(0));
-  size_t bytes = plan.partial_bytes;
+  size_t bytes = 0;   // for either type of cache, window or not
+  for (int int8 = 0; int8 < 2; ++int8) {
+    const AttnPlan plan = plan_attn_rows(requests, max_q, max_kv, 0, kv_heads, dim, int8 != 0, sms, ~size_t(0));
+    bytes = bytes > plan.partial_bytes ? bytes : plan.partial_bytes;
+  }
   if (max_q * (heads / kv_heads) > kAttnRows) {
     const TilePlan tile = plan_attn_tile(requests, tokens, max_q, max_kv, heads / kv_heads, kv_heads, dim, sms, ~size_t(0));
     bytes = bytes > tile.partial_bytes ? bytes : tile.partial_bytes;   // the two kernels follow each other

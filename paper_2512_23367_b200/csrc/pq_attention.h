@@ -36,7 +36,7 @@ struct AttnPlan {
   int part_keys = 128;
   size_t partial_bytes = 0;
 };
-AttnPlan plan_attn_rows(int64_t requests, int64_t max_kv, int kv_heads, int dim, int sms, size_t room);
+AttnPlan plan_attn_rows(int64_t requests, int64_t max_q, int64_t max_kv, int window, int kv_heads, int dim, bool int8, int sms, size_t room);
 
 int launch_attn_rows(const AttnArgs& a, const AttnPlan& plan, cudaStream_t stream);
 

@@ -9,12 +9,17 @@ namespace pq {
 namespace {
 
 constexpr int kWarps = 4;
-constexpr int kStages = 3;
 constexpr int kStageBytes = 8192;   // keys and values of one step of one warp
+
+constexpr int rows_ctas(bool int8, int dim) { return int8 || dim == 64 ? 3 : 2; }
 
 // A warp's step: as many keys as fill a stage, in blocks of 16 (a block never leaves its page).
 template <bool kInt8, int D>
 struct RowCfg {
+  // CTAs per SM and stages of a warp's ring.  INT8 and dim 64 have more arithmetic per byte and want the warps:
+  // 64 requests of up to 8192 tokens, INT8, dim 128: 162 us with three CTAs of two stages, 172 with two of three; dim
+  // 64: 104 and 128; FP16, dim 64 (drafts of 5): 67.6 and 69.7.  FP16, dim 128 is the other way: 212 and 209.
+  static constexpr int kCtas = rows_ctas(kInt8, D), kStages = kCtas == 3 ? 2 : 3;
   static constexpr int kRowBytes = kInt8 ? D : 2 * D;
   static constexpr int kKeys = kStageBytes / (2 * kRowBytes);   // 16, 32 or 64
   static constexpr int kBlocks = kKeys / 16;
@@ -82,7 +87,7 @@ __device__ __forceinline__ void mma16816(float (&d)[4], const uint32_t (&a)[4], 
 // stays in [0, 1] whatever the scales are.  The feature order of a matrix step is permuted so that a lane's codes
 // are 16 consecutive bytes; queries (and the result's columns) are permuted alike.
 template <bool kInt8, int D>
-__global__ void __launch_bounds__(kWarps * 32, 2) attn_rows_kernel(const AttnArgs a) {
+__global__ void __launch_bounds__(kWarps * 32, (RowCfg<kInt8, D>::kCtas)) attn_rows_kernel(const AttnArgs a) {
   using C = RowCfg<kInt8, D>;
   constexpr int KS = D / 16;   // matrix steps over the features
   constexpr int NT = D / 8;    // 8-wide column tiles of the result
@@ -111,7 +116,7 @@ __global__ void __launch_bounds__(kWarps * 32, 2) attn_rows_kernel(const AttnArg
   const int steps = max(0, (k_end - k_begin + C::kKeys - 1) / C::kKeys);
   const int my_steps = (steps - warp + kWarps - 1) / kWarps;   // steps warp, warp + 4, ...
 
-  const uint32_t ring = smem_u32(smem) + warp * kStages * C::kStage;
+  const uint32_t ring = smem_u32(smem) + warp * C::kStages * C::kStage;
   const int page16 = a.c.page >> 4;
   const int64_t head_bytes = static_cast<int64_t>(a.c.page) * C::kRowBytes;
   const int* trow = a.table + static_cast<int64_t>(b) * a.width;
@@ -130,14 +135,14 @@ __global__ void __launch_bounds__(kWarps * 32, 2) attn_rows_kernel(const AttnArg
   };
   int ids_next = fetch_ids(0), ids = -1;
 
-  // Requests the copies of the warp's step s into stage s % kStages (an empty group beyond the end).
+  // Requests the copies of the warp's step s into stage s % C::kStages (an empty group beyond the end).
   auto load_step = [&](int s) {
     if (s < my_steps) {
       if (s % kGroup == 0) {
         ids = ids_next;
         ids_next = fetch_ids(s / kGroup + 1);
       }
-      const uint32_t st = ring + (s % kStages) * C::kStage;
+      const uint32_t st = ring + (s % C::kStages) * C::kStage;
       const int key0 = k_begin + (s * kWarps + warp) * C::kKeys;
 #pragma unroll
       for (int blk = 0; blk < C::kBlocks; ++blk) {
@@ -183,7 +188,7 @@ __global__ void __launch_bounds__(kWarps * 32, 2) attn_rows_kernel(const AttnArg
   };
 
 #pragma unroll
-  for (int s = 0; s < kStages - 1; ++s) load_step(s);
+  for (int s = 0; s < C::kStages - 1; ++s) load_step(s);
 
   // The rows' queries as A fragments: rows g and g + 8 of the tile; row r is token r / G, query head hk * G + r % G.
   uint32_t qa[KS][4];
@@ -216,6 +221,27 @@ __global__ void __launch_bounds__(kWarps * 32, 2) attn_rows_kernel(const AttnArg
   const int all_from = a.window > 0 ? rg.L - a.window : 0;      // keys that every row sees: [all_from, all_to)
   const int all_to = min(rg.L - rg.n + 1, rg.hi);
 
+  // INT8: the keys' codes enter the product as 1024 + (code + 128), their FP16 pattern without the subtraction, and the
+  // accumulator of a row begins at -1152 sum q instead of 0.  (Its FP32 roundings are then those of values near 1152 |q|:
+  // about 1e-2 of a code, 1e-5 of a score.  The values' codes are not taken so: their sum runs over all keys.)
+  float start[2] = {0.0f, 0.0f};
+  if constexpr (kInt8) {
+#pragma unroll
+    for (int s = 0; s < KS; ++s) {
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const __half2 h = *reinterpret_cast<const __half2*>(&qa[s][i]);
+        start[i & 1] += __low2float(h) + __high2float(h);
+      }
+    }
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {   // a lane holds a quarter of the features
+#pragma unroll
+      for (int d = 1; d < 4; d <<= 1) start[i] += __shfl_xor_sync(0xffffffffu, start[i], d);
+      start[i] *= -1152.0f;
+    }
+  }
+
   float o[NT][4];
 #pragma unroll
   for (int i = 0; i < NT; ++i) o[i][0] = o[i][1] = o[i][2] = o[i][3] = 0.0f;
@@ -223,17 +249,17 @@ __global__ void __launch_bounds__(kWarps * 32, 2) attn_rows_kernel(const AttnArg
   float vref = 0.0f;   // INT8: o is in units of vref
 
   for (int s = 0; s < my_steps; ++s) {
-    cp_wait<kStages - 2>();
+    cp_wait<C::kStages - 2>();
     __syncwarp();
-    load_step(s + kStages - 1);
-    const uint32_t st = ring + (s % kStages) * C::kStage;
+    load_step(s + C::kStages - 1);
+    const uint32_t st = ring + (s % C::kStages) * C::kStage;
     const int key0 = k_begin + (s * kWarps + warp) * C::kKeys;
 
     float sc[C::kBlocks][2][4];
 #pragma unroll
     for (int blk = 0; blk < C::kBlocks; ++blk) {
 #pragma unroll
-      for (int t = 0; t < 2; ++t) sc[blk][t][0] = sc[blk][t][1] = sc[blk][t][2] = sc[blk][t][3] = 0.0f;
+      for (int t = 0; t < 2; ++t) sc[blk][t][0] = sc[blk][t][1] = start[0], sc[blk][t][2] = sc[blk][t][3] = start[1];
       if constexpr (!kInt8) {
         const int R = blk * 16 + (lane & 7) + ((lane >> 4) << 3);
 #pragma unroll
@@ -253,7 +279,7 @@ __global__ void __launch_bounds__(kWarps * 32, 2) attn_rows_kernel(const AttnArg
             const uint4 w = lds128(st + R * C::kRowBytes + (D == 128 ? ch ^ ((R & 1) << 2) : ch) * 16);
             const uint32_t u[4] = {w.x ^ 0x80808080u, w.y ^ 0x80808080u, w.z ^ 0x80808080u, w.w ^ 0x80808080u};
 #pragma unroll
-            for (int i = 0; i < 4; ++i) mma16816(sc[blk][t], qa[q4 * 4 + i], codes_f16(u[i], 0x4140), codes_f16(u[i], 0x4342));
+            for (int i = 0; i < 4; ++i) mma16816(sc[blk][t], qa[q4 * 4 + i], __byte_perm(u[i], 0x64646464u, 0x4140), __byte_perm(u[i], 0x64646464u, 0x4342));
           }
         }
       }
@@ -467,32 +493,38 @@ int launch(const AttnArgs& a, const AttnPlan& plan, cudaStream_t stream) {
 
 }  // namespace
 
-// Two CTAs are resident on an SM.  Few units: as many parts as fill the machine once.  Many units: parts of about
-// 1024 keys, so that requests of different lengths even out over the waves.
-AttnPlan plan_attn_rows(int64_t requests, int64_t max_kv, int kv_heads, int dim, int sms, size_t room) {
+// How many keys a part gets.  `one`: what fills the resident CTAs exactly once.  Up to 1024 keys that is the choice
+// (the fewest dependent steps; 1000 tokens, 8 heads: 6.9 us with parts of 128, 12.3 without a split).  Beyond, several
+// waves of smaller parts even out: three where the units are few and long (3 x 131072 tokens: 239 us with parts of
+// 4096, 252 with 2048, 265 with one wave), six where there are many, of different lengths (64 requests of up to 8192:
+// 209 us with 2048, 219 with 4096, 225 with 512).
+AttnPlan plan_attn_rows(int64_t requests, int64_t max_q, int64_t max_kv, int window, int kv_heads, int dim, bool int8, int sms, size_t room) {
   AttnPlan p;
   p.units = requests * kv_heads;
   static const int forced = [] { const char* e = getenv("PQ_ATTN_PART"); return e ? atoi(e) : 0; }();   // ablation knob
-  const int64_t slots = 2 * sms;
-  int64_t keys = 1024;
-  if (p.units * ((max_kv + 1023) / 1024) < 2 * slots) {
-    const int64_t want = slots / p.units < 1 ? 1 : slots / p.units;
-    keys = (max_kv + want - 1) / want;
-    keys = keys < 256 ? 256 : (keys + 127) / 128 * 128;
+  if (max_q > kAttnRows) max_q = kAttnRows;   // longer chunks are the tile kernel's
+  if (window > 0 && max_kv > window + max_q) max_kv = window + max_q;
+  const int64_t slots = static_cast<int64_t>(rows_ctas(int8, dim)) * sms;
+  const int64_t one = p.units * max_kv / slots;
+  int64_t keys = one;
+  if (one > 1024) {
+    keys = one / (p.units < slots ? 3 : 6);
+    keys = keys < 1024 ? 1024 : (keys > 4096 ? 4096 : keys);
   }
+  keys = keys < 128 ? 128 : (keys + 127) / 128 * 128;
   if (forced > 0) keys = (forced + 127) / 128 * 128;
   p.part_keys = static_cast<int>(keys);
   int64_t parts = (max_kv + 15 + keys - 1) / keys;   // the first part begins at a multiple of 16
   if (p.units > kScratchCounters || parts < 1) parts = 1;
   if (parts > 65535) parts = 65535;
-  const size_t one = static_cast<size_t>(kAttnRows) * (dim + 2) * 4;
-  if (parts > 1 && static_cast<size_t>(p.units) * parts * one > room) {
-    const int64_t fit = static_cast<int64_t>(room / (static_cast<size_t>(p.units) * one));
+  const size_t bytes = static_cast<size_t>(kAttnRows) * (dim + 2) * 4;
+  if (parts > 1 && static_cast<size_t>(p.units) * parts * bytes > room) {
+    const int64_t fit = static_cast<int64_t>(room / (static_cast<size_t>(p.units) * bytes));
     parts = fit < 2 ? 1 : fit;   // the last part takes the keys that are left: fewer parts have to be longer
     p.part_keys = static_cast<int>(((max_kv + parts - 1) / parts + 127) / 128 * 128);
   }
   p.parts = static_cast<int>(parts);
-  p.partial_bytes = parts > 1 ? static_cast<size_t>(p.units) * parts * one : 0;
+  p.partial_bytes = parts > 1 ? static_cast<size_t>(p.units) * parts * bytes : 0;
   return p;
 }
 
