@@ -33,7 +33,7 @@ int pq_paged_attention(const void* q_f16, int64_t q_stride, int32_t heads, const
   a.part_keys = plan.part_keys;
   a.counters = sc.counters;
   a.partials = reinterpret_cast<float*>(sc.partials);
-  rc = launch_attn_rows(a, plan, static_cast<cudaStream_t>(stream));
+  rc = launch_attn_rows(a, plan, max_q, static_cast<cudaStream_t>(stream));
   if (rc != PQ_OK || max_q * (heads / cache->heads) <= kAttnRows) return rc;
   const TilePlan tile = plan_attn_tile(requests, tokens, max_q, max_kv, heads / cache->heads, cache->heads, cache->dim,
                                        sm_count(), sc.partial_bytes);

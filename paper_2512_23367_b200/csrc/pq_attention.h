@@ -25,7 +25,7 @@ struct AttnArgs {
   float* partials;           // per unit and part: rows x dim sums, then rows x (maximum, sum)
 };
 
-// Rows of a (request, key/value head) that the row kernel takes: one m16 tile of the legacy matrix instruction.
+// Rows of a (request, key/value head) that the row kernel takes: two 8-wide tiles of the warp's matrix instruction.
 // Requests with more rows go to the tile kernel.
 constexpr int kAttnRows = 16;
 
@@ -38,7 +38,7 @@ struct AttnPlan {
 };
 AttnPlan plan_attn_rows(int64_t requests, int64_t max_q, int64_t max_kv, int window, int kv_heads, int dim, bool int8, int sms, size_t room);
 
-int launch_attn_rows(const AttnArgs& a, const AttnPlan& plan, cudaStream_t stream);
+int launch_attn_rows(const AttnArgs& a, const AttnPlan& plan, int64_t max_q, cudaStream_t stream);
 
 // The tile kernel's schedule: a unit is one tile of 2 x (128 / group) tokens of one key/value head.
 struct TilePlan {

@@ -61,9 +61,9 @@ __device__ __forceinline__ uint2 lds64(uint32_t addr) {
   asm volatile("ld.shared.v2.u32 {%0, %1}, [%2];" : "=r"(v.x), "=r"(v.y) : "r"(addr) : "memory");
   return v;
 }
-__device__ __forceinline__ float2 lds_f2(uint32_t addr) {
-  float2 v;
-  asm volatile("ld.shared.v2.f32 {%0, %1}, [%2];" : "=f"(v.x), "=f"(v.y) : "r"(addr) : "memory");
+__device__ __forceinline__ float lds_f1(uint32_t addr) {
+  float v;
+  asm volatile("ld.shared.f32 %0, [%1];" : "=f"(v) : "r"(addr) : "memory");
   return v;
 }
 // D += A (16 x 16) B (16 x 8), FP16 in, FP32 sums.
@@ -72,12 +72,19 @@ __device__ __forceinline__ void mma16816(float (&d)[4], const uint32_t (&a)[4], 
                : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
                : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
 }
+__device__ __forceinline__ uint32_t transposed(uint32_t v) {   // an 8 x 8 tile of 16-bit values over the warp
+  uint32_t r;
+  asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(r) : "r"(v));
+  return r;
+}
+
 // HBM bound: every cached key and value is read once, 2 * dim * (2 | 1 + 4 / dim) bytes per key and head, against
-// 16 rows' worth of arithmetic at most, of which the tensor cores do the products (m16n8k16: the rows of a group
-// of query heads and of a draft's tokens share one tile).
+// 16 rows' worth of arithmetic at most, of which the tensor cores do the products.  m16n8k16 with the cache as the
+// 16-wide operand: S^T = K Q^T and O^T = V^T P^T, so that up to 8 rows (the query heads of a group times the tokens of
+// a draft) take one 8-wide tile, and up to 16 take two (kTiles).
 //
 // Grid: (part, key/value head, request).  A CTA owns a run of keys; its four warps take steps of 8 KB in turn, each
-// with a ring of its own that it fills with 16-byte asynchronous copies two steps ahead (no barrier between the
+// with a ring of its own that it fills with 16-byte asynchronous copies a step or two ahead (no barrier between the
 // warps until the end) and page ids fetched 32 blocks ahead.  Every warp keeps the running maximum and sum of its
 // keys; the four are merged through shared memory, and parts of one unit through the workspace by the CTA that
 // arrives last, in the order of the parts.
@@ -85,12 +92,12 @@ __device__ __forceinline__ void mma16816(float (&d)[4], const uint32_t (&a)[4], 
 // INT8: the codes go to the tensor cores as FP16 (exact).  The key's scale multiplies the score; the value's scale
 // multiplies the weight, taken relative to a running power of two >= every scale seen, so that the FP16 weight
 // stays in [0, 1] whatever the scales are.  The feature order of a matrix step is permuted so that a lane's codes
-// are 16 consecutive bytes; queries (and the result's columns) are permuted alike.
-template <bool kInt8, int D>
+// are 16 consecutive bytes; queries (and the result's rows) are permuted alike.
+template <bool kInt8, int D, int kTiles>
 __global__ void __launch_bounds__(kWarps * 32, (RowCfg<kInt8, D>::kCtas)) attn_rows_kernel(const AttnArgs a) {
   using C = RowCfg<kInt8, D>;
   constexpr int KS = D / 16;   // matrix steps over the features
-  constexpr int NT = D / 8;    // 8-wide column tiles of the result
+  constexpr int MT = D / 16;   // 16-wide feature tiles of the result
   extern __shared__ __align__(128) uint8_t smem[];
   __shared__ bool s_last;
 
@@ -102,7 +109,7 @@ __global__ void __launch_bounds__(kWarps * 32, (RowCfg<kInt8, D>::kCtas)) attn_r
   const int g = lane >> 2, c = lane & 3;
   const int G = a.heads / a.c.heads;
   const AttnRange rg = attn_range(a, b);
-  if (rg.n <= 0 || rg.n > kAttnRows / G) return;   // nothing to do, or the tile kernel's
+  if (rg.n <= 0 || rg.n > 8 * kTiles / G) return;   // nothing to do, or the tile kernel's
   const int rows = rg.n * G;
   const int64_t row0 = a.q_start[b];
   if (row0 < 0 || row0 + rg.n > a.tokens) return;
@@ -190,62 +197,69 @@ __global__ void __launch_bounds__(kWarps * 32, (RowCfg<kInt8, D>::kCtas)) attn_r
 #pragma unroll
   for (int s = 0; s < C::kStages - 1; ++s) load_step(s);
 
-  // The rows' queries as A fragments: rows g and g + 8 of the tile; row r is token r / G, query head hk * G + r % G.
-  uint32_t qa[KS][4];
-  {
-    const __half* qp[2];
+  // The rows' queries as B fragments: row 8 q + g; row r is token r / G, query head hk * G + r % G.
+  uint32_t qb[kTiles][KS][2];
 #pragma unroll
-    for (int i = 0; i < 2; ++i) {
-      const int r = g + 8 * i;
-      qp[i] = r < rows ? a.q + (row0 + r / G) * a.q_stride + (hk * G + r % G) * D : nullptr;
-    }
+  for (int q = 0; q < kTiles; ++q) {
+    const int r = 8 * q + g;
+    const __half* p = r < rows ? a.q + (row0 + r / G) * a.q_stride + (hk * G + r % G) * D : nullptr;
 #pragma unroll
     for (int s = 0; s < KS; ++s) {
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const int d = kInt8 ? 16 * (c + 4 * (s / 4)) + 4 * (s % 4) + 2 * (i >> 1) : 16 * s + 2 * c + 8 * (i >> 1);
-        const __half* p = qp[i & 1];
-        qa[s][i] = p != nullptr ? __ldg(reinterpret_cast<const uint32_t*>(p + d)) : 0u;
+      for (int i = 0; i < 2; ++i) {
+        const int d = kInt8 ? 16 * (c + 4 * (s / 4)) + 4 * (s % 4) + 2 * i : 16 * s + 2 * c + 8 * i;
+        qb[q][s][i] = p != nullptr ? __ldg(reinterpret_cast<const uint32_t*>(p + d)) : 0u;
       }
     }
   }
-  // Last key that each of the thread's two rows sees, and the first (window).
-  int p_row[2], w_row[2];
+  // The thread's scores are those of rows 8 q + 2 c + i: the last key that each sees, and the first (window).
+  int p_row[kTiles][2], w_row[kTiles][2];
 #pragma unroll
-  for (int i = 0; i < 2; ++i) {
-    const int r = g + 8 * i;
-    const int p = rg.L - rg.n + r / G;
-    p_row[i] = r < rows ? min(p, rg.hi - 1) : -1;
-    w_row[i] = a.window > 0 ? p - a.window : -1;   // keys above it
+  for (int q = 0; q < kTiles; ++q) {
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      const int r = 8 * q + 2 * c + i;
+      const int p = rg.L - rg.n + r / G;
+      p_row[q][i] = r < rows ? min(p, rg.hi - 1) : -1;
+      w_row[q][i] = a.window > 0 ? p - a.window : -1;   // keys above it
+    }
   }
   const int all_from = a.window > 0 ? rg.L - a.window : 0;      // keys that every row sees: [all_from, all_to)
   const int all_to = min(rg.L - rg.n + 1, rg.hi);
 
   // INT8: the keys' codes enter the product as 1024 + (code + 128), their FP16 pattern without the subtraction, and the
-  // accumulator of a row begins at -1152 sum q instead of 0.  (Its FP32 roundings are then those of values near 1152 |q|:
-  // about 1e-2 of a code, 1e-5 of a score.  The values' codes are not taken so: their sum runs over all keys.)
-  float start[2] = {0.0f, 0.0f};
-  if constexpr (kInt8) {
+  // accumulators of a row begin at -1152 sum q instead of 0.  (Their FP32 roundings are then those of values near
+  // 1152 |q|: about 1e-2 of a code, 1e-5 of a score.  The values' codes are not taken so: their sum runs over all keys.)
+  float start[kTiles][2];
 #pragma unroll
-    for (int s = 0; s < KS; ++s) {
+  for (int q = 0; q < kTiles; ++q) {
+    float x = 0.0f;
+    if constexpr (kInt8) {
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const __half2 h = *reinterpret_cast<const __half2*>(&qa[s][i]);
-        start[i & 1] += __low2float(h) + __high2float(h);
+      for (int s = 0; s < KS; ++s) {
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+          const __half2 h = *reinterpret_cast<const __half2*>(&qb[q][s][i]);
+          x += __low2float(h) + __high2float(h);
+        }
       }
+      x += __shfl_xor_sync(0xffffffffu, x, 1);   // a lane holds a quarter of row 8 q + g's features
+      x += __shfl_xor_sync(0xffffffffu, x, 2);
+      x *= -1152.0f;
     }
-#pragma unroll
-    for (int i = 0; i < 2; ++i) {   // a lane holds a quarter of the features
-#pragma unroll
-      for (int d = 1; d < 4; d <<= 1) start[i] += __shfl_xor_sync(0xffffffffu, start[i], d);
-      start[i] *= -1152.0f;
-    }
+    start[q][0] = __shfl_sync(0xffffffffu, x, 8 * c);
+    start[q][1] = __shfl_sync(0xffffffffu, x, 8 * c + 4);
   }
 
-  float o[NT][4];
+  float o[kTiles][MT][4];
 #pragma unroll
-  for (int i = 0; i < NT; ++i) o[i][0] = o[i][1] = o[i][2] = o[i][3] = 0.0f;
-  float m[2] = {-INFINITY, -INFINITY}, l[2] = {0.0f, 0.0f};
+  for (int q = 0; q < kTiles; ++q) {
+#pragma unroll
+    for (int i = 0; i < MT; ++i) o[q][i][0] = o[q][i][1] = o[q][i][2] = o[q][i][3] = 0.0f;
+  }
+  float m[kTiles][2], l[kTiles][2];
+#pragma unroll
+  for (int q = 0; q < kTiles; ++q) m[q][0] = m[q][1] = -INFINITY, l[q][0] = l[q][1] = 0.0f;
   float vref = 0.0f;   // INT8: o is in units of vref
 
   for (int s = 0; s < my_steps; ++s) {
@@ -255,31 +269,36 @@ __global__ void __launch_bounds__(kWarps * 32, (RowCfg<kInt8, D>::kCtas)) attn_r
     const uint32_t st = ring + (s % C::kStages) * C::kStage;
     const int key0 = k_begin + (s * kWarps + warp) * C::kKeys;
 
-    float sc[C::kBlocks][2][4];
+    // S^T: rows of a tile are keys g (first two values, rows 2 c and 2 c + 1 of the queries) and g + 8.
+    float sc[C::kBlocks][kTiles][4];
 #pragma unroll
     for (int blk = 0; blk < C::kBlocks; ++blk) {
 #pragma unroll
-      for (int t = 0; t < 2; ++t) sc[blk][t][0] = sc[blk][t][1] = start[0], sc[blk][t][2] = sc[blk][t][3] = start[1];
+      for (int q = 0; q < kTiles; ++q) sc[blk][q][0] = sc[blk][q][2] = start[q][0], sc[blk][q][1] = sc[blk][q][3] = start[q][1];
       if constexpr (!kInt8) {
-        const int R = blk * 16 + (lane & 7) + ((lane >> 4) << 3);
+        const int R = blk * 16 + (lane & 15);
 #pragma unroll
         for (int k = 0; k < KS; ++k) {
           uint32_t r[4];
-          ldsm4(st + R * C::kRowBytes + (((k * 2 + ((lane >> 3) & 1)) ^ (R & 7)) * 16), r);
-          mma16816(sc[blk][0], qa[k], r[0], r[1]);
-          mma16816(sc[blk][1], qa[k], r[2], r[3]);
+          ldsm4(st + R * C::kRowBytes + (((k * 2 + (lane >> 4)) ^ (R & 7)) * 16), r);
+#pragma unroll
+          for (int q = 0; q < kTiles; ++q) mma16816(sc[blk][q], r, qb[q][k][0], qb[q][k][1]);
         }
       } else {
+        const int R0 = blk * 16 + g, R1 = R0 + 8;
 #pragma unroll
-        for (int t = 0; t < 2; ++t) {
-          const int R = blk * 16 + t * 8 + g;
+        for (int q4 = 0; q4 < KS / 4; ++q4) {
+          const int ch = c + 4 * q4;
+          const uint4 w0 = lds128(st + R0 * C::kRowBytes + (D == 128 ? ch ^ ((R0 & 1) << 2) : ch) * 16);
+          const uint4 w1 = lds128(st + R1 * C::kRowBytes + (D == 128 ? ch ^ ((R1 & 1) << 2) : ch) * 16);
+          const uint32_t u0[4] = {w0.x ^ 0x80808080u, w0.y ^ 0x80808080u, w0.z ^ 0x80808080u, w0.w ^ 0x80808080u};
+          const uint32_t u1[4] = {w1.x ^ 0x80808080u, w1.y ^ 0x80808080u, w1.z ^ 0x80808080u, w1.w ^ 0x80808080u};
 #pragma unroll
-          for (int q4 = 0; q4 < KS / 4; ++q4) {
-            const int ch = c + 4 * q4;
-            const uint4 w = lds128(st + R * C::kRowBytes + (D == 128 ? ch ^ ((R & 1) << 2) : ch) * 16);
-            const uint32_t u[4] = {w.x ^ 0x80808080u, w.y ^ 0x80808080u, w.z ^ 0x80808080u, w.w ^ 0x80808080u};
+          for (int i = 0; i < 4; ++i) {
+            const uint32_t r[4] = {__byte_perm(u0[i], 0x64646464u, 0x4140), __byte_perm(u1[i], 0x64646464u, 0x4140),
+                                   __byte_perm(u0[i], 0x64646464u, 0x4342), __byte_perm(u1[i], 0x64646464u, 0x4342)};
 #pragma unroll
-            for (int i = 0; i < 4; ++i) mma16816(sc[blk][t], qa[q4 * 4 + i], __byte_perm(u[i], 0x64646464u, 0x4140), __byte_perm(u[i], 0x64646464u, 0x4342));
+            for (int q = 0; q < kTiles; ++q) mma16816(sc[blk][q], r, qb[q][q4 * 4 + i][0], qb[q][q4 * 4 + i][1]);
           }
         }
       }
@@ -287,86 +306,98 @@ __global__ void __launch_bounds__(kWarps * 32, (RowCfg<kInt8, D>::kCtas)) attn_r
 
     // Scores in powers of two, masked; the step's maxima.
     const bool all = key0 >= all_from && key0 + C::kKeys <= all_to;
-    float vs[C::kBlocks][2][2];
-    float top[2] = {-INFINITY, -INFINITY}, vtop = 0.0f;
+    float vs[C::kBlocks][2], top[kTiles][2], vtop = 0.0f;
+#pragma unroll
+    for (int q = 0; q < kTiles; ++q) top[q][0] = top[q][1] = -INFINITY;
 #pragma unroll
     for (int blk = 0; blk < C::kBlocks; ++blk) {
 #pragma unroll
-      for (int t = 0; t < 2; ++t) {
-        float2 ks = make_float2(a.scale_log2, a.scale_log2);
-        const int j = blk * 16 + t * 8 + 2 * c;
+      for (int h = 0; h < 2; ++h) {   // keys g and g + 8
+        const int j = blk * 16 + 8 * h + g;
+        float ks = a.scale_log2;
         if constexpr (kInt8) {
-          const float2 kk = lds_f2(st + kStageBytes + j * 4), vv = lds_f2(st + kStageBytes + (C::kKeys + j) * 4);
-          ks = make_float2(ks.x * kk.x, ks.y * kk.y);
-          vs[blk][t][0] = vv.x, vs[blk][t][1] = vv.y;
-          vtop = fmaxf(vtop, fmaxf(vv.x, vv.y));
+          ks *= lds_f1(st + kStageBytes + j * 4);
+          vs[blk][h] = lds_f1(st + kStageBytes + (C::kKeys + j) * 4);
+          vtop = fmaxf(vtop, vs[blk][h]);
         }
+        const int key = key0 + j;
 #pragma unroll
-        for (int i = 0; i < 2; ++i) {
-          sc[blk][t][2 * i] *= ks.x;
-          sc[blk][t][2 * i + 1] *= ks.y;
-          if (!all) {
-            const int key = key0 + j;
-            if (key > p_row[i] || key <= w_row[i]) sc[blk][t][2 * i] = -INFINITY;
-            if (key + 1 > p_row[i] || key + 1 <= w_row[i]) sc[blk][t][2 * i + 1] = -INFINITY;
+        for (int q = 0; q < kTiles; ++q) {
+#pragma unroll
+          for (int i = 0; i < 2; ++i) {
+            float& x = sc[blk][q][2 * h + i];
+            x *= ks;
+            if (!all && (key > p_row[q][i] || key <= w_row[q][i])) x = -INFINITY;
+            top[q][i] = fmaxf(top[q][i], x);
           }
-          top[i] = fmaxf(top[i], fmaxf(sc[blk][t][2 * i], sc[blk][t][2 * i + 1]));
         }
       }
     }
+    bool grown = false;
 #pragma unroll
-    for (int d = 1; d < 4; d <<= 1) {
-      top[0] = fmaxf(top[0], __shfl_xor_sync(0xffffffffu, top[0], d));
-      top[1] = fmaxf(top[1], __shfl_xor_sync(0xffffffffu, top[1], d));
+    for (int d = 4; d < 32; d <<= 1) {
+#pragma unroll
+      for (int q = 0; q < kTiles; ++q) {
+        top[q][0] = fmaxf(top[q][0], __shfl_xor_sync(0xffffffffu, top[q][0], d));
+        top[q][1] = fmaxf(top[q][1], __shfl_xor_sync(0xffffffffu, top[q][1], d));
+      }
       if constexpr (kInt8) vtop = fmaxf(vtop, __shfl_xor_sync(0xffffffffu, vtop, d));
     }
-    const bool grown = top[0] > m[0] || top[1] > m[1] || (kInt8 && vtop > vref);
-    if (__any_sync(0xffffffffu, grown)) {
-      float f[2];
 #pragma unroll
-      for (int i = 0; i < 2; ++i) {
-        const float mn = fmaxf(m[i], top[i]);
-        f[i] = m[i] == -INFINITY ? 0.0f : exp2_approx(m[i] - mn);
-        m[i] = mn;
-        l[i] *= f[i];
-      }
+    for (int q = 0; q < kTiles; ++q) grown = grown || top[q][0] > m[q][0] || top[q][1] > m[q][1];
+    grown = grown || (kInt8 && vtop > vref);
+    if (__any_sync(0xffffffffu, grown)) {
+      float fv = 1.0f;
       if (kInt8 && vtop > vref) {   // the same in every lane: all rows share the keys
         const float vn = scale_unit(vtop);
-        const float fv = vref / vn;
+        fv = vref / vn;
         vref = vn;
-        f[0] *= fv, f[1] *= fv;
       }
 #pragma unroll
-      for (int i = 0; i < NT; ++i) o[i][0] *= f[0], o[i][1] *= f[0], o[i][2] *= f[1], o[i][3] *= f[1];
-    }
-    const float vinv = kInt8 ? (vref > 0.0f ? 1.0f / vref : 0.0f) : 1.0f;
-    const float mm[2] = {m[0] == -INFINITY ? 0.0f : m[0], m[1] == -INFINITY ? 0.0f : m[1]};
-
-    // Weights as A fragments, then the product with the values.
-#pragma unroll
-    for (int blk = 0; blk < C::kBlocks; ++blk) {
-      uint32_t pa[4];
-#pragma unroll
-      for (int t = 0; t < 2; ++t) {
+      for (int q = 0; q < kTiles; ++q) {
+        float f[2];
 #pragma unroll
         for (int i = 0; i < 2; ++i) {
-          const float e0 = exp2_approx(sc[blk][t][2 * i] - mm[i]), e1 = exp2_approx(sc[blk][t][2 * i + 1] - mm[i]);
-          l[i] += e0 + e1;
-          pa[t * 2 + i] = kInt8 ? pack_f16(e0 * (vs[blk][t][0] * vinv), e1 * (vs[blk][t][1] * vinv)) : pack_f16(e0, e1);
+          const float mn = fmaxf(m[q][i], top[q][i]);
+          f[i] = m[q][i] == -INFINITY ? 0.0f : exp2_approx(m[q][i] - mn);
+          m[q][i] = mn;
+          l[q][i] *= f[i];
+          f[i] *= fv;
+        }
+#pragma unroll
+        for (int t = 0; t < MT; ++t) o[q][t][0] *= f[0], o[q][t][1] *= f[1], o[q][t][2] *= f[0], o[q][t][3] *= f[1];
+      }
+    }
+    const float vinv = kInt8 ? (vref > 0.0f ? 1.0f / vref : 0.0f) : 1.0f;
+
+    // Weights as B fragments (transposed: a lane has keys 2 c, 2 c + 1 of row g), then the product with the values.
+#pragma unroll
+    for (int blk = 0; blk < C::kBlocks; ++blk) {
+      uint32_t pb[kTiles][2];
+#pragma unroll
+      for (int q = 0; q < kTiles; ++q) {
+        const float m0 = m[q][0] == -INFINITY ? 0.0f : m[q][0], m1 = m[q][1] == -INFINITY ? 0.0f : m[q][1];
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+          const float e0 = exp2_approx(sc[blk][q][2 * h] - m0), e1 = exp2_approx(sc[blk][q][2 * h + 1] - m1);
+          l[q][0] += e0;
+          l[q][1] += e1;
+          const float w = kInt8 ? vs[blk][h] * vinv : 1.0f;
+          pb[q][h] = transposed(kInt8 ? pack_f16(e0 * w, e1 * w) : pack_f16(e0, e1));
         }
       }
       const uint32_t sv = st + C::kHalf;
       if constexpr (!kInt8) {
-        const int R = blk * 16 + (lane & 7) + (((lane >> 3) & 1) << 3);
+        const int R = blk * 16 + (lane & 7) + ((lane >> 4) << 3);
 #pragma unroll
-        for (int n2 = 0; n2 < NT / 2; ++n2) {
+        for (int t = 0; t < MT; ++t) {
           uint32_t r[4];
-          ldsm4_t(sv + R * C::kRowBytes + (((n2 * 2 + (lane >> 4)) ^ (R & 7)) * 16), r);
-          mma16816(o[2 * n2], pa, r[0], r[1]);
-          mma16816(o[2 * n2 + 1], pa, r[2], r[3]);
+          ldsm4_t(sv + R * C::kRowBytes + (((t * 2 + ((lane >> 3) & 1)) ^ (R & 7)) * 16), r);
+#pragma unroll
+          for (int q = 0; q < kTiles; ++q) mma16816(o[q][t], r, pb[q][0], pb[q][1]);
         }
       } else {
-        uint32_t w[4][NT / 4];   // four keys (2c, 2c + 1, 2c + 8, 2c + 9), NT consecutive features from NT * g
+        uint32_t w[4][D / 32];   // four keys (2c, 2c + 1, 2c + 8, 2c + 9), D / 8 consecutive features from D / 8 * g
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
           const int R = blk * 16 + 2 * c + (i & 1) + 8 * (i >> 1);
@@ -379,13 +410,16 @@ __global__ void __launch_bounds__(kWarps * 32, (RowCfg<kInt8, D>::kCtas)) attn_r
           }
         }
 #pragma unroll
-        for (int i = 0; i < NT / 4; ++i) {
+        for (int i = 0; i < D / 32; ++i) {
           const uint32_t x0 = __byte_perm(w[0][i], w[1][i], 0x5140) ^ 0x80808080u, x1 = __byte_perm(w[0][i], w[1][i], 0x7362) ^ 0x80808080u;
           const uint32_t y0 = __byte_perm(w[2][i], w[3][i], 0x5140) ^ 0x80808080u, y1 = __byte_perm(w[2][i], w[3][i], 0x7362) ^ 0x80808080u;
-          mma16816(o[4 * i], pa, codes_f16(x0, 0x4140), codes_f16(y0, 0x4140));
-          mma16816(o[4 * i + 1], pa, codes_f16(x0, 0x4342), codes_f16(y0, 0x4342));
-          mma16816(o[4 * i + 2], pa, codes_f16(x1, 0x4140), codes_f16(y1, 0x4140));
-          mma16816(o[4 * i + 3], pa, codes_f16(x1, 0x4342), codes_f16(y1, 0x4342));
+          const uint32_t r0[4] = {codes_f16(x0, 0x4140), codes_f16(x0, 0x4342), codes_f16(y0, 0x4140), codes_f16(y0, 0x4342)};
+          const uint32_t r1[4] = {codes_f16(x1, 0x4140), codes_f16(x1, 0x4342), codes_f16(y1, 0x4140), codes_f16(y1, 0x4342)};
+#pragma unroll
+          for (int q = 0; q < kTiles; ++q) {
+            mma16816(o[q][2 * i], r0, pb[q][0], pb[q][1]);
+            mma16816(o[q][2 * i + 1], r1, pb[q][0], pb[q][1]);
+          }
         }
       }
     }
@@ -398,20 +432,23 @@ __global__ void __launch_bounds__(kWarps * 32, (RowCfg<kInt8, D>::kCtas)) attn_r
   float* so = reinterpret_cast<float*>(smem);
   float2* sml = reinterpret_cast<float2*>(so + kWarps * kAttnRows * D);
 #pragma unroll
-  for (int i = 0; i < 2; ++i) {
+  for (int q = 0; q < kTiles; ++q) {
 #pragma unroll
-    for (int d = 1; d < 4; d <<= 1) l[i] += __shfl_xor_sync(0xffffffffu, l[i], d);
-    const int r = g + 8 * i;
-    if (r < rows) {
-      if (c == 0) sml[warp * kAttnRows + r] = make_float2(m[i], l[i]);
-      float* dst = so + (warp * kAttnRows + r) * D;
+    for (int i = 0; i < 2; ++i) {
 #pragma unroll
-      for (int t = 0; t < NT; ++t) {
-        if constexpr (kInt8) {
-          dst[NT * 2 * c + t] = o[t][2 * i] * vref;
-          dst[NT * (2 * c + 1) + t] = o[t][2 * i + 1] * vref;
-        } else {
-          *reinterpret_cast<float2*>(dst + 8 * t + 2 * c) = make_float2(o[t][2 * i], o[t][2 * i + 1]);
+      for (int d = 4; d < 32; d <<= 1) l[q][i] += __shfl_xor_sync(0xffffffffu, l[q][i], d);
+      const int r = 8 * q + 2 * c + i;
+      if (r < rows) {
+        if (g == 0) sml[warp * kAttnRows + r] = make_float2(m[q][i], l[q][i]);
+        float* dst = so + (warp * kAttnRows + r) * D;
+#pragma unroll
+        for (int t = 0; t < MT; ++t) {   // INT8: features D / 8 g + 2 t and the next; FP16: 16 t + g and 8 further
+          if constexpr (kInt8) {
+            *reinterpret_cast<float2*>(dst + D / 8 * g + 2 * t) = make_float2(o[q][t][i] * vref, o[q][t][2 + i] * vref);
+          } else {
+            dst[16 * t + g] = o[q][t][i];
+            dst[16 * t + g + 8] = o[q][t][2 + i];
+          }
         }
       }
     }
@@ -481,14 +518,19 @@ __global__ void __launch_bounds__(kWarps * 32, (RowCfg<kInt8, D>::kCtas)) attn_r
   }
 }
 
-template <bool kInt8, int D>
-int launch(const AttnArgs& a, const AttnPlan& plan, cudaStream_t stream) {
+template <bool kInt8, int D, int kTiles>
+int launch_tiles(const AttnArgs& a, const AttnPlan& plan, cudaStream_t stream) {
   using C = RowCfg<kInt8, D>;
   static_assert(C::kSmem >= kWarps * kAttnRows * (D + 2) * 4, "the merge has to fit the rings");
   static PerDeviceOnce once;
-  if (const int rc = set_dynamic_smem_once(once, attn_rows_kernel<kInt8, D>, C::kSmem); rc != PQ_OK) return rc;
+  if (const int rc = set_dynamic_smem_once(once, attn_rows_kernel<kInt8, D, kTiles>, C::kSmem); rc != PQ_OK) return rc;
   const dim3 grid(static_cast<unsigned>(plan.parts), static_cast<unsigned>(a.c.heads), static_cast<unsigned>(a.requests));
-  return launch_dependent(attn_rows_kernel<kInt8, D>, grid, dim3(kWarps * 32), C::kSmem, stream, a);
+  return launch_dependent(attn_rows_kernel<kInt8, D, kTiles>, grid, dim3(kWarps * 32), C::kSmem, stream, a);
+}
+
+template <bool kInt8, int D>
+int launch(const AttnArgs& a, const AttnPlan& plan, int64_t max_q, cudaStream_t stream) {
+  return max_q * (a.heads / a.c.heads) <= 8 ? launch_tiles<kInt8, D, 1>(a, plan, stream) : launch_tiles<kInt8, D, 2>(a, plan, stream);
 }
 
 }  // namespace
@@ -507,11 +549,17 @@ AttnPlan plan_attn_rows(int64_t requests, int64_t max_q, int64_t max_kv, int win
   const int64_t slots = static_cast<int64_t>(rows_ctas(int8, dim)) * sms;
   const int64_t one = p.units * max_kv / slots;
   int64_t keys = one;
-  if (one > 1024) {
-    keys = one / (p.units < slots ? 3 : 6);
-    keys = keys < 1024 ? 1024 : (keys > 4096 ? 4096 : keys);
+  if (one > 1024 && p.units < slots) {
+    const int64_t some = one * 5 / 8 < 2048 ? one * 5 / 8 : 2048;
+    keys = one / 3 > some ? one / 3 : some;
+  } else if (one > 1024) {
+    keys = one / 6 > 2048 ? one / 6 : 2048;
   }
-  keys = keys < 128 ? 128 : (keys + 127) / 128 * 128;
+  if (keys > 4096) keys = 4096;
+  if (keys < 128) keys = 128;
+  const int64_t n = (max_kv + keys / 2) / keys;   // no part much smaller than the others
+  if (n > 0) keys = (max_kv + 15 + n - 1) / n;
+  keys = (keys + 127) / 128 * 128;
   if (forced > 0) keys = (forced + 127) / 128 * 128;
   p.part_keys = static_cast<int>(keys);
   int64_t parts = (max_kv + 15 + keys - 1) / keys;   // the first part begins at a multiple of 16
@@ -528,9 +576,9 @@ AttnPlan plan_attn_rows(int64_t requests, int64_t max_q, int64_t max_kv, int win
   return p;
 }
 
-int launch_attn_rows(const AttnArgs& a, const AttnPlan& plan, cudaStream_t stream) {
-  if (a.c.type == PQ_KV_INT8) return a.c.dim == 128 ? launch<true, 128>(a, plan, stream) : launch<true, 64>(a, plan, stream);
-  return a.c.dim == 128 ? launch<false, 128>(a, plan, stream) : launch<false, 64>(a, plan, stream);
+int launch_attn_rows(const AttnArgs& a, const AttnPlan& plan, int64_t max_q, cudaStream_t stream) {
+  if (a.c.type == PQ_KV_INT8) return a.c.dim == 128 ? launch<true, 128>(a, plan, max_q, stream) : launch<true, 64>(a, plan, max_q, stream);
+  return a.c.dim == 128 ? launch<false, 128>(a, plan, max_q, stream) : launch<false, 64>(a, plan, max_q, stream);
 }
 
 }  // namespace pq
