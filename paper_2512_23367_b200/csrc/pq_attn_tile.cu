@@ -24,11 +24,10 @@ struct TileCfg {
   static constexpr int kTileBytes = kTile * D * 2;            // one operand tile: D / 64 panels of 128 rows x 128 B
   static constexpr int kPanel = kTile * 128;
   static constexpr int kStages = (kInt8 ? 131072 : 163840) / kTileBytes;   // keys and values alternate
-  // INT8: scales of a tile (keys', values', and the values' units of 32 keys each).  Tile t is written when V of tile
-  // t - kStages / 2 - 1 has been given back, so its softmax is over.
+  // INT8: scales of a tile (keys', values', and the values' units of 32 keys each).
   static constexpr int kScaleTiles = kInt8 ? kStages / 2 + 1 : 0;
   static constexpr int kScaleFloats = 2 * kTile + 4;
-  static constexpr int kBars = 2 * kStages + 7;
+  static constexpr int kBars = 2 * kStages + 7 + kScaleTiles;
   static constexpr int kSmem = (2 + kStages) * kTileBytes + kScaleTiles * kScaleFloats * 4 +
                                6 * 16 * kConv /* the converters' slots */ + 1024 /* alignment */;
 };
@@ -84,7 +83,7 @@ __device__ __forceinline__ void named_bar_arrive(uint32_t id, uint32_t nthreads)
 }
 // Named barriers (0 is __syncthreads): the softmax warpgroups among themselves; "P written", one per accumulator
 // (256 threads arrive, the issuer's warp waits); "operand tile landed", between the watcher's and the issuer's warp;
-// the two warps that share 32 rows, eight pairs; "S read", 256 threads of an accumulator to the issuer.
+// the two warps that share 32 rows, eight pairs; "S read", 256 threads of an accumulator to the issuer, one each.
 // They do not pass through shared memory, which the tensor core keeps busy: a wait on an mbarrier that has long
 // completed takes 200 to 400 cycles here, one on a named barrier about 30.
 constexpr uint32_t kBarSoft = 1, kBarP = 2, kBarTile = 4, kBarPair = 5, kBarRead = 13;
@@ -96,6 +95,18 @@ __device__ __forceinline__ bool pair_any(uint32_t id, bool yes) {
   return r != 0;
 }
 
+// Watcher and issuer meet; whether the operand tile has landed (the watcher's word; the issuer says yes).
+__device__ __forceinline__ bool tile_landed(bool yes) {
+  uint32_t r;
+  asm volatile("{\n\t.reg .pred p, q;\n\tsetp.ne.b32 p, %2, 0;\n\tbar.red.and.pred q, %1, 64, p;\n\tselp.u32 %0, 1, 0, q;\n\t}"
+               : "=r"(r) : "r"(kBarTile), "r"(static_cast<uint32_t>(yes)) : "memory");
+  return r != 0;
+}
+// "Done" to the issuer.  A warp that has given up waiting for S is no longer paced by it: it meets the issuer instead, so
+// that it cannot arrive twice for one of the issuer's waits (which would leave the issuer waiting for good).
+__device__ __forceinline__ void hand_over(uint32_t id, uint32_t nthreads, bool ok) {
+  if (ok) named_bar_arrive(id, nthreads); else named_bar_sync(id, nthreads);
+}
 // The sum, or the larger, of a value of the row's two threads, the same in both: the second half's goes to the first
 // and the result back.
 template <bool kSum>
@@ -216,7 +227,7 @@ attn_tile_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constan
   __shared__ int s_assign[2];
   __shared__ int s_warp_sum[kThreads / 32];
   __shared__ int s_last;
-  __shared__ float s_swap[2 * kTile];   // one word between the two threads of a row
+  __shared__ __align__(16) float s_swap[2 * kTile];   // one word between the two threads of a row
 
   const AttnArgs& a = ta.a;
   const int tid = threadIdx.x, warp = __shfl_sync(0xffffffffu, tid >> 5, 0), lane = tid & 31;
@@ -228,13 +239,14 @@ attn_tile_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constan
   const uint32_t bar0 = smem_u32(bars);
   const uint32_t bar_full = bar0, bar_free = bar0 + 8 * C::kStages;
   const uint32_t bar_s = bar0 + 16 * C::kStages, bar_o = bar_s + 16;   // two of each
-  const uint32_t bar_q = bar_o + 16, bar_fix = bar_q + 8, bar_drain = bar_fix + 8;
+  const uint32_t bar_q = bar_o + 16, bar_fix = bar_q + 8, bar_drain = bar_fix + 8, bar_scale = bar_drain + 8;
   if (tid == 0) {
     for (int i = 0; i < C::kStages; ++i) mbar_init(bar_full + 8 * i, kInt8 ? C::kConv / 32 + (i & 1 ? 0 : 2) : 1), mbar_init(bar_free + 8 * i, 1);
     for (int i = 0; i < 2; ++i) mbar_init(bar_s + 8 * i, 1), mbar_init(bar_o + 8 * i, 1);
     mbar_init(bar_q, kSoft / 32);
     mbar_init(bar_fix, 1);
     mbar_init(bar_drain, 1);
+    for (int i = 0; i < C::kScaleTiles; ++i) mbar_init(bar_scale + 8 * i, 1);
     fence_mbar_init();
     s_abort = 0;
     s_assign[0] = -1;
@@ -305,7 +317,8 @@ attn_tile_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constan
   grid_dep_launch();   // only now: a later launch's CTA may take this SM's tensor memory when it is given back
   const uint32_t tmem = __shfl_sync(0xffffffffu, s_tmem, 0);
   const WaitCtx wc{&s_abort, ta.wait_limit};
-  int issued = 0;   // producers: tiles requested so far
+  int issued = 0;           // producers: tiles requested so far
+  uint32_t fix_phase = 0;   // the values' producer: tiles that came by bar_fix and have landed
 
   if (kInt8 && warp >= 20) {
     // -------------------------------------------------------------------- INT8 converters
@@ -399,7 +412,6 @@ attn_tile_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constan
         if (id < 0 || id >= a.c.pages) return rows_all;
         return static_cast<int>((static_cast<int64_t>(id) * a.c.heads + hk) * a.c.page) + key - col * a.c.page;
       };
-      uint32_t fix_phase = 0;
       int row = row_of(0);
       for (int t = 0; t < n_tiles; ++t) {
         const int i = 2 * t + is_v, st = i % C::kStages;
@@ -456,10 +468,11 @@ attn_tile_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constan
             unit = scale_unit(top);
             factor = __uint_as_float(0x7f000000u - __float_as_uint(unit));   // 1 / unit, a power of two
           }
-          // The slot's last tile is over once V of tile t - kStages / 2 - 1 has been given back: what the loading of V
-          // of tile t - 1 waits for.
-          const int i = 2 * t - 1;
+          // The keys' stage has to be free as for the converters (an arrival ahead of time would count for the tile that
+          // is still being written there), and the product with the weights of the tile that was in the slot taken.
+          const int i = 2 * t;
           if (i >= C::kStages) ok = ok && warp_wait(bar_free + 8 * (i % C::kStages), ((i / C::kStages) & 1) ^ 1, wc);
+          if (t >= C::kScaleTiles) ok = ok && warp_wait(bar_scale + 8 * (t % C::kScaleTiles), ((t / C::kScaleTiles) & 1) ^ 1, wc);
           const uint32_t s0 = scales + (t % C::kScaleTiles) * (C::kScaleFloats * 4) + (is_v ? 4 * kTile : 0);
           asm volatile("st.shared.v4.f32 [%0], {%1, %2, %3, %4};" ::"r"(s0 + 16 * lane), "f"(s.x * factor), "f"(s.y * factor), "f"(s.z * factor), "f"(s.w * factor) : "memory");
           if (is_v && (lane & 7) == 0) asm volatile("st.shared.f32 [%0], %1;" ::"r"(s0 + 4 * kTile + (lane >> 1)), "f"(unit) : "memory");
@@ -469,8 +482,10 @@ attn_tile_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constan
       }
     } else if (warp == kIssuer) {
       // ------------------------------------------------------------------ MMA issuer
-      // The whole warp walks the steps, so that every operand is uniform; one elected thread issues.  After a role has
-      // given up the steps go on (the barriers stay in step), on whatever the tiles hold.
+      // The whole warp walks the steps, so that every operand is uniform; one elected thread issues.  After the watcher has
+      // given up the steps go on, so that the barriers stay in step, without MMAs: a stage must not be given back while
+      // its load is still on the way.
+      bool live = true;
       constexpr uint32_t id_qk = umma_idesc_f16(kTile, false), id_pv = umma_idesc_f16(D, true);
       constexpr uint32_t kStageUnits = C::kTileBytes / 16;
       const uint32_t leader = elect_one();
@@ -478,12 +493,12 @@ attn_tile_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constan
       const uint32_t q_step = two ? kStageUnits : 0;
       warp_wait(bar_q, 0, wc);
       for (int u = 0; u < N + lag; ++u) {
-        if (u > 0 && u <= N) named_bar_sync(kBarRead, 288);   // S(u - 1) is in registers
+        if (u > 0 && u <= N) named_bar_sync(kBarRead + ((u - 1) & 1), 288);   // S(u - 1) is in registers
         if (u < N) {   // S(u) = Q K^T
           const int acc = u & 1, st = (2 * (two ? u >> 1 : u)) % C::kStages;
-          if (!two || acc == 0) named_bar_sync(kBarTile, 64);
+          if (!two || acc == 0) live = tile_landed(true) && live;
           tc_fence_after_sync();
-          if (leader) {
+          if (leader && live) {
             const uint32_t ql = q_lo + acc * q_step, kl = k_lo0 + st * kStageUnits;
             umma_f16_ss<0>(tmem, ql, kl, id_qk);
 #pragma unroll
@@ -495,16 +510,19 @@ attn_tile_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constan
         }
         if (u >= lag) {   // O(u - lag) += P V
           const int v = u - lag, acc = v & 1, st = (2 * (two ? v >> 1 : v) + 1) % C::kStages;
-          if (!two || acc == 0) named_bar_sync(kBarTile, 64);
+          if (!two || acc == 0) live = tile_landed(true) && live;
           named_bar_sync(kBarP + acc, 288);
           tc_fence_after_sync();
-          if (leader) {
+          if (leader && live) {
             const uint32_t vl = v_lo0 + st * kStageUnits, d = tmem + 256 + acc * D, p = tmem + 128 + acc * 64;
             umma_f16_ts(d, p, vl, id_pv, (v >> 1) > 0);
 #pragma unroll
             for (int k = 1; k < PS; ++k) umma_f16_ts(d, p + 8 * k, vl + k * 128, id_pv, 1u);
             umma_commit(bar_o + 8 * acc);
-            if (!two || acc == 1) umma_commit(bar_free + 8 * st);
+            if (!two || acc == 1) {
+              umma_commit(bar_free + 8 * st);
+              if (kInt8) umma_commit(bar_scale + 8 * ((two ? v >> 1 : v) % (kInt8 ? C::kScaleTiles : 1)));
+            }
           }
           __syncwarp();
         }
@@ -519,7 +537,7 @@ attn_tile_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constan
           if (w < 0 || w >= N || (two && (w & 1))) continue;
           const int i = 2 * (two ? w >> 1 : w) + is_v;
           ok = ok && warp_wait(bar_full + 8 * (i % C::kStages), (i / C::kStages) & 1, wc);
-          named_bar_sync(kBarTile, 64);
+          tile_landed(ok);
         }
       }
     }
@@ -578,7 +596,7 @@ attn_tile_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constan
       tmem_ld_32x32(t_sc + 32, s[1]);
       tmem_ld_wait();
       tc_fence_before_sync();
-      named_bar_arrive(kBarRead, 288);
+      hand_over(kBarRead + acc, 288, ok);
       const float* sct = reinterpret_cast<const float*>(smem_raw + (scales - smem_u32(smem_raw))) +
                          (((key0 - key_base) / kTile) % (kInt8 ? C::kScaleTiles : 1)) * C::kScaleFloats;
       float units[2] = {1.0f, 1.0f}, vtop = 0.0f;
@@ -676,7 +694,7 @@ attn_tile_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constan
       tmem_st_32x32(t_p, w);
       tmem_st_wait();
       tc_fence_before_sync();
-      named_bar_arrive(kBarP + acc, 288);
+      hand_over(kBarP + acc, 288, ok);
     }
     if (ok && mine > 0) warp_wait(bar_o + 8 * acc, (mine - 1) & 1, wc);
     tc_fence_after_sync();
@@ -807,7 +825,7 @@ attn_tile_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constan
     if (!kInt8 && lane == 0 && (warp == kLoadK || warp == kLoadV)) {
       for (int i = 2 * issued + (warp == kLoadV) - 2; i >= 0 && i >= 2 * issued - C::kStages; i -= 2)
         mbar_drain(bar_full + 8 * (i % C::kStages), (i / C::kStages) & 1u);
-      if (warp == kLoadV) mbar_drain(bar_fix, 0u);
+      if (warp == kLoadV) mbar_drain(bar_fix, fix_phase & 1u);
     } else if (tid == kIssuer * 32) {
       umma_commit(bar_drain);
       mbar_drain(bar_drain, 0u);
