@@ -78,11 +78,10 @@ __device__ __forceinline__ float scale_unit(float v) {
 struct AttnRange {
   int n, L, lo, hi;
 };
-__device__ __forceinline__ AttnRange attn_range(const AttnArgs& a, int b) {
+__device__ __forceinline__ AttnRange attn_range(const AttnArgs& a, int rows, int cached) {
   AttnRange r;
-  const int q0 = a.q_start[b];
-  r.n = a.q_start[b + 1] - q0;
-  r.L = a.kv_len[b];
+  r.n = rows;
+  r.L = cached;
   const int64_t cap = a.width * a.c.page;
   r.hi = static_cast<int>(min(static_cast<int64_t>(r.L), cap));
   const int64_t lo = static_cast<int64_t>(r.L) - r.n + 1 - a.window;

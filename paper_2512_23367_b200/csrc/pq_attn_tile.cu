@@ -224,7 +224,7 @@ attn_tile_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constan
   __shared__ __align__(8) uint64_t bars[C::kBars];
   __shared__ uint32_t s_tmem;
   __shared__ volatile int s_abort;
-  __shared__ int s_assign[2];
+  __shared__ int s_assign[5];           // request, tile; its first row, rows and cached tokens
   __shared__ int s_warp_sum[kThreads / 32];
   __shared__ int s_last;
   __shared__ __align__(16) float s_swap[2 * kTile];   // one word between the two threads of a row
@@ -252,8 +252,14 @@ attn_tile_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constan
     s_assign[0] = -1;
     if (!kInt8) tma_prefetch_desc(&map_k), tma_prefetch_desc(&map_v);
   }
+  // (All CTAs of the launch before hold their tensor memory by now, or have given it back: they let this one begin.)
+  if (warp == kIssuer) tmem_alloc(smem_u32(&s_tmem), 512);
+  tc_fence_before_sync();
   grid_dep_wait();
   __syncthreads();
+  tc_fence_after_sync();
+  grid_dep_launch();   // only now: a later launch's CTA may take this SM's tensor memory when it is given back
+  const uint32_t tmem = __shfl_sync(0xffffffffu, s_tmem, 0);
 
   // Which request and which of its tiles: the slot-th over all requests that this kernel serves.  A request's
   // last tile, which sees most keys, comes first.
@@ -261,9 +267,11 @@ attn_tile_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constan
     int before = 0;
     for (int base = 0; base < a.requests; base += kThreads) {
       const int b = base + tid;
-      int cnt = 0;
+      int cnt = 0, n = 0, q0 = 0, L = 0;
       if (b < a.requests) {
-        const int n = a.q_start[b + 1] - a.q_start[b];
+        q0 = a.q_start[b];
+        n = a.q_start[b + 1] - q0;
+        L = a.kv_len[b];
         if (n > kAttnRows / G) cnt = (n - 1) / qt + 1;
       }
       int in = cnt;
@@ -280,16 +288,15 @@ attn_tile_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constan
         before += s_warp_sum[w];
       }
       const int mine = slot - (off + in - cnt);
-      if (mine >= 0 && mine < cnt) s_assign[0] = b, s_assign[1] = cnt - 1 - mine;
+      if (mine >= 0 && mine < cnt) s_assign[0] = b, s_assign[1] = cnt - 1 - mine, s_assign[2] = q0, s_assign[3] = n, s_assign[4] = L;
       __syncthreads();
       if (slot < before) break;
     }
   }
   const int b = s_assign[0];
-  if (b < 0) return;
   const int tok0 = s_assign[1] * qt;
-  const AttnRange rg = attn_range(a, b);
-  const int64_t row0 = a.q_start[b];
+  const AttnRange rg = attn_range(a, s_assign[3], s_assign[4]);
+  const int64_t row0 = s_assign[2];
   const int toks = min(qt, rg.n - tok0);
   const bool two = toks > tpt;
   const int p_base = rg.L - rg.n + tok0;                        // position of the CTA's first row
@@ -299,7 +306,13 @@ attn_tile_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constan
   const int per = a.part_keys / kTile;
   const int parts = max(1, min(static_cast<int>(gridDim.y), (all_tiles + per - 1) / per));
   const int part = blockIdx.y;
-  if (part >= parts) return;
+  if (b < 0 || part >= parts) {
+    if (warp == kIssuer) {
+      tmem_relinquish();
+      tmem_dealloc(tmem, 512);
+    }
+    return;
+  }
   const int t0 = part * per;
   const int n_tiles = part == parts - 1 ? all_tiles - t0 : per;   // key tiles of this CTA
   const int key_base = k_lo + t0 * kTile;
@@ -310,12 +323,6 @@ attn_tile_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constan
 
   const uint32_t base = (smem_u32(smem_raw) + 1023u) & ~1023u;
   const uint32_t sq = base, ring = base + 2 * C::kTileBytes, scales = ring + C::kStages * C::kTileBytes;
-  if (warp == kIssuer) tmem_alloc(smem_u32(&s_tmem), 512);
-  tc_fence_before_sync();
-  __syncthreads();
-  tc_fence_after_sync();
-  grid_dep_launch();   // only now: a later launch's CTA may take this SM's tensor memory when it is given back
-  const uint32_t tmem = __shfl_sync(0xffffffffu, s_tmem, 0);
   const WaitCtx wc{&s_abort, ta.wait_limit};
   int issued = 0;           // producers: tiles requested so far
   uint32_t fix_phase = 0;   // the values' producer: tiles that came by bar_fix and have landed
@@ -780,32 +787,50 @@ attn_tile_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constan
         if (s_last) a.counters[unit] = 0u;
       }
       named_bar_sync(kBarSoft, kSoft);
-      if (s_last && writes && live) {
+      if (s_last && live) {
+        // With one query tile the other accumulator's threads have the same rows and take half of the features.
         __threadfence();
+        const int share = two ? half : half + 2 * acc, chunks = (two ? D / 2 : D / 4) / 16;
         const float* p0 = pu + q_tile * kTile * (D + 2);
+        auto stats = [&](int q) { return __ldcg(reinterpret_cast<const float2*>(p0 + static_cast<int64_t>(q) * kPart + kTile * D) + r); };
         float M = -INFINITY, L = 0.0f;
-        for (int q = 0; q < parts; ++q) M = fmaxf(M, __ldcg(reinterpret_cast<const float2*>(p0 + static_cast<int64_t>(q) * kPart + kTile * D) + r).x);
+#pragma unroll 4
+        for (int q = 0; q < parts; ++q) M = fmaxf(M, stats(q).x);
         const float Ms = M == -INFINITY ? 0.0f : M;
+#pragma unroll 4
         for (int q = 0; q < parts; ++q) {
-          const float2 ml = __ldcg(reinterpret_cast<const float2*>(p0 + static_cast<int64_t>(q) * kPart + kTile * D) + r);
+          const float2 ml = stats(q);
           L = fmaf(ml.y, exp2_approx(ml.x - Ms), L);
         }
         const float Li = L > 0.0f ? 1.0f / L : 0.0f;
 #pragma unroll 1
-        for (int h = 0; h < D / 32; ++h) {
+        for (int h = 0; h < chunks; ++h) {
+          const int f4 = (share * chunks + h) * 4;   // of 4 features each
           float4 v[4];
 #pragma unroll
           for (int j = 0; j < 4; ++j) v[j] = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-          for (int q = 0; q < parts; ++q) {
-            const float* pq_ = p0 + static_cast<int64_t>(q) * kPart;
-            const float f = exp2_approx(__ldcg(reinterpret_cast<const float2*>(pq_ + kTile * D) + r).x - Ms) * Li;
+#pragma unroll 1
+          for (int q0 = 0; q0 < parts; q0 += 3) {   // the loads of three parts in flight together
+            float4 x[3][4];
+            float f[3];
 #pragma unroll
-            for (int j = 0; j < 4; ++j) {
-              const float4 x = __ldcg(reinterpret_cast<const float4*>(pq_) + (half * (D / 8) + 4 * h + j) * kTile + r);
-              v[j].x = fmaf(x.x, f, v[j].x), v[j].y = fmaf(x.y, f, v[j].y), v[j].z = fmaf(x.z, f, v[j].z), v[j].w = fmaf(x.w, f, v[j].w);
+            for (int i = 0; i < 3; ++i) {
+              const int q = min(q0 + i, parts - 1);
+              f[i] = stats(q).x;
+#pragma unroll
+              for (int j = 0; j < 4; ++j) x[i][j] = __ldcg(reinterpret_cast<const float4*>(p0 + static_cast<int64_t>(q) * kPart) + (f4 + j) * kTile + r);
+            }
+#pragma unroll
+            for (int i = 0; i < 3; ++i) {
+              const float w = q0 + i < parts ? exp2_approx(f[i] - Ms) * Li : 0.0f;
+              if (q0 + i < parts) {
+#pragma unroll
+                for (int j = 0; j < 4; ++j)
+                  v[j].x = fmaf(x[i][j].x, w, v[j].x), v[j].y = fmaf(x[i][j].y, w, v[j].y), v[j].z = fmaf(x[i][j].z, w, v[j].z), v[j].w = fmaf(x[i][j].w, w, v[j].w);
+              }
             }
           }
-          uint4* dst = reinterpret_cast<uint4*>(a.out + out_row * D + half * (D / 2) + 16 * h);
+          uint4* dst = reinterpret_cast<uint4*>(a.out + out_row * D + 4 * f4);
 #pragma unroll
           for (int j = 0; j < 2; ++j)
             dst[j] = make_uint4(pack_f16(v[2 * j].x, v[2 * j].y), pack_f16(v[2 * j].z, v[2 * j].w),
