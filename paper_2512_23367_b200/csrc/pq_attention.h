@@ -21,7 +21,7 @@ struct AttnArgs {
   int requests, heads, window;
   float scale_log2;          // scale * log2(e): scores are powers of two
   int part_keys;             // keys of one part, a multiple of 128
-  unsigned int* counters;    // arrivals per unit, zero between calls; nullptr: the keys are not split
+  unsigned int* counters;    // row kernel: arrivals per unit, zero between calls
   float* partials;           // per unit and part: rows x dim sums, then rows x (maximum, sum)
 };
 

@@ -188,6 +188,119 @@ struct TileArgs {
   uint32_t q_and, q_xor; // a scale of 0 or below is folded into the queries: (q & q_and) ^ q_xor
 };
 
+// Which request and which of its tiles of `qt` tokens: the slot-th over all requests that this kernel serves (a request's
+// last tile, which sees most keys, comes first).  found: request (-1: there are fewer), tile, first row, rows, cached
+// tokens.  By the whole block; sums: one word per warp.
+template <int kThreads>
+__device__ __forceinline__ void find_slot(const AttnArgs& a, int slot, int qt, volatile int* found, volatile int* sums) {
+  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, G = a.heads / a.c.heads;
+  if (tid == 0) found[0] = -1;
+  int before = 0;
+  for (int base = 0; base < a.requests; base += kThreads) {
+    const int b = base + tid;
+    int cnt = 0, n = 0, q0 = 0, L = 0;
+    if (b < a.requests) {
+      q0 = a.q_start[b];
+      n = a.q_start[b + 1] - q0;
+      L = a.kv_len[b];
+      if (n > kAttnRows / G) cnt = (n - 1) / qt + 1;   // the others are the row kernel's
+    }
+    int in = cnt;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+      const int x = __shfl_up_sync(0xffffffffu, in, o);
+      if (lane >= o) in += x;
+    }
+    if (lane == 31) sums[warp] = in;
+    __syncthreads();
+    int off = before;
+    for (int w = 0; w < kThreads / 32; ++w) {
+      if (w < warp) off += sums[w];
+      before += sums[w];
+    }
+    const int mine = slot - (off + in - cnt);
+    if (mine >= 0 && mine < cnt) found[0] = b, found[1] = cnt - 1 - mine, found[2] = q0, found[3] = n, found[4] = L;
+    __syncthreads();
+    if (slot < before) break;
+  }
+}
+
+// The keys that a slot's rows see, and their division.
+struct SlotKeys {
+  int toks, p_base;        // tokens; position of the first
+  int k_lo, tiles;         // first key (a multiple of 128), key tiles
+  int per, parts;          // tiles of a part
+};
+__device__ __forceinline__ SlotKeys slot_keys(const AttnArgs& a, const AttnRange& rg, int tok0, int qt, int most_parts) {
+  SlotKeys s;
+  s.toks = min(qt, rg.n - tok0);
+  s.p_base = rg.L - rg.n + tok0;
+  const int k_hi = min(rg.hi, s.p_base + s.toks);
+  s.k_lo = (a.window > 0 ? max(0, s.p_base + 1 - a.window) : 0) & ~(kTile - 1);
+  s.tiles = k_hi > s.k_lo ? (k_hi - s.k_lo + kTile - 1) / kTile : 0;
+  s.per = a.part_keys / kTile;
+  s.parts = max(1, min(most_parts, (s.tiles + s.per - 1) / s.per));
+  return s;
+}
+
+// Floats of one part: per query tile [D / 4][128 rows] x 4 sums, then [128 rows] x (reference, sum of weights).
+template <int D>
+constexpr int kPartFloats = 2 * kTile * (D + 2);
+
+// Joins the parts of the units whose keys were split, in their order: grid (unit, 32 rows), a warp per 4 features in
+// turn, lanes along the rows.  (One CTA per unit, the last to arrive, took 30 us for 16 parts of 133 KB.)
+constexpr int kJoinThreads = 256;
+template <int D>
+__global__ void __launch_bounds__(kJoinThreads) attn_join_kernel(const AttnArgs a, int most_parts) {
+  __shared__ int s_assign[5];
+  __shared__ int s_warp_sum[kJoinThreads / 32];
+  grid_dep_launch();
+  grid_dep_wait();
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const int G = a.heads / a.c.heads, tpt = kTile / G, qt = 2 * tpt;
+  const int slot = blockIdx.x / a.c.heads, hk = blockIdx.x - slot * a.c.heads;
+  __syncthreads();
+  find_slot<kJoinThreads>(a, slot, qt, s_assign, s_warp_sum);
+  if (s_assign[0] < 0) return;
+  const int tok0 = s_assign[1] * qt;
+  const SlotKeys sk = slot_keys(a, attn_range(a, s_assign[3], s_assign[4]), tok0, qt, most_parts);
+  const int tile = blockIdx.y / 4, r = (blockIdx.y % 4) * 32 + lane;
+  const int tok = tile * tpt + r / G;
+  const int64_t row = static_cast<int64_t>(s_assign[2]) + tok0 + tok;
+  if (sk.parts == 1 || (tile == 1 && sk.toks <= tpt)) return;
+  const bool live = r < tpt * G && tok < sk.toks && row >= 0 && row < a.tokens;
+  if (!live) return;   // no barrier follows
+  constexpr int kPart = kPartFloats<D>;
+  const float* p0 = a.partials + static_cast<int64_t>(blockIdx.x) * most_parts * kPart + tile * kTile * (D + 2);
+  auto stats = [&](int q) { return __ldcg(reinterpret_cast<const float2*>(p0 + static_cast<int64_t>(q) * kPart + kTile * D) + r); };
+  float M = -INFINITY, L = 0.0f;
+#pragma unroll 8
+  for (int q = 0; q < sk.parts; ++q) M = fmaxf(M, stats(q).x);
+  const float Ms = M == -INFINITY ? 0.0f : M;
+#pragma unroll 8
+  for (int q = 0; q < sk.parts; ++q) {
+    const float2 ml = stats(q);
+    L = fmaf(ml.y, exp2_approx(ml.x - Ms), L);
+  }
+  const float Li = L > 0.0f ? 1.0f / L : 0.0f;
+  constexpr int kMine = D / 32;   // groups of 4 features per warp
+  float4 v[kMine];
+#pragma unroll
+  for (int j = 0; j < kMine; ++j) v[j] = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+#pragma unroll 4
+  for (int q = 0; q < sk.parts; ++q) {
+    const float w = exp2_approx(stats(q).x - Ms) * Li;
+#pragma unroll
+    for (int j = 0; j < kMine; ++j) {
+      const float4 x = __ldcg(reinterpret_cast<const float4*>(p0 + static_cast<int64_t>(q) * kPart) + (warp * kMine + j) * kTile + r);
+      v[j].x = fmaf(x.x, w, v[j].x), v[j].y = fmaf(x.y, w, v[j].y), v[j].z = fmaf(x.z, w, v[j].z), v[j].w = fmaf(x.w, w, v[j].w);
+    }
+  }
+  __half* out = a.out + (row * a.heads + hk * G + r % G) * D + warp * (4 * kMine);
+#pragma unroll
+  for (int j = 0; j < kMine; ++j) *reinterpret_cast<uint2*>(out + 4 * j) = make_uint2(pack_f16(v[j].x, v[j].y), pack_f16(v[j].z, v[j].w));
+}
+
 // Tensor bound for long chunks, HBM bound for wide drafts over long caches.
 //
 // A CTA owns 256 query rows of one key/value head (row = token x query heads of the group) as two accumulators of
@@ -226,7 +339,6 @@ attn_tile_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constan
   __shared__ volatile int s_abort;
   __shared__ int s_assign[5];           // request, tile; its first row, rows and cached tokens
   __shared__ int s_warp_sum[kThreads / 32];
-  __shared__ int s_last;
   __shared__ __align__(16) float s_swap[2 * kTile];   // one word between the two threads of a row
 
   const AttnArgs& a = ta.a;
@@ -249,7 +361,6 @@ attn_tile_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constan
     for (int i = 0; i < C::kScaleTiles; ++i) mbar_init(bar_scale + 8 * i, 1);
     fence_mbar_init();
     s_abort = 0;
-    s_assign[0] = -1;
     if (!kInt8) tma_prefetch_desc(&map_k), tma_prefetch_desc(&map_v);
   }
   // (All CTAs of the launch before hold their tensor memory by now, or have given it back: they let this one begin.)
@@ -261,50 +372,14 @@ attn_tile_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constan
   grid_dep_launch();   // only now: a later launch's CTA may take this SM's tensor memory when it is given back
   const uint32_t tmem = __shfl_sync(0xffffffffu, s_tmem, 0);
 
-  // Which request and which of its tiles: the slot-th over all requests that this kernel serves.  A request's
-  // last tile, which sees most keys, comes first.
-  {
-    int before = 0;
-    for (int base = 0; base < a.requests; base += kThreads) {
-      const int b = base + tid;
-      int cnt = 0, n = 0, q0 = 0, L = 0;
-      if (b < a.requests) {
-        q0 = a.q_start[b];
-        n = a.q_start[b + 1] - q0;
-        L = a.kv_len[b];
-        if (n > kAttnRows / G) cnt = (n - 1) / qt + 1;
-      }
-      int in = cnt;
-#pragma unroll
-      for (int o = 1; o < 32; o <<= 1) {
-        const int x = __shfl_up_sync(0xffffffffu, in, o);
-        if (lane >= o) in += x;
-      }
-      if (lane == 31) s_warp_sum[warp] = in;
-      __syncthreads();
-      int off = before;
-      for (int w = 0; w < kThreads / 32; ++w) {
-        if (w < warp) off += s_warp_sum[w];
-        before += s_warp_sum[w];
-      }
-      const int mine = slot - (off + in - cnt);
-      if (mine >= 0 && mine < cnt) s_assign[0] = b, s_assign[1] = cnt - 1 - mine, s_assign[2] = q0, s_assign[3] = n, s_assign[4] = L;
-      __syncthreads();
-      if (slot < before) break;
-    }
-  }
+  find_slot<kThreads>(a, slot, qt, s_assign, s_warp_sum);
   const int b = s_assign[0];
   const int tok0 = s_assign[1] * qt;
   const AttnRange rg = attn_range(a, s_assign[3], s_assign[4]);
   const int64_t row0 = s_assign[2];
-  const int toks = min(qt, rg.n - tok0);
+  const SlotKeys sk = slot_keys(a, rg, tok0, qt, static_cast<int>(gridDim.y));
+  const int toks = sk.toks, p_base = sk.p_base, parts = sk.parts;
   const bool two = toks > tpt;
-  const int p_base = rg.L - rg.n + tok0;                        // position of the CTA's first row
-  const int k_hi = min(rg.hi, p_base + toks);                   // keys that some row sees: [k_lo, k_hi)
-  const int k_lo = (a.window > 0 ? max(0, p_base + 1 - a.window) : 0) & ~(kTile - 1);
-  const int all_tiles = k_hi > k_lo ? (k_hi - k_lo + kTile - 1) / kTile : 0;
-  const int per = a.part_keys / kTile;
-  const int parts = max(1, min(static_cast<int>(gridDim.y), (all_tiles + per - 1) / per));
   const int part = blockIdx.y;
   if (b < 0 || part >= parts) {
     if (warp == kIssuer) {
@@ -313,9 +388,9 @@ attn_tile_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constan
     }
     return;
   }
-  const int t0 = part * per;
-  const int n_tiles = part == parts - 1 ? all_tiles - t0 : per;   // key tiles of this CTA
-  const int key_base = k_lo + t0 * kTile;
+  const int t0 = part * sk.per;
+  const int n_tiles = part == parts - 1 ? sk.tiles - t0 : sk.per;   // key tiles of this CTA
+  const int key_base = sk.k_lo + t0 * kTile;
   const int N = two ? 2 * n_tiles : n_tiles;                      // (QK, PV) steps
   // Steps that a PV follows its QK by: with two query tiles S(u + 1) is computed while the softmax of u runs; with
   // one, where memory is the bound, operand tiles are given back a step earlier instead.
@@ -740,7 +815,7 @@ attn_tile_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constan
     f0 *= vref;
     const bool writes = two || acc == 0;
     const int64_t unit = blockIdx.x;
-    constexpr int kPart = 2 * kTile * (D + 2);   // floats of one part: per tile [D / 4][128] x 4, then [128] x 2
+    constexpr int kPart = kPartFloats<D>;
     float* pu = a.partials + unit * gridDim.y * kPart;
     const float inv = l > 0.0f ? 1.0f / l : 0.0f;
     if (writes) {
@@ -776,67 +851,6 @@ attn_tile_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constan
         }
       }
       if (parts > 1 && half == 0) reinterpret_cast<float2*>(pp + kTile * D)[r] = make_float2(m, l);
-    }
-    if (parts > 1) {
-      // The CTA that arrives last joins the parts, in their order.
-      __threadfence();
-      named_bar_sync(kBarSoft, kSoft);
-      if (tid == 0) {
-        const unsigned int before = atomicAdd(a.counters + unit, 1u);
-        s_last = before == static_cast<unsigned int>(parts) - 1u;
-        if (s_last) a.counters[unit] = 0u;
-      }
-      named_bar_sync(kBarSoft, kSoft);
-      if (s_last && live) {
-        // With one query tile the other accumulator's threads have the same rows and take half of the features.
-        __threadfence();
-        const int share = two ? half : half + 2 * acc, chunks = (two ? D / 2 : D / 4) / 16;
-        const float* p0 = pu + q_tile * kTile * (D + 2);
-        auto stats = [&](int q) { return __ldcg(reinterpret_cast<const float2*>(p0 + static_cast<int64_t>(q) * kPart + kTile * D) + r); };
-        float M = -INFINITY, L = 0.0f;
-#pragma unroll 4
-        for (int q = 0; q < parts; ++q) M = fmaxf(M, stats(q).x);
-        const float Ms = M == -INFINITY ? 0.0f : M;
-#pragma unroll 4
-        for (int q = 0; q < parts; ++q) {
-          const float2 ml = stats(q);
-          L = fmaf(ml.y, exp2_approx(ml.x - Ms), L);
-        }
-        const float Li = L > 0.0f ? 1.0f / L : 0.0f;
-#pragma unroll 1
-        for (int h = 0; h < chunks; ++h) {
-          const int f4 = (share * chunks + h) * 4;   // of 4 features each
-          float4 v[4];
-#pragma unroll
-          for (int j = 0; j < 4; ++j) v[j] = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-#pragma unroll 1
-          for (int q0 = 0; q0 < parts; q0 += 3) {   // the loads of three parts in flight together
-            float4 x[3][4];
-            float f[3];
-#pragma unroll
-            for (int i = 0; i < 3; ++i) {
-              const int q = min(q0 + i, parts - 1);
-              f[i] = stats(q).x;
-#pragma unroll
-              for (int j = 0; j < 4; ++j) x[i][j] = __ldcg(reinterpret_cast<const float4*>(p0 + static_cast<int64_t>(q) * kPart) + (f4 + j) * kTile + r);
-            }
-#pragma unroll
-            for (int i = 0; i < 3; ++i) {
-              const float w = q0 + i < parts ? exp2_approx(f[i] - Ms) * Li : 0.0f;
-              if (q0 + i < parts) {
-#pragma unroll
-                for (int j = 0; j < 4; ++j)
-                  v[j].x = fmaf(x[i][j].x, w, v[j].x), v[j].y = fmaf(x[i][j].y, w, v[j].y), v[j].z = fmaf(x[i][j].z, w, v[j].z), v[j].w = fmaf(x[i][j].w, w, v[j].w);
-              }
-            }
-          }
-          uint4* dst = reinterpret_cast<uint4*>(a.out + out_row * D + 4 * f4);
-#pragma unroll
-          for (int j = 0; j < 2; ++j)
-            dst[j] = make_uint4(pack_f16(v[2 * j].x, v[2 * j].y), pack_f16(v[2 * j].z, v[2 * j].w),
-                                pack_f16(v[2 * j + 1].x, v[2 * j + 1].y), pack_f16(v[2 * j + 1].z, v[2 * j + 1].w));
-        }
-      }
     }
   }
 
@@ -885,7 +899,8 @@ int launch(TileArgs& t, const TilePlan& plan, cudaStream_t stream) {
     if (const int rc = make_tmap_2d(&mv, c.v, rows, D, t.box, 64, 2, 128); rc != PQ_OK) return rc;
   }
   const dim3 grid(static_cast<unsigned>(plan.units), static_cast<unsigned>(plan.parts));
-  return launch_dependent(kern, grid, dim3(C::kThreads), C::kSmem, stream, mk, mv, t);
+  if (const int rc = launch_dependent(kern, grid, dim3(C::kThreads), C::kSmem, stream, mk, mv, t); rc != PQ_OK || plan.parts == 1) return rc;
+  return launch_dependent(attn_join_kernel<D>, dim3(grid.x, 8), dim3(kJoinThreads), 0, stream, t.a, plan.parts);
 }
 
 }  // namespace
@@ -898,7 +913,7 @@ TilePlan plan_attn_tile(int64_t requests, int64_t tokens, int64_t max_q, int64_t
   const int64_t by_rows = tokens / qt + requests, by_request = requests * ((max_q + qt - 1) / qt);
   p.units = (by_rows < by_request ? by_rows : by_request) * kv_heads;
   int64_t parts = 1, keys = (max_kv + kTile - 1) / kTile * kTile;
-  if (p.units < sms && p.units <= kScratchCounters) {
+  if (p.units < sms) {
     parts = sms / p.units;
     keys = (max_kv + parts - 1) / parts;
     keys = keys < 512 ? 512 : (keys + kTile - 1) / kTile * kTile;
