@@ -24,20 +24,27 @@ int pq_paged_attention(const void* q_f16, int64_t q_stride, int32_t heads, const
   if (!q_f16 || !block_table || !q_start || !kv_len || !out_f16) return PQ_ERR_NULL;
   if (!aligned16(q_f16) || !aligned16(out_f16) || !aligned256(workspace)) return PQ_ERR_ALIGN;
   if ((rc = check_arch()) != PQ_OK) return rc;
+  // Up to 16 rows per request and key/value head go to the row kernel, more to the tile kernel; which of them a request
+  // takes is decided on the device.  A single request of many rows needs no row kernel.
+  const int group = heads / cache->heads;
+  const bool wide = max_q * group > kAttnRows, narrow = !wide || requests > 1;
   AttnArgs a{static_cast<const __half*>(q_f16), q_stride, *cache, block_table, width, q_start, kv_len,
-             static_cast<__half*>(out_f16), tokens, static_cast<int>(requests), heads, window, scale * 1.44269504f,
-             0, nullptr, nullptr};
+             static_cast<__half*>(out_f16), tokens, static_cast<int>(requests), heads, window,
+             narrow ? kAttnRows / group : 0, scale * 1.44269504f, 0, nullptr, nullptr};
   const Scratch sc = scratch_from(workspace, workspace_bytes);
-  const AttnPlan plan = plan_attn_rows(requests, max_q, max_kv, window, cache->heads, cache->dim, cache->type == PQ_KV_INT8,
-                                       sm_count(), sc.partial_bytes);
-  a.part_keys = plan.part_keys;
   a.counters = sc.counters;
   a.partials = reinterpret_cast<float*>(sc.partials);
-  rc = launch_attn_rows(a, plan, max_q, static_cast<cudaStream_t>(stream));
-  if (rc != PQ_OK || max_q * (heads / cache->heads) <= kAttnRows) return rc;
-  const TilePlan tile = plan_attn_tile(requests, tokens, max_q, max_kv, heads / cache->heads, cache->heads, cache->dim,
-                                       sm_count(), sc.partial_bytes);
-  return launch_attn_tile(a, tile, static_cast<cudaStream_t>(stream));
+  cudaStream_t st = static_cast<cudaStream_t>(stream);
+  if (narrow) {
+    const AttnPlan plan = plan_attn_rows(requests, max_q, max_kv, window, cache->heads, cache->dim, cache->type == PQ_KV_INT8,
+                                         sm_count(), sc.partial_bytes);
+    a.part_keys = plan.part_keys;
+    rc = launch_attn_rows(a, plan, max_q, st);
+    if (rc != PQ_OK || !wide) return rc;
+  }
+  const TilePlan tile = plan_attn_tile(requests, tokens, max_q, max_kv, group, cache->heads, cache->dim, sm_count(),
+                                       sc.partial_bytes);
+  return launch_attn_tile(a, tile, st);
 }
 
 size_t pq_attention_workspace_bytes(int64_t requests, int64_t tokens, int64_t max_q, int64_t max_kv, int32_t heads,

@@ -19,6 +19,7 @@ struct AttnArgs {
   __half* out;
   int64_t tokens;
   int requests, heads, window;
+  int row_tokens;            // requests of up to so many tokens are the row kernel's (0: it is not launched)
   float scale_log2;          // scale * log2(e): scores are powers of two
   int part_keys;             // keys of one part, a multiple of 128
   unsigned int* counters;    // row kernel: arrivals per unit, zero between calls

@@ -110,7 +110,7 @@ __global__ void __launch_bounds__(kWarps * 32, (RowCfg<kInt8, D>::kCtas)) attn_r
   const int G = a.heads / a.c.heads;
   const int64_t row0 = a.q_start[b];
   const AttnRange rg = attn_range(a, a.q_start[b + 1] - static_cast<int>(row0), a.kv_len[b]);
-  if (rg.n <= 0 || rg.n > 8 * kTiles / G) return;   // nothing to do, or the tile kernel's
+  if (rg.n <= 0 || rg.n > a.row_tokens || rg.n > 8 * kTiles / G) return;   // nothing to do, or the tile kernel's
   const int rows = rg.n * G;
   if (row0 < 0 || row0 + rg.n > a.tokens) return;
 

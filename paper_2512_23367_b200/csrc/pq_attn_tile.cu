@@ -193,7 +193,7 @@ struct TileArgs {
 // tokens.  By the whole block; sums: one word per warp.
 template <int kThreads>
 __device__ __forceinline__ void find_slot(const AttnArgs& a, int slot, int qt, volatile int* found, volatile int* sums) {
-  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, G = a.heads / a.c.heads;
+  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   if (tid == 0) found[0] = -1;
   int before = 0;
   for (int base = 0; base < a.requests; base += kThreads) {
@@ -203,7 +203,7 @@ __device__ __forceinline__ void find_slot(const AttnArgs& a, int slot, int qt, v
       q0 = a.q_start[b];
       n = a.q_start[b + 1] - q0;
       L = a.kv_len[b];
-      if (n > kAttnRows / G) cnt = (n - 1) / qt + 1;   // the others are the row kernel's
+      if (n > a.row_tokens) cnt = (n - 1) / qt + 1;   // the others are the row kernel's
     }
     int in = cnt;
 #pragma unroll
@@ -339,7 +339,7 @@ attn_tile_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constan
   __shared__ volatile int s_abort;
   __shared__ int s_assign[5];           // request, tile; its first row, rows and cached tokens
   __shared__ int s_warp_sum[kThreads / 32];
-  __shared__ __align__(16) float s_swap[2 * kTile];   // one word between the two threads of a row
+  __shared__ __align__(16) float s_swap[2 * kTile];   // one word between the two threads of a row; a pair per row in the join
 
   const AttnArgs& a = ta.a;
   const int tid = threadIdx.x, warp = __shfl_sync(0xffffffffu, tid >> 5, 0), lane = tid & 31;
@@ -635,21 +635,29 @@ attn_tile_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constan
     const uint32_t pair = kBarPair + acc * 4 + (warp & 3);
     const int q_tile = two ? acc : 0;
     const int tok = q_tile * tpt + r / G;            // token of the row, from tok0
-    const bool live = r < tpt * G && tok < toks && row0 + tok0 + tok >= 0 && row0 + tok0 + tok < a.tokens;
-    const int64_t out_row = (row0 + tok0 + tok) * a.heads + hk * G + r % G;
+    // Where row i of the query tile begins in a matrix of `stride` elements per token: nullptr if there is no such row.
+    auto row_at = [&](const __half* m, int64_t stride, int i) -> const __half* {
+      const int k = q_tile * tpt + i / G;
+      const int64_t row = row0 + tok0 + k;
+      return i < tpt * G && k < toks && row >= 0 && row < a.tokens ? m + row * stride + (hk * G + i % G) * D : nullptr;
+    };
+    // Rows go between global and shared memory whole, D / 8 lanes side by side (a thread per row instead took 3000
+    // cycles at each end): piece c of row i at its swizzled place.
+    constexpr int kLanes = D / 8, kRowsAtOnce = 32 / kLanes;
+    auto place = [&](int i, int c) { return sq + q_tile * C::kTileBytes + (c >> 3) * C::kPanel + i * 128 + (((c & 7) ^ (i & 7)) << 4); };
 
     if (two || acc == 0) {
-      const uint4* qp = live ? reinterpret_cast<const uint4*>(a.q + (row0 + tok0 + tok) * a.q_stride + (hk * G + r % G) * D) + half * (D / 16) : nullptr;
-      uint4 x[D / 16];
+      uint4 x[16 / kRowsAtOnce];
 #pragma unroll
-      for (int i = 0; i < D / 16; ++i) x[i] = live ? __ldg(qp + i) : make_uint4(0, 0, 0, 0);
-      const uint32_t dst = sq + q_tile * C::kTileBytes + r * 128;
+      for (int i = 0; i < 16 / kRowsAtOnce; ++i) {   // 16 rows per warp
+        const __half* p = row_at(a.q, a.q_stride, (warp & 7) * 16 + i * kRowsAtOnce + lane / kLanes);
+        x[i] = p != nullptr ? __ldg(reinterpret_cast<const uint4*>(p) + lane % kLanes) : make_uint4(0, 0, 0, 0);
+      }
 #pragma unroll
-      for (int i = 0; i < D / 16; ++i) {
-        const int ch = half * (D / 16) + i;
+      for (int i = 0; i < 16 / kRowsAtOnce; ++i) {
         x[i].x = (x[i].x & ta.q_and) ^ ta.q_xor, x[i].y = (x[i].y & ta.q_and) ^ ta.q_xor;
         x[i].z = (x[i].z & ta.q_and) ^ ta.q_xor, x[i].w = (x[i].w & ta.q_and) ^ ta.q_xor;
-        asm volatile("st.shared.v4.u32 [%0], {%1, %2, %3, %4};" ::"r"(dst + (ch >> 3) * C::kPanel + (((ch & 7) ^ (r & 7)) << 4)),
+        asm volatile("st.shared.v4.u32 [%0], {%1, %2, %3, %4};" ::"r"(place((warp & 7) * 16 + i * kRowsAtOnce + lane / kLanes, lane % kLanes)),
                      "r"(x[i].x), "r"(x[i].y), "r"(x[i].z), "r"(x[i].w) : "memory");
       }
       fence_proxy_async_smem();
@@ -787,7 +795,7 @@ attn_tile_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constan
     float f0 = 1.0f, f1 = 0.0f;
     const bool join = !two && n_tiles > 1;
     float4* room = reinterpret_cast<float4*>(smem_raw + (ring - smem_u32(smem_raw))) + half * (D / 8) * kTile;   // [D / 4][128 rows]
-    float2* room_ml = reinterpret_cast<float2*>(smem_raw + (sq - smem_u32(smem_raw)));
+    float2* room_ml = reinterpret_cast<float2*>(s_swap);
     if (join) {
       named_bar_sync(kBarSoft, kSoft);   // every MMA has completed: the operand tiles are free
       if (acc == 1) {
@@ -842,12 +850,23 @@ attn_tile_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constan
 #pragma unroll
           for (int j = 0; j < 4; ++j)
             reinterpret_cast<float4*>(pp)[(half * (D / 8) + 4 * h + j) * kTile + r] = make_float4(v[4 * j], v[4 * j + 1], v[4 * j + 2], v[4 * j + 3]);
-        } else if (live) {
-          uint4* dst = reinterpret_cast<uint4*>(a.out + out_row * D + half * (D / 2) + 16 * h);
+        } else {   // by way of the query tile, which no MMA reads any more
 #pragma unroll
           for (int j = 0; j < 2; ++j)
-            dst[j] = make_uint4(pack_f16(v[8 * j] * inv, v[8 * j + 1] * inv), pack_f16(v[8 * j + 2] * inv, v[8 * j + 3] * inv),
-                                pack_f16(v[8 * j + 4] * inv, v[8 * j + 5] * inv), pack_f16(v[8 * j + 6] * inv, v[8 * j + 7] * inv));
+            asm volatile("st.shared.v4.u32 [%0], {%1, %2, %3, %4};" ::"r"(place(r, half * (D / 16) + 2 * h + j)),
+                         "r"(pack_f16(v[8 * j] * inv, v[8 * j + 1] * inv)), "r"(pack_f16(v[8 * j + 2] * inv, v[8 * j + 3] * inv)),
+                         "r"(pack_f16(v[8 * j + 4] * inv, v[8 * j + 5] * inv)), "r"(pack_f16(v[8 * j + 6] * inv, v[8 * j + 7] * inv)) : "memory");
+        }
+      }
+      if (parts == 1) {
+        named_bar_sync(pair, 64);   // the row's other half
+#pragma unroll
+        for (int i = 0; i < 16 / kRowsAtOnce; ++i) {   // of the pair's 32 rows
+          const int row = (warp & 3) * 32 + half * 16 + i * kRowsAtOnce + lane / kLanes;
+          uint4 x;
+          asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(x.x), "=r"(x.y), "=r"(x.z), "=r"(x.w) : "r"(place(row, lane % kLanes)) : "memory");
+          const __half* p = row_at(a.out, static_cast<int64_t>(a.heads) * D, row);
+          if (p != nullptr) reinterpret_cast<uint4*>(const_cast<__half*>(p))[lane % kLanes] = x;
         }
       }
       if (parts > 1 && half == 0) reinterpret_cast<float2*>(pp + kTile * D)[r] = make_float2(m, l);
