@@ -247,8 +247,8 @@ __device__ __forceinline__ SlotKeys slot_keys(const AttnArgs& a, const AttnRange
 template <int D>
 constexpr int kPartFloats = 2 * kTile * (D + 2);
 
-// Joins the parts of the units whose keys were split, in their order: grid (unit, 32 rows), a warp per 4 features in
-// turn, lanes along the rows.  (One CTA per unit, the last to arrive, took 30 us for 16 parts of 133 KB.)
+// Joins the parts of the units whose keys were split, in their order: grid (unit, 32 rows, 32 features), a warp per 4
+// features, lanes along the rows; L2 latency, so one short chain of loads per thread.  (One CTA per unit, the last to arrive, took 30 us for 16 parts of 133 KB.)
 constexpr int kJoinThreads = 256;
 template <int D>
 __global__ void __launch_bounds__(kJoinThreads) attn_join_kernel(const AttnArgs a, int most_parts) {
@@ -283,22 +283,15 @@ __global__ void __launch_bounds__(kJoinThreads) attn_join_kernel(const AttnArgs 
     L = fmaf(ml.y, exp2_approx(ml.x - Ms), L);
   }
   const float Li = L > 0.0f ? 1.0f / L : 0.0f;
-  constexpr int kMine = D / 32;   // groups of 4 features per warp
-  float4 v[kMine];
-#pragma unroll
-  for (int j = 0; j < kMine; ++j) v[j] = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-#pragma unroll 4
+  const int f4 = blockIdx.z * (kJoinThreads / 32) + warp;   // of 4 features each
+  float4 v = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+#pragma unroll 8
   for (int q = 0; q < sk.parts; ++q) {
     const float w = exp2_approx(stats(q).x - Ms) * Li;
-#pragma unroll
-    for (int j = 0; j < kMine; ++j) {
-      const float4 x = __ldcg(reinterpret_cast<const float4*>(p0 + static_cast<int64_t>(q) * kPart) + (warp * kMine + j) * kTile + r);
-      v[j].x = fmaf(x.x, w, v[j].x), v[j].y = fmaf(x.y, w, v[j].y), v[j].z = fmaf(x.z, w, v[j].z), v[j].w = fmaf(x.w, w, v[j].w);
-    }
+    const float4 x = __ldcg(reinterpret_cast<const float4*>(p0 + static_cast<int64_t>(q) * kPart) + f4 * kTile + r);
+    v.x = fmaf(x.x, w, v.x), v.y = fmaf(x.y, w, v.y), v.z = fmaf(x.z, w, v.z), v.w = fmaf(x.w, w, v.w);
   }
-  __half* out = a.out + (row * a.heads + hk * G + r % G) * D + warp * (4 * kMine);
-#pragma unroll
-  for (int j = 0; j < kMine; ++j) *reinterpret_cast<uint2*>(out + 4 * j) = make_uint2(pack_f16(v[j].x, v[j].y), pack_f16(v[j].z, v[j].w));
+  *reinterpret_cast<uint2*>(a.out + (row * a.heads + hk * G + r % G) * D + 4 * f4) = make_uint2(pack_f16(v.x, v.y), pack_f16(v.z, v.w));
 }
 
 // Tensor bound for long chunks, HBM bound for wide drafts over long caches.
@@ -919,7 +912,7 @@ int launch(TileArgs& t, const TilePlan& plan, cudaStream_t stream) {
   }
   const dim3 grid(static_cast<unsigned>(plan.units), static_cast<unsigned>(plan.parts));
   if (const int rc = launch_dependent(kern, grid, dim3(C::kThreads), C::kSmem, stream, mk, mv, t); rc != PQ_OK || plan.parts == 1) return rc;
-  return launch_dependent(attn_join_kernel<D>, dim3(grid.x, 8), dim3(kJoinThreads), 0, stream, t.a, plan.parts);
+  return launch_dependent(attn_join_kernel<D>, dim3(grid.x, 8, D / 32), dim3(kJoinThreads), 0, stream, t.a, plan.parts);
 }
 
 }  // namespace
