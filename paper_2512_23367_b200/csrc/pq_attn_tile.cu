@@ -84,10 +84,11 @@ __device__ __forceinline__ void named_bar_arrive(uint32_t id, uint32_t nthreads)
 }
 // Named barriers (0 is __syncthreads): the softmax warpgroups among themselves; "P written", one per accumulator
 // (256 threads arrive, the issuer's warp waits); "operand tile landed", between the watcher's and the issuer's warp;
-// the two warps that share 32 rows, eight pairs; "S read", 256 threads of an accumulator to the issuer, one each.
+// the two warps that share 32 rows, eight pairs; "S read", 256 threads of an accumulator to the issuer, one each;
+// "tensor memory read", all softmax threads to the issuer, at the end.
 // They do not pass through shared memory, which the tensor core keeps busy: a wait on an mbarrier that has long
 // completed takes 200 to 400 cycles here, one on a named barrier about 30.
-constexpr uint32_t kBarSoft = 1, kBarP = 2, kBarTile = 4, kBarPair = 5, kBarRead = 13;
+constexpr uint32_t kBarSoft = 1, kBarP = 2, kBarTile = 4, kBarPair = 5, kBarRead = 13, kBarFree = 15;
 // Meets the other warp of the pair; whether any of the 64 threads says yes.
 __device__ __forceinline__ bool pair_any(uint32_t id, bool yes) {
   uint32_t r;
@@ -150,25 +151,24 @@ __device__ __forceinline__ float max3(float a, float b, float c) {
   asm("max.f32 %0, %1, %2, %3;" : "=f"(d) : "f"(a), "f"(b), "f"(c));
   return d;
 }
-// Blocks of 16 keys of one request, eight to a tile (`block` of them): the index of the block's first cache vector, tile
-// by tile, or -1 where there is nothing to read.  The page id of a tile is fetched while the one before is in use.
-template <bool kUsed>
+// Blocks of 16 keys of one request, a lane each, so that one look-up serves four key tiles: the index of the block's first
+// cache vector, or -1 where there is nothing to read.  The page ids of the next 32 blocks are on the way meanwhile.
 struct BlockWalk {
   const int* trow;
-  int key, hi, lo, left, page16, col, off, step_col, step_off, heads, hk, id;
-  int64_t pages;
-  __device__ __forceinline__ BlockWalk(const AttnArgs& a, const AttnRange& rg, int b, int head, int key_base, int tiles, int block)
-      : trow(a.table + static_cast<int64_t>(b) * a.width), key(key_base + 16 * block), hi(rg.hi), lo(rg.lo), left(tiles),
-        page16(a.c.page >> 4), heads(a.c.heads), hk(head), pages(a.c.pages) {
-    col = (key >> 4) / page16, off = (key >> 4) - col * page16;
-    step_col = 8 / page16, step_off = 8 - step_col * page16;
+  int64_t key, pages;
+  int hi, lo, page16, col, off, step_col, step_off, heads, hk, id;
+  __device__ __forceinline__ BlockWalk(const AttnArgs& a, const AttnRange& rg, int b, int head, int key_base, int lane)
+      : trow(a.table + static_cast<int64_t>(b) * a.width), key(key_base + 16 * lane), pages(a.c.pages), hi(rg.hi), lo(rg.lo),
+        page16(a.c.page >> 4), heads(a.c.heads), hk(head) {
+    const int block = (key_base >> 4) + lane;
+    col = block / page16, off = block - col * page16;
+    step_col = 32 / page16, step_off = 32 - step_col * page16;
     fetch();
   }
-  __device__ __forceinline__ void fetch() { id = left > 0 && key < hi && key + 16 > lo ? trow[col] : -1; }
+  __device__ __forceinline__ void fetch() { id = key < hi && key + 16 > lo ? trow[col] : -1; }
   __device__ __forceinline__ int next() {
     const int v = id < 0 || id >= pages ? -1 : static_cast<int>(((static_cast<int64_t>(id) * heads + hk) * page16 + off) * 16);
-    key += kTile;
-    --left;
+    key += 4 * kTile;
     col += step_col, off += step_off;
     if (off >= page16) off -= page16, ++col;
     fetch();
@@ -186,8 +186,18 @@ struct TileArgs {
   int* status;
   uint32_t wait_limit;
   int box;               // rows of a TMA box: the largest power of two that divides both the page and 128
+  uint32_t group_mul;    // i / group = i * group_mul >> 16 for i up to 256
   uint32_t q_and, q_xor; // a scale of 0 or below is folded into the queries: (q & q_and) ^ q_xor
 };
+
+__device__ __forceinline__ int warp_prefix(int v, int lane) {   // inclusive sums
+#pragma unroll
+  for (int o = 1; o < 32; o <<= 1) {
+    const int x = __shfl_up_sync(0xffffffffu, v, o);
+    if (lane >= o) v += x;
+  }
+  return v;
+}
 
 // Which request and which of its tiles of `qt` tokens: the slot-th over all requests that this kernel serves (a request's
 // last tile, which sees most keys, comes first).  found: request (-1: there are fewer), tile, first row, rows, cached
@@ -206,19 +216,12 @@ __device__ __forceinline__ void find_slot(const AttnArgs& a, int slot, int qt, v
       L = a.kv_len[b];
       if (n > a.row_tokens) cnt = (n - 1) / qt + 1;   // the others are the row kernel's
     }
-    int in = cnt;
-#pragma unroll
-    for (int o = 1; o < 32; o <<= 1) {
-      const int x = __shfl_up_sync(0xffffffffu, in, o);
-      if (lane >= o) in += x;
-    }
+    const int in = warp_prefix(cnt, lane);
     if (lane == 31) sums[warp] = in;
     __syncthreads();
-    int off = before;
-    for (int w = 0; w < kThreads / 32; ++w) {
-      if (w < warp) off += sums[w];
-      before += sums[w];
-    }
+    const int of_warp = lane < kThreads / 32 ? sums[lane] : 0, to_warp = warp_prefix(of_warp, lane);
+    const int off = before + __shfl_sync(0xffffffffu, to_warp - of_warp, warp);
+    before += __shfl_sync(0xffffffffu, to_warp, 31);
     const int mine = slot - (off + in - cnt);
     if (mine >= 0 && mine < cnt) found[0] = b, found[1] = cnt - 1 - mine, found[2] = q0, found[3] = n, found[4] = L;
     __syncthreads();
@@ -240,7 +243,7 @@ __device__ __forceinline__ SlotKeys slot_keys(const AttnArgs& a, const AttnRange
   s.k_lo = (a.window > 0 ? max(0, s.p_base + 1 - a.window) : 0) & ~(kTile - 1);
   s.tiles = k_hi > s.k_lo ? (k_hi - s.k_lo + kTile - 1) / kTile : 0;
   s.per = a.part_keys / kTile;
-  s.parts = max(1, min(most_parts, (s.tiles + s.per - 1) / s.per));
+  s.parts = most_parts == 1 ? 1 : max(1, min(most_parts, (s.tiles + s.per - 1) / s.per));
   return s;
 }
 
@@ -338,7 +341,8 @@ attn_tile_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constan
   const AttnArgs& a = ta.a;
   const int tid = threadIdx.x, warp = __shfl_sync(0xffffffffu, tid >> 5, 0), lane = tid & 31;
   const int G = a.heads / a.c.heads;
-  const int tpt = kTile / G;          // tokens of one accumulator
+  auto by_group = [&](int i) { return static_cast<int>(static_cast<uint32_t>(i) * ta.group_mul >> 16); };
+  const int tpt = by_group(kTile);    // tokens of one accumulator
   const int qt = 2 * tpt;             // tokens of one CTA
   const int slot = blockIdx.x / a.c.heads, hk = blockIdx.x - slot * a.c.heads;
 
@@ -358,15 +362,17 @@ attn_tile_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constan
     if (!kInt8) tma_prefetch_desc(&map_k), tma_prefetch_desc(&map_v);
   }
   // (All CTAs of the launch before hold their tensor memory by now, or have given it back: they let this one begin.)
-  if (warp == kIssuer) tmem_alloc(smem_u32(&s_tmem), 512);
+  if (warp == kIssuer) {
+    tmem_alloc(smem_u32(&s_tmem), 512);
+    tmem_relinquish();
+  }
   tc_fence_before_sync();
   grid_dep_wait();
-  __syncthreads();
+  find_slot<kThreads>(a, slot, qt, s_assign, s_warp_sum);   // at least two barriers of the block
   tc_fence_after_sync();
   grid_dep_launch();   // only now: a later launch's CTA may take this SM's tensor memory when it is given back
   const uint32_t tmem = __shfl_sync(0xffffffffu, s_tmem, 0);
 
-  find_slot<kThreads>(a, slot, qt, s_assign, s_warp_sum);
   const int b = s_assign[0];
   const int tok0 = s_assign[1] * qt;
   const AttnRange rg = attn_range(a, s_assign[3], s_assign[4]);
@@ -376,10 +382,7 @@ attn_tile_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constan
   const bool two = toks > tpt;
   const int part = blockIdx.y;
   if (b < 0 || part >= parts) {
-    if (warp == kIssuer) {
-      tmem_relinquish();
-      tmem_dealloc(tmem, 512);
-    }
+    if (warp == kIssuer) tmem_dealloc(tmem, 512);
     return;
   }
   const int t0 = part * sk.per;
@@ -405,19 +408,19 @@ attn_tile_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constan
       const int c = tid - 20 * 32;
       constexpr int kStep = C::kConv / kRow;
       const int piece = c % kRow, row_in = c / kRow;    // item k: row k * kStep + row_in
-      BlockWalk<kInt8> walk(a, rg, b, hk, key_base, n_tiles, lane & 7);
-      int vec = walk.next(), vec1 = walk.next(), vec2 = walk.next();   // tiles t, t + 1, t + 2
+      BlockWalk walk(a, rg, b, hk, key_base, lane);
+      int vec = walk.next(), vec4 = -1;   // of the four tiles that t is one of, and of the next four
       // Work goes in batches of two items; the batch three further on is copied into the slots that one leaves (the
       // thread's own: no other thread reads them), or zeros.
       constexpr int kBatches = kItems / 2;              // per operand tile
       const uint32_t raw = scales + C::kScaleTiles * C::kScaleFloats * 4 + c * 16;
-      auto request = [&](int n, int v) {                // batch n of all
-        const int i = n / kBatches;
+      auto request = [&](int n, int t) {                // batch n of all, while tile t is in work
+        const int i = n / kBatches, v = (i >> 3) == (t >> 2) ? vec : vec4;
         if (i < 2 * n_tiles) {
 #pragma unroll
           for (int q = 0; q < 2; ++q) {
             const int r = ((n % kBatches) * 2 + q) * kStep + row_in;
-            const int first = __shfl_sync(0xffffffffu, v, r >> 4);
+            const int first = __shfl_sync(0xffffffffu, v, 8 * ((i >> 1) & 3) + (r >> 4));
             const uint4* src = static_cast<const uint4*>((i & 1) ? a.c.v : a.c.k) + (static_cast<int64_t>(max(first, 0)) + (r & 15)) * kRow + piece;
             asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(raw + ((n % 3) * 2 + q) * (16 * C::kConv)), "l"(src), "r"(first < 0 ? 0 : 16) : "memory");
           }
@@ -425,7 +428,7 @@ attn_tile_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constan
         asm volatile("cp.async.commit_group;" ::: "memory");
       };
 #pragma unroll
-      for (int n = 0; n < 3; ++n) request(n, n / kBatches < 2 ? vec : vec1);
+      for (int n = 0; n < 3; ++n) request(n, 0);
       bool ok = true, free_next = false;
       for (int i = 0; i < 2 * n_tiles; ++i) {
         const int st = i % C::kStages, t = i >> 1;
@@ -458,10 +461,10 @@ attn_tile_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constan
                            "r"(codes_f16(w0, 0x4140)), "r"(codes_f16(w0, 0x4342)), "r"(codes_f16(w1, 0x4140)), "r"(codes_f16(w1, 0x4342)) : "memory");
             }
           }
-          const int ahead = ((n + 3) / kBatches) / 2 - t;   // tiles
-          request(n + 3, ahead == 0 ? vec : (ahead == 1 ? vec1 : vec2));
+          request(n + 3, t);   // two tiles ahead at most
         }
-        if (is_v) vec = vec1, vec1 = vec2, vec2 = walk.next();
+        if (is_v && (t & 3) == 1) vec4 = walk.next();
+        if (is_v && (t & 3) == 3) vec = vec4;
         free_next = __all_sync(0xffffffffu, asked);
         fence_proxy_async_smem();
         __syncwarp();
@@ -480,18 +483,20 @@ attn_tile_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constan
       const bool mine = lane < boxes * halves;
       const int rows_all = static_cast<int>(a.c.pages * a.c.heads * a.c.page);
       const int* trow = a.table + static_cast<int64_t>(b) * a.width;
-      auto row_of = [&](int t) {   // of the tensor map; rows_all lies beyond the tensor: zeros
+      int id = -1, off = 0;        // page of the box and the place in it
+      auto look_up = [&](int t) {
         const int key = key_base + t * kTile + y * ta.box;
-        if (!mine || t >= n_tiles || key >= rg.hi || key + ta.box <= rg.lo) return rows_all;
+        id = -1;
+        if (!mine || t >= n_tiles || key >= rg.hi || key + ta.box <= rg.lo) return;
         const int col = key / a.c.page;
-        const int id = trow[col];
-        if (id < 0 || id >= a.c.pages) return rows_all;
-        return static_cast<int>((static_cast<int64_t>(id) * a.c.heads + hk) * a.c.page) + key - col * a.c.page;
+        off = key - col * a.c.page;
+        id = trow[col];
       };
-      int row = row_of(0);
+      look_up(0);
       for (int t = 0; t < n_tiles; ++t) {
         const int i = 2 * t + is_v, st = i % C::kStages;
-        const int next = row_of(t + 1);
+        // row of the tensor map; rows_all lies beyond the tensor: zeros
+        const int row = id < 0 || id >= a.c.pages ? rows_all : static_cast<int>((static_cast<int64_t>(id) * a.c.heads + hk) * a.c.page) + off;
         if (i >= C::kStages && !warp_wait(bar_free + 8 * st, ((i / C::kStages) & 1) ^ 1, wc)) break;
         const int key0 = key_base + t * kTile;
         // rows of the tile that were never written: before the request's window, beyond its length
@@ -501,7 +506,7 @@ attn_tile_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constan
         if (lane == 0) mbar_arrive_expect_tx(bar, C::kTileBytes);
         __syncwarp();
         if (mine) tma_load_2d(dst + x * C::kPanel + y * ta.box * 128, is_v ? &map_v : &map_k, bar, x * 64, row);
-        row = next;
+        look_up(t + 1);   // used, and so waited for, in the next round
         issued = t + 1;
         if (fix) {
           if (!warp_wait(bar_fix, fix_phase & 1, wc)) break;
@@ -523,16 +528,18 @@ attn_tile_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constan
       if constexpr (kInt8) {
         const bool is_v = warp == kLoadV;
         const float* from = is_v ? a.c.v_scale : a.c.k_scale;
-        BlockWalk<kInt8> walk(a, rg, b, hk, key_base, n_tiles, lane >> 2);
-        auto load = [&]() {
-          const int v = walk.next();
+        BlockWalk walk(a, rg, b, hk, key_base, lane);
+        int vec = -1;
+        auto load = [&](int t) {
+          if ((t & 3) == 0) vec = walk.next();
+          const int v = __shfl_sync(0xffffffffu, vec, 8 * (t & 3) + (lane >> 2));
           return v < 0 ? make_float4(0.0f, 0.0f, 0.0f, 0.0f) : __ldg(reinterpret_cast<const float4*>(from + v) + (lane & 3));
         };
-        float4 next = load();
+        float4 next = load(0);
         bool ok = true;
         for (int t = 0; t < n_tiles; ++t) {
           float4 s = next;
-          next = load();
+          next = load(t + 1);
           const int key = key_base + t * kTile + 4 * lane;   // 0 where nothing was written
           s.x = key >= rg.lo && key < rg.hi ? s.x : 0.0f, s.y = key + 1 >= rg.lo && key + 1 < rg.hi ? s.y : 0.0f;
           s.z = key + 2 >= rg.lo && key + 2 < rg.hi ? s.z : 0.0f, s.w = key + 3 >= rg.lo && key + 3 < rg.hi ? s.w : 0.0f;
@@ -603,6 +610,16 @@ attn_tile_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constan
           __syncwarp();
         }
       }
+      // Giving tensor memory back takes 2000 cycles: under the results' way to global memory.  MMAs that the softmax
+      // threads have not waited for (only after one of them gave up) have to end first.
+      named_bar_sync(kBarFree, kSoft + 32);
+      tc_fence_after_sync();
+      if (s_abort && leader) {
+        umma_commit(bar_drain);
+        mbar_drain(bar_drain, 0u);
+      }
+      __syncwarp();
+      tmem_dealloc(tmem, 512);
     } else if (warp == kWatcher) {
       // ------------------------------------------------------------------ watcher: waits for the operand tiles a step ahead
       bool ok = true;
@@ -619,6 +636,10 @@ attn_tile_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constan
     }
   } else {
     // -------------------------------------------------------------------- softmax, two threads per row
+    auto release_tmem = [&]() {   // the warp has read its last
+      tc_fence_before_sync();
+      named_bar_arrive(kBarFree, kSoft + 32);
+    };
     asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(C::kSoftRegs));
     const int acc = warp >> 3;                       // accumulator
     const int half = (warp >> 2) & 1;                // the thread's 64 keys of a tile, and its half of the features
@@ -628,24 +649,26 @@ attn_tile_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constan
     float* swap = s_swap + acc * kTile + r;
     const uint32_t pair = kBarPair + acc * 4 + (warp & 3);
     const int q_tile = two ? acc : 0;
-    const int tok = q_tile * tpt + r / G;            // token of the row, from tok0
-    // Where row i of the query tile begins in a matrix of `stride` elements per token: nullptr if there is no such row.
-    auto row_at = [&](const __half* m, int64_t stride, int i) -> const __half* {
-      const int k = q_tile * tpt + i / G;
+    const int tok = q_tile * tpt + by_group(r);      // token of the row, from tok0
+    // Where row i of the query tile begins in a matrix of `stride` elements per token: -1 if there is no such row.
+    auto row_at = [&](int64_t stride, int i) -> int64_t {
+      const int it = by_group(i), k = q_tile * tpt + it;
       const int64_t row = row0 + tok0 + k;
-      return i < tpt * G && k < toks && row >= 0 && row < a.tokens ? m + row * stride + (hk * G + i % G) * D : nullptr;
+      return it < tpt && k < toks && row >= 0 && row < a.tokens ? row * stride + (hk * G + i - it * G) * D : -1;
     };
     // Rows go between global and shared memory whole, D / 8 lanes side by side (a thread per row instead took 3000
-    // cycles at each end): piece c of row i at its swizzled place.
+    // cycles at each end): piece c of row i at its swizzled place.  A warp moves 16 rows; a lane works out where one
+    // begins and the others ask it.
     constexpr int kLanes = D / 8, kRowsAtOnce = 32 / kLanes;
     auto place = [&](int i, int c) { return sq + q_tile * C::kTileBytes + (c >> 3) * C::kPanel + i * 128 + (((c & 7) ^ (i & 7)) << 4); };
 
     if (two || acc == 0) {
+      const int64_t begin = row_at(a.q_stride, (warp & 7) * 16 + (lane & 15));
       uint4 x[16 / kRowsAtOnce];
 #pragma unroll
-      for (int i = 0; i < 16 / kRowsAtOnce; ++i) {   // 16 rows per warp
-        const __half* p = row_at(a.q, a.q_stride, (warp & 7) * 16 + i * kRowsAtOnce + lane / kLanes);
-        x[i] = p != nullptr ? __ldg(reinterpret_cast<const uint4*>(p) + lane % kLanes) : make_uint4(0, 0, 0, 0);
+      for (int i = 0; i < 16 / kRowsAtOnce; ++i) {
+        const int64_t p = __shfl_sync(0xffffffffu, begin, i * kRowsAtOnce + lane / kLanes);
+        x[i] = p >= 0 ? __ldg(reinterpret_cast<const uint4*>(a.q + p) + lane % kLanes) : make_uint4(0, 0, 0, 0);
       }
 #pragma unroll
       for (int i = 0; i < 16 / kRowsAtOnce; ++i) {
@@ -820,6 +843,7 @@ attn_tile_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constan
     constexpr int kPart = kPartFloats<D>;
     float* pu = a.partials + unit * gridDim.y * kPart;
     const float inv = l > 0.0f ? 1.0f / l : 0.0f;
+    if (!writes) release_tmem();
     if (writes) {
       float* pp = pu + part * kPart + q_tile * kTile * (D + 2);
 #pragma unroll 1
@@ -852,15 +876,18 @@ attn_tile_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constan
                          "r"(pack_f16(v[8 * j + 4] * inv, v[8 * j + 5] * inv)), "r"(pack_f16(v[8 * j + 6] * inv, v[8 * j + 7] * inv)) : "memory");
         }
       }
+      release_tmem();
       if (parts == 1) {
+        const int row16 = (warp & 3) * 32 + half * 16;   // of the pair's 32 rows
+        const int64_t begin = row_at(static_cast<int64_t>(a.heads) * D, row16 + (lane & 15));
         named_bar_sync(pair, 64);   // the row's other half
 #pragma unroll
-        for (int i = 0; i < 16 / kRowsAtOnce; ++i) {   // of the pair's 32 rows
-          const int row = (warp & 3) * 32 + half * 16 + i * kRowsAtOnce + lane / kLanes;
+        for (int i = 0; i < 16 / kRowsAtOnce; ++i) {
           uint4 x;
-          asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(x.x), "=r"(x.y), "=r"(x.z), "=r"(x.w) : "r"(place(row, lane % kLanes)) : "memory");
-          const __half* p = row_at(a.out, static_cast<int64_t>(a.heads) * D, row);
-          if (p != nullptr) reinterpret_cast<uint4*>(const_cast<__half*>(p))[lane % kLanes] = x;
+          asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(x.x), "=r"(x.y), "=r"(x.z), "=r"(x.w)
+                       : "r"(place(row16 + i * kRowsAtOnce + lane / kLanes, lane % kLanes)) : "memory");
+          const int64_t p = __shfl_sync(0xffffffffu, begin, i * kRowsAtOnce + lane / kLanes);
+          if (p >= 0) reinterpret_cast<uint4*>(a.out + p)[lane % kLanes] = x;
         }
       }
       if (parts > 1 && half == 0) reinterpret_cast<float2*>(pp + kTile * D)[r] = make_float2(m, l);
@@ -868,27 +895,17 @@ attn_tile_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constan
   }
 
   // ---------------------------------------------------------------------- teardown
-  __syncwarp();
-  tc_fence_before_sync();
   __syncthreads();
   if (s_abort) {
     // Some role gave up.  What has been handed to the hardware still completes by itself and must have done so
-    // before shared and tensor memory go away: the producer's loads and the issuer's MMAs.
+    // before shared memory goes away: the producers' loads, and the issuer's MMAs (which it has seen to).
     if (!kInt8 && lane == 0 && (warp == kLoadK || warp == kLoadV)) {
       for (int i = 2 * issued + (warp == kLoadV) - 2; i >= 0 && i >= 2 * issued - C::kStages; i -= 2)
         mbar_drain(bar_full + 8 * (i % C::kStages), (i / C::kStages) & 1u);
       if (warp == kLoadV) mbar_drain(bar_fix, fix_phase & 1u);
-    } else if (tid == kIssuer * 32) {
-      umma_commit(bar_drain);
-      mbar_drain(bar_drain, 0u);
     }
     __syncthreads();
     if (tid == 0) atomicExch(ta.status, static_cast<int>(PQ_ERR_TIMEOUT));
-  }
-  tc_fence_after_sync();
-  if (warp == kIssuer) {
-    tmem_relinquish();
-    tmem_dealloc(tmem, 512);
   }
 }
 
@@ -949,7 +966,8 @@ TilePlan plan_attn_tile(int64_t requests, int64_t tokens, int64_t max_q, int64_t
 int launch_attn_tile(const AttnArgs& a, const TilePlan& plan, cudaStream_t stream) {
   if (plan.units < 1) return PQ_OK;
   if (plan.units > 0x7fffffff) return PQ_ERR_SHAPE;
-  TileArgs t{a, device_status_ptr(), wait_limit(), 128, 0xffffffffu, 0u};
+  const uint32_t group = static_cast<uint32_t>(a.heads / a.c.heads);
+  TileArgs t{a, device_status_ptr(), wait_limit(), 128, (65535u + group) / group, 0xffffffffu, 0u};
   if (t.status == nullptr) return PQ_ERR_CUDA;
   while (a.c.page % t.box != 0) t.box /= 2;   // the page is a multiple of 16
   t.a.part_keys = plan.part_keys;
