@@ -42,8 +42,8 @@ int pq_paged_attention(const void* q_f16, int64_t q_stride, int32_t heads, const
     rc = launch_attn_rows(a, plan, max_q, st);
     if (rc != PQ_OK || !wide) return rc;
   }
-  const TilePlan tile = plan_attn_tile(requests, tokens, max_q, max_kv, group, cache->heads, cache->dim, sm_count(),
-                                       sc.partial_bytes);
+  const TilePlan tile = plan_attn_tile(requests, tokens, max_q, max_kv, window, group, cache->heads, cache->dim,
+                                       sm_count(), sc.partial_bytes);
   return launch_attn_tile(a, tile, st);
 }
 
@@ -59,7 +59,7 @@ size_t pq_attention_workspace_bytes(int64_t requests, int64_t tokens, int64_t ma
     bytes = bytes > plan.partial_bytes ? bytes : plan.partial_bytes;
   }
   if (max_q * (heads / kv_heads) > kAttnRows) {
-    const TilePlan tile = plan_attn_tile(requests, tokens, max_q, max_kv, heads / kv_heads, kv_heads, dim, sms, ~size_t(0));
+    const TilePlan tile = plan_attn_tile(requests, tokens, max_q, max_kv, 0, heads / kv_heads, kv_heads, dim, sms, ~size_t(0));
     bytes = bytes > tile.partial_bytes ? bytes : tile.partial_bytes;   // the two kernels follow each other
   }
   return bytes > 0 ? kScratchHeaderBytes + bytes : 0;

@@ -43,13 +43,14 @@ int launch_attn_rows(const AttnArgs& a, const AttnPlan& plan, int64_t max_q, cud
 
 // The tile kernel's schedule: a unit is one tile of 2 x (128 / group) tokens of one key/value head.
 struct TilePlan {
-  int64_t units = 0;      // CTAs per part: an upper bound of the units there are
+  int64_t whole = 0;      // units that one CTA serves whole
+  int64_t split = 0;      // units after those, whose keys are cut into up to `parts` parts; both are upper bounds
   int parts = 1;
   int part_keys = 128;
   size_t partial_bytes = 0;
 };
-TilePlan plan_attn_tile(int64_t requests, int64_t tokens, int64_t max_q, int64_t max_kv, int group, int kv_heads, int dim,
-                        int sms, size_t room);
+TilePlan plan_attn_tile(int64_t requests, int64_t tokens, int64_t max_q, int64_t max_kv, int window, int group, int kv_heads,
+                        int dim, int sms, size_t room);
 int launch_attn_tile(const AttnArgs& a, const TilePlan& plan, cudaStream_t stream);
 
 __device__ __forceinline__ float exp2_approx(float x) {

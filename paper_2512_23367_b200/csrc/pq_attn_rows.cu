@@ -1,6 +1,4 @@
 // Attention of up to 16 query rows per (request, key/value head) over the paged cache: decode steps and short drafts.
-#include <cstdlib>
-
 #include "pq_attention.h"
 #include "pq_ptx.cuh"
 
@@ -543,7 +541,6 @@ int launch(const AttnArgs& a, const AttnPlan& plan, int64_t max_q, cudaStream_t 
 AttnPlan plan_attn_rows(int64_t requests, int64_t max_q, int64_t max_kv, int window, int kv_heads, int dim, bool int8, int sms, size_t room) {
   AttnPlan p;
   p.units = requests * kv_heads;
-  static const int forced = [] { const char* e = getenv("PQ_ATTN_PART"); return e ? atoi(e) : 0; }();   // ablation knob
   if (max_q > kAttnRows) max_q = kAttnRows;   // longer chunks are the tile kernel's
   if (window > 0 && max_kv > window + max_q) max_kv = window + max_q;
   const int64_t slots = static_cast<int64_t>(rows_ctas(int8, dim)) * sms;
@@ -560,7 +557,6 @@ AttnPlan plan_attn_rows(int64_t requests, int64_t max_q, int64_t max_kv, int win
   const int64_t n = (max_kv + keys / 2) / keys;   // no part much smaller than the others
   if (n > 0) keys = (max_kv + 15 + n - 1) / n;
   keys = (keys + 127) / 128 * 128;
-  if (forced > 0) keys = (forced + 127) / 128 * 128;
   p.part_keys = static_cast<int>(keys);
   int64_t parts = (max_kv + 15 + keys - 1) / keys;   // the first part begins at a multiple of 16
   if (p.units > kScratchCounters || parts < 1) parts = 1;

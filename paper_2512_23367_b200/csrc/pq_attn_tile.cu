@@ -1,7 +1,5 @@
 // Attention of more than 16 query rows per (request, key/value head) over the paged cache, on the tcgen05 tensor
 // cores: prompts, chunks of prompts and wide drafts.
-#include <cstdlib>
-
 #include "pq_attention.h"
 #include "pq_ptx.cuh"
 
@@ -187,6 +185,7 @@ struct TileArgs {
   uint32_t wait_limit;
   int box;               // rows of a TMA box: the largest power of two that divides both the page and 128
   uint32_t group_mul;    // i / group = i * group_mul >> 16 for i up to 256
+  int whole, split, parts;   // as planned: CTAs of whole units, then part 0 of the others, part 1, ...
   uint32_t q_and, q_xor; // a scale of 0 or below is folded into the queries: (q & q_and) ^ q_xor
 };
 
@@ -252,17 +251,18 @@ template <int D>
 constexpr int kPartFloats = 2 * kTile * (D + 2);
 
 // Joins the parts of the units whose keys were split, in their order: grid (unit, 32 rows, 32 features), a warp per 4
-// features, lanes along the rows; L2 latency, so one short chain of loads per thread.  (One CTA per unit, the last to arrive, took 30 us for 16 parts of 133 KB.)
+// features, lanes along the rows; L2 latency, so one short chain of
+// loads per thread.  (One CTA per unit, the last to arrive, took 30 us for 16 parts of 133 KB.)
 constexpr int kJoinThreads = 256;
 template <int D>
-__global__ void __launch_bounds__(kJoinThreads) attn_join_kernel(const AttnArgs a, int most_parts) {
+__global__ void __launch_bounds__(kJoinThreads) attn_join_kernel(const AttnArgs a, int whole, int most_parts) {
   __shared__ int s_assign[5];
   __shared__ int s_warp_sum[kJoinThreads / 32];
   grid_dep_launch();
   grid_dep_wait();
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const int G = a.heads / a.c.heads, tpt = kTile / G, qt = 2 * tpt;
-  const int slot = blockIdx.x / a.c.heads, hk = blockIdx.x - slot * a.c.heads;
+  const int unit = whole + blockIdx.x, slot = unit / a.c.heads, hk = unit - slot * a.c.heads;
   __syncthreads();
   find_slot<kJoinThreads>(a, slot, qt, s_assign, s_warp_sum);
   if (s_assign[0] < 0) return;
@@ -276,25 +276,34 @@ __global__ void __launch_bounds__(kJoinThreads) attn_join_kernel(const AttnArgs 
   if (!live) return;   // no barrier follows
   constexpr int kPart = kPartFloats<D>;
   const float* p0 = a.partials + static_cast<int64_t>(blockIdx.x) * most_parts * kPart + tile * kTile * (D + 2);
-  auto stats = [&](int q) { return __ldcg(reinterpret_cast<const float2*>(p0 + static_cast<int64_t>(q) * kPart + kTile * D) + r); };
-  float M = -INFINITY, L = 0.0f;
-#pragma unroll 8
-  for (int q = 0; q < sk.parts; ++q) M = fmaxf(M, stats(q).x);
-  const float Ms = M == -INFINITY ? 0.0f : M;
-#pragma unroll 8
-  for (int q = 0; q < sk.parts; ++q) {
-    const float2 ml = stats(q);
-    L = fmaf(ml.y, exp2_approx(ml.x - Ms), L);
-  }
-  const float Li = L > 0.0f ? 1.0f / L : 0.0f;
   const int f4 = blockIdx.z * (kJoinThreads / 32) + warp;   // of 4 features each
+  float M = -INFINITY, L = 0.0f;
   float4 v = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-#pragma unroll 8
-  for (int q = 0; q < sk.parts; ++q) {
-    const float w = exp2_approx(stats(q).x - Ms) * Li;
-    const float4 x = __ldcg(reinterpret_cast<const float4*>(p0 + static_cast<int64_t>(q) * kPart) + f4 * kTile + r);
-    v.x = fmaf(x.x, w, v.x), v.y = fmaf(x.y, w, v.y), v.z = fmaf(x.z, w, v.z), v.w = fmaf(x.w, w, v.w);
+  constexpr int kBatch = 8;   // parts whose loads are in flight together
+  for (int q0 = 0; q0 < sk.parts; q0 += kBatch) {
+    float2 ml[kBatch];   // reference, sum of weights
+    float4 x[kBatch];
+#pragma unroll
+    for (int j = 0; j < kBatch; ++j) {
+      const float* pq = p0 + static_cast<int64_t>(min(q0 + j, sk.parts - 1)) * kPart;
+      ml[j] = __ldcg(reinterpret_cast<const float2*>(pq + kTile * D) + r);
+      x[j] = __ldcg(reinterpret_cast<const float4*>(pq) + f4 * kTile + r);
+    }
+    float top = M;
+#pragma unroll
+    for (int j = 0; j < kBatch; ++j) top = fmaxf(top, ml[j].x);
+    const float ref = top == -INFINITY ? 0.0f : top, f = exp2_approx(M - ref);
+    M = top;
+    L *= f, v.x *= f, v.y *= f, v.z *= f, v.w *= f;
+#pragma unroll
+    for (int j = 0; j < kBatch; ++j) {
+      const float w = q0 + j < sk.parts ? exp2_approx(ml[j].x - ref) : 0.0f;
+      L = fmaf(ml[j].y, w, L);
+      v.x = fmaf(x[j].x, w, v.x), v.y = fmaf(x[j].y, w, v.y), v.z = fmaf(x[j].z, w, v.z), v.w = fmaf(x[j].w, w, v.w);
+    }
   }
+  const float inv = L > 0.0f ? 1.0f / L : 0.0f;
+  v.x *= inv, v.y *= inv, v.z *= inv, v.w *= inv;
   *reinterpret_cast<uint2*>(a.out + (row * a.heads + hk * G + r % G) * D + 4 * f4) = make_uint2(pack_f16(v.x, v.y), pack_f16(v.z, v.w));
 }
 
@@ -344,7 +353,10 @@ attn_tile_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constan
   auto by_group = [&](int i) { return static_cast<int>(static_cast<uint32_t>(i) * ta.group_mul >> 16); };
   const int tpt = by_group(kTile);    // tokens of one accumulator
   const int qt = 2 * tpt;             // tokens of one CTA
-  const int slot = blockIdx.x / a.c.heads, hk = blockIdx.x - slot * a.c.heads;
+  int unit = blockIdx.x, part = 0;
+  const int most_parts = unit < ta.whole ? 1 : ta.parts;
+  if (unit >= ta.whole) part = (unit - ta.whole) / ta.split, unit -= part * ta.split;
+  const int slot = unit / a.c.heads, hk = unit - slot * a.c.heads;
 
   const uint32_t bar0 = smem_u32(bars);
   const uint32_t bar_full = bar0, bar_free = bar0 + 8 * C::kStages;
@@ -377,10 +389,9 @@ attn_tile_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constan
   const int tok0 = s_assign[1] * qt;
   const AttnRange rg = attn_range(a, s_assign[3], s_assign[4]);
   const int64_t row0 = s_assign[2];
-  const SlotKeys sk = slot_keys(a, rg, tok0, qt, static_cast<int>(gridDim.y));
+  const SlotKeys sk = slot_keys(a, rg, tok0, qt, most_parts);
   const int toks = sk.toks, p_base = sk.p_base, parts = sk.parts;
   const bool two = toks > tpt;
-  const int part = blockIdx.y;
   if (b < 0 || part >= parts) {
     if (warp == kIssuer) tmem_dealloc(tmem, 512);
     return;
@@ -839,9 +850,8 @@ attn_tile_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constan
     }
     f0 *= vref;
     const bool writes = two || acc == 0;
-    const int64_t unit = blockIdx.x;
     constexpr int kPart = kPartFloats<D>;
-    float* pu = a.partials + unit * gridDim.y * kPart;
+    float* pu = a.partials + static_cast<int64_t>(unit - ta.whole) * most_parts * kPart;   // of a unit in parts
     const float inv = l > 0.0f ? 1.0f / l : 0.0f;
     if (!writes) release_tmem();
     if (writes) {
@@ -928,46 +938,70 @@ int launch(TileArgs& t, const TilePlan& plan, cudaStream_t stream) {
     if (const int rc = make_tmap_2d(&mk, c.k, rows, D, t.box, 64, 2, 128); rc != PQ_OK) return rc;
     if (const int rc = make_tmap_2d(&mv, c.v, rows, D, t.box, 64, 2, 128); rc != PQ_OK) return rc;
   }
-  const dim3 grid(static_cast<unsigned>(plan.units), static_cast<unsigned>(plan.parts));
-  if (const int rc = launch_dependent(kern, grid, dim3(C::kThreads), C::kSmem, stream, mk, mv, t); rc != PQ_OK || plan.parts == 1) return rc;
-  return launch_dependent(attn_join_kernel<D>, dim3(grid.x, 8, D / 32), dim3(kJoinThreads), 0, stream, t.a, plan.parts);
+  const dim3 grid(static_cast<unsigned>(plan.whole + plan.split * plan.parts));
+  if (const int rc = launch_dependent(kern, grid, dim3(C::kThreads), C::kSmem, stream, mk, mv, t); rc != PQ_OK || plan.split == 0) return rc;
+  return launch_dependent(attn_join_kernel<D>, dim3(static_cast<unsigned>(plan.split), 8, D / 32), dim3(kJoinThreads), 0, stream, t.a,
+                          t.whole, plan.parts);
 }
 
 }  // namespace
 
-// Fewer units than SMs: the keys of each are cut into parts, of 512 keys at least.
-TilePlan plan_attn_tile(int64_t requests, int64_t tokens, int64_t max_q, int64_t max_kv, int group, int kv_heads, int dim,
-                        int sms, size_t room) {
+// Units run on the SMs in waves.  Those of the last, incomplete wave (of the only one, where there are fewer units than
+// SMs) have their keys cut into as many parts, of 384 keys or more, as the sum below is least for, counted in steps of 128
+// keys: every CTA takes 6 steps more than its keys do, every part 0.04 to be joined, the joining kernel 4.
+// (32 heads over 8 of 128, FP16: 1220 tokens over 12176, 160 units, 240 us, 329 with all of them whole; 64 tokens over
+// 8000, 8 units in 17 parts, 25 us, 300 tokens of two requests over 3000, 80 units in 3, 50, 58 whole.)
+TilePlan plan_attn_tile(int64_t requests, int64_t tokens, int64_t max_q, int64_t max_kv, int window, int group, int kv_heads,
+                        int dim, int sms, size_t room) {
   TilePlan p;
+  if (max_kv > 0x7fffffff) max_kv = 0x7fffffff;
   const int64_t qt = 2 * (kTile / group);
-  const int64_t by_rows = tokens / qt + requests, by_request = requests * ((max_q + qt - 1) / qt);
-  p.units = (by_rows < by_request ? by_rows : by_request) * kv_heads;
-  int64_t parts = 1, keys = (max_kv + kTile - 1) / kTile * kTile;
-  if (p.units < sms) {
-    parts = sms / p.units;
-    keys = (max_kv + parts - 1) / parts;
-    keys = keys < 512 ? 512 : (keys + kTile - 1) / kTile * kTile;
-    parts = (max_kv + kTile + keys - 1) / keys;   // the first part begins at a multiple of 128 before the window
-    if (parts > 65535) parts = 65535;
+  const int64_t few = kAttnRows / group + 1;   // tokens that make a request this kernel's, if there are several
+  const int64_t served = requests == 1 || tokens / few > requests ? requests : tokens / few;
+  const int64_t by_rows = tokens / qt + served, by_request = requests * ((max_q + qt - 1) / qt);
+  const int64_t units = (by_rows < by_request ? by_rows : by_request) * kv_heads;
+  auto steps_of = [&](int64_t keys) {
+    if (window > 0 && keys > window + qt) keys = window + qt;
+    return (keys + kTile - 1) / kTile;
+  };
+  const int64_t all = steps_of(max_kv), waves = units / sms, rest = units - waves * sms;
+  p.whole = units;
+  p.part_keys = 1 << 30;
+  if (rest > 0) {
+    // a single request's last units are its first tokens and see fewest keys
+    int64_t keys = max_kv;
+    if (waves > 0 && requests == 1) keys -= max_q - (max_q < (rest / kv_heads + 1) * qt ? max_q : (rest / kv_heads + 1) * qt);
+    const int64_t steps = steps_of(keys);
+    int64_t best = 1;
+    double least = static_cast<double>(waves * (all + 6) + steps + 6) * 0.95;   // to be worth the other kernel
+    // (Units of one query tile are bound by memory: once all SMs have had work, cutting the last of them gains nothing.)
+    for (int64_t k = 2; k <= (waves > 0 && 2 * max_q <= qt ? 1 : steps / 3); ++k) {
+      const double sum = static_cast<double>(waves * (all + 6)) + static_cast<double>((rest * k + sms - 1) / sms) * (static_cast<double>(steps) / k + 6) +
+                         4 + 0.04 * static_cast<double>(rest * k);
+      if (sum < least) least = sum, best = k;
+      if (rest * k > 8 * sms) break;
+    }
+    const size_t one = static_cast<size_t>(2 * kTile) * (dim + 2) * 4;
+    const int64_t fit = static_cast<int64_t>(room / (static_cast<size_t>(rest) * one));
+    if (best > fit) best = fit;
+    if (best > 1) {
+      p.whole = units - rest;
+      p.split = rest;
+      p.part_keys = static_cast<int>((steps + best - 1) / best * kTile);
+      p.parts = static_cast<int>(((steps + 1) * kTile + p.part_keys - 1) / p.part_keys);   // a window may begin inside a step
+      if (p.parts > fit) p.parts = static_cast<int>(fit);   // the last part takes the keys that are left
+      p.partial_bytes = static_cast<size_t>(rest) * p.parts * one;
+    }
   }
-  const size_t one = static_cast<size_t>(2 * kTile) * (dim + 2) * 4;
-  if (parts > 1 && static_cast<size_t>(p.units) * parts * one > room) {
-    const int64_t fit = static_cast<int64_t>(room / (static_cast<size_t>(p.units) * one));
-    parts = fit < 2 ? 1 : fit;
-    keys = ((max_kv + parts - 1) / parts + kTile - 1) / kTile * kTile;
-  }
-  if (keys > (1 << 30)) keys = 1 << 30;
-  p.parts = static_cast<int>(parts);
-  p.part_keys = static_cast<int>(keys < kTile ? kTile : keys);
-  p.partial_bytes = parts > 1 ? static_cast<size_t>(p.units) * parts * one : 0;
   return p;
 }
 
 int launch_attn_tile(const AttnArgs& a, const TilePlan& plan, cudaStream_t stream) {
-  if (plan.units < 1) return PQ_OK;
-  if (plan.units > 0x7fffffff) return PQ_ERR_SHAPE;
+  if (plan.whole + plan.split < 1) return PQ_OK;
+  if (plan.whole + plan.split * plan.parts > 0x7fffffff) return PQ_ERR_SHAPE;
   const uint32_t group = static_cast<uint32_t>(a.heads / a.c.heads);
-  TileArgs t{a, device_status_ptr(), wait_limit(), 128, (65535u + group) / group, 0xffffffffu, 0u};
+  TileArgs t{a, device_status_ptr(), wait_limit(), 128, (65535u + group) / group,
+             static_cast<int>(plan.whole), static_cast<int>(plan.split), plan.parts, 0xffffffffu, 0u};
   if (t.status == nullptr) return PQ_ERR_CUDA;
   while (a.c.page % t.box != 0) t.box /= 2;   // the page is a multiple of 16
   t.a.part_keys = plan.part_keys;

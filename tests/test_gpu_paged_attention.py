@@ -187,3 +187,27 @@ def test_offsets_beyond_32_bits():
     out = pq.pq_paged_attention(_t(d["q"]), pq.PagedKV(k, v), _t(table), _t(d["q_start"]), _t(d["kv_len"]), 130, 130)
     y, bound = ref.attention(d)
     assert (np.abs(out.cpu().numpy() - y) <= bound).all()
+
+
+@pytest.mark.parametrize("cache", ["f16", "int8"])
+@pytest.mark.parametrize("heads,kv_heads,dim,new,total,window", [
+    (32, 8, 64, [1220], [2720], 0),                  # 160 units, the last 12 in parts
+    (16, 8, 64, [1250, 3, 1190], [1700, 900, 2500], 0),
+    (32, 8, 64, [1220], [2720], 1300)])
+def test_units_of_the_last_wave_in_parts(heads, kv_heads, dim, new, total, window, cache):
+    d = ref.attention_inputs(heads, kv_heads, dim, 32, cache, new, total, window=window, seed=sum(total))
+    _check(d)
+    _check(d, workspace=False)                       # every unit whole
+
+
+def test_a_workspace_too_small_for_all_parts_still_serves():
+    d = ref.attention_inputs(8, 2, 128, 16, "f16", [70], [6000], seed=77)
+    y, bound = ref.attention(d)
+    cache = pq.PagedKV(_t(d["k"]), _t(d["v"]))
+    q, table, qs, kl = _t(d["q"]), _t(d["table"]), _t(d["q_start"]), _t(d["kv_len"])
+    full = pq.pq_attention_workspace(q, cache, 1, 70, 6000)
+    for share in (2, 5, 50):
+        ws = full[: 65536 + (full.numel() - 65536) // share]
+        out = pq.pq_paged_attention(q, cache, table, qs, kl, 70, 6000, workspace=ws)
+        assert (np.abs(out.cpu().numpy() - y) <= bound).all()
+        assert pq.pq_device_status() == 0
