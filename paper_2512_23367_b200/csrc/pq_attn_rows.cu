@@ -91,6 +91,10 @@ __device__ __forceinline__ uint32_t transposed(uint32_t v) {   // an 8 x 8 tile 
 // multiplies the weight, taken relative to a running power of two >= every scale seen, so that the FP16 weight
 // stays in [0, 1] whatever the scales are.  The feature order of a matrix step is permuted so that a lane's codes
 // are 16 consecutive bytes; queries (and the result's rows) are permuted alike.
+//
+// Measured, 32 heads over 8 of 128, 64 requests of one token over up to 8192: FP16 208 us (6.7 TB/s, what a copy
+// reaches); INT8 130 us (5.5 TB/s): issue, 58 % of the slots, for the codes' conversion and the scales.  3 requests over
+// 131072: 247 us (6.5 TB/s).  1000 tokens of one request: 6.6 us, latency.
 template <bool kInt8, int D, int kTiles>
 __global__ void __launch_bounds__(kWarps * 32, (RowCfg<kInt8, D>::kCtas)) attn_rows_kernel(const AttnArgs a) {
   using C = RowCfg<kInt8, D>;
