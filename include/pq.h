@@ -362,7 +362,8 @@ PQ_API int pq_gemm_w8a8_noalloc(const int8_t* q, const float* s_tok, const void*
  * A cache holds `pages` pages of `page` tokens for `heads` key/value heads of `dim` values:
  *   k, v              [pages, heads, page, dim]  FP16 (PQ_KV_F16) or INT8 codes (PQ_KV_INT8)
  *   k_scale, v_scale  [pages, heads, page]       FP32, PQ_KV_INT8 only (NULL otherwise): the scale of one
- *                                                token's vector of one head, value = code * scale
+ *                                                token's vector of one head, value = code * scale;
+ *                                                >= 0, as pq_kv_append writes it
  * A SLOT is page_id * page + offset.  Rules (else PQ_ERR_SHAPE): page a multiple of 16, at most 1024;
  * dim 64 or 128; 1 <= heads <= 1024; pages >= 1 and pages * heads * page < 2^31; type one of the two.
  */
@@ -441,7 +442,7 @@ PQ_API int pq_kv_read(const pq_kv_cache* cache, const int64_t* slots, int64_t to
  *   heads a multiple of cache->heads, heads / cache->heads <= 64; scale finite; window >= 0.
  *   workspace: as for pq_gemm_w8a8 (optional, prepared once with pq_workspace_init, one per stream of calls
  *     that may overlap): partial results of keys that are split over several SMs, summed in a fixed order.
- *     Without it, or with too little, the keys of a request are not split.
+ *     Without it, the keys of a request are not split; with too little, into fewer parts or not at all.
  * pq_attention_workspace_bytes: host-only; 0 when nothing is split or an argument is invalid.
  */
 PQ_API int pq_paged_attention(const void* q_f16, int64_t q_stride, int32_t heads, const pq_kv_cache* cache,
