@@ -339,7 +339,7 @@ __global__ void __launch_bounds__(kJoinThreads) attn_join_kernel(const AttnArgs 
 // key's scale (times the softmax scale) multiplies the score.  The value's scale multiplies the weight before it is
 // rounded, relative to the power of two above the largest scale of its 32 keys, and the quotient of that unit and
 // the running unit of O goes into the exponent, exactly.
-// Six requests, chunks of up to 700 over up to 5000: 217 us (0.65 PFLOP/s), FP16 153; issue, 71 % of the slots: the
+// Six requests, chunks of up to 700 over up to 5000: 210 us (0.67 PFLOP/s), FP16 153; issue, 71 % of the slots: the
 // conversion is done again for every 256 rows, and each score takes two products more.
 template <bool kInt8, int D>
 __global__ void __launch_bounds__((TileCfg<kInt8, D>::kThreads), 1)
