@@ -431,6 +431,9 @@ PQ_API int pq_kv_read(const pq_kv_cache* cache, const int64_t* slots, int64_t to
  * for query head h over the key/value head h / (heads / cache->heads).  Scores, maxima and sums are FP32;
  * the weights are rounded to FP16 for their product with the values (they lie in [0, 256]), and the
  * product is summed in FP32.  A row that sees no key (kv_len shorter than the chunk, window or not) gives 0.
+ * A key that a row does not see does not reach it, whatever it holds, and nothing beyond kv_len or before
+ * the window of a chunk's first row is used.  The VALUES in between are taken as finite: one that is infinite
+ * or NaN also reaches rows of its request that do not see it (0 times it).
  *   q: FP16, row t at q + t * q_stride elements (a multiple of 8, >= heads * dim), heads * dim values
  *   block_table i32 [requests, width]; q_start i32 [requests + 1]; kv_len i32 [requests], tokens in the
  *     cache with the chunk's own (kv_total of pq_block_tables).  A page id outside the cache reads as

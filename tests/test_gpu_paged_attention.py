@@ -211,3 +211,21 @@ def test_a_workspace_too_small_for_all_parts_still_serves():
         out = pq.pq_paged_attention(q, cache, table, qs, kl, 70, 6000, workspace=ws)
         assert (np.abs(out.cpu().numpy() - y) <= bound).all()
         assert pq.pq_device_status() == 0
+
+
+@pytest.mark.parametrize("cache", ["f16", "int8"])
+@pytest.mark.parametrize("new,total", [([5, 1], [90, 33]), ([40, 3], [40, 17]), ([300], [400])])
+def test_a_key_that_is_not_a_number_reaches_only_the_rows_that_see_it(new, total, cache):
+    d = ref.attention_inputs(8, 2, 128, 16, cache, new, total, seed=sum(total) + 1)
+    y, bound = ref.attention(d)
+    at = total[0] - 1                                # the first request's newest key
+    page, off = d["table"][0][at // 16], at % 16
+    if cache == "f16":
+        d["k"][page, :, off] = np.nan
+    else:
+        d["ks"][page, :, off] = np.nan
+    got = _run(d).cpu().numpy().astype(np.float64)
+    hit = new[0] - 1
+    assert np.isnan(got[hit]).all()
+    rest = np.arange(sum(new)) != hit
+    assert (np.abs(got - y)[rest] <= bound[rest]).all()
