@@ -1,6 +1,7 @@
 // Attention of a step's tokens over the paged key/value cache.  See include/pq.h for the contract.
 #include <cuda_fp16.h>
 
+#include <algorithm>
 #include <cmath>
 
 #include "pq_attention.h"
@@ -27,6 +28,8 @@ int pq_paged_attention(const void* q_f16, int64_t q_stride, int32_t heads, const
   // Up to 16 rows per request and key/value head go to the row kernel, more to the tile kernel; which of them a request
   // takes is decided on the device.  A single request of many rows needs no row kernel.
   const int group = heads / cache->heads;
+  // No request has keys beyond its table: a larger bound would only make the parts longer than the keys.
+  max_kv = bounded_keys(std::min(max_kv, width * cache->page));
   const bool wide = max_q * group > kAttnRows, narrow = !wide || requests > 1;
   AttnArgs a{static_cast<const __half*>(q_f16), q_stride, *cache, block_table, width, q_start, kv_len,
              static_cast<__half*>(out_f16), tokens, static_cast<int>(requests), heads, window,
@@ -53,6 +56,7 @@ size_t pq_attention_workspace_bytes(int64_t requests, int64_t tokens, int64_t ma
       heads < kv_heads || heads % kv_heads != 0 || (dim != 64 && dim != 128) || sms < 1) {
     return 0;
   }
+  max_kv = bounded_keys(max_kv);
   size_t bytes = 0;   // for either type of cache, window or not
   for (int int8 = 0; int8 < 2; ++int8) {
     const AttnPlan plan = plan_attn_rows(requests, max_q, max_kv, 0, kv_heads, dim, int8 != 0, sms, ~size_t(0));

@@ -30,6 +30,11 @@ struct AttnArgs {
 // Requests with more rows go to the tile kernel.
 constexpr int kAttnRows = 16;
 
+// Lengths are 32 bits wide, and the schedules round up to parts of 128 keys in 32 bits: 2^30 keys are as good as more
+// (the last part of a unit takes the keys that are left).
+constexpr int64_t kMostKeys = int64_t(1) << 30;
+inline int64_t bounded_keys(int64_t max_kv) { return max_kv < kMostKeys ? max_kv : kMostKeys; }
+
 // Schedule of a call, from sizes that the host knows: how many parts a unit's keys may be cut into.
 struct AttnPlan {
   int64_t units = 0;      // units of the row kernel: requests x key/value heads

@@ -995,7 +995,6 @@ int launch(TileArgs& t, const TilePlan& plan, cudaStream_t stream) {
 TilePlan plan_attn_tile(int64_t requests, int64_t tokens, int64_t max_q, int64_t max_kv, int window, int group, int kv_heads,
                         int dim, int sms, size_t room) {
   TilePlan p;
-  if (max_kv > 0x7fffffff) max_kv = 0x7fffffff;
   const int64_t qt = 2 * (kTile / group);
   const int64_t few = kAttnRows / group + 1;   // tokens that make a request this kernel's, if there are several
   const int64_t served = requests == 1 || tokens / few > requests ? requests : tokens / few;
