@@ -28,7 +28,8 @@ int pq_paged_attention(const void* q_f16, int64_t q_stride, int32_t heads, const
   // Up to 16 rows per request and key/value head go to the row kernel, more to the tile kernel; which of them a request
   // takes is decided on the device.  A single request of many rows needs no row kernel.
   const int group = heads / cache->heads;
-  // No request has keys beyond its table: a larger bound would only make the parts longer than the keys.
+  // No request has more rows than the step, nor keys beyond its table: larger bounds say no more.
+  max_q = std::min(max_q, tokens);
   max_kv = bounded_keys(std::min(max_kv, width * cache->page));
   const bool wide = max_q * group > kAttnRows, narrow = !wide || requests > 1;
   AttnArgs a{static_cast<const __half*>(q_f16), q_stride, *cache, block_table, width, q_start, kv_len,
@@ -52,10 +53,11 @@ int pq_paged_attention(const void* q_f16, int64_t q_stride, int32_t heads, const
 
 size_t pq_attention_workspace_bytes(int64_t requests, int64_t tokens, int64_t max_q, int64_t max_kv, int32_t heads,
                                     int32_t kv_heads, int32_t dim, int32_t sms) {
-  if (requests < 1 || requests > PQ_MAX_REQUESTS || tokens < 1 || max_q < 1 || max_kv < 1 || kv_heads < 1 ||
+  if (requests < 1 || requests > PQ_MAX_REQUESTS || tokens < 1 || tokens > 0x7fffffff || max_q < 1 || max_kv < 1 || kv_heads < 1 ||
       heads < kv_heads || heads % kv_heads != 0 || (dim != 64 && dim != 128) || sms < 1) {
     return 0;
   }
+  max_q = std::min(max_q, tokens);
   max_kv = bounded_keys(max_kv);
   size_t bytes = 0;   // for either type of cache, window or not
   for (int int8 = 0; int8 < 2; ++int8) {

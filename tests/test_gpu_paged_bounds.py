@@ -2,11 +2,31 @@
 size, workspaces cut short."""
 import numpy as np
 import pytest
+import torch
 
 import paged_reference as ref
-from test_gpu_paged_attention import _check, _run
+import paper_2512_23367_b200 as pq
+from test_gpu_paged_attention import DEV, _check, _run, _t
 
 pytestmark = pytest.mark.gpu
+
+
+def _serve(d, max_q=None, max_kv=None, workspace=None, window=None):
+    """One call over the inputs `d`; the workspace is the caller's."""
+    out = torch.full(d["q"].shape, float("nan"), dtype=torch.float16, device=DEV)
+    pq.pq_paged_attention(_t(d["q"]), pq.PagedKV(_t(d["k"]), _t(d["v"]), _t(d["ks"]), _t(d["vs"])), _t(d["table"]),
+                          _t(d["q_start"]), _t(d["kv_len"]), int(np.diff(d["q_start"]).max()) if max_q is None else max_q,
+                          int(d["kv_len"].max()) if max_kv is None else max_kv,
+                          window=d["window"] if window is None else window, out=out, workspace=workspace)
+    assert pq.pq_device_status() == 0
+    return out.cpu().numpy().astype(np.float64)
+
+
+def _workspace(d, max_q=None, max_kv=None, **more):
+    kv_heads, _, dim = d["k"].shape[1:]
+    n = pq.pq_attention_workspace_bytes(len(d["kv_len"]), d["q"].shape[0], int(np.diff(d["q_start"]).max()) if max_q is None else max_q,
+                                        int(d["kv_len"].max()) if max_kv is None else max_kv, d["q"].shape[1], kv_heads, dim, **more)
+    return pq.pq_workspace_init(torch.empty((n,), dtype=torch.uint8, device=DEV)) if n else None
 
 
 @pytest.mark.parametrize("cache", ["f16", "int8"])
@@ -16,3 +36,12 @@ def test_a_bound_of_the_cached_tokens_may_be_anything(new, total, max_kv, cache)
     d = ref.attention_inputs(8, 2, 128, 16, cache, new, total, seed=sum(total))
     _check(d, workspace=False, max_kv=max_kv)
     assert np.array_equal(_run(d, workspace=False, max_kv=max_kv).cpu().numpy(), _run(d, workspace=False).cpu().numpy())
+
+
+@pytest.mark.parametrize("max_q", [2**31, 1 << 40, 2**61, 2**62, 2**63 - 1])
+@pytest.mark.parametrize("new,total", [([40, 2], [300, 500]), ([70], [900]), ([1, 3], [50, 60])])
+def test_a_bound_of_the_rows_may_be_anything(new, total, max_q):
+    d = ref.attention_inputs(8, 2, 128, 16, "f16", new, total, seed=sum(total))
+    y, bound = ref.attention(d)
+    for workspace in (_workspace(d, max_q=max_q), None):
+        assert (np.abs(_serve(d, max_q=max_q, workspace=workspace) - y) <= bound).all()

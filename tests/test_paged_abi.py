@@ -165,3 +165,13 @@ def test_the_plain_block_tables_by_hand():
         np.array([15, 0]), np.array([2, 1]), np.array([[9, -1], [-1, -1]], np.int32), np.array([5, 6, 7]), 1, 16, 4)
     assert table.tolist() == [[9, 6], [7, -1]] and q_start.tolist() == [0, 2, 3] and total.tolist() == [17, 1]
     assert slots.tolist() == [9 * 16 + 15, 6 * 16, 7 * 16, -1] and pos.tolist() == [15, 16, 0, -1] and head == 3
+
+
+def test_workspace_query_takes_bounds_of_any_size():
+    size = pq.pq_attention_workspace_bytes
+    assert size(1, 300, 300, 8192, 32, 8, 128) > 65536
+    for max_q in (301, 2**31, 2**61, 2**62, 2**63 - 1):         # no request has more rows than the step
+        assert size(1, 300, max_q, 8192, 32, 8, 128) == size(1, 300, 300, 8192, 32, 8, 128)
+    for max_kv in (2**31 - 1, 2**40, 2**63 - 1):
+        assert size(1, 300, 300, max_kv, 32, 8, 128) == size(1, 300, 300, 2**30, 32, 8, 128)
+    assert size(1, 2**31, 300, 8192, 32, 8, 128) == 0
