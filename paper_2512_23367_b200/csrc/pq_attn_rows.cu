@@ -229,30 +229,6 @@ __global__ void __launch_bounds__(kWarps * 32, (RowCfg<kInt8, D>::kCtas)) attn_r
   const int all_from = a.window > 0 ? rg.L - a.window : 0;      // keys that every row sees: [all_from, all_to)
   const int all_to = min(rg.L - rg.n + 1, rg.hi);
 
-  // INT8: the keys' codes enter the product as 1024 + (code + 128), their FP16 pattern without the subtraction, and the
-  // accumulators of a row begin at -1152 sum q instead of 0.  (Their FP32 roundings are then those of values near
-  // 1152 |q|: about 1e-2 of a code, 1e-5 of a score.  The values' codes are not taken so: their sum runs over all keys.)
-  float start[kTiles][2];
-#pragma unroll
-  for (int q = 0; q < kTiles; ++q) {
-    float x = 0.0f;
-    if constexpr (kInt8) {
-#pragma unroll
-      for (int s = 0; s < KS; ++s) {
-#pragma unroll
-        for (int i = 0; i < 2; ++i) {
-          const __half2 h = *reinterpret_cast<const __half2*>(&qb[q][s][i]);
-          x += __low2float(h) + __high2float(h);
-        }
-      }
-      x += __shfl_xor_sync(0xffffffffu, x, 1);   // a lane holds a quarter of row 8 q + g's features
-      x += __shfl_xor_sync(0xffffffffu, x, 2);
-      x *= -1152.0f;
-    }
-    start[q][0] = __shfl_sync(0xffffffffu, x, 8 * c);
-    start[q][1] = __shfl_sync(0xffffffffu, x, 8 * c + 4);
-  }
-
   float o[kTiles][MT][4];
 #pragma unroll
   for (int q = 0; q < kTiles; ++q) {
@@ -276,7 +252,7 @@ __global__ void __launch_bounds__(kWarps * 32, (RowCfg<kInt8, D>::kCtas)) attn_r
 #pragma unroll
     for (int blk = 0; blk < C::kBlocks; ++blk) {
 #pragma unroll
-      for (int q = 0; q < kTiles; ++q) sc[blk][q][0] = sc[blk][q][2] = start[q][0], sc[blk][q][1] = sc[blk][q][3] = start[q][1];
+      for (int q = 0; q < kTiles; ++q) sc[blk][q][0] = sc[blk][q][1] = sc[blk][q][2] = sc[blk][q][3] = 0.0f;
       if constexpr (!kInt8) {
         const int R = blk * 16 + (lane & 15);
 #pragma unroll
@@ -297,8 +273,7 @@ __global__ void __launch_bounds__(kWarps * 32, (RowCfg<kInt8, D>::kCtas)) attn_r
           const uint32_t u1[4] = {w1.x ^ 0x80808080u, w1.y ^ 0x80808080u, w1.z ^ 0x80808080u, w1.w ^ 0x80808080u};
 #pragma unroll
           for (int i = 0; i < 4; ++i) {
-            const uint32_t r[4] = {__byte_perm(u0[i], 0x64646464u, 0x4140), __byte_perm(u1[i], 0x64646464u, 0x4140),
-                                   __byte_perm(u0[i], 0x64646464u, 0x4342), __byte_perm(u1[i], 0x64646464u, 0x4342)};
+            const uint32_t r[4] = {codes_f16(u0[i], 0x4140), codes_f16(u1[i], 0x4140), codes_f16(u0[i], 0x4342), codes_f16(u1[i], 0x4342)};
 #pragma unroll
             for (int q = 0; q < kTiles; ++q) mma16816(sc[blk][q], r, qb[q][q4 * 4 + i][0], qb[q][q4 * 4 + i][1]);
           }
