@@ -75,6 +75,10 @@ __device__ __forceinline__ uint32_t codes_f16(uint32_t u, uint32_t sel) {
   const __half2 r = __hsub2(*reinterpret_cast<const __half2*>(&h), __half2(__ushort_as_half(0x6480), __ushort_as_half(0x6480)));
   return *reinterpret_cast<const uint32_t*>(&r);
 }
+__device__ __forceinline__ float power_of_two(int e) { return __uint_as_float(static_cast<uint32_t>(127 + e) << 23); }   // |e| <= 126
+// The exponent of an INT8 value scale, within [-40, 60]: scales of FP16 values lie in [2^-31, 2^10), and with a range of
+// 100 no weight that counts leaves FP32's on the way to its sum, nor does a sum of them.
+__device__ __forceinline__ int scale_exponent(float v) { return min(max(static_cast<int>(__float_as_uint(v) << 1 >> 24) - 127, -40), 60); }
 // The smallest power of two >= v (at least 2^-126): the unit that a run of INT8 value scales is taken in.
 __device__ __forceinline__ float scale_unit(float v) {
   const uint32_t u = (__float_as_uint(fminf(fmaxf(v, 0.0f), 1e37f)) + 0x7fffffu) & 0x7f800000u;

@@ -87,9 +87,11 @@ __device__ __forceinline__ uint32_t transposed(uint32_t v) {   // an 8 x 8 tile 
 // keys; the four are merged through shared memory, and parts of one unit through the workspace by the CTA that
 // arrives last, in the order of the parts.
 //
-// INT8: the codes go to the tensor cores as FP16 (exact).  The key's scale multiplies the score; the value's scale
-// multiplies the weight, taken relative to a running power of two >= every scale seen, so that the FP16 weight
-// stays in [0, 1] whatever the scales are.  The feature order of a matrix step is permuted so that a lane's codes
+// INT8: the codes go to the tensor cores as FP16 (exact).  The key's scale multiplies the score.  The value's scale is
+// split into 2^e and a rest in [1, 2); e is added to the score in powers of two, x, and the running maximum is that of
+// x + e over the keys that the row sees: the FP16 weight, 2^(x + e - max + 14) times the rest, then stays below 2^15 and
+// keeps its bits down to 2^-29 of the row's largest product of weight and scale, whatever the scales are.  The sum of the
+// weights, FP32, takes 2^(x + e - max + 14) times 2^-e.  The feature order of a matrix step is permuted so that a lane's codes
 // are 16 consecutive bytes; queries (and the result's rows) are permuted alike.
 //
 // Measured, 32 heads over 8 of 128, 64 requests of one token over up to 8192: FP16 208 us (6.7 TB/s, what a copy
@@ -100,6 +102,7 @@ __global__ void __launch_bounds__(kWarps * 32, (RowCfg<kInt8, D>::kCtas)) attn_r
   using C = RowCfg<kInt8, D>;
   constexpr int KS = D / 16;   // matrix steps over the features
   constexpr int MT = D / 16;   // 16-wide feature tiles of the result
+  constexpr float kTop = kInt8 ? 14.0f : 0.0f;   // the largest weight is 2^kTop (INT8: times the rest of its scale, below 2)
   extern __shared__ __align__(128) uint8_t smem[];
   __shared__ bool s_last;
 
@@ -238,7 +241,6 @@ __global__ void __launch_bounds__(kWarps * 32, (RowCfg<kInt8, D>::kCtas)) attn_r
   float m[kTiles][2], l[kTiles][2];
 #pragma unroll
   for (int q = 0; q < kTiles; ++q) m[q][0] = m[q][1] = -INFINITY, l[q][0] = l[q][1] = 0.0f;
-  float vref = 0.0f;   // INT8: o is in units of vref
 
   for (int s = 0; s < my_steps; ++s) {
     cp_wait<C::kStages - 2>();
@@ -283,7 +285,7 @@ __global__ void __launch_bounds__(kWarps * 32, (RowCfg<kInt8, D>::kCtas)) attn_r
 
     // Scores in powers of two, masked; the step's maxima.
     const bool all = key0 >= all_from && key0 + C::kKeys <= all_to;
-    float vs[C::kBlocks][2], top[kTiles][2], vtop = 0.0f;
+    float vs[C::kBlocks][2], vinv[C::kBlocks][2], top[kTiles][2];
 #pragma unroll
     for (int q = 0; q < kTiles; ++q) top[q][0] = top[q][1] = -INFINITY;
 #pragma unroll
@@ -291,11 +293,14 @@ __global__ void __launch_bounds__(kWarps * 32, (RowCfg<kInt8, D>::kCtas)) attn_r
 #pragma unroll
       for (int h = 0; h < 2; ++h) {   // keys g and g + 8
         const int j = blk * 16 + 8 * h + g;
-        float ks = a.scale_log2;
+        float ks = a.scale_log2, vlog = 0.0f;
         if constexpr (kInt8) {
           ks *= lds_f1(st + kStageBytes + j * 4);
-          vs[blk][h] = lds_f1(st + kStageBytes + (C::kKeys + j) * 4);
-          vtop = fmaxf(vtop, vs[blk][h]);
+          const float v = lds_f1(st + kStageBytes + (C::kKeys + j) * 4);
+          const int e = scale_exponent(v);
+          vlog = static_cast<float>(e);
+          vinv[blk][h] = power_of_two(-e);
+          vs[blk][h] = v * vinv[blk][h];
         }
         const int key = key0 + j;
 #pragma unroll
@@ -303,7 +308,7 @@ __global__ void __launch_bounds__(kWarps * 32, (RowCfg<kInt8, D>::kCtas)) attn_r
 #pragma unroll
           for (int i = 0; i < 2; ++i) {
             float& x = sc[blk][q][2 * h + i];
-            x *= ks;
+            x = kInt8 ? fmaf(x, ks, vlog) : x * ks;
             if (!all && (key > p_row[q][i] || key <= w_row[q][i])) x = -INFINITY;
             top[q][i] = fmaxf(top[q][i], x);
           }
@@ -318,18 +323,10 @@ __global__ void __launch_bounds__(kWarps * 32, (RowCfg<kInt8, D>::kCtas)) attn_r
         top[q][0] = fmaxf(top[q][0], __shfl_xor_sync(0xffffffffu, top[q][0], d));
         top[q][1] = fmaxf(top[q][1], __shfl_xor_sync(0xffffffffu, top[q][1], d));
       }
-      if constexpr (kInt8) vtop = fmaxf(vtop, __shfl_xor_sync(0xffffffffu, vtop, d));
     }
 #pragma unroll
     for (int q = 0; q < kTiles; ++q) grown = grown || top[q][0] > m[q][0] || top[q][1] > m[q][1];
-    grown = grown || (kInt8 && vtop > vref);
     if (__any_sync(0xffffffffu, grown)) {
-      float fv = 1.0f;
-      if (kInt8 && vtop > vref) {   // the same in every lane: all rows share the keys
-        const float vn = scale_unit(vtop);
-        fv = vref / vn;
-        vref = vn;
-      }
 #pragma unroll
       for (int q = 0; q < kTiles; ++q) {
         float f[2];
@@ -339,13 +336,11 @@ __global__ void __launch_bounds__(kWarps * 32, (RowCfg<kInt8, D>::kCtas)) attn_r
           f[i] = m[q][i] == -INFINITY ? 0.0f : exp2_approx(m[q][i] - mn);
           m[q][i] = mn;
           l[q][i] *= f[i];
-          f[i] *= fv;
         }
 #pragma unroll
         for (int t = 0; t < MT; ++t) o[q][t][0] *= f[0], o[q][t][1] *= f[1], o[q][t][2] *= f[0], o[q][t][3] *= f[1];
       }
     }
-    const float vinv = kInt8 ? (vref > 0.0f ? 1.0f / vref : 0.0f) : 1.0f;
 
     // Weights as B fragments (transposed: a lane has keys 2 c, 2 c + 1 of row g), then the product with the values.
 #pragma unroll
@@ -353,14 +348,13 @@ __global__ void __launch_bounds__(kWarps * 32, (RowCfg<kInt8, D>::kCtas)) attn_r
       uint32_t pb[kTiles][2];
 #pragma unroll
       for (int q = 0; q < kTiles; ++q) {
-        const float m0 = m[q][0] == -INFINITY ? 0.0f : m[q][0], m1 = m[q][1] == -INFINITY ? 0.0f : m[q][1];
+        const float m0 = (m[q][0] == -INFINITY ? 0.0f : m[q][0]) - kTop, m1 = (m[q][1] == -INFINITY ? 0.0f : m[q][1]) - kTop;
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
           const float e0 = exp2_approx(sc[blk][q][2 * h] - m0), e1 = exp2_approx(sc[blk][q][2 * h + 1] - m1);
-          l[q][0] += e0;
-          l[q][1] += e1;
-          const float w = kInt8 ? vs[blk][h] * vinv : 1.0f;
-          pb[q][h] = transposed(kInt8 ? pack_f16(e0 * w, e1 * w) : pack_f16(e0, e1));
+          l[q][0] = kInt8 ? fmaf(e0, vinv[blk][h], l[q][0]) : l[q][0] + e0;
+          l[q][1] = kInt8 ? fmaf(e1, vinv[blk][h], l[q][1]) : l[q][1] + e1;
+          pb[q][h] = transposed(kInt8 ? pack_f16(e0 * vs[blk][h], e1 * vs[blk][h]) : pack_f16(e0, e1));
         }
       }
       const uint32_t sv = st + C::kHalf;
@@ -421,7 +415,7 @@ __global__ void __launch_bounds__(kWarps * 32, (RowCfg<kInt8, D>::kCtas)) attn_r
 #pragma unroll
         for (int t = 0; t < MT; ++t) {   // INT8: features D / 8 g + 2 t and the next; FP16: 16 t + g and 8 further
           if constexpr (kInt8) {
-            *reinterpret_cast<float2*>(dst + D / 8 * g + 2 * t) = make_float2(o[q][t][i] * vref, o[q][t][2 + i] * vref);
+            *reinterpret_cast<float2*>(dst + D / 8 * g + 2 * t) = make_float2(o[q][t][i], o[q][t][2 + i]);
           } else {
             dst[16 * t + g] = o[q][t][i];
             dst[16 * t + g + 8] = o[q][t][2 + i];
