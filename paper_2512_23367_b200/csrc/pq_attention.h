@@ -64,6 +64,12 @@ __device__ __forceinline__ float exp2_approx(float x) {
   return y;
 }
 
+__device__ __forceinline__ float log2_approx(float x) {
+  float y;
+  asm("lg2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
+}
+
 __device__ __forceinline__ uint32_t pack_f16(float a, float b) {
   const __half2 h = __floats2half2_rn(a, b);
   return *reinterpret_cast<const uint32_t*>(&h);
@@ -79,10 +85,10 @@ __device__ __forceinline__ float power_of_two(int e) { return __uint_as_float(st
 // The exponent of an INT8 value scale, within [-40, 60]: scales of FP16 values lie in [2^-31, 2^10), and with a range of
 // 100 no weight that counts leaves FP32's on the way to its sum, nor does a sum of them.
 __device__ __forceinline__ int scale_exponent(float v) { return min(max(static_cast<int>(__float_as_uint(v) << 1 >> 24) - 127, -40), 60); }
-// The smallest power of two >= v (at least 2^-126): the unit that a run of INT8 value scales is taken in.
+__device__ __forceinline__ float scale_log(float v) { return fminf(fmaxf(log2_approx(v), -40.0f), 60.0f); }   // within the same range
+// The smallest power of two >= v, within the same range: the unit that a run of INT8 value scales is taken in.
 __device__ __forceinline__ float scale_unit(float v) {
-  const uint32_t u = (__float_as_uint(fminf(fmaxf(v, 0.0f), 1e37f)) + 0x7fffffu) & 0x7f800000u;
-  return __uint_as_float(u < 0x00800000u ? 0x00800000u : u);
+  return __uint_as_float((__float_as_uint(fminf(fmaxf(v, 0x1p-40f), 0x1p60f)) + 0x7fffffu) & 0x7f800000u);
 }
 
 // Keys [lo, hi) that a request's rows may see: lo from the window of its first row, hi from its length and its table.

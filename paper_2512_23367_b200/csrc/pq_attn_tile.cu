@@ -23,9 +23,10 @@ struct TileCfg {
   static constexpr int kTileBytes = kTile * D * 2;            // one operand tile: D / 64 panels of 128 rows x 128 B
   static constexpr int kPanel = kTile * 128;
   static constexpr int kStages = (kInt8 ? 131072 : 163840) / kTileBytes;   // keys and values alternate
-  // INT8: scales of a tile (keys', values', the values' units of 32 keys each, the largest of the keys'), and 128 ones.
+  // INT8: scales of a tile (keys'; values' over their units; log2 of the values'; the units, of 32 keys each; the largest of
+  // the keys'), and 128 ones.
   static constexpr int kScaleTiles = kInt8 ? kStages / 2 + 1 : 0;
-  static constexpr int kScaleFloats = 2 * kTile + 8;
+  static constexpr int kScaleFloats = 3 * kTile + 8;
   static constexpr int kBars = 2 * kStages + 7 + kScaleTiles;
   static constexpr int kSmem = (2 + kStages) * kTileBytes + kScaleTiles * kScaleFloats * 4 + (kInt8 ? 4 * kTile : 0) +
                                6 * 16 * kConv /* the converters' slots */ + 1024 /* alignment */;
@@ -337,8 +338,9 @@ __global__ void __launch_bounds__(kJoinThreads) attn_join_kernel(const AttnArgs 
 // 16 codes in flight into slots of its own, turns the codes into FP16 (exact) and stores them in the layout that TMA
 // would have left.  (Copies into registers cost spills: 4000 cycles per operand tile.)  The
 // key's scale (times the softmax scale) multiplies the score.  The value's scale multiplies the weight before it is
-// rounded, relative to the power of two above the largest scale of its 32 keys, and the quotient of that unit and
-// the running unit of O goes into the exponent, exactly.
+// rounded: the power of two above the largest scale of its 32 keys goes into the exponent, the quotient of the two
+// multiplies.  The reference is the largest product of weight and value scale, up to 2^8, over the keys that the row
+// sees (a key that it does not see moves nothing), and FP16 weights keep their bits down to 2^-21 of that at least.
 // Six requests, chunks of up to 700 over up to 5000: 210 us (0.67 PFLOP/s), FP16 153; issue, 71 % of the slots: the
 // conversion is done again for every 256 rows, and each score takes two products more.
 template <bool kInt8, int D>
@@ -348,6 +350,7 @@ attn_tile_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constan
   constexpr int kThreads = C::kThreads;
   constexpr int KS = D / 16;        // MMAs of one QK
   constexpr int PS = kTile / 16;    // MMAs of one PV
+  constexpr float kTop = kInt8 ? 7.0f : 0.0f;   // a weight at the reference is 2^kTop
   extern __shared__ uint8_t smem_raw[];
   __shared__ __align__(8) uint64_t bars[C::kBars];
   __shared__ uint32_t s_tmem;
@@ -586,9 +589,13 @@ attn_tile_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constan
             float top = fmaxf(fmaxf(s.x, s.y), fmaxf(s.z, s.w)) * factor;
 #pragma unroll
             for (int o = 1; o < 32; o <<= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
-            if (lane == 0) asm volatile("st.shared.f32 [%0], %1;" ::"r"(s0 + 4 * (2 * kTile + 4)), "f"(top) : "memory");
+            if (lane == 0) asm volatile("st.shared.f32 [%0], %1;" ::"r"(s0 + 4 * (3 * kTile + 4)), "f"(top) : "memory");
           }
-          if (is_v && (lane & 7) == 0) asm volatile("st.shared.f32 [%0], %1;" ::"r"(s0 + 4 * kTile + (lane >> 1)), "f"(unit) : "memory");
+          if (is_v) {   // s0: of the values' scales
+            const float4 g = make_float4(scale_log(s.x), scale_log(s.y), scale_log(s.z), scale_log(s.w));
+            asm volatile("st.shared.v4.f32 [%0], {%1, %2, %3, %4};" ::"r"(s0 + 4 * kTile + 16 * lane), "f"(g.x), "f"(g.y), "f"(g.z), "f"(g.w) : "memory");
+            if ((lane & 7) == 0) asm volatile("st.shared.f32 [%0], %1;" ::"r"(s0 + 8 * kTile + (lane >> 1)), "f"(unit) : "memory");
+          }
           __syncwarp();
           if (lane == 0) mbar_arrive(bar_full + 8 * ((2 * t) % C::kStages));
         }
@@ -719,8 +726,6 @@ attn_tile_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constan
     const int all_from = a.window > 0 ? p_base + toks - a.window : 0;
     const int mine = two ? n_tiles : (n_tiles - acc + 1) >> 1;
     const float sc = kInt8 ? 1.0f : a.scale_log2;   // INT8: in the keys' scales
-    float vref = 1.0f;               // INT8: the unit of O; 0 as long as there is none
-    if (kInt8) vref = 0.0f;
     const float* ones = reinterpret_cast<const float*>(smem_raw + (scales - smem_u32(smem_raw))) + C::kScaleTiles * C::kScaleFloats;
     float m = -INFINITY, l = 0.0f;   // m: the reference that is subtracted, in powers of two; l: the thread's own keys
 
@@ -739,11 +744,11 @@ attn_tile_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constan
                          (((key0 - key_base) / kTile) % (kInt8 ? C::kScaleTiles : 1)) * C::kScaleFloats;
       const bool edge = key0 < all_from || key0 + kTile > all_to;   // some row does not see all keys
       const float* ksc = sct + 64 * half;   // INT8: what is still to be multiplied to the scores
-      float units[2] = {1.0f, 1.0f}, vtop = 0.0f;
+      int unit_log[2] = {0, 0};             // of the thread's two runs of 32 keys
       if constexpr (kInt8) {
-        const float4 u = *reinterpret_cast<const float4*>(sct + 2 * kTile);
-        units[0] = half ? u.z : u.x, units[1] = half ? u.w : u.y;
-        vtop = fmaxf(fmaxf(u.x, u.y), fmaxf(u.z, u.w));
+        const float4 u = *reinterpret_cast<const float4*>(sct + 3 * kTile);
+        unit_log[0] = static_cast<int>(__float_as_uint(half ? u.z : u.x) >> 23) - 127;
+        unit_log[1] = static_cast<int>(__float_as_uint(half ? u.w : u.y) >> 23) - 127;
       }
       float t;
       bool moves;   // the row's reference
@@ -759,10 +764,13 @@ attn_tile_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constan
         }
         return fmaxf(max3(top[0], top[1], top[2]), top[3]);
       };
-      // INT8: no score exceeds the largest product of codes times the largest scale; as long as that does not move the
-      // reference, the keys' scales go into the exponents' FMA below (prompt of 4096: 177 to 170 us).
+      // INT8: no product of weight and value scale exceeds the largest product of codes times the largest key scale, in
+      // powers of two, times the larger unit; as long as that does not move the reference, the keys' scales go into the
+      // exponents' FMA below (prompt of 4096: 177 to 170 us).
       bool exact = true;
-      if constexpr (kInt8) exact = edge || pair_any(pair, !(fmaxf(largest(), 0.0f) * sct[2 * kTile + 4] <= m + 8.0f) || vtop > vref);
+      if constexpr (kInt8) {
+        exact = edge || pair_any(pair, !(fmaf(fmaxf(largest(), 0.0f), sct[3 * kTile + 4], static_cast<float>(max(unit_log[0], unit_log[1]))) <= m + 8.0f));
+      }
       if (exact) {
         if constexpr (kInt8) {
 #pragma unroll
@@ -785,8 +793,21 @@ attn_tile_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constan
               if (32 * h + j > to || 32 * h + j <= from) s[h][j] = 0xff800000u;   // -inf
           }
         }
-        t = largest() * sc;
-        moves = pair_any(pair, t > m + 8.0f || (kInt8 && vtop > vref));   // rare after the first tiles: some row of the 32
+        if constexpr (kInt8) {   // of the products of weight and value scale, over the keys that the row sees
+          t = -INFINITY;
+#pragma unroll
+          for (int j = 0; j < 64; j += 4) {
+            const float4 v = *reinterpret_cast<const float4*>(sct + 2 * kTile + 64 * half + j);
+            const uint32_t* x = &s[j >> 5][j & 31];
+            float x0, x1, x2, x3;
+            unpair_f32(add_f32x2(pair_f32(v.x, v.y), pair_f32(__uint_as_float(x[0]), __uint_as_float(x[1]))), x0, x1);
+            unpair_f32(add_f32x2(pair_f32(v.z, v.w), pair_f32(__uint_as_float(x[2]), __uint_as_float(x[3]))), x2, x3);
+            t = max3(max3(t, x0, x1), x2, x3);
+          }
+        } else {
+          t = largest() * sc;
+        }
+        moves = pair_any(pair, t > m + 8.0f);   // rare after the first tiles: some row of the 32
       } else {
         moves = false, t = 0.0f;
       }
@@ -794,13 +815,9 @@ attn_tile_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constan
       if (moves) {
         t = pair_combine<false>(swap, pair, half, t);
         const bool grown = t > m + 8.0f;
-        float f = grown ? (m == -INFINITY ? 0.0f : exp2_approx(m - t)) : 1.0f;
+        const float f = grown ? (m == -INFINITY ? 0.0f : exp2_approx(m - t)) : 1.0f;
         if (grown) m = t;
         l *= f;
-        if (kInt8 && vtop > vref) {   // the same in every thread
-          f *= vref / vtop;
-          vref = vtop;
-        }
         if (i > 0) {   // O holds the sums up to the tile before
           ok = ok && warp_wait(bar_o + 8 * acc, (i - 1) & 1, wc);
           done = true;
@@ -821,9 +838,7 @@ attn_tile_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constan
       uint32_t w[32], asked = 0;
 #pragma unroll
       for (int q = 0; q < 2; ++q) {
-        // INT8: weights in units of units[q] / vref, a power of two <= 1 (2^-60 at least, where all weights round to 0)
-        const int shift = kInt8 ? max(static_cast<int>(__float_as_uint(units[q]) >> 23) - static_cast<int>(__float_as_uint(vref) >> 23), -60) : 0;
-        const float off = kInt8 ? static_cast<float>(shift) - ms : -ms;
+        const float off = kInt8 ? static_cast<float>(unit_log[q]) + (kTop - ms) : kTop - ms;
         const uint64_t off2 = pair_f32(off, off);
         uint64_t sum = 0;
         float4 vsc = make_float4(0.0f, 0.0f, 0.0f, 0.0f), kf = vsc;
@@ -846,7 +861,7 @@ attn_tile_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constan
         if (q == 0) asked = mbar_test2(bar_o + 8 * acc, (i - 1) & 1, bar_o + 8 * acc, (i - 1) & 1);
         float l0, l1;
         unpair_f32(sum, l0, l1);
-        l += kInt8 ? (l0 + l1) * __uint_as_float(static_cast<uint32_t>(127 - shift) << 23) : l0 + l1;
+        l += kInt8 ? (l0 + l1) * power_of_two(-unit_log[q]) : l0 + l1;
       }
       if (!done && !__all_sync(0xffffffffu, asked)) ok = ok && warp_wait(bar_o + 8 * acc, (i - 1) & 1, wc);
       tc_fence_after_sync();
@@ -875,8 +890,7 @@ attn_tile_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constan
           tmem_ld_wait();
 #pragma unroll
           for (int j = 0; j < 4; ++j)
-            room[(4 * h + j) * kTile + r] = make_float4(__uint_as_float(o[4 * j]) * vref, __uint_as_float(o[4 * j + 1]) * vref,
-                                                        __uint_as_float(o[4 * j + 2]) * vref, __uint_as_float(o[4 * j + 3]) * vref);
+            room[(4 * h + j) * kTile + r] = make_float4(__uint_as_float(o[4 * j]), __uint_as_float(o[4 * j + 1]), __uint_as_float(o[4 * j + 2]), __uint_as_float(o[4 * j + 3]));
         }
         if (half == 0) room_ml[r] = make_float2(m, l);
       }
@@ -889,7 +903,6 @@ attn_tile_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constan
         m = M;
       }
     }
-    f0 *= vref;
     const bool writes = two || acc == 0;
     constexpr int kPart = kPartFloats<D>;
     float* pu = a.partials + static_cast<int64_t>(unit - ta.whole) * most_parts * kPart;   // of a unit in parts

@@ -92,3 +92,22 @@ def _far_larger_scale_on_a_key_of_little_weight(new, total, heavy):
 def test_weights_keep_their_bits_beside_a_far_larger_value_scale(new, total, heavy):
     d, y, bound = _far_larger_scale_on_a_key_of_little_weight(new, total, heavy)
     assert (np.abs(_serve(d, workspace=_workspace(d)) - y) <= bound).all()
+
+
+# The same for requests of more rows: one tile of 128, two, several.  Up to 128 keys are seen, which half a step of FP16,
+# 2^-25 under a largest weight of 2^7 at least, adds up to 2^-25 of the largest product over.
+MANY = [([5], [20], 0), ([20, 3], [100, 7], 0), ([40, 2], [100, 20], 0), ([100], [128], 0), ([5], [200], 16), ([300], [400], 50), ([70], [60], 1)]
+
+
+@pytest.mark.parametrize("new,total,window", MANY)
+def test_a_value_that_a_row_does_not_see_leaves_its_weights_alone_in_long_chunks(new, total, window):
+    d = _far_larger_scale_on_an_unseen_key(new, total, window, seed=sum(total))
+    y, bound = ref.attention(d)
+    off = np.abs(_serve(d, workspace=_workspace(d)) - y)
+    assert (off <= bound).all(), f"rows {np.unique(np.argwhere(off > bound)[:, 0])}"
+
+
+@pytest.mark.parametrize("new,total,heavy", [([5], [50], 3), ([20], [120], 40), ([40], [300], 17), ([200], [700], 450)])
+def test_weights_keep_their_bits_beside_a_far_larger_value_scale_in_long_chunks(new, total, heavy):
+    d, y, bound = _far_larger_scale_on_a_key_of_little_weight(new, total, heavy)
+    assert (np.abs(_serve(d, workspace=_workspace(d)) - y) <= bound).all()
