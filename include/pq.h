@@ -428,9 +428,10 @@ PQ_API int pq_kv_read(const pq_kv_cache* cache, const int64_t* slots, int64_t to
  * L = kv_len[b] cached tokens, stands at position p = L - n + (t - q_start[b]) and sees the keys
  *   j <= p, j >= 0, and j > p - window when window > 0:
  *   s_j = scale * sum_d q[d] k_j[d],  y = sum_j e^(s_j - max) v_j / sum_j e^(s_j - max)
- * for query head h over the key/value head h / (heads / cache->heads).  Scores, maxima and sums are FP32;
- * the weights are rounded to FP16 for their product with the values (they lie in [0, 256]), and the
- * product is summed in FP32.  A row that sees no key (kv_len shorter than the chunk, window or not) gives 0.
+ * for query head h over the key/value head h / (heads / cache->heads).  Scores, maxima and sums are FP32, and so is
+ * the sum of the products with the values.  For that product the weights (PQ_KV_INT8: times their value's scale) are
+ * rounded to FP16, relative to the largest that the row sees: 11 bits down to 2^-21 of it, half a step of 2^-32 of it
+ * below.  A row that sees no key (kv_len shorter than the chunk, window or not) gives 0.
  * A key that a row does not see does not reach it, whatever it holds, and nothing beyond kv_len or before
  * the window of a chunk's first row is used.  The VALUES in between are taken as finite: one that is infinite
  * or NaN also reaches rows of its request that do not see it (0 times it).

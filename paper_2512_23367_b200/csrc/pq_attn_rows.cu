@@ -94,6 +94,9 @@ __device__ __forceinline__ uint32_t transposed(uint32_t v) {   // an 8 x 8 tile 
 // weights, FP32, takes 2^(x + e - max + 14) times 2^-e.  The feature order of a matrix step is permuted so that a lane's codes
 // are 16 consecutive bytes; queries (and the result's rows) are permuted alike.
 //
+// FP16 holds weights up to 2^15 (kTop), so that they keep their bits down to 2^-29 of the largest and count down to 2^-39:
+// 131072 keys of 2^-26 each are 0.2 % of a row, and with weights up to 1 they would be lost.
+//
 // Measured, 32 heads over 8 of 128, 64 requests of one token over up to 8192: FP16 208 us (6.7 TB/s, what a copy
 // reaches); INT8 130 us (5.5 TB/s): issue, 58 % of the slots, for the codes' conversion and the scales.  3 requests over
 // 131072: 247 us (6.5 TB/s).  1000 tokens of one request: 6.6 us, latency.
@@ -102,7 +105,7 @@ __global__ void __launch_bounds__(kWarps * 32, (RowCfg<kInt8, D>::kCtas)) attn_r
   using C = RowCfg<kInt8, D>;
   constexpr int KS = D / 16;   // matrix steps over the features
   constexpr int MT = D / 16;   // 16-wide feature tiles of the result
-  constexpr float kTop = kInt8 ? 14.0f : 0.0f;   // the largest weight is 2^kTop (INT8: times the rest of its scale, below 2)
+  constexpr float kTop = kInt8 ? 14.0f : 15.0f;   // the largest weight is 2^kTop (INT8: times the rest of its scale, below 2)
   extern __shared__ __align__(128) uint8_t smem[];
   __shared__ bool s_last;
 

@@ -314,10 +314,11 @@ __global__ void __launch_bounds__(kJoinThreads) attn_join_kernel(const AttnArgs 
 // 128, or up to 128 rows as two accumulators that take the even and the odd key tiles and are joined at the end:
 // either way one accumulator's softmax runs while the tensor core works for the other.  Per 128 keys and accumulator:
 //   S = Q K^T            8 (D / 16) MMAs from shared memory into tensor memory
-//   softmax              two threads per row: S to registers, running maximum, P = 2^(S - max) as FP16
+//   softmax              two threads per row: S to registers, running maximum, P = 2^(S - max + 7) as FP16
 //   O += P V             8 MMAs with P from tensor memory, V as it lies in the cache (features contiguous)
 // The reference that is subtracted is only moved (and O rescaled, in tensor memory) when the maximum has grown by
-// more than 2^8: P stays within [0, 256], exact enough in FP16, and O is almost never touched.
+// more than 2^8: O is almost never touched, P stays below 2^15, and FP16 keeps its bits down to 2^-21 of the maximum and
+// counts it down to 2^-31.
 // Tensor memory (512 columns): S, shared by the accumulators in turn, 128; P of each, 64; O of each, 64 or 128.  S is
 // free as soon as the softmax threads hold it in registers, so that QK(u + 1) runs under the softmax of u; MMA order
 // QK(u), PV(u - 2), u counting the accumulators in turn.  With P over S and one S per accumulator the chain
@@ -350,7 +351,7 @@ attn_tile_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constan
   constexpr int kThreads = C::kThreads;
   constexpr int KS = D / 16;        // MMAs of one QK
   constexpr int PS = kTile / 16;    // MMAs of one PV
-  constexpr float kTop = kInt8 ? 7.0f : 0.0f;   // a weight at the reference is 2^kTop
+  constexpr float kTop = 7.0f;      // a weight at the reference is 2^kTop
   extern __shared__ uint8_t smem_raw[];
   __shared__ __align__(8) uint64_t bars[C::kBars];
   __shared__ uint32_t s_tmem;
