@@ -91,6 +91,13 @@ __device__ __forceinline__ float scale_unit(float v) {
   return __uint_as_float((__float_as_uint(fminf(fmaxf(v, 0x1p-40f), 0x1p60f)) + 0x7fffffu) & 0x7f800000u);
 }
 
+// First key that a row at position p sees.  In 64 bits: p may be negative (a row before its request's first key) and
+// the window up to 2^31 - 1.
+__device__ __forceinline__ int first_key(int p, int window) {
+  const int64_t first = static_cast<int64_t>(p) + 1 - window;
+  return window > 0 && first > 0 ? static_cast<int>(first) : 0;
+}
+
 // Keys [lo, hi) that a request's rows may see: lo from the window of its first row, hi from its length and its table.
 struct AttnRange {
   int n, L, lo, hi;
@@ -98,11 +105,10 @@ struct AttnRange {
 __device__ __forceinline__ AttnRange attn_range(const AttnArgs& a, int rows, int cached) {
   AttnRange r;
   r.n = rows;
-  r.L = cached;
+  r.L = max(cached, 0);   // positions from -n on stay within 32 bits
   const int64_t cap = a.width * a.c.page;
   r.hi = static_cast<int>(min(static_cast<int64_t>(r.L), cap));
-  const int64_t lo = static_cast<int64_t>(r.L) - r.n + 1 - a.window;
-  r.lo = (a.window > 0 && lo > 0) ? static_cast<int>(lo) : 0;
+  r.lo = first_key(r.L - r.n, a.window);
   return r;
 }
 

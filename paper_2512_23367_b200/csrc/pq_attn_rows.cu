@@ -229,10 +229,10 @@ __global__ void __launch_bounds__(kWarps * 32, (RowCfg<kInt8, D>::kCtas)) attn_r
       const int r = 8 * q + 2 * c + i;
       const int p = rg.L - rg.n + r / G;
       p_row[q][i] = r < rows ? min(p, rg.hi - 1) : -1;
-      w_row[q][i] = a.window > 0 ? p - a.window : -1;   // keys above it
+      w_row[q][i] = first_key(p, a.window) - 1;   // keys above it
     }
   }
-  const int all_from = a.window > 0 ? rg.L - a.window : 0;      // keys that every row sees: [all_from, all_to)
+  const int all_from = first_key(rg.L - 1, a.window);           // keys that every row sees: [all_from, all_to)
   const int all_to = min(rg.L - rg.n + 1, rg.hi);
 
   float o[kTiles][MT][4];

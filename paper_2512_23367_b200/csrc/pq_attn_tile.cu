@@ -240,7 +240,7 @@ __device__ __forceinline__ SlotKeys slot_keys(const AttnArgs& a, const AttnRange
   s.toks = min(qt, rg.n - tok0);
   s.p_base = rg.L - rg.n + tok0;
   const int k_hi = min(rg.hi, s.p_base + s.toks);
-  s.k_lo = (a.window > 0 ? max(0, s.p_base + 1 - a.window) : 0) & ~(kTile - 1);
+  s.k_lo = first_key(s.p_base, a.window) & ~(kTile - 1);
   s.tiles = k_hi > s.k_lo ? (k_hi - s.k_lo + kTile - 1) / kTile : 0;
   s.per = a.part_keys / kTile;
   s.parts = most_parts == 1 ? 1 : max(1, min(most_parts, (s.tiles + s.per - 1) / s.per));
@@ -722,9 +722,9 @@ attn_tile_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constan
 
     const int p = p_base + tok;
     const int see_to = min(p, rg.hi - 1) - 64 * half;                        // last key of the row, from the thread's first
-    const int see_from = (a.window > 0 ? p - a.window : -1) - 64 * half;     // keys above it
+    const int see_from = first_key(p, a.window) - 1 - 64 * half;             // keys above it
     const int all_to = min(p_base + q_tile * tpt + 1, rg.hi);                // every row of the tile sees [all_from, all_to)
-    const int all_from = a.window > 0 ? p_base + toks - a.window : 0;
+    const int all_from = first_key(p_base + toks - 1, a.window);
     const int mine = two ? n_tiles : (n_tiles - acc + 1) >> 1;
     const float sc = kInt8 ? 1.0f : a.scale_log2;   // INT8: in the keys' scales
     const float* ones = reinterpret_cast<const float*>(smem_raw + (scales - smem_u32(smem_raw))) + C::kScaleTiles * C::kScaleFloats;

@@ -45,3 +45,14 @@ def test_a_bound_of_the_rows_may_be_anything(new, total, max_q):
     y, bound = ref.attention(d)
     for workspace in (_workspace(d, max_q=max_q), None):
         assert (np.abs(_serve(d, max_q=max_q, workspace=workspace) - y) <= bound).all()
+
+
+@pytest.mark.parametrize("cache", ["f16", "int8"])
+@pytest.mark.parametrize("window", [2**31 - 1, 2**31 - 64, 2**30, 301])
+@pytest.mark.parametrize("new,total", [([200], [100]), ([300, 3], [7, 1]), ([4, 2], [2, 300]), ([70], [300])])
+def test_a_window_as_long_as_anything_is_none(new, total, window, cache):
+    """Also where the chunk is longer than what is cached, so that its first rows stand before the first key."""
+    d = ref.attention_inputs(8, 2, 128, 16, cache, new, total, seed=sum(new))
+    y, bound = ref.attention(d)
+    for workspace in (_workspace(d), None):
+        assert (np.abs(_serve(d, window=window, workspace=workspace) - y) <= bound).all()
