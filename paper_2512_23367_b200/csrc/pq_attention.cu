@@ -16,7 +16,7 @@ int pq_paged_attention(const void* q_f16, int64_t q_stride, int32_t heads, const
                        void* out_f16, void* workspace, size_t workspace_bytes, void* stream) {
   int rc = check_kv_cache(cache);
   if (rc != PQ_OK) return rc;
-  if (heads < 1 || heads % cache->heads != 0 || heads / cache->heads > 64) return PQ_ERR_SHAPE;
+  if (heads < 1 || heads % cache->heads != 0 || heads / cache->heads > kMostGroup) return PQ_ERR_SHAPE;
   if (requests < 0 || requests > 0x7fffffff || tokens < 0 || tokens > 0x7fffffff) return PQ_ERR_SHAPE;
   if (width < 1 || width > 0x7fffffff || max_q < 0 || max_kv < 0 || window < 0 || !std::isfinite(scale)) return PQ_ERR_SHAPE;
   if (q_stride < static_cast<int64_t>(heads) * cache->dim || q_stride % 8 != 0) return PQ_ERR_SHAPE;
@@ -54,7 +54,7 @@ int pq_paged_attention(const void* q_f16, int64_t q_stride, int32_t heads, const
 size_t pq_attention_workspace_bytes(int64_t requests, int64_t tokens, int64_t max_q, int64_t max_kv, int32_t heads,
                                     int32_t kv_heads, int32_t dim, int32_t sms) {
   if (requests < 1 || requests > PQ_MAX_REQUESTS || tokens < 1 || tokens > 0x7fffffff || max_q < 1 || max_kv < 1 || kv_heads < 1 ||
-      heads < kv_heads || heads % kv_heads != 0 || (dim != 64 && dim != 128) || sms < 1) {
+      kv_heads > kMostKvHeads || heads < kv_heads || heads % kv_heads != 0 || heads / kv_heads > kMostGroup || (dim != 64 && dim != 128) || sms < 1) {
     return 0;
   }
   max_q = std::min(max_q, tokens);

@@ -30,6 +30,8 @@ struct AttnArgs {
 // Requests with more rows go to the tile kernel.
 constexpr int kAttnRows = 16;
 
+constexpr int kMostGroup = 64;   // query heads of one key/value head
+
 // Lengths are 32 bits wide, and the schedules round up to parts of 128 keys in 32 bits: 2^30 keys are as good as more
 // (the last part of a unit takes the keys that are left).
 constexpr int64_t kMostKeys = int64_t(1) << 30;

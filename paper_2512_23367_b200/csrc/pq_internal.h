@@ -80,6 +80,7 @@ inline bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 
 inline bool aligned256(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 255u) == 0; }
 // The rules of pq.h for a paged cache's geometry and pointers.
 int check_kv_cache(const pq_kv_cache* c);
+constexpr int kMostKvHeads = 1024;
 
 // ---- launchers (each returns a pq_status; all are asynchronous on `stream`) ----
 // col (nullable, [K] FP32): per-column factor applied before the maximum is taken (Eq. 3).

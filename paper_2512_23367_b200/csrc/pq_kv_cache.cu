@@ -16,7 +16,7 @@ int check_kv_cache(const pq_kv_cache* c) {
   if (c->type == PQ_KV_INT8 && (c->k_scale == nullptr || c->v_scale == nullptr)) return PQ_ERR_NULL;
   if (c->dim != 64 && c->dim != 128) return PQ_ERR_SHAPE;
   if (c->page < 16 || c->page > 1024 || c->page % 16 != 0) return PQ_ERR_SHAPE;
-  if (c->heads < 1 || c->heads > 1024 || c->pages < 1 || c->pages > 0x7fffffff) return PQ_ERR_SHAPE;
+  if (c->heads < 1 || c->heads > kMostKvHeads || c->pages < 1 || c->pages > 0x7fffffff) return PQ_ERR_SHAPE;
   if (c->pages * c->heads * c->page > 0x7fffffff) return PQ_ERR_SHAPE;
   if (!aligned16(c->k) || !aligned16(c->v)) return PQ_ERR_ALIGN;
   if (c->type == PQ_KV_INT8 && (!aligned16(c->k_scale) || !aligned16(c->v_scale))) return PQ_ERR_ALIGN;

@@ -175,3 +175,11 @@ def test_workspace_query_takes_bounds_of_any_size():
     for max_kv in (2**31 - 1, 2**40, 2**63 - 1):
         assert size(1, 300, 300, max_kv, 32, 8, 128) == size(1, 300, 300, 2**30, 32, 8, 128)
     assert size(1, 2**31, 300, 8192, 32, 8, 128) == 0
+
+
+def test_workspace_query_refuses_what_the_call_refuses():
+    size = pq.pq_attention_workspace_bytes
+    assert size(1, 100, 100, 9000, 64, 1, 64) > 0
+    for heads, kv_heads in ((65, 1), (129, 1), (100000, 1), (4096, 2048), (3, 2), (0, 1), (4, 0)):   # groups of 65 and more, ...
+        assert size(1, 100, 100, 9000, heads, kv_heads, 64) == 0
+    assert size(1, 100, 100, 9000, 8, 2, 80) == 0 and size(4097, 5000, 2, 9000, 8, 2, 64) == 0
