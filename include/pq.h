@@ -447,7 +447,9 @@ PQ_API int pq_kv_read(const pq_kv_cache* cache, const int64_t* slots, int64_t to
  *   workspace: as for pq_gemm_w8a8 (optional, prepared once with pq_workspace_init, one per stream of calls
  *     that may overlap): partial results of keys that are split over several SMs, summed in a fixed order.
  *     Without it, the keys of a request are not split; with too little, into fewer parts or not at all.
- * pq_attention_workspace_bytes: host-only; 0 when nothing is split or an argument is invalid.
+ * pq_attention_workspace_bytes: host-only; the workspace with which a call of these sizes without a window splits its
+ *   keys as it would with unlimited room, for either type of cache; 0 when nothing is split or an argument is
+ *   invalid.  pq_attention_workspace_bytes_window: the same with a window (0: none), which may want more or less.
  */
 PQ_API int pq_paged_attention(const void* q_f16, int64_t q_stride, int32_t heads, const pq_kv_cache* cache,
                               const int32_t* block_table, int64_t width, const int32_t* q_start,
@@ -456,6 +458,9 @@ PQ_API int pq_paged_attention(const void* q_f16, int64_t q_stride, int32_t heads
                               size_t workspace_bytes, void* stream);
 PQ_API size_t pq_attention_workspace_bytes(int64_t requests, int64_t tokens, int64_t max_q, int64_t max_kv,
                                            int32_t heads, int32_t kv_heads, int32_t dim, int32_t sms);
+PQ_API size_t pq_attention_workspace_bytes_window(int64_t requests, int64_t tokens, int64_t max_q, int64_t max_kv,
+                                                  int32_t heads, int32_t kv_heads, int32_t dim, int32_t sms,
+                                                  int32_t window);
 
 /*
  * Reads the device status word of the current device into *host_status (PQ_OK or

@@ -63,6 +63,7 @@ SIGNATURES = {
     "pq_paged_attention": (ctypes.c_int, [_vp, _i64, _i32, _vp, _vp, _i64, _vp, _vp, _i64, _i64, _i64, _i64,
                                           ctypes.c_float, _i32, _vp, _vp, ctypes.c_size_t, _vp]),
     "pq_attention_workspace_bytes": (ctypes.c_size_t, [_i64, _i64, _i64, _i64, _i32, _i32, _i32, _i32]),
+    "pq_attention_workspace_bytes_window": (ctypes.c_size_t, [_i64, _i64, _i64, _i64, _i32, _i32, _i32, _i32, _i32]),
 }
 MAX_GROUP = 4
 MAX_REQUESTS = 4096
@@ -688,17 +689,19 @@ def pq_kv_read(cache: PagedKV, slots: torch.Tensor) -> tuple[torch.Tensor, torch
 
 
 def pq_attention_workspace_bytes(requests: int, tokens: int, max_q: int, max_kv: int, heads: int, kv_heads: int,
-                                 dim: int, sms: int = 148) -> int:
-    """Bytes of workspace with which pq_paged_attention splits the keys as it would with unlimited room; 0 if it
-    does not split them.  Host-only, needs no GPU."""
-    return int(lib().pq_attention_workspace_bytes(requests, tokens, max_q, max_kv, heads, kv_heads, dim, sms))
+                                 dim: int, sms: int = 148, window: int = 0) -> int:
+    """Bytes of workspace with which pq_paged_attention splits the keys as it would with unlimited room, at these
+    sizes and this window (another window may want more); 0 if it does not split them.  Host-only, needs no GPU."""
+    return int(lib().pq_attention_workspace_bytes_window(requests, tokens, max_q, max_kv, heads, kv_heads, dim, sms, window))
 
 
-def pq_attention_workspace(q: torch.Tensor, cache: PagedKV, requests: int, max_q: int, max_kv: int) -> torch.Tensor | None:
-    """A prepared workspace for pq_paged_attention over these sizes (None where the call has no use for one)."""
+def pq_attention_workspace(q: torch.Tensor, cache: PagedKV, requests: int, max_q: int, max_kv: int,
+                           window: int = 0) -> torch.Tensor | None:
+    """A prepared workspace for pq_paged_attention over these sizes and this window (None where the call has no use
+    for one)."""
     T, H, _ = _token_rows(q, None, cache.dim, "q")
     sms = torch.cuda.get_device_properties(q.device).multi_processor_count
-    n = pq_attention_workspace_bytes(requests, T, max_q, max_kv, H, cache.heads, cache.dim, sms)
+    n = pq_attention_workspace_bytes(requests, T, max_q, max_kv, H, cache.heads, cache.dim, sms, window)
     return pq_workspace_init(torch.empty((n,), dtype=torch.uint8, device=q.device)) if n else None
 
 

@@ -53,19 +53,24 @@ int pq_paged_attention(const void* q_f16, int64_t q_stride, int32_t heads, const
 
 size_t pq_attention_workspace_bytes(int64_t requests, int64_t tokens, int64_t max_q, int64_t max_kv, int32_t heads,
                                     int32_t kv_heads, int32_t dim, int32_t sms) {
+  return pq_attention_workspace_bytes_window(requests, tokens, max_q, max_kv, heads, kv_heads, dim, sms, 0);
+}
+
+size_t pq_attention_workspace_bytes_window(int64_t requests, int64_t tokens, int64_t max_q, int64_t max_kv, int32_t heads,
+                                           int32_t kv_heads, int32_t dim, int32_t sms, int32_t window) {
   if (requests < 1 || requests > PQ_MAX_REQUESTS || tokens < 1 || tokens > 0x7fffffff || max_q < 1 || max_kv < 1 || kv_heads < 1 ||
-      kv_heads > kMostKvHeads || heads < kv_heads || heads % kv_heads != 0 || heads / kv_heads > kMostGroup || (dim != 64 && dim != 128) || sms < 1) {
+      kv_heads > kMostKvHeads || heads < kv_heads || heads % kv_heads != 0 || heads / kv_heads > kMostGroup || (dim != 64 && dim != 128) || sms < 1 || window < 0) {
     return 0;
   }
   max_q = std::min(max_q, tokens);
   max_kv = bounded_keys(max_kv);
-  size_t bytes = 0;   // for either type of cache, window or not
+  size_t bytes = 0;   // for either type of cache
   for (int int8 = 0; int8 < 2; ++int8) {
-    const AttnPlan plan = plan_attn_rows(requests, max_q, max_kv, 0, kv_heads, dim, int8 != 0, sms, ~size_t(0));
+    const AttnPlan plan = plan_attn_rows(requests, max_q, max_kv, window, kv_heads, dim, int8 != 0, sms, ~size_t(0));
     bytes = bytes > plan.partial_bytes ? bytes : plan.partial_bytes;
   }
   if (max_q * (heads / kv_heads) > kAttnRows) {
-    const TilePlan tile = plan_attn_tile(requests, tokens, max_q, max_kv, 0, heads / kv_heads, kv_heads, dim, sms, ~size_t(0));
+    const TilePlan tile = plan_attn_tile(requests, tokens, max_q, max_kv, window, heads / kv_heads, kv_heads, dim, sms, ~size_t(0));
     bytes = bytes > tile.partial_bytes ? bytes : tile.partial_bytes;   // the two kernels follow each other
   }
   return bytes > 0 ? kScratchHeaderBytes + bytes : 0;

@@ -56,3 +56,42 @@ def test_a_window_as_long_as_anything_is_none(new, total, window, cache):
     y, bound = ref.attention(d)
     for workspace in (_workspace(d), None):
         assert (np.abs(_serve(d, window=window, workspace=workspace) - y) <= bound).all()
+
+
+def _split(d, share=1.0, window=0):
+    """One call with `share` of the workspace that the query asks for at this window."""
+    full = _workspace(d, window=window)
+    header = 65536
+    pq.pq_workspace_init(full)
+    return _serve(d, window=window, workspace=full[: header + int((full.numel() - header) * share)] if share < 1 else full)
+
+
+@pytest.mark.parametrize("heads,kv_heads,dim,new,total,window", [
+    (32, 8, 128, [300], [4300], 4096), (32, 8, 128, [150, 150], [3000, 3000], 2048), (32, 32, 64, [1, 1, 1], [1300] * 3, 1024),
+    (8, 2, 128, [3], [2600], 1500)])
+def test_the_workspace_for_a_window_is_all_that_the_call_uses(heads, kv_heads, dim, new, total, window):
+    d = ref.attention_inputs(heads, kv_heads, dim, 16, "f16", new, total, window=window, seed=sum(total))
+    y, bound = ref.attention(d)
+    a = _split(d, window=window)
+    assert (np.abs(a - y) <= bound).all()
+    room = pq.pq_workspace_init(torch.empty((1 << 28,), dtype=torch.uint8, device=DEV))
+    assert np.array_equal(a, _serve(d, workspace=room))            # the same parts as with any amount of room
+
+
+@pytest.mark.parametrize("cache", ["f16", "int8"])
+@pytest.mark.parametrize("new,total", [([1], [5000]), ([3, 1], [4100, 700]), ([3], [2500])])
+def test_a_workspace_cut_short_still_serves_few_rows(new, total, cache):
+    d = ref.attention_inputs(8, 2, 128, 16, cache, new, total, seed=sum(total))
+    y, bound = ref.attention(d)
+    for share in (0.5, 0.2, 0.02):
+        assert (np.abs(_split(d, share) - y) <= bound).all()
+
+
+@pytest.mark.parametrize("cache", ["f16", "int8"])
+@pytest.mark.parametrize("new,total", [([1], [5000]), ([3, 1], [4100, 700]), ([70], [6000]), ([2, 40], [3000, 2000])])
+def test_a_bound_of_the_cached_tokens_that_is_too_small_costs_speed_only(new, total, cache):
+    """With parts all the same: the last one takes the keys that are left."""
+    d = ref.attention_inputs(8, 2, 128, 16, cache, new, total, seed=sum(total))
+    y, bound = ref.attention(d)
+    for hint in (1500, 700, 200):
+        assert (np.abs(_serve(d, max_kv=hint, workspace=_workspace(d)) - y) <= bound).all()

@@ -183,3 +183,12 @@ def test_workspace_query_refuses_what_the_call_refuses():
     for heads, kv_heads in ((65, 1), (129, 1), (100000, 1), (4096, 2048), (3, 2), (0, 1), (4, 0)):   # groups of 65 and more, ...
         assert size(1, 100, 100, 9000, heads, kv_heads, 64) == 0
     assert size(1, 100, 100, 9000, 8, 2, 80) == 0 and size(4097, 5000, 2, 9000, 8, 2, 64) == 0
+
+
+def test_workspace_query_knows_the_window():
+    size = lambda window: pq.pq_attention_workspace_bytes(1, 300, 300, 4300, 32, 8, 128, window=window)  # noqa: E731
+    part = 2 * 128 * (128 + 2) * 4                   # 40 units of 256 rows, in 3 parts without a window, in 4 with this one
+    assert size(0) == 65536 + 40 * 3 * part and size(4096) == 65536 + 40 * 4 * part
+    assert size(1) == 0 and size(2**31 - 1) == size(0) and size(-1) == 0
+    L = pq.lib()
+    assert L.pq_attention_workspace_bytes(1, 300, 300, 4300, 32, 8, 128, 148) == size(0)
