@@ -26,12 +26,13 @@ int pq_paged_attention(const void* q_f16, int64_t q_stride, int32_t heads, const
   if (!aligned16(q_f16) || !aligned16(out_f16) || !aligned256(workspace)) return PQ_ERR_ALIGN;
   if ((rc = check_arch()) != PQ_OK) return rc;
   // Up to 16 rows per request and key/value head go to the row kernel, more to the tile kernel; which of them a request
-  // takes is decided on the device.  A single request of many rows needs no row kernel.
+  // takes is decided on the device.  A single request of many rows needs no row kernel, nor do groups of more than 16
+  // heads, where a single token is more rows than it serves.
   const int group = heads / cache->heads;
   // No request has more rows than the step, nor keys beyond its table: larger bounds say no more.
   max_q = std::min(max_q, tokens);
   max_kv = bounded_keys(std::min(max_kv, width * cache->page));
-  const bool wide = max_q * group > kAttnRows, narrow = !wide || requests > 1;
+  const bool wide = max_q * group > kAttnRows, narrow = group <= kAttnRows && (!wide || requests > 1);
   AttnArgs a{static_cast<const __half*>(q_f16), q_stride, *cache, block_table, width, q_start, kv_len,
              static_cast<__half*>(out_f16), tokens, static_cast<int>(requests), heads, window,
              narrow ? kAttnRows / group : 0, scale * 1.44269504f, 0, nullptr, nullptr};
@@ -44,8 +45,9 @@ int pq_paged_attention(const void* q_f16, int64_t q_stride, int32_t heads, const
                                          sm_count(), sc.partial_bytes);
     a.part_keys = plan.part_keys;
     rc = launch_attn_rows(a, plan, max_q, st);
-    if (rc != PQ_OK || !wide) return rc;
+    if (rc != PQ_OK) return rc;
   }
+  if (!wide) return PQ_OK;
   const TilePlan tile = plan_attn_tile(requests, tokens, max_q, max_kv, window, group, cache->heads, cache->dim,
                                        sm_count(), sc.partial_bytes);
   return launch_attn_tile(a, tile, st);
@@ -65,12 +67,13 @@ size_t pq_attention_workspace_bytes_window(int64_t requests, int64_t tokens, int
   max_q = std::min(max_q, tokens);
   max_kv = bounded_keys(max_kv);
   size_t bytes = 0;   // for either type of cache
-  for (int int8 = 0; int8 < 2; ++int8) {
+  const int group = heads / kv_heads;
+  for (int int8 = 0; int8 < 2 && group <= kAttnRows; ++int8) {
     const AttnPlan plan = plan_attn_rows(requests, max_q, max_kv, window, kv_heads, dim, int8 != 0, sms, ~size_t(0));
     bytes = bytes > plan.partial_bytes ? bytes : plan.partial_bytes;
   }
-  if (max_q * (heads / kv_heads) > kAttnRows) {
-    const TilePlan tile = plan_attn_tile(requests, tokens, max_q, max_kv, window, heads / kv_heads, kv_heads, dim, sms, ~size_t(0));
+  if (max_q * group > kAttnRows) {
+    const TilePlan tile = plan_attn_tile(requests, tokens, max_q, max_kv, window, group, kv_heads, dim, sms, ~size_t(0));
     bytes = bytes > tile.partial_bytes ? bytes : tile.partial_bytes;   // the two kernels follow each other
   }
   return bytes > 0 ? kScratchHeaderBytes + bytes : 0;

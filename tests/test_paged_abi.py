@@ -192,3 +192,13 @@ def test_workspace_query_knows_the_window():
     assert size(1) == 0 and size(2**31 - 1) == size(0) and size(-1) == 0
     L = pq.lib()
     assert L.pq_attention_workspace_bytes(1, 300, 300, 4300, 32, 8, 128, 148) == size(0)
+
+
+def test_workspace_query_leaves_out_the_kernel_that_a_call_does_not_use():
+    """More than 16 query heads per key/value head: every request is the tile kernel's, whose parts are of one size."""
+    part = 2 * 128 * (64 + 2) * 4
+    for heads in (17, 32, 64):
+        for max_kv in (300, 1000, 200_000):
+            n = pq.pq_attention_workspace_bytes(3, 3, 1, max_kv, heads, 1, 64)
+            assert n == 0 or (n - 65536) % (3 * part) == 0
+    assert (pq.pq_attention_workspace_bytes(3, 3, 1, 1000, 16, 1, 64) - 65536) % (16 * (64 + 2) * 4) == 0
