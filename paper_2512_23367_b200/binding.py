@@ -618,6 +618,13 @@ def _operands(device: int, *checks) -> None:
         raise ValueError(f"operands on cuda:{device}, but the current device is cuda:{_device()}")
 
 
+def _in_32_bits(**sizes: int) -> None:
+    """ctypes keeps the low 32 bits of a larger number, which may be a valid other size."""
+    for name, n in sizes.items():
+        if not -1 << 31 <= n < 1 << 31:
+            raise ValueError(f"{name}: {n} is beyond 32 bits")
+
+
 def pq_block_tables(kv_len, new_len, block_table, free_list, free_head, page: int, tokens: int | None = None,
                     step: PagedStep | None = None) -> PagedStep:
     """Block tables, slot map and positions of one step.  kv_len, new_len i32 [requests]; block_table
@@ -625,6 +632,7 @@ def pq_block_tables(kv_len, new_len, block_table, free_list, free_head, page: in
     tokens: rows of the step, at least the sum of new_len; or step: buffers from PagedStep.empty, filled and
     returned."""
     B = kv_len.numel()
+    _in_32_bits(page=page)
     if block_table.dim() != 2:
         raise ValueError("block_table: expected a 2-D tensor [requests, width]")
     width, F = block_table.shape[1], free_list.numel()
@@ -692,6 +700,7 @@ def pq_attention_workspace_bytes(requests: int, tokens: int, max_q: int, max_kv:
                                  dim: int, sms: int = 148, window: int = 0) -> int:
     """Bytes of workspace with which pq_paged_attention splits the keys as it would with unlimited room, at these
     sizes and this window (another window may want more); 0 if it does not split them.  Host-only, needs no GPU."""
+    _in_32_bits(heads=heads, kv_heads=kv_heads, dim=dim, sms=sms, window=window)
     return int(lib().pq_attention_workspace_bytes_window(requests, tokens, max_q, max_kv, heads, kv_heads, dim, sms, window))
 
 
@@ -715,6 +724,7 @@ def pq_paged_attention(q: torch.Tensor, cache: PagedKV, block_table: torch.Tenso
     sees at most (0: all); workspace: from pq_attention_workspace (without it the keys are not split)."""
     T, H, qs = _token_rows(q, None, cache.dim, "q")
     B = kv_len.numel()
+    _in_32_bits(window=window)
     if block_table.dim() != 2:
         raise ValueError("block_table: expected a 2-D tensor [requests, width]")
     width = block_table.shape[1]

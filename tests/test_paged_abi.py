@@ -202,3 +202,18 @@ def test_workspace_query_leaves_out_the_kernel_that_a_call_does_not_use():
             n = pq.pq_attention_workspace_bytes(3, 3, 1, max_kv, heads, 1, 64)
             assert n == 0 or (n - 65536) % (3 * part) == 0
     assert (pq.pq_attention_workspace_bytes(3, 3, 1, 1000, 16, 1, 64) - 65536) % (16 * (64 + 2) * 4) == 0
+
+
+def test_sizes_beyond_32_bits_are_refused_not_cut():
+    i32 = lambda *s: torch.zeros(s, dtype=torch.int32)  # noqa: E731
+    Fake = types.SimpleNamespace(heads=2, dim=64, page=16, pages=4, device=-1, _ref=0)
+    q = torch.zeros((3, 4, 64), dtype=torch.float16)
+    for window in (2**32 + 5, 2**31, -2**31 - 1):
+        with pytest.raises(ValueError, match="window: .* 32 bits"):
+            pq.pq_paged_attention(q, Fake, i32(2, 4), i32(3), i32(2), 2, 9, window=window)
+        with pytest.raises(ValueError, match="window: .* 32 bits"):
+            pq.pq_attention_workspace_bytes(1, 300, 300, 4300, 32, 8, 128, window=window)
+    with pytest.raises(ValueError, match="page: .* 32 bits"):
+        pq.pq_block_tables(i32(2), i32(2), i32(2, 4), i32(5), i32(1), 2**32 + 16, 3)
+    with pytest.raises(ValueError, match="heads: .* 32 bits"):
+        pq.pq_attention_workspace_bytes(1, 300, 300, 4300, 2**32 + 32, 8, 128)
