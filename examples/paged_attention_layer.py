@@ -27,6 +27,7 @@ class PagedAttentionLayer:
     def __init__(self, heads: int, kv_heads: int, dim: int, requests: int, pages: int, width: int, page: int = 16,
                  cache: torch.dtype = torch.float16, seed: int = 0, device: str = "cuda:0"):
         self.heads, self.kv_heads, self.dim, self.device = heads, kv_heads, dim, device
+        self.sms = torch.cuda.get_device_properties(device).multi_processor_count
         hidden, kv = heads * dim, kv_heads * dim
         w = lambda n, k, s: torch.from_numpy(synth.weights(n, k, seed + s)).to(device)  # noqa: E731
         self.qkv = [(*pq.pq_pack_w8(w(n, hidden, i)), n) for i, n in enumerate((hidden, kv, kv))]
@@ -38,6 +39,7 @@ class PagedAttentionLayer:
         self.free_list = torch.arange(pages, dtype=torch.int32, device=device)   # pages are handed out in this order
         self.free_head = i32(1)
         self.lengths = [0] * requests      # the scheduler's own copy of kv_len: it chose the chunks
+        self.workspace = None              # of the attention; kept from step to step, made anew when a step wants more
 
     def project(self, x: torch.Tensor) -> list[torch.Tensor]:
         """x f16 [T, hidden] -> q [T, heads * dim], k, v [T, kv_heads * dim]."""
@@ -53,8 +55,10 @@ class PagedAttentionLayer:
         q, k, v = self.project(x)
         pq.pq_kv_append(self.cache, k, v, step.slots)
         max_q, max_kv = max(new), max(self.lengths)
-        workspace = pq.pq_attention_workspace(q.view(-1, self.heads, self.dim), self.cache, len(new), max_q, max_kv)
-        y = pq.pq_paged_attention(q, self.cache, self.table, step.q_start, step.kv_len, max_q, max_kv, workspace=workspace)
+        room = pq.pq_attention_workspace_bytes(len(new), x.shape[0], max_q, max_kv, self.heads, self.kv_heads, self.dim, self.sms)
+        if room > (0 if self.workspace is None else self.workspace.numel()):
+            self.workspace = pq.pq_workspace_init(torch.empty((room,), dtype=torch.uint8, device=self.device))
+        y = pq.pq_paged_attention(q, self.cache, self.table, step.q_start, step.kv_len, max_q, max_kv, workspace=self.workspace)
         self.kv_len, self.free_head = step.kv_len, step.free_head
         return pq.pq_linear_w8a8(y, *self.o, self.heads * self.dim)
 

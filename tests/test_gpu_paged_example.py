@@ -62,3 +62,19 @@ def test_the_example_runs_as_a_command():
     for cache in ("f16", "int8"):
         r = subprocess.run([sys.executable, example.__file__, "--cache", cache], capture_output=True, text=True, timeout=300)
         assert r.returncode == 0 and "status 0 finite True" in r.stdout, r.stdout + r.stderr
+
+
+def _inputs(new, seed):
+    return torch.from_numpy(synth.activations(sum(new), 512, seed=seed)).to(DEV)
+
+
+def test_the_workspace_is_kept_from_step_to_step():
+    layer = example.PagedAttentionLayer(8, 2, 64, 2, pages=130, page=16, width=64)
+    layer.step(_inputs([900, 100], 1), [900, 100])
+    seen = []
+    for i in range(12):
+        layer.step(_inputs([1, 1], 2 + i), [1, 1])
+        seen.append((layer.workspace.data_ptr(), layer.workspace.numel()))
+    sizes = [n for _, n in seen]
+    assert sizes == sorted(sizes) and len(set(seen)) == len(set(sizes)) <= 2
+    assert pq.pq_device_status() == 0
