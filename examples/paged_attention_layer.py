@@ -49,7 +49,12 @@ class PagedAttentionLayer:
         """x f16 [sum(new), hidden]: new[b] tokens of request b, one request after the other -> f16 of the same shape."""
         if sum(new) != x.shape[0] or len(new) != len(self.lengths):
             raise ValueError("new: one number of tokens per request, x their rows")
-        self.lengths = [a + b for a, b in zip(self.lengths, new)]
+        lengths = [a + b for a, b in zip(self.lengths, new)]
+        columns = [-(-n // self.cache.page) for n in lengths]
+        if max(columns) > self.table.shape[1] or sum(columns) > self.cache.pages:
+            raise ValueError(f"{sum(columns)} pages, {max(columns)} for one request: the cache has {self.cache.pages}, "
+                             f"a table row {self.table.shape[1]}")
+        self.lengths = lengths
         new_len = torch.tensor(new, dtype=torch.int32, device=self.device)
         step = pq.pq_block_tables(self.kv_len, new_len, self.table, self.free_list, self.free_head, self.cache.page, x.shape[0])
         q, k, v = self.project(x)

@@ -78,3 +78,14 @@ def test_the_workspace_is_kept_from_step_to_step():
     sizes = [n for _, n in seen]
     assert sizes == sorted(sizes) and len(set(seen)) == len(set(sizes)) <= 2
     assert pq.pq_device_status() == 0
+
+
+def test_a_step_that_the_pages_do_not_hold_is_refused():
+    layer = example.PagedAttentionLayer(8, 2, 64, 2, pages=6, page=16, width=4)
+    layer.step(_inputs([40, 10], 1), [40, 10])                   # 3 + 1 pages
+    for new in ([20, 30], [30, 1]):                              # 4 + 3 pages, 5 columns
+        with pytest.raises(ValueError, match="pages"):
+            layer.step(_inputs(new, 2), new)
+        assert layer.lengths == [40, 10]
+    y = layer.step(_inputs([20, 7], 3), [20, 7])                 # 4 + 2
+    assert torch.isfinite(y).all() and int(layer.free_head) == 6 and pq.pq_device_status() == 0
