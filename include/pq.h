@@ -409,7 +409,7 @@ PQ_API int pq_block_tables(const int32_t* kv_len, const int32_t* new_len, int64_
 
 /*
  * Writes the keys and values of `tokens` new tokens into the cache, token t at slots[t] (rows whose slot is
- * negative or beyond the cache are skipped; two rows with one slot leave either).  PQ_KV_INT8: every
+ * negative or beyond the cache are skipped; two rows with one slot leave a mixture of the two).  PQ_KV_INT8: every
  * (token, head) vector is quantized by the rule of pq_quantize_act (one scale over its `dim` values).
  *   k, v: FP16, row t at k + t * stride elements, heads * dim values each (stride >= heads * dim, a
  *   multiple of 8, so that slices of one wide q/k/v output serve as they are); 16-byte aligned.
@@ -430,8 +430,8 @@ PQ_API int pq_kv_read(const pq_kv_cache* cache, const int64_t* slots, int64_t to
  *   s_j = scale * sum_d q[d] k_j[d],  y = sum_j e^(s_j - max) v_j / sum_j e^(s_j - max)
  * for query head h over the key/value head h / (heads / cache->heads).  Scores, maxima and sums are FP32, and so is
  * the sum of the products with the values.  For that product the weights (PQ_KV_INT8: times their value's scale) are
- * rounded to FP16, relative to the largest that the row sees: 11 bits down to 2^-21 of it, half a step of 2^-32 of it
- * below.  A row that sees no key (kv_len shorter than the chunk, window or not) gives 0.
+ * rounded to FP16, relative to the largest that the row sees: to 11 bits down to 2^-21 of it, below that to within
+ * 2^-32 of it.  A row that sees no key (kv_len shorter than the chunk, window or not) gives 0.
  * A key that a row does not see does not reach it, whatever it holds, and nothing beyond kv_len or before
  * the window of a chunk's first row is used.  The VALUES in between are taken as finite: one that is infinite
  * or NaN also reaches rows of its request that do not see it (0 times it).

@@ -15,8 +15,9 @@ constexpr int rows_ctas(bool int8, int dim) { return int8 || dim == 64 ? 3 : 2; 
 template <bool kInt8, int D>
 struct RowCfg {
   // CTAs per SM and stages of a warp's ring.  INT8 and dim 64 have more arithmetic per byte and want the warps:
-  // 64 requests of up to 8192 tokens, INT8, dim 128: 162 us with three CTAs of two stages, 172 with two of three; dim
-  // 64: 104 and 128; FP16, dim 64 (drafts of 5): 67.6 and 69.7.  FP16, dim 128 is the other way: 212 and 209.
+  // 64 requests of up to 8192 tokens, INT8, dim 128: 127 us with three CTAs of two stages, 140 with two of three; dim
+  // 64: 87 and 99; FP16, dim 64 (drafts of 5): 67.4 and 69.5.  FP16, dim 128 is even for one token (206; 3 x 131072: 242
+  // and 247) and the other way for drafts of three, whose two tiles do not fit the registers: 173 and 166.
   static constexpr int kCtas = rows_ctas(kInt8, D), kStages = kCtas == 3 ? 2 : 3;
   static constexpr int kRowBytes = kInt8 ? D : 2 * D;
   static constexpr int kKeys = kStageBytes / (2 * kRowBytes);   // 16, 32 or 64
@@ -97,9 +98,9 @@ __device__ __forceinline__ uint32_t transposed(uint32_t v) {   // an 8 x 8 tile 
 // FP16 holds weights up to 2^15 (kTop), so that they keep their bits down to 2^-29 of the largest and count down to 2^-39:
 // 131072 keys of 2^-26 each are 0.2 % of a row, and with weights up to 1 they would be lost.
 //
-// Measured, 32 heads over 8 of 128, 64 requests of one token over up to 8192: FP16 208 us (6.7 TB/s, what a copy
-// reaches); INT8 130 us (5.5 TB/s): issue, 58 % of the slots, for the codes' conversion and the scales.  3 requests over
-// 131072: 247 us (6.5 TB/s).  1000 tokens of one request: 6.6 us, latency.
+// Measured, 32 heads over 8 of 128, 64 requests of one token over up to 8192: FP16 207 us (6.7 TB/s, what a copy
+// reaches); INT8 127 us (5.7 TB/s): issue, 62 % of the slots, for the codes' conversion and the scales.  3 requests over
+// 131072: 246 us (6.5 TB/s).  1000 tokens of one request: 6.6 us, INT8 6.2, latency.
 template <bool kInt8, int D, int kTiles>
 __global__ void __launch_bounds__(kWarps * 32, (RowCfg<kInt8, D>::kCtas)) attn_rows_kernel(const AttnArgs a) {
   using C = RowCfg<kInt8, D>;
@@ -510,10 +511,12 @@ int launch(const AttnArgs& a, const AttnPlan& plan, int64_t max_q, cudaStream_t 
 }  // namespace
 
 // How many keys a part gets.  `one`: what fills the resident CTAs exactly once.  Up to 1024 keys that is the choice
-// (the fewest dependent steps; 1000 tokens, 8 heads: 6.9 us with parts of 128, 12.3 without a split).  Beyond, several
-// waves of smaller parts even out: three where the units are few and long (3 x 131072 tokens: 239 us with parts of
-// 4096, 252 with 2048, 265 with one wave), six where there are many, of different lengths (64 requests of up to 8192:
-// 209 us with 2048, 219 with 4096, 225 with 512).
+// (the fewest dependent steps; 1000 tokens, 8 heads: 6.6 us with parts of 128, 9.1 with 512, 11.4 without a split).
+// Beyond, several waves of smaller parts even out: three where the units are few and long (3 x 131072 tokens, INT8:
+// 141 us with the parts of 2432 that the rule gives, 163 with 1024, 151 with 4096, 175 with one wave; FP16: 246 with 3584,
+// 258 with 1024 and 8192, but 237 with 4096 and 241 with one wave), six where there are many, of different lengths
+// (64 requests of up to 8192, FP16: 209 us with the 2816 that the rule gives and with 2048, 216 with 4096, 215 with 512,
+// 231 with one wave; INT8: 127 with the rule's 2176 and with 2048, 138 with 4096, 141 with 512, 155 with one wave).
 AttnPlan plan_attn_rows(int64_t requests, int64_t max_q, int64_t max_kv, int window, int kv_heads, int dim, bool int8, int sms, size_t room) {
   AttnPlan p;
   p.units = requests * kv_heads;

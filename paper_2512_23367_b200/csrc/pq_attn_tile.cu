@@ -17,7 +17,7 @@ struct TileCfg {
   static constexpr int kThreads = 640 + kConv;
   // Registers: softmax, issuer's warpgroup, converters.  512 x 104 + 128 x 64 = 640 x 96 and
   // 512 x 96 + 128 x 40 + 256 x 40 = 896 x 72, what the launch holds.  With 88 and 56
-  // for INT8 a chunk of 2048 over 18432 tokens took 734 us in place of 692.
+  // for INT8 six chunks of up to 700 over up to 5000 took 217 us in place of 211.
   static constexpr int kSoftRegs = kInt8 ? 96 : 104, kRestRegs = kInt8 ? 40 : 64, kConvRegs = 40;
   static constexpr int kRegsNeeded = kSoft * kSoftRegs + 128 * kRestRegs + kConv * kConvRegs;
   static constexpr int kTileBytes = kTile * D * 2;            // one operand tile: D / 64 panels of 128 rows x 128 B
@@ -326,7 +326,7 @@ __global__ void __launch_bounds__(kJoinThreads) attn_join_kernel(const AttnArgs 
 // 2048 and so do the exponentials (16 per cycle and SM).  Computing some of them by a polynomial gained nothing: the
 // softmax warps' issue slots are the scarcer.
 //
-// Measured, 32 heads over 8 of 128, FP16: a prompt of 4096 125 us (1.10 PFLOP/s); 2048 tokens over 16384, 540 us in a
+// Measured, 32 heads over 8 of 128, FP16: a prompt of 4096 125 us (1.10 PFLOP/s); 2048 tokens over 16384, 545 us in a
 // row (1.08 PFLOP/s, SMs at 1.62 GHz under the power cap), 461 in a short burst (1.27).  A unit takes 9 us beyond its
 // steps: requests' lengths, page ids, queries and first keys come one after the other out of global memory (8700 cycles up
 // to the first S), the results go back (4000), the next CTA starts (1300).
@@ -342,7 +342,7 @@ __global__ void __launch_bounds__(kJoinThreads) attn_join_kernel(const AttnArgs 
 // rounded: the power of two above the largest scale of its 32 keys goes into the exponent, the quotient of the two
 // multiplies.  The reference is the largest product of weight and value scale, up to 2^8, over the keys that the row
 // sees (a key that it does not see moves nothing), and FP16 weights keep their bits down to 2^-21 of that at least.
-// Six requests, chunks of up to 700 over up to 5000: 210 us (0.67 PFLOP/s), FP16 153; issue, 71 % of the slots: the
+// Six requests, chunks of up to 700 over up to 5000: 211 us (0.67 PFLOP/s), FP16 158; issue, 70 % of the slots: the
 // conversion is done again for every 256 rows, and each score takes two products more.
 template <bool kInt8, int D>
 __global__ void __launch_bounds__((TileCfg<kInt8, D>::kThreads), 1)
@@ -767,7 +767,7 @@ attn_tile_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constan
       };
       // INT8: no product of weight and value scale exceeds the largest product of codes times the largest key scale, in
       // powers of two, times the larger unit; as long as that does not move the reference, the keys' scales go into the
-      // exponents' FMA below (prompt of 4096: 177 to 170 us).
+      // exponents' FMA below (prompt of 4096: 182 us without, 165 with; 2048 over 18432: 755 and 677).
       bool exact = true;
       if constexpr (kInt8) {
         exact = edge || pair_any(pair, !(fmaf(fmaxf(largest(), 0.0f), sct[3 * kTile + 4], static_cast<float>(max(unit_log[0], unit_log[1]))) <= m + 8.0f));
@@ -1004,8 +1004,8 @@ int launch(TileArgs& t, const TilePlan& plan, cudaStream_t stream) {
 // Units run on the SMs in waves.  Those of the last, incomplete wave (of the only one, where there are fewer units than
 // SMs) have their keys cut into as many parts, of 384 keys or more, as the sum below is least for, counted in steps of 128
 // keys: every CTA takes 6 steps more than its keys do, every part 0.04 to be joined, the joining kernel 4.
-// (32 heads over 8 of 128, FP16: 1220 tokens over 12176, 160 units, 240 us, 329 with all of them whole; 64 tokens over
-// 8000, 8 units in 17 parts, 25 us, 300 tokens of two requests over 3000, 80 units in 3, 50, 58 whole.)
+// (32 heads over 8 of 128, FP16: 1220 tokens over 12176, the last 12 of 160 units in 11 parts, 202 us, 303 with all of
+// them whole; 64 tokens over 8064, 8 units in 13 parts, 25 and 105; 512 over 8704, 64 units in 3, 79 and 115.)
 TilePlan plan_attn_tile(int64_t requests, int64_t tokens, int64_t max_q, int64_t max_kv, int window, int group, int kv_heads,
                         int dim, int sms, size_t room) {
   TilePlan p;
