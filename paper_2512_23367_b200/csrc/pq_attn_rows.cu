@@ -91,7 +91,7 @@ __device__ __forceinline__ uint32_t transposed(uint32_t v) {   // an 8 x 8 tile 
 // INT8: the codes go to the tensor cores as FP16 (exact).  The key's scale multiplies the score.  The value's scale is
 // split into 2^e and a rest in [1, 2); e is added to the score in powers of two, x, and the running maximum is that of
 // x + e over the keys that the row sees: the FP16 weight, 2^(x + e - max + 14) times the rest, then stays below 2^15 and
-// keeps its bits down to 2^-29 of the row's largest product of weight and scale, whatever the scales are.  The sum of the
+// keeps its bits down to 2^-28 of the row's largest product of weight and scale, whatever the scales are.  The sum of the
 // weights, FP32, takes 2^(x + e - max + 14) times 2^-e.  The feature order of a matrix step is permuted so that a lane's codes
 // are 16 consecutive bytes; queries (and the result's rows) are permuted alike.
 //
