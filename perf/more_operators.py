@@ -332,8 +332,9 @@ def run(s):
             return pq.pq_latent_append(s["cache"], s["c"], s["k_rope"], s["slots"], s["pos"], s["rotary"], q=s["q"], out=s["out"]), s["data"]
         q = pq.pq_kv_append_rotated(s["cache"], s["new_k"], s["new_v"], s["slots"], s["pos"], s["rotary"], q=s["q"], out=s["out"])
         return (q, s["k"], s["v"]) if case["cache"] == "f16" else (q, *pq.pq_kv_read(s["cache"], s["slots"]))
-    if op == "latent" and "cache" not in s:
-        s["cache"], s["workspace"] = pq.LatentKV(s["data"]), pq.pq_latent_workspace(DEV)
+    if op in ("latent", "expanded") and "workspace" not in s:
+        s["workspace"] = pq.pq_latent_workspace(DEV)
+        s["cache"] = pq.LatentKV(s["data"]) if op == "latent" else None
     if "out" not in s:
         x = s["x"] if "x" in s else s["q"]
         wide = {"rotate": case.get("width"), "absorb": case.get("out"), "latent": case.get("latent"), "expanded": VALUE}[op]
@@ -345,7 +346,8 @@ def run(s):
     if op == "latent":
         return pq.pq_latent_attention(s["q"], s["cache"], s["table"], s["q_start"], s["kv_len"], s["scale"], out=s["out"],
                                       workspace=s["workspace"])
-    return pq.pq_expanded_attention(s["q"], s["kv"], s["k_rope"], s["q_start"], s["kv_start"], s["max_q"], s["scale"], out=s["out"])
+    return pq.pq_expanded_attention(s["q"], s["kv"], s["k_rope"], s["q_start"], s["kv_start"], s["max_q"], s["scale"], out=s["out"],
+                                    workspace=s["workspace"])
 
 
 def _exact_turned(x, pos, case):
