@@ -462,6 +462,156 @@ PQ_API size_t pq_attention_workspace_bytes_window(int64_t requests, int64_t toke
                                                   int32_t heads, int32_t kv_heads, int32_t dim, int32_t sms,
                                                   int32_t window);
 
+/* ------------------------------------------------------------------------------------------------
+ * Rotary positions.  The first `dim` values of every head of a row at position p are turned pair by pair; pair i,
+ * 0 <= i < dim / 2, by p * freq[i] turns:
+ *   (a, b) -> amplitude * (a cos - b sin, b cos + a sin)
+ * with (a, b) the values i and i + dim / 2 (PQ_ROTARY_HALF) or 2 i and 2 i + 1 (PQ_ROTARY_PAIRS).  The values behind
+ * the first `dim` are left as they are.  Angles are exact modulo a turn at every 32-bit position (negative ones turn
+ * backwards); cosines, sines and products are FP32, and an FP16 result is rounded once.
+ *   freq: DEVICE array [dim / 2], turns per position in units of 2^-64, 8-byte aligned; a constant of the model
+ *   dim a multiple of 16, 16 .. 256; 2^-16 <= amplitude <= 2^16
+ */
+#define PQ_ROTARY_HALF 0
+#define PQ_ROTARY_PAIRS 1
+typedef struct {
+  const uint64_t* freq;
+  int32_t dim;
+  int32_t layout;
+  float amplitude;
+} pq_rotary;
+
+/*
+ * Host-only (touches no device): the frequencies and the amplitude of a rotation.  Pair i makes base^(-2 i / dim)
+ * radians per position, which `scaling` stretches by `factor` >= 1 for contexts beyond the `original` length:
+ *   PQ_ROTARY_PLAIN   not at all
+ *   PQ_ROTARY_LINEAR  all pairs by `factor`
+ *   PQ_ROTARY_BASE    through the base: base * factor^(dim / (dim - 2))
+ *   PQ_ROTARY_BANDS   pairs that make fewer than `low` turns over `original` positions by `factor`, those that make more
+ *                     than `high` not, linearly in the pair's index in between; amplitude 0.1 ln(factor) + 1
+ *   PQ_ROTARY_WAVES   the same by original / wavelength, linearly in it between `low` and `high`; amplitude 1
+ * freq: HOST array [dim / 2], amplitude: one host float (1 but for BANDS).  Arguments that a scaling does not name are not
+ * looked at; base > 1, 0 < low < high, original >= 1 (else PQ_ERR_SHAPE).
+ */
+#define PQ_ROTARY_PLAIN 0
+#define PQ_ROTARY_LINEAR 1
+#define PQ_ROTARY_BASE 2
+#define PQ_ROTARY_BANDS 3
+#define PQ_ROTARY_WAVES 4
+PQ_API int pq_rotary_frequencies(int32_t dim, double base, int32_t scaling, double factor, double original, double low,
+                                 double high, uint64_t* freq, float* amplitude);
+
+/*
+ * Rows of heads turned by their positions: head h of row t is `width` values at x + t * x_stride + h * x_head_stride and
+ * goes to out + t * out_stride + h * out_head_stride (elements; FP16).
+ *   width a multiple of 16, rotary->dim .. 1024; 1 <= heads <= 1024; strides multiples of 8, head strides >= width (with
+ *   one head not looked at), out_stride >= width; 16-byte aligned.  out may be x with the same strides (in place), and may
+ *   not overlap it otherwise.
+ *   pos i32 [tokens]
+ */
+PQ_API int pq_rotate(const pq_rotary* rotary, const void* x_f16, int64_t x_stride, int64_t x_head_stride, int32_t heads,
+                     int32_t width, const int32_t* pos, int64_t tokens, void* out_f16, int64_t out_stride,
+                     int64_t out_head_stride, void* stream);
+
+/*
+ * pq_kv_append with the keys turned on the way, and the step's queries beside them, in one launch.  Keys are turned
+ * over the first rotary->dim <= cache->dim values of a head; PQ_KV_INT8 quantizes the turned FP32 values.
+ *   k, v, slots, tokens: as for pq_kv_append;  pos i32 [tokens]
+ *   q: q_heads heads of cache->dim values per row, out: the same turned, both as for pq_rotate (q_heads 0: no queries, the
+ *   pointers and strides are not looked at).  Queries are turned whatever their row's slot is.
+ */
+PQ_API int pq_kv_append_rotated(const pq_kv_cache* cache, const pq_rotary* rotary, const void* k_f16, int64_t k_stride,
+                                const void* v_f16, int64_t v_stride, const int64_t* slots, const int32_t* pos,
+                                int64_t tokens, const void* q_f16, int64_t q_stride, int64_t q_head_stride,
+                                int32_t q_heads, void* out_f16, int64_t out_stride, int64_t out_head_stride, void* stream);
+
+/* ------------------------------------------------------------------------------------------------
+ * Latent attention: keys and values of all heads come from one latent vector a token, beside one rotary key of
+ * PQ_LATENT_ROPE values that all heads share.  The cache holds a token's latent vector with its turned rotary key:
+ *   data [pages, page, latent + PQ_LATENT_ROPE]  FP16
+ * Slots and block tables are those of the paged key/value cache.  Rules (else PQ_ERR_SHAPE): latent 256 or 512; page a
+ * multiple of 16, at most 1024; pages >= 1, pages * page < 2^31.
+ */
+#define PQ_LATENT_ROPE 64
+typedef struct {
+  void* data;
+  int64_t pages;
+  int32_t page;
+  int32_t latent;
+} pq_latent_cache;
+
+/*
+ * Writes the latent vectors and, turned by their positions, the rotary keys of `tokens` new tokens into the cache, token t
+ * at slots[t] (rows whose slot is negative or beyond the cache are skipped; of two rows with one slot a mixture is
+ * left), and turns the rotary part of the step's queries, in one launch.
+ *   c: FP16, row t at c + t * c_stride (>= latent);  k_rope: FP16, row t at k_rope + t * k_rope_stride (>=
+ *   PQ_LATENT_ROPE); strides multiples of 8, 16-byte aligned: slices of one linear's output serve as they are
+ *   rotary->dim <= PQ_LATENT_ROPE;  slots i64, pos i32 [tokens]
+ *   q, out: as for pq_kv_append_rotated, with heads of PQ_LATENT_ROPE values
+ */
+PQ_API int pq_latent_append(const pq_latent_cache* cache, const pq_rotary* rotary, const void* c_f16, int64_t c_stride,
+                            const void* k_rope_f16, int64_t k_rope_stride, const int64_t* slots, const int32_t* pos,
+                            int64_t tokens, const void* q_f16, int64_t q_stride, int64_t q_head_stride, int32_t q_heads,
+                            void* out_f16, int64_t out_stride, int64_t out_head_stride, void* stream);
+
+/* The reverse: latent vectors [tokens, latent] and turned rotary keys [tokens, PQ_LATENT_ROPE] at `slots`, dense (zeros
+ * where a slot is negative or beyond the cache): what the expanded form multiplies out for tokens of earlier steps. */
+PQ_API int pq_latent_read(const pq_latent_cache* cache, const int64_t* slots, int64_t tokens, void* c_f16, void* k_rope_f16,
+                          void* stream);
+
+/*
+ * One matrix per head: y[t, h, :] = W[h] x[t, h, :], the products that take queries into the latent space (K values of a
+ * head to N = latent) and results out of it (K = latent).  FP16 in and out, FP32 sums.
+ *   x: head h of row t is K values at x + t * x_stride + h * x_head_stride;  w: dense [heads, N, K];
+ *   y: N values at y + t * y_stride + h * y_head_stride
+ *   K a multiple of 64 up to 512, N a multiple of 128 up to 1024, 1 <= heads <= 1024; strides as for pq_rotate, with K and
+ *   N for the widths; y may not overlap x.  Weights are constants of the model, read ahead of the wait as in pq_gemm_w8a8.
+ */
+PQ_API int pq_head_linear(const void* x_f16, int64_t x_stride, int64_t x_head_stride, const void* w_f16, int32_t heads, int64_t N,
+                          int64_t K, int64_t tokens, void* y_f16, int64_t y_stride, int64_t y_head_stride, void* stream);
+
+/*
+ * Latent attention, absorbed form: the step's queries in the latent space over the paged latent cache, which already holds
+ * their own tokens.  Row t, head h of request b, with n = q_start[b + 1] - q_start[b] rows and L = kv_len[b] cached
+ * tokens, stands at position p = L - n + (t - q_start[b]) and sees the tokens 0 <= j <= p:
+ *   s_j = scale * q . data_j (latent + PQ_LATENT_ROPE values),  y = sum_j e^(s_j - max) data_j[: latent] / sum_j e^(s_j - max)
+ * Precision, rows that see nothing (0), unusable page ids (zeros) and vectors that are not finite: as for
+ * pq_paged_attention, the data taking the values' place.
+ *   q: FP16 [tokens, heads, latent + PQ_LATENT_ROPE] dense;  out: FP16 [tokens, heads, latent] dense.  Rows outside every
+ *     request are left as they are.  1 <= heads <= 1024, tokens * heads < 2^31; scale finite.
+ *   block_table i32 [requests, width], q_start i32 [requests + 1], kv_len i32 [requests]: as for pq_paged_attention
+ *   workspace: as for pq_gemm_w8a8; partial results of tokens that are split over several SMs, joined in a fixed order.
+ *     The schedule is made on the GPU from the lengths.  Without a workspace, or with less than
+ *     pq_latent_workspace_bytes, the tokens of a request are not split.
+ * pq_latent_workspace_bytes: host-only; what every call of pq_latent_attention and pq_expanded_attention wants on a GPU
+ *   with `sms` multiprocessors, whatever the sizes (0: sms < 1).
+ */
+PQ_API int pq_latent_attention(const void* q_f16, int32_t heads, const pq_latent_cache* cache, const int32_t* block_table,
+                               int64_t width, const int32_t* q_start, const int32_t* kv_len, int64_t requests, int64_t tokens,
+                               float scale, void* out_f16, void* workspace, size_t workspace_bytes, void* stream);
+PQ_API size_t pq_latent_workspace_bytes(int32_t sms);
+
+/*
+ * Latent attention, expanded form: ragged queries over keys and values that have been multiplied out per head, as one
+ * linear over the latent vectors gives them, beside the shared rotary key.  Row t of request b, with n = q_start[b + 1] -
+ * q_start[b] rows and L = kv_start[b + 1] - kv_start[b] keys, stands at position p = L - n + (t - q_start[b]) and sees
+ * the request's keys 0 <= j <= p; head h:
+ *   s_j = scale * (q[: 128] . kv[j, h, : 128] + q[128 :] . k_rope[j]),  y = sum_j e^(s_j - max) kv[j, h, 128 :] / sum_j e^(s_j - max)
+ * Precision, rows that see nothing (0) and values that are not finite: as for pq_paged_attention.
+ *   q: FP16, row t at q + t * q_stride, heads * (128 + PQ_LATENT_ROPE) values (the rotary part last, turned)
+ *   kv: FP16, row j at kv + j * kv_stride, heads * (128 + 128) values: a head's key, then its value
+ *   k_rope: FP16, row j at k_rope + j * k_rope_stride, PQ_LATENT_ROPE values;  keys: rows of kv and k_rope
+ *   strides multiples of 8 and >= the row; 16-byte aligned
+ *   q_start, kv_start i32 [requests + 1] within tokens and keys;  max_q: a bound of the rows of any request (a request
+ *     with more leaves outputs unspecified)
+ *   workspace: as for pq_latent_attention
+ *   out: FP16 [tokens, heads, 128] dense.  Rows outside every request are left as they are.  1 <= heads <= 1024.
+ */
+PQ_API int pq_expanded_attention(const void* q_f16, int64_t q_stride, int32_t heads, const void* kv_f16, int64_t kv_stride,
+                                 const void* k_rope_f16, int64_t k_rope_stride, int64_t keys, const int32_t* q_start,
+                                 const int32_t* kv_start, int64_t requests, int64_t tokens, int64_t max_q, float scale,
+                                 void* out_f16, void* workspace, size_t workspace_bytes, void* stream);
+
 /*
  * Reads the device status word of the current device into *host_status (PQ_OK or
  * PQ_ERR_TIMEOUT) and clears it.  Synchronizes the device; call it outside timed

@@ -14,7 +14,7 @@ GROUP = 128
 
 _lib = None
 
-_i64, _i32, _vp = ctypes.c_int64, ctypes.c_int32, ctypes.c_void_p
+_i64, _i32, _vp, _f64 = ctypes.c_int64, ctypes.c_int32, ctypes.c_void_p, ctypes.c_double
 
 # name -> (restype, argtypes); mirrors include/pq.h
 SIGNATURES = {
@@ -63,6 +63,17 @@ SIGNATURES = {
     "pq_paged_attention": (ctypes.c_int, [_vp, _i64, _i32, _vp, _vp, _i64, _vp, _vp, _i64, _i64, _i64, _i64,
                                           ctypes.c_float, _i32, _vp, _vp, ctypes.c_size_t, _vp]),
     "pq_attention_workspace_bytes": (ctypes.c_size_t, [_i64, _i64, _i64, _i64, _i32, _i32, _i32, _i32]),
+    "pq_rotary_frequencies": (ctypes.c_int, [_i32, _f64, _i32, _f64, _f64, _f64, _f64, _vp, _vp]),
+    "pq_rotate": (ctypes.c_int, [_vp, _vp, _i64, _i64, _i32, _i32, _vp, _i64, _vp, _i64, _i64, _vp]),
+    "pq_kv_append_rotated": (ctypes.c_int, [_vp, _vp, _vp, _i64, _vp, _i64, _vp, _vp, _i64, _vp, _i64, _i64, _i32, _vp, _i64, _i64, _vp]),
+    "pq_latent_append": (ctypes.c_int, [_vp, _vp, _vp, _i64, _vp, _i64, _vp, _vp, _i64, _vp, _i64, _i64, _i32, _vp, _i64, _i64, _vp]),
+    "pq_latent_read": (ctypes.c_int, [_vp, _vp, _i64, _vp, _vp, _vp]),
+    "pq_head_linear": (ctypes.c_int, [_vp, _i64, _i64, _vp, _i32, _i64, _i64, _i64, _vp, _i64, _i64, _vp]),
+    "pq_latent_attention": (ctypes.c_int, [_vp, _i32, _vp, _vp, _i64, _vp, _vp, _i64, _i64, ctypes.c_float, _vp, _vp,
+                                           ctypes.c_size_t, _vp]),
+    "pq_latent_workspace_bytes": (ctypes.c_size_t, [_i32]),
+    "pq_expanded_attention": (ctypes.c_int, [_vp, _i64, _i32, _vp, _i64, _vp, _i64, _i64, _vp, _vp, _i64, _i64, _i64,
+                                             ctypes.c_float, _vp, _vp, ctypes.c_size_t, _vp]),
     "pq_attention_workspace_bytes_window": (ctypes.c_size_t, [_i64, _i64, _i64, _i64, _i32, _i32, _i32, _i32, _i32]),
 }
 MAX_GROUP = 4
@@ -744,6 +755,273 @@ def pq_paged_attention(q: torch.Tensor, cache: PagedKV, block_table: torch.Tenso
     _check("pq_paged_attention", lib().pq_paged_attention(
         q.data_ptr(), qs, H, cache._ref, block_table.data_ptr(), width, q_start.data_ptr(), kv_len.data_ptr(), B, T,
         max_q, max_kv, cache.dim ** -0.5 if scale is None else scale, window, out.data_ptr(), ws, ws_bytes, _stream()))
+    return out
+
+
+# ---- rotary positions and latent attention ---------------------------------------------------------------
+
+LATENT_ROPE = 64   # rotary values of a head of latent attention
+NOPE = VALUE = 128   # of the expanded form: the other values of a query or key, values
+
+
+class _Rotary(ctypes.Structure):   # pq_rotary of include/pq.h
+    _fields_ = [("freq", _vp), ("dim", _i32), ("layout", _i32), ("amplitude", ctypes.c_float)]
+
+
+class _LatentCache(ctypes.Structure):   # pq_latent_cache
+    _fields_ = [("data", _vp), ("pages", _i64), ("page", _i32), ("latent", _i32)]
+
+
+class Rotary:
+    """Frequencies of rotary positions over the first `dim` values of a head, made once for a model and kept on `device`.
+    layout: "half" turns the values i and i + dim / 2 together, "pairs" 2 i and 2 i + 1.  scaling stretches them by
+    `factor` for contexts beyond the `original` length: "none", "linear" (all), "base" (through the base), "bands" (by
+    the turns of a pair over the original length, between `low` and `high` in its index) or "waves" (between `low` and `high`
+    in original / wavelength).  amplitude multiplies cosines and sines (default: as the scaling has it)."""
+
+    LAYOUTS = {"half": 0, "pairs": 1}
+    SCALINGS = {"none": 0, "linear": 1, "base": 2, "bands": 3, "waves": 4}
+    __slots__ = ("dim", "layout", "amplitude", "freq", "device", "_struct", "_ref")
+
+    def __init__(self, dim: int, base: float = 10000.0, layout: str = "half", scaling: str = "none", factor: float = 1.0,
+                 original: float = 0.0, low: float = 1.0, high: float = 32.0, amplitude: float | None = None, device="cuda"):
+        _in_32_bits(dim=dim)
+        if layout not in self.LAYOUTS:
+            raise ValueError(f"layout: expected one of {list(self.LAYOUTS)}, got {layout!r}")
+        if scaling not in self.SCALINGS:
+            raise ValueError(f"scaling: expected one of {list(self.SCALINGS)}, got {scaling!r}")
+        host, own = (ctypes.c_int64 * max(dim // 2, 1))(), ctypes.c_float()
+        _check("pq_rotary_frequencies", lib().pq_rotary_frequencies(dim, base, self.SCALINGS[scaling], factor, original, low, high,
+                                                                    ctypes.addressof(host), ctypes.addressof(own)))
+        freq = torch.tensor(list(host), dtype=torch.int64).to(device)
+        if not freq.is_cuda:
+            raise ValueError("expected CUDA tensors (this library has no CPU path)")
+        put = object.__setattr__
+        put(self, "dim", dim), put(self, "layout", layout), put(self, "freq", freq), put(self, "device", freq.get_device())
+        put(self, "amplitude", own.value if amplitude is None else amplitude)
+        put(self, "_struct", _Rotary(freq.data_ptr(), dim, self.LAYOUTS[layout], self.amplitude))
+        put(self, "_ref", ctypes.addressof(self._struct))
+
+    def __setattr__(self, name, value):
+        raise AttributeError("a Rotary is fixed; make another one")
+
+
+class LatentKV:
+    """A paged cache of latent vectors and turned rotary keys: data f16 [pages, page, latent + 64].  Measures its tensor
+    once and keeps it; page a multiple of 16, latent 256 or 512."""
+
+    __slots__ = ("data", "pages", "page", "latent", "device", "_struct", "_ref")
+
+    def __init__(self, data: torch.Tensor):
+        if data.dim() != 3:
+            raise ValueError("data: expected a 3-D tensor [pages, page, latent + 64]")
+        pages, page, wide = data.shape
+        _sized(data, torch.float16, data.numel(), "data")
+        if wide - LATENT_ROPE not in (256, 512):
+            raise ValueError(f"data: expected 256 + {LATENT_ROPE} or 512 + {LATENT_ROPE} values a token, got {wide}")
+        _together(data)
+        put = object.__setattr__
+        put(self, "data", data), put(self, "pages", pages), put(self, "page", page), put(self, "latent", wide - LATENT_ROPE)
+        put(self, "device", data.get_device())
+        put(self, "_struct", _LatentCache(data.data_ptr(), pages, page, wide - LATENT_ROPE))
+        put(self, "_ref", ctypes.addressof(self._struct))
+
+    def __setattr__(self, name, value):
+        raise AttributeError("a LatentKV is fixed; make another one over another tensor")
+
+    @classmethod
+    def empty(cls, pages: int, page: int, latent: int = 512, device="cuda"):
+        """A zero-filled cache."""
+        return cls(torch.zeros((pages, page, latent + LATENT_ROPE), dtype=torch.float16, device=device))
+
+
+def _head_rows(x: torch.Tensor, heads: int | None, dim: int | None, what: str) -> tuple[int, int, int, int, int]:
+    """f16 [T, heads, dim], a head's values dense, rows and heads any distance apart.  Returns (T, heads, dim, row stride,
+    head stride) in elements."""
+    if x.dtype != torch.float16:
+        raise TypeError(f"{what}: expected torch.float16, got {x.dtype}")
+    if x.dim() != 3 or (heads is not None and x.shape[1] != heads) or (dim is not None and x.shape[2] != dim) or x.stride(2) != 1:
+        raise ValueError(f"{what}: expected [rows, {'heads' if heads is None else heads}, {'values' if dim is None else dim}] "
+                         "with the values of a head contiguous")
+    T, H, D = x.shape
+    hs = x.stride(1) if H > 1 else D
+    return T, H, D, (x.stride(0) if T > 1 else H * hs), hs
+
+
+def _strided_rows(x: torch.Tensor, width: int, what: str) -> tuple[int, int]:
+    """f16 [T, ...] with `width` values per row, dense inside a row.  Returns (T, row stride)."""
+    if x.dtype != torch.float16:
+        raise TypeError(f"{what}: expected torch.float16, got {x.dtype}")
+    if x.dim() < 2 or x[:1].numel() != (width if x.shape[0] else 0) or (x.shape[0] and not x[0].is_contiguous()):
+        raise ValueError(f"{what}: expected rows of {width} contiguous values")
+    return x.shape[0], (x.stride(0) if x.shape[0] > 1 else width)
+
+
+def _on(device: int, **tensors) -> None:
+    for name, x in tensors.items():
+        if x is not None and x.get_device() != device:
+            raise ValueError(f"{name}: on {x.device}, other operands on cuda:{device}")
+
+
+def _outputs_for(q: torch.Tensor, out: torch.Tensor | None, heads: int, dim: int) -> tuple[torch.Tensor, int, int]:
+    if out is None:
+        out = torch.empty((q.shape[0], heads, dim), dtype=torch.float16, device=q.device)
+    T, _, _, os, ohs = _head_rows(out, heads, dim, "out")
+    if T != q.shape[0]:
+        raise ValueError(f"out: expected {q.shape[0]} rows, got {T}")
+    return out, os, ohs
+
+
+def pq_rotate(x: torch.Tensor, pos: torch.Tensor, rotary: Rotary, out: torch.Tensor | None = None) -> torch.Tensor:
+    """Rows x f16 [T, heads, width] turned by their positions i32 [T] over the first rotary.dim values of each head -> out
+    f16 of the same shape.  Rows and heads may be slices of wider tensors; out may be x itself (in place)."""
+    T, H, D, xs, xhs = _head_rows(x, None, None, "x")
+    out, os, ohs = _outputs_for(x, out, H, D)
+    _operands(rotary.device, (pos, torch.int32, T, "pos"))
+    _on(rotary.device, x=x, out=out)
+    _check("pq_rotate", lib().pq_rotate(rotary._ref, x.data_ptr(), xs, xhs, H, D, pos.data_ptr(), T, out.data_ptr(), os, ohs, _stream()))
+    return out
+
+
+def _queries(q, out, T: int, dim: int):
+    """The optional queries of an append: (out, pointer, strides, heads, pointer, strides)."""
+    if q is None:
+        if out is not None:
+            raise ValueError("out: there are no queries")
+        return None, (None, 0, 0, 0, None, 0, 0)
+    Tq, H, _, qs, qhs = _head_rows(q, None, dim, "q")
+    if Tq != T:
+        raise ValueError(f"q: expected {T} rows, got {Tq}")
+    out, os, ohs = _outputs_for(q, out, H, dim)
+    return out, (q.data_ptr(), qs, qhs, H, out.data_ptr(), os, ohs)
+
+
+def pq_kv_append_rotated(cache: PagedKV, k: torch.Tensor, v: torch.Tensor, slots: torch.Tensor, pos: torch.Tensor, rotary: Rotary,
+                         q: torch.Tensor | None = None, out: torch.Tensor | None = None) -> torch.Tensor | None:
+    """pq_kv_append with the keys turned by pos i32 [T] on the way; q f16 [T, heads, dim], where given, is turned beside them
+    into out (which may be q) and returned."""
+    T, _, ks = _token_rows(k, cache.heads, cache.dim, "k")
+    Tv, _, vs = _token_rows(v, cache.heads, cache.dim, "v")
+    if Tv != T:
+        raise ValueError(f"v: expected {T} rows, got {Tv}")
+    out, queries = _queries(q, out, T, cache.dim)
+    _operands(cache.device, (slots, torch.int64, T, "slots"), (pos, torch.int32, T, "pos"), (rotary.freq, torch.int64, rotary.dim // 2, "rotary"))
+    _on(cache.device, k=k, v=v, q=q, out=out)
+    _check("pq_kv_append_rotated", lib().pq_kv_append_rotated(cache._ref, rotary._ref, k.data_ptr(), ks, v.data_ptr(), vs, slots.data_ptr(),
+                                                              pos.data_ptr(), T, *queries, _stream()))
+    return out
+
+
+def pq_latent_append(cache: LatentKV, c: torch.Tensor, k_rope: torch.Tensor, slots: torch.Tensor, pos: torch.Tensor, rotary: Rotary,
+                     q: torch.Tensor | None = None, out: torch.Tensor | None = None) -> torch.Tensor | None:
+    """Writes c f16 [T, latent] and, turned by pos i32 [T], k_rope f16 [T, 64] into the cache at slots i64 [T]; rows with a
+    negative slot are skipped.  q f16 [T, heads, 64], where given, is turned beside them into out (which may be q, or
+    the end of the latent queries' heads) and returned."""
+    T, cs = _strided_rows(c, cache.latent, "c")
+    Tk, ks = _strided_rows(k_rope, LATENT_ROPE, "k_rope")
+    if Tk != T:
+        raise ValueError(f"k_rope: expected {T} rows, got {Tk}")
+    out, queries = _queries(q, out, T, LATENT_ROPE)
+    _operands(cache.device, (slots, torch.int64, T, "slots"), (pos, torch.int32, T, "pos"), (rotary.freq, torch.int64, rotary.dim // 2, "rotary"))
+    _on(cache.device, c=c, k_rope=k_rope, q=q, out=out)
+    _check("pq_latent_append", lib().pq_latent_append(cache._ref, rotary._ref, c.data_ptr(), cs, k_rope.data_ptr(), ks, slots.data_ptr(),
+                                                      pos.data_ptr(), T, *queries, _stream()))
+    return out
+
+
+def pq_latent_read(cache: LatentKV, slots: torch.Tensor) -> tuple[torch.Tensor, torch.Tensor]:
+    """Latent vectors f16 [T, latent] and turned rotary keys f16 [T, 64] at slots i64 [T]; zeros where a slot is outside the
+    cache."""
+    T = slots.numel()
+    _operands(cache.device, (slots, torch.int64, T, "slots"))
+    c, k = (torch.empty((T, n), dtype=torch.float16, device=slots.device) for n in (cache.latent, LATENT_ROPE))
+    _check("pq_latent_read", lib().pq_latent_read(cache._ref, slots.data_ptr(), T, c.data_ptr(), k.data_ptr(), _stream()))
+    return c, k
+
+
+def pq_head_linear(x: torch.Tensor, w: torch.Tensor, out: torch.Tensor | None = None) -> torch.Tensor:
+    """One matrix per head: x f16 [T, heads, K], w f16 [heads, N, K] -> out f16 [T, heads, N], out[t, h] = w[h] x[t, h].  Rows and
+    heads of x and out may be slices of wider tensors."""
+    T, H, K, xs, xhs = _head_rows(x, None, None, "x")
+    if w.dim() != 3:
+        raise ValueError("w: expected a 3-D tensor [heads, N, K]")
+    N = w.shape[1]
+    _sized(w, torch.float16, H * N * K, "w")
+    if w.shape != (H, N, K):
+        raise ValueError(f"w: expected [{H}, N, {K}], got {tuple(w.shape)}")
+    out, os, ohs = _outputs_for(x, out, H, N)
+    _operands(w.get_device())
+    _on(w.get_device(), x=x, out=out)
+    _check("pq_head_linear", lib().pq_head_linear(x.data_ptr(), xs, xhs, w.data_ptr(), H, N, K, T, out.data_ptr(), os, ohs, _stream()))
+    return out
+
+
+def pq_latent_workspace(device="cuda") -> torch.Tensor:
+    """A prepared workspace for pq_latent_attention and pq_expanded_attention, of any sizes, on `device`."""
+    n = int(lib().pq_latent_workspace_bytes(torch.cuda.get_device_properties(device).multi_processor_count))
+    return pq_workspace_init(torch.empty((n,), dtype=torch.uint8, device=device))
+
+
+def _workspace_check(workspace: torch.Tensor | None):
+    """(pointer, bytes, operand checks) of an optional workspace."""
+    if workspace is None:
+        return None, 0, ()
+    return workspace.data_ptr(), workspace.numel(), ((workspace, torch.uint8, workspace.numel(), "workspace"),)
+
+
+def pq_latent_attention(q: torch.Tensor, cache: LatentKV, block_table: torch.Tensor, q_start: torch.Tensor, kv_len: torch.Tensor,
+                        scale: float, out: torch.Tensor | None = None, workspace: torch.Tensor | None = None) -> torch.Tensor:
+    """Latent attention, absorbed form, of a step's tokens over the paged latent cache that already holds them.  q f16
+    [T, heads, latent + 64], dense, the turned rotary part last -> out f16 [T, heads, latent].  block_table i32
+    [requests, width], q_start i32 [requests + 1], kv_len i32 [requests] (with the step's own tokens); workspace: from
+    pq_latent_workspace (without it the tokens of a request are not split)."""
+    if q.dim() != 3:
+        raise ValueError("q: expected a 3-D tensor [rows, heads, latent + 64]")
+    T, H, _ = q.shape
+    B = kv_len.numel()
+    if block_table.dim() != 2:
+        raise ValueError("block_table: expected a 2-D tensor [requests, width]")
+    width = block_table.shape[1]
+    checks = ((q, torch.float16, T * H * (cache.latent + LATENT_ROPE), "q"), (block_table, torch.int32, B * width, "block_table"),
+              (q_start, torch.int32, B + 1, "q_start"), (kv_len, torch.int32, B, "kv_len"))
+    if out is not None:
+        checks += ((out, torch.float16, T * H * cache.latent, "out"),)
+    ws, ws_bytes, more = _workspace_check(workspace)
+    _operands(cache.device, *checks, *more)
+    if out is None:
+        out = torch.empty((T, H, cache.latent), dtype=torch.float16, device=q.device)
+    _check("pq_latent_attention", lib().pq_latent_attention(q.data_ptr(), H, cache._ref, block_table.data_ptr(), width, q_start.data_ptr(),
+                                                            kv_len.data_ptr(), B, T, scale, out.data_ptr(), ws, ws_bytes, _stream()))
+    return out
+
+
+def pq_expanded_attention(q: torch.Tensor, kv: torch.Tensor, k_rope: torch.Tensor, q_start: torch.Tensor, kv_start: torch.Tensor,
+                          max_q: int, scale: float, out: torch.Tensor | None = None, workspace: torch.Tensor | None = None) -> torch.Tensor:
+    """Latent attention, expanded form: ragged queries q f16 [T, heads, 128 + 64] (the turned rotary part last) over keys and
+    values kv f16 [S, heads, 128 + 128] and the turned rotary keys k_rope f16 [S, 64] that all heads share -> out f16
+    [T, heads, 128].  Rows of q, kv and k_rope may be slices of wider matrices.  q_start, kv_start i32 [requests + 1]: the
+    rows and the keys of each request, whose last row sees all of its keys; max_q: a bound of its rows; workspace: from
+    pq_latent_workspace (without it the keys of a request are not split)."""
+    if q.dim() != 3:
+        raise ValueError(f"q: expected a 3-D tensor [rows, heads, {NOPE + LATENT_ROPE}]")
+    H = q.shape[1]
+    T, qs = _strided_rows(q, H * (NOPE + LATENT_ROPE), "q")
+    S, kvs = _strided_rows(kv, H * (NOPE + VALUE), "kv")
+    Sr, krs = _strided_rows(k_rope, LATENT_ROPE, "k_rope")
+    if Sr != S:
+        raise ValueError(f"k_rope: expected {S} rows, got {Sr}")
+    B = q_start.numel() - 1
+    checks = ((q_start, torch.int32, B + 1, "q_start"), (kv_start, torch.int32, B + 1, "kv_start"))
+    if out is not None:
+        checks += ((out, torch.float16, T * H * VALUE, "out"),)
+    ws, ws_bytes, more = _workspace_check(workspace)
+    _operands(q.get_device(), *checks, *more)
+    _on(q.get_device(), kv=kv, k_rope=k_rope)
+    if out is None:
+        out = torch.empty((T, H, VALUE), dtype=torch.float16, device=q.device)
+    _check("pq_expanded_attention", lib().pq_expanded_attention(q.data_ptr(), qs, H, kv.data_ptr(), kvs, k_rope.data_ptr(), krs, S,
+                                                                q_start.data_ptr(), kv_start.data_ptr(), B, T, max_q, scale, out.data_ptr(),
+                                                                ws, ws_bytes, _stream()))
     return out
 
 

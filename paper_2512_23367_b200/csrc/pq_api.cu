@@ -172,6 +172,20 @@ int make_tmap_2d(CUtensorMap* out, const void* base, uint64_t rows, uint64_t col
   return r == CUDA_SUCCESS ? PQ_OK : PQ_ERR_CUDA;
 }
 
+int make_tmap_heads(CUtensorMap* out, const void* base, uint64_t rows, uint64_t heads, uint64_t cols, uint64_t row_stride,
+                    uint64_t head_stride, uint32_t box_rows) {
+  const EncodeTiledFn encode = encode_fn();
+  if (encode == nullptr) return PQ_ERR_CUDA;
+  cuuint64_t dims[3] = {cols, heads, rows};
+  cuuint64_t strides[2] = {head_stride * 2, row_stride * 2};
+  cuuint32_t box[3] = {64, 1, box_rows};
+  cuuint32_t estr[3] = {1, 1, 1};
+  const CUresult r = encode(out, CU_TENSOR_MAP_DATA_TYPE_UINT16, 3, const_cast<void*>(base), dims, strides, box, estr,
+                            CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+                            CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+  return r == CUDA_SUCCESS ? PQ_OK : PQ_ERR_CUDA;
+}
+
 }  // namespace pq
 
 using namespace pq;

@@ -1,6 +1,7 @@
 // Attention of more than 16 query rows per (request, key/value head) over the paged cache, on the tcgen05 tensor
 // cores: prompts, chunks of prompts and wide drafts.
 #include "pq_attention.h"
+#include "pq_attn_mma.cuh"
 #include "pq_ptx.cuh"
 
 namespace pq {
@@ -32,55 +33,6 @@ struct TileCfg {
                                6 * 16 * kConv /* the converters' slots */ + 1024 /* alignment */;
 };
 
-// ---- tcgen05 with 16-bit floating-point operands
-// kind::f16, FP16 A and B, FP32 accumulator, M = 128; b_mn: B is stored with its N dimension contiguous.
-__host__ __device__ constexpr uint32_t umma_idesc_f16(uint32_t N, bool b_mn) {
-  return (1u << 4) | (b_mn ? (1u << 16) : 0u) | ((N >> 3) << 17) | ((128u >> 4) << 24);
-}
-// Shared-memory operand descriptors, low word: start address in 16-byte units and the leading byte offset.  The high
-// word is the same for both kinds: groups of 8 rows of 128 bytes lie 1024 bytes apart, 128-byte swizzle.
-//   K-major (Q, K):   64 features per 128-byte row; a k step of 16 is 32 bytes further.
-//   MN-major (V):     panels of 64 columns, `panel` bytes apart; a k step of 16 keys is 2048 bytes further.
-constexpr uint32_t kDescHi = (1024u >> 4) | (1u << 14) | (2u << 29);
-__device__ __forceinline__ uint32_t desc_k(uint32_t saddr) { return ((saddr & 0x3FFFFu) >> 4) | (1u << 16); }
-__device__ __forceinline__ uint32_t desc_mn(uint32_t saddr, uint32_t panel) { return ((saddr & 0x3FFFFu) >> 4) | ((panel >> 4) << 16); }
-// One MMA of 128 x N x 16.  Operands stay in uniform registers (the whole warp computes them, one elected thread
-// issues): with per-thread operands an issue took 93 to 120 cycles against the 64 that the tensor core needs.
-template <int kAccumulate>
-__device__ __forceinline__ void umma_f16_ss(uint32_t d, uint32_t a_lo, uint32_t b_lo, uint32_t idesc) {
-  asm volatile("{\n\t.reg .pred p;\n\t.reg .b64 a, b;\n\tsetp.ne.b32 p, %4, 0;\n\tmov.b64 a, {%1, %5};\n\tmov.b64 b, {%2, %5};\n\t"
-               "tcgen05.mma.cta_group::1.kind::f16 [%0], a, b, %3, p;\n\t}"
-               ::"r"(d), "r"(a_lo), "r"(b_lo), "r"(idesc), "n"(kAccumulate), "n"(kDescHi) : "memory");
-}
-// A in tensor memory: lane = row, a 32-bit column holds two neighbouring k.
-__device__ __forceinline__ void umma_f16_ts(uint32_t d, uint32_t a, uint32_t b_lo, uint32_t idesc, uint32_t accumulate) {
-  asm volatile("{\n\t.reg .pred p;\n\t.reg .b64 b;\n\tsetp.ne.b32 p, %4, 0;\n\tmov.b64 b, {%2, %5};\n\t"
-               "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], b, %3, p;\n\t}"
-               ::"r"(d), "r"(a), "r"(b_lo), "r"(idesc), "r"(accumulate), "n"(kDescHi) : "memory");
-}
-__device__ __forceinline__ void tmem_st_32x32(uint32_t taddr, const uint32_t (&r)[32]) {
-  asm volatile(
-      "tcgen05.st.sync.aligned.32x32b.x32.b32 [%0], "
-      "{%1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16, "
-      "%17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31, %32};" ::"r"(taddr),
-      "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]), "r"(r[9]),
-      "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15]), "r"(r[16]), "r"(r[17]), "r"(r[18]),
-      "r"(r[19]), "r"(r[20]), "r"(r[21]), "r"(r[22]), "r"(r[23]), "r"(r[24]), "r"(r[25]), "r"(r[26]), "r"(r[27]),
-      "r"(r[28]), "r"(r[29]), "r"(r[30]), "r"(r[31])
-      : "memory");
-}
-__device__ __forceinline__ void tmem_st_32x16(uint32_t taddr, const uint32_t (&r)[16]) {
-  asm volatile(
-      "tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16};" ::"r"(taddr),
-      "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]), "r"(r[9]),
-      "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15])
-      : "memory");
-}
-__device__ __forceinline__ void tmem_st_wait() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
-
-__device__ __forceinline__ void named_bar_arrive(uint32_t id, uint32_t nthreads) {
-  asm volatile("bar.arrive %0, %1;" ::"r"(id), "r"(nthreads) : "memory");
-}
 // Named barriers (0 is __syncthreads): the softmax warpgroups among themselves; "P written", one per accumulator
 // (256 threads arrive, the issuer's warp waits); "operand tile landed", between the watcher's and the issuer's warp;
 // the two warps that share 32 rows, eight pairs; "S read", 256 threads of an accumulator to the issuer, one each;
@@ -88,68 +40,6 @@ __device__ __forceinline__ void named_bar_arrive(uint32_t id, uint32_t nthreads)
 // They do not pass through shared memory, which the tensor core keeps busy: a wait on an mbarrier that has long
 // completed takes 200 to 400 cycles here, one on a named barrier about 30.
 constexpr uint32_t kBarSoft = 1, kBarP = 2, kBarTile = 4, kBarPair = 5, kBarRead = 13, kBarFree = 15;
-// Meets the other warp of the pair; whether any of the 64 threads says yes.
-__device__ __forceinline__ bool pair_any(uint32_t id, bool yes) {
-  uint32_t r;
-  asm volatile("{\n\t.reg .pred p, q;\n\tsetp.ne.b32 p, %2, 0;\n\tbar.red.or.pred q, %1, 64, p;\n\tselp.u32 %0, 1, 0, q;\n\t}"
-               : "=r"(r) : "r"(id), "r"(static_cast<uint32_t>(yes)) : "memory");
-  return r != 0;
-}
-
-// Watcher and issuer meet; whether the operand tile has landed (the watcher's word; the issuer says yes).
-__device__ __forceinline__ bool tile_landed(bool yes) {
-  uint32_t r;
-  asm volatile("{\n\t.reg .pred p, q;\n\tsetp.ne.b32 p, %2, 0;\n\tbar.red.and.pred q, %1, 64, p;\n\tselp.u32 %0, 1, 0, q;\n\t}"
-               : "=r"(r) : "r"(kBarTile), "r"(static_cast<uint32_t>(yes)) : "memory");
-  return r != 0;
-}
-// "Done" to the issuer.  A warp that has given up waiting for S is no longer paced by it: it meets the issuer instead, so
-// that it cannot arrive twice for one of the issuer's waits (which would leave the issuer waiting for good).
-__device__ __forceinline__ void hand_over(uint32_t id, uint32_t nthreads, bool ok) {
-  if (ok) named_bar_arrive(id, nthreads); else named_bar_sync(id, nthreads);
-}
-// The sum, or the larger, of a value of the row's two threads, the same in both: the second half's goes to the first
-// and the result back.
-template <bool kSum>
-__device__ __forceinline__ float pair_combine(float* word, uint32_t id, int half, float v) {
-  if (half == 1) *word = v;
-  named_bar_sync(id, 64);
-  if (half == 0) {
-    v = kSum ? v + *word : fmaxf(v, *word);
-    *word = v;
-  }
-  named_bar_sync(id, 64);
-  if (half == 1) v = *word;
-  return v;
-}
-
-// Two FP32 operations in one instruction.
-__device__ __forceinline__ uint64_t pair_f32(float a, float b) {
-  uint64_t r;
-  asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(a), "f"(b));
-  return r;
-}
-__device__ __forceinline__ void unpair_f32(uint64_t v, float& a, float& b) { asm("mov.b64 {%0, %1}, %2;" : "=f"(a), "=f"(b) : "l"(v)); }
-__device__ __forceinline__ uint64_t fma_f32x2(uint64_t a, uint64_t b, uint64_t c) {
-  uint64_t d;
-  asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(d) : "l"(a), "l"(b), "l"(c));
-  return d;
-}
-__device__ __forceinline__ uint64_t add_f32x2(uint64_t a, uint64_t b) {
-  uint64_t d;
-  asm("add.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b));
-  return d;
-}
-__device__ __forceinline__ uint64_t mul_f32x2(uint64_t a, uint64_t b) {
-  uint64_t d;
-  asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b));
-  return d;
-}
-__device__ __forceinline__ float max3(float a, float b, float c) {
-  float d;
-  asm("max.f32 %0, %1, %2, %3;" : "=f"(d) : "f"(a), "f"(b), "f"(c));
-  return d;
-}
 // Blocks of 16 keys of one request, a lane each, so that one look-up serves four key tiles: the index of the block's first
 // cache vector, or -1 where there is nothing to read.  The page ids of the next 32 blocks are on the way meanwhile.
 struct BlockWalk {
@@ -175,11 +65,6 @@ struct BlockWalk {
   }
 };
 
-// A wait of a whole warp whose lanes go on, or give up, together.
-__device__ __forceinline__ bool warp_wait(uint32_t bar, uint32_t parity, const WaitCtx& wc) {
-  return __all_sync(0xffffffffu, mbar_wait(bar, parity, wc));
-}
-
 struct TileArgs {
   AttnArgs a;
   int* status;
@@ -189,15 +74,6 @@ struct TileArgs {
   int whole, split, parts;   // as planned: CTAs of whole units, then part 0 of the others, part 1, ...
   uint32_t q_and, q_xor; // a scale of 0 or below is folded into the queries: (q & q_and) ^ q_xor
 };
-
-__device__ __forceinline__ int warp_prefix(int v, int lane) {   // inclusive sums
-#pragma unroll
-  for (int o = 1; o < 32; o <<= 1) {
-    const int x = __shfl_up_sync(0xffffffffu, v, o);
-    if (lane >= o) v += x;
-  }
-  return v;
-}
 
 // Which request and which of its tiles of `qt` tokens: the slot-th over all requests that this kernel serves (a request's
 // last tile, which sees most keys, comes first).  found: request (-1: there are fewer), tile, first row, rows, cached
@@ -617,7 +493,7 @@ attn_tile_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constan
         if (u > 0 && u <= N) named_bar_sync(kBarRead + ((u - 1) & 1), 288);   // S(u - 1) is in registers
         if (u < N) {   // S(u) = Q K^T
           const int acc = u & 1, st = (2 * (two ? u >> 1 : u)) % C::kStages;
-          if (!two || acc == 0) live = tile_landed(true) && live;
+          if (!two || acc == 0) live = tile_landed(kBarTile, true) && live;
           tc_fence_after_sync();
           if (leader && live) {
             const uint32_t ql = q_lo + acc * q_step, kl = k_lo0 + st * kStageUnits;
@@ -631,7 +507,7 @@ attn_tile_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constan
         }
         if (u >= lag) {   // O(u - lag) += P V
           const int v = u - lag, acc = v & 1, st = (2 * (two ? v >> 1 : v) + 1) % C::kStages;
-          if (!two || acc == 0) live = tile_landed(true) && live;
+          if (!two || acc == 0) live = tile_landed(kBarTile, true) && live;
           named_bar_sync(kBarP + acc, 288);
           tc_fence_after_sync();
           if (leader && live) {
@@ -668,7 +544,7 @@ attn_tile_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constan
           if (w < 0 || w >= N || (two && (w & 1))) continue;
           const int i = 2 * (two ? w >> 1 : w) + is_v;
           ok = ok && warp_wait(bar_full + 8 * (i % C::kStages), (i / C::kStages) & 1, wc);
-          tile_landed(ok);
+          tile_landed(kBarTile, ok);
         }
       }
     }

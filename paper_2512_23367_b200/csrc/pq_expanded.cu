@@ -1,0 +1,554 @@
+// Latent attention, expanded form: ragged queries over keys and values multiplied out per head, with one rotary key a token
+// for all heads, on the tcgen05 tensor cores.  See include/pq.h for the contract.
+#include <cuda_fp16.h>
+
+#include <cmath>
+
+#include "pq_attention.h"
+#include "pq_attn_mma.cuh"
+#include "pq_internal.h"
+#include "pq_ptx.cuh"
+#include "pq_schedule.cuh"
+
+namespace pq {
+
+namespace {
+
+constexpr int kTile = 128;          // query rows of one accumulator
+constexpr int kUnit = 2 * kTile;    // of a unit
+constexpr int kKeys = 96;           // keys of one step
+constexpr int kNope = 128, kValue = 128, kQuery = kNope + PQ_LATENT_ROPE;
+constexpr int kSoft = 512;          // threads of the four softmax warpgroups, two per accumulator
+constexpr int kIssuer = 16, kLoadK = 17, kWatcher = 18, kLoadV = 19, kThreads = 640;   // warps
+constexpr int kSoftRegs = 104, kRestRegs = 64;   // 512 x 104 + 128 x 64 = 640 x 96, what the launch holds
+constexpr int kPanelQ = kTile * 128, kPanelK = kKeys * 128;   // bytes of 64 values of all rows
+constexpr int kQueryBytes = 3 * kPanelQ, kKeyBytes = 3 * kPanelK, kValueBytes = 2 * kPanelK;
+constexpr int kSmem = 2 * kQueryBytes + 2 * kKeyBytes + 2 * kValueBytes + 1024 /* alignment */;
+constexpr int kPartFloats = kUnit * (kValue + 2);   // per query tile [32][128 rows] x 4 sums, then [128 rows] x (reference, sum of weights)
+constexpr int kLeastSteps = 4;      // of a CTA, so that its parts are worth joining
+// Tensor memory: S, shared by the accumulators in turn; P of each; O of each.
+constexpr uint32_t kColP = 96, kColO = 256;
+// Named barriers, as in the paged tile kernel: "P written" (two), "operand tile landed", the two warps that share 32 rows
+// (eight pairs), "S read" (two), accumulators' sums.
+constexpr uint32_t kBarP = 1, kBarTile = 3, kBarPair = 4, kBarRead = 12, kBarSoft = 14;
+
+struct ExpandedArgs {
+  const int* q_start;
+  const int* kv_start;
+  __half* out;
+  int64_t tokens;
+  int requests, heads;
+  float scale_log2;      // > 0
+  uint32_t q_and, q_xor; // a scale of 0 or below is folded into the products: (s & q_and) ^ q_xor
+  int shares;            // units are handed out in equal runs of steps, with parts to join
+  float* partials;       // two parts per CTA
+  int4* joins;           // per CTA: first token, tokens, head, parts
+  int* status;
+  uint32_t wait_limit;
+
+  __device__ __forceinline__ Request request(int b) const {
+    Request r;
+    r.s = UnitShape{kUnit, 1, kKeys, heads};
+    r.q0 = q_start[b];
+    r.n = max(q_start[b + 1] - r.q0, 0);
+    r.k0 = kv_start[b];
+    r.L = r.hi = max(kv_start[b + 1] - r.k0, 0);
+    r.settle();
+    return r;
+  }
+};
+
+// The steps of a unit, or of the part of one that a CTA has.
+struct Part {
+  int toks, N, lag;      // tokens; (S, O) steps; steps that an O follows its S by
+  bool two;              // more than one accumulator's rows: the accumulators are two query tiles, else the even and the odd key tiles
+  __device__ __forceinline__ explicit Part(const Walk<ExpandedArgs>& w)
+      : toks(min(kUnit, w.r.n - w.tile * kUnit)), two(toks > kTile) {
+    N = two ? 2 * w.count : w.count;
+    lag = two ? 2 : 1;
+  }
+};
+
+// Tensor bound.  A unit is 256 query rows of one head as two accumulators of 128, or up to 128 rows as two accumulators that
+// take the even and the odd key tiles and are joined at the end: one's softmax runs while the tensor core works for the
+// other, as in the paged tile kernel.  What differs:
+//   - the product with the keys goes over 192 values, 128 of the head and 64 that all heads share, so that queries and keys
+//     take half as much shared memory again.  With steps of 128 keys one step and a half would fit; with 96 two steps do, and
+//     loads run a whole step ahead.  S takes 12 MMAs of N = 96 (56 cycles each, bound by shared memory; 48 by arithmetic),
+//     O 6 of N = 128: 2112 cycles per 256 x 96 scores where arithmetic alone would take 1920.
+//   - a CTA stays on its SM and walks through its units: queries of the next one are on the way, and its first S computed,
+//     while the results of the last one go out.
+//   - keys and values are rows of one linear's output, read through one tensor map with heads as its second dimension.
+__global__ void __launch_bounds__(kThreads, 1)
+expanded_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUtensorMap map_kv, const __grid_constant__ CUtensorMap map_rope,
+                const ExpandedArgs a) {
+  constexpr float kTop = 7.0f;      // a weight at the reference is 2^kTop
+  extern __shared__ uint8_t smem_raw[];
+  __shared__ __align__(8) uint64_t bars[17];
+  __shared__ uint32_t s_tmem;
+  __shared__ volatile int s_abort;
+  __shared__ Share s_share;
+  __shared__ int64_t s_sums[kThreads / 32];
+  __shared__ float s_swap[2 * kTile];
+  __shared__ float2 s_ml[kTile];
+
+  const int tid = threadIdx.x, warp = __shfl_sync(0xffffffffu, tid >> 5, 0), lane = tid & 31;
+  const uint32_t bar_k = smem_u32(bars), bar_v = bar_k + 16, bar_kfree = bar_v + 16, bar_vfree = bar_kfree + 16;   // two of each
+  const uint32_t bar_s = bar_vfree + 16, bar_o = bar_s + 16;                                                       // per accumulator
+  const uint32_t bar_q = bar_o + 16, bar_qfree = bar_q + 8, bar_read = bar_qfree + 8, bar_fix = bar_read + 8, bar_drain = bar_fix + 8;
+  if (tid == 0) {
+    for (int i = 0; i < 12; ++i) mbar_init(bar_k + 8 * i, 1);
+    mbar_init(bar_q, 1);
+    mbar_init(bar_qfree, 1);
+    mbar_init(bar_read, 1);
+    mbar_init(bar_fix, 1);
+    mbar_init(bar_drain, 1);
+    fence_mbar_init();
+    s_abort = 0;
+    tma_prefetch_desc(&map_q), tma_prefetch_desc(&map_kv), tma_prefetch_desc(&map_rope);
+  }
+  if (warp == kIssuer) {
+    tmem_alloc(smem_u32(&s_tmem), 512);
+    tmem_relinquish();
+  }
+  tc_fence_before_sync();
+  grid_dep_wait();
+  const bool shares = a.shares != 0;
+  if (shares) find_share<kThreads>(a, blockIdx.x, gridDim.x, kLeastSteps, &s_share, s_sums); else __syncthreads();
+  tc_fence_after_sync();
+  grid_dep_launch();   // only now: a later launch's CTA may take this SM's tensor memory when it is given back
+  const uint32_t tmem = __shfl_sync(0xffffffffu, s_tmem, 0);
+  const uint32_t sq = (smem_u32(smem_raw) + 1023u) & ~1023u, ring_k = sq + 2 * kQueryBytes, ring_v = ring_k + 2 * kKeyBytes;
+  const WaitCtx wc{&s_abort, a.wait_limit};
+  uint32_t issued = 0, fixes = 0, units = 0;   // producers: tiles requested, of them by way of bar_fix; units
+
+  if (warp >= kSoft / 32) {
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kRestRegs));
+    if (warp == kLoadK) {
+      // ------------------------------------------------------------------ queries and keys
+      bool ok = true;
+      for (Walk<ExpandedArgs> w(a, s_share, shares, blockIdx.x, gridDim.x); ok && w.more(); w.next()) {
+        const Part part(w);
+        if (units > 0 && !(ok = warp_wait(bar_qfree, (units - 1) & 1, wc))) break;
+        if (lane == 0) mbar_arrive_expect_tx(bar_q, part.two ? 2 * kQueryBytes : kQueryBytes);
+        __syncwarp();
+        if (lane < (part.two ? 6 : 3)) {
+          const int tile = lane / 3, x = lane % 3;
+          tma_load_3d(sq + lane * kPanelQ, &map_q, bar_q, x * 64, w.copy, w.r.q0 + w.tile * kUnit + tile * kTile);
+        }
+        ++units;
+        for (int i = 0; i < w.count; ++i) {
+          const uint32_t st = issued & 1, dst = ring_k + st * kKeyBytes, bar = bar_k + 8 * st;
+          if (issued >= 2 && !(ok = warp_wait(bar_kfree + 8 * st, ((issued >> 1) & 1) ^ 1, wc))) break;
+          const int row = w.r.k0 + (w.step + i) * kKeys;
+          if (lane == 0) mbar_arrive_expect_tx(bar, kKeyBytes);
+          __syncwarp();
+          if (lane < 2) tma_load_3d(dst + lane * kPanelK, &map_kv, bar, lane * 64, w.copy, row);
+          if (lane == 2) tma_load_3d(dst + 2 * kPanelK, &map_rope, bar, 0, 0, row);
+          ++issued;
+          __syncwarp();
+        }
+      }
+    } else if (warp == kLoadV) {
+      // ------------------------------------------------------------------ values
+      bool ok = true;
+      for (Walk<ExpandedArgs> w(a, s_share, shares, blockIdx.x, gridDim.x); ok && w.more(); w.next()) {
+        for (int i = 0; i < w.count; ++i) {
+          const uint32_t st = issued & 1, dst = ring_v + st * kValueBytes;
+          if (issued >= 2 && !(ok = warp_wait(bar_vfree + 8 * st, ((issued >> 1) & 1) ^ 1, wc))) break;
+          const int key0 = (w.step + i) * kKeys;
+          const int dead = min(max(w.r.hi - key0, 0), kKeys);   // from here on rows are not the request's
+          const uint32_t bar = dead < kKeys ? bar_fix : bar_v + 8 * st;
+          if (lane == 0) mbar_arrive_expect_tx(bar, kValueBytes);
+          __syncwarp();
+          if (lane < 2) tma_load_3d(dst + lane * kPanelK, &map_kv, bar, kNope + lane * 64, w.copy, w.r.k0 + key0);
+          ++issued;
+          if (dead < kKeys) {   // their weights are 0, but 0 x NaN is not
+            if (!(ok = warp_wait(bar_fix, fixes & 1, wc))) break;
+            ++fixes;
+            for (int j = lane; j < (kKeys - dead) * 16; j += 32) {
+              const int r = dead + (j >> 4), c = j & 15;
+              asm volatile("st.shared.v4.u32 [%0], {%1, %1, %1, %1};" ::"r"(dst + (c >> 3) * kPanelK + r * 128 + (c & 7) * 16), "r"(0) : "memory");
+            }
+            fence_proxy_async_smem();
+            __syncwarp();
+            if (lane == 0) mbar_arrive(bar_v + 8 * st);
+          }
+          __syncwarp();
+        }
+      }
+    } else if (warp == kIssuer) {
+      // ------------------------------------------------------------------ MMA issuer
+      // As in the paged tile kernel: the whole warp walks, one elected thread issues, and after the watcher has given up the
+      // steps go on without MMAs, so that the named barriers stay in step.
+      constexpr uint32_t id_qk = umma_idesc_f16(kKeys, false), id_pv = umma_idesc_f16(kValue, true);
+      const uint32_t leader = elect_one();
+      const uint32_t q_lo = desc_k(sq), k_lo0 = desc_k(ring_k), v_lo0 = desc_mn(ring_v, kPanelK);
+      bool live = true;
+      uint32_t g = 0, seg = 0;   // key tiles, units before this one
+      for (Walk<ExpandedArgs> w(a, s_share, shares, blockIdx.x, gridDim.x); w.more(); w.next()) {
+        const Part part(w);
+        const bool two = part.two;
+        live = live && warp_wait(bar_q, seg & 1, wc);
+        for (int u = 0; u < part.N + part.lag; ++u) {
+          if (u > 0 && u <= part.N) named_bar_sync(kBarRead + ((u - 1) & 1), 288);   // S(u - 1) is in registers
+          if (u < part.N) {   // S(u) = Q K^T
+            const uint32_t acc = u & 1, st = (g + (two ? u >> 1 : u)) & 1;
+            if (!two || acc == 0) live = tile_landed(kBarTile, true) && live;
+            tc_fence_after_sync();
+            if (leader && live) {
+              const uint32_t ql = q_lo + (two ? acc * (kQueryBytes / 16) : 0), kl = k_lo0 + st * (kKeyBytes / 16);
+              umma_f16_ss<0>(tmem, ql, kl, id_qk);
+#pragma unroll
+              for (int k = 1; k < kQuery / 16; ++k) umma_f16_ss<1>(tmem, ql + (k / 4) * (kPanelQ / 16) + (k % 4) * 2, kl + (k / 4) * (kPanelK / 16) + (k % 4) * 2, id_qk);
+              umma_commit(bar_s + 8 * acc);
+              if (!two || acc == 1) umma_commit(bar_kfree + 8 * st);
+              if (u == part.N - 1) umma_commit(bar_qfree);
+            }
+            __syncwarp();
+          }
+          if (u >= part.lag) {   // O(u - lag) += P V
+            const int v = u - part.lag;
+            const uint32_t acc = v & 1, st = (g + (two ? v >> 1 : v)) & 1;
+            if (!two || acc == 0) live = tile_landed(kBarTile, true) && live;
+            if (v == 0 && seg > 0) live = warp_wait(bar_read, (seg - 1) & 1, wc) && live;   // the sums of the unit before have been read
+            named_bar_sync(kBarP + acc, 288);
+            tc_fence_after_sync();
+            if (leader && live) {
+              const uint32_t vl = v_lo0 + st * (kValueBytes / 16), d = tmem + kColO + acc * kValue, p = tmem + kColP + acc * (kKeys / 2);
+              umma_f16_ts(d, p, vl, id_pv, (v >> 1) > 0);
+#pragma unroll
+              for (int k = 1; k < kKeys / 16; ++k) umma_f16_ts(d, p + 8 * k, vl + k * 128, id_pv, 1u);
+              umma_commit(bar_o + 8 * acc);
+              if (!two || acc == 1) umma_commit(bar_vfree + 8 * st);
+            }
+            __syncwarp();
+          }
+        }
+        g += w.count, ++seg;
+      }
+    } else if (warp == kWatcher) {
+      // ------------------------------------------------------------------ watcher: waits for the operand tiles a step ahead
+      bool ok = true;
+      uint32_t g = 0;
+      for (Walk<ExpandedArgs> w(a, s_share, shares, blockIdx.x, gridDim.x); w.more(); w.next()) {
+        const Part part(w);
+        for (int u = 0; u < part.N + part.lag; ++u) {
+#pragma unroll
+          for (int is_v = 0; is_v < 2; ++is_v) {
+            const int x = u - is_v * part.lag;
+            if (x < 0 || x >= part.N || (part.two && (x & 1))) continue;
+            const uint32_t t = g + (part.two ? x >> 1 : x);
+            ok = ok && warp_wait((is_v ? bar_v : bar_k) + 8 * (t & 1), (t >> 1) & 1, wc);
+            tile_landed(kBarTile, ok);
+          }
+        }
+        g += w.count;
+      }
+    }
+  } else {
+    // -------------------------------------------------------------------- softmax, two threads per row
+    asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kSoftRegs));
+    const int acc = warp >> 3;                       // accumulator
+    const int half = (warp >> 2) & 1;                // the thread's 48 keys of a tile, and its half of the values
+    const int r = tid & 127;                         // row of the tile
+    const uint32_t lane_off = static_cast<uint32_t>(warp & 3) << 21;   // 32 lanes per warp, lane in bits 16 and up
+    const uint32_t t_s = tmem + 48 * half + lane_off, t_p = tmem + kColP + acc * (kKeys / 2) + 24 * half + lane_off;
+    const uint32_t t_out = tmem + kColO + acc * kValue + half * (kValue / 2) + lane_off;
+    float* swap = s_swap + acc * kTile + r;
+    const uint32_t pair = kBarPair + acc * 4 + (warp & 3);
+    const float sc = a.scale_log2;
+    const uint64_t sc2 = pair_f32(sc, sc);
+    uint32_t n = 0;                                  // the accumulator's steps so far
+    int4 join = make_int4(0, 0, 0, 0);
+    bool ok = true;
+    for (Walk<ExpandedArgs> w(a, s_share, shares, blockIdx.x, gridDim.x); w.more(); w.next()) {
+      const Part part(w);
+      const bool two = part.two;
+      const int tok = (two ? acc * kTile : 0) + r;   // of the unit
+      const int p0 = w.r.L - w.r.n + w.tile * kUnit + (two ? acc * kTile : 0);   // position of the tile's first row
+      const int see_to = min(p0 + r, w.r.hi - 1) - 48 * half;                    // last key of the row, from the thread's first
+      const int all_to = min(p0 + 1, w.r.hi);                                    // every row sees the keys before
+      const int mine = two ? w.count : (w.count - acc + 1) >> 1;
+      float m = -INFINITY, l = 0.0f;   // m: the reference that is subtracted, in powers of two; l: the thread's own keys
+      for (int i = 0; i < mine; ++i, ++n) {
+        const int key0 = (w.step + (two ? i : 2 * i + acc)) * kKeys;
+        ok = ok && warp_wait(bar_s + 8 * acc, n & 1, wc);
+        tc_fence_after_sync();
+        uint32_t s[32], s2[16];
+        tmem_ld_32x32(t_s, s);
+        tmem_ld_32x16(t_s + 32, s2);
+        tmem_ld_wait();
+        tc_fence_before_sync();
+        hand_over(kBarRead + acc, 288, ok);
+        if (a.q_xor != 0u || a.q_and == 0u) {
+#pragma unroll
+          for (int j = 0; j < 32; ++j) s[j] = (s[j] & a.q_and) ^ a.q_xor;
+#pragma unroll
+          for (int j = 0; j < 16; ++j) s2[j] = (s2[j] & a.q_and) ^ a.q_xor;
+        }
+        if (key0 + kKeys > all_to) {   // some row does not see all keys
+          const int to = see_to - key0;
+#pragma unroll
+          for (int j = 0; j < 32; ++j)
+            if (j > to) s[j] = 0xff800000u;   // -inf
+#pragma unroll
+          for (int j = 0; j < 16; ++j)
+            if (32 + j > to) s2[j] = 0xff800000u;
+        }
+        float top[3];
+#pragma unroll
+        for (int h = 0; h < 3; ++h) {
+          const uint32_t* v = h < 2 ? s + 16 * h : s2;
+          top[h] = max3(__uint_as_float(v[0]), __uint_as_float(v[1]), __uint_as_float(v[2]));
+#pragma unroll
+          for (int j = 3; j < 15; j += 2) top[h] = max3(top[h], __uint_as_float(v[j]), __uint_as_float(v[j + 1]));
+          top[h] = fmaxf(top[h], __uint_as_float(v[15]));
+        }
+        float t = max3(top[0], top[1], top[2]) * sc;
+        bool done = i == 0;   // the product with the weights before these has been taken
+        if (pair_any(pair, t > m + 8.0f)) {   // rare after the first tiles: some row of the 32
+          t = pair_combine<false>(swap, pair, half, t);
+          const bool grown = t > m + 8.0f;
+          const float f = grown ? (m == -INFINITY ? 0.0f : exp2_approx(m - t)) : 1.0f;
+          if (grown) m = t;
+          l *= f;
+          if (i > 0) {   // O holds the sums up to the tile before
+            ok = ok && warp_wait(bar_o + 8 * acc, (n - 1) & 1, wc);
+            done = true;
+            tc_fence_after_sync();
+#pragma unroll 1
+            for (int h = 0; h < kValue / 32; ++h) {
+              uint32_t o[16];
+              tmem_ld_32x16(t_out + 16 * h, o);
+              tmem_ld_wait();
+#pragma unroll
+              for (int j = 0; j < 16; ++j) o[j] = __float_as_uint(__uint_as_float(o[j]) * f);
+              tmem_st_32x16(t_out + 16 * h, o);
+            }
+          }
+        }
+        const float off = kTop - (m == -INFINITY ? 0.0f : m);
+        const uint64_t off2 = pair_f32(off, off);
+        uint32_t p[16], p2[8], asked = 0;
+        uint64_t sum = 0;
+        auto weigh = [&](uint32_t x0, uint32_t x1) {
+          float e0, e1;
+          unpair_f32(fma_f32x2(pair_f32(__uint_as_float(x0), __uint_as_float(x1)), sc2, off2), e0, e1);
+          e0 = exp2_approx(e0);
+          e1 = exp2_approx(e1);
+          sum = add_f32x2(sum, pair_f32(e0, e1));
+          return pack_f16(e0, e1);
+        };
+#pragma unroll
+        for (int j = 0; j < 16; ++j) p[j] = weigh(s[2 * j], s[2 * j + 1]);
+        asked = mbar_test2(bar_o + 8 * acc, (n - 1) & 1, bar_o + 8 * acc, (n - 1) & 1);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) p2[j] = weigh(s2[2 * j], s2[2 * j + 1]);
+        float l0, l1;
+        unpair_f32(sum, l0, l1);
+        l += l0 + l1;
+        if (!done && !__all_sync(0xffffffffu, asked)) ok = ok && warp_wait(bar_o + 8 * acc, (n - 1) & 1, wc);
+        tc_fence_after_sync();
+        tmem_st_32x16(t_p, p);
+        tmem_st_32x8(t_p + 16, p2);
+        tmem_st_wait();
+        tc_fence_before_sync();
+        hand_over(kBarP + acc, 288, ok);
+      }
+      // ------------------------------------------------------------------ the unit's (or part's) end
+      if (mine > 0) ok = ok && warp_wait(bar_o + 8 * acc, (n - 1) & 1, wc);
+      tc_fence_after_sync();
+      l = pair_combine<true>(swap, pair, half, l);   // the sum of the row's two threads
+      // Accumulators of the even and the odd tiles are joined in the first one's threads: both lie in the same lanes.
+      float f0 = 1.0f, f1 = 0.0f;
+      const bool both = !two && w.count > 1;
+      if (both) {
+        if (acc == 1 && half == 0) s_ml[r] = make_float2(m, l);
+        tc_fence_before_sync();
+        named_bar_sync(kBarSoft, kSoft);
+        tc_fence_after_sync();
+        if (acc == 0) {
+          const float2 ml = s_ml[r];
+          const float M = fmaxf(m, ml.x), Ms = M == -INFINITY ? 0.0f : M;
+          f0 = exp2_approx(m - Ms), f1 = exp2_approx(ml.x - Ms);
+          l = l * f0 + ml.y * f1;
+          m = M;
+        }
+      }
+      if (two || acc == 0) {
+        const float inv = l > 0.0f ? 1.0f / l : 0.0f;
+        const int64_t row = static_cast<int64_t>(w.r.q0) + w.tile * kUnit + tok;
+        const bool writes = tok < part.toks && row >= 0 && row < a.tokens, whole = w.whole(), begins = w.step == 0;
+        __half* to = a.out + (row * a.heads + w.copy) * kValue + half * (kValue / 2);
+        float* pp = a.partials + (2 * static_cast<int64_t>(blockIdx.x) + begins) * kPartFloats + (two ? acc : 0) * (kTile * (kValue + 2));
+#pragma unroll 1
+        for (int h = 0; h < kValue / 32; ++h) {
+          uint32_t o[16];
+          tmem_ld_32x16(t_out + 16 * h, o);
+          float v[16];
+          if (both) {
+            uint32_t o1[16];
+            tmem_ld_32x16(t_out + kValue + 16 * h, o1);
+            tmem_ld_wait();
+#pragma unroll
+            for (int j = 0; j < 16; ++j) v[j] = fmaf(__uint_as_float(o1[j]), f1, __uint_as_float(o[j]) * f0);
+          } else {
+            tmem_ld_wait();
+#pragma unroll
+            for (int j = 0; j < 16; ++j) v[j] = __uint_as_float(o[j]);
+          }
+          if (!writes) continue;
+          if (whole) {
+#pragma unroll
+            for (int j = 0; j < 2; ++j)
+              reinterpret_cast<uint4*>(to)[2 * h + j] = make_uint4(pack_f16(v[8 * j] * inv, v[8 * j + 1] * inv), pack_f16(v[8 * j + 2] * inv, v[8 * j + 3] * inv),
+                                                                   pack_f16(v[8 * j + 4] * inv, v[8 * j + 5] * inv), pack_f16(v[8 * j + 6] * inv, v[8 * j + 7] * inv));
+          } else {
+#pragma unroll
+            for (int j = 0; j < 4; ++j)
+              reinterpret_cast<float4*>(pp)[(half * 16 + 4 * h + j) * kTile + r] = make_float4(v[4 * j], v[4 * j + 1], v[4 * j + 2], v[4 * j + 3]);
+          }
+        }
+        if (!whole && half == 0) reinterpret_cast<float2*>(pp + kTile * kValue)[r] = make_float2(m, l);
+        if (!whole && begins) join = make_int4(w.r.q0 + w.tile * kUnit, part.toks, w.copy, 1 + (w.all_steps - w.count + s_share.per - 1) / s_share.per);
+      }
+      // All together go to the next unit: the second accumulator's threads may have had nothing to do in this one, and
+      // must not run ahead of the sums, and of s_ml, that the first one's threads still read.
+      tc_fence_before_sync();
+      named_bar_sync(kBarSoft, kSoft);
+      if (tid == 0) mbar_arrive(bar_read);
+    }
+    if (shares && tid == 0) a.joins[blockIdx.x] = join;
+  }
+
+  // ---------------------------------------------------------------------- teardown
+  tc_fence_before_sync();
+  __syncthreads();
+  tc_fence_after_sync();
+  if (s_abort) {
+    // Some role gave up.  What has been handed to the hardware still completes by itself and must have done so before shared
+    // and tensor memory go away: the producers' copies and the issuer's MMAs.
+    if (warp == kIssuer && elect_one()) {
+      umma_commit(bar_drain);
+      mbar_drain(bar_drain, 0u);
+    }
+    if ((warp == kLoadK || warp == kLoadV) && lane == 0) {
+      for (uint32_t i = issued > 2 ? issued - 2 : 0; i < issued; ++i) mbar_drain((warp == kLoadK ? bar_k : bar_v) + 8 * (i & 1), (i >> 1) & 1);
+      if (warp == kLoadK && units > 0) mbar_drain(bar_q, (units - 1) & 1);
+      if (warp == kLoadV) mbar_drain(bar_fix, fixes & 1);
+    }
+    __syncthreads();
+    if (tid == 0) atomicExch(a.status, static_cast<int>(PQ_ERR_TIMEOUT));
+  }
+  if (warp == kIssuer) tmem_dealloc(tmem, 512);
+}
+
+// Joins the parts of units that were cut: a block per CTA that had a unit's first part, 32 rows and 32 values, a warp per 4
+// of them, lanes along the rows.
+constexpr int kJoinThreads = 256;
+__global__ void __launch_bounds__(kJoinThreads) expanded_join_kernel(const ExpandedArgs a) {
+  grid_dep_launch();
+  grid_dep_wait();
+  const int4 join = a.joins[blockIdx.x];
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const int tile = blockIdx.y / 4, r = (blockIdx.y % 4) * 32 + lane, tok = tile * kTile + r, f4 = blockIdx.z * 8 + warp;
+  const int64_t row = static_cast<int64_t>(join.x) + tok;
+  if (join.w == 0 || tok >= join.y || row < 0 || row >= a.tokens) return;
+  // the unit's first part is the second one of its CTA, the others the first of theirs
+  auto part = [&](int i) { return a.partials + (2 * (static_cast<int64_t>(blockIdx.x) + i) + (i == 0)) * kPartFloats + tile * (kTile * (kValue + 2)); };
+  float M = -INFINITY, L = 0.0f;
+  float4 v = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+  constexpr int kBatch = 8;   // parts whose loads are in flight together
+  for (int i0 = 0; i0 < join.w; i0 += kBatch) {
+    float2 ml[kBatch];
+    float4 x[kBatch];
+#pragma unroll
+    for (int j = 0; j < kBatch; ++j) {
+      const float* p = part(min(i0 + j, join.w - 1));
+      ml[j] = __ldcg(reinterpret_cast<const float2*>(p + kTile * kValue) + r);
+      x[j] = __ldcg(reinterpret_cast<const float4*>(p) + f4 * kTile + r);
+    }
+    float top = M;
+#pragma unroll
+    for (int j = 0; j < kBatch; ++j) top = fmaxf(top, ml[j].x);
+    const float ref = top == -INFINITY ? 0.0f : top, f = exp2_approx(M - ref);
+    M = top;
+    L *= f, v.x *= f, v.y *= f, v.z *= f, v.w *= f;
+#pragma unroll
+    for (int j = 0; j < kBatch; ++j) {
+      const float wt = i0 + j < join.w ? exp2_approx(ml[j].x - ref) : 0.0f;
+      L = fmaf(ml[j].y, wt, L);
+      v.x = fmaf(x[j].x, wt, v.x), v.y = fmaf(x[j].y, wt, v.y), v.z = fmaf(x[j].z, wt, v.z), v.w = fmaf(x[j].w, wt, v.w);
+    }
+  }
+  const float inv = L > 0.0f ? 1.0f / L : 0.0f;
+  *reinterpret_cast<uint2*>(a.out + (row * a.heads + join.z) * kValue + 4 * f4) = make_uint2(pack_f16(v.x * inv, v.y * inv), pack_f16(v.z * inv, v.w * inv));
+}
+
+}  // namespace
+
+size_t expanded_partial_bytes(int sms) { return static_cast<size_t>(sms) * (2 * kPartFloats * sizeof(float) + sizeof(int4)); }
+
+}  // namespace pq
+
+using namespace pq;
+
+extern "C" {
+
+int pq_expanded_attention(const void* q_f16, int64_t q_stride, int32_t heads, const void* kv_f16, int64_t kv_stride, const void* k_rope_f16,
+                          int64_t k_rope_stride, int64_t keys, const int32_t* q_start, const int32_t* kv_start, int64_t requests,
+                          int64_t tokens, int64_t max_q, float scale, void* out_f16, void* workspace, size_t workspace_bytes, void* stream) {
+  if (heads < 1 || heads > 1024 || requests < 0 || requests > 0x7fffffff || tokens < 0 || tokens > 0x7fffffff / heads) return PQ_ERR_SHAPE;
+  if (keys < 0 || keys > 0x7fffffff || max_q < 0 || !std::isfinite(scale)) return PQ_ERR_SHAPE;
+  const int64_t limit = int64_t(1) << 38;   // what a tensor map holds
+  if (q_stride < static_cast<int64_t>(heads) * kQuery || kv_stride < static_cast<int64_t>(heads) * (kNope + kValue) || k_rope_stride < PQ_LATENT_ROPE) return PQ_ERR_SHAPE;
+  if (q_stride % 8 != 0 || kv_stride % 8 != 0 || k_rope_stride % 8 != 0 || q_stride >= limit || kv_stride >= limit || k_rope_stride >= limit) return PQ_ERR_SHAPE;
+  if (requests > PQ_MAX_REQUESTS) return PQ_ERR_LIMIT;
+  if (requests == 0 || tokens == 0) return PQ_OK;
+  if (!q_f16 || !q_start || !kv_start || !out_f16 || (keys > 0 && (!kv_f16 || !k_rope_f16))) return PQ_ERR_NULL;
+  if (!aligned16(q_f16) || !aligned16(kv_f16) || !aligned16(k_rope_f16) || !aligned16(out_f16) || !aligned256(workspace)) return PQ_ERR_ALIGN;
+  int rc = check_arch();
+  if (rc != PQ_OK) return rc;
+  cudaStream_t st = static_cast<cudaStream_t>(stream);
+  if (keys == 0) {   // nothing is seen, and a tensor map needs a row: one of the queries', masked
+    kv_f16 = k_rope_f16 = q_f16;
+    keys = 1;
+  }
+  ExpandedArgs a{q_start, kv_start, static_cast<__half*>(out_f16), tokens, static_cast<int>(requests), heads, scale * 1.44269504f,
+                 0xffffffffu, 0u, 0, nullptr, nullptr, device_status_ptr(), wait_limit()};
+  if (a.status == nullptr) return PQ_ERR_CUDA;
+  if (a.scale_log2 == 0.0f) {
+    a.q_and = 0u, a.scale_log2 = 1.0f;
+  } else if (a.scale_log2 < 0.0f) {
+    a.q_xor = 0x80000000u, a.scale_log2 = -a.scale_log2;
+  }
+  const int sms = sm_count();
+  // Units, at most.  Many of them are handed out whole, in turn; of few, every SM takes an equal share.
+  if (max_q > tokens) max_q = tokens;
+  const int64_t by_rows = tokens / kUnit + requests, by_request = requests * ((max_q + kUnit - 1) / kUnit);
+  const int64_t units = (by_rows < by_request ? by_rows : by_request) * heads;
+  const Scratch sc = scratch_from(workspace, workspace_bytes);
+  if (sc.partials != nullptr && sc.partial_bytes >= expanded_partial_bytes(sms) && units < 3 * sms) {
+    a.shares = 1;
+    a.partials = reinterpret_cast<float*>(sc.partials);
+    a.joins = reinterpret_cast<int4*>(a.partials + static_cast<size_t>(sms) * 2 * kPartFloats);
+  }
+  static PerDeviceOnce once;
+  if ((rc = set_dynamic_smem_once(once, expanded_kernel, kSmem)) != PQ_OK) return rc;
+  // The kernel's register split draws on what the launch holds: a build whose launch holds less must not run.
+  static const int regs = [] {
+    cudaFuncAttributes f = {};
+    return cudaFuncGetAttributes(&f, expanded_kernel) == cudaSuccess ? f.numRegs : 0;
+  }();
+  if (regs * kThreads < kSoft * kSoftRegs + (kThreads - kSoft) * kRestRegs) return PQ_ERR_CUDA;
+  CUtensorMap mq = {}, mkv = {}, mr = {};
+  if ((rc = make_tmap_heads(&mq, q_f16, tokens, heads, kQuery, q_stride, kQuery, kTile)) != PQ_OK) return rc;
+  const bool none = kv_f16 == q_f16;
+  if ((rc = make_tmap_heads(&mkv, kv_f16, keys, none ? 1 : heads, none ? kQuery : kNope + kValue, kv_stride, kNope + kValue, kKeys)) != PQ_OK) return rc;
+  if ((rc = make_tmap_heads(&mr, k_rope_f16, keys, 1, PQ_LATENT_ROPE, k_rope_stride, PQ_LATENT_ROPE, kKeys)) != PQ_OK) return rc;
+  if ((rc = launch_dependent(expanded_kernel, dim3(sms), dim3(kThreads), kSmem, st, mq, mkv, mr, a)) != PQ_OK || !a.shares) return rc;
+  return launch_dependent(expanded_join_kernel, dim3(sms, kUnit / 32, kValue / 32), dim3(kJoinThreads), 0, st, a);
+}
+
+}  // extern "C"

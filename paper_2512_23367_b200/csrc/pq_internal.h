@@ -74,6 +74,11 @@ bool pdl_enabled();
 int make_tmap_2d(CUtensorMap* out, const void* base, uint64_t rows, uint64_t cols, uint32_t box_rows,
                  uint32_t box_cols, uint32_t elem_bytes, int swizzle_bytes);
 
+// FP16 rows of heads, [rows, heads, cols] with the given strides in elements, in boxes of [box_rows, 1, 64] with the
+// 128-byte swizzle.  Strides are multiples of 8.
+int make_tmap_heads(CUtensorMap* out, const void* base, uint64_t rows, uint64_t heads, uint64_t cols, uint64_t row_stride,
+                    uint64_t head_stride, uint32_t box_rows);
+
 // PQ_OK if the current device is compute capability 10.0, else PQ_ERR_ARCH / PQ_ERR_CUDA.
 int check_arch();
 inline bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
@@ -81,6 +86,8 @@ inline bool aligned256(const void* p) { return (reinterpret_cast<uintptr_t>(p) &
 // The rules of pq.h for a paged cache's geometry and pointers.
 int check_kv_cache(const pq_kv_cache* c);
 constexpr int kMostKvHeads = 1024;
+int check_latent_cache(const pq_latent_cache* c);
+size_t expanded_partial_bytes(int sms);   // partial results of pq_expanded_attention
 
 // ---- launchers (each returns a pq_status; all are asynchronous on `stream`) ----
 // col (nullable, [K] FP32): per-column factor applied before the maximum is taken (Eq. 3).

@@ -1,0 +1,522 @@
+// Latent attention, absorbed form: queries in the latent space over the paged cache of latent vectors and rotary keys, on
+// the tcgen05 tensor cores.  See include/pq.h for the contract.
+#include <cuda_fp16.h>
+
+#include <cmath>
+
+#include "pq_attention.h"
+#include "pq_attn_mma.cuh"
+#include "pq_internal.h"
+#include "pq_ptx.cuh"
+#include "pq_schedule.cuh"
+
+namespace pq {
+
+namespace {
+
+constexpr int kRows = 64;            // query rows (token x head) of a CTA
+constexpr int kKeys = 64;            // cached tokens of one step
+constexpr int kPanel = kKeys * 128;  // 64 rows of 64 values
+constexpr int kSoft = 128;           // softmax threads: two per row
+constexpr int kIssuer = 4, kLoader = 5, kThreads = 192;   // warps
+constexpr int kLeastSteps = 2;       // of a CTA, so that its parts are worth joining
+
+template <int kLatent>
+struct LatentCfg {
+  static constexpr int kPanels = kLatent / 64 + 1;        // the last one holds the rotary key
+  static constexpr int kStage = kPanels * kPanel;         // a step's tokens; the queries take the same room
+  static constexpr int kStages = (220 * 1024 - kStage) / kStage;
+  static constexpr int kSmem = (1 + kStages) * kStage + 1024 /* alignment */;
+  static constexpr int kPartFloats = kRows * (kLatent + 2);   // [kLatent / 4][64 rows] x 4 sums, [64 rows] x (reference, sum of weights)
+};
+
+struct LatentArgs {
+  pq_latent_cache c;
+  const int* table;
+  int64_t width;
+  const int* q_start;
+  const int* kv_len;
+  __half* out;
+  int64_t tokens;
+  int requests, heads;
+  int paired;            // two CTAs serve the two halves of a unit of 128 rows
+  float scale_log2;      // > 0
+  uint32_t q_and, q_xor; // a scale of 0 or below is folded into the products: (s & q_and) ^ q_xor
+  float* partials;       // two parts per CTA (nullptr: units are handed out whole, in turn)
+  int4* joins;           // per CTA: first row (a 64-bit number), rows, parts
+  int box;               // tokens of a TMA box: the largest power of two that divides both the page and 64
+  int* status;
+  uint32_t wait_limit;
+
+  __device__ __forceinline__ Request request(int b) const {
+    Request r;
+    r.s = UnitShape{paired ? 2 * kRows : kRows, heads, kKeys, 1};
+    r.q0 = q_start[b];
+    r.n = max(q_start[b + 1] - r.q0, 0);
+    r.k0 = 0;
+    r.L = max(kv_len[b], 0);
+    r.hi = static_cast<int>(min(static_cast<int64_t>(r.L), width * c.page));
+    r.settle();
+    return r;
+  }
+};
+
+// A CTA's units, with the 64 rows of a unit that are its own.
+struct LatentWalk : Walk<LatentArgs> {
+  using Walk<LatentArgs>::Walk;
+  __device__ __forceinline__ int64_t row0() const { return static_cast<int64_t>(tile) * r.s.rows + (a.paired ? (blockIdx.x & 1) * kRows : 0); }
+  __device__ __forceinline__ int rows() const { return static_cast<int>(max(min(r.all - row0(), static_cast<int64_t>(kRows)), static_cast<int64_t>(0))); }
+};
+
+// MMAs with M = 64 in the form that keeps B in place: all 128 lanes of tensor memory take part, lane r and lane 64 + r
+// holding the lower and the upper half of row r's columns.  Per 16 of K: 32 cycles with N = 64 and 80 with 256, the time
+// that shared memory takes to give the operands; the other form of M = 64 takes 32 and 128, and half of the lanes stay empty.
+template <int kAccumulate>
+__device__ __forceinline__ void umma_ws(uint32_t d, uint32_t a_lo, uint32_t b_lo, uint32_t idesc) {
+  asm volatile("{\n\t.reg .pred p;\n\t.reg .b64 a, b;\n\tsetp.ne.b32 p, %4, 0;\n\tmov.b64 a, {%1, %5};\n\tmov.b64 b, {%2, %5};\n\t"
+               "tcgen05.mma.ws.cta_group::1.kind::f16 [%0], a, b, %3, p;\n\t}"
+               ::"r"(d), "r"(a_lo), "r"(b_lo), "r"(idesc), "n"(kAccumulate), "n"(kDescHi) : "memory");
+}
+__device__ __forceinline__ void umma_ws_first(uint32_t d, uint32_t a_lo, uint32_t b_lo, uint32_t idesc, uint32_t accumulate) {
+  asm volatile("{\n\t.reg .pred p;\n\t.reg .b64 a, b;\n\tsetp.ne.b32 p, %4, 0;\n\tmov.b64 a, {%1, %5};\n\tmov.b64 b, {%2, %5};\n\t"
+               "tcgen05.mma.ws.cta_group::1.kind::f16 [%0], a, b, %3, p;\n\t}"
+               ::"r"(d), "r"(a_lo), "r"(b_lo), "r"(idesc), "r"(accumulate), "n"(kDescHi) : "memory");
+}
+
+constexpr uint32_t kBarPair = 1;   // named barriers of the two warps that share 32 rows: two pairs
+
+// A CTA serves 64 rows over its share of the steps.  All heads share the cache, so a row is any (token, head) and a step's
+// 64 tokens are read once for 64 rows: HBM bound up to 64 rows a request; 128 rows, which two CTAs share,
+// are where the tensor cores take about as long.  Per step, with the tokens as panels of 64 values:
+//   S = Q C^T            36 (latent 512) MMAs with N = 64 from shared memory, into one of two 32-column buffers
+//   softmax              two threads per row: S to registers, running maximum, P = 2^(S - reference + 7) as FP16 into the
+//                        panel of the rotary keys, which only this S needed: P is exactly as large
+//   O += P C             8 MMAs with N = 256, C as it lies (values contiguous), O of 64 rows in 256 columns
+// in the order S(u + 1), O(u), so that a softmax runs under the next S.  The reference moves, and O is multiplied, only when
+// the maximum has grown by more than 2^8.
+template <int kLatent>
+__global__ void __launch_bounds__(kThreads, 1)
+latent_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUtensorMap map_c, const LatentArgs a) {
+  using C = LatentCfg<kLatent>;
+  constexpr float kTop = 7.0f;          // a weight at the reference is 2^kTop
+  constexpr int kCols = kLatent / 2;    // tensor memory columns of O
+  extern __shared__ uint8_t smem_raw[];
+  __shared__ __align__(8) uint64_t bars[2 * C::kStages + 11];
+  __shared__ uint32_t s_tmem;
+  __shared__ volatile int s_abort;
+  __shared__ Share s_share;
+  __shared__ int64_t s_sums[kThreads / 32];
+  __shared__ float s_swap[kRows];
+
+  const int tid = threadIdx.x, warp = __shfl_sync(0xffffffffu, tid >> 5, 0), lane = tid & 31;
+  const uint32_t bar_full = smem_u32(bars), bar_free = bar_full + 8 * C::kStages;
+  const uint32_t bar_s = bar_free + 8 * C::kStages, bar_p = bar_s + 16, bar_o = bar_p + 16;   // two of each, steps in turn
+  const uint32_t bar_q = bar_o + 16, bar_qfree = bar_q + 8, bar_read = bar_qfree + 8, bar_fix = bar_read + 8, bar_drain = bar_fix + 8;
+  if (tid == 0) {
+    for (int i = 0; i < C::kStages; ++i) mbar_init(bar_full + 8 * i, 1), mbar_init(bar_free + 8 * i, 1);
+    for (int i = 0; i < 2; ++i) mbar_init(bar_s + 8 * i, 1), mbar_init(bar_p + 8 * i, kSoft / 32), mbar_init(bar_o + 8 * i, 1);
+    mbar_init(bar_q, 1);
+    mbar_init(bar_qfree, 1);
+    mbar_init(bar_read, kSoft / 32);
+    mbar_init(bar_fix, 1);
+    mbar_init(bar_drain, 1);
+    fence_mbar_init();
+    s_abort = 0;
+    tma_prefetch_desc(&map_q), tma_prefetch_desc(&map_c);
+  }
+  if (warp == kIssuer) {
+    tmem_alloc(smem_u32(&s_tmem), 512);
+    tmem_relinquish();
+  }
+  tc_fence_before_sync();
+  grid_dep_wait();
+  const int worker = a.paired ? blockIdx.x >> 1 : blockIdx.x, workers = a.paired ? gridDim.x >> 1 : gridDim.x;
+  const bool shares = a.partials != nullptr;
+  if (shares) find_share<kThreads>(a, worker, workers, kLeastSteps, &s_share, s_sums); else __syncthreads();
+  tc_fence_after_sync();
+  grid_dep_launch();   // only now: a later launch's CTA may take this SM's tensor memory when it is given back
+  const uint32_t tmem = __shfl_sync(0xffffffffu, s_tmem, 0), tmem_s = tmem + kCols;
+  const uint32_t sq = (smem_u32(smem_raw) + 1023u) & ~1023u, ring = sq + C::kStage;
+  const WaitCtx wc{&s_abort, a.wait_limit};
+  uint32_t issued = 0, fixes = 0, units = 0;   // loader: steps requested, of them by way of bar_fix; units
+
+  if (warp == kLoader) {
+    // -------------------------------------------------------------------- loader: queries and cached tokens by TMA
+    // A lane requests one box of one panel (and a second, where small pages make more than 32 of them).
+    const int pieces = kKeys / a.box, boxes = C::kPanels * pieces;
+    const int rows_all = static_cast<int>(a.c.pages * a.c.page);
+    const int y = lane % pieces;   // pieces divides 32
+    bool ok = true;
+    for (LatentWalk w(a, s_share, shares, worker, workers); ok && w.more(); w.next()) {
+      if (w.rows() == 0) continue;
+      if (units > 0) ok = warp_wait(bar_qfree, (units - 1) & 1, wc);
+      if (!ok) break;
+      if (lane == 0) mbar_arrive_expect_tx(bar_q, C::kStage);
+      __syncwarp();
+      if (lane < C::kPanels) tma_load_2d(sq + lane * kPanel, &map_q, bar_q, lane * 64, static_cast<int>(static_cast<int64_t>(w.r.q0) * a.heads + w.row0()));
+      ++units;
+      const int* trow = a.table + static_cast<int64_t>(w.b) * a.width;
+      int id = -1, off = 0;
+      auto look_up = [&](int i) {
+        const int key = (w.step + i) * kKeys + y * a.box;
+        id = -1;
+        if (i >= w.count || key >= w.r.hi) return;
+        const int col = key / a.c.page;
+        off = key - col * a.c.page;
+        id = trow[col];
+      };
+      look_up(0);
+      for (int i = 0; i < w.count; ++i) {
+        const int st = issued % C::kStages;
+        const int row = id < 0 || id >= a.c.pages ? rows_all : id * a.c.page + off;   // beyond the tensor: zeros
+        if (issued >= C::kStages && !(ok = warp_wait(bar_free + 8 * st, ((issued / C::kStages) & 1) ^ 1, wc))) break;
+        const int key0 = (w.step + i) * kKeys;
+        const int dead = min(max(w.r.hi - key0, 0), kKeys);   // first token of the step that was never written
+        const uint32_t dst = ring + st * C::kStage, bar = dead < kKeys ? bar_fix : bar_full + 8 * st;
+        if (lane == 0) mbar_arrive_expect_tx(bar, C::kStage);
+        __syncwarp();
+        for (int x = lane; x < boxes; x += 32) {
+          const int panel = x / pieces;
+          tma_load_2d(dst + panel * kPanel + y * a.box * 128, &map_c, bar, panel * 64, row);
+        }
+        look_up(i + 1);   // used, and so waited for, in the next round
+        ++issued;
+        if (dead < kKeys) {   // 0 x NaN is not 0: the weights' side of such tokens is, their vectors have to be
+          if (!(ok = warp_wait(bar_fix, fixes & 1, wc))) break;
+          ++fixes;
+          for (int j = lane; j < (kKeys - dead) * (kLatent / 8); j += 32) {
+            const int r = dead + j / (kLatent / 8), c = j % (kLatent / 8);
+            asm volatile("st.shared.v4.u32 [%0], {%1, %1, %1, %1};" ::"r"(dst + (c >> 3) * kPanel + r * 128 + (c & 7) * 16), "r"(0) : "memory");
+          }
+          fence_proxy_async_smem();
+          __syncwarp();
+          if (lane == 0) mbar_arrive(bar_full + 8 * st);
+        }
+        __syncwarp();
+      }
+    }
+  } else if (warp == kIssuer) {
+    // -------------------------------------------------------------------- MMA issuer: the whole warp walks, one thread issues
+    constexpr uint32_t id_s = umma_idesc_f16(kKeys, false, kRows), id_o = umma_idesc_f16(256, true, kRows);
+    constexpr uint32_t kUnits16 = C::kStage / 16, kPanel16 = kPanel / 16;
+    const uint32_t leader = elect_one();
+    const uint32_t q_lo = desc_k(sq), k_lo0 = desc_k(ring), v_lo0 = desc_mn(ring, kPanel);
+    uint32_t u = 0, seg = 0;
+    bool ok = true;
+    for (LatentWalk w(a, s_share, shares, worker, workers); ok && w.more(); w.next()) {
+      if (w.rows() == 0) continue;
+      ok = warp_wait(bar_q, seg & 1, wc);
+      for (int i = 0; ok && i <= w.count; ++i) {
+        if (i < w.count) {   // S(u) = Q C^T
+          const uint32_t st = u % C::kStages;
+          if (!(ok = warp_wait(bar_full + 8 * st, (u / C::kStages) & 1, wc))) break;
+          tc_fence_after_sync();
+          if (leader) {
+            const uint32_t d = tmem_s + (u & 1) * (kKeys / 2), kl = k_lo0 + st * kUnits16;
+            umma_ws<0>(d, q_lo, kl, id_s);
+#pragma unroll
+            for (int k = 1; k < 4 * C::kPanels; ++k) umma_ws<1>(d, q_lo + (k / 4) * kPanel16 + (k % 4) * 2, kl + (k / 4) * kPanel16 + (k % 4) * 2, id_s);
+            umma_commit(bar_s + 8 * (u & 1));
+            if (i == w.count - 1) umma_commit(bar_qfree);
+          }
+          __syncwarp();
+          ++u;
+        }
+        if (i > 0) {         // O += P C of the step before
+          const uint32_t v = i < w.count ? u - 2 : u - 1, st = v % C::kStages;
+          if (!(ok = warp_wait(bar_p + 8 * (v & 1), (v >> 1) & 1, wc))) break;
+          if (i == 1 && seg > 0 && !(ok = warp_wait(bar_read, (seg - 1) & 1, wc))) break;   // O of the unit before has been read
+          tc_fence_after_sync();
+          if (leader) {
+            const uint32_t p = k_lo0 + st * kUnits16 + (C::kPanels - 1) * kPanel16, vl = v_lo0 + st * kUnits16;
+#pragma unroll
+            for (int h = 0; h < kLatent / 256; ++h) {
+              umma_ws_first(tmem + 128 * h, p, vl + 4 * h * kPanel16, id_o, i > 1);
+#pragma unroll
+              for (int k = 1; k < kKeys / 16; ++k) umma_ws<1>(tmem + 128 * h, p + 2 * k, vl + 4 * h * kPanel16 + k * 128, id_o);
+            }
+            umma_commit(bar_o + 8 * (v & 1));
+            umma_commit(bar_free + 8 * st);
+          }
+          __syncwarp();
+        }
+      }
+      ++seg;
+    }
+  } else {
+    // -------------------------------------------------------------------- softmax, two threads per row
+    const int r = tid & 63, half = warp >> 1;      // the thread's 32 tokens of a step, its halves of the sums
+    const uint32_t lane_off = static_cast<uint32_t>(warp) << 21;   // 32 lanes per warp, lane in bits 16 and up
+    const uint32_t pair = kBarPair + (warp & 1);
+    float* swap = s_swap + r;
+    const float sc = a.scale_log2;
+    const uint64_t sc2 = pair_f32(sc, sc);
+    uint32_t u = 0;
+    int4 join = make_int4(0, 0, 0, 0);
+    bool ok = true;
+    for (LatentWalk w(a, s_share, shares, worker, workers); w.more(); w.next()) {
+      if (w.rows() == 0) continue;
+      const int rows = w.rows(), shift = w.r.L - w.r.n;
+      const int64_t row0 = w.row0(), row = row0 + r;
+      const bool live = r < rows;
+      const int p0 = shift + static_cast<int>(row0 / a.heads);                  // the first row's position
+      const int see_to = live ? min(shift + static_cast<int>(row / a.heads), w.r.hi - 1) - 32 * half : -1;   // from the thread's first token
+      const int all_to = min(p0 + 1, w.r.hi);                                     // every row sees the tokens before
+      float m = -INFINITY, l = 0.0f;   // m: the reference, in powers of two; l: the thread's own tokens
+      for (int i = 0; i < w.count; ++i, ++u) {
+        const int key0 = (w.step + i) * kKeys;
+        ok = ok && warp_wait(bar_s + 8 * (u & 1), (u >> 1) & 1, wc);
+        tc_fence_after_sync();
+        uint32_t s[32];
+        tmem_ld_32x32(tmem_s + (u & 1) * (kKeys / 2) + lane_off, s);
+        tmem_ld_wait();
+        if (a.q_xor != 0u || a.q_and == 0u) {
+#pragma unroll
+          for (int j = 0; j < 32; ++j) s[j] = (s[j] & a.q_and) ^ a.q_xor;
+        }
+        if (key0 + kKeys > all_to || rows < kRows) {
+          const int to = see_to - key0;
+#pragma unroll
+          for (int j = 0; j < 32; ++j)
+            if (j > to) s[j] = 0xff800000u;   // -inf
+        }
+        float top[4];
+#pragma unroll
+        for (int h = 0; h < 4; ++h) {
+          const uint32_t* v = s + 8 * h;
+          top[h] = max3(__uint_as_float(v[0]), __uint_as_float(v[1]), __uint_as_float(v[2]));
+          top[h] = max3(top[h], __uint_as_float(v[3]), __uint_as_float(v[4]));
+          top[h] = max3(top[h], __uint_as_float(v[5]), __uint_as_float(v[6]));
+          top[h] = fmaxf(top[h], __uint_as_float(v[7]));
+        }
+        float t = fmaxf(max3(top[0], top[1], top[2]), top[3]) * sc;
+        if (pair_any(pair, t > m + 8.0f)) {   // rare after the first steps: some row of the 32
+          t = pair_combine<false>(swap, pair, half, t);
+          const bool grown = t > m + 8.0f;
+          const float f = grown ? (m == -INFINITY ? 0.0f : exp2_approx(m - t)) : 1.0f;
+          if (grown) m = t;
+          l *= f;
+          if (i > 0) {   // O holds the sums up to the step before
+            ok = ok && warp_wait(bar_o + 8 * ((u - 1) & 1), ((u - 1) >> 1) & 1, wc);
+            tc_fence_after_sync();
+#pragma unroll 1
+            for (int c = 0; c < kCols; c += 32) {
+              uint32_t o[32];
+              tmem_ld_32x32(tmem + c + lane_off, o);
+              tmem_ld_wait();
+#pragma unroll
+              for (int j = 0; j < 32; ++j) o[j] = __float_as_uint(__uint_as_float(o[j]) * f);
+              tmem_st_32x32(tmem + c + lane_off, o);
+            }
+            tmem_st_wait();
+          }
+        }
+        const float off = kTop - (m == -INFINITY ? 0.0f : m);
+        const uint64_t off2 = pair_f32(off, off);
+        uint64_t sum = 0;
+        uint32_t q[16];
+#pragma unroll
+        for (int j = 0; j < 16; ++j) {
+          float e0, e1;
+          unpair_f32(fma_f32x2(pair_f32(__uint_as_float(s[2 * j]), __uint_as_float(s[2 * j + 1])), sc2, off2), e0, e1);
+          e0 = exp2_approx(e0);
+          e1 = exp2_approx(e1);
+          sum = add_f32x2(sum, pair_f32(e0, e1));
+          q[j] = pack_f16(e0, e1);
+        }
+        float l0, l1;
+        unpair_f32(sum, l0, l1);
+        l += l0 + l1;
+        const uint32_t to = ring + (u % C::kStages) * C::kStage + (C::kPanels - 1) * kPanel + r * 128;
+#pragma unroll
+        for (int c = 0; c < 4; ++c)
+          asm volatile("st.shared.v4.u32 [%0], {%1, %2, %3, %4};" ::"r"(to + (((4 * half + c) ^ (r & 7)) << 4)),
+                       "r"(q[4 * c]), "r"(q[4 * c + 1]), "r"(q[4 * c + 2]), "r"(q[4 * c + 3]) : "memory");
+        fence_proxy_async_smem();
+        tc_fence_before_sync();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(bar_p + 8 * (u & 1));
+      }
+      // ------------------------------------------------------------------ the unit's (or part's) end
+      ok = ok && warp_wait(bar_o + 8 * ((u - 1) & 1), ((u - 1) >> 1) & 1, wc);
+      tc_fence_after_sync();
+      l = pair_combine<true>(swap, pair, half, l);
+      const int64_t at = static_cast<int64_t>(w.r.q0) * a.heads + row;   // of the output
+      const bool writes = live && at >= 0 && at < a.tokens * a.heads;
+      if (w.whole()) {
+        const float inv = l > 0.0f ? 1.0f / l : 0.0f;
+#pragma unroll 1
+        for (int c = 0; c < kCols; c += 32) {
+          uint32_t o[32];
+          tmem_ld_32x32(tmem + c + lane_off, o);
+          tmem_ld_wait();
+          // columns 128 h .. of tensor memory are the values 256 h + 128 half ..
+          uint4* to = reinterpret_cast<uint4*>(a.out + at * kLatent + (c >> 7) * 256 + half * 128 + (c & 127));
+          if (writes) {
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+              uint32_t x[4];
+#pragma unroll
+              for (int k = 0; k < 4; ++k) x[k] = pack_f16(__uint_as_float(o[8 * j + 2 * k]) * inv, __uint_as_float(o[8 * j + 2 * k + 1]) * inv);
+              to[j] = make_uint4(x[0], x[1], x[2], x[3]);
+            }
+          }
+        }
+      } else {
+        const bool begins = w.step == 0;
+        float* pp = a.partials + (2 * static_cast<int64_t>(blockIdx.x) + begins) * C::kPartFloats;
+#pragma unroll 1
+        for (int c = 0; c < kCols; c += 32) {
+          uint32_t o[32];
+          tmem_ld_32x32(tmem + c + lane_off, o);
+          tmem_ld_wait();
+          float4* to = reinterpret_cast<float4*>(pp) + (((c >> 7) * 256 + half * 128 + (c & 127)) / 4) * kRows + r;
+          if (writes) {
+#pragma unroll
+            for (int j = 0; j < 8; ++j)
+              to[j * kRows] = make_float4(__uint_as_float(o[4 * j]), __uint_as_float(o[4 * j + 1]), __uint_as_float(o[4 * j + 2]), __uint_as_float(o[4 * j + 3]));
+          }
+        }
+        if (writes && half == 0) reinterpret_cast<float2*>(pp + kRows * kLatent)[r] = make_float2(m, l);
+        if (begins) {
+          const int64_t first = static_cast<int64_t>(w.r.q0) * a.heads + row0;
+          join = make_int4(static_cast<int>(first & 0xffffffff), static_cast<int>(first >> 32), rows,
+                           1 + (w.all_steps - w.count + s_share.per - 1) / s_share.per);
+        }
+      }
+      tc_fence_before_sync();
+      __syncwarp();
+      if (lane == 0) mbar_arrive(bar_read);
+    }
+    if (a.partials && tid == 0) a.joins[blockIdx.x] = join;
+  }
+
+  // ---------------------------------------------------------------------- teardown
+  tc_fence_before_sync();
+  __syncthreads();
+  tc_fence_after_sync();
+  if (s_abort) {
+    // Some role gave up.  What has been handed to the hardware still completes by itself and must have done so before shared
+    // and tensor memory go away: the loader's copies and the issuer's MMAs.
+    if (warp == kIssuer && elect_one()) {
+      umma_commit(bar_drain);
+      mbar_drain(bar_drain, 0u);
+    }
+    if (warp == kLoader && lane == 0) {
+      for (uint32_t i = issued > C::kStages ? issued - C::kStages : 0; i < issued; ++i) mbar_drain(bar_full + 8 * (i % C::kStages), (i / C::kStages) & 1);
+      mbar_drain(bar_fix, fixes & 1);
+      if (units > 0) mbar_drain(bar_q, (units - 1) & 1);
+    }
+    __syncthreads();
+    if (tid == 0) atomicExch(a.status, static_cast<int>(PQ_ERR_TIMEOUT));
+  }
+  if (warp == kIssuer) tmem_dealloc(tmem, 512);
+}
+
+// Joins the parts of units that were cut: a block per CTA that had a unit's first part and 16 values, a thread per row and
+// 4 of them, lanes along the rows.  L2 latency, so the loads of several parts are in flight together.
+constexpr int kJoinThreads = 256;
+template <int kLatent>
+__global__ void __launch_bounds__(kJoinThreads) latent_join_kernel(const LatentArgs a) {
+  grid_dep_launch();
+  grid_dep_wait();
+  const int4 join = a.joins[blockIdx.x];
+  const int r = threadIdx.x & 63, f4 = blockIdx.y * 4 + (threadIdx.x >> 6);
+  if (r >= join.z) return;
+  const int64_t at = (static_cast<int64_t>(join.y) << 32 | static_cast<uint32_t>(join.x)) + r;
+  if (at < 0 || at >= a.tokens * a.heads) return;
+  constexpr int kPart = LatentCfg<kLatent>::kPartFloats;
+  const int next = a.paired ? 2 : 1;
+  // the unit's first part is the second one of its CTA, the others the first of theirs
+  auto part = [&](int i) { return a.partials + (2 * (static_cast<int64_t>(blockIdx.x) + i * next) + (i == 0)) * kPart; };
+  float M = -INFINITY, L = 0.0f;
+  float4 v = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+  constexpr int kBatch = 8;
+  for (int i0 = 0; i0 < join.w; i0 += kBatch) {
+    float2 ml[kBatch];
+    float4 x[kBatch];
+#pragma unroll
+    for (int j = 0; j < kBatch; ++j) {
+      const float* p = part(min(i0 + j, join.w - 1));
+      ml[j] = __ldcg(reinterpret_cast<const float2*>(p + kRows * kLatent) + r);
+      x[j] = __ldcg(reinterpret_cast<const float4*>(p) + f4 * kRows + r);
+    }
+    float top = M;
+#pragma unroll
+    for (int j = 0; j < kBatch; ++j) top = fmaxf(top, ml[j].x);
+    const float ref = top == -INFINITY ? 0.0f : top, f = exp2_approx(M - ref);
+    M = top;
+    L *= f, v.x *= f, v.y *= f, v.z *= f, v.w *= f;
+#pragma unroll
+    for (int j = 0; j < kBatch; ++j) {
+      const float w = i0 + j < join.w ? exp2_approx(ml[j].x - ref) : 0.0f;
+      L = fmaf(ml[j].y, w, L);
+      v.x = fmaf(x[j].x, w, v.x), v.y = fmaf(x[j].y, w, v.y), v.z = fmaf(x[j].z, w, v.z), v.w = fmaf(x[j].w, w, v.w);
+    }
+  }
+  const float inv = L > 0.0f ? 1.0f / L : 0.0f;
+  *reinterpret_cast<uint2*>(a.out + at * kLatent + 4 * f4) = make_uint2(pack_f16(v.x * inv, v.y * inv), pack_f16(v.z * inv, v.w * inv));
+}
+
+size_t partial_bytes(int latent, int sms) { return static_cast<size_t>(sms) * (2 * kRows * (latent + 2) * sizeof(float) + sizeof(int4)); }
+
+template <int kLatent>
+int launch(LatentArgs& a, const void* q, int sms, cudaStream_t stream) {
+  using C = LatentCfg<kLatent>;
+  auto kern = latent_kernel<kLatent>;
+  static PerDeviceOnce once;
+  if (const int rc = set_dynamic_smem_once(once, kern, C::kSmem); rc != PQ_OK) return rc;
+  CUtensorMap mq = {}, mc = {};
+  const uint64_t wide = kLatent + PQ_LATENT_ROPE;
+  if (const int rc = make_tmap_2d(&mq, q, static_cast<uint64_t>(a.tokens) * a.heads, wide, kRows, 64, 2, 128); rc != PQ_OK) return rc;
+  if (const int rc = make_tmap_2d(&mc, a.c.data, static_cast<uint64_t>(a.c.pages) * a.c.page, wide, a.box, 64, 2, 128); rc != PQ_OK) return rc;
+  const unsigned grid = static_cast<unsigned>(a.paired ? sms & ~1 : sms);
+  if (const int rc = launch_dependent(kern, dim3(grid), dim3(kThreads), C::kSmem, stream, mq, mc, a); rc != PQ_OK || !a.partials) return rc;
+  return launch_dependent(latent_join_kernel<kLatent>, dim3(grid, kLatent / 16), dim3(kJoinThreads), 0, stream, a);
+}
+
+}  // namespace
+}  // namespace pq
+
+using namespace pq;
+
+extern "C" {
+
+int pq_latent_attention(const void* q_f16, int32_t heads, const pq_latent_cache* cache, const int32_t* block_table, int64_t width,
+                        const int32_t* q_start, const int32_t* kv_len, int64_t requests, int64_t tokens, float scale, void* out_f16,
+                        void* workspace, size_t workspace_bytes, void* stream) {
+  int rc = check_latent_cache(cache);
+  if (rc != PQ_OK) return rc;
+  if (heads < 1 || heads > 1024 || requests < 0 || requests > 0x7fffffff || tokens < 0 || tokens > 0x7fffffff / heads) return PQ_ERR_SHAPE;
+  if (width < 1 || width > 0x7fffffff || !std::isfinite(scale)) return PQ_ERR_SHAPE;
+  if (requests > PQ_MAX_REQUESTS) return PQ_ERR_LIMIT;
+  if (requests == 0 || tokens == 0) return PQ_OK;
+  if (!q_f16 || !block_table || !q_start || !kv_len || !out_f16) return PQ_ERR_NULL;
+  if (!aligned16(q_f16) || !aligned16(out_f16) || !aligned256(workspace)) return PQ_ERR_ALIGN;
+  if ((rc = check_arch()) != PQ_OK) return rc;
+  LatentArgs a{*cache, block_table, width, q_start, kv_len, static_cast<__half*>(out_f16), tokens, static_cast<int>(requests), heads,
+               0, scale * 1.44269504f, 0xffffffffu, 0u, nullptr, nullptr, kKeys, device_status_ptr(), wait_limit()};
+  if (a.status == nullptr) return PQ_ERR_CUDA;
+  while (cache->page % a.box != 0) a.box /= 2;   // the page is a multiple of 16
+  if (a.scale_log2 == 0.0f) {
+    a.q_and = 0u, a.scale_log2 = 1.0f;
+  } else if (a.scale_log2 < 0.0f) {
+    a.q_xor = 0x80000000u, a.scale_log2 = -a.scale_log2;
+  }
+  a.paired = static_cast<int64_t>(tokens) * heads > kRows * requests;   // more than 64 rows a request, on average
+  const int sms = sm_count();
+  const Scratch sc = scratch_from(workspace, workspace_bytes);
+  if (sc.partials != nullptr && sc.partial_bytes >= partial_bytes(cache->latent, sms)) {
+    a.partials = reinterpret_cast<float*>(sc.partials);
+    a.joins = reinterpret_cast<int4*>(a.partials + static_cast<size_t>(sms) * 2 * kRows * (cache->latent + 2));
+  }
+  return cache->latent == 512 ? launch<512>(a, q_f16, sms, static_cast<cudaStream_t>(stream)) : launch<256>(a, q_f16, sms, static_cast<cudaStream_t>(stream));
+}
+
+size_t pq_latent_workspace_bytes(int32_t sms) {
+  if (sms < 1) return 0;
+  const size_t absorbed = partial_bytes(512, sms), expanded = expanded_partial_bytes(sms);
+  return kScratchHeaderBytes + (absorbed > expanded ? absorbed : expanded);
+}
+
+}  // extern "C"
