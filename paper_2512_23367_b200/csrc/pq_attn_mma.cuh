@@ -61,11 +61,12 @@ __device__ __forceinline__ void tmem_st_wait() { asm volatile("tcgen05.wait::st.
 __device__ __forceinline__ void named_bar_arrive(uint32_t id, uint32_t nthreads) {
   asm volatile("bar.arrive %0, %1;" ::"r"(id), "r"(nthreads) : "memory");
 }
-// Meets the other warp of the pair; whether any of the 64 threads says yes.
+// Meets the other warps that share the barrier (of the pair: 64 threads); whether any of their threads says yes.
+template <int kThreads = 64>
 __device__ __forceinline__ bool pair_any(uint32_t id, bool yes) {
   uint32_t r;
-  asm volatile("{\n\t.reg .pred p, q;\n\tsetp.ne.b32 p, %2, 0;\n\tbar.red.or.pred q, %1, 64, p;\n\tselp.u32 %0, 1, 0, q;\n\t}"
-               : "=r"(r) : "r"(id), "r"(static_cast<uint32_t>(yes)) : "memory");
+  asm volatile("{\n\t.reg .pred p, q;\n\tsetp.ne.b32 p, %2, 0;\n\tbar.red.or.pred q, %1, %3, p;\n\tselp.u32 %0, 1, 0, q;\n\t}"
+               : "=r"(r) : "r"(id), "r"(static_cast<uint32_t>(yes)), "n"(kThreads) : "memory");
   return r != 0;
 }
 
@@ -127,7 +128,12 @@ __device__ __forceinline__ float max3(float a, float b, float c) {
 __device__ __forceinline__ bool warp_wait(uint32_t bar, uint32_t parity, const WaitCtx& wc) {
   return __all_sync(0xffffffffu, mbar_wait(bar, parity, wc));
 }
-
+// Whether a phase has completed, asked by one lane for the warp.
+__device__ __forceinline__ bool warp_test(uint32_t bar, uint32_t parity) {
+  uint32_t done = 0;
+  if ((threadIdx.x & 31) == 0) done = mbar_test(bar, parity);
+  return __shfl_sync(0xffffffffu, done, 0) != 0;
+}
 __device__ __forceinline__ int warp_prefix(int v, int lane) {   // inclusive sums
 #pragma unroll
   for (int o = 1; o < 32; o <<= 1) {

@@ -50,7 +50,7 @@ struct ExpandedArgs {
     Request r;
     r.s = UnitShape{kUnit, 1, kKeys, heads};
     r.q0 = q_start[b];
-    r.n = max(q_start[b + 1] - r.q0, 0);
+    r.n = static_cast<int>(min(static_cast<int64_t>(max(q_start[b + 1] - r.q0, 0)), tokens));
     r.k0 = kv_start[b];
     r.L = r.hi = max(kv_start[b + 1] - r.k0, 0);
     r.settle();

@@ -17,17 +17,25 @@ namespace {
 constexpr int kRows = 64;            // query rows (token x head) of a CTA
 constexpr int kKeys = 64;            // cached tokens of one step
 constexpr int kPanel = kKeys * 128;  // 64 rows of 64 values
-constexpr int kSoft = 128;           // softmax threads: two per row
-constexpr int kIssuer = 4, kLoader = 5, kThreads = 192;   // warps
+constexpr int kSoft = 256;           // softmax threads: four per row
+constexpr int kIssuer = 8, kLoader = 9, kWatcher = 10, kAhead = 11, kThreads = 384;   // warps
+constexpr int kDistance = 6;         // steps that tokens are brought into L2 ahead of their use
 constexpr int kLeastSteps = 2;       // of a CTA, so that its parts are worth joining
 
 template <int kLatent>
 struct LatentCfg {
-  static constexpr int kPanels = kLatent / 64 + 1;        // the last one holds the rotary key
-  static constexpr int kStage = kPanels * kPanel;         // a step's tokens; the queries take the same room
-  static constexpr int kStages = (220 * 1024 - kStage) / kStage;
-  static constexpr int kSmem = (1 + kStages) * kStage + 1024 /* alignment */;
+  static constexpr int kPanels = kLatent / 64 + 1;        // of a row: the last one holds the rotary values
+  static constexpr int kValuePanels = kLatent / 64;
+  static constexpr int kGroups = kLatent / 256;           // panels are brought in and given back four at a time, the values of one MMA
+  // Queries lie in tensor memory, as many panels of them as there is room for, the others in shared memory.
+  static constexpr int kHeld = kLatent == 512 ? 7 : kPanels, kQueryPanels = kPanels - kHeld;
+  static constexpr int kStages = kLatent == 512 ? 3 : 6;   // steps whose latent vectors fit at once
+  static constexpr int kStage = kValuePanels * kPanel, kStep = kPanels * kPanel;
+  static constexpr int kSmem = kQueryPanels * kPanel + kStages * kStage + 2 * kPanel /* rotary keys, P */ + 1024 /* alignment */;
   static constexpr int kPartFloats = kRows * (kLatent + 2);   // [kLatent / 4][64 rows] x 4 sums, [64 rows] x (reference, sum of weights)
+  // Tensor memory columns: O; S; the queries, two FP16 values each.
+  static constexpr uint32_t kCols = kLatent / 2, kColS = kCols, kColQ = kColS + kKeys / 2;
+  static_assert(kColQ + 32 * kHeld <= 512, "tensor memory");
 };
 
 struct LatentArgs {
@@ -36,6 +44,7 @@ struct LatentArgs {
   int64_t width;
   const int* q_start;
   const int* kv_len;
+  const __half* q;
   __half* out;
   int64_t tokens;
   int requests, heads;
@@ -52,7 +61,7 @@ struct LatentArgs {
     Request r;
     r.s = UnitShape{paired ? 2 * kRows : kRows, heads, kKeys, 1};
     r.q0 = q_start[b];
-    r.n = max(q_start[b + 1] - r.q0, 0);
+    r.n = static_cast<int>(min(static_cast<int64_t>(max(q_start[b + 1] - r.q0, 0)), tokens));
     r.k0 = 0;
     r.L = max(kv_len[b], 0);
     r.hi = static_cast<int>(min(static_cast<int64_t>(r.L), width * c.page));
@@ -64,8 +73,8 @@ struct LatentArgs {
 // A CTA's units, with the 64 rows of a unit that are its own.
 struct LatentWalk : Walk<LatentArgs> {
   using Walk<LatentArgs>::Walk;
-  __device__ __forceinline__ int64_t row0() const { return static_cast<int64_t>(tile) * r.s.rows + (a.paired ? (blockIdx.x & 1) * kRows : 0); }
-  __device__ __forceinline__ int rows() const { return static_cast<int>(max(min(r.all - row0(), static_cast<int64_t>(kRows)), static_cast<int64_t>(0))); }
+  __device__ __forceinline__ int row0() const { return tile * r.s.rows + (a.paired ? (blockIdx.x & 1) * kRows : 0); }
+  __device__ __forceinline__ int rows() const { return max(min(static_cast<int>(r.all) - row0(), kRows), 0); }
 };
 
 // MMAs with M = 64 in the form that keeps B in place: all 128 lanes of tensor memory take part, lane r and lane 64 + r
@@ -82,8 +91,30 @@ __device__ __forceinline__ void umma_ws_first(uint32_t d, uint32_t a_lo, uint32_
                "tcgen05.mma.ws.cta_group::1.kind::f16 [%0], a, b, %3, p;\n\t}"
                ::"r"(d), "r"(a_lo), "r"(b_lo), "r"(idesc), "r"(accumulate), "n"(kDescHi) : "memory");
 }
+// A in tensor memory, row r in lane r and again in lane 64 + r, which multiplies it with the upper half of the columns.
+template <int kAccumulate>
+__device__ __forceinline__ void umma_ws_ts(uint32_t d, uint32_t a, uint32_t b_lo, uint32_t idesc) {
+  asm volatile("{\n\t.reg .pred p;\n\t.reg .b64 b;\n\tsetp.ne.b32 p, %4, 0;\n\tmov.b64 b, {%2, %5};\n\t"
+               "tcgen05.mma.ws.cta_group::1.kind::f16 [%0], [%1], b, %3, p;\n\t}"
+               ::"r"(d), "r"(a), "r"(b_lo), "r"(idesc), "n"(kAccumulate), "n"(kDescHi) : "memory");
+}
 
-constexpr uint32_t kBarPair = 1;   // named barriers of the two warps that share 32 rows: two pairs
+// The sum, or the largest, of a value of the row's four threads, the same in all: `mine` is the thread's word, the others'
+// lie 64 floats apart.
+template <bool kSum>
+__device__ __forceinline__ float row_combine(float* mine, const float* row, uint32_t id, float v) {
+  *mine = v;
+  named_bar_sync(id, 128);
+  const float a = row[0], b = row[kRows], c = row[2 * kRows], d = row[3 * kRows];
+  named_bar_sync(id, 128);
+  return kSum ? (a + b) + (c + d) : fmaxf(fmaxf(a, b), fmaxf(c, d));
+}
+
+// Named barriers: the four warps that share 32 rows (two of them); "operands landed", between the watcher's and the issuer's
+// warp; "S read" and "P written", 256 threads to the issuer's (S of the next step is only there when the issuer has had both).
+// They do not pass through shared memory, which the tensor core
+// keeps busy: with mbarriers, polled for in whichever order they came, a step took 3200 cycles.
+constexpr uint32_t kBarRow = 1, kBarTile = 3, kBarRead = 4, kBarP = 5;
 
 // A CTA serves 64 rows over its share of the steps.  All heads share the cache, so a row is any (token, head) and a step's
 // 64 tokens are read once for 64 rows: HBM bound up to 64 rows a request; 128 rows, which two CTAs share,
@@ -99,29 +130,31 @@ __global__ void __launch_bounds__(kThreads, 1)
 latent_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUtensorMap map_c, const LatentArgs a) {
   using C = LatentCfg<kLatent>;
   constexpr float kTop = 7.0f;          // a weight at the reference is 2^kTop
-  constexpr int kCols = kLatent / 2;    // tensor memory columns of O
+  constexpr int kCols = C::kCols;
   extern __shared__ uint8_t smem_raw[];
-  __shared__ __align__(8) uint64_t bars[2 * C::kStages + 11];
+  __shared__ __align__(8) uint64_t bars[2 * C::kStages * C::kGroups + 9];
   __shared__ uint32_t s_tmem;
   __shared__ volatile int s_abort;
+  __shared__ volatile uint32_t s_landed;   // steps
   __shared__ Share s_share;
   __shared__ int64_t s_sums[kThreads / 32];
-  __shared__ float s_swap[kRows];
+  __shared__ float s_swap[4][kRows];
 
   const int tid = threadIdx.x, warp = __shfl_sync(0xffffffffu, tid >> 5, 0), lane = tid & 31;
-  const uint32_t bar_full = smem_u32(bars), bar_free = bar_full + 8 * C::kStages;
-  const uint32_t bar_s = bar_free + 8 * C::kStages, bar_p = bar_s + 16, bar_o = bar_p + 16;   // two of each, steps in turn
-  const uint32_t bar_q = bar_o + 16, bar_qfree = bar_q + 8, bar_read = bar_qfree + 8, bar_fix = bar_read + 8, bar_drain = bar_fix + 8;
+  // Of every stage's groups, of the rotary keys: they are there, they are free.  S is there; O has been summed.
+  const uint32_t bar_full = smem_u32(bars), bar_free = bar_full + 8 * C::kStages * C::kGroups, bar_rope = bar_free + 8 * C::kStages * C::kGroups;
+  const uint32_t bar_rfree = bar_rope + 8, bar_s = bar_rfree + 8, bar_o = bar_s + 8;
+  // A unit's queries are there, are free; its sums have been read.
+  const uint32_t bar_q = bar_o + 8, bar_qfree = bar_q + 8, bar_read = bar_qfree + 8, bar_fix = bar_read + 8, bar_drain = bar_fix + 8;
   if (tid == 0) {
-    for (int i = 0; i < C::kStages; ++i) mbar_init(bar_full + 8 * i, 1), mbar_init(bar_free + 8 * i, 1);
-    for (int i = 0; i < 2; ++i) mbar_init(bar_s + 8 * i, 1), mbar_init(bar_p + 8 * i, kSoft / 32), mbar_init(bar_o + 8 * i, 1);
-    mbar_init(bar_q, 1);
+    for (int i = 0; i < 2 * C::kStages * C::kGroups + 4; ++i) mbar_init(bar_full + 8 * i, 1);   // up to bar_o
+    mbar_init(bar_q, kSoft / 32 + (C::kQueryPanels > 0 ? 1 : 0));
     mbar_init(bar_qfree, 1);
     mbar_init(bar_read, kSoft / 32);
     mbar_init(bar_fix, 1);
     mbar_init(bar_drain, 1);
     fence_mbar_init();
-    s_abort = 0;
+    s_abort = 0, s_landed = 0;
     tma_prefetch_desc(&map_q), tma_prefetch_desc(&map_c);
   }
   if (warp == kIssuer) {
@@ -135,26 +168,26 @@ latent_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__
   if (shares) find_share<kThreads>(a, worker, workers, kLeastSteps, &s_share, s_sums); else __syncthreads();
   tc_fence_after_sync();
   grid_dep_launch();   // only now: a later launch's CTA may take this SM's tensor memory when it is given back
-  const uint32_t tmem = __shfl_sync(0xffffffffu, s_tmem, 0), tmem_s = tmem + kCols;
-  const uint32_t sq = (smem_u32(smem_raw) + 1023u) & ~1023u, ring = sq + C::kStage;
+  const uint32_t tmem = __shfl_sync(0xffffffffu, s_tmem, 0), tmem_s = tmem + C::kColS;
+  const uint32_t sq = (smem_u32(smem_raw) + 1023u) & ~1023u, ring = sq + C::kQueryPanels * kPanel, rope = ring + C::kStages * C::kStage, weights = rope + kPanel;
   const WaitCtx wc{&s_abort, a.wait_limit};
   uint32_t issued = 0, fixes = 0, units = 0;   // loader: steps requested, of them by way of bar_fix; units
 
   if (warp == kLoader) {
-    // -------------------------------------------------------------------- loader: queries and cached tokens by TMA
-    // A lane requests one box of one panel (and a second, where small pages make more than 32 of them).
-    const int pieces = kKeys / a.box, boxes = C::kPanels * pieces;
+    // -------------------------------------------------------------------- loader: a lane requests one box of one panel of a group
+    const int pieces = kKeys / a.box;
     const int rows_all = static_cast<int>(a.c.pages * a.c.page);
-    const int y = lane % pieces;   // pieces divides 32
+    const int panel = lane / pieces, y = lane - panel * pieces;
     bool ok = true;
     for (LatentWalk w(a, s_share, shares, worker, workers); ok && w.more(); w.next()) {
       if (w.rows() == 0) continue;
-      if (units > 0) ok = warp_wait(bar_qfree, (units - 1) & 1, wc);
-      if (!ok) break;
-      if (lane == 0) mbar_arrive_expect_tx(bar_q, C::kStage);
-      __syncwarp();
-      if (lane < C::kPanels) tma_load_2d(sq + lane * kPanel, &map_q, bar_q, lane * 64, static_cast<int>(static_cast<int64_t>(w.r.q0) * a.heads + w.row0()));
-      ++units;
+      if (C::kQueryPanels > 0) {
+        if (units > 0 && !(ok = warp_wait(bar_qfree, (units - 1) & 1, wc))) break;
+        if (lane == 0) mbar_arrive_expect_tx(bar_q, C::kQueryPanels * kPanel);
+        __syncwarp();
+        if (lane < C::kQueryPanels) tma_load_2d(sq + lane * kPanel, &map_q, bar_q, (C::kHeld + lane) * 64, w.r.q0 * a.heads + w.row0());
+        ++units;
+      }
       const int* trow = a.table + static_cast<int64_t>(w.b) * a.width;
       int id = -1, off = 0;
       auto look_up = [&](int i) {
@@ -167,88 +200,166 @@ latent_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__
       };
       look_up(0);
       for (int i = 0; i < w.count; ++i) {
-        const int st = issued % C::kStages;
+        const uint32_t st = issued % C::kStages, phase = (issued / C::kStages) & 1;
         const int row = id < 0 || id >= a.c.pages ? rows_all : id * a.c.page + off;   // beyond the tensor: zeros
-        if (issued >= C::kStages && !(ok = warp_wait(bar_free + 8 * st, ((issued / C::kStages) & 1) ^ 1, wc))) break;
-        const int key0 = (w.step + i) * kKeys;
-        const int dead = min(max(w.r.hi - key0, 0), kKeys);   // first token of the step that was never written
-        const uint32_t dst = ring + st * C::kStage, bar = dead < kKeys ? bar_fix : bar_full + 8 * st;
-        if (lane == 0) mbar_arrive_expect_tx(bar, C::kStage);
-        __syncwarp();
-        for (int x = lane; x < boxes; x += 32) {
-          const int panel = x / pieces;
-          tma_load_2d(dst + panel * kPanel + y * a.box * 128, &map_c, bar, panel * 64, row);
+        const int dead = min(max(w.r.hi - (w.step + i) * kKeys, 0), kKeys);   // first token of the step that was never written
+        const uint32_t dst = ring + st * C::kStage + y * a.box * 128;
+        if (dead < kKeys && lane == 0) mbar_arrive_expect_tx(bar_fix, C::kStep);
+#pragma unroll
+        for (int g = 0; g < C::kGroups; ++g) {
+          const uint32_t full = bar_full + 8 * (st * C::kGroups + g);
+          if (ok && issued >= C::kStages) ok = warp_wait(bar_free + 8 * (st * C::kGroups + g), phase ^ 1, wc);
+          if (ok && dead == kKeys && lane == 0) mbar_arrive_expect_tx(full, 4 * kPanel);
+          __syncwarp();
+          if (ok && panel < 4) tma_load_2d(dst + (4 * g + panel) * kPanel, &map_c, dead < kKeys ? bar_fix : full, (4 * g + panel) * 64, row);
         }
+        if (ok && issued > 0) ok = warp_wait(bar_rfree, (issued & 1) ^ 1, wc);
+        if (!ok) break;
+        if (dead == kKeys && lane == 0) mbar_arrive_expect_tx(bar_rope, kPanel);
+        __syncwarp();
+        if (panel == 0) tma_load_2d(rope + y * a.box * 128, &map_c, dead < kKeys ? bar_fix : bar_rope, kLatent, row);
         look_up(i + 1);   // used, and so waited for, in the next round
         ++issued;
-        if (dead < kKeys) {   // 0 x NaN is not 0: the weights' side of such tokens is, their vectors have to be
+        if (dead < kKeys) {   // 0 x NaN is not 0: the weights of such tokens are, their vectors have to be
           if (!(ok = warp_wait(bar_fix, fixes & 1, wc))) break;
           ++fixes;
           for (int j = lane; j < (kKeys - dead) * (kLatent / 8); j += 32) {
             const int r = dead + j / (kLatent / 8), c = j % (kLatent / 8);
-            asm volatile("st.shared.v4.u32 [%0], {%1, %1, %1, %1};" ::"r"(dst + (c >> 3) * kPanel + r * 128 + (c & 7) * 16), "r"(0) : "memory");
+            asm volatile("st.shared.v4.u32 [%0], {%1, %1, %1, %1};" ::"r"(ring + st * C::kStage + (c >> 3) * kPanel + r * 128 + (c & 7) * 16), "r"(0) : "memory");
           }
           fence_proxy_async_smem();
           __syncwarp();
-          if (lane == 0) mbar_arrive(bar_full + 8 * st);
+          if (lane < C::kGroups) mbar_arrive(bar_full + 8 * (st * C::kGroups + lane));
+          if (lane == C::kGroups) mbar_arrive(bar_rope);
         }
         __syncwarp();
       }
     }
   } else if (warp == kIssuer) {
     // -------------------------------------------------------------------- MMA issuer: the whole warp walks, one thread issues
+    // (Descriptors have to stay in uniform registers, or an MMA takes 100 cycles to issue: hence plain loops over steps and
+    // groups, and immediate accumulate flags.)  After the watcher has given up the steps go on without MMAs, so that the
+    // named barriers stay in step.
     constexpr uint32_t id_s = umma_idesc_f16(kKeys, false, kRows), id_o = umma_idesc_f16(256, true, kRows);
-    constexpr uint32_t kUnits16 = C::kStage / 16, kPanel16 = kPanel / 16;
+    constexpr uint32_t kStage16 = C::kStage / 16, kPanel16 = kPanel / 16;
     const uint32_t leader = elect_one();
-    const uint32_t q_lo = desc_k(sq), k_lo0 = desc_k(ring), v_lo0 = desc_mn(ring, kPanel);
+    const uint32_t q_lo = desc_k(sq), k_lo0 = desc_k(ring), v_lo0 = desc_mn(ring, kPanel), r_lo = desc_k(rope), p_lo = desc_k(weights), t_q = tmem + C::kColQ;
     uint32_t u = 0, seg = 0;
-    bool ok = true;
-    for (LatentWalk w(a, s_share, shares, worker, workers); ok && w.more(); w.next()) {
+    bool on = true;
+    for (LatentWalk w(a, s_share, shares, worker, workers); w.more(); w.next()) {
       if (w.rows() == 0) continue;
-      ok = warp_wait(bar_q, seg & 1, wc);
-      for (int i = 0; ok && i <= w.count; ++i) {
-        if (i < w.count) {   // S(u) = Q C^T
-          const uint32_t st = u % C::kStages;
-          if (!(ok = warp_wait(bar_full + 8 * st, (u / C::kStages) & 1, wc))) break;
+      on = on && warp_wait(bar_q, seg & 1, wc);
+      for (int i = 0; i <= w.count; ++i) {
+        if (i > 0) named_bar_sync(kBarRead, kSoft + 32);   // S(u - 1) is in registers
+        if (i < w.count) {   // S(u) = Q C^T: the latent vectors, then the rotary keys, whose room is single
+          on = tile_landed(kBarTile, true) && on;
           tc_fence_after_sync();
-          if (leader) {
-            const uint32_t d = tmem_s + (u & 1) * (kKeys / 2), kl = k_lo0 + st * kUnits16;
-            umma_ws<0>(d, q_lo, kl, id_s);
+          if (leader && on) {
+            const uint32_t kl = k_lo0 + (u % C::kStages) * kStage16;
+            umma_ws_ts<0>(tmem_s, t_q, kl, id_s);
 #pragma unroll
-            for (int k = 1; k < 4 * C::kPanels; ++k) umma_ws<1>(d, q_lo + (k / 4) * kPanel16 + (k % 4) * 2, kl + (k / 4) * kPanel16 + (k % 4) * 2, id_s);
-            umma_commit(bar_s + 8 * (u & 1));
+            for (int k = 1; k < 4 * C::kValuePanels; ++k) {
+              const uint32_t b = kl + (k / 4) * kPanel16 + (k % 4) * 2;
+              if (k / 4 < C::kHeld) umma_ws_ts<1>(tmem_s, t_q + 8 * k, b, id_s);
+              else umma_ws<1>(tmem_s, q_lo + (k / 4 - C::kHeld) * kPanel16 + (k % 4) * 2, b, id_s);
+            }
+          }
+          __syncwarp();
+          on = tile_landed(kBarTile, true) && on;
+          tc_fence_after_sync();
+          if (leader && on) {
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+              if (C::kValuePanels < C::kHeld) umma_ws_ts<1>(tmem_s, t_q + 8 * (4 * C::kValuePanels + k), r_lo + 2 * k, id_s);
+              else umma_ws<1>(tmem_s, q_lo + (C::kQueryPanels - 1) * kPanel16 + 2 * k, r_lo + 2 * k, id_s);
+            }
+            umma_commit(bar_s);
+            umma_commit(bar_rfree);
             if (i == w.count - 1) umma_commit(bar_qfree);
           }
           __syncwarp();
-          ++u;
         }
-        if (i > 0) {         // O += P C of the step before
-          const uint32_t v = i < w.count ? u - 2 : u - 1, st = v % C::kStages;
-          if (!(ok = warp_wait(bar_p + 8 * (v & 1), (v >> 1) & 1, wc))) break;
-          if (i == 1 && seg > 0 && !(ok = warp_wait(bar_read, (seg - 1) & 1, wc))) break;   // O of the unit before has been read
+        if (i > 0) {         // O += P C of the step before, while S(u) is read
+          const uint32_t st = (u - 1) % C::kStages;
+          if (i == 1 && seg > 0) on = warp_wait(bar_read, (seg - 1) & 1, wc) && on;   // O of the unit before has been read
+          named_bar_sync(kBarP, kSoft + 32);
           tc_fence_after_sync();
-          if (leader) {
-            const uint32_t p = k_lo0 + st * kUnits16 + (C::kPanels - 1) * kPanel16, vl = v_lo0 + st * kUnits16;
+          if (leader && on) {
+            const uint32_t vl = v_lo0 + st * kStage16;
 #pragma unroll
-            for (int h = 0; h < kLatent / 256; ++h) {
-              umma_ws_first(tmem + 128 * h, p, vl + 4 * h * kPanel16, id_o, i > 1);
+            for (int h = 0; h < C::kGroups; ++h) {
+              umma_ws_first(tmem + 128 * h, p_lo, vl + 4 * h * kPanel16, id_o, i > 1);
 #pragma unroll
-              for (int k = 1; k < kKeys / 16; ++k) umma_ws<1>(tmem + 128 * h, p + 2 * k, vl + 4 * h * kPanel16 + k * 128, id_o);
+              for (int k = 1; k < kKeys / 16; ++k) umma_ws<1>(tmem + 128 * h, p_lo + 2 * k, vl + 4 * h * kPanel16 + k * 128, id_o);
+              umma_commit(bar_free + 8 * (st * C::kGroups + h));
             }
-            umma_commit(bar_o + 8 * (v & 1));
-            umma_commit(bar_free + 8 * st);
+            umma_commit(bar_o);
           }
           __syncwarp();
         }
+        if (i < w.count) ++u;
       }
       ++seg;
     }
+  } else if (warp == kWatcher) {
+    // -------------------------------------------------------------------- watcher: waits for the operands a step ahead
+    bool ok = true;
+    uint32_t u = 0;
+    for (LatentWalk w(a, s_share, shares, worker, workers); w.more(); w.next()) {
+      if (w.rows() == 0) continue;
+      for (int i = 0; i < w.count; ++i, ++u) {
+#pragma unroll
+        for (int g = 0; g < C::kGroups; ++g) ok = ok && warp_wait(bar_full + 8 * ((u % C::kStages) * C::kGroups + g), (u / C::kStages) & 1, wc);
+        tile_landed(kBarTile, ok);
+        if (lane == 0) s_landed = u + 1;
+        ok = ok && warp_wait(bar_rope, u & 1, wc);
+        tile_landed(kBarTile, ok);
+      }
+    }
+  } else if (warp == kAhead) {
+    // -------------------------------------------------------------------- into L2 ahead of their use: the next unit's queries, and
+    // the tokens kDistance steps on where two CTAs share them.  There three steps of room are less than what memory's latency asks
+    // for at twice the rate (2550 cycles a step without, 2380 with); one CTA by itself is bound by memory, and slower with
+    // (87 thousand cycles for 20 steps, 109 with).
+    const char* data = static_cast<const char*>(a.c.data);
+    constexpr int kLines = C::kPanels;   // of 128 bytes, per token and per query
+    const int tokens = a.paired ? kKeys / 2 : 0, first = static_cast<int>(blockIdx.x & 1) * tokens;
+    uint32_t n = 0;
+    bool on = true;
+    for (LatentWalk w(a, s_share, shares, worker, workers); on && w.more(); w.next()) {
+      if (w.rows() == 0) continue;
+      const int* trow = a.table + static_cast<int64_t>(w.b) * a.width;
+      for (int t = lane; t < w.rows(); t += 32) {
+        const int64_t row = static_cast<int64_t>(w.r.q0) * a.heads + w.row0() + t;
+        if (row < 0 || row >= a.tokens * a.heads) continue;
+        const char* at = reinterpret_cast<const char*>(a.q) + row * (kLines * 128);
+#pragma unroll
+        for (int j = 0; j < kLines; ++j) asm volatile("prefetch.global.L2 [%0];" ::"l"(at + 128 * j));
+      }
+      for (int i = 0; on && i < w.count; ++i, ++n) {
+        for (uint32_t polls = 0; on && s_landed + kDistance < n; ++polls) {
+          __nanosleep(100);
+          on = polls < wc.limit && !s_abort;
+        }
+        for (int t = lane; t < tokens; t += 32) {
+          const int key = (w.step + i) * kKeys + first + t;
+          const int id = key < w.r.hi ? trow[key / a.c.page] : -1;
+          if (id < 0 || id >= a.c.pages) continue;
+          const char* at = data + (static_cast<int64_t>(id) * a.c.page + key % a.c.page) * (kLines * 128);
+#pragma unroll
+          for (int j = 0; j < kLines; ++j) asm volatile("prefetch.global.L2 [%0];" ::"l"(at + 128 * j));
+        }
+      }
+    }
   } else {
-    // -------------------------------------------------------------------- softmax, two threads per row
-    const int r = tid & 63, half = warp >> 1;      // the thread's 32 tokens of a step, its halves of the sums
-    const uint32_t lane_off = static_cast<uint32_t>(warp) << 21;   // 32 lanes per warp, lane in bits 16 and up
-    const uint32_t pair = kBarPair + (warp & 1);
-    float* swap = s_swap + r;
+    // -------------------------------------------------------------------- softmax, four threads per row
+    const int r = tid & 63;
+    const int half = (warp >> 1) & 1, part = 2 * half + (warp >> 2);   // the lanes' 32 tokens of a step; the thread's 16 of them
+    const uint32_t lane_off = static_cast<uint32_t>(warp & 3) << 21;   // 32 lanes per warp, lane in bits 16 and up
+    const uint32_t t_s = tmem_s + 16 * (warp >> 2) + lane_off, t_q = tmem + C::kColQ + 16 * C::kHeld * (warp >> 2) + lane_off, t_o = tmem + (kCols / 2) * (warp >> 2) + lane_off;
+    const uint32_t id = kBarRow + (warp & 1);
+    float* swap = &s_swap[part][r];
+    const float* swap_row = &s_swap[0][r];
     const float sc = a.scale_log2;
     const uint64_t sc2 = pair_f32(sc, sc);
     uint32_t u = 0;
@@ -257,56 +368,86 @@ latent_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__
     for (LatentWalk w(a, s_share, shares, worker, workers); w.more(); w.next()) {
       if (w.rows() == 0) continue;
       const int rows = w.rows(), shift = w.r.L - w.r.n;
-      const int64_t row0 = w.row0(), row = row0 + r;
+      const int row0 = w.row0(), row = row0 + r;
       const bool live = r < rows;
-      const int p0 = shift + static_cast<int>(row0 / a.heads);                  // the first row's position
-      const int see_to = live ? min(shift + static_cast<int>(row / a.heads), w.r.hi - 1) - 32 * half : -1;   // from the thread's first token
-      const int all_to = min(p0 + 1, w.r.hi);                                     // every row sees the tokens before
+      const int64_t at = static_cast<int64_t>(w.r.q0) * a.heads + row;   // of the queries and the output
+      const bool there = live && at >= 0 && at < a.tokens * a.heads;
+      // the unit's queries: the two warps of a lane bring half of the row each, with all loads of a part of it in flight
+      {
+        const uint4* from = reinterpret_cast<const uint4*>(a.q + at * (kLatent + PQ_LATENT_ROPE)) + 4 * C::kHeld * (warp >> 2);
+        constexpr int kBatch = 4;   // of 32 values
+#pragma unroll
+        for (int c0 = 0; c0 < C::kHeld; c0 += kBatch) {
+          uint32_t x[kBatch][16];
+#pragma unroll
+          for (int c = 0; c < kBatch; ++c) {
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+              const uint4 v = there && c0 + c < C::kHeld ? __ldg(from + 4 * (c0 + c) + j) : make_uint4(0, 0, 0, 0);
+              x[c][4 * j] = v.x, x[c][4 * j + 1] = v.y, x[c][4 * j + 2] = v.z, x[c][4 * j + 3] = v.w;
+            }
+          }
+#pragma unroll
+          for (int c = 0; c < kBatch; ++c)
+            if (c0 + c < C::kHeld) tmem_st_32x16(t_q + 16 * (c0 + c), x[c]);
+        }
+        tmem_st_wait();
+        tc_fence_before_sync();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(bar_q);
+      }
+      const int p0 = shift + row0 / a.heads;                                     // the first row's position
+      const int see_to = live ? min(shift + row / a.heads, w.r.hi - 1) - 16 * part : -1;   // from the thread's first token
+      const int all_to = min(p0 + 1, w.r.hi);                                    // every row sees the tokens before
       float m = -INFINITY, l = 0.0f;   // m: the reference, in powers of two; l: the thread's own tokens
       for (int i = 0; i < w.count; ++i, ++u) {
         const int key0 = (w.step + i) * kKeys;
-        ok = ok && warp_wait(bar_s + 8 * (u & 1), (u >> 1) & 1, wc);
+        ok = ok && warp_wait(bar_s, u & 1, wc);
         tc_fence_after_sync();
-        uint32_t s[32];
-        tmem_ld_32x32(tmem_s + (u & 1) * (kKeys / 2) + lane_off, s);
+        uint32_t s[16];
+        tmem_ld_32x16(t_s, s);
         tmem_ld_wait();
+        tc_fence_before_sync();
+        hand_over(kBarRead, kSoft + 32, ok);
         if (a.q_xor != 0u || a.q_and == 0u) {
 #pragma unroll
-          for (int j = 0; j < 32; ++j) s[j] = (s[j] & a.q_and) ^ a.q_xor;
+          for (int j = 0; j < 16; ++j) s[j] = (s[j] & a.q_and) ^ a.q_xor;
         }
         if (key0 + kKeys > all_to || rows < kRows) {
           const int to = see_to - key0;
 #pragma unroll
-          for (int j = 0; j < 32; ++j)
+          for (int j = 0; j < 16; ++j)
             if (j > to) s[j] = 0xff800000u;   // -inf
         }
-        float top[4];
+        float top[2];
 #pragma unroll
-        for (int h = 0; h < 4; ++h) {
+        for (int h = 0; h < 2; ++h) {
           const uint32_t* v = s + 8 * h;
           top[h] = max3(__uint_as_float(v[0]), __uint_as_float(v[1]), __uint_as_float(v[2]));
           top[h] = max3(top[h], __uint_as_float(v[3]), __uint_as_float(v[4]));
           top[h] = max3(top[h], __uint_as_float(v[5]), __uint_as_float(v[6]));
           top[h] = fmaxf(top[h], __uint_as_float(v[7]));
         }
-        float t = fmaxf(max3(top[0], top[1], top[2]), top[3]) * sc;
-        if (pair_any(pair, t > m + 8.0f)) {   // rare after the first steps: some row of the 32
-          t = pair_combine<false>(swap, pair, half, t);
+        float t = fmaxf(top[0], top[1]) * sc;
+        bool taken = i == 0;   // the weights of the step before
+        if (pair_any<128>(id, t > m + 8.0f)) {   // rare after the first steps: some row of the 32
+          t = row_combine<false>(swap, swap_row, id, t);
           const bool grown = t > m + 8.0f;
           const float f = grown ? (m == -INFINITY ? 0.0f : exp2_approx(m - t)) : 1.0f;
           if (grown) m = t;
           l *= f;
           if (i > 0) {   // O holds the sums up to the step before
-            ok = ok && warp_wait(bar_o + 8 * ((u - 1) & 1), ((u - 1) >> 1) & 1, wc);
+            ok = ok && warp_wait(bar_o, (u - 1) & 1, wc);
+            taken = true;
             tc_fence_after_sync();
 #pragma unroll 1
-            for (int c = 0; c < kCols; c += 32) {
+            for (int c = 0; c < kCols / 2; c += 32) {
               uint32_t o[32];
-              tmem_ld_32x32(tmem + c + lane_off, o);
+              tmem_ld_32x32(t_o + c, o);
               tmem_ld_wait();
 #pragma unroll
               for (int j = 0; j < 32; ++j) o[j] = __float_as_uint(__uint_as_float(o[j]) * f);
-              tmem_st_32x32(tmem + c + lane_off, o);
+              tmem_st_32x32(t_o + c, o);
             }
             tmem_st_wait();
           }
@@ -314,9 +455,9 @@ latent_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__
         const float off = kTop - (m == -INFINITY ? 0.0f : m);
         const uint64_t off2 = pair_f32(off, off);
         uint64_t sum = 0;
-        uint32_t q[16];
+        uint32_t q[8];
 #pragma unroll
-        for (int j = 0; j < 16; ++j) {
+        for (int j = 0; j < 8; ++j) {
           float e0, e1;
           unpair_f32(fma_f32x2(pair_f32(__uint_as_float(s[2 * j]), __uint_as_float(s[2 * j + 1])), sc2, off2), e0, e1);
           e0 = exp2_approx(e0);
@@ -324,65 +465,54 @@ latent_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__
           sum = add_f32x2(sum, pair_f32(e0, e1));
           q[j] = pack_f16(e0, e1);
         }
-        float l0, l1;
-        unpair_f32(sum, l0, l1);
-        l += l0 + l1;
-        const uint32_t to = ring + (u % C::kStages) * C::kStage + (C::kPanels - 1) * kPanel + r * 128;
+        if (!taken) ok = ok && warp_wait(bar_o, (u - 1) & 1, wc);
+        const uint32_t to = weights + r * 128;
 #pragma unroll
-        for (int c = 0; c < 4; ++c)
-          asm volatile("st.shared.v4.u32 [%0], {%1, %2, %3, %4};" ::"r"(to + (((4 * half + c) ^ (r & 7)) << 4)),
+        for (int c = 0; c < 2; ++c)
+          asm volatile("st.shared.v4.u32 [%0], {%1, %2, %3, %4};" ::"r"(to + (((2 * part + c) ^ (r & 7)) << 4)),
                        "r"(q[4 * c]), "r"(q[4 * c + 1]), "r"(q[4 * c + 2]), "r"(q[4 * c + 3]) : "memory");
         fence_proxy_async_smem();
         tc_fence_before_sync();
-        __syncwarp();
-        if (lane == 0) mbar_arrive(bar_p + 8 * (u & 1));
+        hand_over(kBarP, kSoft + 32, ok);
+        float l0, l1;
+        unpair_f32(sum, l0, l1);
+        l += l0 + l1;
       }
       // ------------------------------------------------------------------ the unit's (or part's) end
-      ok = ok && warp_wait(bar_o + 8 * ((u - 1) & 1), ((u - 1) >> 1) & 1, wc);
+      ok = ok && warp_wait(bar_o, (u - 1) & 1, wc);
       tc_fence_after_sync();
-      l = pair_combine<true>(swap, pair, half, l);
-      const int64_t at = static_cast<int64_t>(w.r.q0) * a.heads + row;   // of the output
-      const bool writes = live && at >= 0 && at < a.tokens * a.heads;
-      if (w.whole()) {
-        const float inv = l > 0.0f ? 1.0f / l : 0.0f;
+      l = row_combine<true>(swap, swap_row, id, l);
+      const bool whole = w.whole(), begins = w.step == 0;
+      const float inv = l > 0.0f ? 1.0f / l : 0.0f;
+      float* pp = a.partials + (2 * static_cast<int64_t>(blockIdx.x) + begins) * C::kPartFloats;
 #pragma unroll 1
-        for (int c = 0; c < kCols; c += 32) {
-          uint32_t o[32];
-          tmem_ld_32x32(tmem + c + lane_off, o);
-          tmem_ld_wait();
-          // columns 128 h .. of tensor memory are the values 256 h + 128 half ..
-          uint4* to = reinterpret_cast<uint4*>(a.out + at * kLatent + (c >> 7) * 256 + half * 128 + (c & 127));
-          if (writes) {
+      for (int c = (kCols / 2) * (warp >> 2), n = 0; n < kCols / 2; n += 32, c += 32) {
+        uint32_t o[32];
+        tmem_ld_32x32(t_o + n, o);
+        tmem_ld_wait();
+        const int value = (c >> 7) * 256 + half * 128 + (c & 127);   // columns 128 h .. of tensor memory are the values 256 h + 128 half ..
+        if (!there) continue;
+        if (whole) {
+          uint4* to = reinterpret_cast<uint4*>(a.out + at * kLatent + value);
 #pragma unroll
-            for (int j = 0; j < 4; ++j) {
-              uint32_t x[4];
+          for (int j = 0; j < 4; ++j) {
+            uint32_t x[4];
 #pragma unroll
-              for (int k = 0; k < 4; ++k) x[k] = pack_f16(__uint_as_float(o[8 * j + 2 * k]) * inv, __uint_as_float(o[8 * j + 2 * k + 1]) * inv);
-              to[j] = make_uint4(x[0], x[1], x[2], x[3]);
-            }
+            for (int k = 0; k < 4; ++k) x[k] = pack_f16(__uint_as_float(o[8 * j + 2 * k]) * inv, __uint_as_float(o[8 * j + 2 * k + 1]) * inv);
+            to[j] = make_uint4(x[0], x[1], x[2], x[3]);
           }
-        }
-      } else {
-        const bool begins = w.step == 0;
-        float* pp = a.partials + (2 * static_cast<int64_t>(blockIdx.x) + begins) * C::kPartFloats;
-#pragma unroll 1
-        for (int c = 0; c < kCols; c += 32) {
-          uint32_t o[32];
-          tmem_ld_32x32(tmem + c + lane_off, o);
-          tmem_ld_wait();
-          float4* to = reinterpret_cast<float4*>(pp) + (((c >> 7) * 256 + half * 128 + (c & 127)) / 4) * kRows + r;
-          if (writes) {
+        } else {
+          float4* to = reinterpret_cast<float4*>(pp) + (value / 4) * kRows + r;
 #pragma unroll
-            for (int j = 0; j < 8; ++j)
-              to[j * kRows] = make_float4(__uint_as_float(o[4 * j]), __uint_as_float(o[4 * j + 1]), __uint_as_float(o[4 * j + 2]), __uint_as_float(o[4 * j + 3]));
-          }
+          for (int j = 0; j < 8; ++j)
+            to[j * kRows] = make_float4(__uint_as_float(o[4 * j]), __uint_as_float(o[4 * j + 1]), __uint_as_float(o[4 * j + 2]), __uint_as_float(o[4 * j + 3]));
         }
-        if (writes && half == 0) reinterpret_cast<float2*>(pp + kRows * kLatent)[r] = make_float2(m, l);
-        if (begins) {
-          const int64_t first = static_cast<int64_t>(w.r.q0) * a.heads + row0;
-          join = make_int4(static_cast<int>(first & 0xffffffff), static_cast<int>(first >> 32), rows,
-                           1 + (w.all_steps - w.count + s_share.per - 1) / s_share.per);
-        }
+      }
+      if (!whole && there && part == 0) reinterpret_cast<float2*>(pp + kRows * kLatent)[r] = make_float2(m, l);
+      if (!whole && begins) {
+        const int64_t first = static_cast<int64_t>(w.r.q0) * a.heads + row0;
+        join = make_int4(static_cast<int>(first & 0xffffffff), static_cast<int>(first >> 32), rows,
+                         1 + (w.all_steps - w.count + s_share.per - 1) / s_share.per);
       }
       tc_fence_before_sync();
       __syncwarp();
@@ -403,7 +533,10 @@ latent_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__
       mbar_drain(bar_drain, 0u);
     }
     if (warp == kLoader && lane == 0) {
-      for (uint32_t i = issued > C::kStages ? issued - C::kStages : 0; i < issued; ++i) mbar_drain(bar_full + 8 * (i % C::kStages), (i / C::kStages) & 1);
+      for (uint32_t i = issued >= C::kStages ? issued + 1 - C::kStages : 0; i <= issued; ++i) {   // the last may be in part on its way
+        for (int g = 0; g < C::kGroups; ++g) mbar_drain(bar_full + 8 * ((i % C::kStages) * C::kGroups + g), (i / C::kStages) & 1);
+      }
+      mbar_drain(bar_rope, (issued & 1) ^ 1), mbar_drain(bar_rope, issued & 1);
       mbar_drain(bar_fix, fixes & 1);
       if (units > 0) mbar_drain(bar_q, (units - 1) & 1);
     }
@@ -494,7 +627,7 @@ int pq_latent_attention(const void* q_f16, int32_t heads, const pq_latent_cache*
   if (!q_f16 || !block_table || !q_start || !kv_len || !out_f16) return PQ_ERR_NULL;
   if (!aligned16(q_f16) || !aligned16(out_f16) || !aligned256(workspace)) return PQ_ERR_ALIGN;
   if ((rc = check_arch()) != PQ_OK) return rc;
-  LatentArgs a{*cache, block_table, width, q_start, kv_len, static_cast<__half*>(out_f16), tokens, static_cast<int>(requests), heads,
+  LatentArgs a{*cache, block_table, width, q_start, kv_len, static_cast<const __half*>(q_f16), static_cast<__half*>(out_f16), tokens, static_cast<int>(requests), heads,
                0, scale * 1.44269504f, 0xffffffffu, 0u, nullptr, nullptr, kKeys, device_status_ptr(), wait_limit()};
   if (a.status == nullptr) return PQ_ERR_CUDA;
   while (cache->page % a.box != 0) a.box /= 2;   // the page is a multiple of 16

@@ -36,30 +36,30 @@ struct UnitShape {
 };
 
 struct Request {
-  int q0, n;              // first token, tokens
+  int q0, n;              // first token, tokens (n * heads, and units over all requests, below 2^31)
   int k0, L, hi;          // first key (where keys are ragged rows), keys, keys that can be read
   UnitShape s;
-  int64_t all;            // rows
+  uint32_t all;           // rows: below 2^31
   int tiles;
   int same;               // > 0: steps of every unit (fewer keys than rows, or than the table holds)
   __device__ __forceinline__ void settle() {
-    all = static_cast<int64_t>(n) * s.heads;
-    tiles = static_cast<int>((all + s.rows - 1) / s.rows);
+    all = static_cast<uint32_t>(n) * static_cast<uint32_t>(s.heads);
+    tiles = static_cast<int>((all + s.rows - 1) / static_cast<uint32_t>(s.rows));
     same = L < n || hi < L ? max((hi + s.keys - 1) / s.keys, 1) : 0;
   }
-  __device__ __forceinline__ int64_t units() const { return static_cast<int64_t>(tiles) * s.copies; }
+  __device__ __forceinline__ int units() const { return tiles * s.copies; }
   __device__ __forceinline__ int steps(int tile) const {
     if (same) return same;
-    const int64_t last = min(static_cast<int64_t>(tile + 1) * s.rows, all) - 1;
-    return (L - n + static_cast<int>(last / s.heads)) / s.keys + 1;
+    const uint32_t last = min(static_cast<uint32_t>(tile + 1) * s.rows, all) - 1;
+    return (L - n + static_cast<int>(last / static_cast<uint32_t>(s.heads))) / s.keys + 1;
   }
   __device__ __forceinline__ int64_t before_tile(int tile) const {   // steps of one copy of the tiles before; tile < tiles
     if (same) return static_cast<int64_t>(same) * tile;
     if (tile == 0) return 0;
     return static_cast<int64_t>(floor_sum(tile, static_cast<uint64_t>(s.keys) * s.heads, s.rows, s.rows - 1 + static_cast<uint64_t>(L - n) * s.heads)) + tile;
   }
-  __device__ __forceinline__ int64_t before(int64_t unit) const {    // unit < units()
-    const int tile = static_cast<int>(unit / s.copies), copy = static_cast<int>(unit % s.copies);
+  __device__ __forceinline__ int64_t before(int unit) const {        // unit < units()
+    const int tile = unit / s.copies, copy = unit - tile * s.copies;
     return before_tile(tile) * s.copies + static_cast<int64_t>(copy) * (copy ? steps(tile) : 0);
   }
   __device__ __forceinline__ int64_t total() const { return tiles == 0 ? 0 : (before_tile(tiles - 1) + steps(tiles - 1)) * s.copies; }
@@ -67,8 +67,8 @@ struct Request {
 
 // Shares: `left` steps from step `step` of unit `unit` of request `b` on.
 struct Share {
-  int b, step, per;
-  int64_t unit, left;
+  int b, unit, step, per;
+  int64_t left;
 };
 
 // By the whole block; sums: one word per warp.
@@ -106,9 +106,9 @@ __device__ __forceinline__ void find_share(const Args& a, int worker, int worker
         at -= t;
         continue;
       }
-      int64_t lo = 0, hi = r.units() - 1;   // the last unit that begins at or before the step
+      int lo = 0, hi = r.units() - 1;   // the last unit that begins at or before the step
       while (lo < hi) {
-        const int64_t mid = (lo + hi + 1) >> 1;
+        const int mid = lo + (hi - lo + 1) / 2;
         if (r.before(mid) <= at) lo = mid; else hi = mid - 1;
       }
       share->b = b, share->unit = lo, share->step = static_cast<int>(at - r.before(lo));
@@ -127,7 +127,8 @@ struct Walk {
   const bool shares;
   const int workers;
   int b;
-  int64_t unit, left;               // shares: as in Share; turns: the unit, counted from request b's first, and 1 as long as there are any
+  int unit;                         // shares: as in Share; turns: counted from request b's first
+  int64_t left;                     // turns: 1 as long as there are any
   int step, count, all_steps;       // the unit's steps: first, how many, of all
   int tile, copy;
   Request r;
@@ -155,16 +156,16 @@ struct Walk {
     }
     const int lane = threadIdx.x & 31;
     for (; b < a.requests; b += 32) {   // 32 requests at a time
-      int64_t in = b + lane < a.requests ? a.request(b + lane).units() : 0;
+      int in = b + lane < a.requests ? a.request(b + lane).units() : 0;
 #pragma unroll
       for (int o = 1; o < 32; o <<= 1) {
-        const int64_t x = __shfl_up_sync(0xffffffffu, in, o);
+        const int x = __shfl_up_sync(0xffffffffu, in, o);
         if (lane >= o) in += x;
       }
       const uint32_t behind = __ballot_sync(0xffffffffu, in > unit);
       if (behind) {
         const int at = __ffs(behind) - 1;
-        const int64_t before = __shfl_sync(0xffffffffu, in, max(at - 1, 0));
+        const int before = __shfl_sync(0xffffffffu, in, max(at - 1, 0));
         if (at > 0) unit -= before;
         b += at;
         r = a.request(b);
@@ -175,7 +176,7 @@ struct Walk {
     left = 0;
   }
   __device__ __forceinline__ void take() {
-    tile = static_cast<int>(unit / r.s.copies), copy = static_cast<int>(unit % r.s.copies);
+    tile = unit / r.s.copies, copy = unit - tile * r.s.copies;
     if (!shares) tile = r.tiles - 1 - tile;
     all_steps = r.steps(tile);
     count = shares ? static_cast<int>(min(static_cast<int64_t>(all_steps - step), left)) : all_steps;
