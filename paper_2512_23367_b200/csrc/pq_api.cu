@@ -172,18 +172,23 @@ int make_tmap_2d(CUtensorMap* out, const void* base, uint64_t rows, uint64_t col
   return r == CUDA_SUCCESS ? PQ_OK : PQ_ERR_CUDA;
 }
 
-int make_tmap_heads(CUtensorMap* out, const void* base, uint64_t rows, uint64_t heads, uint64_t cols, uint64_t row_stride,
-                    uint64_t head_stride, uint32_t box_rows) {
+int make_tmap_f16(CUtensorMap* out, const void* base, uint32_t rank, const uint64_t* dims, const uint64_t* strides, const uint32_t* box) {
   const EncodeTiledFn encode = encode_fn();
   if (encode == nullptr) return PQ_ERR_CUDA;
-  cuuint64_t dims[3] = {cols, heads, rows};
-  cuuint64_t strides[2] = {head_stride * 2, row_stride * 2};
-  cuuint32_t box[3] = {64, 1, box_rows};
-  cuuint32_t estr[3] = {1, 1, 1};
-  const CUresult r = encode(out, CU_TENSOR_MAP_DATA_TYPE_UINT16, 3, const_cast<void*>(base), dims, strides, box, estr,
-                            CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
-                            CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+  cuuint64_t d[5], s[4];
+  cuuint32_t b[5], e[5];
+  for (uint32_t i = 0; i < rank; ++i) d[i] = dims[i], b[i] = box[i], e[i] = 1;
+  for (uint32_t i = 0; i + 1 < rank; ++i) s[i] = strides[i];
+  const CUresult r = encode(out, CU_TENSOR_MAP_DATA_TYPE_UINT16, rank, const_cast<void*>(base), d, s, b, e, CU_TENSOR_MAP_INTERLEAVE_NONE,
+                            CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
   return r == CUDA_SUCCESS ? PQ_OK : PQ_ERR_CUDA;
+}
+
+int make_tmap_heads(CUtensorMap* out, const void* base, uint64_t rows, uint64_t heads, uint64_t cols, uint64_t row_stride,
+                    uint64_t head_stride, uint32_t box_rows) {
+  const uint64_t dims[3] = {cols, heads, rows}, strides[2] = {head_stride * 2, row_stride * 2};
+  const uint32_t box[3] = {64, 1, box_rows};
+  return make_tmap_f16(out, base, 3, dims, strides, box);
 }
 
 }  // namespace pq

@@ -74,6 +74,8 @@ bool pdl_enabled();
 int make_tmap_2d(CUtensorMap* out, const void* base, uint64_t rows, uint64_t cols, uint32_t box_rows,
                  uint32_t box_cols, uint32_t elem_bytes, int swizzle_bytes);
 
+// An FP16 tensor of up to 5 dimensions, innermost first; strides in bytes of all but the first; boxes with the 128-byte swizzle.
+int make_tmap_f16(CUtensorMap* out, const void* base, uint32_t rank, const uint64_t* dims, const uint64_t* strides, const uint32_t* box);
 // FP16 rows of heads, [rows, heads, cols] with the given strides in elements, in boxes of [box_rows, 1, 64] with the
 // 128-byte swizzle.  Strides are multiples of 8.
 int make_tmap_heads(CUtensorMap* out, const void* base, uint64_t rows, uint64_t heads, uint64_t cols, uint64_t row_stride,

@@ -28,7 +28,7 @@ struct LatentCfg {
   static constexpr int kValuePanels = kLatent / 64;
   static constexpr int kGroups = kLatent / 256;           // panels are brought in and given back four at a time, the values of one MMA
   // Queries lie in tensor memory, as many panels of them as there is room for, the others in shared memory.
-  static constexpr int kHeld = kLatent == 512 ? 7 : kPanels, kQueryPanels = kPanels - kHeld;
+  static constexpr int kHeld = kLatent == 512 ? 7 : 4, kQueryPanels = kPanels - kHeld;
   static constexpr int kStages = kLatent == 512 ? 3 : 6;   // steps whose latent vectors fit at once
   static constexpr int kStage = kValuePanels * kPanel, kStep = kPanels * kPanel;
   static constexpr int kSmem = kQueryPanels * kPanel + kStages * kStage + 2 * kPanel /* rotary keys, P */ + 1024 /* alignment */;
@@ -44,7 +44,6 @@ struct LatentArgs {
   int64_t width;
   const int* q_start;
   const int* kv_len;
-  const __half* q;
   __half* out;
   int64_t tokens;
   int requests, heads;
@@ -80,23 +79,28 @@ struct LatentWalk : Walk<LatentArgs> {
 // MMAs with M = 64 in the form that keeps B in place: all 128 lanes of tensor memory take part, lane r and lane 64 + r
 // holding the lower and the upper half of row r's columns.  Per 16 of K: 32 cycles with N = 64 and 80 with 256, the time
 // that shared memory takes to give the operands; the other form of M = 64 takes 32 and 128, and half of the lanes stay empty.
-template <int kAccumulate>
+// Tokens lie in shared memory as [group of four panels][8 tokens][panel][128-byte rows, swizzled]: the swizzle's atoms of 8 rows
+// stay whole, panels are 1024 bytes apart and groups of 8 tokens 4096, so that one TMA box brings all four panels of as many
+// tokens as a page holds in a row.  (Panel after panel, a page of 16 tokens takes 36 boxes a step, 100 cycles each.)
+constexpr uint32_t kAtom = 1024, kTokens8 = 4 * kAtom;
+constexpr uint32_t kTokenHi = (kTokens8 >> 4) | (1u << 14) | (2u << 29);
+template <int kAccumulate, uint32_t kHi>
 __device__ __forceinline__ void umma_ws(uint32_t d, uint32_t a_lo, uint32_t b_lo, uint32_t idesc) {
-  asm volatile("{\n\t.reg .pred p;\n\t.reg .b64 a, b;\n\tsetp.ne.b32 p, %4, 0;\n\tmov.b64 a, {%1, %5};\n\tmov.b64 b, {%2, %5};\n\t"
+  asm volatile("{\n\t.reg .pred p;\n\t.reg .b64 a, b;\n\tsetp.ne.b32 p, %4, 0;\n\tmov.b64 a, {%1, %5};\n\tmov.b64 b, {%2, %6};\n\t"
                "tcgen05.mma.ws.cta_group::1.kind::f16 [%0], a, b, %3, p;\n\t}"
-               ::"r"(d), "r"(a_lo), "r"(b_lo), "r"(idesc), "n"(kAccumulate), "n"(kDescHi) : "memory");
+               ::"r"(d), "r"(a_lo), "r"(b_lo), "r"(idesc), "n"(kAccumulate), "n"(kDescHi), "n"(kHi) : "memory");
 }
 __device__ __forceinline__ void umma_ws_first(uint32_t d, uint32_t a_lo, uint32_t b_lo, uint32_t idesc, uint32_t accumulate) {
-  asm volatile("{\n\t.reg .pred p;\n\t.reg .b64 a, b;\n\tsetp.ne.b32 p, %4, 0;\n\tmov.b64 a, {%1, %5};\n\tmov.b64 b, {%2, %5};\n\t"
+  asm volatile("{\n\t.reg .pred p;\n\t.reg .b64 a, b;\n\tsetp.ne.b32 p, %4, 0;\n\tmov.b64 a, {%1, %5};\n\tmov.b64 b, {%2, %6};\n\t"
                "tcgen05.mma.ws.cta_group::1.kind::f16 [%0], a, b, %3, p;\n\t}"
-               ::"r"(d), "r"(a_lo), "r"(b_lo), "r"(idesc), "r"(accumulate), "n"(kDescHi) : "memory");
+               ::"r"(d), "r"(a_lo), "r"(b_lo), "r"(idesc), "r"(accumulate), "n"(kDescHi), "n"(kTokenHi) : "memory");
 }
 // A in tensor memory, row r in lane r and again in lane 64 + r, which multiplies it with the upper half of the columns.
 template <int kAccumulate>
 __device__ __forceinline__ void umma_ws_ts(uint32_t d, uint32_t a, uint32_t b_lo, uint32_t idesc) {
   asm volatile("{\n\t.reg .pred p;\n\t.reg .b64 b;\n\tsetp.ne.b32 p, %4, 0;\n\tmov.b64 b, {%2, %5};\n\t"
                "tcgen05.mma.ws.cta_group::1.kind::f16 [%0], [%1], b, %3, p;\n\t}"
-               ::"r"(d), "r"(a), "r"(b_lo), "r"(idesc), "n"(kAccumulate), "n"(kDescHi) : "memory");
+               ::"r"(d), "r"(a), "r"(b_lo), "r"(idesc), "n"(kAccumulate), "n"(kTokenHi) : "memory");
 }
 
 // The sum, or the largest, of a value of the row's four threads, the same in all: `mine` is the thread's word, the others'
@@ -127,7 +131,7 @@ constexpr uint32_t kBarRow = 1, kBarTile = 3, kBarRead = 4, kBarP = 5;
 // the maximum has grown by more than 2^8.
 template <int kLatent>
 __global__ void __launch_bounds__(kThreads, 1)
-latent_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUtensorMap map_c, const LatentArgs a) {
+latent_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUtensorMap map_c, const __grid_constant__ CUtensorMap map_r, const LatentArgs a) {
   using C = LatentCfg<kLatent>;
   constexpr float kTop = 7.0f;          // a weight at the reference is 2^kTop
   constexpr int kCols = C::kCols;
@@ -155,7 +159,7 @@ latent_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__
     mbar_init(bar_drain, 1);
     fence_mbar_init();
     s_abort = 0, s_landed = 0;
-    tma_prefetch_desc(&map_q), tma_prefetch_desc(&map_c);
+    tma_prefetch_desc(&map_q), tma_prefetch_desc(&map_c), tma_prefetch_desc(&map_r);
   }
   if (warp == kIssuer) {
     tmem_alloc(smem_u32(&s_tmem), 512);
@@ -171,61 +175,76 @@ latent_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__
   const uint32_t tmem = __shfl_sync(0xffffffffu, s_tmem, 0), tmem_s = tmem + C::kColS;
   const uint32_t sq = (smem_u32(smem_raw) + 1023u) & ~1023u, ring = sq + C::kQueryPanels * kPanel, rope = ring + C::kStages * C::kStage, weights = rope + kPanel;
   const WaitCtx wc{&s_abort, a.wait_limit};
-  uint32_t issued = 0, fixes = 0, units = 0;   // loader: steps requested, of them by way of bar_fix; units
+  // loader: stages filled, steps (a unit's queries take a stage, too), steps by way of bar_fix; units
+  uint32_t filled = 0, issued = 0, fixes = 0, units = 0;
 
   if (warp == kLoader) {
-    // -------------------------------------------------------------------- loader: a lane requests one box of one panel of a group
-    const int pieces = kKeys / a.box;
+    // -------------------------------------------------------------------- loader: a lane requests one box
+    const int pieces = kKeys / a.box, groups8 = a.box / 8;
     const int rows_all = static_cast<int>(a.c.pages * a.c.page);
-    const int panel = lane / pieces, y = lane - panel * pieces;
+    const bool mine = lane < pieces;
     bool ok = true;
+    auto wait_free = [&](int g) {
+      if (ok && filled >= C::kStages) ok = warp_wait(bar_free + 8 * ((filled % C::kStages) * C::kGroups + g), ((filled / C::kStages) & 1) ^ 1, wc);
+    };
     for (LatentWalk w(a, s_share, shares, worker, workers); ok && w.more(); w.next()) {
       if (w.rows() == 0) continue;
-      if (C::kQueryPanels > 0) {
-        if (units > 0 && !(ok = warp_wait(bar_qfree, (units - 1) & 1, wc))) break;
-        if (lane == 0) mbar_arrive_expect_tx(bar_q, C::kQueryPanels * kPanel);
-        __syncwarp();
-        if (lane < C::kQueryPanels) tma_load_2d(sq + lane * kPanel, &map_q, bar_q, (C::kHeld + lane) * 64, w.r.q0 * a.heads + w.row0());
-        ++units;
-      }
       const int* trow = a.table + static_cast<int64_t>(w.b) * a.width;
       int id = -1, off = 0;
       auto look_up = [&](int i) {
-        const int key = (w.step + i) * kKeys + y * a.box;
+        const int key = (w.step + i) * kKeys + lane * a.box;
         id = -1;
-        if (i >= w.count || key >= w.r.hi) return;
+        if (!mine || i >= w.count || key >= w.r.hi) return;
         const int col = key / a.c.page;
         off = key - col * a.c.page;
         id = trow[col];
       };
       look_up(0);
+      // The unit's queries: panels for tensor memory by way of a stage, from which the softmax threads take them, the others to stay.
+      const int q_row = w.r.q0 * a.heads + w.row0();
+#pragma unroll
+      for (int g = 0; g < C::kGroups; ++g) {
+        const int panels = min(4, C::kHeld - 4 * g);
+        const uint32_t full = bar_full + 8 * ((filled % C::kStages) * C::kGroups + g);
+        wait_free(g);
+        if (ok && lane == 0) mbar_arrive_expect_tx(full, panels * kPanel);
+        __syncwarp();
+        if (ok && lane < panels) tma_load_2d(ring + (filled % C::kStages) * C::kStage + (4 * g + lane) * kPanel, &map_q, full, (4 * g + lane) * 64, q_row);
+      }
+      if (ok && units > 0) ok = warp_wait(bar_qfree, (units - 1) & 1, wc);
+      if (!ok) break;
+      if (lane == 0) mbar_arrive_expect_tx(bar_q, C::kQueryPanels * kPanel);
+      __syncwarp();
+      if (lane < C::kQueryPanels) tma_load_2d(sq + lane * kPanel, &map_q, bar_q, (C::kHeld + lane) * 64, q_row);
+      ++units, ++filled;
       for (int i = 0; i < w.count; ++i) {
-        const uint32_t st = issued % C::kStages, phase = (issued / C::kStages) & 1;
-        const int row = id < 0 || id >= a.c.pages ? rows_all : id * a.c.page + off;   // beyond the tensor: zeros
+        const uint32_t st = filled % C::kStages;
+        const int row = (id < 0 || id >= a.c.pages ? rows_all : id * a.c.page + off) / 8;   // beyond the tensor: zeros
         const int dead = min(max(w.r.hi - (w.step + i) * kKeys, 0), kKeys);   // first token of the step that was never written
-        const uint32_t dst = ring + st * C::kStage + y * a.box * 128;
+        const uint32_t dst = ring + st * C::kStage;
         if (dead < kKeys && lane == 0) mbar_arrive_expect_tx(bar_fix, C::kStep);
 #pragma unroll
         for (int g = 0; g < C::kGroups; ++g) {
           const uint32_t full = bar_full + 8 * (st * C::kGroups + g);
-          if (ok && issued >= C::kStages) ok = warp_wait(bar_free + 8 * (st * C::kGroups + g), phase ^ 1, wc);
+          wait_free(g);
           if (ok && dead == kKeys && lane == 0) mbar_arrive_expect_tx(full, 4 * kPanel);
           __syncwarp();
-          if (ok && panel < 4) tma_load_2d(dst + (4 * g + panel) * kPanel, &map_c, dead < kKeys ? bar_fix : full, (4 * g + panel) * 64, row);
+          if (ok && mine) tma_load_4d(dst + 4 * g * kPanel + lane * groups8 * kTokens8, &map_c, dead < kKeys ? bar_fix : full, 0, 0, 4 * g, row);
         }
         if (ok && issued > 0) ok = warp_wait(bar_rfree, (issued & 1) ^ 1, wc);
         if (!ok) break;
         if (dead == kKeys && lane == 0) mbar_arrive_expect_tx(bar_rope, kPanel);
         __syncwarp();
-        if (panel == 0) tma_load_2d(rope + y * a.box * 128, &map_c, dead < kKeys ? bar_fix : bar_rope, kLatent, row);
+        if (mine) tma_load_4d(rope + lane * groups8 * kAtom, &map_r, dead < kKeys ? bar_fix : bar_rope, 0, 0, C::kValuePanels, row);
         look_up(i + 1);   // used, and so waited for, in the next round
-        ++issued;
+        ++issued, ++filled;
         if (dead < kKeys) {   // 0 x NaN is not 0: the weights of such tokens are, their vectors have to be
           if (!(ok = warp_wait(bar_fix, fixes & 1, wc))) break;
           ++fixes;
           for (int j = lane; j < (kKeys - dead) * (kLatent / 8); j += 32) {
-            const int r = dead + j / (kLatent / 8), c = j % (kLatent / 8);
-            asm volatile("st.shared.v4.u32 [%0], {%1, %1, %1, %1};" ::"r"(ring + st * C::kStage + (c >> 3) * kPanel + r * 128 + (c & 7) * 16), "r"(0) : "memory");
+            const int r = dead + j / (kLatent / 8), c = j % (kLatent / 8), panel = c >> 3;
+            const uint32_t at = dst + (panel >> 2) * (4 * kPanel) + (r >> 3) * kTokens8 + (panel & 3) * kAtom + (r & 7) * 128 + (c & 7) * 16;
+            asm volatile("st.shared.v4.u32 [%0], {%1, %1, %1, %1};" ::"r"(at), "r"(0) : "memory");
           }
           fence_proxy_async_smem();
           __syncwarp();
@@ -243,25 +262,31 @@ latent_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__
     constexpr uint32_t id_s = umma_idesc_f16(kKeys, false, kRows), id_o = umma_idesc_f16(256, true, kRows);
     constexpr uint32_t kStage16 = C::kStage / 16, kPanel16 = kPanel / 16;
     const uint32_t leader = elect_one();
-    const uint32_t q_lo = desc_k(sq), k_lo0 = desc_k(ring), v_lo0 = desc_mn(ring, kPanel), r_lo = desc_k(rope), p_lo = desc_k(weights), t_q = tmem + C::kColQ;
-    uint32_t u = 0, seg = 0;
+    const uint32_t q_lo = desc_k(sq), k_lo0 = desc_k(ring), v_lo0 = desc_mn(ring, kAtom), r_lo = desc_k(rope), p_lo = desc_k(weights), t_q = tmem + C::kColQ;
+    uint32_t n = 0, seg = 0;   // stages, units before
     bool on = true;
     for (LatentWalk w(a, s_share, shares, worker, workers); w.more(); w.next()) {
       if (w.rows() == 0) continue;
       on = on && warp_wait(bar_q, seg & 1, wc);
+      if (leader && on) {   // the queries have been taken out of their stage
+#pragma unroll
+        for (int g = 0; g < C::kGroups; ++g) mbar_arrive(bar_free + 8 * ((n % C::kStages) * C::kGroups + g));
+      }
+      __syncwarp();
+      ++n;
       for (int i = 0; i <= w.count; ++i) {
         if (i > 0) named_bar_sync(kBarRead, kSoft + 32);   // S(u - 1) is in registers
         if (i < w.count) {   // S(u) = Q C^T: the latent vectors, then the rotary keys, whose room is single
           on = tile_landed(kBarTile, true) && on;
           tc_fence_after_sync();
           if (leader && on) {
-            const uint32_t kl = k_lo0 + (u % C::kStages) * kStage16;
+            const uint32_t kl = k_lo0 + (n % C::kStages) * kStage16;
             umma_ws_ts<0>(tmem_s, t_q, kl, id_s);
 #pragma unroll
             for (int k = 1; k < 4 * C::kValuePanels; ++k) {
-              const uint32_t b = kl + (k / 4) * kPanel16 + (k % 4) * 2;
+              const uint32_t b = kl + (k / 16) * (4 * kPanel16) + (k / 4 % 4) * (kAtom / 16) + (k % 4) * 2;
               if (k / 4 < C::kHeld) umma_ws_ts<1>(tmem_s, t_q + 8 * k, b, id_s);
-              else umma_ws<1>(tmem_s, q_lo + (k / 4 - C::kHeld) * kPanel16 + (k % 4) * 2, b, id_s);
+              else umma_ws<1, kTokenHi>(tmem_s, q_lo + (k / 4 - C::kHeld) * kPanel16 + (k % 4) * 2, b, id_s);
             }
           }
           __syncwarp();
@@ -269,10 +294,7 @@ latent_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__
           tc_fence_after_sync();
           if (leader && on) {
 #pragma unroll
-            for (int k = 0; k < 4; ++k) {
-              if (C::kValuePanels < C::kHeld) umma_ws_ts<1>(tmem_s, t_q + 8 * (4 * C::kValuePanels + k), r_lo + 2 * k, id_s);
-              else umma_ws<1>(tmem_s, q_lo + (C::kQueryPanels - 1) * kPanel16 + 2 * k, r_lo + 2 * k, id_s);
-            }
+            for (int k = 0; k < 4; ++k) umma_ws<1, kDescHi>(tmem_s, q_lo + (C::kQueryPanels - 1) * kPanel16 + 2 * k, r_lo + 2 * k, id_s);
             umma_commit(bar_s);
             umma_commit(bar_rfree);
             if (i == w.count - 1) umma_commit(bar_qfree);
@@ -280,7 +302,7 @@ latent_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__
           __syncwarp();
         }
         if (i > 0) {         // O += P C of the step before, while S(u) is read
-          const uint32_t st = (u - 1) % C::kStages;
+          const uint32_t st = (n - 1) % C::kStages;
           if (i == 1 && seg > 0) on = warp_wait(bar_read, (seg - 1) & 1, wc) && on;   // O of the unit before has been read
           named_bar_sync(kBarP, kSoft + 32);
           tc_fence_after_sync();
@@ -290,26 +312,27 @@ latent_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__
             for (int h = 0; h < C::kGroups; ++h) {
               umma_ws_first(tmem + 128 * h, p_lo, vl + 4 * h * kPanel16, id_o, i > 1);
 #pragma unroll
-              for (int k = 1; k < kKeys / 16; ++k) umma_ws<1>(tmem + 128 * h, p_lo + 2 * k, vl + 4 * h * kPanel16 + k * 128, id_o);
+              for (int k = 1; k < kKeys / 16; ++k) umma_ws<1, kTokenHi>(tmem + 128 * h, p_lo + 2 * k, vl + 4 * h * kPanel16 + k * (2 * kTokens8 / 16), id_o);
               umma_commit(bar_free + 8 * (st * C::kGroups + h));
             }
             umma_commit(bar_o);
           }
           __syncwarp();
         }
-        if (i < w.count) ++u;
+        if (i < w.count) ++n;
       }
       ++seg;
     }
   } else if (warp == kWatcher) {
     // -------------------------------------------------------------------- watcher: waits for the operands a step ahead
     bool ok = true;
-    uint32_t u = 0;
+    uint32_t u = 0, n = 0;
     for (LatentWalk w(a, s_share, shares, worker, workers); w.more(); w.next()) {
       if (w.rows() == 0) continue;
-      for (int i = 0; i < w.count; ++i, ++u) {
+      ++n;   // the queries' stage is the softmax threads'
+      for (int i = 0; i < w.count; ++i, ++u, ++n) {
 #pragma unroll
-        for (int g = 0; g < C::kGroups; ++g) ok = ok && warp_wait(bar_full + 8 * ((u % C::kStages) * C::kGroups + g), (u / C::kStages) & 1, wc);
+        for (int g = 0; g < C::kGroups; ++g) ok = ok && warp_wait(bar_full + 8 * ((n % C::kStages) * C::kGroups + g), (n / C::kStages) & 1, wc);
         tile_landed(kBarTile, ok);
         if (lane == 0) s_landed = u + 1;
         ok = ok && warp_wait(bar_rope, u & 1, wc);
@@ -317,27 +340,21 @@ latent_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__
       }
     }
   } else if (warp == kAhead) {
-    // -------------------------------------------------------------------- into L2 ahead of their use: the next unit's queries, and
-    // the tokens kDistance steps on where two CTAs share them.  There three steps of room are less than what memory's latency asks
-    // for at twice the rate (2550 cycles a step without, 2380 with); one CTA by itself is bound by memory, and slower with
-    // (87 thousand cycles for 20 steps, 109 with).
+    // -------------------------------------------------------------------- tokens into L2, kDistance steps ahead of their use,
+    // where two CTAs share them.  There three steps of room are less than what memory's latency asks for at twice the rate
+    // (2550 cycles a step without, 2250 with); one CTA by itself is bound by memory, and slower with (87 thousand cycles for
+    // 20 steps, 109 with).
     const char* data = static_cast<const char*>(a.c.data);
-    constexpr int kLines = C::kPanels;   // of 128 bytes, per token and per query
-    const int tokens = a.paired ? kKeys / 2 : 0, first = static_cast<int>(blockIdx.x & 1) * tokens;
+    constexpr int kLines = C::kPanels;   // of 128 bytes, per token
+    const int tokens = kKeys / 2, first = static_cast<int>(blockIdx.x & 1) * tokens;
     uint32_t n = 0;
-    bool on = true;
+    bool on = a.paired != 0;
     for (LatentWalk w(a, s_share, shares, worker, workers); on && w.more(); w.next()) {
       if (w.rows() == 0) continue;
       const int* trow = a.table + static_cast<int64_t>(w.b) * a.width;
-      for (int t = lane; t < w.rows(); t += 32) {
-        const int64_t row = static_cast<int64_t>(w.r.q0) * a.heads + w.row0() + t;
-        if (row < 0 || row >= a.tokens * a.heads) continue;
-        const char* at = reinterpret_cast<const char*>(a.q) + row * (kLines * 128);
-#pragma unroll
-        for (int j = 0; j < kLines; ++j) asm volatile("prefetch.global.L2 [%0];" ::"l"(at + 128 * j));
-      }
       for (int i = 0; on && i < w.count; ++i, ++n) {
-        for (uint32_t polls = 0; on && s_landed + kDistance < n; ++polls) {
+        if (n < static_cast<uint32_t>(C::kStages)) continue;   // being loaded
+        for (uint32_t polls = 0; on && (s_landed == 0 || s_landed + kDistance < n); ++polls) {   // (not in the way of the first ones)
           __nanosleep(100);
           on = polls < wc.limit && !s_abort;
         }
@@ -356,13 +373,13 @@ latent_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__
     const int r = tid & 63;
     const int half = (warp >> 1) & 1, part = 2 * half + (warp >> 2);   // the lanes' 32 tokens of a step; the thread's 16 of them
     const uint32_t lane_off = static_cast<uint32_t>(warp & 3) << 21;   // 32 lanes per warp, lane in bits 16 and up
-    const uint32_t t_s = tmem_s + 16 * (warp >> 2) + lane_off, t_q = tmem + C::kColQ + 16 * C::kHeld * (warp >> 2) + lane_off, t_o = tmem + (kCols / 2) * (warp >> 2) + lane_off;
+    const uint32_t t_s = tmem_s + 16 * (warp >> 2) + lane_off, t_q = tmem + C::kColQ + lane_off, t_o = tmem + (kCols / 2) * (warp >> 2) + lane_off;
     const uint32_t id = kBarRow + (warp & 1);
     float* swap = &s_swap[part][r];
     const float* swap_row = &s_swap[0][r];
     const float sc = a.scale_log2;
     const uint64_t sc2 = pair_f32(sc, sc);
-    uint32_t u = 0;
+    uint32_t u = 0, n = 0;   // steps, stages
     int4 join = make_int4(0, 0, 0, 0);
     bool ok = true;
     for (LatentWalk w(a, s_share, shares, worker, workers); w.more(); w.next()) {
@@ -370,31 +387,26 @@ latent_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__
       const int rows = w.rows(), shift = w.r.L - w.r.n;
       const int row0 = w.row0(), row = row0 + r;
       const bool live = r < rows;
-      const int64_t at = static_cast<int64_t>(w.r.q0) * a.heads + row;   // of the queries and the output
+      const int64_t at = static_cast<int64_t>(w.r.q0) * a.heads + row;   // of the output
       const bool there = live && at >= 0 && at < a.tokens * a.heads;
-      // the unit's queries: the two warps of a lane bring half of the row each, with all loads of a part of it in flight
+      // the unit's queries out of their stage: the two warps of a lane take half of the row's panels each
       {
-        const uint4* from = reinterpret_cast<const uint4*>(a.q + at * (kLatent + PQ_LATENT_ROPE)) + 4 * C::kHeld * (warp >> 2);
-        constexpr int kBatch = 4;   // of 32 values
+        const uint32_t stage = ring + (n % C::kStages) * C::kStage + r * 128;
 #pragma unroll
-        for (int c0 = 0; c0 < C::kHeld; c0 += kBatch) {
-          uint32_t x[kBatch][16];
+        for (int g = 0; g < C::kGroups; ++g) ok = ok && warp_wait(bar_full + 8 * ((n % C::kStages) * C::kGroups + g), (n / C::kStages) & 1, wc);
+        for (int c = warp >> 2; c < 2 * C::kHeld; c += 2) {   // of 32 values
+          uint32_t x[16];
 #pragma unroll
-          for (int c = 0; c < kBatch; ++c) {
-#pragma unroll
-            for (int j = 0; j < 4; ++j) {
-              const uint4 v = there && c0 + c < C::kHeld ? __ldg(from + 4 * (c0 + c) + j) : make_uint4(0, 0, 0, 0);
-              x[c][4 * j] = v.x, x[c][4 * j + 1] = v.y, x[c][4 * j + 2] = v.z, x[c][4 * j + 3] = v.w;
-            }
-          }
-#pragma unroll
-          for (int c = 0; c < kBatch; ++c)
-            if (c0 + c < C::kHeld) tmem_st_32x16(t_q + 16 * (c0 + c), x[c]);
+          for (int j = 0; j < 4; ++j)
+            asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(x[4 * j]), "=r"(x[4 * j + 1]), "=r"(x[4 * j + 2]), "=r"(x[4 * j + 3])
+                         : "r"(stage + (c >> 1) * kPanel + ((((c & 1) * 4 + j) ^ (r & 7)) << 4)) : "memory");
+          tmem_st_32x16(t_q + 16 * c, x);
         }
         tmem_st_wait();
         tc_fence_before_sync();
         __syncwarp();
         if (lane == 0) mbar_arrive(bar_q);
+        n += 1 + w.count;
       }
       const int p0 = shift + row0 / a.heads;                                     // the first row's position
       const int see_to = live ? min(shift + row / a.heads, w.r.hi - 1) - 16 * part : -1;   // from the thread's first token
@@ -493,13 +505,14 @@ latent_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__
         const int value = (c >> 7) * 256 + half * 128 + (c & 127);   // columns 128 h .. of tensor memory are the values 256 h + 128 half ..
         if (!there) continue;
         if (whole) {
-          uint4* to = reinterpret_cast<uint4*>(a.out + at * kLatent + value);
+          __half* to = a.out + at * kLatent + value;
 #pragma unroll
-          for (int j = 0; j < 4; ++j) {
-            uint32_t x[4];
+          for (int j = 0; j < 2; ++j) {   // whole 32-byte sectors
+            uint32_t x[8];
 #pragma unroll
-            for (int k = 0; k < 4; ++k) x[k] = pack_f16(__uint_as_float(o[8 * j + 2 * k]) * inv, __uint_as_float(o[8 * j + 2 * k + 1]) * inv);
-            to[j] = make_uint4(x[0], x[1], x[2], x[3]);
+            for (int k = 0; k < 8; ++k) x[k] = pack_f16(__uint_as_float(o[16 * j + 2 * k]) * inv, __uint_as_float(o[16 * j + 2 * k + 1]) * inv);
+            asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(to + 16 * j), "r"(x[0]), "r"(x[1]), "r"(x[2]), "r"(x[3]), "r"(x[4]),
+                         "r"(x[5]), "r"(x[6]), "r"(x[7]) : "memory");
           }
         } else {
           float4* to = reinterpret_cast<float4*>(pp) + (value / 4) * kRows + r;
@@ -533,7 +546,7 @@ latent_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__
       mbar_drain(bar_drain, 0u);
     }
     if (warp == kLoader && lane == 0) {
-      for (uint32_t i = issued >= C::kStages ? issued + 1 - C::kStages : 0; i <= issued; ++i) {   // the last may be in part on its way
+      for (uint32_t i = filled >= C::kStages ? filled + 1 - C::kStages : 0; i <= filled; ++i) {   // the last may be in part on its way
         for (int g = 0; g < C::kGroups; ++g) mbar_drain(bar_full + 8 * ((i % C::kStages) * C::kGroups + g), (i / C::kStages) & 1);
       }
       mbar_drain(bar_rope, (issued & 1) ^ 1), mbar_drain(bar_rope, issued & 1);
@@ -599,12 +612,16 @@ int launch(LatentArgs& a, const void* q, int sms, cudaStream_t stream) {
   auto kern = latent_kernel<kLatent>;
   static PerDeviceOnce once;
   if (const int rc = set_dynamic_smem_once(once, kern, C::kSmem); rc != PQ_OK) return rc;
-  CUtensorMap mq = {}, mc = {};
-  const uint64_t wide = kLatent + PQ_LATENT_ROPE;
+  CUtensorMap mq = {}, mc = {}, mr = {};
+  const uint64_t wide = kLatent + PQ_LATENT_ROPE, rows = static_cast<uint64_t>(a.c.pages) * a.c.page;
   if (const int rc = make_tmap_2d(&mq, q, static_cast<uint64_t>(a.tokens) * a.heads, wide, kRows, 64, 2, 128); rc != PQ_OK) return rc;
-  if (const int rc = make_tmap_2d(&mc, a.c.data, static_cast<uint64_t>(a.c.pages) * a.c.page, wide, a.box, 64, 2, 128); rc != PQ_OK) return rc;
+  // values of a panel, rows of 8, panels, groups of 8 rows
+  const uint64_t dims[4] = {64, 8, static_cast<uint64_t>(C::kPanels), rows / 8}, strides[3] = {wide * 2, 128, wide * 16};
+  const uint32_t box[4] = {64, 8, 4, static_cast<uint32_t>(a.box / 8)}, rope_box[4] = {64, 8, 1, static_cast<uint32_t>(a.box / 8)};
+  if (const int rc = make_tmap_f16(&mc, a.c.data, 4, dims, strides, box); rc != PQ_OK) return rc;
+  if (const int rc = make_tmap_f16(&mr, a.c.data, 4, dims, strides, rope_box); rc != PQ_OK) return rc;
   const unsigned grid = static_cast<unsigned>(a.paired ? sms & ~1 : sms);
-  if (const int rc = launch_dependent(kern, dim3(grid), dim3(kThreads), C::kSmem, stream, mq, mc, a); rc != PQ_OK || !a.partials) return rc;
+  if (const int rc = launch_dependent(kern, dim3(grid), dim3(kThreads), C::kSmem, stream, mq, mc, mr, a); rc != PQ_OK || !a.partials) return rc;
   return launch_dependent(latent_join_kernel<kLatent>, dim3(grid, kLatent / 16), dim3(kJoinThreads), 0, stream, a);
 }
 
@@ -627,7 +644,7 @@ int pq_latent_attention(const void* q_f16, int32_t heads, const pq_latent_cache*
   if (!q_f16 || !block_table || !q_start || !kv_len || !out_f16) return PQ_ERR_NULL;
   if (!aligned16(q_f16) || !aligned16(out_f16) || !aligned256(workspace)) return PQ_ERR_ALIGN;
   if ((rc = check_arch()) != PQ_OK) return rc;
-  LatentArgs a{*cache, block_table, width, q_start, kv_len, static_cast<const __half*>(q_f16), static_cast<__half*>(out_f16), tokens, static_cast<int>(requests), heads,
+  LatentArgs a{*cache, block_table, width, q_start, kv_len, static_cast<__half*>(out_f16), tokens, static_cast<int>(requests), heads,
                0, scale * 1.44269504f, 0xffffffffu, 0u, nullptr, nullptr, kKeys, device_status_ptr(), wait_limit()};
   if (a.status == nullptr) return PQ_ERR_CUDA;
   while (cache->page % a.box != 0) a.box /= 2;   // the page is a multiple of 16
