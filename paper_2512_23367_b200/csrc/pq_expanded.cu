@@ -3,6 +3,7 @@
 #include <cuda_fp16.h>
 
 #include <cmath>
+#include <type_traits>
 
 #include "pq_attention.h"
 #include "pq_attn_mma.cuh"
@@ -185,47 +186,75 @@ expanded_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant
       const uint32_t leader = elect_one();
       const uint32_t q_lo = desc_k(sq), k_lo0 = desc_k(ring_k), v_lo0 = desc_mn(ring_v, kPanelK);
       bool live = true;
-      uint32_t g = 0, seg = 0;   // key tiles, units before this one
+      uint32_t n = 0, seg = 0;   // key tiles, units before
+      // S = Q K^T of the accumulator's query tile, O += P V of the step before it.  Which accumulator, and so every operand but the
+      // stage, is known at compile time: with operands in other than uniform registers an MMA takes 85 to 100 cycles to issue, and
+      // a step took 3300.
+      auto scores = [&](auto acc, auto tile, uint32_t stage, bool gives_back, bool last) {
+        if (leader && live) {
+          const uint32_t ql = q_lo + decltype(tile)::value * (kQueryBytes / 16), kl = k_lo0 + stage * (kKeyBytes / 16);
+          umma_f16_ss<0>(tmem, ql, kl, id_qk);
+#pragma unroll
+          for (int k = 1; k < kQuery / 16; ++k) umma_f16_ss<1>(tmem, ql + (k / 4) * (kPanelQ / 16) + (k % 4) * 2, kl + (k / 4) * (kPanelK / 16) + (k % 4) * 2, id_qk);
+          umma_commit(bar_s + 8 * decltype(acc)::value);
+          if (gives_back) umma_commit(bar_kfree + 8 * stage);
+          if (last) umma_commit(bar_qfree);
+        }
+        __syncwarp();
+      };
+      auto sums = [&](auto acc, uint32_t stage, bool first, bool gives_back) {
+        named_bar_sync(kBarP + decltype(acc)::value, 288);
+        tc_fence_after_sync();
+        if (leader && live) {
+          const uint32_t vl = v_lo0 + stage * (kValueBytes / 16), d = tmem + kColO + decltype(acc)::value * kValue, p = tmem + kColP + decltype(acc)::value * (kKeys / 2);
+          umma_f16_ts(d, p, vl, id_pv, first ? 0u : 1u);
+#pragma unroll
+          for (int k = 1; k < kKeys / 16; ++k) umma_f16_ts(d, p + 8 * k, vl + k * 128, id_pv, 1u);
+          umma_commit(bar_o + 8 * decltype(acc)::value);
+          if (gives_back) umma_commit(bar_vfree + 8 * stage);
+        }
+        __syncwarp();
+      };
+      auto landed = [&]() {
+        live = tile_landed(kBarTile, true) && live;
+        tc_fence_after_sync();
+      };
+      auto read = [&](auto acc) {   // the accumulator's S is in registers
+        named_bar_sync(kBarRead + decltype(acc)::value, 288);
+        tc_fence_after_sync();
+      };
+      constexpr std::integral_constant<int, 0> k0{};
+      constexpr std::integral_constant<int, 1> k1{};
       for (Walk<ExpandedArgs> w(a, s_share, shares, blockIdx.x, gridDim.x); w.more(); w.next()) {
-        const Part part(w);
-        const bool two = part.two;
+        const bool two = Part(w).two;
         live = live && warp_wait(bar_q, seg & 1, wc);
-        for (int u = 0; u < part.N + part.lag; ++u) {
-          if (u > 0 && u <= part.N) named_bar_sync(kBarRead + ((u - 1) & 1), 288);   // S(u - 1) is in registers
-          if (u < part.N) {   // S(u) = Q K^T
-            const uint32_t acc = u & 1, st = (g + (two ? u >> 1 : u)) & 1;
-            if (!two || acc == 0) live = tile_landed(kBarTile, true) && live;
-            tc_fence_after_sync();
-            if (leader && live) {
-              const uint32_t ql = q_lo + (two ? acc * (kQueryBytes / 16) : 0), kl = k_lo0 + st * (kKeyBytes / 16);
-              umma_f16_ss<0>(tmem, ql, kl, id_qk);
-#pragma unroll
-              for (int k = 1; k < kQuery / 16; ++k) umma_f16_ss<1>(tmem, ql + (k / 4) * (kPanelQ / 16) + (k % 4) * 2, kl + (k / 4) * (kPanelK / 16) + (k % 4) * 2, id_qk);
-              umma_commit(bar_s + 8 * acc);
-              if (!two || acc == 1) umma_commit(bar_kfree + 8 * st);
-              if (u == part.N - 1) umma_commit(bar_qfree);
-            }
-            __syncwarp();
+        auto sums_free = [&](int t) {   // the sums of the unit before have been read
+          if (t == 1 && seg > 0) live = warp_wait(bar_read, (seg - 1) & 1, wc) && live;
+        };
+        if (two) {   // S of both query tiles, then O of both of the key tile before
+          for (int t = 0; t <= w.count; ++t) {
+            const bool more = t < w.count;
+            if (t > 0) read(k1);
+            if (more) landed(), scores(k0, k0, n & 1, false, false);
+            if (t > 0) landed(), sums_free(t), sums(k0, (n - 1) & 1, t == 1, false);
+            if (more) read(k0), scores(k1, k1, n & 1, true, t == w.count - 1);
+            if (t > 0) sums(k1, (n - 1) & 1, t == 1, true);
+            if (more) ++n;
           }
-          if (u >= part.lag) {   // O(u - lag) += P V
-            const int v = u - part.lag;
-            const uint32_t acc = v & 1, st = (g + (two ? v >> 1 : v)) & 1;
-            if (!two || acc == 0) live = tile_landed(kBarTile, true) && live;
-            if (v == 0 && seg > 0) live = warp_wait(bar_read, (seg - 1) & 1, wc) && live;   // the sums of the unit before have been read
-            named_bar_sync(kBarP + acc, 288);
-            tc_fence_after_sync();
-            if (leader && live) {
-              const uint32_t vl = v_lo0 + st * (kValueBytes / 16), d = tmem + kColO + acc * kValue, p = tmem + kColP + acc * (kKeys / 2);
-              umma_f16_ts(d, p, vl, id_pv, (v >> 1) > 0);
-#pragma unroll
-              for (int k = 1; k < kKeys / 16; ++k) umma_f16_ts(d, p + 8 * k, vl + k * 128, id_pv, 1u);
-              umma_commit(bar_o + 8 * acc);
-              if (!two || acc == 1) umma_commit(bar_vfree + 8 * st);
-            }
-            __syncwarp();
+        } else {     // the accumulators take the even and the odd key tiles of one query tile
+          for (int t = 0; t <= w.count; t += 2) {
+            if (t > 0) read(k1);
+            if (t < w.count) landed(), scores(k0, k0, n & 1, true, t == w.count - 1);
+            if (t > 0) landed(), sums(k1, (n - 1) & 1, t == 2, true);
+            if (t < w.count) ++n;
+            if (t + 1 > w.count) break;
+            read(k0);
+            if (t + 1 < w.count) landed(), scores(k1, k0, n & 1, true, t + 1 == w.count - 1);
+            landed(), sums_free(t + 1), sums(k0, (n - 1) & 1, t == 0, true);
+            if (t + 1 < w.count) ++n;
           }
         }
-        g += w.count, ++seg;
+        ++seg;
       }
     } else if (warp == kWatcher) {
       // ------------------------------------------------------------------ watcher: waits for the operand tiles a step ahead
