@@ -17,7 +17,7 @@ namespace {
 
 constexpr int kTile = 128;          // query rows of one accumulator
 constexpr int kUnit = 2 * kTile;    // of a unit
-constexpr int kKeys = 96;           // keys of one step
+constexpr int kKeys = 80;           // keys of one step
 constexpr int kNope = 128, kValue = 128, kQuery = kNope + PQ_LATENT_ROPE;
 constexpr int kSoft = 512;          // threads of the four softmax warpgroups, two per accumulator
 constexpr int kIssuer = 16, kLoadK = 17, kWatcher = 18, kLoadV = 19, kThreads = 640;   // warps
@@ -27,8 +27,9 @@ constexpr int kQueryBytes = 3 * kPanelQ, kKeyBytes = 3 * kPanelK, kValueBytes = 
 constexpr int kSmem = 2 * kQueryBytes + 2 * kKeyBytes + 2 * kValueBytes + 1024 /* alignment */;
 constexpr int kPartFloats = kUnit * (kValue + 2);   // per query tile [32][128 rows] x 4 sums, then [128 rows] x (reference, sum of weights)
 constexpr int kLeastSteps = 4;      // of a CTA, so that its parts are worth joining
-// Tensor memory: S, shared by the accumulators in turn; P of each; O of each.
-constexpr uint32_t kColP = 96, kColO = 256;
+// Tensor memory columns: S, P and O of each accumulator.
+constexpr uint32_t kColP = 2 * kKeys, kColO = 256;
+static_assert(kColP + kKeys <= kColO, "tensor memory");
 // Named barriers, as in the paged tile kernel: "P written" (two), "operand tile landed", the two warps that share 32 rows
 // (eight pairs), "S read" (two), accumulators' sums.
 constexpr uint32_t kBarP = 1, kBarTile = 3, kBarPair = 4, kBarRead = 12, kBarSoft = 14;
@@ -47,9 +48,10 @@ struct ExpandedArgs {
   int* status;
   uint32_t wait_limit;
 
+  __device__ __forceinline__ UnitShape shape() const { return UnitShape{kUnit, 1, kKeys, heads}; }
   __device__ __forceinline__ Request request(int b) const {
     Request r;
-    r.s = UnitShape{kUnit, 1, kKeys, heads};
+    r.s = shape();
     r.q0 = q_start[b];
     r.n = static_cast<int>(min(static_cast<int64_t>(max(q_start[b + 1] - r.q0, 0)), tokens));
     r.k0 = kv_start[b];
@@ -74,9 +76,11 @@ struct Part {
 // take the even and the odd key tiles and are joined at the end: one's softmax runs while the tensor core works for the
 // other, as in the paged tile kernel.  What differs:
 //   - the product with the keys goes over 192 values, 128 of the head and 64 that all heads share, so that queries and keys
-//     take half as much shared memory again.  With steps of 128 keys one step and a half would fit; with 96 two steps do, and
-//     loads run a whole step ahead.  S takes 12 MMAs of N = 96 (56 cycles each, bound by shared memory; 48 by arithmetic),
-//     O 6 of N = 128: 2112 cycles per 256 x 96 scores where arithmetic alone would take 1920.
+//     take half as much shared memory again.  With steps of 128 keys one step and a half would fit; with 80 two steps do, loads
+//     run a whole step ahead, and tensor memory has room for an S of each accumulator (with 96 keys and one S in turn, the
+//     tensor core waited 300 of 1390 cycles for S to be read: a prompt of 4096 took 180 us).  S takes 12 MMAs of N = 80 (51
+//     cycles each, bound by shared memory; 40 by arithmetic), O 5 of N = 128 (64): 1864 cycles per 256 x 80 scores where
+//     arithmetic alone would take 1600.
 //   - a CTA stays on its SM and walks through its units: queries of the next one are on the way, and its first S computed,
 //     while the results of the last one go out.
 //   - keys and values are rows of one linear's output, read through one tensor map with heads as its second dimension.
@@ -193,9 +197,10 @@ expanded_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant
       auto scores = [&](auto acc, auto tile, uint32_t stage, bool gives_back, bool last) {
         if (leader && live) {
           const uint32_t ql = q_lo + decltype(tile)::value * (kQueryBytes / 16), kl = k_lo0 + stage * (kKeyBytes / 16);
-          umma_f16_ss<0>(tmem, ql, kl, id_qk);
+          const uint32_t d = tmem + decltype(acc)::value * kKeys;
+          umma_f16_ss<0>(d, ql, kl, id_qk);
 #pragma unroll
-          for (int k = 1; k < kQuery / 16; ++k) umma_f16_ss<1>(tmem, ql + (k / 4) * (kPanelQ / 16) + (k % 4) * 2, kl + (k / 4) * (kPanelK / 16) + (k % 4) * 2, id_qk);
+          for (int k = 1; k < kQuery / 16; ++k) umma_f16_ss<1>(d, ql + (k / 4) * (kPanelQ / 16) + (k % 4) * 2, kl + (k / 4) * (kPanelK / 16) + (k % 4) * 2, id_qk);
           umma_commit(bar_s + 8 * decltype(acc)::value);
           if (gives_back) umma_commit(bar_kfree + 8 * stage);
           if (last) umma_commit(bar_qfree);
@@ -234,23 +239,22 @@ expanded_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant
         if (two) {   // S of both query tiles, then O of both of the key tile before
           for (int t = 0; t <= w.count; ++t) {
             const bool more = t < w.count;
-            if (t > 0) read(k1);
+            if (t > 0) read(k0);
             if (more) landed(), scores(k0, k0, n & 1, false, false);
             if (t > 0) landed(), sums_free(t), sums(k0, (n - 1) & 1, t == 1, false);
-            if (more) read(k0), scores(k1, k1, n & 1, true, t == w.count - 1);
+            if (t > 0) read(k1);
+            if (more) scores(k1, k1, n & 1, true, t == w.count - 1);
             if (t > 0) sums(k1, (n - 1) & 1, t == 1, true);
             if (more) ++n;
           }
         } else {     // the accumulators take the even and the odd key tiles of one query tile
           for (int t = 0; t <= w.count; t += 2) {
-            if (t > 0) read(k1);
             if (t < w.count) landed(), scores(k0, k0, n & 1, true, t == w.count - 1);
-            if (t > 0) landed(), sums(k1, (n - 1) & 1, t == 2, true);
+            if (t > 0) landed(), read(k1), sums(k1, (n - 1) & 1, t == 2, true);
             if (t < w.count) ++n;
             if (t + 1 > w.count) break;
-            read(k0);
             if (t + 1 < w.count) landed(), scores(k1, k0, n & 1, true, t + 1 == w.count - 1);
-            landed(), sums_free(t + 1), sums(k0, (n - 1) & 1, t == 0, true);
+            landed(), sums_free(t + 1), read(k0), sums(k0, (n - 1) & 1, t == 0, true);
             if (t + 1 < w.count) ++n;
           }
         }
@@ -279,10 +283,10 @@ expanded_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant
     // -------------------------------------------------------------------- softmax, two threads per row
     asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kSoftRegs));
     const int acc = warp >> 3;                       // accumulator
-    const int half = (warp >> 2) & 1;                // the thread's 48 keys of a tile, and its half of the values
+    const int half = (warp >> 2) & 1;                // the thread's 40 keys of a tile, and its half of the values
     const int r = tid & 127;                         // row of the tile
     const uint32_t lane_off = static_cast<uint32_t>(warp & 3) << 21;   // 32 lanes per warp, lane in bits 16 and up
-    const uint32_t t_s = tmem + 48 * half + lane_off, t_p = tmem + kColP + acc * (kKeys / 2) + 24 * half + lane_off;
+    const uint32_t t_s = tmem + acc * kKeys + 40 * half + lane_off, t_p = tmem + kColP + acc * (kKeys / 2) + 20 * half + lane_off;
     const uint32_t t_out = tmem + kColO + acc * kValue + half * (kValue / 2) + lane_off;
     float* swap = s_swap + acc * kTile + r;
     const uint32_t pair = kBarPair + acc * 4 + (warp & 3);
@@ -296,7 +300,7 @@ expanded_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant
       const bool two = part.two;
       const int tok = (two ? acc * kTile : 0) + r;   // of the unit
       const int p0 = w.r.L - w.r.n + w.tile * kUnit + (two ? acc * kTile : 0);   // position of the tile's first row
-      const int see_to = min(p0 + r, w.r.hi - 1) - 48 * half;                    // last key of the row, from the thread's first
+      const int see_to = min(p0 + r, w.r.hi - 1) - 40 * half;                    // last key of the row, from the thread's first
       const int all_to = min(p0 + 1, w.r.hi);                                    // every row sees the keys before
       const int mine = two ? w.count : (w.count - acc + 1) >> 1;
       float m = -INFINITY, l = 0.0f;   // m: the reference that is subtracted, in powers of two; l: the thread's own keys
@@ -304,9 +308,9 @@ expanded_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant
         const int key0 = (w.step + (two ? i : 2 * i + acc)) * kKeys;
         ok = ok && warp_wait(bar_s + 8 * acc, n & 1, wc);
         tc_fence_after_sync();
-        uint32_t s[32], s2[16];
+        uint32_t s[32], s2[8];
         tmem_ld_32x32(t_s, s);
-        tmem_ld_32x16(t_s + 32, s2);
+        tmem_ld_32x8(t_s + 32, s2);
         tmem_ld_wait();
         tc_fence_before_sync();
         hand_over(kBarRead + acc, 288, ok);
@@ -314,7 +318,7 @@ expanded_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant
 #pragma unroll
           for (int j = 0; j < 32; ++j) s[j] = (s[j] & a.q_and) ^ a.q_xor;
 #pragma unroll
-          for (int j = 0; j < 16; ++j) s2[j] = (s2[j] & a.q_and) ^ a.q_xor;
+          for (int j = 0; j < 8; ++j) s2[j] = (s2[j] & a.q_and) ^ a.q_xor;
         }
         if (key0 + kKeys > all_to) {   // some row does not see all keys
           const int to = see_to - key0;
@@ -322,19 +326,20 @@ expanded_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant
           for (int j = 0; j < 32; ++j)
             if (j > to) s[j] = 0xff800000u;   // -inf
 #pragma unroll
-          for (int j = 0; j < 16; ++j)
+          for (int j = 0; j < 8; ++j)
             if (32 + j > to) s2[j] = 0xff800000u;
         }
-        float top[3];
+        float top[4];   // of the eights at 8 h, and of those left at 32
 #pragma unroll
-        for (int h = 0; h < 3; ++h) {
-          const uint32_t* v = h < 2 ? s + 16 * h : s2;
+        for (int h = 0; h < 4; ++h) {
+          const uint32_t* v = s + 8 * h;
           top[h] = max3(__uint_as_float(v[0]), __uint_as_float(v[1]), __uint_as_float(v[2]));
-#pragma unroll
-          for (int j = 3; j < 15; j += 2) top[h] = max3(top[h], __uint_as_float(v[j]), __uint_as_float(v[j + 1]));
-          top[h] = fmaxf(top[h], __uint_as_float(v[15]));
+          top[h] = max3(top[h], __uint_as_float(v[3]), __uint_as_float(v[4]));
+          top[h] = max3(top[h], __uint_as_float(v[5]), __uint_as_float(v[6]));
+          top[h] = max3(top[h], __uint_as_float(v[7]), __uint_as_float(s2[2 * h]));
+          top[h] = fmaxf(top[h], __uint_as_float(s2[2 * h + 1]));
         }
-        float t = max3(top[0], top[1], top[2]) * sc;
+        float t = fmaxf(max3(top[0], top[1], top[2]), top[3]) * sc;
         bool done = i == 0;   // the product with the weights before these has been taken
         if (pair_any(pair, t > m + 8.0f)) {   // rare after the first tiles: some row of the 32
           t = pair_combine<false>(swap, pair, half, t);
@@ -359,7 +364,7 @@ expanded_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant
         }
         const float off = kTop - (m == -INFINITY ? 0.0f : m);
         const uint64_t off2 = pair_f32(off, off);
-        uint32_t p[16], p2[8], asked = 0;
+        uint32_t p[16], p2[4], asked = 0;
         uint64_t sum = 0;
         auto weigh = [&](uint32_t x0, uint32_t x1) {
           float e0, e1;
@@ -373,14 +378,14 @@ expanded_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant
         for (int j = 0; j < 16; ++j) p[j] = weigh(s[2 * j], s[2 * j + 1]);
         asked = mbar_test2(bar_o + 8 * acc, (n - 1) & 1, bar_o + 8 * acc, (n - 1) & 1);
 #pragma unroll
-        for (int j = 0; j < 8; ++j) p2[j] = weigh(s2[2 * j], s2[2 * j + 1]);
+        for (int j = 0; j < 4; ++j) p2[j] = weigh(s2[2 * j], s2[2 * j + 1]);
         float l0, l1;
         unpair_f32(sum, l0, l1);
         l += l0 + l1;
         if (!done && !__all_sync(0xffffffffu, asked)) ok = ok && warp_wait(bar_o + 8 * acc, (n - 1) & 1, wc);
         tc_fence_after_sync();
         tmem_st_32x16(t_p, p);
-        tmem_st_32x8(t_p + 16, p2);
+        tmem_st_32x4(t_p + 16, p2);
         tmem_st_wait();
         tc_fence_before_sync();
         hand_over(kBarP + acc, 288, ok);
@@ -429,10 +434,9 @@ expanded_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant
           }
           if (!writes) continue;
           if (whole) {
-#pragma unroll
-            for (int j = 0; j < 2; ++j)
-              reinterpret_cast<uint4*>(to)[2 * h + j] = make_uint4(pack_f16(v[8 * j] * inv, v[8 * j + 1] * inv), pack_f16(v[8 * j + 2] * inv, v[8 * j + 3] * inv),
-                                                                   pack_f16(v[8 * j + 4] * inv, v[8 * j + 5] * inv), pack_f16(v[8 * j + 6] * inv, v[8 * j + 7] * inv));
+            store_32_bytes(to + 16 * h, pack_f16(v[0] * inv, v[1] * inv), pack_f16(v[2] * inv, v[3] * inv), pack_f16(v[4] * inv, v[5] * inv),
+                           pack_f16(v[6] * inv, v[7] * inv), pack_f16(v[8] * inv, v[9] * inv), pack_f16(v[10] * inv, v[11] * inv),
+                           pack_f16(v[12] * inv, v[13] * inv), pack_f16(v[14] * inv, v[15] * inv));
           } else {
 #pragma unroll
             for (int j = 0; j < 4; ++j)
@@ -473,46 +477,21 @@ expanded_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant
   if (warp == kIssuer) tmem_dealloc(tmem, 512);
 }
 
-// Joins the parts of units that were cut: a block per CTA that had a unit's first part, 32 rows and 32 values, a warp per 4
-// of them, lanes along the rows.
-constexpr int kJoinThreads = 256;
-__global__ void __launch_bounds__(kJoinThreads) expanded_join_kernel(const ExpandedArgs a) {
+// Joins the parts of units that were cut: blocks per CTA that had a unit's first part, query tile and 32 values with one group of
+// threads per row, 16 with four.
+template <int kGroups>
+__global__ void __launch_bounds__((kGroups > 1 ? kGroups : 2) * kTile) expanded_join_kernel(const ExpandedArgs a) {
   grid_dep_launch();
   grid_dep_wait();
-  const int4 join = a.joins[blockIdx.x];
-  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  const int tile = blockIdx.y / 4, r = (blockIdx.y % 4) * 32 + lane, tok = tile * kTile + r, f4 = blockIdx.z * 8 + warp;
+  const int4 join = a.joins[blockIdx.x];   // first token, tokens, head, parts
+  const int tile = blockIdx.y, tok = tile * kTile + static_cast<int>(threadIdx.x % kTile);
+  const int first = kGroups > 1 ? blockIdx.z * 16 : blockIdx.z * 32 + static_cast<int>(threadIdx.x / kTile) * 16;
+  if (join.w == 0 || tile * kTile >= join.y) return;
   const int64_t row = static_cast<int64_t>(join.x) + tok;
-  if (join.w == 0 || tok >= join.y || row < 0 || row >= a.tokens) return;
   // the unit's first part is the second one of its CTA, the others the first of theirs
   auto part = [&](int i) { return a.partials + (2 * (static_cast<int64_t>(blockIdx.x) + i) + (i == 0)) * kPartFloats + tile * (kTile * (kValue + 2)); };
-  float M = -INFINITY, L = 0.0f;
-  float4 v = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-  constexpr int kBatch = 8;   // parts whose loads are in flight together
-  for (int i0 = 0; i0 < join.w; i0 += kBatch) {
-    float2 ml[kBatch];
-    float4 x[kBatch];
-#pragma unroll
-    for (int j = 0; j < kBatch; ++j) {
-      const float* p = part(min(i0 + j, join.w - 1));
-      ml[j] = __ldcg(reinterpret_cast<const float2*>(p + kTile * kValue) + r);
-      x[j] = __ldcg(reinterpret_cast<const float4*>(p) + f4 * kTile + r);
-    }
-    float top = M;
-#pragma unroll
-    for (int j = 0; j < kBatch; ++j) top = fmaxf(top, ml[j].x);
-    const float ref = top == -INFINITY ? 0.0f : top, f = exp2_approx(M - ref);
-    M = top;
-    L *= f, v.x *= f, v.y *= f, v.z *= f, v.w *= f;
-#pragma unroll
-    for (int j = 0; j < kBatch; ++j) {
-      const float wt = i0 + j < join.w ? exp2_approx(ml[j].x - ref) : 0.0f;
-      L = fmaf(ml[j].y, wt, L);
-      v.x = fmaf(x[j].x, wt, v.x), v.y = fmaf(x[j].y, wt, v.y), v.z = fmaf(x[j].z, wt, v.z), v.w = fmaf(x[j].w, wt, v.w);
-    }
-  }
-  const float inv = L > 0.0f ? 1.0f / L : 0.0f;
-  *reinterpret_cast<uint2*>(a.out + (row * a.heads + join.z) * kValue + 4 * f4) = make_uint2(pack_f16(v.x * inv, v.y * inv), pack_f16(v.z * inv, v.w * inv));
+  const bool there = tok < join.y && row >= 0 && row < a.tokens;
+  join_parts<kTile, kValue, kGroups>(part, join.w, first, there ? a.out + (row * a.heads + join.z) * kValue + first : nullptr);
 }
 
 }  // namespace
@@ -577,7 +556,8 @@ int pq_expanded_attention(const void* q_f16, int64_t q_stride, int32_t heads, co
   if ((rc = make_tmap_heads(&mkv, kv_f16, keys, none ? 1 : heads, none ? kQuery : kNope + kValue, kv_stride, kNope + kValue, kKeys)) != PQ_OK) return rc;
   if ((rc = make_tmap_heads(&mr, k_rope_f16, keys, 1, PQ_LATENT_ROPE, k_rope_stride, PQ_LATENT_ROPE, kKeys)) != PQ_OK) return rc;
   if ((rc = launch_dependent(expanded_kernel, dim3(sms), dim3(kThreads), kSmem, st, mq, mkv, mr, a)) != PQ_OK || !a.shares) return rc;
-  return launch_dependent(expanded_join_kernel, dim3(sms, kUnit / 32, kValue / 32), dim3(kJoinThreads), 0, st, a);
+  return many_parts(units, sms, keys / kKeys, kLeastSteps) ? launch_dependent(expanded_join_kernel<4>, dim3(sms, kUnit / kTile, kValue / 16), dim3(4 * kTile), 0, st, a)
+                          : launch_dependent(expanded_join_kernel<1>, dim3(sms, kUnit / kTile, kValue / 32), dim3(2 * kTile), 0, st, a);
 }
 
 }  // extern "C"

@@ -56,9 +56,10 @@ struct LatentArgs {
   int* status;
   uint32_t wait_limit;
 
+  __device__ __forceinline__ UnitShape shape() const { return UnitShape{paired ? 2 * kRows : kRows, heads, kKeys, 1}; }
   __device__ __forceinline__ Request request(int b) const {
     Request r;
-    r.s = UnitShape{paired ? 2 * kRows : kRows, heads, kKeys, 1};
+    r.s = shape();
     r.q0 = q_start[b];
     r.n = static_cast<int>(min(static_cast<int64_t>(max(q_start[b + 1] - r.q0, 0)), tokens));
     r.k0 = 0;
@@ -511,8 +512,7 @@ latent_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__
             uint32_t x[8];
 #pragma unroll
             for (int k = 0; k < 8; ++k) x[k] = pack_f16(__uint_as_float(o[16 * j + 2 * k]) * inv, __uint_as_float(o[16 * j + 2 * k + 1]) * inv);
-            asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(to + 16 * j), "r"(x[0]), "r"(x[1]), "r"(x[2]), "r"(x[3]), "r"(x[4]),
-                         "r"(x[5]), "r"(x[6]), "r"(x[7]) : "memory");
+            store_32_bytes(to + 16 * j, x[0], x[1], x[2], x[3], x[4], x[5], x[6], x[7]);
           }
         } else {
           float4* to = reinterpret_cast<float4*>(pp) + (value / 4) * kRows + r;
@@ -559,49 +559,22 @@ latent_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__
   if (warp == kIssuer) tmem_dealloc(tmem, 512);
 }
 
-// Joins the parts of units that were cut: a block per CTA that had a unit's first part and 16 values, a thread per row and
-// 4 of them, lanes along the rows.  L2 latency, so the loads of several parts are in flight together.
-constexpr int kJoinThreads = 256;
-template <int kLatent>
+// Joins the parts of units that were cut: blocks per CTA that had a unit's first part, of 16 values with four groups of threads
+// per row, of 64 with one.
+constexpr int kJoinGroups = 4, kJoinThreads = 4 * kRows;
+template <int kLatent, int kGroups>
 __global__ void __launch_bounds__(kJoinThreads) latent_join_kernel(const LatentArgs a) {
   grid_dep_launch();
   grid_dep_wait();
-  const int4 join = a.joins[blockIdx.x];
-  const int r = threadIdx.x & 63, f4 = blockIdx.y * 4 + (threadIdx.x >> 6);
-  if (r >= join.z) return;
+  const int4 join = a.joins[blockIdx.x];   // first row (64 bits), rows, parts
+  if (join.w == 0) return;
+  const int r = threadIdx.x % kRows, first = kGroups > 1 ? blockIdx.y * 16 : blockIdx.y * 64 + threadIdx.x / kRows * 16;
   const int64_t at = (static_cast<int64_t>(join.y) << 32 | static_cast<uint32_t>(join.x)) + r;
-  if (at < 0 || at >= a.tokens * a.heads) return;
-  constexpr int kPart = LatentCfg<kLatent>::kPartFloats;
   const int next = a.paired ? 2 : 1;
   // the unit's first part is the second one of its CTA, the others the first of theirs
-  auto part = [&](int i) { return a.partials + (2 * (static_cast<int64_t>(blockIdx.x) + i * next) + (i == 0)) * kPart; };
-  float M = -INFINITY, L = 0.0f;
-  float4 v = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-  constexpr int kBatch = 8;
-  for (int i0 = 0; i0 < join.w; i0 += kBatch) {
-    float2 ml[kBatch];
-    float4 x[kBatch];
-#pragma unroll
-    for (int j = 0; j < kBatch; ++j) {
-      const float* p = part(min(i0 + j, join.w - 1));
-      ml[j] = __ldcg(reinterpret_cast<const float2*>(p + kRows * kLatent) + r);
-      x[j] = __ldcg(reinterpret_cast<const float4*>(p) + f4 * kRows + r);
-    }
-    float top = M;
-#pragma unroll
-    for (int j = 0; j < kBatch; ++j) top = fmaxf(top, ml[j].x);
-    const float ref = top == -INFINITY ? 0.0f : top, f = exp2_approx(M - ref);
-    M = top;
-    L *= f, v.x *= f, v.y *= f, v.z *= f, v.w *= f;
-#pragma unroll
-    for (int j = 0; j < kBatch; ++j) {
-      const float w = i0 + j < join.w ? exp2_approx(ml[j].x - ref) : 0.0f;
-      L = fmaf(ml[j].y, w, L);
-      v.x = fmaf(x[j].x, w, v.x), v.y = fmaf(x[j].y, w, v.y), v.z = fmaf(x[j].z, w, v.z), v.w = fmaf(x[j].w, w, v.w);
-    }
-  }
-  const float inv = L > 0.0f ? 1.0f / L : 0.0f;
-  *reinterpret_cast<uint2*>(a.out + at * kLatent + 4 * f4) = make_uint2(pack_f16(v.x * inv, v.y * inv), pack_f16(v.z * inv, v.w * inv));
+  auto part = [&](int i) { return a.partials + (2 * (static_cast<int64_t>(blockIdx.x) + i * next) + (i == 0)) * LatentCfg<kLatent>::kPartFloats; };
+  const bool there = r < join.z && at >= 0 && at < a.tokens * a.heads;
+  join_parts<kRows, kLatent, kGroups>(part, join.w, first, there ? a.out + at * kLatent + first : nullptr);
 }
 
 size_t partial_bytes(int latent, int sms) { return static_cast<size_t>(sms) * (2 * kRows * (latent + 2) * sizeof(float) + sizeof(int4)); }
@@ -622,7 +595,9 @@ int launch(LatentArgs& a, const void* q, int sms, cudaStream_t stream) {
   if (const int rc = make_tmap_f16(&mr, a.c.data, 4, dims, strides, rope_box); rc != PQ_OK) return rc;
   const unsigned grid = static_cast<unsigned>(a.paired ? sms & ~1 : sms);
   if (const int rc = launch_dependent(kern, dim3(grid), dim3(kThreads), C::kSmem, stream, mq, mc, mr, a); rc != PQ_OK || !a.partials) return rc;
-  return launch_dependent(latent_join_kernel<kLatent>, dim3(grid, kLatent / 16), dim3(kJoinThreads), 0, stream, a);
+  const int64_t units = a.tokens * a.heads / (a.paired ? 2 * kRows : kRows) + a.requests;
+  return many_parts(units, static_cast<int>(grid), a.width * a.c.page / kKeys, kLeastSteps) ? launch_dependent(latent_join_kernel<kLatent, kJoinGroups>, dim3(grid, kLatent / 16), dim3(kJoinThreads), 0, stream, a)
+                           : launch_dependent(latent_join_kernel<kLatent, 1>, dim3(grid, kLatent / 64), dim3(kJoinThreads), 0, stream, a);
 }
 
 }  // namespace

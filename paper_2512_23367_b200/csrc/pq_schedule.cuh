@@ -5,10 +5,14 @@
 // its last row sees.  Two ways to hand units out:
 //   shares   the steps of all units, in order, are cut into runs of one length, one per CTA, so that every SM takes the same
 //            share whatever the lengths are.  A share may begin and end inside a unit: that unit's parts are joined later.
-//   turns    CTA c takes the units c, c + CTAs, ...: whole units, a request's last tile, which sees most keys, first.
+//   turns    whole units, a request's last tile, which sees most keys, first: CTA c of n takes the units c, 2n - 1 - c, 2n + c, ...,
+//            there and back again, so that who has the largest of one turn has the smallest of the next (512 units of a prompt of
+//            4096: the longest CTA has 3 % more than its share; with c, n + c, 2n + c, ... it had 26).
 #pragma once
 #include <cstdint>
 
+#include "pq_attention.h"
+#include "pq_attn_mma.cuh"
 #include "pq_ptx.cuh"
 
 namespace pq {
@@ -120,67 +124,168 @@ __device__ __forceinline__ void find_share(const Args& a, int worker, int worker
   __syncthreads();
 }
 
-// Walks the units of one CTA, as every warp of it does for itself; all lanes together.
+// Walks the units of one CTA, as every warp of it does for itself; all lanes together.  By turns, a lane keeps one of 32
+// requests, so that going on to the next unit reads no memory (it took 3000 cycles between a unit's end and the next one's begin).
 template <class Args>
 struct Walk {
   const Args& a;
   const bool shares;
-  const int workers;
-  int b;
-  int unit;                         // shares: as in Share; turns: counted from request b's first
+  int step_there, step_back;        // turns: to the next unit
+  int b;                            // request
+  int unit;                         // shares: as in Share; turns: counted from request `base`'s first
   int64_t left;                     // turns: 1 as long as there are any
   int step, count, all_steps;       // the unit's steps: first, how many, of all
   int tile, copy;
   Request r;
+  Request mine;                     // turns: the lane's, base + lane
+  int base, in;                     // units of the requests from base to the lane's, its own included
   __device__ __forceinline__ Walk(const Args& args, const Share& s, bool by_shares, int worker, int of)
-      : a(args), shares(by_shares), workers(of), b(by_shares ? s.b : 0), unit(by_shares ? s.unit : worker), left(by_shares ? s.left : 1),
-        step(by_shares ? s.step : 0) {
+      : a(args), shares(by_shares), step_there(2 * (of - 1 - worker) + 1), step_back(2 * worker + 1), b(by_shares ? s.b : -1), unit(by_shares ? s.unit : worker), left(by_shares ? s.left : 1),
+        step(by_shares ? s.step : 0), base(0) {
+    if (shares) {
+      if (left > 0) r = a.request(b);
+    } else {
+      fetch();
+    }
     find();
   }
   __device__ __forceinline__ bool more() const { return left > 0; }
   __device__ __forceinline__ bool whole() const { return count == all_steps; }
   __device__ __forceinline__ void next() {
-    if (shares) left -= count, ++unit; else unit += workers;
+    if (shares) {
+      left -= count, ++unit;
+    } else {
+      const int x = step_there;
+      unit += x, step_there = step_back, step_back = x;
+    }
     step = 0;
     find();
+  }
+  __device__ __forceinline__ void fetch() {
+    const int lane = threadIdx.x & 31;
+    in = 0;
+    if (base + lane < a.requests) mine = a.request(base + lane), in = mine.units();
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+      const int x = __shfl_up_sync(0xffffffffu, in, o);
+      if (lane >= o) in += x;
+    }
   }
   __device__ __forceinline__ void find() {
     if (left <= 0) return;
     if (shares) {
-      for (; b < a.requests; ++b, unit = 0) {
-        r = a.request(b);
-        if (unit < r.units()) return take();
+      while (unit >= r.units()) {
+        if (++b >= a.requests) {
+          left = 0;
+          return;
+        }
+        r = a.request(b), unit = 0;
       }
-      left = 0;
-      return;
+      return take(unit);
     }
-    const int lane = threadIdx.x & 31;
-    for (; b < a.requests; b += 32) {   // 32 requests at a time
-      int in = b + lane < a.requests ? a.request(b + lane).units() : 0;
-#pragma unroll
-      for (int o = 1; o < 32; o <<= 1) {
-        const int x = __shfl_up_sync(0xffffffffu, in, o);
-        if (lane >= o) in += x;
-      }
+    for (;;) {
       const uint32_t behind = __ballot_sync(0xffffffffu, in > unit);
       if (behind) {
         const int at = __ffs(behind) - 1;
         const int before = __shfl_sync(0xffffffffu, in, max(at - 1, 0));
-        if (at > 0) unit -= before;
-        b += at;
-        r = a.request(b);
-        return take();
+        b = base + at;
+        r.q0 = __shfl_sync(0xffffffffu, mine.q0, at), r.n = __shfl_sync(0xffffffffu, mine.n, at);
+        r.k0 = __shfl_sync(0xffffffffu, mine.k0, at), r.L = __shfl_sync(0xffffffffu, mine.L, at), r.hi = __shfl_sync(0xffffffffu, mine.hi, at);
+        r.s = a.shape();
+        r.settle();
+        return take(unit - (at > 0 ? before : 0));
       }
       unit -= __shfl_sync(0xffffffffu, in, 31);
+      base += 32;
+      if (base >= a.requests) break;
+      fetch();
     }
     left = 0;
   }
-  __device__ __forceinline__ void take() {
-    tile = unit / r.s.copies, copy = unit - tile * r.s.copies;
+  __device__ __forceinline__ void take(int of_request) {
+    tile = of_request / r.s.copies, copy = of_request - tile * r.s.copies;
     if (!shares) tile = r.tiles - 1 - tile;
     all_steps = r.steps(tile);
     count = shares ? static_cast<int>(min(static_cast<int64_t>(all_steps - step), left)) : all_steps;
   }
 };
+
+// Joins the parts of a unit that was cut: a thread has 16 values of one row, lanes along the rows.  A part is [values / 4][kRows]
+// x 4 sums, then [kRows] x (reference, sum of weights); part(i) is the i-th of `parts`, `first` the thread's first value, `to` where
+// its row has them (nullptr: there is no such row).  All of four parts is loaded at once: L2 latency bounds it.
+// kGroups > 1: so many threads of a block share a row's parts, in blocks of kGroups x kRows threads.  One request of 52000 tokens
+// in 148 parts: 49 us with one group, 36 with four; 64 requests in two or three parts each, where four times the blocks
+// come in waves: 141 and 155.
+// many_parts: whether a unit may be in more than 16, from bounds of the units and of the steps of one.
+inline bool many_parts(int64_t units, int workers, int64_t steps, int least) {
+  return units * 16 < workers && steps > 16 * least;
+}
+template <int kRows, int kValues, int kGroups, class Part>
+__device__ __forceinline__ void join_parts(const Part& part, int parts, int first, __half* to) {
+  __shared__ float s_join[kGroups > 1 ? kGroups - 1 : 1][18][kGroups > 1 ? kRows : 1];
+  const int row = threadIdx.x % kRows, group = kGroups > 1 ? threadIdx.x / kRows : 0;
+  float M = -INFINITY, L = 0.0f;
+  float v[16];
+#pragma unroll
+  for (int j = 0; j < 16; ++j) v[j] = 0.0f;
+  constexpr int kBatch = 4;
+  for (int i0 = group; to != nullptr && i0 < parts; i0 += kBatch * kGroups) {
+    float2 ml[kBatch];
+    float4 x[kBatch][4];
+#pragma unroll
+    for (int i = 0; i < kBatch; ++i) {
+      ml[i] = make_float2(-INFINITY, 0.0f);
+#pragma unroll
+      for (int j = 0; j < 4; ++j) x[i][j] = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+      if (i0 + i * kGroups >= parts) continue;
+      const float* p = part(i0 + i * kGroups);
+      ml[i] = __ldcg(reinterpret_cast<const float2*>(p + kRows * kValues) + row);
+#pragma unroll
+      for (int j = 0; j < 4; ++j) x[i][j] = __ldcg(reinterpret_cast<const float4*>(p) + (first / 4 + j) * kRows + row);
+    }
+    float top = M;
+#pragma unroll
+    for (int i = 0; i < kBatch; ++i) top = fmaxf(top, ml[i].x);
+    const float ref = top == -INFINITY ? 0.0f : top, f = exp2_approx(M - ref);
+    M = top;
+    L *= f;
+#pragma unroll
+    for (int j = 0; j < 16; ++j) v[j] *= f;
+#pragma unroll
+    for (int i = 0; i < kBatch; ++i) {
+      const float w = exp2_approx(ml[i].x - ref);   // 0 for a part that is not there, or whose row saw nothing
+      L = fmaf(ml[i].y, w, L);
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        v[4 * j] = fmaf(x[i][j].x, w, v[4 * j]), v[4 * j + 1] = fmaf(x[i][j].y, w, v[4 * j + 1]);
+        v[4 * j + 2] = fmaf(x[i][j].z, w, v[4 * j + 2]), v[4 * j + 3] = fmaf(x[i][j].w, w, v[4 * j + 3]);
+      }
+    }
+  }
+  if constexpr (kGroups > 1) {
+    if (group > 0 && group < parts) {
+      float (*mine)[kRows] = s_join[group - 1];
+      mine[0][row] = M, mine[1][row] = L;
+#pragma unroll
+      for (int j = 0; j < 16; ++j) mine[2 + j][row] = v[j];
+    }
+    __syncthreads();
+    if (group > 0) return;
+    for (int g = 1; g < min(parts, kGroups); ++g) {
+      const float (*other)[kRows] = s_join[g - 1];
+      const float m = other[0][row], top = fmaxf(M, m), ref = top == -INFINITY ? 0.0f : top;
+      const float f = exp2_approx(M - ref), w = exp2_approx(m - ref);
+      M = top, L = fmaf(other[1][row], w, L * f);
+#pragma unroll
+      for (int j = 0; j < 16; ++j) v[j] = fmaf(other[2 + j][row], w, v[j] * f);
+    }
+  }
+  if (to == nullptr) return;
+  const float inv = L > 0.0f ? 1.0f / L : 0.0f;
+  uint32_t h[8];
+#pragma unroll
+  for (int j = 0; j < 8; ++j) h[j] = pack_f16(v[2 * j] * inv, v[2 * j + 1] * inv);
+  store_32_bytes(to, h[0], h[1], h[2], h[3], h[4], h[5], h[6], h[7]);
+}
 
 }  // namespace pq
