@@ -579,7 +579,8 @@ PQ_API int pq_head_linear(const void* x_f16, int64_t x_stride, int64_t x_head_st
  * pq_paged_attention, the data taking the values' place.
  *   q: FP16 [tokens, heads, latent + PQ_LATENT_ROPE] dense;  out: FP16 [tokens, heads, latent] dense.  Rows outside every
  *     request are left as they are.  1 <= heads <= 1024, tokens * heads < 2^31; scale finite.
- *   block_table i32 [requests, width], q_start i32 [requests + 1], kv_len i32 [requests]: as for pq_paged_attention
+ *   block_table i32 [requests, width], q_start i32 [requests + 1], kv_len i32 [requests]: as for pq_paged_attention;
+ *     width * page <= 2^30 (else PQ_ERR_LIMIT)
  *   workspace: as for pq_gemm_w8a8; partial results of tokens that are split over several SMs, joined in a fixed order.
  *     The schedule is made on the GPU from the lengths.  Without a workspace, or with less than
  *     pq_latent_workspace_bytes, the tokens of a request are not split.

@@ -838,37 +838,48 @@ class LatentKV:
 def _head_rows(x: torch.Tensor, heads: int | None, dim: int | None, what: str) -> tuple[int, int, int, int, int]:
     """f16 [T, heads, dim], a head's values dense, rows and heads any distance apart.  Returns (T, heads, dim, row stride,
     head stride) in elements."""
-    if x.dtype != torch.float16:
+    if x.dtype is not torch.float16:
         raise TypeError(f"{what}: expected torch.float16, got {x.dtype}")
-    if x.dim() != 3 or (heads is not None and x.shape[1] != heads) or (dim is not None and x.shape[2] != dim) or x.stride(2) != 1:
+    shape, stride = x.shape, x.stride()
+    if len(shape) != 3 or (stride[2] != 1 and x.numel() > 0) or (heads is not None and shape[1] != heads) or (dim is not None and shape[2] != dim):
         raise ValueError(f"{what}: expected [rows, {'heads' if heads is None else heads}, {'values' if dim is None else dim}] "
                          "with the values of a head contiguous")
-    T, H, D = x.shape
-    hs = x.stride(1) if H > 1 else D
-    return T, H, D, (x.stride(0) if T > 1 else H * hs), hs
+    T, H, D = shape
+    hs = stride[1] if H > 1 else D
+    return T, H, D, (stride[0] if T > 1 else H * hs), hs
 
 
 def _strided_rows(x: torch.Tensor, width: int, what: str) -> tuple[int, int]:
-    """f16 [T, ...] with `width` values per row, dense inside a row.  Returns (T, row stride)."""
-    if x.dtype != torch.float16:
+    """f16 [T, width] or [T, heads, width / heads], dense inside a row.  Returns (T, row stride)."""
+    if x.dtype is not torch.float16:
         raise TypeError(f"{what}: expected torch.float16, got {x.dtype}")
-    if x.dim() < 2 or x[:1].numel() != (width if x.shape[0] else 0) or (x.shape[0] and not x[0].is_contiguous()):
+    shape, stride = x.shape, x.stride()
+    if len(shape) >= 2 and shape[0] == 0:   # whose strides say nothing
+        return 0, width
+    if len(shape) == 2:
+        dense = shape[1] == width and stride[1] == 1
+    elif len(shape) == 3:
+        dense = shape[1] * shape[2] == width and stride[2] == 1 and (shape[1] == 1 or stride[1] == shape[2])
+    else:
+        dense = False
+    if not dense:
         raise ValueError(f"{what}: expected rows of {width} contiguous values")
-    return x.shape[0], (x.stride(0) if x.shape[0] > 1 else width)
+    return shape[0], (stride[0] if shape[0] > 1 else width)
 
 
-def _on(device: int, **tensors) -> None:
-    for name, x in tensors.items():
+def _on(device: int, names: tuple, *tensors) -> None:
+    """The tensors whose elements have been measured otherwise lie on `device`, too."""
+    for name, x in zip(names, tensors):
         if x is not None and x.get_device() != device:
             raise ValueError(f"{name}: on {x.device}, other operands on cuda:{device}")
 
 
-def _outputs_for(q: torch.Tensor, out: torch.Tensor | None, heads: int, dim: int) -> tuple[torch.Tensor, int, int]:
+def _outputs_for(q: torch.Tensor, out: torch.Tensor | None, T: int, heads: int, dim: int) -> tuple[torch.Tensor, int, int]:
     if out is None:
-        out = torch.empty((q.shape[0], heads, dim), dtype=torch.float16, device=q.device)
-    T, _, _, os, ohs = _head_rows(out, heads, dim, "out")
-    if T != q.shape[0]:
-        raise ValueError(f"out: expected {q.shape[0]} rows, got {T}")
+        return torch.empty((T, heads, dim), dtype=torch.float16, device=q.device), heads * dim, dim
+    rows, _, _, os, ohs = _head_rows(out, heads, dim, "out")
+    if rows != T:
+        raise ValueError(f"out: expected {T} rows, got {rows}")
     return out, os, ohs
 
 
@@ -876,9 +887,9 @@ def pq_rotate(x: torch.Tensor, pos: torch.Tensor, rotary: Rotary, out: torch.Ten
     """Rows x f16 [T, heads, width] turned by their positions i32 [T] over the first rotary.dim values of each head -> out
     f16 of the same shape.  Rows and heads may be slices of wider tensors; out may be x itself (in place)."""
     T, H, D, xs, xhs = _head_rows(x, None, None, "x")
-    out, os, ohs = _outputs_for(x, out, H, D)
+    out, os, ohs = _outputs_for(x, out, T, H, D)
     _operands(rotary.device, (pos, torch.int32, T, "pos"))
-    _on(rotary.device, x=x, out=out)
+    _on(rotary.device, ("x", "out"), x, out)
     _check("pq_rotate", lib().pq_rotate(rotary._ref, x.data_ptr(), xs, xhs, H, D, pos.data_ptr(), T, out.data_ptr(), os, ohs, _stream()))
     return out
 
@@ -892,7 +903,7 @@ def _queries(q, out, T: int, dim: int):
     Tq, H, _, qs, qhs = _head_rows(q, None, dim, "q")
     if Tq != T:
         raise ValueError(f"q: expected {T} rows, got {Tq}")
-    out, os, ohs = _outputs_for(q, out, H, dim)
+    out, os, ohs = _outputs_for(q, out, T, H, dim)
     return out, (q.data_ptr(), qs, qhs, H, out.data_ptr(), os, ohs)
 
 
@@ -906,7 +917,7 @@ def pq_kv_append_rotated(cache: PagedKV, k: torch.Tensor, v: torch.Tensor, slots
         raise ValueError(f"v: expected {T} rows, got {Tv}")
     out, queries = _queries(q, out, T, cache.dim)
     _operands(cache.device, (slots, torch.int64, T, "slots"), (pos, torch.int32, T, "pos"), (rotary.freq, torch.int64, rotary.dim // 2, "rotary"))
-    _on(cache.device, k=k, v=v, q=q, out=out)
+    _on(cache.device, ("k", "v", "q", "out"), k, v, q, out)
     _check("pq_kv_append_rotated", lib().pq_kv_append_rotated(cache._ref, rotary._ref, k.data_ptr(), ks, v.data_ptr(), vs, slots.data_ptr(),
                                                               pos.data_ptr(), T, *queries, _stream()))
     return out
@@ -923,7 +934,7 @@ def pq_latent_append(cache: LatentKV, c: torch.Tensor, k_rope: torch.Tensor, slo
         raise ValueError(f"k_rope: expected {T} rows, got {Tk}")
     out, queries = _queries(q, out, T, LATENT_ROPE)
     _operands(cache.device, (slots, torch.int64, T, "slots"), (pos, torch.int32, T, "pos"), (rotary.freq, torch.int64, rotary.dim // 2, "rotary"))
-    _on(cache.device, c=c, k_rope=k_rope, q=q, out=out)
+    _on(cache.device, ("c", "k_rope", "q", "out"), c, k_rope, q, out)
     _check("pq_latent_append", lib().pq_latent_append(cache._ref, rotary._ref, c.data_ptr(), cs, k_rope.data_ptr(), ks, slots.data_ptr(),
                                                       pos.data_ptr(), T, *queries, _stream()))
     return out
@@ -943,15 +954,13 @@ def pq_head_linear(x: torch.Tensor, w: torch.Tensor, out: torch.Tensor | None = 
     """One matrix per head: x f16 [T, heads, K], w f16 [heads, N, K] -> out f16 [T, heads, N], out[t, h] = w[h] x[t, h].  Rows and
     heads of x and out may be slices of wider tensors."""
     T, H, K, xs, xhs = _head_rows(x, None, None, "x")
-    if w.dim() != 3:
-        raise ValueError("w: expected a 3-D tensor [heads, N, K]")
-    N = w.shape[1]
-    _sized(w, torch.float16, H * N * K, "w")
-    if w.shape != (H, N, K):
-        raise ValueError(f"w: expected [{H}, N, {K}], got {tuple(w.shape)}")
-    out, os, ohs = _outputs_for(x, out, H, N)
-    _operands(w.get_device())
-    _on(w.get_device(), x=x, out=out)
+    shape = w.shape
+    if len(shape) != 3 or shape[0] != H or shape[2] != K:
+        raise ValueError(f"w: expected [{H}, N, {K}], got {tuple(shape)}")
+    N, device = shape[1], w.get_device()
+    out, os, ohs = _outputs_for(x, out, T, H, N)
+    _operands(device, (w, torch.float16, H * N * K, "w"))
+    _on(device, ("x", "out"), x, out)
     _check("pq_head_linear", lib().pq_head_linear(x.data_ptr(), xs, xhs, w.data_ptr(), H, N, K, T, out.data_ptr(), os, ohs, _stream()))
     return out
 
@@ -1016,7 +1025,7 @@ def pq_expanded_attention(q: torch.Tensor, kv: torch.Tensor, k_rope: torch.Tenso
         checks += ((out, torch.float16, T * H * VALUE, "out"),)
     ws, ws_bytes, more = _workspace_check(workspace)
     _operands(q.get_device(), *checks, *more)
-    _on(q.get_device(), kv=kv, k_rope=k_rope)
+    _on(q.get_device(), ("kv", "k_rope"), kv, k_rope)
     if out is None:
         out = torch.empty((T, H, VALUE), dtype=torch.float16, device=q.device)
     _check("pq_expanded_attention", lib().pq_expanded_attention(q.data_ptr(), qs, H, kv.data_ptr(), kvs, k_rope.data_ptr(), krs, S,

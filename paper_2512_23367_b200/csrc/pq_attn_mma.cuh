@@ -134,12 +134,6 @@ __device__ __forceinline__ float max3(float a, float b, float c) {
 __device__ __forceinline__ bool warp_wait(uint32_t bar, uint32_t parity, const WaitCtx& wc) {
   return __all_sync(0xffffffffu, mbar_wait(bar, parity, wc));
 }
-// Whether a phase has completed, asked by one lane for the warp.
-__device__ __forceinline__ bool warp_test(uint32_t bar, uint32_t parity) {
-  uint32_t done = 0;
-  if ((threadIdx.x & 31) == 0) done = mbar_test(bar, parity);
-  return __shfl_sync(0xffffffffu, done, 0) != 0;
-}
 __device__ __forceinline__ int warp_prefix(int v, int lane) {   // inclusive sums
 #pragma unroll
   for (int o = 1; o < 32; o <<= 1) {

@@ -537,7 +537,7 @@ int pq_expanded_attention(const void* q_f16, int64_t q_stride, int32_t heads, co
   const int64_t by_rows = tokens / kUnit + requests, by_request = requests * ((max_q + kUnit - 1) / kUnit);
   const int64_t units = (by_rows < by_request ? by_rows : by_request) * heads;
   const Scratch sc = scratch_from(workspace, workspace_bytes);
-  if (sc.partials != nullptr && sc.partial_bytes >= expanded_partial_bytes(sms) && units < 3 * sms) {
+  if (sc.partials != nullptr && sc.partial_bytes >= expanded_partial_bytes(sms) && units < 3 * sms && keys > kFewSteps * kKeys) {
     a.shares = 1;
     a.partials = reinterpret_cast<float*>(sc.partials);
     a.joins = reinterpret_cast<int4*>(a.partials + static_cast<size_t>(sms) * 2 * kPartFloats);

@@ -178,25 +178,6 @@ inline int cuda_status(cudaError_t e) {
 
 // Launches a kernel with programmatic stream serialization (unless PQ_PDL=0): it may begin while the kernel
 // before it in the stream drains, and calls grid_dep_wait() before it touches what that kernel may touch.
-// launch_dependent_pairs: the same on clusters of two CTAs.
-template <typename... Params, typename... Args>
-int launch_dependent_pairs(void (*kern)(Params...), dim3 grid, dim3 block, size_t smem, cudaStream_t stream, Args... args) {
-  cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = grid;
-  cfg.blockDim = block;
-  cfg.dynamicSmemBytes = smem;
-  cfg.stream = stream;
-  cudaLaunchAttribute attr[2];
-  attr[0].id = cudaLaunchAttributeClusterDimension;
-  attr[0].val.clusterDim.x = 2;
-  attr[0].val.clusterDim.y = 1;
-  attr[0].val.clusterDim.z = 1;
-  attr[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-  attr[1].val.programmaticStreamSerializationAllowed = 1;
-  cfg.attrs = attr;
-  cfg.numAttrs = pdl_enabled() ? 2 : 1;
-  return cuda_status(cudaLaunchKernelEx(&cfg, kern, args...));
-}
 template <typename... Params, typename... Args>
 int launch_dependent(void (*kern)(Params...), dim3 grid, dim3 block, size_t smem, cudaStream_t stream, Args... args) {
   cudaLaunchConfig_t cfg = {};

@@ -121,15 +121,22 @@ __device__ __forceinline__ float row_combine(float* mine, const float* row, uint
 // keeps busy: with mbarriers, polled for in whichever order they came, a step took 3200 cycles.
 constexpr uint32_t kBarRow = 1, kBarTile = 3, kBarRead = 4, kBarP = 5;
 
-// A CTA serves 64 rows over its share of the steps.  All heads share the cache, so a row is any (token, head) and a step's
-// 64 tokens are read once for 64 rows: HBM bound up to 64 rows a request; 128 rows, which two CTAs share,
-// are where the tensor cores take about as long.  Per step, with the tokens as panels of 64 values:
-//   S = Q C^T            36 (latent 512) MMAs with N = 64 from shared memory, into one of two 32-column buffers
-//   softmax              two threads per row: S to registers, running maximum, P = 2^(S - reference + 7) as FP16 into the
-//                        panel of the rotary keys, which only this S needed: P is exactly as large
-//   O += P C             8 MMAs with N = 256, C as it lies (values contiguous), O of 64 rows in 256 columns
-// in the order S(u + 1), O(u), so that a softmax runs under the next S.  The reference moves, and O is multiplied, only when
-// the maximum has grown by more than 2^8.
+// A CTA serves 64 rows over its share of the steps.  All heads share the cache, so a row is any (token, head) and a step's 64
+// tokens are read once for 64 rows; units of 128 rows are served by two CTAs, the second of which finds the tokens in L2.
+// Per step, latent 512:
+//   S = Q C^T            28 MMAs with A in tensor memory (28 cycles each: without it shared memory, which has to give A and B,
+//                        takes 32) and 8 from shared memory; the latent vectors first, then the rotary keys, which have room
+//                        for one step and are brought in while the vectors are multiplied
+//   softmax              four threads per row: S to registers, running maximum, P = 2^(S - reference + 7) as FP16 to shared memory
+//   O += P C             8 MMAs with N = 256 (80 cycles each), C as it lies (values contiguous), O of 64 rows in 256 columns
+// in the order S(u + 1), O(u), so that a softmax runs under the next S: 1680 cycles of MMAs.  The reference moves, and O is
+// multiplied, only when the maximum has grown by more than 2^8.
+//
+// Bound by HBM up to 64 rows a request: 72 KB a step take an SM's share of the bandwidth 3150 cycles, and steps come every
+// 3300.  Two CTAs that share their tokens have 1580 cycles of bandwidth a step and take 2080: the tensor cores wait for S to be
+// read and for P.  (64 requests of 16 heads and 1000 to 8000 tokens: 131 us, where their bytes take 63; 16 requests of 3 tokens
+// each: 64, where 26.)  Taken back for being slower: queries in shared memory and two steps of tokens (236 us for the 131), two
+// CTAs as a cluster that exchange halves of S (5300 cycles a step), MMAs over a pair of CTAs (2340).
 template <int kLatent>
 __global__ void __launch_bounds__(kThreads, 1)
 latent_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUtensorMap map_c, const __grid_constant__ CUtensorMap map_r, const LatentArgs a) {
@@ -614,7 +621,7 @@ int pq_latent_attention(const void* q_f16, int32_t heads, const pq_latent_cache*
   if (rc != PQ_OK) return rc;
   if (heads < 1 || heads > 1024 || requests < 0 || requests > 0x7fffffff || tokens < 0 || tokens > 0x7fffffff / heads) return PQ_ERR_SHAPE;
   if (width < 1 || width > 0x7fffffff || !std::isfinite(scale)) return PQ_ERR_SHAPE;
-  if (requests > PQ_MAX_REQUESTS) return PQ_ERR_LIMIT;
+  if (requests > PQ_MAX_REQUESTS || width > kMostKeys / cache->page) return PQ_ERR_LIMIT;
   if (requests == 0 || tokens == 0) return PQ_OK;
   if (!q_f16 || !block_table || !q_start || !kv_len || !out_f16) return PQ_ERR_NULL;
   if (!aligned16(q_f16) || !aligned16(out_f16) || !aligned256(workspace)) return PQ_ERR_ALIGN;
@@ -631,7 +638,8 @@ int pq_latent_attention(const void* q_f16, int32_t heads, const pq_latent_cache*
   a.paired = static_cast<int64_t>(tokens) * heads > kRows * requests;   // more than 64 rows a request, on average
   const int sms = sm_count();
   const Scratch sc = scratch_from(workspace, workspace_bytes);
-  if (sc.partials != nullptr && sc.partial_bytes >= partial_bytes(cache->latent, sms)) {
+  // (Where the table holds so few tokens, whole units are done sooner than the parts' joining.)
+  if (width * cache->page > kFewSteps * kKeys && sc.partials != nullptr && sc.partial_bytes >= partial_bytes(cache->latent, sms)) {
     a.partials = reinterpret_cast<float*>(sc.partials);
     a.joins = reinterpret_cast<int4*>(a.partials + static_cast<size_t>(sms) * 2 * kRows * (cache->latent + 2));
   }

@@ -175,19 +175,6 @@ __device__ __forceinline__ uint32_t mbar_test2(uint32_t bar_a, uint32_t par_a, u
   return ok;   // not consumed here: the caller can let the round trip overlap with other work
 }
 
-// The same for one barrier.
-__device__ __forceinline__ uint32_t mbar_test(uint32_t bar, uint32_t parity) {
-  uint32_t ok;
-  asm volatile(
-      "{\n\t.reg .pred P;\n\t"
-      "mbarrier.test_wait.parity.shared::cta.b64 P, [%1], %2;\n\t"
-      "selp.u32 %0, 1, 0, P;\n\t}"
-      : "=r"(ok)
-      : "r"(bar), "r"(parity)
-      : "memory");
-  return ok;
-}
-
 // Give-up path only: a short bounded wait for a copy or an MMA that is already in flight (it needs
 // nothing from anybody and ends by itself within microseconds).  Does not touch the abort flag.
 constexpr uint32_t kDrainPollLimit = 1u << 16;

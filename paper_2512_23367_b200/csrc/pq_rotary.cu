@@ -25,12 +25,23 @@ constexpr int kItem = 16;   // values of one work item: two 16-byte chunks, 8 pa
 
 enum Target { kRotate, kKvF16, kKvInt8, kLatent };
 
+// n / d for n below 2^20 and d up to 2^20: n * ceil(2^40 / d) exceeds n / d * 2^40 by less than n <= 2^20, less than the 2^40 / d that
+// the next whole number is away.
+struct Divisor {
+  uint32_t d;
+  uint64_t mul;
+  Divisor() = default;
+  explicit Divisor(int by) : d(by), mul(((uint64_t(1) << 40) + by - 1) / by) {}
+  __device__ __forceinline__ int divide(int n) const { return static_cast<int>(static_cast<uint64_t>(n) * mul >> 40); }
+};
+
 // Rows of one operand: head h of token t at p + t * stride + h * head_stride.
 struct Rows {
   const __half* p;
   int64_t stride, head_stride;
   int heads;
   int items;   // of a head: its values / 16
+  Divisor by_items;
 };
 
 struct TurnArgs {
@@ -39,6 +50,7 @@ struct TurnArgs {
   const int64_t* slots;
   int64_t tokens;
   int per_token;    // items of a token: queries', keys', values'
+  Divisor by_token;
   int turned;       // of a head: its first dim / 16 items are turned (0: none)
   Rows q, k, v;     // kLatent: k the rotary key, v the latent vector
   __half* out;      // of the queries
@@ -92,7 +104,7 @@ __global__ void __launch_bounds__(kThreads) rotary_kernel(const TurnArgs a) {
 #pragma unroll
   for (int u = 0; u < kItems; ++u) {
     const int flat = lead + tid + u * kThreads;
-    tok[u] = flat / a.per_token;
+    tok[u] = a.by_token.divide(flat);
     int rest = flat - tok[u] * a.per_token;
     part[u] = tok[u] >= toks ? -1 : 0;
     Rows r = a.q;
@@ -104,7 +116,7 @@ __global__ void __launch_bounds__(kThreads) rotary_kernel(const TurnArgs a) {
         r = a.v, part[u] = tok[u] >= toks ? -1 : 2;
       }
     }
-    head[u] = rest / r.items, item[u] = rest - head[u] * r.items;
+    head[u] = r.by_items.divide(rest), item[u] = rest - head[u] * r.items;
     lo[u] = hi[u] = make_uint4(0, 0, 0, 0);
     if (part[u] >= 0) {
       const uint4* p = reinterpret_cast<const uint4*>(r.p + (tok0 + tok[u]) * r.stride + head[u] * r.head_stride);
@@ -189,7 +201,8 @@ __global__ void __launch_bounds__(kThreads) rotary_kernel(const TurnArgs a) {
 // Two items per thread where the grid still fills the machine several times over.
 constexpr int kManyItems = 2;
 template <Target kTarget, bool kHalf>
-int launch_items(const TurnArgs& a, cudaStream_t stream) {
+int launch_items(TurnArgs a, cudaStream_t stream) {
+  a.by_token = Divisor(a.per_token);
   const int64_t items = a.tokens * a.per_token;
   const bool many = items >= static_cast<int64_t>(kThreads) * kManyItems * 8 * sm_count();
   const int64_t block = kThreads * (many ? kManyItems : 1), grid = (items + block - 1) / block;
@@ -215,9 +228,8 @@ int check_rotary(const pq_rotary* r, int width) {
 }
 // Rows of heads that can be read and written in 16-byte chunks.
 bool strides_ok(int64_t stride, int64_t head_stride, int heads, int width) {
-  if (head_stride % 8 != 0 || stride % 8 != 0 || stride < 0 || head_stride < 0) return false;
-  if (heads > 1 && head_stride < width) return false;
-  return true;
+  if (stride % 8 != 0 || stride < 0) return false;
+  return heads == 1 || (head_stride % 8 == 0 && head_stride >= width);
 }
 
 struct QueryRows {   // the optional queries of an append
@@ -229,7 +241,7 @@ struct QueryRows {   // the optional queries of an append
 };
 int set_queries(TurnArgs& a, const QueryRows& q, int width) {
   if (q.heads < 0 || q.heads > 1024) return PQ_ERR_SHAPE;
-  a.q = Rows{static_cast<const __half*>(q.q), q.stride, q.head_stride, q.heads, width / kItem};
+  a.q = Rows{static_cast<const __half*>(q.q), q.stride, q.head_stride, q.heads, width / kItem, Divisor(width / kItem)};
   a.out = static_cast<__half*>(q.out), a.out_stride = q.out_stride, a.out_head_stride = q.out_head_stride;
   if (q.heads == 0) return PQ_OK;
   if (!strides_ok(q.stride, q.head_stride, q.heads, width) || !strides_ok(q.out_stride, q.out_head_stride, q.heads, width)) return PQ_ERR_SHAPE;
@@ -328,8 +340,8 @@ int pq_kv_append_rotated(const pq_kv_cache* cache, const pq_rotary* rotary, cons
   if (!aligned16(k_f16) || !aligned16(v_f16)) return PQ_ERR_ALIGN;
   if ((rc = check_arch()) != PQ_OK) return rc;
   const int items = cache->dim / kItem;
-  a.k = Rows{static_cast<const __half*>(k_f16), k_stride, cache->dim, cache->heads, items};
-  a.v = Rows{static_cast<const __half*>(v_f16), v_stride, cache->dim, cache->heads, items};
+  a.k = Rows{static_cast<const __half*>(k_f16), k_stride, cache->dim, cache->heads, items, Divisor(items)};
+  a.v = Rows{static_cast<const __half*>(v_f16), v_stride, cache->dim, cache->heads, items, Divisor(items)};
   a.per_token = (q_heads + 2 * cache->heads) * items;
   return cache->type == PQ_KV_INT8 ? launch_turn<kKvInt8>(a, static_cast<cudaStream_t>(stream))
                                    : launch_turn<kKvF16>(a, static_cast<cudaStream_t>(stream));
@@ -349,8 +361,8 @@ int pq_latent_append(const pq_latent_cache* cache, const pq_rotary* rotary, cons
   if (!c_f16 || !k_rope_f16 || !slots || !pos) return PQ_ERR_NULL;
   if (!aligned16(c_f16) || !aligned16(k_rope_f16)) return PQ_ERR_ALIGN;
   if ((rc = check_arch()) != PQ_OK) return rc;
-  a.k = Rows{static_cast<const __half*>(k_rope_f16), k_rope_stride, PQ_LATENT_ROPE, 1, PQ_LATENT_ROPE / kItem};
-  a.v = Rows{static_cast<const __half*>(c_f16), c_stride, cache->latent, 1, cache->latent / kItem};
+  a.k = Rows{static_cast<const __half*>(k_rope_f16), k_rope_stride, PQ_LATENT_ROPE, 1, PQ_LATENT_ROPE / kItem, Divisor(PQ_LATENT_ROPE / kItem)};
+  a.v = Rows{static_cast<const __half*>(c_f16), c_stride, cache->latent, 1, cache->latent / kItem, Divisor(cache->latent / kItem)};
   a.per_token = q_heads * a.q.items + a.k.items + a.v.items;
   return launch_turn<kLatent>(a, static_cast<cudaStream_t>(stream));
 }

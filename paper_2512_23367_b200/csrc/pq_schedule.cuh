@@ -32,6 +32,8 @@ __device__ inline uint64_t floor_sum(uint64_t n, uint64_t m, uint64_t a, uint64_
   return sum;
 }
 
+constexpr int kFewSteps = 6;   // of a unit at most: shares are not worth their joining
+
 struct UnitShape {
   int rows;      // query rows of a tile
   int heads;     // rows per token: row r of a request is of token r / heads

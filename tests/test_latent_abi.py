@@ -237,3 +237,29 @@ def test_the_two_plain_forms_of_latent_attention_are_one():
     e = dict(q=q.reshape(n, -1), kv=np.einsum("lc,hkc->lhk", c, up).reshape(L, -1), k_rope=rope, heads=heads, q_start=np.array([0, n]),
              kv_start=np.array([0, L]))
     assert np.allclose(ref.expanded_attention(e, 0.07)[0], absorbed, atol=1e-12)
+
+
+def test_one_heads_strides_are_not_looked_at():
+    assert pq.lib().pq_rotate(_rotary(), 16, 128, 3, 1, 128, None, 0, 16, 128, -5, None) == 0
+    assert pq.lib().pq_rotate(_rotary(), 16, 128, 3, 2, 128, None, 0, 16, 128, 128, None) == SHAPE
+    assert pq.lib().pq_head_linear(16, 128, 3, 16, 1, 512, 128, 0, 16, 512, -5, None) == 0
+
+
+def test_a_tables_width_is_bounded_by_its_tokens():
+    """Steps round up to whole tokens of 64 in 32 bits."""
+    def call(width, page):
+        return pq.lib().pq_latent_attention(16, 4, _latent(page=page), None, width, None, None, 0, 3, 0.1, None, None, 0, None)
+
+    assert call(1 << 26, 16) == 0 and call((1 << 26) + 1, 16) == LIMIT
+    assert call(1 << 20, 1024) == 0 and call((1 << 20) + 1, 1024) == LIMIT and call(0x7fffffff, 16) == LIMIT
+
+
+def test_empty_operands_have_rows_of_any_stride():
+    """An empty tensor's strides say nothing about its rows."""
+    f16 = lambda *s: torch.zeros(s, dtype=torch.float16)  # noqa: E731
+    assert binding._strided_rows(f16(64, 0).t(), 64, "x") == (0, 64)
+    assert binding._head_rows(f16(128, 2, 0).permute(2, 1, 0), 2, 128, "x")[:3] == (0, 2, 128)
+    with pytest.raises(ValueError, match="x: expected"):
+        binding._strided_rows(f16(64, 3).t(), 64, "x")
+    with pytest.raises(ValueError, match="x: expected"):
+        binding._head_rows(f16(128, 2, 3).permute(2, 1, 0), 2, 128, "x")
