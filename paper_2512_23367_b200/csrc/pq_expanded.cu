@@ -34,7 +34,15 @@ static_assert(kColP + kKeys <= kColO, "tensor memory");
 // (eight pairs), "S read" (two), accumulators' sums.
 constexpr uint32_t kBarP = 1, kBarTile = 3, kBarPair = 4, kBarRead = 12, kBarSoft = 14;
 
+// Halves take a key tile by the accumulators in turn, which costs five eighths of a step of both query tiles (1430 of 2330 cycles:
+// keys and values come from L2 for half as many products), and a unit about as much as three steps.
+struct ExpandedShape {
+  static constexpr int rows = kUnit, heads = 1, keys = kKeys, half_keys = kKeys, halves = 1, cost = 8, half_cost = 5, unit_cost = 20;
+  int copies;
+  __device__ __forceinline__ static uint64_t floors(uint64_t n, uint64_t b) { return floor_sum_of<kKeys, kUnit>(n, b); }
+};
 struct ExpandedArgs {
+  using Shape = ExpandedShape;
   const int* q_start;
   const int* kv_start;
   __half* out;
@@ -48,25 +56,29 @@ struct ExpandedArgs {
   int* status;
   uint32_t wait_limit;
 
-  __device__ __forceinline__ UnitShape shape() const { return UnitShape{kUnit, 1, kKeys, heads}; }
-  __device__ __forceinline__ Request request(int b) const {
-    Request r;
+  __device__ __forceinline__ Shape shape() const { return Shape{heads}; }
+  __device__ __forceinline__ Request<Shape> request(int b, bool halves) const {
+    Request<Shape> r;
     r.s = shape();
     r.q0 = q_start[b];
     r.n = static_cast<int>(min(static_cast<int64_t>(max(q_start[b + 1] - r.q0, 0)), tokens));
     r.k0 = kv_start[b];
     r.L = r.hi = max(kv_start[b + 1] - r.k0, 0);
-    r.settle();
+    r.settle(halves);
     return r;
   }
 };
 
-// The steps of a unit, or of the part of one that a CTA has.
+// A CTA's units.
+struct ExpandedWalk : Walk<ExpandedArgs> {
+  __device__ __forceinline__ ExpandedWalk(const ExpandedArgs& args, const Share& s, bool by_shares) : Walk<ExpandedArgs>(args, s, by_shares, true, blockIdx.x, gridDim.x) {}
+};
+// The key tiles of a unit, or of the part of one that a CTA has.
 struct Part {
   int toks, N, lag;      // tokens; (S, O) steps; steps that an O follows its S by
   bool two;              // more than one accumulator's rows: the accumulators are two query tiles, else the even and the odd key tiles
-  __device__ __forceinline__ explicit Part(const Walk<ExpandedArgs>& w)
-      : toks(min(kUnit, w.r.n - w.tile * kUnit)), two(toks > kTile) {
+  __device__ __forceinline__ explicit Part(const ExpandedWalk& w)
+      : toks(min(kUnit, w.r.n - w.tile * kUnit)), two(!w.half()) {
     N = two ? 2 * w.count : w.count;
     lag = two ? 2 : 1;
   }
@@ -89,27 +101,25 @@ expanded_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant
                 const ExpandedArgs a) {
   constexpr float kTop = 7.0f;      // a weight at the reference is 2^kTop
   extern __shared__ uint8_t smem_raw[];
-  __shared__ __align__(8) uint64_t bars[17];
+  __shared__ __align__(8) uint64_t bars[16];
   __shared__ uint32_t s_tmem;
   __shared__ volatile int s_abort;
-  __shared__ Share s_share;
-  __shared__ int64_t s_sums[kThreads / 32];
+  __shared__ ShareRoom s_share;
   __shared__ float s_swap[2 * kTile];
   __shared__ float2 s_ml[kTile];
 
   const int tid = threadIdx.x, warp = __shfl_sync(0xffffffffu, tid >> 5, 0), lane = tid & 31;
   const uint32_t bar_k = smem_u32(bars), bar_v = bar_k + 16, bar_kfree = bar_v + 16, bar_vfree = bar_kfree + 16;   // two of each
   const uint32_t bar_s = bar_vfree + 16, bar_o = bar_s + 16;                                                       // per accumulator
-  const uint32_t bar_q = bar_o + 16, bar_qfree = bar_q + 8, bar_read = bar_qfree + 8, bar_fix = bar_read + 8, bar_drain = bar_fix + 8;
+  const uint32_t bar_q = bar_o + 16, bar_qfree = bar_q + 8, bar_read = bar_qfree + 8, bar_drain = bar_read + 8;
   if (tid == 0) {
     for (int i = 0; i < 12; ++i) mbar_init(bar_k + 8 * i, 1);
     mbar_init(bar_q, 1);
     mbar_init(bar_qfree, 1);
     mbar_init(bar_read, 1);
-    mbar_init(bar_fix, 1);
     mbar_init(bar_drain, 1);
     fence_mbar_init();
-    s_abort = 0;
+    s_abort = 0, s_share.clear();
     tma_prefetch_desc(&map_q), tma_prefetch_desc(&map_kv), tma_prefetch_desc(&map_rope);
   }
   if (warp == kIssuer) {
@@ -117,22 +127,22 @@ expanded_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant
     tmem_relinquish();
   }
   tc_fence_before_sync();
-  grid_dep_wait();
-  const bool shares = a.shares != 0;
-  if (shares) find_share<kThreads>(a, blockIdx.x, gridDim.x, kLeastSteps, &s_share, s_sums); else __syncthreads();
+  __syncthreads();
   tc_fence_after_sync();
+  grid_dep_wait();
+  const bool shares = a.shares != 0 && find_share<kThreads, kHalvesAlways>(a, blockIdx.x, gridDim.x, kLeastSteps * ExpandedShape::cost, s_share);
   grid_dep_launch();   // only now: a later launch's CTA may take this SM's tensor memory when it is given back
   const uint32_t tmem = __shfl_sync(0xffffffffu, s_tmem, 0);
   const uint32_t sq = (smem_u32(smem_raw) + 1023u) & ~1023u, ring_k = sq + 2 * kQueryBytes, ring_v = ring_k + 2 * kKeyBytes;
   const WaitCtx wc{&s_abort, a.wait_limit};
-  uint32_t issued = 0, fixes = 0, units = 0;   // producers: tiles requested, of them by way of bar_fix; units
+  uint32_t issued = 0, units = 0;   // producers: tiles requested; units
 
   if (warp >= kSoft / 32) {
     asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kRestRegs));
     if (warp == kLoadK) {
       // ------------------------------------------------------------------ queries and keys
       bool ok = true;
-      for (Walk<ExpandedArgs> w(a, s_share, shares, blockIdx.x, gridDim.x); ok && w.more(); w.next()) {
+      for (ExpandedWalk w(a, s_share.share, shares); ok && w.more(); w.next()) {
         const Part part(w);
         if (units > 0 && !(ok = warp_wait(bar_qfree, (units - 1) & 1, wc))) break;
         if (lane == 0) mbar_arrive_expect_tx(bar_q, part.two ? 2 * kQueryBytes : kQueryBytes);
@@ -157,28 +167,16 @@ expanded_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant
     } else if (warp == kLoadV) {
       // ------------------------------------------------------------------ values
       bool ok = true;
-      for (Walk<ExpandedArgs> w(a, s_share, shares, blockIdx.x, gridDim.x); ok && w.more(); w.next()) {
+      for (ExpandedWalk w(a, s_share.share, shares); ok && w.more(); w.next()) {
+        const Part part(w);
         for (int i = 0; i < w.count; ++i) {
           const uint32_t st = issued & 1, dst = ring_v + st * kValueBytes;
           if (issued >= 2 && !(ok = warp_wait(bar_vfree + 8 * st, ((issued >> 1) & 1) ^ 1, wc))) break;
-          const int key0 = (w.step + i) * kKeys;
-          const int dead = min(max(w.r.hi - key0, 0), kKeys);   // from here on rows are not the request's
-          const uint32_t bar = dead < kKeys ? bar_fix : bar_v + 8 * st;
+          const uint32_t bar = bar_v + 8 * st;
           if (lane == 0) mbar_arrive_expect_tx(bar, kValueBytes);
           __syncwarp();
-          if (lane < 2) tma_load_3d(dst + lane * kPanelK, &map_kv, bar, kNope + lane * 64, w.copy, w.r.k0 + key0);
+          if (lane < 2) tma_load_3d(dst + lane * kPanelK, &map_kv, bar, kNope + lane * 64, w.copy, w.r.k0 + (w.step + i) * kKeys);
           ++issued;
-          if (dead < kKeys) {   // their weights are 0, but 0 x NaN is not
-            if (!(ok = warp_wait(bar_fix, fixes & 1, wc))) break;
-            ++fixes;
-            for (int j = lane; j < (kKeys - dead) * 16; j += 32) {
-              const int r = dead + (j >> 4), c = j & 15;
-              asm volatile("st.shared.v4.u32 [%0], {%1, %1, %1, %1};" ::"r"(dst + (c >> 3) * kPanelK + r * 128 + (c & 7) * 16), "r"(0) : "memory");
-            }
-            fence_proxy_async_smem();
-            __syncwarp();
-            if (lane == 0) mbar_arrive(bar_v + 8 * st);
-          }
           __syncwarp();
         }
       }
@@ -230,13 +228,13 @@ expanded_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant
       };
       constexpr std::integral_constant<int, 0> k0{};
       constexpr std::integral_constant<int, 1> k1{};
-      for (Walk<ExpandedArgs> w(a, s_share, shares, blockIdx.x, gridDim.x); w.more(); w.next()) {
-        const bool two = Part(w).two;
+      for (ExpandedWalk w(a, s_share.share, shares); w.more(); w.next()) {
+        const Part part(w);
         live = live && warp_wait(bar_q, seg & 1, wc);
         auto sums_free = [&](int t) {   // the sums of the unit before have been read
           if (t == 1 && seg > 0) live = warp_wait(bar_read, (seg - 1) & 1, wc) && live;
         };
-        if (two) {   // S of both query tiles, then O of both of the key tile before
+        if (part.two) {   // S of both query tiles, then O of both of the key tile before
           for (int t = 0; t <= w.count; ++t) {
             const bool more = t < w.count;
             if (t > 0) read(k0);
@@ -264,7 +262,7 @@ expanded_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant
       // ------------------------------------------------------------------ watcher: waits for the operand tiles a step ahead
       bool ok = true;
       uint32_t g = 0;
-      for (Walk<ExpandedArgs> w(a, s_share, shares, blockIdx.x, gridDim.x); w.more(); w.next()) {
+      for (ExpandedWalk w(a, s_share.share, shares); w.more(); w.next()) {
         const Part part(w);
         for (int u = 0; u < part.N + part.lag; ++u) {
 #pragma unroll
@@ -273,6 +271,15 @@ expanded_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant
             if (x < 0 || x >= part.N || (part.two && (x & 1))) continue;
             const uint32_t t = g + (part.two ? x >> 1 : x);
             ok = ok && warp_wait((is_v ? bar_v : bar_k) + 8 * (t & 1), (t >> 1) & 1, wc);
+            const int dead = w.r.hi - (w.step + (part.two ? x >> 1 : x)) * kKeys;   // from here on rows are not the request's
+            if (is_v && ok && dead < kKeys) {   // their weights are 0, but 0 x NaN is not
+              for (int j = lane; j < (kKeys - max(dead, 0)) * 16; j += 32) {
+                const int r = max(dead, 0) + (j >> 4), c = j & 15;
+                asm volatile("st.shared.v4.u32 [%0], {%1, %1, %1, %1};" ::"r"(ring_v + (t & 1) * kValueBytes + (c >> 3) * kPanelK + r * 128 + (c & 7) * 16), "r"(0) : "memory");
+              }
+              fence_proxy_async_smem();
+              __syncwarp();
+            }
             tile_landed(kBarTile, ok);
           }
         }
@@ -295,7 +302,7 @@ expanded_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant
     uint32_t n = 0;                                  // the accumulator's steps so far
     int4 join = make_int4(0, 0, 0, 0);
     bool ok = true;
-    for (Walk<ExpandedArgs> w(a, s_share, shares, blockIdx.x, gridDim.x); w.more(); w.next()) {
+    for (ExpandedWalk w(a, s_share.share, shares); w.more();) {
       const Part part(w);
       const bool two = part.two;
       const int tok = (two ? acc * kTile : 0) + r;   // of the unit
@@ -391,12 +398,17 @@ expanded_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant
         hand_over(kBarP + acc, 288, ok);
       }
       // ------------------------------------------------------------------ the unit's (or part's) end
+      const bool both = !two && w.count > 1, writer = two || acc == 0, whole = w.whole(), begins = w.step == 0;
+      const int64_t row = static_cast<int64_t>(w.r.q0) + w.tile * kUnit + tok;
+      const bool writes = tok < part.toks && row >= 0 && row < a.tokens;
+      __half* to = a.out + (row * a.heads + w.copy) * kValue + half * (kValue / 2);
+      if (!whole && begins) join = make_int4(w.r.q0 + w.tile * kUnit, part.toks, w.copy, w.parts(s_share.share.per));
+      w.next();   // (the next request's lengths are on the way while the last product is waited for)
       if (mine > 0) ok = ok && warp_wait(bar_o + 8 * acc, (n - 1) & 1, wc);
       tc_fence_after_sync();
       l = pair_combine<true>(swap, pair, half, l);   // the sum of the row's two threads
       // Accumulators of the even and the odd tiles are joined in the first one's threads: both lie in the same lanes.
       float f0 = 1.0f, f1 = 0.0f;
-      const bool both = !two && w.count > 1;
       if (both) {
         if (acc == 1 && half == 0) s_ml[r] = make_float2(m, l);
         tc_fence_before_sync();
@@ -410,11 +422,8 @@ expanded_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant
           m = M;
         }
       }
-      if (two || acc == 0) {
+      if (writer) {
         const float inv = l > 0.0f ? 1.0f / l : 0.0f;
-        const int64_t row = static_cast<int64_t>(w.r.q0) + w.tile * kUnit + tok;
-        const bool writes = tok < part.toks && row >= 0 && row < a.tokens, whole = w.whole(), begins = w.step == 0;
-        __half* to = a.out + (row * a.heads + w.copy) * kValue + half * (kValue / 2);
         float* pp = a.partials + (2 * static_cast<int64_t>(blockIdx.x) + begins) * kPartFloats + (two ? acc : 0) * (kTile * (kValue + 2));
 #pragma unroll 1
         for (int h = 0; h < kValue / 32; ++h) {
@@ -444,7 +453,6 @@ expanded_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant
           }
         }
         if (!whole && half == 0) reinterpret_cast<float2*>(pp + kTile * kValue)[r] = make_float2(m, l);
-        if (!whole && begins) join = make_int4(w.r.q0 + w.tile * kUnit, part.toks, w.copy, 1 + (w.all_steps - w.count + s_share.per - 1) / s_share.per);
       }
       // All together go to the next unit: the second accumulator's threads may have had nothing to do in this one, and
       // must not run ahead of the sums, and of s_ml, that the first one's threads still read.
@@ -452,7 +460,7 @@ expanded_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant
       named_bar_sync(kBarSoft, kSoft);
       if (tid == 0) mbar_arrive(bar_read);
     }
-    if (shares && tid == 0) a.joins[blockIdx.x] = join;
+    if (a.shares != 0 && tid == 0) a.joins[blockIdx.x] = join;
   }
 
   // ---------------------------------------------------------------------- teardown
@@ -469,7 +477,6 @@ expanded_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant
     if ((warp == kLoadK || warp == kLoadV) && lane == 0) {
       for (uint32_t i = issued > 2 ? issued - 2 : 0; i < issued; ++i) mbar_drain((warp == kLoadK ? bar_k : bar_v) + 8 * (i & 1), (i >> 1) & 1);
       if (warp == kLoadK && units > 0) mbar_drain(bar_q, (units - 1) & 1);
-      if (warp == kLoadV) mbar_drain(bar_fix, fixes & 1);
     }
     __syncthreads();
     if (tid == 0) atomicExch(a.status, static_cast<int>(PQ_ERR_TIMEOUT));

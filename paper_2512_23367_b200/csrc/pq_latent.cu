@@ -30,7 +30,7 @@ struct LatentCfg {
   // Queries lie in tensor memory, as many panels of them as there is room for, the others in shared memory.
   static constexpr int kHeld = kLatent == 512 ? 7 : 4, kQueryPanels = kPanels - kHeld;
   static constexpr int kStages = kLatent == 512 ? 3 : 6;   // steps whose latent vectors fit at once
-  static constexpr int kStage = kValuePanels * kPanel, kStep = kPanels * kPanel;
+  static constexpr int kStage = kValuePanels * kPanel;
   static constexpr int kSmem = kQueryPanels * kPanel + kStages * kStage + 2 * kPanel /* rotary keys, P */ + 1024 /* alignment */;
   static constexpr int kPartFloats = kRows * (kLatent + 2);   // [kLatent / 4][64 rows] x 4 sums, [64 rows] x (reference, sum of weights)
   // Tensor memory columns: O; S; the queries, two FP16 values each.
@@ -38,7 +38,15 @@ struct LatentCfg {
   static_assert(kColQ + 32 * kHeld <= 512, "tensor memory");
 };
 
+// Halves, of no more than 64 rows where two CTAs serve units: each takes every second one of their steps of 64 tokens, for five
+// quarters of the time (3100 of 2450 cycles: no other CTA reads the tokens); a unit takes about as much as four steps.
+struct LatentShape {
+  static constexpr int keys = kKeys, half_keys = 2 * kKeys, copies = 1, cost = 4, half_cost = 5, unit_cost = 16;
+  int rows, heads, halves;
+  __device__ __forceinline__ uint64_t floors(uint64_t n, uint64_t b) const { return floor_sum(n, static_cast<uint64_t>(keys) * heads, rows, b); }
+};
 struct LatentArgs {
+  using Shape = LatentShape;
   pq_latent_cache c;
   const int* table;
   int64_t width;
@@ -51,30 +59,34 @@ struct LatentArgs {
   float scale_log2;      // > 0
   uint32_t q_and, q_xor; // a scale of 0 or below is folded into the products: (s & q_and) ^ q_xor
   float* partials;       // two parts per CTA (nullptr: units are handed out whole, in turn)
-  int4* joins;           // per CTA: first row (a 64-bit number), rows, parts
+  int4* joins;           // per CTA: first row (a 64-bit number), rows, parts (negative: of both CTAs each)
   int box;               // tokens of a TMA box: the largest power of two that divides both the page and 64
   int* status;
   uint32_t wait_limit;
 
-  __device__ __forceinline__ UnitShape shape() const { return UnitShape{paired ? 2 * kRows : kRows, heads, kKeys, 1}; }
-  __device__ __forceinline__ Request request(int b) const {
-    Request r;
+  __device__ __forceinline__ Shape shape() const { return Shape{paired ? 2 * kRows : kRows, heads, paired}; }
+  __device__ __forceinline__ Request<Shape> request(int b, bool halves) const {
+    Request<Shape> r;
     r.s = shape();
     r.q0 = q_start[b];
     r.n = static_cast<int>(min(static_cast<int64_t>(max(q_start[b + 1] - r.q0, 0)), tokens));
     r.k0 = 0;
     r.L = max(kv_len[b], 0);
     r.hi = static_cast<int>(min(static_cast<int64_t>(r.L), width * c.page));
-    r.settle();
+    r.settle(halves);
     return r;
   }
 };
 
 // A CTA's units, with the 64 rows of a unit that are its own.
 struct LatentWalk : Walk<LatentArgs> {
-  using Walk<LatentArgs>::Walk;
-  __device__ __forceinline__ int row0() const { return tile * r.s.rows + (a.paired ? (blockIdx.x & 1) * kRows : 0); }
+  __device__ __forceinline__ LatentWalk(const LatentArgs& args, const Share& s, bool by_shares)
+      : Walk<LatentArgs>(args, s, by_shares, false, args.paired ? blockIdx.x >> 1 : blockIdx.x, args.paired ? gridDim.x >> 1 : gridDim.x) {}
+  __device__ __forceinline__ int second() const { return a.paired ? blockIdx.x & 1 : 0; }
+  __device__ __forceinline__ int row0() const { return tile * r.s.rows + (half() ? 0 : second() * kRows); }
   __device__ __forceinline__ int rows() const { return max(min(static_cast<int>(r.all) - row0(), kRows), 0); }
+  __device__ __forceinline__ int key0(int i) const { return (half() ? 2 * (step + i) + second() : step + i) * kKeys; }
+  __device__ __forceinline__ bool whole() const { return !half() && count == all_steps; }
 };
 
 // MMAs with M = 64 in the form that keeps B in place: all 128 lanes of tensor memory take part, lane r and lane 64 + r
@@ -144,12 +156,11 @@ latent_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__
   constexpr float kTop = 7.0f;          // a weight at the reference is 2^kTop
   constexpr int kCols = C::kCols;
   extern __shared__ uint8_t smem_raw[];
-  __shared__ __align__(8) uint64_t bars[2 * C::kStages * C::kGroups + 9];
+  __shared__ __align__(8) uint64_t bars[2 * C::kStages * C::kGroups + 8];
   __shared__ uint32_t s_tmem;
   __shared__ volatile int s_abort;
+  __shared__ ShareRoom s_share;
   __shared__ volatile uint32_t s_landed;   // steps
-  __shared__ Share s_share;
-  __shared__ int64_t s_sums[kThreads / 32];
   __shared__ float s_swap[4][kRows];
 
   const int tid = threadIdx.x, warp = __shfl_sync(0xffffffffu, tid >> 5, 0), lane = tid & 31;
@@ -157,16 +168,15 @@ latent_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__
   const uint32_t bar_full = smem_u32(bars), bar_free = bar_full + 8 * C::kStages * C::kGroups, bar_rope = bar_free + 8 * C::kStages * C::kGroups;
   const uint32_t bar_rfree = bar_rope + 8, bar_s = bar_rfree + 8, bar_o = bar_s + 8;
   // A unit's queries are there, are free; its sums have been read.
-  const uint32_t bar_q = bar_o + 8, bar_qfree = bar_q + 8, bar_read = bar_qfree + 8, bar_fix = bar_read + 8, bar_drain = bar_fix + 8;
+  const uint32_t bar_q = bar_o + 8, bar_qfree = bar_q + 8, bar_read = bar_qfree + 8, bar_drain = bar_read + 8;
   if (tid == 0) {
     for (int i = 0; i < 2 * C::kStages * C::kGroups + 4; ++i) mbar_init(bar_full + 8 * i, 1);   // up to bar_o
     mbar_init(bar_q, kSoft / 32 + (C::kQueryPanels > 0 ? 1 : 0));
     mbar_init(bar_qfree, 1);
     mbar_init(bar_read, kSoft / 32);
-    mbar_init(bar_fix, 1);
     mbar_init(bar_drain, 1);
     fence_mbar_init();
-    s_abort = 0, s_landed = 0;
+    s_abort = 0, s_landed = 0, s_share.clear();
     tma_prefetch_desc(&map_q), tma_prefetch_desc(&map_c), tma_prefetch_desc(&map_r);
   }
   if (warp == kIssuer) {
@@ -174,17 +184,15 @@ latent_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__
     tmem_relinquish();
   }
   tc_fence_before_sync();
-  grid_dep_wait();
-  const int worker = a.paired ? blockIdx.x >> 1 : blockIdx.x, workers = a.paired ? gridDim.x >> 1 : gridDim.x;
-  const bool shares = a.partials != nullptr;
-  if (shares) find_share<kThreads>(a, worker, workers, kLeastSteps, &s_share, s_sums); else __syncthreads();
+  __syncthreads();
   tc_fence_after_sync();
+  grid_dep_wait();
+  const bool shares = a.partials != nullptr && find_share<kThreads, kHalvesCut>(a, blockIdx.x >> a.paired, gridDim.x >> a.paired, kLeastSteps * LatentShape::cost, s_share);
   grid_dep_launch();   // only now: a later launch's CTA may take this SM's tensor memory when it is given back
   const uint32_t tmem = __shfl_sync(0xffffffffu, s_tmem, 0), tmem_s = tmem + C::kColS;
   const uint32_t sq = (smem_u32(smem_raw) + 1023u) & ~1023u, ring = sq + C::kQueryPanels * kPanel, rope = ring + C::kStages * C::kStage, weights = rope + kPanel;
   const WaitCtx wc{&s_abort, a.wait_limit};
-  // loader: stages filled, steps (a unit's queries take a stage, too), steps by way of bar_fix; units
-  uint32_t filled = 0, issued = 0, fixes = 0, units = 0;
+  uint32_t filled = 0, issued = 0, units = 0;   // loader: stages filled, steps (a unit's queries take a stage, too); units
 
   if (warp == kLoader) {
     // -------------------------------------------------------------------- loader: a lane requests one box
@@ -195,12 +203,12 @@ latent_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__
     auto wait_free = [&](int g) {
       if (ok && filled >= C::kStages) ok = warp_wait(bar_free + 8 * ((filled % C::kStages) * C::kGroups + g), ((filled / C::kStages) & 1) ^ 1, wc);
     };
-    for (LatentWalk w(a, s_share, shares, worker, workers); ok && w.more(); w.next()) {
+    for (LatentWalk w(a, s_share.share, shares); ok && w.more(); w.next()) {
       if (w.rows() == 0) continue;
       const int* trow = a.table + static_cast<int64_t>(w.b) * a.width;
       int id = -1, off = 0;
       auto look_up = [&](int i) {
-        const int key = (w.step + i) * kKeys + lane * a.box;
+        const int key = w.key0(i) + lane * a.box;
         id = -1;
         if (!mine || i >= w.count || key >= w.r.hi) return;
         const int col = key / a.c.page;
@@ -228,37 +236,22 @@ latent_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__
       for (int i = 0; i < w.count; ++i) {
         const uint32_t st = filled % C::kStages;
         const int row = (id < 0 || id >= a.c.pages ? rows_all : id * a.c.page + off) / 8;   // beyond the tensor: zeros
-        const int dead = min(max(w.r.hi - (w.step + i) * kKeys, 0), kKeys);   // first token of the step that was never written
         const uint32_t dst = ring + st * C::kStage;
-        if (dead < kKeys && lane == 0) mbar_arrive_expect_tx(bar_fix, C::kStep);
 #pragma unroll
         for (int g = 0; g < C::kGroups; ++g) {
           const uint32_t full = bar_full + 8 * (st * C::kGroups + g);
           wait_free(g);
-          if (ok && dead == kKeys && lane == 0) mbar_arrive_expect_tx(full, 4 * kPanel);
+          if (ok && lane == 0) mbar_arrive_expect_tx(full, 4 * kPanel);
           __syncwarp();
-          if (ok && mine) tma_load_4d(dst + 4 * g * kPanel + lane * groups8 * kTokens8, &map_c, dead < kKeys ? bar_fix : full, 0, 0, 4 * g, row);
+          if (ok && mine) tma_load_4d(dst + 4 * g * kPanel + lane * groups8 * kTokens8, &map_c, full, 0, 0, 4 * g, row);
         }
         if (ok && issued > 0) ok = warp_wait(bar_rfree, (issued & 1) ^ 1, wc);
         if (!ok) break;
-        if (dead == kKeys && lane == 0) mbar_arrive_expect_tx(bar_rope, kPanel);
+        if (lane == 0) mbar_arrive_expect_tx(bar_rope, kPanel);
         __syncwarp();
-        if (mine) tma_load_4d(rope + lane * groups8 * kAtom, &map_r, dead < kKeys ? bar_fix : bar_rope, 0, 0, C::kValuePanels, row);
+        if (mine) tma_load_4d(rope + lane * groups8 * kAtom, &map_r, bar_rope, 0, 0, C::kValuePanels, row);
         look_up(i + 1);   // used, and so waited for, in the next round
         ++issued, ++filled;
-        if (dead < kKeys) {   // 0 x NaN is not 0: the weights of such tokens are, their vectors have to be
-          if (!(ok = warp_wait(bar_fix, fixes & 1, wc))) break;
-          ++fixes;
-          for (int j = lane; j < (kKeys - dead) * (kLatent / 8); j += 32) {
-            const int r = dead + j / (kLatent / 8), c = j % (kLatent / 8), panel = c >> 3;
-            const uint32_t at = dst + (panel >> 2) * (4 * kPanel) + (r >> 3) * kTokens8 + (panel & 3) * kAtom + (r & 7) * 128 + (c & 7) * 16;
-            asm volatile("st.shared.v4.u32 [%0], {%1, %1, %1, %1};" ::"r"(at), "r"(0) : "memory");
-          }
-          fence_proxy_async_smem();
-          __syncwarp();
-          if (lane < C::kGroups) mbar_arrive(bar_full + 8 * (st * C::kGroups + lane));
-          if (lane == C::kGroups) mbar_arrive(bar_rope);
-        }
         __syncwarp();
       }
     }
@@ -273,7 +266,7 @@ latent_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__
     const uint32_t q_lo = desc_k(sq), k_lo0 = desc_k(ring), v_lo0 = desc_mn(ring, kAtom), r_lo = desc_k(rope), p_lo = desc_k(weights), t_q = tmem + C::kColQ;
     uint32_t n = 0, seg = 0;   // stages, units before
     bool on = true;
-    for (LatentWalk w(a, s_share, shares, worker, workers); w.more(); w.next()) {
+    for (LatentWalk w(a, s_share.share, shares); w.more(); w.next()) {
       if (w.rows() == 0) continue;
       on = on && warp_wait(bar_q, seg & 1, wc);
       if (leader && on) {   // the queries have been taken out of their stage
@@ -335,12 +328,22 @@ latent_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__
     // -------------------------------------------------------------------- watcher: waits for the operands a step ahead
     bool ok = true;
     uint32_t u = 0, n = 0;
-    for (LatentWalk w(a, s_share, shares, worker, workers); w.more(); w.next()) {
+    for (LatentWalk w(a, s_share.share, shares); w.more(); w.next()) {
       if (w.rows() == 0) continue;
       ++n;   // the queries' stage is the softmax threads'
       for (int i = 0; i < w.count; ++i, ++u, ++n) {
 #pragma unroll
         for (int g = 0; g < C::kGroups; ++g) ok = ok && warp_wait(bar_full + 8 * ((n % C::kStages) * C::kGroups + g), (n / C::kStages) & 1, wc);
+        const int dead = max(w.r.hi - w.key0(i), 0);   // first token of the step that was never written
+        if (ok && dead < kKeys) {   // 0 x NaN is not 0: the weights of such tokens are, their vectors have to be
+          for (int j = lane; j < (kKeys - dead) * (kLatent / 8); j += 32) {
+            const int r = dead + j / (kLatent / 8), c = j % (kLatent / 8), panel = c >> 3;
+            const uint32_t at = ring + (n % C::kStages) * C::kStage + (panel >> 2) * (4 * kPanel) + (r >> 3) * kTokens8 + (panel & 3) * kAtom + (r & 7) * 128 + (c & 7) * 16;
+            asm volatile("st.shared.v4.u32 [%0], {%1, %1, %1, %1};" ::"r"(at), "r"(0) : "memory");
+          }
+          fence_proxy_async_smem();
+          __syncwarp();
+        }
         tile_landed(kBarTile, ok);
         if (lane == 0) s_landed = u + 1;
         ok = ok && warp_wait(bar_rope, u & 1, wc);
@@ -357,17 +360,17 @@ latent_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__
     const int tokens = kKeys / 2, first = static_cast<int>(blockIdx.x & 1) * tokens;
     uint32_t n = 0;
     bool on = a.paired != 0;
-    for (LatentWalk w(a, s_share, shares, worker, workers); on && w.more(); w.next()) {
+    for (LatentWalk w(a, s_share.share, shares); on && w.more(); w.next()) {
       if (w.rows() == 0) continue;
       const int* trow = a.table + static_cast<int64_t>(w.b) * a.width;
       for (int i = 0; on && i < w.count; ++i, ++n) {
-        if (n < static_cast<uint32_t>(C::kStages)) continue;   // being loaded
+        if (n < static_cast<uint32_t>(C::kStages) || w.half()) continue;   // being loaded; not shared
         for (uint32_t polls = 0; on && (s_landed == 0 || s_landed + kDistance < n); ++polls) {   // (not in the way of the first ones)
           __nanosleep(100);
           on = polls < wc.limit && !s_abort;
         }
         for (int t = lane; t < tokens; t += 32) {
-          const int key = (w.step + i) * kKeys + first + t;
+          const int key = w.key0(i) + first + t;
           const int id = key < w.r.hi ? trow[key / a.c.page] : -1;
           if (id < 0 || id >= a.c.pages) continue;
           const char* at = data + (static_cast<int64_t>(id) * a.c.page + key % a.c.page) * (kLines * 128);
@@ -390,15 +393,15 @@ latent_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__
     uint32_t u = 0, n = 0;   // steps, stages
     int4 join = make_int4(0, 0, 0, 0);
     bool ok = true;
-    for (LatentWalk w(a, s_share, shares, worker, workers); w.more(); w.next()) {
-      if (w.rows() == 0) continue;
-      const int rows = w.rows(), shift = w.r.L - w.r.n;
-      const int row0 = w.row0(), row = row0 + r;
-      const bool live = r < rows;
-      const int64_t at = static_cast<int64_t>(w.r.q0) * a.heads + row;   // of the output
-      const bool there = live && at >= 0 && at < a.tokens * a.heads;
-      // the unit's queries out of their stage: the two warps of a lane take half of the row's panels each
-      {
+    // A unit's queries are taken, and its first S computed, before the sums of the unit before go out.
+    LatentWalk w(a, s_share.share, shares);
+    bool begins = false, whole = false, there = false, open = false;   // of the unit before
+    float m = 0.0f, l = 0.0f;
+    int64_t at = 0;   // row of the output
+    for (;;) {
+      while (w.more() && w.rows() == 0) w.next();
+      const bool more = w.more();
+      if (more) {   // the unit's queries out of their stage: the two warps of a lane take half of the row's panels each
         const uint32_t stage = ring + (n % C::kStages) * C::kStage + r * 128;
 #pragma unroll
         for (int g = 0; g < C::kGroups; ++g) ok = ok && warp_wait(bar_full + 8 * ((n % C::kStages) * C::kGroups + g), (n / C::kStages) & 1, wc);
@@ -416,12 +419,50 @@ latent_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__
         if (lane == 0) mbar_arrive(bar_q);
         n += 1 + w.count;
       }
+      if (open) {   // ---------------------------------------------------- the end of the unit (or part) before
+        ok = ok && warp_wait(bar_o, (u - 1) & 1, wc);
+        tc_fence_after_sync();
+        l = row_combine<true>(swap, swap_row, id, l);
+        const float inv = l > 0.0f ? 1.0f / l : 0.0f;
+        float* pp = a.partials + (2 * static_cast<int64_t>(blockIdx.x) + begins) * C::kPartFloats;
+#pragma unroll 1
+        for (int c = (kCols / 2) * (warp >> 2), k = 0; k < kCols / 2; k += 32, c += 32) {
+          uint32_t o[32];
+          tmem_ld_32x32(t_o + k, o);
+          tmem_ld_wait();
+          const int value = (c >> 7) * 256 + half * 128 + (c & 127);   // columns 128 h .. of tensor memory are the values 256 h + 128 half ..
+          if (!there) continue;
+          if (whole) {
+            __half* to = a.out + at * kLatent + value;
+#pragma unroll
+            for (int j = 0; j < 2; ++j) {   // whole 32-byte sectors
+              uint32_t x[8];
+#pragma unroll
+              for (int i = 0; i < 8; ++i) x[i] = pack_f16(__uint_as_float(o[16 * j + 2 * i]) * inv, __uint_as_float(o[16 * j + 2 * i + 1]) * inv);
+              store_32_bytes(to + 16 * j, x[0], x[1], x[2], x[3], x[4], x[5], x[6], x[7]);
+            }
+          } else {
+            float4* to = reinterpret_cast<float4*>(pp) + (value / 4) * kRows + r;
+#pragma unroll
+            for (int j = 0; j < 8; ++j)
+              to[j * kRows] = make_float4(__uint_as_float(o[4 * j]), __uint_as_float(o[4 * j + 1]), __uint_as_float(o[4 * j + 2]), __uint_as_float(o[4 * j + 3]));
+          }
+        }
+        if (!whole && there && part == 0) reinterpret_cast<float2*>(pp + kRows * kLatent)[r] = make_float2(m, l);
+        tc_fence_before_sync();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(bar_read);
+      }
+      if (!more) break;
+      const int rows = w.rows(), shift = w.r.L - w.r.n;
+      const int row0 = w.row0(), row = row0 + r;
+      const bool live = r < rows;
       const int p0 = shift + row0 / a.heads;                                     // the first row's position
       const int see_to = live ? min(shift + row / a.heads, w.r.hi - 1) - 16 * part : -1;   // from the thread's first token
       const int all_to = min(p0 + 1, w.r.hi);                                    // every row sees the tokens before
-      float m = -INFINITY, l = 0.0f;   // m: the reference, in powers of two; l: the thread's own tokens
+      m = -INFINITY, l = 0.0f;   // m: the reference, in powers of two; l: the thread's own tokens
       for (int i = 0; i < w.count; ++i, ++u) {
-        const int key0 = (w.step + i) * kKeys;
+        const int key0 = w.key0(i);
         ok = ok && warp_wait(bar_s, u & 1, wc);
         tc_fence_after_sync();
         uint32_t s[16];
@@ -498,45 +539,14 @@ latent_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__
         unpair_f32(sum, l0, l1);
         l += l0 + l1;
       }
-      // ------------------------------------------------------------------ the unit's (or part's) end
-      ok = ok && warp_wait(bar_o, (u - 1) & 1, wc);
-      tc_fence_after_sync();
-      l = row_combine<true>(swap, swap_row, id, l);
-      const bool whole = w.whole(), begins = w.step == 0;
-      const float inv = l > 0.0f ? 1.0f / l : 0.0f;
-      float* pp = a.partials + (2 * static_cast<int64_t>(blockIdx.x) + begins) * C::kPartFloats;
-#pragma unroll 1
-      for (int c = (kCols / 2) * (warp >> 2), n = 0; n < kCols / 2; n += 32, c += 32) {
-        uint32_t o[32];
-        tmem_ld_32x32(t_o + n, o);
-        tmem_ld_wait();
-        const int value = (c >> 7) * 256 + half * 128 + (c & 127);   // columns 128 h .. of tensor memory are the values 256 h + 128 half ..
-        if (!there) continue;
-        if (whole) {
-          __half* to = a.out + at * kLatent + value;
-#pragma unroll
-          for (int j = 0; j < 2; ++j) {   // whole 32-byte sectors
-            uint32_t x[8];
-#pragma unroll
-            for (int k = 0; k < 8; ++k) x[k] = pack_f16(__uint_as_float(o[16 * j + 2 * k]) * inv, __uint_as_float(o[16 * j + 2 * k + 1]) * inv);
-            store_32_bytes(to + 16 * j, x[0], x[1], x[2], x[3], x[4], x[5], x[6], x[7]);
-          }
-        } else {
-          float4* to = reinterpret_cast<float4*>(pp) + (value / 4) * kRows + r;
-#pragma unroll
-          for (int j = 0; j < 8; ++j)
-            to[j * kRows] = make_float4(__uint_as_float(o[4 * j]), __uint_as_float(o[4 * j + 1]), __uint_as_float(o[4 * j + 2]), __uint_as_float(o[4 * j + 3]));
-        }
-      }
-      if (!whole && there && part == 0) reinterpret_cast<float2*>(pp + kRows * kLatent)[r] = make_float2(m, l);
+      at = static_cast<int64_t>(w.r.q0) * a.heads + row;
+      there = live && at >= 0 && at < a.tokens * a.heads, whole = w.whole(), begins = w.step == 0, open = true;
       if (!whole && begins) {
-        const int64_t first = static_cast<int64_t>(w.r.q0) * a.heads + row0;
+        const int64_t first = at - r;
         join = make_int4(static_cast<int>(first & 0xffffffff), static_cast<int>(first >> 32), rows,
-                         1 + (w.all_steps - w.count + s_share.per - 1) / s_share.per);
+                         w.parts(s_share.share.per) * (w.half() ? -2 : 1));
       }
-      tc_fence_before_sync();
-      __syncwarp();
-      if (lane == 0) mbar_arrive(bar_read);
+      w.next();
     }
     if (a.partials && tid == 0) a.joins[blockIdx.x] = join;
   }
@@ -557,7 +567,6 @@ latent_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__
         for (int g = 0; g < C::kGroups; ++g) mbar_drain(bar_full + 8 * ((i % C::kStages) * C::kGroups + g), (i / C::kStages) & 1);
       }
       mbar_drain(bar_rope, (issued & 1) ^ 1), mbar_drain(bar_rope, issued & 1);
-      mbar_drain(bar_fix, fixes & 1);
       if (units > 0) mbar_drain(bar_q, (units - 1) & 1);
     }
     __syncthreads();
@@ -573,15 +582,16 @@ template <int kLatent, int kGroups>
 __global__ void __launch_bounds__(kJoinThreads) latent_join_kernel(const LatentArgs a) {
   grid_dep_launch();
   grid_dep_wait();
-  const int4 join = a.joins[blockIdx.x];   // first row (64 bits), rows, parts
-  if (join.w == 0) return;
+  const int4 join = a.joins[blockIdx.x];
+  const bool both = join.w < 0;   // the parts of two neighbouring CTAs each; the first one joins them
+  if (join.w == 0 || (both && (blockIdx.x & 1))) return;
   const int r = threadIdx.x % kRows, first = kGroups > 1 ? blockIdx.y * 16 : blockIdx.y * 64 + threadIdx.x / kRows * 16;
   const int64_t at = (static_cast<int64_t>(join.y) << 32 | static_cast<uint32_t>(join.x)) + r;
-  const int next = a.paired ? 2 : 1;
-  // the unit's first part is the second one of its CTA, the others the first of theirs
-  auto part = [&](int i) { return a.partials + (2 * (static_cast<int64_t>(blockIdx.x) + i * next) + (i == 0)) * LatentCfg<kLatent>::kPartFloats; };
+  const int next = a.paired && !both ? 2 : 1, begin = both ? 2 : 1;
+  // the unit's first parts are the second ones of their CTAs, the others the first
+  auto part = [&](int i) { return a.partials + (2 * (static_cast<int64_t>(blockIdx.x) + i * next) + (i < begin)) * LatentCfg<kLatent>::kPartFloats; };
   const bool there = r < join.z && at >= 0 && at < a.tokens * a.heads;
-  join_parts<kRows, kLatent, kGroups>(part, join.w, first, there ? a.out + at * kLatent + first : nullptr);
+  join_parts<kRows, kLatent, kGroups>(part, abs(join.w), first, there ? a.out + at * kLatent + first : nullptr);
 }
 
 size_t partial_bytes(int latent, int sms) { return static_cast<size_t>(sms) * (2 * kRows * (latent + 2) * sizeof(float) + sizeof(int4)); }

@@ -2,9 +2,11 @@
 // the requests' lengths.
 //
 // A UNIT is a tile of a request's query rows (for one head, where heads have keys of their own) with the STEPS of keys that
-// its last row sees.  Two ways to hand units out:
-//   shares   the steps of all units, in order, are cut into runs of one length, one per CTA, so that every SM takes the same
-//            share whatever the lengths are.  A share may begin and end inside a unit: that unit's parts are joined later.
+// its last row sees.  A request's last tile may have no more than half of a tile's rows; its steps take less than twice the time per
+// row then, in a way of the kernel's own (HALVES).  Two ways to hand units out:
+//   shares   the steps of all units, in order, weighed by what they take (COST), are cut into runs of one cost, one per CTA, so that
+//            every SM takes the same share whatever the lengths are.  A share may begin and end inside a unit, a step being its
+//            who has the step's begin: that unit's parts are joined later.
 //   turns    whole units, a request's last tile, which sees most keys, first: CTA c of n takes the units c, 2n - 1 - c, 2n + c, ...,
 //            there and back again, so that who has the largest of one turn has the smallest of the next (512 units of a prompt of
 //            4096: the longest CTA has 3 % more than its share; with c, n + c, 2n + c, ... it had 26).
@@ -17,135 +19,219 @@
 
 namespace pq {
 
-// sum over 0 <= i < n of floor((a i + b) / m), by the Euclidean algorithm.
-__device__ inline uint64_t floor_sum(uint64_t n, uint64_t m, uint64_t a, uint64_t b) {
+// sum over 0 <= i < n of floor((a i + b) / m), by the Euclidean algorithm.  a n + b only falls: in 32 bits if it fits them at first
+// (a 64-bit division is some hundred instructions).
+template <typename T>
+__device__ __forceinline__ uint64_t floor_sum_in(T n, T m, T a, T b) {
   uint64_t sum = 0;
   while (n > 0) {
-    if (a >= m) sum += (n - 1) * n / 2 * (a / m), a %= m;
-    if (b >= m) sum += n * (b / m), b %= m;
-    const uint64_t top = a * n + b;
+    if (a >= m) sum += static_cast<uint64_t>(n - 1) * n / 2 * (a / m), a %= m;
+    if (b >= m) sum += static_cast<uint64_t>(n) * (b / m), b %= m;
+    const T top = a * n + b;
     if (top < m) break;
     n = top / m, b = top % m;
-    const uint64_t x = a;
+    const T x = a;
     a = m, m = x;
   }
   return sum;
 }
+__device__ inline uint64_t floor_sum(uint64_t n, uint64_t m, uint64_t a, uint64_t b) {
+  if (m <= 0xffffffffu && a * n + b <= 0xffffffffu)   // n >= 1: a and b, too
+    return floor_sum_in(static_cast<uint32_t>(n), static_cast<uint32_t>(m), static_cast<uint32_t>(a), static_cast<uint32_t>(b));
+  return floor_sum_in(n, m, a, b);
+}
 
 constexpr int kFewSteps = 6;   // of a unit at most: shares are not worth their joining
 
-struct UnitShape {
-  int rows;      // query rows of a tile
-  int heads;     // rows per token: row r of a request is of token r / heads
-  int keys;      // keys of a step
-  int copies;    // units per tile
-};
+// The same where a and m are constants: without a division but by them.
+template <uint32_t m, uint32_t a>
+__device__ __forceinline__ uint64_t floor_sum_of(uint64_t n, uint64_t b) {
+  uint64_t sum = (n - 1) * n / 2 * (a / m) + n * (b / m);   // n >= 1
+  b %= m;
+  if constexpr (a % m != 0) {
+    const uint64_t top = a % m * n + b;
+    if (top >= m) sum += floor_sum_of<a % m, m>(top / m, top % m);
+  }
+  return sum;
+}
 
+// A kernel's units.  Shape has
+//   rows     query rows of a tile
+//   heads    rows per token: row r of a request is of token r / heads
+//   keys     keys of a step;  half_keys: of one of a half
+//   copies   units per tile
+//   halves   whether a last tile of half the rows has steps of its own kind
+//   cost, half_cost, unit_cost   of a step, of the beginning and the end of a unit
+//   uint64_t floors(n, b)   sum over 0 <= i < n of floor((rows i + b) / (keys heads)), n >= 1
+template <class Shape>
 struct Request {
   int q0, n;              // first token, tokens (n * heads, and units over all requests, below 2^31)
-  int k0, L, hi;          // first key (where keys are ragged rows), keys, keys that can be read
-  UnitShape s;
+  int k0, L, hi;          // first key (where keys are ragged rows), keys, keys that can be read (below 2^31 - 2 half_keys)
+  Shape s;
   uint32_t all;           // rows: below 2^31
   int tiles;
-  int same;               // > 0: steps of every unit (fewer keys than rows, or than the table holds)
-  __device__ __forceinline__ void settle() {
+  int half;               // the tile that is a half (none: -1)
+  __device__ __forceinline__ void settle(bool halves) {
     all = static_cast<uint32_t>(n) * static_cast<uint32_t>(s.heads);
     tiles = static_cast<int>((all + s.rows - 1) / static_cast<uint32_t>(s.rows));
-    same = L < n || hi < L ? max((hi + s.keys - 1) / s.keys, 1) : 0;
+    half = halves && may_halve() ? tiles - 1 : -1;
   }
+  __device__ __forceinline__ bool may_halve() const { return s.halves && tiles > 0 && all - static_cast<uint32_t>(tiles - 1) * s.rows <= static_cast<uint32_t>(s.rows / 2); }
   __device__ __forceinline__ int units() const { return tiles * s.copies; }
-  __device__ __forceinline__ int steps(int tile) const {
-    if (same) return same;
+  __device__ __forceinline__ bool same() const { return L < n || hi < L; }   // all rows end alike: fewer keys than rows, or than the table holds
+  __device__ __forceinline__ int seen(int tile) const {   // keys, 1 at least
+    if (same()) return max(hi, 1);
     const uint32_t last = min(static_cast<uint32_t>(tile + 1) * s.rows, all) - 1;
-    return (L - n + static_cast<int>(last / static_cast<uint32_t>(s.heads))) / s.keys + 1;
+    return L - n + static_cast<int>(last / static_cast<uint32_t>(s.heads)) + 1;
   }
-  __device__ __forceinline__ int64_t before_tile(int tile) const {   // steps of one copy of the tiles before; tile < tiles
-    if (same) return static_cast<int64_t>(same) * tile;
+  __device__ __forceinline__ int steps(int tile, bool as_half) const { return as_half ? (seen(tile) - 1) / s.half_keys + 1 : (seen(tile) - 1) / s.keys + 1; }
+  __device__ __forceinline__ int steps(int tile) const { return steps(tile, tile == half); }
+  __device__ __forceinline__ int cost(int tile, bool as_half) const { return steps(tile, as_half) * (as_half ? s.half_cost : s.cost) + s.unit_cost; }
+  __device__ __forceinline__ int64_t before_tile(int tile) const {   // of one copy of the tiles before; tile < tiles
     if (tile == 0) return 0;
-    return static_cast<int64_t>(floor_sum(tile, static_cast<uint64_t>(s.keys) * s.heads, s.rows, s.rows - 1 + static_cast<uint64_t>(L - n) * s.heads)) + tile;
+    if (same()) return static_cast<int64_t>(cost(0, false)) * tile;
+    return static_cast<int64_t>(s.floors(tile, s.rows - 1 + static_cast<uint64_t>(L - n) * s.heads)) * s.cost + static_cast<int64_t>(tile) * (s.cost + s.unit_cost);
   }
   __device__ __forceinline__ int64_t before(int unit) const {        // unit < units()
     const int tile = unit / s.copies, copy = unit - tile * s.copies;
-    return before_tile(tile) * s.copies + static_cast<int64_t>(copy) * (copy ? steps(tile) : 0);
+    return before_tile(tile) * s.copies + static_cast<int64_t>(copy) * (copy ? cost(tile, tile == half) : 0);
   }
-  __device__ __forceinline__ int64_t total() const { return tiles == 0 ? 0 : (before_tile(tiles - 1) + steps(tiles - 1)) * s.copies; }
 };
 
-// Shares: `left` steps from step `step` of unit `unit` of request `b` on.
+// Shares: `left` of cost from `off` of unit `unit` of request `b` on; `per` of a whole share.
 struct Share {
-  int b, unit, step, per;
-  int64_t left;
+  int b, unit, off, per;
+  int halves;
+  int64_t left, at;
+};
+// Halves: in kHalvesCut only where none of them fits a share, so that all of them are cut.
+enum Halves { kHalvesCut, kHalvesAlways };
+struct ShareRoom {   // shared memory
+  Share share;
+  int64_t sums[2][32];
+  int shortest, longest, units;   // set by the kernel to the largest int, 0, 0
+  __device__ __forceinline__ void clear() { shortest = 0x7fffffff, longest = units = 0; }
 };
 
-// By the whole block; sums: one word per warp.
-template <int kThreads, class Args>
-__device__ __forceinline__ void find_share(const Args& a, int worker, int workers, int least, Share* share, int64_t* sums) {
+// By the whole block; false: whole units by turns take no longer.  They are not cut, which costs about two units' begins and ends,
+// one for the other part and one for the joining (35 requests of two units each, of eight steps, on 74 pairs of CTAs: 33 us; 43 in shares).
+template <int kThreads, Halves kHalves, class Args>
+__device__ __forceinline__ bool find_share(const Args& a, int worker, int workers, int least, ShareRoom& room) {
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   const int each = (a.requests + kThreads - 1) / kThreads;
   const int b0 = min(tid * each, a.requests), b1 = min(b0 + each, a.requests);
-  int64_t mine = 0;
-  for (int b = b0; b < b1; ++b) mine += a.request(b).total();
-  int64_t in = mine;
-#pragma unroll
-  for (int o = 1; o < 32; o <<= 1) {
-    const int64_t x = __shfl_up_sync(0xffffffffu, in, o);
-    if (lane >= o) in += x;
+  int shortest = 0x7fffffff, longest = 0, units = 0;   // of the halves; of all units, their number
+  auto total = [&](int b, int64_t (&t)[2]) {   // cost without, with halves
+    const auto r = a.request(b, false);
+    t[0] = t[1] = 0;
+    if (r.tiles == 0) return;
+    const int64_t before = r.before_tile(r.tiles - 1);
+    const int last = r.cost(r.tiles - 1, false);
+    t[0] = t[1] = (before + last) * r.s.copies;
+    longest = max(longest, last), units += r.units();
+    if (!r.may_halve()) return;
+    const int half = r.cost(r.tiles - 1, true);
+    t[1] = (before + half) * r.s.copies;
+    shortest = min(shortest, half);
+  };
+  int64_t mine[2] = {0, 0};
+#pragma unroll 1
+  for (int b = b0; b < b1; ++b) {
+    int64_t t[2];
+    total(b, t);
+    mine[0] += t[0], mine[1] += t[1];
   }
-  if (lane == 31) sums[warp] = in;
-  if (tid == 0) share->left = 0, share->b = a.requests, share->unit = 0, share->step = 0;
+  constexpr int kFirst = kHalves == kHalvesAlways ? 1 : 0;
+  int64_t in[2] = {mine[0], mine[1]};
+#pragma unroll
+  for (int h = kFirst; h < 2; ++h) {
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+      const int64_t x = __shfl_up_sync(0xffffffffu, in[h], o);
+      if (lane >= o) in[h] += x;
+    }
+    if (lane == 31) room.sums[h][warp] = in[h];
+  }
+  if (kHalves == kHalvesCut) shortest = __reduce_min_sync(0xffffffffu, shortest);
+  longest = __reduce_max_sync(0xffffffffu, longest), units = __reduce_add_sync(0xffffffffu, units);
+  if (lane == 0 && units > 0) {
+    if (kHalves == kHalvesCut) atomicMin(&room.shortest, shortest);
+    atomicMax(&room.longest, longest), atomicAdd(&room.units, units);
+  }
+  if (tid == 0) room.share.left = 0, room.share.b = a.requests, room.share.unit = 0, room.share.off = 0;
   __syncthreads();
-  int64_t off = in - mine, all = 0;
+  int64_t off[2] = {in[0] - mine[0], in[1] - mine[1]}, all[2] = {0, 0};
 #pragma unroll
-  for (int w = 0; w < kThreads / 32; ++w) {
-    if (w < warp) off += sums[w];
-    all += sums[w];
-  }
-  int64_t per = (all + workers - 1) / workers;
-  if (per < least) per = least;
-  const int64_t first = per * worker;
-  if (first < all && first >= off && first < off + mine) {
-    int64_t at = first - off;
-    for (int b = b0; b < b1; ++b) {
-      const Request r = a.request(b);
-      const int64_t t = r.total();
-      if (at >= t) {
-        at -= t;
-        continue;
-      }
-      int lo = 0, hi = r.units() - 1;   // the last unit that begins at or before the step
-      while (lo < hi) {
-        const int mid = lo + (hi - lo + 1) / 2;
-        if (r.before(mid) <= at) lo = mid; else hi = mid - 1;
-      }
-      share->b = b, share->unit = lo, share->step = static_cast<int>(at - r.before(lo));
-      share->left = min(per, all - first);
-      break;
+  for (int h = kFirst; h < 2; ++h) {
+#pragma unroll
+    for (int w = 0; w < kThreads / 32; ++w) {
+      const int64_t x = room.sums[h][w];
+      all[h] += x;
+      if (w < warp) off[h] += x;
     }
   }
-  if (tid == 0) share->per = static_cast<int>(min(per, static_cast<int64_t>(0x7fffffff)));
+  auto per_of = [&](int64_t cost) {   // (a 64-bit division takes 700 cycles)
+    const uint64_t up = static_cast<uint64_t>(cost + workers - 1);
+    return max(static_cast<int64_t>(up >> 32 ? up / workers : static_cast<uint32_t>(up) / static_cast<uint32_t>(workers)), static_cast<int64_t>(least));
+  };
+  int h = 1;
+  int64_t per = per_of(all[1]);
+  if (kHalves == kHalvesCut && room.shortest <= per) h = 0, per = per_of(all[0]);
+  if ((room.units + workers - 1) / workers * static_cast<int64_t>(room.longest) <= per + 2 * a.shape().unit_cost) return false;
+  const int64_t all_h = h ? all[1] : all[0], off_h = h ? off[1] : off[0], mine_h = h ? mine[1] : mine[0];
+  const int64_t first = per * worker;
+  if (first < all_h && first >= off_h && first < off_h + mine_h) {   // one thread's
+    int64_t at = first - off_h;
+    int b = b0;
+    for (; b < b1 - 1; ++b) {
+      int64_t t[2];
+      total(b, t);
+      const int64_t x = h ? t[1] : t[0];
+      if (at < x) break;
+      at -= x;
+    }
+    room.share.b = b, room.share.at = at, room.share.left = min(per, all_h - first);
+  }
+  if (tid == 0) room.share.per = static_cast<int>(min(per, static_cast<int64_t>(0x7fffffff))), room.share.halves = h;
   __syncthreads();
+  if (warp == 0 && room.share.left > 0) {   // the last unit of the request that begins at or before that: 32 at a time
+    const auto r = a.request(room.share.b, h != 0);
+    const int64_t at = room.share.at;
+    int lo = 0, n = r.units();
+    while (n > 1) {
+      const int stride = (n + 31) / 32, probe = lane * stride;
+      const uint32_t yes = __ballot_sync(0xffffffffu, probe < n && r.before(lo + probe) <= at);   // of lane 0 always
+      const int k = 31 - __clz(yes);
+      lo += k * stride, n = min(stride, n - k * stride);
+    }
+    if (lane == 0) room.share.unit = lo, room.share.off = static_cast<int>(at - r.before(lo));
+  }
+  __syncthreads();
+  return true;
 }
 
 // Walks the units of one CTA, as every warp of it does for itself; all lanes together.  By turns, a lane keeps one of 32
 // requests, so that going on to the next unit reads no memory (it took 3000 cycles between a unit's end and the next one's begin).
 template <class Args>
 struct Walk {
+  using Shape = typename Args::Shape;
   const Args& a;
-  const bool shares;
+  const bool shares, halves;
   int step_there, step_back;        // turns: to the next unit
   int b;                            // request
   int unit;                         // shares: as in Share; turns: counted from request `base`'s first
-  int64_t left;                     // turns: 1 as long as there are any
+  int64_t left;                     // shares: cost, this unit's included; turns: 1 as long as there are any
+  int off, spent, rest;             // shares: cost of the unit that is the shares' before, this one's, those' behind
   int step, count, all_steps;       // the unit's steps: first, how many, of all
   int tile, copy;
-  Request r;
-  Request mine;                     // turns: the lane's, base + lane
+  Request<Shape> r;
+  Request<Shape> mine;              // turns: the lane's, base + lane
   int base, in;                     // units of the requests from base to the lane's, its own included
-  __device__ __forceinline__ Walk(const Args& args, const Share& s, bool by_shares, int worker, int of)
-      : a(args), shares(by_shares), step_there(2 * (of - 1 - worker) + 1), step_back(2 * worker + 1), b(by_shares ? s.b : -1), unit(by_shares ? s.unit : worker), left(by_shares ? s.left : 1),
-        step(by_shares ? s.step : 0), base(0) {
+  __device__ __forceinline__ Walk(const Args& args, const Share& s, bool by_shares, bool halve, int worker, int of)
+      : a(args), shares(by_shares), halves(by_shares ? s.halves != 0 : halve), step_there(2 * (of - 1 - worker) + 1), step_back(2 * worker + 1), b(by_shares ? s.b : -1), unit(by_shares ? s.unit : worker), left(by_shares ? s.left : 1),
+        off(by_shares ? s.off : 0), base(0) {
     if (shares) {
-      if (left > 0) r = a.request(b);
+      if (left > 0) r = a.request(b, halves);
     } else {
       fetch();
     }
@@ -153,20 +239,24 @@ struct Walk {
   }
   __device__ __forceinline__ bool more() const { return left > 0; }
   __device__ __forceinline__ bool whole() const { return count == all_steps; }
+  __device__ __forceinline__ bool half() const { return tile == r.half; }
   __device__ __forceinline__ void next() {
     if (shares) {
-      left -= count, ++unit;
+      left -= spent, ++unit, off = 0;
     } else {
       const int x = step_there;
       unit += x, step_there = step_back, step_back = x;
     }
-    step = 0;
     find();
+  }
+  // Parts of a unit whose first steps are this share's: every share behind it that has the begin of a step has one.
+  __device__ __forceinline__ int parts(int per) const {
+    return 1 + (max(rest - ((half() ? r.s.half_cost : r.s.cost) - 1), 0) + per - 1) / per;
   }
   __device__ __forceinline__ void fetch() {
     const int lane = threadIdx.x & 31;
     in = 0;
-    if (base + lane < a.requests) mine = a.request(base + lane), in = mine.units();
+    if (base + lane < a.requests) mine = a.request(base + lane, halves), in = mine.units();
 #pragma unroll
     for (int o = 1; o < 32; o <<= 1) {
       const int x = __shfl_up_sync(0xffffffffu, in, o);
@@ -176,14 +266,26 @@ struct Walk {
   __device__ __forceinline__ void find() {
     if (left <= 0) return;
     if (shares) {
-      while (unit >= r.units()) {
-        if (++b >= a.requests) {
-          left = 0;
-          return;
+      for (;; left -= spent, ++unit, off = 0) {
+        if (left <= 0) return;
+        while (unit >= r.units()) {
+          if (++b >= a.requests) {
+            left = 0;
+            return;
+          }
+          r = a.request(b, halves), unit = 0;
         }
-        r = a.request(b), unit = 0;
+        tile = unit / r.s.copies, copy = unit - tile * r.s.copies;
+        all_steps = r.steps(tile);
+        rest = all_steps * (half() ? r.s.half_cost : r.s.cost) + r.s.unit_cost - off;
+        spent = static_cast<int>(min(static_cast<int64_t>(rest), left)), rest -= spent;
+        auto begun = [&](int x) {   // steps that begin before x; what the unit itself takes comes first
+          x = max(x - r.s.unit_cost, 0);
+          return half() ? (x + r.s.half_cost - 1) / r.s.half_cost : (x + r.s.cost - 1) / r.s.cost;
+        };
+        step = begun(off), count = begun(off + spent) - step;
+        if (count > 0) return;
       }
-      return take(unit);
     }
     for (;;) {
       const uint32_t behind = __ballot_sync(0xffffffffu, in > unit);
@@ -194,8 +296,12 @@ struct Walk {
         r.q0 = __shfl_sync(0xffffffffu, mine.q0, at), r.n = __shfl_sync(0xffffffffu, mine.n, at);
         r.k0 = __shfl_sync(0xffffffffu, mine.k0, at), r.L = __shfl_sync(0xffffffffu, mine.L, at), r.hi = __shfl_sync(0xffffffffu, mine.hi, at);
         r.s = a.shape();
-        r.settle();
-        return take(unit - (at > 0 ? before : 0));
+        r.settle(halves);
+        const int of_request = unit - (at > 0 ? before : 0);
+        tile = of_request / r.s.copies, copy = of_request - tile * r.s.copies;
+        tile = r.tiles - 1 - tile;
+        step = 0, count = all_steps = r.steps(tile);
+        return;
       }
       unit -= __shfl_sync(0xffffffffu, in, 31);
       base += 32;
@@ -203,12 +309,6 @@ struct Walk {
       fetch();
     }
     left = 0;
-  }
-  __device__ __forceinline__ void take(int of_request) {
-    tile = of_request / r.s.copies, copy = of_request - tile * r.s.copies;
-    if (!shares) tile = r.tiles - 1 - tile;
-    all_steps = r.steps(tile);
-    count = shares ? static_cast<int>(min(static_cast<int64_t>(all_steps - step), left)) : all_steps;
   }
 };
 
