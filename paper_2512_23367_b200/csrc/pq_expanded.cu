@@ -71,7 +71,7 @@ struct ExpandedArgs {
 
 // A CTA's units.
 struct ExpandedWalk : Walk<ExpandedArgs> {
-  __device__ __forceinline__ ExpandedWalk(const ExpandedArgs& args, const Share& s, bool by_shares) : Walk<ExpandedArgs>(args, s, by_shares, true, blockIdx.x, gridDim.x) {}
+  __device__ __forceinline__ ExpandedWalk(const ExpandedArgs& args, const ShareRoom<Shape>& room, bool by_shares) : Walk<ExpandedArgs>(args, room, by_shares, true, blockIdx.x, gridDim.x) {}
 };
 // The key tiles of a unit, or of the part of one that a CTA has.
 struct Part {
@@ -104,7 +104,7 @@ expanded_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant
   __shared__ __align__(8) uint64_t bars[16];
   __shared__ uint32_t s_tmem;
   __shared__ volatile int s_abort;
-  __shared__ ShareRoom s_share;
+  __shared__ ShareRoom<ExpandedShape> s_share;
   __shared__ float s_swap[2 * kTile];
   __shared__ float2 s_ml[kTile];
 
@@ -142,7 +142,7 @@ expanded_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant
     if (warp == kLoadK) {
       // ------------------------------------------------------------------ queries and keys
       bool ok = true;
-      for (ExpandedWalk w(a, s_share.share, shares); ok && w.more(); w.next()) {
+      for (ExpandedWalk w(a, s_share, shares); ok && w.more(); w.next()) {
         const Part part(w);
         if (units > 0 && !(ok = warp_wait(bar_qfree, (units - 1) & 1, wc))) break;
         if (lane == 0) mbar_arrive_expect_tx(bar_q, part.two ? 2 * kQueryBytes : kQueryBytes);
@@ -167,7 +167,7 @@ expanded_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant
     } else if (warp == kLoadV) {
       // ------------------------------------------------------------------ values
       bool ok = true;
-      for (ExpandedWalk w(a, s_share.share, shares); ok && w.more(); w.next()) {
+      for (ExpandedWalk w(a, s_share, shares); ok && w.more(); w.next()) {
         const Part part(w);
         for (int i = 0; i < w.count; ++i) {
           const uint32_t st = issued & 1, dst = ring_v + st * kValueBytes;
@@ -228,7 +228,7 @@ expanded_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant
       };
       constexpr std::integral_constant<int, 0> k0{};
       constexpr std::integral_constant<int, 1> k1{};
-      for (ExpandedWalk w(a, s_share.share, shares); w.more(); w.next()) {
+      for (ExpandedWalk w(a, s_share, shares); w.more(); w.next()) {
         const Part part(w);
         live = live && warp_wait(bar_q, seg & 1, wc);
         auto sums_free = [&](int t) {   // the sums of the unit before have been read
@@ -262,7 +262,7 @@ expanded_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant
       // ------------------------------------------------------------------ watcher: waits for the operand tiles a step ahead
       bool ok = true;
       uint32_t g = 0;
-      for (ExpandedWalk w(a, s_share.share, shares); w.more(); w.next()) {
+      for (ExpandedWalk w(a, s_share, shares); w.more(); w.next()) {
         const Part part(w);
         for (int u = 0; u < part.N + part.lag; ++u) {
 #pragma unroll
@@ -302,7 +302,7 @@ expanded_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant
     uint32_t n = 0;                                  // the accumulator's steps so far
     int4 join = make_int4(0, 0, 0, 0);
     bool ok = true;
-    for (ExpandedWalk w(a, s_share.share, shares); w.more();) {
+    for (ExpandedWalk w(a, s_share, shares); w.more();) {
       const Part part(w);
       const bool two = part.two;
       const int tok = (two ? acc * kTile : 0) + r;   // of the unit
@@ -402,7 +402,7 @@ expanded_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant
       const int64_t row = static_cast<int64_t>(w.r.q0) + w.tile * kUnit + tok;
       const bool writes = tok < part.toks && row >= 0 && row < a.tokens;
       __half* to = a.out + (row * a.heads + w.copy) * kValue + half * (kValue / 2);
-      if (!whole && begins) join = make_int4(w.r.q0 + w.tile * kUnit, part.toks, w.copy, w.parts(s_share.share.per));
+      if (!whole && begins) join = make_int4(w.r.q0 + w.tile * kUnit, part.toks, w.copy, w.parts(s_share.per));
       w.next();   // (the next request's lengths are on the way while the last product is waited for)
       if (mine > 0) ok = ok && warp_wait(bar_o + 8 * acc, (n - 1) & 1, wc);
       tc_fence_after_sync();

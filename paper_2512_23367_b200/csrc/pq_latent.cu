@@ -80,8 +80,8 @@ struct LatentArgs {
 
 // A CTA's units, with the 64 rows of a unit that are its own.
 struct LatentWalk : Walk<LatentArgs> {
-  __device__ __forceinline__ LatentWalk(const LatentArgs& args, const Share& s, bool by_shares)
-      : Walk<LatentArgs>(args, s, by_shares, false, args.paired ? blockIdx.x >> 1 : blockIdx.x, args.paired ? gridDim.x >> 1 : gridDim.x) {}
+  __device__ __forceinline__ LatentWalk(const LatentArgs& args, const ShareRoom<Shape>& room, bool by_shares)
+      : Walk<LatentArgs>(args, room, by_shares, false, args.paired ? blockIdx.x >> 1 : blockIdx.x, args.paired ? gridDim.x >> 1 : gridDim.x) {}
   __device__ __forceinline__ int second() const { return a.paired ? blockIdx.x & 1 : 0; }
   __device__ __forceinline__ int row0() const { return tile * r.s.rows + (half() ? 0 : second() * kRows); }
   __device__ __forceinline__ int rows() const { return max(min(static_cast<int>(r.all) - row0(), kRows), 0); }
@@ -159,7 +159,7 @@ latent_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__
   __shared__ __align__(8) uint64_t bars[2 * C::kStages * C::kGroups + 8];
   __shared__ uint32_t s_tmem;
   __shared__ volatile int s_abort;
-  __shared__ ShareRoom s_share;
+  __shared__ ShareRoom<LatentShape> s_share;
   __shared__ volatile uint32_t s_landed;   // steps
   __shared__ float s_swap[4][kRows];
 
@@ -203,7 +203,7 @@ latent_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__
     auto wait_free = [&](int g) {
       if (ok && filled >= C::kStages) ok = warp_wait(bar_free + 8 * ((filled % C::kStages) * C::kGroups + g), ((filled / C::kStages) & 1) ^ 1, wc);
     };
-    for (LatentWalk w(a, s_share.share, shares); ok && w.more(); w.next()) {
+    for (LatentWalk w(a, s_share, shares); ok && w.more(); w.next()) {
       if (w.rows() == 0) continue;
       const int* trow = a.table + static_cast<int64_t>(w.b) * a.width;
       int id = -1, off = 0;
@@ -266,7 +266,7 @@ latent_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__
     const uint32_t q_lo = desc_k(sq), k_lo0 = desc_k(ring), v_lo0 = desc_mn(ring, kAtom), r_lo = desc_k(rope), p_lo = desc_k(weights), t_q = tmem + C::kColQ;
     uint32_t n = 0, seg = 0;   // stages, units before
     bool on = true;
-    for (LatentWalk w(a, s_share.share, shares); w.more(); w.next()) {
+    for (LatentWalk w(a, s_share, shares); w.more(); w.next()) {
       if (w.rows() == 0) continue;
       on = on && warp_wait(bar_q, seg & 1, wc);
       if (leader && on) {   // the queries have been taken out of their stage
@@ -328,7 +328,7 @@ latent_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__
     // -------------------------------------------------------------------- watcher: waits for the operands a step ahead
     bool ok = true;
     uint32_t u = 0, n = 0;
-    for (LatentWalk w(a, s_share.share, shares); w.more(); w.next()) {
+    for (LatentWalk w(a, s_share, shares); w.more(); w.next()) {
       if (w.rows() == 0) continue;
       ++n;   // the queries' stage is the softmax threads'
       for (int i = 0; i < w.count; ++i, ++u, ++n) {
@@ -360,7 +360,7 @@ latent_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__
     const int tokens = kKeys / 2, first = static_cast<int>(blockIdx.x & 1) * tokens;
     uint32_t n = 0;
     bool on = a.paired != 0;
-    for (LatentWalk w(a, s_share.share, shares); on && w.more(); w.next()) {
+    for (LatentWalk w(a, s_share, shares); on && w.more(); w.next()) {
       if (w.rows() == 0) continue;
       const int* trow = a.table + static_cast<int64_t>(w.b) * a.width;
       for (int i = 0; on && i < w.count; ++i, ++n) {
@@ -394,7 +394,7 @@ latent_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__
     int4 join = make_int4(0, 0, 0, 0);
     bool ok = true;
     // A unit's queries are taken, and its first S computed, before the sums of the unit before go out.
-    LatentWalk w(a, s_share.share, shares);
+    LatentWalk w(a, s_share, shares);
     bool begins = false, whole = false, there = false, open = false;   // of the unit before
     float m = 0.0f, l = 0.0f;
     int64_t at = 0;   // row of the output
@@ -544,7 +544,7 @@ latent_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__
       if (!whole && begins) {
         const int64_t first = at - r;
         join = make_int4(static_cast<int>(first & 0xffffffff), static_cast<int>(first >> 32), rows,
-                         w.parts(s_share.share.per) * (w.half() ? -2 : 1));
+                         w.parts(s_share.per) * (w.half() ? -2 : 1));
       }
       w.next();
     }

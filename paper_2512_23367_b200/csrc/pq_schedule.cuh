@@ -98,25 +98,58 @@ struct Request {
   }
 };
 
-// Shares: `left` of cost from `off` of unit `unit` of request `b` on; `per` of a whole share.
-struct Share {
-  int b, unit, off, per;
-  int halves;
-  int64_t left, at;
+// A unit of a CTA, or its part of one.
+template <class Shape>
+struct Unit {
+  int b;                            // request
+  int unit;                         // shares: of the request; turns: counted from request `base`'s first
+  int64_t left;                     // shares: cost, this unit's included; turns: 1 as long as there are any
+  int off, spent, rest;             // shares: cost of the unit that is the shares' before, this one's, those' behind
+  int step, count, all_steps;       // the unit's steps: first, how many, of all
+  int tile, copy;
+  Request<Shape> r;
+  __device__ __forceinline__ bool half() const { return tile == r.half; }
+  // Shares: the first unit from `unit` of request `b` on that has the begin of a step in this share (which ends inside the last one).
+  template <class Args>
+  __device__ __forceinline__ void find(const Args& a, bool halves) {
+    for (;; left -= spent, ++unit, off = 0) {
+      if (left <= 0) return;
+      while (unit >= r.units()) {
+        if (++b >= a.requests) {
+          left = 0;
+          return;
+        }
+        r = a.request(b, halves), unit = 0;
+      }
+      tile = unit / r.s.copies, copy = unit - tile * r.s.copies;
+      all_steps = r.steps(tile);
+      rest = all_steps * (half() ? r.s.half_cost : r.s.cost) + r.s.unit_cost - off;
+      spent = static_cast<int>(min(static_cast<int64_t>(rest), left)), rest -= spent;
+      auto begun = [&](int x) {   // steps that begin before x; what the unit itself takes comes first
+        x = max(x - r.s.unit_cost, 0);
+        return half() ? (x + r.s.half_cost - 1) / r.s.half_cost : (x + r.s.cost - 1) / r.s.cost;
+      };
+      step = begun(off), count = begun(off + spent) - step;
+      if (count > 0) return;
+    }
+  }
 };
+
 // Halves: in kHalvesCut only where none of them fits a share, so that all of them are cut.
 enum Halves { kHalvesCut, kHalvesAlways };
+template <class Shape>
 struct ShareRoom {   // shared memory
-  Share share;
-  int64_t sums[2][32];
-  int shortest, longest, units;   // set by the kernel to the largest int, 0, 0
-  __device__ __forceinline__ void clear() { shortest = 0x7fffffff, longest = units = 0; }
+  Unit<Shape> first;
+  int per, halves;   // cost of a share; whether halves are told apart
+  int64_t sums[2][32], at;
+  int shortest, longest, units;
+  __device__ __forceinline__ void clear() { shortest = 0x7fffffff, longest = units = 0; }   // before find_share
 };
 
 // By the whole block; false: whole units by turns take no longer.  They are not cut, which costs about two units' begins and ends,
 // one for the other part and one for the joining (35 requests of two units each, of eight steps, on 74 pairs of CTAs: 33 us; 43 in shares).
 template <int kThreads, Halves kHalves, class Args>
-__device__ __forceinline__ bool find_share(const Args& a, int worker, int workers, int least, ShareRoom& room) {
+__device__ __forceinline__ bool find_share(const Args& a, int worker, int workers, int least, ShareRoom<typename Args::Shape>& room) {
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   const int each = (a.requests + kThreads - 1) / kThreads;
   const int b0 = min(tid * each, a.requests), b1 = min(b0 + each, a.requests);
@@ -158,7 +191,7 @@ __device__ __forceinline__ bool find_share(const Args& a, int worker, int worker
     if (kHalves == kHalvesCut) atomicMin(&room.shortest, shortest);
     atomicMax(&room.longest, longest), atomicAdd(&room.units, units);
   }
-  if (tid == 0) room.share.left = 0, room.share.b = a.requests, room.share.unit = 0, room.share.off = 0;
+  if (tid == 0) room.first.left = 0;
   __syncthreads();
   int64_t off[2] = {in[0] - mine[0], in[1] - mine[1]}, all[2] = {0, 0};
 #pragma unroll
@@ -190,56 +223,55 @@ __device__ __forceinline__ bool find_share(const Args& a, int worker, int worker
       if (at < x) break;
       at -= x;
     }
-    room.share.b = b, room.share.at = at, room.share.left = min(per, all_h - first);
+    room.first.b = b, room.at = at, room.first.left = min(per, all_h - first);
   }
-  if (tid == 0) room.share.per = static_cast<int>(min(per, static_cast<int64_t>(0x7fffffff))), room.share.halves = h;
+  if (tid == 0) room.per = static_cast<int>(min(per, static_cast<int64_t>(0x7fffffff))), room.halves = h;
   __syncthreads();
-  if (warp == 0 && room.share.left > 0) {   // the last unit of the request that begins at or before that: 32 at a time
-    const auto r = a.request(room.share.b, h != 0);
-    const int64_t at = room.share.at;
-    int lo = 0, n = r.units();
+  if (warp == 0 && room.first.left > 0) {   // the last unit of the request that begins at or before that: 32 at a time
+    Unit<typename Args::Shape> u;
+    u.b = room.first.b, u.left = room.first.left, u.r = a.request(u.b, h != 0), u.unit = 0;
+    const int64_t at = room.at;
+    int n = u.r.units();
     while (n > 1) {
       const int stride = (n + 31) / 32, probe = lane * stride;
-      const uint32_t yes = __ballot_sync(0xffffffffu, probe < n && r.before(lo + probe) <= at);   // of lane 0 always
+      const uint32_t yes = __ballot_sync(0xffffffffu, probe < n && u.r.before(u.unit + probe) <= at);   // of lane 0 always
       const int k = 31 - __clz(yes);
-      lo += k * stride, n = min(stride, n - k * stride);
+      u.unit += k * stride, n = min(stride, n - k * stride);
     }
-    if (lane == 0) room.share.unit = lo, room.share.off = static_cast<int>(at - r.before(lo));
+    u.off = static_cast<int>(at - u.r.before(u.unit));
+    u.find(a, h != 0);
+    __syncwarp();
+    if (lane == 0) room.first = u;
   }
   __syncthreads();
   return true;
 }
 
-// Walks the units of one CTA, as every warp of it does for itself; all lanes together.  By turns, a lane keeps one of 32
-// requests, so that going on to the next unit reads no memory (it took 3000 cycles between a unit's end and the next one's begin).
+// Walks the units of one CTA, as every warp of it does for itself; all lanes together.  The first one of a share is found once for
+// all warps (each by itself, from code of its own, took up to 5000 cycles).  By turns, a lane keeps one of 32 requests, so that going
+// on to the next unit reads no memory (it took 3000 cycles between a unit's end and the next one's begin).
 template <class Args>
-struct Walk {
+struct Walk : Unit<typename Args::Shape> {
   using Shape = typename Args::Shape;
+  using Base = Unit<Shape>;
+  using Base::b, Base::unit, Base::left, Base::off, Base::spent, Base::rest, Base::step, Base::count, Base::all_steps, Base::tile, Base::copy, Base::r, Base::half;
   const Args& a;
   const bool shares, halves;
   int step_there, step_back;        // turns: to the next unit
-  int b;                            // request
-  int unit;                         // shares: as in Share; turns: counted from request `base`'s first
-  int64_t left;                     // shares: cost, this unit's included; turns: 1 as long as there are any
-  int off, spent, rest;             // shares: cost of the unit that is the shares' before, this one's, those' behind
-  int step, count, all_steps;       // the unit's steps: first, how many, of all
-  int tile, copy;
-  Request<Shape> r;
   Request<Shape> mine;              // turns: the lane's, base + lane
   int base, in;                     // units of the requests from base to the lane's, its own included
-  __device__ __forceinline__ Walk(const Args& args, const Share& s, bool by_shares, bool halve, int worker, int of)
-      : a(args), shares(by_shares), halves(by_shares ? s.halves != 0 : halve), step_there(2 * (of - 1 - worker) + 1), step_back(2 * worker + 1), b(by_shares ? s.b : -1), unit(by_shares ? s.unit : worker), left(by_shares ? s.left : 1),
-        off(by_shares ? s.off : 0), base(0) {
+  __device__ __forceinline__ Walk(const Args& args, const ShareRoom<Shape>& room, bool by_shares, bool halve, int worker, int of)
+      : a(args), shares(by_shares), halves(by_shares ? room.halves != 0 : halve) {
     if (shares) {
-      if (left > 0) r = a.request(b, halves);
+      static_cast<Base&>(*this) = room.first;
     } else {
+      step_there = 2 * (of - 1 - worker) + 1, step_back = 2 * worker + 1, unit = worker, left = 1, base = 0;
       fetch();
+      find();
     }
-    find();
   }
   __device__ __forceinline__ bool more() const { return left > 0; }
   __device__ __forceinline__ bool whole() const { return count == all_steps; }
-  __device__ __forceinline__ bool half() const { return tile == r.half; }
   __device__ __forceinline__ void next() {
     if (shares) {
       left -= spent, ++unit, off = 0;
@@ -265,28 +297,7 @@ struct Walk {
   }
   __device__ __forceinline__ void find() {
     if (left <= 0) return;
-    if (shares) {
-      for (;; left -= spent, ++unit, off = 0) {
-        if (left <= 0) return;
-        while (unit >= r.units()) {
-          if (++b >= a.requests) {
-            left = 0;
-            return;
-          }
-          r = a.request(b, halves), unit = 0;
-        }
-        tile = unit / r.s.copies, copy = unit - tile * r.s.copies;
-        all_steps = r.steps(tile);
-        rest = all_steps * (half() ? r.s.half_cost : r.s.cost) + r.s.unit_cost - off;
-        spent = static_cast<int>(min(static_cast<int64_t>(rest), left)), rest -= spent;
-        auto begun = [&](int x) {   // steps that begin before x; what the unit itself takes comes first
-          x = max(x - r.s.unit_cost, 0);
-          return half() ? (x + r.s.half_cost - 1) / r.s.half_cost : (x + r.s.cost - 1) / r.s.cost;
-        };
-        step = begun(off), count = begun(off + spent) - step;
-        if (count > 0) return;
-      }
-    }
+    if (shares) return Base::find(a, halves);
     for (;;) {
       const uint32_t behind = __ballot_sync(0xffffffffu, in > unit);
       if (behind) {
