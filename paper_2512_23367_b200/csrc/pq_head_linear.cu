@@ -28,7 +28,8 @@ struct HeadArgs {
 // Y^T = W X^T: a CTA takes 128 outputs of one head as the MMA's rows and up to 128 tokens as its columns, so that one to
 // sixteen tokens cost no more tensor time than the weights' way in takes.  Bound by that way for the token counts that the
 // absorbed form serves: all of a CTA's panels are requested at once, the weights' before the wait on the kernel
-// before, and multiplied as they land.  Results pass through shared memory to leave as whole rows of 256 bytes.
+// before, and multiplied as they land: 128 heads of 128 x 512 and 64 tokens 9.3 us by itself, 7.1 after another kernel, where
+// the bytes take 4.2; 32 heads of 512 x 128 and one token 4.9.  Results pass through shared memory to leave as whole rows of 256 bytes.
 __global__ void __launch_bounds__(kThreads) head_linear_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constant__ CUtensorMap map_x,
                                                               const HeadArgs a) {
   extern __shared__ uint8_t smem_raw[];

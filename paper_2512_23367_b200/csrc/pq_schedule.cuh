@@ -328,7 +328,7 @@ struct Walk : Unit<typename Args::Shape> {
 // its row has them (nullptr: there is no such row).  All of four parts is loaded at once: L2 latency bounds it.
 // kGroups > 1: so many threads of a block share a row's parts, in blocks of kGroups x kRows threads.  One request of 52000 tokens
 // in 148 parts: 49 us with one group, 36 with four; 64 requests in two or three parts each, where four times the blocks
-// come in waves: 141 and 155.
+// come in waves: 141 and 155 (with shares of equal steps).
 // many_parts: whether a unit may be in more than 16, from bounds of the units and of the steps of one.
 inline bool many_parts(int64_t units, int workers, int64_t steps, int least) {
   return units * 16 < workers && steps > 16 * least;
