@@ -40,3 +40,26 @@ def test_lengths_of_all_sizes_expanded(seed):
     new = [int(x) for x in rng.integers(0, 600, n)]
     total = [int(x) for x in np.exp(rng.uniform(0, np.log(4000), n))]
     check_expanded(ref.expanded_inputs(int(rng.choice([1, 3, 8])), new, total, seed=seed, gap=1))
+
+
+@pytest.mark.parametrize("heads", [1, 40])
+def test_more_requests_than_threads_absorbed(heads):
+    """Runs of several requests per thread of the schedule; one long request among short and empty ones."""
+    rng = np.random.default_rng(heads)
+    new = [int(x) for x in rng.integers(0, 4, 1500)]
+    total = [int(x) for x in rng.integers(0, 90, 1500)]
+    total[777], new[777] = 6000, 3
+    check_latent(ref.latent_inputs(heads, 256, 16, new, total, seed=1))
+
+
+def test_more_requests_than_threads_expanded():
+    rng = np.random.default_rng(2)
+    new = [int(x) for x in rng.integers(0, 3, 1500)]
+    total = [int(x) for x in rng.integers(0, 60, 1500)]
+    total[1201], new[1201] = 5000, 300
+    check_expanded(ref.expanded_inputs(2, new, total, seed=1))
+
+
+def test_the_most_requests():
+    """4096 of one token each: the limit of a call."""
+    check_latent(ref.latent_inputs(2, 256, 16, [1] * 4096, [1 + 7 * i % 40 for i in range(4096)], seed=1))
