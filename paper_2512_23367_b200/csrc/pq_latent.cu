@@ -278,20 +278,24 @@ latent_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__
       ++n;
       for (int i = 0; i <= w.count; ++i) {
         if (i > 0) named_bar_sync(kBarRead, kSoft + 32);   // S(u - 1) is in registers
-        if (i < w.count) {   // S(u) = Q C^T: the latent vectors, then the rotary keys, whose room is single
-          on = tile_landed(kBarTile, true) && on;
-          tc_fence_after_sync();
-          if (leader && on) {
-            const uint32_t kl = k_lo0 + (n % C::kStages) * kStage16;
-            umma_ws_ts<0>(tmem_s, t_q, kl, id_s);
+        if (i < w.count) {   // S(u) = Q C^T: the latent vectors, a group as it lands, then the rotary keys, whose room is single
 #pragma unroll
-            for (int k = 1; k < 4 * C::kValuePanels; ++k) {
-              const uint32_t b = kl + (k / 16) * (4 * kPanel16) + (k / 4 % 4) * (kAtom / 16) + (k % 4) * 2;
-              if (k / 4 < C::kHeld) umma_ws_ts<1>(tmem_s, t_q + 8 * k, b, id_s);
-              else umma_ws<1, kTokenHi>(tmem_s, q_lo + (k / 4 - C::kHeld) * kPanel16 + (k % 4) * 2, b, id_s);
+          for (int g = 0; g < C::kGroups; ++g) {
+            on = tile_landed(kBarTile, true) && on;
+            tc_fence_after_sync();
+            if (leader && on) {
+              const uint32_t kl = k_lo0 + (n % C::kStages) * kStage16 + g * (4 * kPanel16);
+              if (g == 0) umma_ws_ts<0>(tmem_s, t_q, kl, id_s);
+#pragma unroll
+              for (int j = g == 0 ? 1 : 0; j < 16; ++j) {
+                const uint32_t b = kl + (j / 4) * (kAtom / 16) + (j % 4) * 2;
+                const int panel = 4 * g + j / 4;
+                if (panel < C::kHeld) umma_ws_ts<1>(tmem_s, t_q + 8 * (16 * g + j), b, id_s);
+                else umma_ws<1, kTokenHi>(tmem_s, q_lo + (panel - C::kHeld) * kPanel16 + (j % 4) * 2, b, id_s);
+              }
             }
+            __syncwarp();
           }
-          __syncwarp();
           on = tile_landed(kBarTile, true) && on;
           tc_fence_after_sync();
           if (leader && on) {
@@ -333,19 +337,21 @@ latent_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__
       if (w.rows() == 0) continue;
       ++n;   // the queries' stage is the softmax threads'
       for (int i = 0; i < w.count; ++i, ++u, ++n) {
-#pragma unroll
-        for (int g = 0; g < C::kGroups; ++g) ok = ok && warp_wait(bar_full + 8 * ((n % C::kStages) * C::kGroups + g), (n / C::kStages) & 1, wc);
         const int dead = max(w.r.hi - w.key0(i), 0);   // first token of the step that was never written
-        if (ok && dead < kKeys) {   // 0 x NaN is not 0: the weights of such tokens are, their vectors have to be
-          for (int j = lane; j < (kKeys - dead) * (kLatent / 8); j += 32) {
-            const int r = dead + j / (kLatent / 8), c = j % (kLatent / 8), panel = c >> 3;
-            const uint32_t at = ring + (n % C::kStages) * C::kStage + (panel >> 2) * (4 * kPanel) + (r >> 3) * kTokens8 + (panel & 3) * kAtom + (r & 7) * 128 + (c & 7) * 16;
-            asm volatile("st.shared.v4.u32 [%0], {%1, %1, %1, %1};" ::"r"(at), "r"(0) : "memory");
+#pragma unroll
+        for (int g = 0; g < C::kGroups; ++g) {
+          ok = ok && warp_wait(bar_full + 8 * ((n % C::kStages) * C::kGroups + g), (n / C::kStages) & 1, wc);
+          if (ok && dead < kKeys) {   // 0 x NaN is not 0: the weights of such tokens are, their vectors have to be
+            for (int j = lane; j < (kKeys - dead) * 32; j += 32) {
+              const int r = dead + (j >> 5), c = j & 31;
+              const uint32_t at = ring + (n % C::kStages) * C::kStage + g * (4 * kPanel) + (r >> 3) * kTokens8 + (c >> 3) * kAtom + (r & 7) * 128 + (c & 7) * 16;
+              asm volatile("st.shared.v4.u32 [%0], {%1, %1, %1, %1};" ::"r"(at), "r"(0) : "memory");
+            }
+            fence_proxy_async_smem();
+            __syncwarp();
           }
-          fence_proxy_async_smem();
-          __syncwarp();
+          tile_landed(kBarTile, ok);
         }
-        tile_landed(kBarTile, ok);
         if (lane == 0) s_landed = u + 1;
         ok = ok && warp_wait(bar_rope, u & 1, wc);
         tile_landed(kBarTile, ok);
