@@ -141,12 +141,13 @@ template <class Shape>
 struct ShareRoom {   // shared memory
   Unit<Shape> first;
   int per, halves;   // cost of a share; whether halves are told apart
-  int64_t sums[2][32], at;
-  int shortest, longest, units;
+  int64_t sums[2][32];
+  int shortest, longest, units, cut;
   __device__ __forceinline__ void clear() { shortest = 0x7fffffff, longest = units = 0; }   // before find_share
 };
 
-// By the whole block; false: whole units by turns take no longer.  They are not cut, which costs about two units' begins and ends,
+// By the whole block up to the sums over requests, then by one warp (all of them take turns issuing: 1000 to 2000 cycles more);
+// false: whole units by turns take no longer.  They are not cut, which costs about two units' begins and ends,
 // one for the other part and one for the joining (35 requests of two units each, of eight steps, on 74 pairs of CTAs: 33 us; 43 in shares).
 template <int kThreads, Halves kHalves, class Args>
 __device__ __forceinline__ bool find_share(const Args& a, int worker, int workers, int least, ShareRoom<typename Args::Shape>& room) {
@@ -175,15 +176,18 @@ __device__ __forceinline__ bool find_share(const Args& a, int worker, int worker
     mine[0] += t[0], mine[1] += t[1];
   }
   constexpr int kFirst = kHalves == kHalvesAlways ? 1 : 0;
-  int64_t in[2] = {mine[0], mine[1]};
-#pragma unroll
-  for (int h = kFirst; h < 2; ++h) {
+  auto inclusive = [&](int64_t v) {
 #pragma unroll
     for (int o = 1; o < 32; o <<= 1) {
-      const int64_t x = __shfl_up_sync(0xffffffffu, in[h], o);
-      if (lane >= o) in[h] += x;
+      const int64_t x = __shfl_up_sync(0xffffffffu, v, o);
+      if (lane >= o) v += x;
     }
-    if (lane == 31) room.sums[h][warp] = in[h];
+    return v;
+  };
+#pragma unroll
+  for (int h = kFirst; h < 2; ++h) {
+    const int64_t in = inclusive(mine[h]);
+    if (lane == 31) room.sums[h][warp] = in;
   }
   if (kHalves == kHalvesCut) shortest = __reduce_min_sync(0xffffffffu, shortest);
   longest = __reduce_max_sync(0xffffffffu, longest), units = __reduce_add_sync(0xffffffffu, units);
@@ -191,60 +195,66 @@ __device__ __forceinline__ bool find_share(const Args& a, int worker, int worker
     if (kHalves == kHalvesCut) atomicMin(&room.shortest, shortest);
     atomicMax(&room.longest, longest), atomicAdd(&room.units, units);
   }
-  if (tid == 0) room.first.left = 0;
   __syncthreads();
-  int64_t off[2] = {in[0] - mine[0], in[1] - mine[1]}, all[2] = {0, 0};
-#pragma unroll
-  for (int h = kFirst; h < 2; ++h) {
-#pragma unroll
-    for (int w = 0; w < kThreads / 32; ++w) {
-      const int64_t x = room.sums[h][w];
-      all[h] += x;
-      if (w < warp) off[h] += x;
+  if (warp == 0) {
+    auto per_of = [&](int64_t cost) {   // (a 64-bit division takes 700 cycles)
+      const uint64_t up = static_cast<uint64_t>(cost + workers - 1);
+      return max(static_cast<int64_t>(up >> 32 ? up / workers : static_cast<uint32_t>(up) / static_cast<uint32_t>(workers)), static_cast<int64_t>(least));
+    };
+    int h = 1;
+    int64_t of_warp = lane < kThreads / 32 ? room.sums[1][lane] : 0, in = inclusive(of_warp), all = __shfl_sync(0xffffffffu, in, 31), per = per_of(all);
+    if (kHalves == kHalvesCut && room.shortest <= per) {
+      h = 0, of_warp = lane < kThreads / 32 ? room.sums[0][lane] : 0, in = inclusive(of_warp), all = __shfl_sync(0xffffffffu, in, 31);
+      per = per_of(all);
     }
-  }
-  auto per_of = [&](int64_t cost) {   // (a 64-bit division takes 700 cycles)
-    const uint64_t up = static_cast<uint64_t>(cost + workers - 1);
-    return max(static_cast<int64_t>(up >> 32 ? up / workers : static_cast<uint32_t>(up) / static_cast<uint32_t>(workers)), static_cast<int64_t>(least));
-  };
-  int h = 1;
-  int64_t per = per_of(all[1]);
-  if (kHalves == kHalvesCut && room.shortest <= per) h = 0, per = per_of(all[0]);
-  if ((room.units + workers - 1) / workers * static_cast<int64_t>(room.longest) <= per + 2 * a.shape().unit_cost) return false;
-  const int64_t all_h = h ? all[1] : all[0], off_h = h ? off[1] : off[0], mine_h = h ? mine[1] : mine[0];
-  const int64_t first = per * worker;
-  if (first < all_h && first >= off_h && first < off_h + mine_h) {   // one thread's
-    int64_t at = first - off_h;
-    int b = b0;
-    for (; b < b1 - 1; ++b) {
-      int64_t t[2];
-      total(b, t);
-      const int64_t x = h ? t[1] : t[0];
-      if (at < x) break;
-      at -= x;
-    }
-    room.first.b = b, room.at = at, room.first.left = min(per, all_h - first);
-  }
-  if (tid == 0) room.per = static_cast<int>(min(per, static_cast<int64_t>(0x7fffffff))), room.halves = h;
-  __syncthreads();
-  if (warp == 0 && room.first.left > 0) {   // the last unit of the request that begins at or before that: 32 at a time
+    const bool cut = (room.units + workers - 1) / workers * static_cast<int64_t>(room.longest) > per + 2 * a.shape().unit_cost;
+    const int64_t first = per * worker;
     Unit<typename Args::Shape> u;
-    u.b = room.first.b, u.left = room.first.left, u.r = a.request(u.b, h != 0), u.unit = 0;
-    const int64_t at = room.at;
-    int n = u.r.units();
-    while (n > 1) {
-      const int stride = (n + 31) / 32, probe = lane * stride;
-      const uint32_t yes = __ballot_sync(0xffffffffu, probe < n && u.r.before(u.unit + probe) <= at);   // of lane 0 always
-      const int k = 31 - __clz(yes);
-      u.unit += k * stride, n = min(stride, n - k * stride);
+    u.left = cut ? max(min(per, all - first), static_cast<int64_t>(0)) : 0;
+    if (u.left > 0) {
+      // whose requests: a warp's, a thread's, one of them; then the last unit of it that begins at or before `first`, 32 at a time
+      const int w = __ffs(__ballot_sync(0xffffffffu, first < in)) - 1;
+      int64_t at = first - __shfl_sync(0xffffffffu, in - of_warp, w);
+      const int r0 = min((w * 32 + lane) * each, a.requests), r1 = min(r0 + each, a.requests);
+      int64_t of_lane = h ? mine[1] : mine[0];
+      if (w > 0) {
+        of_lane = 0;
+#pragma unroll 1
+        for (int b = r0; b < r1; ++b) {
+          int64_t t[2];
+          total(b, t);
+          of_lane += h ? t[1] : t[0];
+        }
+      }
+      in = inclusive(of_lane);
+      const int owner = __ffs(__ballot_sync(0xffffffffu, at < in)) - 1;
+      at -= in - of_lane;
+      u.b = r0;
+      if (lane == owner) {
+        for (; u.b < r1 - 1; ++u.b) {
+          int64_t t[2];
+          total(u.b, t);
+          const int64_t x = h ? t[1] : t[0];
+          if (at < x) break;
+          at -= x;
+        }
+      }
+      u.b = __shfl_sync(0xffffffffu, u.b, owner), at = __shfl_sync(0xffffffffu, at, owner);
+      u.r = a.request(u.b, h != 0), u.unit = 0;
+      int n = u.r.units();
+      while (n > 1) {
+        const int stride = (n + 31) / 32, probe = lane * stride;
+        const uint32_t yes = __ballot_sync(0xffffffffu, probe < n && u.r.before(u.unit + probe) <= at);   // of lane 0 always
+        const int k = 31 - __clz(yes);
+        u.unit += k * stride, n = min(stride, n - k * stride);
+      }
+      u.off = static_cast<int>(at - u.r.before(u.unit));
+      u.find(a, h != 0);
     }
-    u.off = static_cast<int>(at - u.r.before(u.unit));
-    u.find(a, h != 0);
-    __syncwarp();
-    if (lane == 0) room.first = u;
+    if (lane == 0) room.first = u, room.per = static_cast<int>(min(per, static_cast<int64_t>(0x7fffffff))), room.halves = h, room.cut = cut;
   }
   __syncthreads();
-  return true;
+  return room.cut != 0;
 }
 
 // Walks the units of one CTA, as every warp of it does for itself; all lanes together.  The first one of a share is found once for
