@@ -39,7 +39,8 @@ constexpr uint32_t kBarP = 1, kBarTile = 3, kBarPair = 4, kBarRead = 12, kBarSof
 struct ExpandedShape {
   static constexpr int rows = kUnit, heads = 1, keys = kKeys, half_keys = kKeys, halves = 1, cost = 8, half_cost = 5, unit_cost = 20;
   int copies;
-  __device__ __forceinline__ static uint64_t floors(uint64_t n, uint64_t b) { return floor_sum_of<kKeys, kUnit>(n, b); }
+  // (rows and keys are below 2^31)
+  __device__ __forceinline__ static uint64_t floors(uint64_t n, uint64_t b) { return floor_sum_of<kKeys, kUnit>(static_cast<uint32_t>(n), static_cast<uint32_t>(b)); }
 };
 struct ExpandedArgs {
   using Shape = ExpandedShape;

@@ -43,13 +43,13 @@ __device__ inline uint64_t floor_sum(uint64_t n, uint64_t m, uint64_t a, uint64_
 
 constexpr int kFewSteps = 6;   // of a unit at most: shares are not worth their joining
 
-// The same where a and m are constants: without a division but by them.
+// The same where a and m are constants and a n + b is below 2^32: without a division but by them.
 template <uint32_t m, uint32_t a>
-__device__ __forceinline__ uint64_t floor_sum_of(uint64_t n, uint64_t b) {
-  uint64_t sum = (n - 1) * n / 2 * (a / m) + n * (b / m);   // n >= 1
+__device__ __forceinline__ uint64_t floor_sum_of(uint32_t n, uint32_t b) {
+  uint64_t sum = static_cast<uint64_t>(n - 1) * n / 2 * (a / m) + static_cast<uint64_t>(n) * (b / m);   // n >= 1
   b %= m;
   if constexpr (a % m != 0) {
-    const uint64_t top = a % m * n + b;
+    const uint32_t top = a % m * n + b;
     if (top >= m) sum += floor_sum_of<a % m, m>(top / m, top % m);
   }
   return sum;
