@@ -84,11 +84,12 @@ __device__ __forceinline__ uint4 pack8(const float* x) {
 // (token, pair) into shared memory, for all heads; in FP32, as the products are.  FP16 results are rounded once; an INT8 key is
 // quantized from its FP32 values, so that it is rounded once, too.
 //
-// HBM bound beyond a few hundred tokens, latency below: 8192 tokens of 40 heads of 128, half of each turned, 29 us (5.8 TB/s);
-// one token 3.4.  With an INT8 cache by instructions, 61 % of the issue slots: 8192 tokens, 32 and 8 heads, 41 us where the bytes take
-// 28 (48 with one item per thread).
+// HBM bound beyond a few hundred tokens, latency below: 8192 tokens of 40 heads of 128, half of each turned, 27 us (6.2 TB/s);
+// one token 3.4.  With an INT8 cache by instructions, 61 % of the issue slots: 8192 tokens, 32 and 8 heads, 39 us where the bytes take
+// 28 (48 with one item per thread).  Five blocks an SM, 48 registers, of which the INT8 kernels
+// spill a few: with four and 64 registers the same calls took 2 to 3 us more, with six 4 to 9.
 template <Target kTarget, bool kHalf, int kItems>
-__global__ void __launch_bounds__(kThreads) rotary_kernel(const TurnArgs a) {
+__global__ void __launch_bounds__(kThreads, 5) rotary_kernel(const TurnArgs a) {
   extern __shared__ float s_cos[];
   grid_dep_launch();
   const int tid = threadIdx.x;
