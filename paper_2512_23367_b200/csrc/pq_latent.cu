@@ -146,8 +146,8 @@ constexpr uint32_t kBarRow = 1, kBarTile = 3, kBarRead = 4, kBarP = 5;
 //
 // Bound by HBM up to 64 rows a request: 72 KB a step take an SM's share of the bandwidth 3150 cycles, and steps come every
 // 3300.  Two CTAs that share their tokens have 1580 cycles of bandwidth a step and take 2080: the tensor cores wait for S to be
-// read and for P.  (64 requests of 128 heads and 1000 to 8200 tokens: 123 us and 9 for joining the parts, where their bytes take 63;
-// 7 requests of up to four tokens of 32 heads and 4000 to 30000 tokens: 57 and 10, where 26; 1000 tokens of 16 heads: 13 and 5.)  A
+// read and for P.  (64 requests of 128 heads and 1000 to 8200 tokens: 121 us and 9 for joining the parts, where their bytes take 63;
+// 7 requests of up to four tokens of 32 heads and 4000 to 30000 tokens: 55 and 10, where 26; 1000 tokens of 16 heads: 13 and 5.)  A
 // unit's begin and end take about 9000 cycles: queries, the first tokens, 128 KB of partial sums at 30 bytes a cycle.  Taken back for being slower: queries in shared memory and two steps of tokens (236 us for the 131), two
 // CTAs as a cluster that exchange halves of S (5300 cycles a step), MMAs over a pair of CTAs (2340).
 template <int kLatent>
