@@ -845,6 +845,8 @@ def _head_rows(x: torch.Tensor, heads: int | None, dim: int | None, what: str) -
         raise ValueError(f"{what}: expected [rows, {'heads' if heads is None else heads}, {'values' if dim is None else dim}] "
                          "with the values of a head contiguous")
     T, H, D = shape
+    if (H | D) >> 31:
+        _in_32_bits(**{f"{what}'s heads": H, f"{what}'s width": D})
     hs = stride[1] if H > 1 else D
     return T, H, D, (stride[0] if T > 1 else H * hs), hs
 

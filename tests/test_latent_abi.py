@@ -263,3 +263,10 @@ def test_empty_operands_have_rows_of_any_stride():
         binding._strided_rows(f16(64, 3).t(), 64, "x")
     with pytest.raises(ValueError, match="x: expected"):
         binding._head_rows(f16(128, 2, 3).permute(2, 1, 0), 2, 128, "x")
+
+
+def test_heads_and_widths_are_not_cut_to_32_bits():
+    """A view of 2^32 + 1 heads takes no memory, and 2^32 + 1 cut to 32 bits would be one head."""
+    x = torch.zeros(128, dtype=torch.float16).expand(1, 2**32 + 1, 128)
+    with pytest.raises(ValueError, match="x's heads: .* 32 bits"):
+        binding._head_rows(x, None, None, "x")
