@@ -19,7 +19,7 @@ constexpr int kKeys = 64;            // cached tokens of one step
 constexpr int kPanel = kKeys * 128;  // 64 rows of 64 values
 constexpr int kSoft = 256;           // softmax threads: four per row
 constexpr int kIssuer = 8, kLoader = 9, kWatcher = 10, kAhead = 11, kThreads = 384;   // warps
-constexpr int kDistance = 6;         // steps that tokens are brought into L2 ahead of their use
+constexpr int kDistance = 2;         // steps that tokens are brought into L2 ahead of their use
 constexpr int kLeastSteps = 2;       // of a CTA, so that its parts are worth joining
 
 template <int kLatent>
@@ -146,7 +146,7 @@ constexpr uint32_t kBarRow = 1, kBarTile = 3, kBarRead = 4, kBarP = 5;
 //
 // Bound by HBM up to 64 rows a request: 72 KB a step take an SM's share of the bandwidth 3150 cycles, and steps come every
 // 3300.  Two CTAs that share their tokens have 1580 cycles of bandwidth a step and take 2080: the tensor cores wait for S to be
-// read and for P.  (64 requests of 128 heads and 1000 to 8200 tokens: 121 us and 9 for joining the parts, where their bytes take 63;
+// read and for P.  (64 requests of 128 heads and 1000 to 8200 tokens: 117 us and 9 for joining the parts, where their bytes take 63;
 // 7 requests of up to four tokens of 32 heads and 4000 to 30000 tokens: 55 and 10, where 26; 1000 tokens of 16 heads: 13 and 5.)  A
 // unit's begin and end take about 9000 cycles: queries, the first tokens, 128 KB of partial sums at 30 bytes a cycle.  Taken back for being slower: queries in shared memory and two steps of tokens (236 us for the 131), two
 // CTAs as a cluster that exchange halves of S (5300 cycles a step), MMAs over a pair of CTAs (2340).
@@ -360,7 +360,7 @@ latent_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__
   } else if (warp == kAhead) {
     // -------------------------------------------------------------------- tokens into L2, kDistance steps ahead of their use,
     // where two CTAs share them.  There three steps of room are less than what memory's latency asks for at twice the rate
-    // (2550 cycles a step without, 2250 with); one CTA by itself is bound by memory, and slower with (87 thousand cycles for
+    // (64 ragged requests: 131 us without, 127 with two steps ahead, 133 with six, whose lines come too early); one CTA by itself is bound by memory, and slower with (87 thousand cycles for
     // 20 steps, 109 with).
     const char* data = static_cast<const char*>(a.c.data);
     constexpr int kLines = C::kPanels;   // of 128 bytes, per token
