@@ -60,9 +60,16 @@ __device__ __forceinline__ void tmem_ld_32x8(uint32_t taddr, uint32_t (&r)[8]) {
 }
 __device__ __forceinline__ void tmem_st_wait() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
 
-// A whole 32-byte sector by one thread: what a lane per row leaves of a warp's store.
+// 32 bytes by one thread: what a lane per row leaves of a warp's store.  The wide store writes a whole sector, but faults unless its
+// address is a multiple of 32, and a caller's output is one of 16 only: there two stores of 16 bytes.  The rows of a call's output
+// are multiples of 32 bytes apart, so that all of its stores go the same way.
 __device__ __forceinline__ void store_32_bytes(void* to, uint32_t a, uint32_t b, uint32_t c, uint32_t d, uint32_t e, uint32_t f, uint32_t g, uint32_t h) {
-  asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(to), "r"(a), "r"(b), "r"(c), "r"(d), "r"(e), "r"(f), "r"(g), "r"(h) : "memory");
+  if ((reinterpret_cast<uintptr_t>(to) & 16u) == 0) {
+    asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(to), "r"(a), "r"(b), "r"(c), "r"(d), "r"(e), "r"(f), "r"(g), "r"(h) : "memory");
+  } else {
+    static_cast<uint4*>(to)[0] = make_uint4(a, b, c, d);
+    static_cast<uint4*>(to)[1] = make_uint4(e, f, g, h);
+  }
 }
 __device__ __forceinline__ void named_bar_arrive(uint32_t id, uint32_t nthreads) {
   asm volatile("bar.arrive %0, %1;" ::"r"(id), "r"(nthreads) : "memory");
