@@ -74,7 +74,7 @@ __device__ __forceinline__ void store_32_bytes(void* to, uint32_t a, uint32_t b,
 __device__ __forceinline__ void named_bar_arrive(uint32_t id, uint32_t nthreads) {
   asm volatile("bar.arrive %0, %1;" ::"r"(id), "r"(nthreads) : "memory");
 }
-// Meets the other warps that share the barrier (of the pair: 64 threads); whether any of their threads says yes.
+// Meets the other warps that share the barrier (of a pair: 64 threads); whether any of their threads says yes.
 template <int kThreads = 64>
 __device__ __forceinline__ bool pair_any(uint32_t id, bool yes) {
   uint32_t r;

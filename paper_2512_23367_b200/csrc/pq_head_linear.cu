@@ -85,20 +85,21 @@ __global__ void __launch_bounds__(kThreads) head_linear_kernel(const __grid_cons
     __syncwarp();
   } else {
     grid_dep_wait();
-    const bool ok = __all_sync(0xffffffffu, mbar_wait(bar_done, 0, wc));
+    const bool done = __all_sync(0xffffffffu, mbar_wait(bar_done, 0, wc));
     tc_fence_after_sync();
-    if (ok) {
-      // 16 tokens at a time: a thread has one output of each; rows of 128 outputs in shared memory, where the weights were
-      uint16_t* room = reinterpret_cast<uint16_t*>(smem_raw + (sw - smem_u32(smem_raw)));
-      const int live = static_cast<int>(min(static_cast<int64_t>(a.batch), a.tokens - t0));
-      for (int c = 0; c < live; c += 16) {
-        uint32_t v[16];
-        tmem_ld_32x16(tmem + c + (static_cast<uint32_t>(warp) << 21), v);
-        tmem_ld_wait();
+    // 16 tokens at a time: a thread has one output of each; rows of 128 outputs in shared memory, where the weights were
+    uint16_t* room = reinterpret_cast<uint16_t*>(smem_raw + (sw - smem_u32(smem_raw)));
+    const int live = static_cast<int>(min(static_cast<int64_t>(a.batch), a.tokens - t0));
+    for (int c = 0; done && c < live; c += 16) {
+      uint32_t v[16];
+      tmem_ld_32x16(tmem + c + (static_cast<uint32_t>(warp) << 21), v);
+      tmem_ld_wait();
 #pragma unroll
-        for (int j = 0; j < 16; ++j) room[(c + j) * kOut + tid] = __half_as_ushort(__float2half_rn(__uint_as_float(v[j])));
-      }
-      named_bar_sync(1, 128);
+      for (int j = 0; j < 16; ++j) room[(c + j) * kOut + tid] = __half_as_ushort(__float2half_rn(__uint_as_float(v[j])));
+    }
+    // The four warps meet whatever their own waits came to (one may run out of polls where the next one's last poll succeeds), and
+    // store only if all have their outputs there.
+    if (!pair_any<128>(1, !done)) {
       for (int i = tid; i < live * (kOut / 8); i += 128) {
         const int t = i / (kOut / 8), c = i % (kOut / 8);
         reinterpret_cast<uint4*>(a.y + (t0 + t) * a.y_stride + head * a.y_head_stride + n0)[c] = reinterpret_cast<const uint4*>(room + t * kOut)[c];
