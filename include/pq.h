@@ -565,7 +565,7 @@ PQ_API int pq_latent_read(const pq_latent_cache* cache, const int64_t* slots, in
  *   x: head h of row t is K values at x + t * x_stride + h * x_head_stride;  w: dense [heads, N, K];
  *   y: N values at y + t * y_stride + h * y_head_stride
  *   K a multiple of 64 up to 512, N a multiple of 128 up to 1024, 1 <= heads <= 1024; strides as for pq_rotate, with K and
- *   N for the widths; y may not overlap x.  Weights are constants of the model, read ahead of the wait as in pq_gemm_w8a8.
+ *   N for the widths; y may not overlap x.  Unlike packed weights, w may be written by the operation right before the call.
  */
 PQ_API int pq_head_linear(const void* x_f16, int64_t x_stride, int64_t x_head_stride, const void* w_f16, int32_t heads, int64_t N,
                           int64_t K, int64_t tokens, void* y_f16, int64_t y_stride, int64_t y_head_stride, void* stream);

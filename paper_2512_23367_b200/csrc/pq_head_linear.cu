@@ -17,6 +17,7 @@ constexpr int kPanelK = 64;     // K of one panel
 constexpr int kMostPanels = 8;
 
 struct HeadArgs {
+  const __half* w;
   __half* y;
   int64_t y_stride, y_head_stride, tokens;
   int N, panels, batch;         // outputs of a head, K / 64, tokens of a CTA (a multiple of 16)
@@ -27,8 +28,11 @@ struct HeadArgs {
 
 // Y^T = W X^T: a CTA takes 128 outputs of one head as the MMA's rows and up to 128 tokens as its columns, so that one to
 // sixteen tokens cost no more tensor time than the weights' way in takes.  Bound by that way for the token counts that the
-// absorbed form serves: all of a CTA's panels are requested at once, the weights' before the wait on the kernel
-// before, and multiplied as they land: 128 heads of 128 x 512 and 64 tokens 9.3 us by itself, 7.1 after another kernel, where
+// absorbed form serves: all of a CTA's panels are requested at once, behind the wait on the kernel before, and multiplied as they
+// land; before it the weights are only brought into L2, which is right whoever writes them.  (The three launches of a decode step of
+// 32 tokens and 128 heads over 1000 cached ones, weights in no cache: 43.8 us; 45.0 without bringing them into L2; 42.3 with the weights
+// requested before the wait, which takes another operation between their writing and the call.)
+// 128 heads of 128 x 512 and 64 tokens 9.3 us by itself, 7.1 after another kernel, where
 // the bytes take 4.2; 32 heads of 512 x 128 and one token 4.9.  Results pass through shared memory to leave as whole rows of 256 bytes.
 __global__ void __launch_bounds__(kThreads) head_linear_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constant__ CUtensorMap map_x,
                                                               const HeadArgs a) {
@@ -60,12 +64,15 @@ __global__ void __launch_bounds__(kThreads) head_linear_kernel(const __grid_cons
   const WaitCtx wc{&s_abort, a.wait_limit};
 
   if (warp == kLoader) {
+    // The weights come from operations like any others, so that they are read behind the wait; into L2 they go before it.
+    const int row = head * a.N + n0;
+    if (t0 == 0 && lane < a.panels) l2_prefetch(a.w + static_cast<int64_t>(row) * (a.panels * kPanelK) + lane * (kOut * kPanelK), kOut * kPanelK * 2);
+    grid_dep_wait();
     if (lane < a.panels) {
       mbar_arrive_expect_tx(bar_full + 8 * lane, kOut * 128u + panel_x);
-      tma_load_2d(sw + lane * (kOut * 128u), &map_w, bar_full + 8 * lane, lane * kPanelK, head * a.N + n0);
+      tma_load_2d(sw + lane * (kOut * 128u), &map_w, bar_full + 8 * lane, lane * kPanelK, row);
+      tma_load_3d(sx + lane * panel_x, &map_x, bar_full + 8 * lane, lane * kPanelK, head, static_cast<int>(t0));
     }
-    grid_dep_wait();
-    if (lane < a.panels) tma_load_3d(sx + lane * panel_x, &map_x, bar_full + 8 * lane, lane * kPanelK, head, static_cast<int>(t0));
   } else if (warp == kIssuer) {
     const uint32_t leader = elect_one(), idesc = umma_idesc_f16(a.batch, false);
     const uint32_t w_lo = desc_k(sw), x_lo = desc_k(sx);
@@ -143,7 +150,7 @@ int pq_head_linear(const void* x_f16, int64_t x_stride, int64_t x_head_stride, c
   if (rc != PQ_OK) return rc;
   // tokens of a CTA: as many as there are, up to 128, or 64 where the weights' panels leave no more room
   const int64_t most = K > 256 ? 64 : 128, up = (tokens + 15) / 16 * 16;
-  HeadArgs a{static_cast<__half*>(y_f16), y_stride, y_head_stride, tokens, static_cast<int>(N), static_cast<int>(K / kPanelK),
+  HeadArgs a{static_cast<const __half*>(w_f16), static_cast<__half*>(y_f16), y_stride, y_head_stride, tokens, static_cast<int>(N), static_cast<int>(K / kPanelK),
              static_cast<int>(up < most ? up : most), 32, device_status_ptr(), wait_limit()};
   if (a.status == nullptr) return PQ_ERR_CUDA;
   while (a.cols < static_cast<uint32_t>(a.batch)) a.cols *= 2;

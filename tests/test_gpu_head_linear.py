@@ -41,3 +41,39 @@ def test_a_wait_that_runs_out_anywhere_is_reported_and_leaves_everything_usable(
             assert status == PQ_ERR_TIMEOUT if limit == WAIT_NONE else status in (0, PQ_ERR_TIMEOUT)
             assert status != 0 or torch.equal(got, good)
         assert torch.equal(pq.pq_head_linear(x, w), good) and pq.pq_device_status() == 0
+
+
+@pytest.mark.parametrize("captured", [False, True])
+@pytest.mark.parametrize("T,heads,K,N", [(1, 8, 128, 512), (64, 128, 512, 128), (16, 128, 128, 512)])
+def test_weights_may_be_written_by_the_launch_right_before(T, heads, K, N, captured):
+    """Matrices that a kernel of this library (which lets the next launch begin early; a rotation by nothing is a copy) or one of
+    torch's leaves, another one's at every call."""
+    x, w = _operands(T, heads, K, N)
+    sources = [w, _operands(T, heads, K, N, 1)[1], _operands(T, heads, K, N, 2)[1]]
+    good = [pq.pq_head_linear(x, s) for s in sources]
+    for g, s in zip(good, sources):
+        _check(g, x, s)
+    room, out = torch.zeros_like(w), [torch.zeros_like(good[0]) for _ in range(30)]
+    rotary, pos = pq.Rotary(16, device=DEV), torch.zeros(heads * N, dtype=torch.int32, device=DEV)
+
+    def run():
+        for i, y in enumerate(out):
+            if i % 5 == 4:
+                room.copy_(sources[i % 3])
+            else:
+                pq.pq_rotate(sources[i % 3].view(-1, 1, K), pos, rotary, out=room.view(-1, 1, K))
+            pq.pq_head_linear(x, room, out=y)
+
+    if captured:
+        run()
+        torch.cuda.synchronize()
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            run()
+        for y in out:
+            y.zero_()
+        graph.replay()
+    else:
+        torch.cuda.synchronize()
+        run()
+    assert all(torch.equal(y, good[i % 3]) for i, y in enumerate(out)) and pq.pq_device_status() == 0
