@@ -42,8 +42,8 @@ __global__ void __launch_bounds__(kThreads) head_linear_kernel(const __grid_cons
   __shared__ volatile int s_abort;
   const int tid = threadIdx.x, warp = __shfl_sync(0xffffffffu, tid >> 5, 0), lane = tid & 31;
   const uint32_t bar_full = smem_u32(bars), bar_done = bar_full + 8 * kMostPanels;
-  const int n0 = blockIdx.x * kOut, head = blockIdx.y;
-  const int64_t t0 = static_cast<int64_t>(blockIdx.z) * a.batch;
+  const int n0 = blockIdx.z * kOut, head = blockIdx.y;
+  const int64_t t0 = static_cast<int64_t>(blockIdx.x) * a.batch;   // only the grid's first dimension has room for any number of tokens
   if (tid == 0) {
     for (int i = 0; i < a.panels; ++i) mbar_init(bar_full + 8 * i, 1);
     mbar_init(bar_done, 1);
@@ -155,7 +155,6 @@ int pq_head_linear(const void* x_f16, int64_t x_stride, int64_t x_head_stride, c
   if (a.status == nullptr) return PQ_ERR_CUDA;
   while (a.cols < static_cast<uint32_t>(a.batch)) a.cols *= 2;
   const int64_t batches = (tokens + a.batch - 1) / a.batch;
-  if (batches > 65535) return PQ_ERR_LIMIT;
   CUtensorMap mw = {}, mx = {};
   if ((rc = make_tmap_2d(&mw, w_f16, static_cast<uint64_t>(heads) * N, K, kOut, kPanelK, 2, 128)) != PQ_OK) return rc;
   if ((rc = make_tmap_heads(&mx, x_f16, tokens, heads, K, x_stride, x_head_stride, a.batch)) != PQ_OK) return rc;
@@ -163,7 +162,7 @@ int pq_head_linear(const void* x_f16, int64_t x_stride, int64_t x_head_stride, c
   constexpr int kMostSmem = kMostPanels * (kOut + 64) * 128 + 1024;   // K = 512 with 64 tokens; 256 with 128 is less
   if ((rc = set_dynamic_smem_once(once, head_linear_kernel, kMostSmem)) != PQ_OK) return rc;
   const size_t smem = static_cast<size_t>(a.panels) * (kOut + a.batch) * 128 + 1024;
-  return launch_dependent(head_linear_kernel, dim3(static_cast<unsigned>(N / kOut), heads, static_cast<unsigned>(batches)), dim3(kThreads), smem,
+  return launch_dependent(head_linear_kernel, dim3(static_cast<unsigned>(batches), heads, static_cast<unsigned>(N / kOut)), dim3(kThreads), smem,
                           static_cast<cudaStream_t>(stream), mw, mx, a);
 }
 

@@ -77,3 +77,14 @@ def test_weights_may_be_written_by_the_launch_right_before(T, heads, K, N, captu
         torch.cuda.synchronize()
         run()
     assert all(torch.equal(y, good[i % 3]) for i, y in enumerate(out)) and pq.pq_device_status() == 0
+
+
+def test_more_tokens_than_a_grids_outer_dimensions_hold():
+    """65536 batches of 128 tokens and a ragged one, of one head."""
+    T, w = 65536 * 128 + 77, _operands(1, 1, 64, 128)[1]
+    gen = torch.Generator(DEV).manual_seed(3)
+    x = torch.empty((T, 1, 64), dtype=torch.float16, device=DEV).normal_(generator=gen)
+    y = pq.pq_head_linear(x, w)
+    assert pq.pq_device_status() == 0
+    for t0 in range(0, T, 1 << 20):
+        _check(y[t0: t0 + (1 << 20)], x[t0: t0 + (1 << 20)], w)
