@@ -530,7 +530,8 @@ int pq_expanded_attention(const void* q_f16, int64_t q_stride, int32_t heads, co
   int rc = check_arch();
   if (rc != PQ_OK) return rc;
   cudaStream_t st = static_cast<cudaStream_t>(stream);
-  if (keys == 0) {   // nothing is seen, and a tensor map needs a row: one of the queries', masked
+  const bool none = keys == 0;
+  if (none) {   // nothing is seen, and a tensor map needs a row: one of the queries', masked
     kv_f16 = k_rope_f16 = q_f16;
     keys = 1;
   }
@@ -563,7 +564,6 @@ int pq_expanded_attention(const void* q_f16, int64_t q_stride, int32_t heads, co
   if (regs * kThreads < kSoft * kSoftRegs + (kThreads - kSoft) * kRestRegs) return PQ_ERR_CUDA;
   CUtensorMap mq = {}, mkv = {}, mr = {};
   if ((rc = make_tmap_heads(&mq, q_f16, tokens, heads, kQuery, q_stride, kQuery, kTile)) != PQ_OK) return rc;
-  const bool none = kv_f16 == q_f16;
   if ((rc = make_tmap_heads(&mkv, kv_f16, keys, none ? 1 : heads, none ? kQuery : kNope + kValue, kv_stride, kNope + kValue, kKeys)) != PQ_OK) return rc;
   if ((rc = make_tmap_heads(&mr, k_rope_f16, keys, 1, PQ_LATENT_ROPE, k_rope_stride, PQ_LATENT_ROPE, kKeys)) != PQ_OK) return rc;
   if ((rc = launch_dependent(expanded_kernel, dim3(sms), dim3(kThreads), kSmem, st, mq, mkv, mr, a)) != PQ_OK || !a.shares) return rc;

@@ -59,3 +59,17 @@ def test_a_slice_of_a_wider_allocation_holds_the_formula():
     _shifted(call, 8)
     y, bound = ref.latent_attention(d, 0.04)
     assert (np.abs(call().cpu().numpy().astype(np.float64) - y) <= bound).all() and pq.pq_device_status() == 0
+
+
+@pytest.mark.parametrize("kind", ["whole", "parts"])
+def test_operands_that_begin_at_one_address(kind):
+    """Queries, keys and values as columns of one matrix, from its first one on."""
+    heads, new, _ = EXPANDED[kind]
+    d = ref.expanded_inputs(heads, new, new, seed=5)
+    d["q"] = d["kv"][:, : heads * 192].copy()
+    apart = Expanded(d, 192 ** -0.5)
+    want = apart().clone()
+    together = Expanded(d, 192 ** -0.5)
+    together.q = together.kv.flatten(1)[:, : heads * 192].unflatten(1, (heads, 192))
+    assert together.q.data_ptr() == together.kv.data_ptr()
+    assert torch.equal(together(), want) and pq.pq_device_status() == 0
