@@ -565,7 +565,7 @@ PQ_API int pq_latent_read(const pq_latent_cache* cache, const int64_t* slots, in
  *   x: head h of row t is K values at x + t * x_stride + h * x_head_stride;  w: dense [heads, N, K];
  *   y: N values at y + t * y_stride + h * y_head_stride
  *   K a multiple of 64 up to 512, N a multiple of 128 up to 1024, 1 <= heads <= 1024; strides as for pq_rotate, with K and
- *   N for the widths; y may not overlap x.  Unlike packed weights, w may be written by the operation right before the call.
+ *   N for the widths, and those of x below 2^38; y may not overlap x.  Unlike packed weights, w may be written by the operation right before the call.
  */
 PQ_API int pq_head_linear(const void* x_f16, int64_t x_stride, int64_t x_head_stride, const void* w_f16, int32_t heads, int64_t N,
                           int64_t K, int64_t tokens, void* y_f16, int64_t y_stride, int64_t y_head_stride, void* stream);
@@ -580,7 +580,7 @@ PQ_API int pq_head_linear(const void* x_f16, int64_t x_stride, int64_t x_head_st
  *   q: FP16 [tokens, heads, latent + PQ_LATENT_ROPE] dense;  out: FP16 [tokens, heads, latent] dense.  Rows outside every
  *     request are left as they are.  1 <= heads <= 1024, tokens * heads < 2^31; scale finite.
  *   block_table i32 [requests, width], q_start i32 [requests + 1], kv_len i32 [requests]: as for pq_paged_attention;
- *     width * page <= 2^30 (else PQ_ERR_LIMIT)
+ *     width * page <= 2^30 and requests <= PQ_MAX_REQUESTS (else PQ_ERR_LIMIT)
  *   workspace: as for pq_gemm_w8a8; partial results of tokens that are split over several SMs, joined in a fixed order.
  *     The schedule is made on the GPU from the lengths.  Without a workspace, or with less than
  *     pq_latent_workspace_bytes, the tokens of a request are not split.
@@ -602,11 +602,12 @@ PQ_API size_t pq_latent_workspace_bytes(int32_t sms);
  *   q: FP16, row t at q + t * q_stride, heads * (128 + PQ_LATENT_ROPE) values (the rotary part last, turned)
  *   kv: FP16, row j at kv + j * kv_stride, heads * (128 + 128) values: a head's key, then its value
  *   k_rope: FP16, row j at k_rope + j * k_rope_stride, PQ_LATENT_ROPE values;  keys: rows of kv and k_rope
- *   strides multiples of 8 and >= the row; 16-byte aligned
+ *   strides multiples of 8, >= the row and below 2^38; 16-byte aligned;  requests <= PQ_MAX_REQUESTS (else PQ_ERR_LIMIT)
  *   q_start, kv_start i32 [requests + 1] within tokens and keys;  max_q: a bound of the rows of any request (a request
  *     with more leaves outputs unspecified)
  *   workspace: as for pq_latent_attention
- *   out: FP16 [tokens, heads, 128] dense.  Rows outside every request are left as they are.  1 <= heads <= 1024.
+ *   out: FP16 [tokens, heads, 128] dense.  Rows outside every request are left as they are.  1 <= heads <= 1024,
+ *     tokens * heads < 2^31; scale finite.
  */
 PQ_API int pq_expanded_attention(const void* q_f16, int64_t q_stride, int32_t heads, const void* kv_f16, int64_t kv_stride,
                                  const void* k_rope_f16, int64_t k_rope_stride, int64_t keys, const int32_t* q_start,
@@ -622,7 +623,8 @@ PQ_API int pq_device_status(int* host_status);
 
 /*
  * The poll bound of the waits inside the kernels launched from now on (process-wide; 0 restores
- * the default of 2^24 polls, about a second).  For tests of the give-up path: with PQ_WAIT_NONE no
+ * the default of 2^24 polls, some 25 seconds: a poll of a barrier that nothing arrives on lasts 1.5
+ * us, and a wait may have to outlast the kernel before in the stream).  For tests of the give-up path: with PQ_WAIT_NONE no
  * wait polls at all, so every role of a kernel gives up at its first wait although nothing is
  * wrong; with a bound of a few polls some wait runs out somewhere in the middle.  Either way the
  * kernel reports PQ_ERR_TIMEOUT through the status word and returns with unspecified outputs.

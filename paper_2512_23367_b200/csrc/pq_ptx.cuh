@@ -9,7 +9,9 @@
 namespace pq {
 
 // Default upper bound on polls of one mbarrier wait.  Legitimate waits in these kernels last
-// microseconds; the bound only turns a protocol bug into an error code instead of a hang.  The
+// microseconds, or as long as the kernel before still runs; the bound only turns a protocol bug into an
+// error code instead of a hang.  A poll that finds nothing suspends its thread for 1.48 us (2900 cycles,
+// by one warp or twelve on every SM), so that the bound is some 25 seconds.  The
 // bound in force travels to the kernels as an argument (pq_set_wait_limit), so that a test can
 // make a wait run out without anything being broken.
 constexpr uint32_t kWaitPollLimit = 1u << 24;
