@@ -98,7 +98,7 @@ struct Part {
 //     while the results of the last one go out.
 //   - keys and values are rows of one linear's output, read through one tensor map with heads as its second dimension.
 // A step of 256 x 80 takes 2150 to 2200 cycles, and a unit's begin and end 7000: the next queries' way in, and the sums' way out, which
-// the next unit's first S overlaps.  A prompt of 4096 of 32 heads: 156 us at 1.6 GHz, where the tensor cores at
+// the next unit's first S overlaps.  A prompt of 4096 of 32 heads: 158 us alone, 175 to 180 in a row under the power cap, where the tensor cores at
 // cuBLAS's rate take 106; chunks of up to 700 tokens of 16 heads over up to 5000: 98 and 9 for joining the parts, where 53.
 __global__ void __launch_bounds__(kThreads, 1)
 expanded_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUtensorMap map_kv, const __grid_constant__ CUtensorMap map_rope,

@@ -32,8 +32,8 @@ struct HeadArgs {
 // land; before it the weights are only brought into L2, which is right whoever writes them.  (The three launches of a decode step of
 // 32 tokens and 128 heads over 1000 cached ones, weights in no cache: 43.8 us; 45.0 without bringing them into L2; 42.3 with the weights
 // requested before the wait, which takes another operation between their writing and the call.)
-// 128 heads of 128 x 512 and 64 tokens 9.3 us by itself, 7.1 after another kernel, where
-// the bytes take 4.2; 32 heads of 512 x 128 and one token 4.9.  Results pass through shared memory to leave as whole rows of 256 bytes.
+// 128 heads of 128 x 512 and 64 tokens 11.7 us alone, 5.2 in a row with the weights in L2, where the bytes take 4.2; 32 heads of
+// 512 x 128 and one token 5.7 and 2.5.  Results pass through shared memory to leave as whole rows of 256 bytes.
 __global__ void __launch_bounds__(kThreads) head_linear_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constant__ CUtensorMap map_x,
                                                               const HeadArgs a) {
   extern __shared__ uint8_t smem_raw[];

@@ -145,10 +145,11 @@ constexpr uint32_t kBarRow = 1, kBarTile = 3, kBarRead = 4, kBarP = 5;
 // multiplied, only when the maximum has grown by more than 2^8.
 //
 // Bound by HBM up to 64 rows a request: 72 KB a step take an SM's share of the bandwidth 3150 cycles, and steps come every
-// 3300.  Two CTAs that share their tokens have 1580 cycles of bandwidth a step and take 2080: the tensor cores wait for S to be
-// read and for P.  (64 requests of 128 heads and 1000 to 8200 tokens: 117 us and 9 for joining the parts, where their bytes take 63;
-// 7 requests of up to four tokens of 32 heads and 4000 to 30000 tokens: 55 and 10, where 26; 1000 tokens of 16 heads: 13 and 5.)  A
-// unit's begin and end take about 9000 cycles: queries, the first tokens, 128 KB of partial sums at 30 bytes a cycle.  Taken back for being slower: queries in shared memory and two steps of tokens (236 us for the 131), two
+// 3300.  Two CTAs that share their tokens have 1580 cycles of bandwidth a step and take 2080 to 2300: the tensor cores wait for S to be
+// read and for P.  (64 requests of 128 heads and 1000 to 8200 tokens: 115 us and 10 for joining the parts, where their bytes take 63;
+// with latent 256 84 in all, where 35; 7 requests of up to four tokens of 32 heads and 4000 to 30000 tokens: 53 and 11, where 26; 1000 tokens
+// of 16 heads: 13 and 5.)  A unit's begin and end take about 9000 cycles: queries, the first tokens, 128 KB of partial sums at 30 bytes
+// a cycle.  Taken back for being slower: queries in shared memory and two steps of tokens (236 us for the 131 that it took then), two
 // CTAs as a cluster that exchange halves of S (5300 cycles a step), MMAs over a pair of CTAs (2340).
 template <int kLatent>
 __global__ void __launch_bounds__(kThreads, 1)
@@ -360,8 +361,9 @@ latent_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__
   } else if (warp == kAhead) {
     // -------------------------------------------------------------------- tokens into L2, kDistance steps ahead of their use,
     // where two CTAs share them.  There three steps of room are less than what memory's latency asks for at twice the rate
-    // (64 ragged requests: 131 us without, 127 with two steps ahead, 133 with six, whose lines come too early); one CTA by itself is bound by memory, and slower with (87 thousand cycles for
-    // 20 steps, 109 with).
+    // (64 ragged requests: 130 us without, 126 with one or two steps ahead, 130 with six, whose lines come too early; with latent 256
+    // 103 without, 88, 84 and 86; 32 requests of 4000 tokens 69, 66, 64 and 70).  One CTA by itself is bound by memory, and gains nothing
+    // (148 requests of 2000 tokens of 16 heads: 84.6 us without, 85.6 with).
     const char* data = static_cast<const char*>(a.c.data);
     constexpr int kLines = C::kPanels;   // of 128 bytes, per token
     const int tokens = kKeys / 2, first = static_cast<int>(blockIdx.x & 1) * tokens;

@@ -84,10 +84,12 @@ __device__ __forceinline__ uint4 pack8(const float* x) {
 // (token, pair) into shared memory, for all heads; in FP32, as the products are.  FP16 results are rounded once; an INT8 key is
 // quantized from its FP32 values, so that it is rounded once, too.
 //
-// HBM bound beyond a few hundred tokens, latency below: 8192 tokens of 40 heads of 128, half of each turned, 27 us (6.2 TB/s);
-// one token 3.4.  With an INT8 cache by instructions, 61 % of the issue slots: 8192 tokens, 32 and 8 heads, 39 us where the bytes take
-// 28 (48 with one item per thread).  Five blocks an SM, 48 registers, of which the INT8 kernels
-// spill a few: with four and 64 registers the same calls took 2 to 3 us more, with six 4 to 9.
+// HBM bound beyond a few hundred tokens, latency below: 8192 tokens of 40 heads of 128, half of each turned, 27 us in a row (6.2 TB/s)
+// and 31 alone; one token 1.5 and 3.7.  8192 tokens of 32 query and 8 key/value heads into an FP16 cache 34 and 38.5, where the bytes take 31.
+// Into an INT8 cache 38.5 and 44 (44 and 49 with one item per thread), where they take 28: quantization makes it nearest to instructions,
+// 75 % of the issue slots, while memory is at 43 %; a warp that does not issue waits for its loads, for the block's cosines or for a fixed latency.
+// Five blocks an SM, 48 registers, of which the kernels with two items spill a few: with four and 64 registers the calls for 8192 tokens
+// took 2 to 4 us more, with six 1 to 8.
 template <Target kTarget, bool kHalf, int kItems>
 __global__ void __launch_bounds__(kThreads, 5) rotary_kernel(const TurnArgs a) {
   extern __shared__ float s_cos[];

@@ -148,7 +148,7 @@ struct ShareRoom {   // shared memory
 
 // By the whole block up to the sums over requests, then by one warp (all of them take turns issuing: 1000 to 2000 cycles more);
 // false: whole units by turns take no longer.  They are not cut, which costs about two units' begins and ends,
-// one for the other part and one for the joining (35 requests of two units each, of eight steps, on 74 pairs of CTAs: 33 us; 43 in shares).
+// one for the other part and one for the joining (35 requests of two units each, of eight steps, on 74 pairs of CTAs: 29 us; 39 in shares).
 template <int kThreads, Halves kHalves, class Args>
 __device__ __forceinline__ bool find_share(const Args& a, int worker, int workers, int least, ShareRoom<typename Args::Shape>& room) {
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
@@ -337,8 +337,8 @@ struct Walk : Unit<typename Args::Shape> {
 // x 4 sums, then [kRows] x (reference, sum of weights); part(i) is the i-th of `parts`, `first` the thread's first value, `to` where
 // its row has them (nullptr: there is no such row).  All of four parts is loaded at once: L2 latency bounds it.
 // kGroups > 1: so many threads of a block share a row's parts, in blocks of kGroups x kRows threads.  One request of 52000 tokens
-// in 148 parts: 49 us with one group, 36 with four; 64 requests in two or three parts each, where four times the blocks
-// come in waves: 141 and 155 (with shares of equal steps).
+// in 148 parts: 54 us with one group, 40 with four; 64 requests in two or three parts each, where four times the blocks
+// come in waves: 123 and 140.
 // many_parts: whether a unit may be in more than 16, from bounds of the units and of the steps of one.
 inline bool many_parts(int64_t units, int workers, int64_t steps, int least) {
   return units * 16 < workers && steps > 16 * least;
